@@ -174,6 +174,104 @@ astro_status_t astro_chunk_attn_bwd_dkv(const void* q, const void* k_chunk, cons
                                         int n_q, int n_kc, float scale, void* dk_chunk, void* dv_chunk,
                                         void* stream);
 
+/* Continue a cache as another one: empties `dst` and copies frames of `src` into it, as if they had been appended to it
+ * in the order of `frames` (its first S_dst frames become the sink).  frames: HOST array of n_frames logical frame
+ * indices of src (0 = oldest: sink frames, then the window oldest to newest; repeats allowed); null with
+ * n_frames = -1 takes every held frame.  So the call copies, forks (one shared prefix, cache_batch 1, into one cache per
+ * candidate), reorders and compacts.
+ * parents: device int32 [dst cache_batch], the sample of src that each sample of dst continues; null: sample b
+ * continues sample b, or sample 0 of a one-sample src.  A parent outside src leaves zeros in the copied frames.
+ * dst's frames_seen becomes src's.  ASTRO_ERR_SHAPE: other heads, head_dim or tokens_per_frame; parents null and
+ * cache batches that are neither equal nor 1; a frame index that src does not hold; storage of dst that overlaps src's.
+ * ASTRO_ERR_CAPACITY: more frames than dst holds.  Calls on dst and src obey the rules of calls that change a cache
+ * (dst) and of calls that take it as const (src). */
+astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* src, const int32_t* parents,
+                                  const int* frames, int n_frames, void* stream);
+
+/* ---- rotary positions -------------------------------------------------------------------------------------------
+ * The attention calls take Q and K with their positions already in them; this is the operator that puts them there.
+ * A token has `axes` integer coordinates (1 for plain sequences; 3 for frame, row and column of a latent video).  The
+ * first rot_dim elements of a head form rot_dim/2 pairs, dealt to the axes in order (axis_pairs[0] pairs turn with
+ * coordinate 0, and so on); pair i of an axis with n pairs turns by f_i = base^(-i/n) radians per position.
+ * Contexts longer than the trained one, for the axes in the bit mask scaled_axes:
+ *   NONE    f_i
+ *   LINEAR  f_i / factor
+ *   BASE    base replaced by base * factor^(n/(n-1)): the fastest pair is left alone, the slowest divided by factor
+ *   RAMP    with r = original_length f_i / 2 pi turns over the trained length and g = (r - ramp_low) /
+ *           (ramp_high - ramp_low) clamped to [0, 1]:  f_i (g + (1 - g) / factor)
+ * magnitude multiplies cosines and sines; 0 means 1, or 0.1 ln(factor) + 1 for RAMP. */
+typedef struct astro_rope astro_rope_t; /* opaque, host side, owns no device memory */
+enum { ASTRO_ROPE_INTERLEAVED = 0, ASTRO_ROPE_HALVES = 1 };       /* pairs (2p, 2p+1) or (p, p + rot_dim/2) */
+enum { ASTRO_ROPE_SCALE_NONE = 0, ASTRO_ROPE_SCALE_LINEAR = 1, ASTRO_ROPE_SCALE_BASE = 2, ASTRO_ROPE_SCALE_RAMP = 3 };
+enum { ASTRO_BF16 = 0, ASTRO_F16 = 1, ASTRO_F32 = 2 };
+typedef struct {
+  int head_dim;        /* multiple of 8, 8..256 */
+  int rot_dim;         /* even, 2..head_dim; the elements behind it are copied */
+  int layout;
+  int axes;            /* 1..4 */
+  int axis_pairs[4];   /* each >= 1, sum = rot_dim / 2 */
+  double base;         /* > 0 */
+  int scaling;
+  int scaled_axes;     /* bit a: axis a is scaled */
+  double factor;       /* >= 1 */
+  double original_length, ramp_low, ramp_high; /* RAMP only: > 0, ramp_low < ramp_high */
+  double magnitude;    /* >= 0 */
+} astro_rope_desc_t;
+typedef struct {
+  int64_t batch, token, head; /* strides in elements; the elements of a head are contiguous */
+} astro_strides_t;
+
+astro_status_t astro_rope_create(const astro_rope_desc_t* desc, astro_rope_t** out);
+astro_status_t astro_rope_destroy(astro_rope_t* rope);
+/* Inspection aid: radians per position of every pair (HOST, rot_dim/2 values) and the factor on cosines and sines. */
+astro_status_t astro_rope_frequencies(const astro_rope_t* rope, double* frequencies, double* magnitude);
+/* Rotates q [batch, n_tokens, heads_q, head_dim] and, unless null, k [batch, n_tokens, heads_k, head_dim] into q_out and
+ * k_out.  inverse = 1 applies the transpose (rotates back, with the same magnitude): the gradient of the inputs from the
+ * gradient of the outputs.  dtype: type of all four tensors; fp32 arithmetic, one rounding.
+ * positions: device int32 [positions_batch, n_tokens, axes], positions_batch = batch or 1 (the same for every
+ * sample); any int32 value, angles keep their accuracy to the far end of it.
+ * in_strides (of q and k alike) and out_strides (of q_out and k_out): null = contiguous.  Pointers and strides must be
+ * multiples of 16 bytes (ASTRO_ERR_ALIGN).  An input stride may be 0 (a broadcast input); outputs must not overlap
+ * themselves (ASTRO_ERR_SHAPE).  q_out = q (and k_out = k) rotates in place, with equal strides; otherwise outputs
+ * must not overlap inputs.  n_tokens = 0 is an empty call. */
+astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const void* q, const void* k,
+                                const int32_t* positions, int positions_batch, int batch, int n_tokens, int heads_q,
+                                int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
+                                const astro_strides_t* out_strides, void* stream);
+
+/* ---- attention over chosen key blocks ---------------------------------------------------------------------------
+ * The keys of a call are cut into blocks of block_tokens tokens (a multiple of 8, 8..128): every held cache frame, in
+ * logical order, into ceil(T / block_tokens) blocks, then the chunk's n_kc tokens into ceil(n_kc / block_tokens).
+ * The last block of a frame and of the chunk may be shorter.  Blocks are numbered in that order, from 0.
+ * ASTRO_QUERY_BLOCK neighbouring queries share one list of key blocks; a query block that is shorter (the last one,
+ * or a single query) has its list to itself. */
+#define ASTRO_QUERY_BLOCK 128
+/* Host only: number of cache blocks and of chunk blocks (HOST pointers, either may be null). */
+astro_status_t astro_block_count(const astro_kvcache_t* cache, int n_kc, int block_tokens, int* ctx_blocks,
+                                 int* chunk_blocks);
+
+/* Means of the keys of cache blocks: for the n_frames held frames from logical frame first_frame on,
+ * pooled[b, h, slot, i, :] = mean over the tokens of block i of the frame's keys, fp32 from fp64 sums.
+ * pooled: device fp32 [B_c, H, S+L, ceil(T / block_tokens), D], indexed by storage slot, so an evict or an append
+ * leaves the means of the other frames valid: a caller pools new frames once, when they are appended. */
+astro_status_t astro_block_pool(const astro_kvcache_t* cache, int first_frame, int n_frames, int block_tokens,
+                                float* pooled, void* stream);
+
+/* Chooses key blocks: score(i, j) = (mean of the queries of query block i) . (mean of the keys of block j), means in
+ * fp32, products and sums in fp64.  blocks: device int32 [batch, H, ceil(n_q / ASTRO_QUERY_BLOCK), n_select] receives
+ * the n_select blocks of the highest scores in ascending order, with -1 behind them if there are fewer blocks.  Equal
+ * scores go to the lower block; NaN ranks below every number.  keep: blocks that come before every other one
+ * whatever their score (the lower ones first), ASTRO_KEEP_SINK those of the sink frames, ASTRO_KEEP_CHUNK the chunk's.
+ * pooled: the means of every held frame (may be null if the cache is null or empty); k_chunk null when n_kc = 0.
+ * workspace: device scratch, 16-byte aligned, at least astro_block_select_workspace_bytes().
+ * ASTRO_ERR_SHAPE as for the attention calls, and for more than ASTRO_SELECT_MAX_BLOCKS blocks. */
+#define ASTRO_SELECT_MAX_BLOCKS 24576
+enum { ASTRO_KEEP_SINK = 1, ASTRO_KEEP_CHUNK = 2 };
+size_t astro_block_select_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens);
+astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* pooled, const void* q, const void* k_chunk,
+                                  int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens, int n_select,
+                                  int keep, int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Eq. 1, Eq. 2 and the selective KL term of Sec. 3.4 (Algorithm 2, "Policy loss on window"), fused with
  * the gradient for the current policy, over the velocity tensors of the active window:
  *   v+ = (1-beta) v_old + beta v_theta;  v- = (1+beta) v_old - beta v_theta;

@@ -21,7 +21,9 @@ EXPORTED = ("astro_kvcache_key_segments", "astro_selftest_wait_timeout", "astro_
             "astro_chunk_attn_fwd", "astro_chunk_attn_bwd_workspace_bytes", "astro_chunk_attn_bwd",
             "astro_chunk_attn_bwd_delta", "astro_chunk_attn_bwd_dq", "astro_chunk_attn_bwd_dkv",
             "astro_chunk_attn_bwd_static", "astro_debug_forward_mode", "astro_debug_pair_flag",
-            "astro_last_device_status", "astro_status_string")
+            "astro_last_device_status", "astro_status_string", "astro_kvcache_fork", "astro_rope_create",
+            "astro_rope_destroy", "astro_rope_frequencies", "astro_rope_apply", "astro_block_count", "astro_block_pool",
+            "astro_block_select_workspace_bytes", "astro_block_select")
 
 
 class AstroError(RuntimeError):
@@ -39,6 +41,17 @@ class KVCacheDesc(C.Structure):
 class KVCacheState(C.Structure):
     _fields_ = [("sink_held", C.c_int), ("window_head", C.c_int), ("window_held", C.c_int),
                 ("frames_seen", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int), ("rot_dim", C.c_int), ("layout", C.c_int), ("axes", C.c_int),
+                ("axis_pairs", C.c_int * 4), ("base", C.c_double), ("scaling", C.c_int), ("scaled_axes", C.c_int),
+                ("factor", C.c_double), ("original_length", C.c_double), ("ramp_low", C.c_double),
+                ("ramp_high", C.c_double), ("magnitude", C.c_double)]
+
+
+class Strides(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
 
 
 _lib = None
@@ -90,6 +103,25 @@ def lib():
     L.astro_chunk_attn_bwd_static.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, cf, vp, vp, vp, vp]
     L.astro_nft_loss.restype = ci
     L.astro_nft_loss.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, C.c_longlong, cf, vp, vp, vp, vp]
+    L.astro_kvcache_fork.restype = ci
+    L.astro_kvcache_fork.argtypes = [vp, vp, vp, C.POINTER(ci), ci, vp]
+    L.astro_rope_create.restype = ci
+    L.astro_rope_create.argtypes = [C.POINTER(RopeDesc), C.POINTER(vp)]
+    L.astro_rope_destroy.restype = ci
+    L.astro_rope_destroy.argtypes = [vp]
+    L.astro_rope_frequencies.restype = ci
+    L.astro_rope_frequencies.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    L.astro_rope_apply.restype = ci
+    L.astro_rope_apply.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, ci, ci, ci, C.POINTER(Strides), vp, vp,
+                                   C.POINTER(Strides), vp]
+    L.astro_block_count.restype = ci
+    L.astro_block_count.argtypes = [vp, ci, ci, C.POINTER(ci), C.POINTER(ci)]
+    L.astro_block_pool.restype = ci
+    L.astro_block_pool.argtypes = [vp, ci, ci, ci, vp, vp]
+    L.astro_block_select_workspace_bytes.restype = sz
+    L.astro_block_select_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
+    L.astro_block_select.restype = ci
+    L.astro_block_select.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, vp, vp, sz, vp]
     L.astro_debug_forward_mode.restype = ci
     L.astro_debug_forward_mode.argtypes = [ci]
     L.astro_debug_pair_flag.restype = ci
@@ -127,6 +159,44 @@ def _contiguous(*tensors):
     for t in tensors:
         if t is not None and not t.is_contiguous():
             raise ValueError("tensor arguments must be contiguous")
+
+
+def _typed(kind, *tensors):
+    """Index and statistics tensors are read as the type their name says."""
+    import torch
+    for t in tensors:
+        if t is not None and t.dtype != getattr(torch, kind):
+            raise ValueError("expected a %s tensor, got %s" % (kind, t.dtype))
+
+
+def _here(stream, *tensors):
+    """Kernels run on the current device (or the given stream's, which must be the same one): a tensor that lives
+    elsewhere, on the host included, is refused before its address reaches one."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    if stream is not None and stream.device.index != dev:
+        raise ValueError("the stream belongs to another device than the current one")
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError("tensor on %s, the current device is %s" % (t.device, dev))
+
+
+def _chunk_shape(q, *chunk):
+    """n_kc of the chunk tensors, which must fit q [B, n_q, H, D]."""
+    n_kc = 0
+    for t in chunk:
+        if t is not None:
+            if t.dim() != 4 or (t.shape[0], t.shape[2], t.shape[3]) != (q.shape[0], q.shape[2], q.shape[3]) or (n_kc and t.shape[1] != n_kc):
+                raise ValueError("chunk tensors must be [B, n_kc, H, D] like q")
+            n_kc = t.shape[1]
+    return n_kc
+
+
+def _numel(shape):
+    n = 1
+    for s in shape:
+        n *= s
+    return n
 
 
 def _used_on(stream, *tensors):
@@ -336,6 +406,187 @@ def astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, scale: float,
                                         D, n_q, n_kc, float(scale), _ptr(dk_chunk), _ptr(dv_chunk), _stream(stream))
     _check(st, "astro_chunk_attn_bwd_dkv")
     return dk_chunk, dv_chunk
+
+
+def astro_kvcache_fork(dst: KVCache, src: KVCache, parents=None, frames=None, stream=None) -> None:
+    """Empty `dst` and copy the listed held frames of `src` (logical indices, None = all) into it; parents: int32 [dst
+    cache_batch] on the device, the sample of src that each sample of dst continues."""
+    _typed("int32", parents)
+    _contiguous(parents)
+    _here(stream, parents, dst.k_storage, dst.v_storage, src.k_storage, src.v_storage)
+    if parents is not None and parents.numel() != dst.desc.cache_batch:
+        raise ValueError("parents must hold one entry per sample of the destination")
+    if frames is None:
+        arr, n = None, -1
+    else:
+        arr, n = (C.c_int * max(1, len(frames)))(*[int(f) for f in frames]), len(frames)
+    _check(lib().astro_kvcache_fork(dst.handle, src.handle, _ptr(parents), arr, n, _stream(stream)), "astro_kvcache_fork")
+
+
+ROPE_LAYOUTS = {"interleaved": 0, "halves": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+class Rope:
+    """Handle of one table of rotary frequencies (host memory only)."""
+
+    def __init__(self, handle, desc):
+        self.handle = handle
+        self.desc = desc
+
+    def __del__(self):
+        try:
+            astro_rope_destroy(self)
+        except Exception:
+            pass
+
+
+def astro_rope_create(head_dim, rot_dim, layout, axis_pairs, base=10000.0, scaling="none", factor=1.0, scaled_axes=None,
+                      original_length=4096.0, ramp_low=1.0, ramp_high=32.0, magnitude=0.0) -> Rope:
+    """axis_pairs: pairs of each position axis, e.g. (64,) or (22, 21, 21); scaled_axes: axes that `scaling` applies to
+    (None = all); magnitude 0 = the scaling's own."""
+    if len(axis_pairs) > 4:
+        raise AstroError(2, "astro_rope_create")
+    axes = range(len(axis_pairs)) if scaled_axes is None else scaled_axes
+    d = RopeDesc(int(head_dim), int(rot_dim), ROPE_LAYOUTS[layout], len(axis_pairs), (C.c_int * 4)(*[int(p) for p in axis_pairs]),
+                 float(base), ROPE_SCALINGS[scaling], sum(1 << int(a) for a in axes), float(factor), float(original_length),
+                 float(ramp_low), float(ramp_high), float(magnitude))
+    out = C.c_void_p()
+    _check(lib().astro_rope_create(C.byref(d), C.byref(out)), "astro_rope_create")
+    return Rope(out, d)
+
+
+def astro_rope_destroy(rope: Rope) -> None:
+    if rope.handle is not None and _lib is not None:
+        h, rope.handle = rope.handle, None
+        _check(_lib.astro_rope_destroy(h), "astro_rope_destroy")
+
+
+def astro_rope_frequencies(rope: Rope):
+    """(radians per position of every pair, factor on cosines and sines)."""
+    f, m = (C.c_double * (rope.desc.rot_dim // 2))(), C.c_double()
+    _check(lib().astro_rope_frequencies(rope.handle, f, C.byref(m)), "astro_rope_frequencies")
+    return list(f), m.value
+
+
+def _rope_strides(t):
+    """(batch, token, head) strides, those of axes of size 1 as in a contiguous tensor (torch leaves them open)."""
+    B, n, H, D = t.shape
+    dense = (n * H * D, H * D, D)
+    return tuple(s if size > 1 else d for s, size, d in zip(t.stride(), (B, n, H), dense))
+
+
+def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotate q [B, n, H, D] and k (same type; other head count allowed; None: q alone) by their tokens' positions, int32
+    [B or 1, n, axes] on the device.  Inputs and outputs may be strided as long as a head's elements are contiguous;
+    q_out = q and k_out = k rotate in place.  inverse=True turns back: the gradient of q and k from that of the outputs."""
+    import torch
+    kinds = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    fresh = []
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device); fresh.append(q_out)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device); fresh.append(k_out)
+    pairs = [(x, y) for x, y in ((q, q_out), (k, k_out)) if x is not None]
+    B, n, _, D = q.shape
+    for x, y in pairs:
+        if x.dim() != 4 or x.shape != y.shape or x.dtype != y.dtype or x.dtype != q.dtype or x.shape[:2] != q.shape[:2] or \
+                x.shape[3] != rope.desc.head_dim:
+            raise ValueError("q, k and their outputs must be [B, n, heads, head_dim] of one type")
+        if n and (x.stride(3) != 1 or y.stride(3) != 1):
+            raise ValueError("the elements of a head must be contiguous")
+    if q.dtype not in kinds:
+        raise ValueError("q and k must be bf16, fp16 or fp32")
+    _typed("int32", positions)
+    _contiguous(positions)
+    _here(stream, q, k, q_out, k_out, positions)
+    if tuple(positions.shape) not in {(B, n, rope.desc.axes), (1, n, rope.desc.axes)}:
+        raise ValueError("positions must be [B or 1, n, axes]")
+    _used_on(stream, *fresh)
+    layouts = [(_rope_strides(x), _rope_strides(y)) for x, y in pairs]
+    # one launch for q and k; two where their strides differ
+    together = len(pairs) == 2 and layouts[0] == layouts[1]
+    calls = [(q, k, q_out, k_out, layouts[0])] if together else [(x, None, y, None, l) for (x, y), l in zip(pairs, layouts)]
+    for x, x2, y, y2, (si, so) in calls:
+        st = lib().astro_rope_apply(rope.handle, int(bool(inverse)), _ptr(x), _ptr(x2), _ptr(positions), positions.shape[0], B, n,
+                                    x.shape[2], 0 if x2 is None else x2.shape[2], kinds[q.dtype], C.byref(Strides(*si)),
+                                    _ptr(y), _ptr(y2), C.byref(Strides(*so)), _stream(stream))
+        _check(st, "astro_rope_apply")
+    return q_out, k_out
+
+
+QUERY_BLOCK = 128
+KEEP_SINK, KEEP_CHUNK = 1, 2
+
+
+def astro_block_count(cache, n_kc: int, block_tokens: int):
+    """(cache blocks, chunk blocks) that a call numbers (host only)."""
+    a, b = C.c_int(), C.c_int()
+    _check(lib().astro_block_count(None if cache is None else cache.handle, int(n_kc), int(block_tokens), C.byref(a), C.byref(b)),
+           "astro_block_count")
+    return a.value, b.value
+
+
+def _pooled_shape(cache, block_tokens):
+    d = cache.desc
+    return (d.cache_batch, d.heads, d.sink_frames + d.window_frames, -(-d.tokens_per_frame // int(block_tokens)), d.head_dim)
+
+
+def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_frames=None, pooled=None, stream=None):
+    """Means of the keys of the blocks of `n_frames` held frames from `first_frame` on (None: all behind it), fp32 [B_c, H,
+    S+L, blocks per frame, D] by storage slot; `pooled` keeps the means of the other frames."""
+    import torch
+    if n_frames is None:
+        sink, win, _ = astro_kvcache_query(cache)
+        n_frames = sink + win - int(first_frame)
+    if pooled is None:
+        if int(block_tokens) < 1:
+            raise AstroError(2, "astro_block_pool")
+        pooled = torch.zeros(_pooled_shape(cache, block_tokens), dtype=torch.float32, device=cache.k_storage.device)
+        _used_on(stream, pooled)
+    _typed("float32", pooled)
+    _contiguous(pooled)
+    _here(stream, pooled, cache.k_storage)
+    if int(block_tokens) >= 1 and pooled.numel() != _numel(_pooled_shape(cache, block_tokens)):
+        raise ValueError("pooled must be [B_c, H, S+L, blocks per frame, D]")
+    _check(lib().astro_block_pool(cache.handle, int(first_frame), int(n_frames), int(block_tokens), _ptr(pooled), _stream(stream)),
+           "astro_block_pool")
+    return pooled
+
+
+def astro_block_select_workspace_bytes(batch, heads, head_dim, n_q, n_kc, block_tokens) -> int:
+    return int(lib().astro_block_select_workspace_bytes(int(batch), int(heads), int(head_dim), int(n_q), int(n_kc), int(block_tokens)))
+
+
+def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: int, keep: int = 0, blocks=None, workspace=None,
+                       stream=None):
+    """int32 [B, H, ceil(n_q / QUERY_BLOCK), n_select]: per query block the key blocks of the highest scores, ascending,
+    -1 behind them.  pooled: astro_block_pool's means of every held frame (None without a cache)."""
+    import torch
+    B, n_q, H, D = q.shape
+    n_kc = _chunk_shape(q, k_chunk)
+    shape = (B, H, -(-n_q // QUERY_BLOCK), max(1, int(n_select)))
+    fresh = []
+    if blocks is None:
+        blocks = torch.empty(shape, dtype=torch.int32, device=q.device); fresh.append(blocks)
+    if workspace is None:
+        need = astro_block_select_workspace_bytes(B, H, D, n_q, n_kc, block_tokens)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _typed("int32", blocks)
+    _typed("float32", pooled)
+    _typed("bfloat16", q, k_chunk)
+    _contiguous(q, k_chunk, blocks, pooled, workspace)
+    _here(stream, q, k_chunk, blocks, pooled, workspace, None if cache is None else cache.k_storage)
+    if blocks.numel() != _numel(shape):
+        raise ValueError("blocks must be [B, H, query blocks, n_select]")
+    if cache is not None and pooled is not None and int(block_tokens) >= 1 and pooled.numel() != _numel(_pooled_shape(cache, block_tokens)):
+        raise ValueError("pooled must be [B_c, H, S+L, blocks per frame, D]")
+    _used_on(stream, *fresh)
+    st = lib().astro_block_select(None if cache is None else cache.handle, _ptr(pooled), _ptr(q), _ptr(k_chunk), B, H, D, n_q,
+                                  n_kc, int(block_tokens), int(n_select), int(keep), _ptr(blocks), _ptr(workspace),
+                                  workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "astro_block_select")
+    return blocks
 
 
 def astro_nft_loss(v_theta, v_old, v_ref, v_target, r_tilde, beta: float, w_policy=None, w_kl=None, grad=True,

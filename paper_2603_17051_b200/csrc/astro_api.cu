@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 #include <new>
@@ -13,8 +14,10 @@
 #include "attn_bwd.cuh"
 #include "attn_fwd.cuh"
 #include "attn_fwd_pair.cuh"
+#include "block_select.cuh"
 #include "kv_ring.cuh"
 #include "nft_loss.cuh"
+#include "rope.cuh"
 
 using namespace astro;
 
@@ -31,6 +34,13 @@ struct astro_kvcache {
   mutable std::once_flag maps_once;
   mutable astro_status_t maps_status;
   mutable CUtensorMap tm_k, tm_v;
+};
+
+struct astro_rope {
+  astro_rope_desc_t d;
+  double frequency[kRopeMaxPairs];
+  double magnitude;
+  RopeTable table;
 };
 
 namespace astro {
@@ -350,6 +360,104 @@ astro_status_t launch_ring_copy(const astro_kvcache* c, void* k_user, void* v_us
   return launch_status();
 }
 
+// Whether a tensor of these sizes and strides (elements) with contiguous rows of `row` elements overlaps itself.
+bool overlaps_itself(const long long (&size)[3], const long long (&stride)[3], long long row) {
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (stride[order[j]] < stride[order[i]]) { const int x = order[i]; order[i] = order[j]; order[j] = x; }
+  long long span = row;
+  for (int i = 0; i < 3; ++i) {
+    if (size[order[i]] <= 1) continue;
+    if (stride[order[i]] < span) return true;
+    span += stride[order[i]] * (size[order[i]] - 1);
+  }
+  return false;
+}
+
+template <typename T, int MODE>
+astro_status_t launch_rope(const astro_rope* rope, const RopeTensors& x, const int* positions, int per_sample, int n_tokens,
+                           int total_tokens, float sign, cudaStream_t st) {
+  const int items = (x.heads_q + x.heads_k) * rope_items_per_row(MODE, rope->d.head_dim, rope->d.rot_dim, RopeVec<T>::kElems);
+  const int sms = sm_count();
+  if (sms <= 0) return ASTRO_ERR_CUDA;
+  // a token's items side by side in whole warps, several tokens side by side when a token has few
+  const int passes = (items + kRopeMaxThreads - 1) / kRopeMaxThreads;
+  const int width = ((items + passes - 1) / passes + 31) / 32 * 32;
+  const int lanes = kRopeMaxThreads / 2 / width > 1 ? kRopeMaxThreads / 2 / width : 1;
+  // tokens of a block: enough for kRopeUnroll loads in flight per thread, fewer while that leaves SMs without a block
+  int tokens = lanes * kRopeUnroll < kRopeMaxTokens ? lanes * kRopeUnroll : kRopeMaxTokens;
+  while (tokens > 1 && (total_tokens + tokens - 1) / tokens < 2 * sms) tokens /= 2;
+  const dim3 threads(width, lanes < tokens ? lanes : tokens);
+  const size_t smem = sizeof(float2) * tokens * rope->table.pairs;   // at most 32 KB
+  rope_kernel<T, MODE><<<(total_tokens + tokens - 1) / tokens, threads, smem, st>>>(
+      rope->table, x, positions, per_sample, n_tokens, total_tokens, rope->d.head_dim, rope->d.rot_dim, tokens, sign);
+  return launch_status();
+}
+
+template <typename T>
+astro_status_t launch_rope_typed(const astro_rope* rope, const RopeTensors& x, const int* positions, int per_sample,
+                                 int n_tokens, int total_tokens, float sign, cudaStream_t st) {
+  if (rope->d.layout == ASTRO_ROPE_INTERLEAVED)
+    return launch_rope<T, kRopeInterleaved>(rope, x, positions, per_sample, n_tokens, total_tokens, sign, st);
+  if (rope->d.rot_dim / 2 % RopeVec<T>::kElems == 0)
+    return launch_rope<T, kRopeHalves>(rope, x, positions, per_sample, n_tokens, total_tokens, sign, st);
+  return launch_rope<T, kRopeHalvesScalar>(rope, x, positions, per_sample, n_tokens, total_tokens, sign, st);
+}
+
+bool block_tokens_ok(int block) { return block >= 8 && block <= kTile && block % 8 == 0; }
+
+// The key blocks of a call (block size and counts already checked); false if their number does not fit an int.
+bool build_key_blocks(const astro_kvcache* c, int n_kc, int block, KeyBlocks* out) {
+  KeyBlocks kb;
+  std::memset(&kb, 0, sizeof(kb));
+  kb.block = block;
+  kb.n_kc = n_kc;
+  long long ctx = 0;
+  kb.per_frame = kb.tokens_per_frame = kb.win_slots = 1;
+  if (c) {
+    kb.tokens_per_frame = c->d.tokens_per_frame;
+    kb.per_frame = (kb.tokens_per_frame - 1) / block + 1;
+    kb.sink_held = c->sink_held;
+    kb.sink_slots = c->d.sink_frames;
+    kb.win_head = c->win_head;
+    kb.win_slots = c->d.window_frames;
+    ctx = static_cast<long long>(c->sink_held + c->win_held) * kb.per_frame;
+  }
+  const long long total = ctx + (static_cast<long long>(n_kc) + block - 1) / block;
+  if (total > 0x3fffffffLL) return false;
+  kb.ctx = static_cast<int>(ctx);
+  kb.total = static_cast<int>(total);
+  *out = kb;
+  return true;
+}
+
+template <int D, int R>
+astro_status_t launch_select(const SelectArgs& a, const KeyBlocks& kb, int batch, cudaStream_t st) {
+  static std::atomic<int> done[kMaxDevices];
+  astro_status_t s = set_smem_once(block_select_kernel<D, R>, ASTRO_SELECT_MAX_BLOCKS * 8, done);
+  if (s != ASTRO_OK) return s;
+  dim3 grid((a.q_blocks + R - 1) / R, a.heads, batch);
+  block_select_kernel<D, R><<<grid, kSelectThreads, static_cast<size_t>(R) * kb.total * 8, st>>>(a, kb);
+  return launch_status();
+}
+
+template <int D>
+astro_status_t launch_select_all(const PoolSource& q, const PoolSource& kc, SelectArgs a, const KeyBlocks& kb, int batch,
+                                 cudaStream_t st) {
+  dim3 grid(q.blocks + kc.blocks, a.heads, batch);
+  block_pool_kernel<D><<<grid, kPoolThreads, 0, st>>>(q, kc, q.blocks, kb, 0, 0);
+  astro_status_t s = launch_status();
+  if (s != ASTRO_OK) return s;
+  // four query blocks share a reading of the key means when there are enough of them to fill the GPU and their keys fit
+  // into shared memory
+  const int sms = sm_count();
+  if (sms <= 0) return ASTRO_ERR_CUDA;
+  const bool four = 4ll * kb.total <= ASTRO_SELECT_MAX_BLOCKS &&
+                    static_cast<long long>((a.q_blocks + 3) / 4) * a.heads * batch * 2 >= sms;
+  return four ? launch_select<D, 4>(a, kb, batch, st) : launch_select<D, 1>(a, kb, batch, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -641,6 +749,275 @@ astro_status_t astro_chunk_attn_bwd(const astro_kvcache_t* cache, const void* q,
   if (s != ASTRO_OK || n_kc == 0) return s;
   return astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, batch, heads, head_dim, n_q, n_kc, scale,
                                   dk_chunk, dv_chunk, stream);
+}
+
+astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* src, const int32_t* parents,
+                                  const int* frames, int n_frames, void* stream) {
+  if (!dst || !src || (!frames && n_frames >= 0)) return ASTRO_ERR_NULL;
+  const auto &a = src->d, &d = dst->d;
+  const int held = src->sink_held + src->win_held;
+  if (!frames) n_frames = held;
+  if (n_frames < 0 || dst == src || a.heads != d.heads || a.head_dim != d.head_dim ||
+      a.tokens_per_frame != d.tokens_per_frame)
+    return ASTRO_ERR_SHAPE;
+  if (!parents && a.cache_batch != 1 && a.cache_batch != d.cache_batch) return ASTRO_ERR_SHAPE;
+  if (reinterpret_cast<uintptr_t>(parents) & 3u) return ASTRO_ERR_ALIGN;
+  const size_t src_bytes = astro_kvcache_storage_bytes(&a), dst_bytes = astro_kvcache_storage_bytes(&d);
+  const uintptr_t from[2] = {reinterpret_cast<uintptr_t>(src->k), reinterpret_cast<uintptr_t>(src->v)};
+  const uintptr_t to[2] = {reinterpret_cast<uintptr_t>(dst->k), reinterpret_cast<uintptr_t>(dst->v)};
+  for (uintptr_t f : from)
+    for (uintptr_t t : to)
+      if (f < t + dst_bytes && t < f + src_bytes) return ASTRO_ERR_SHAPE;
+  if (n_frames > static_cast<long long>(d.sink_frames) + d.window_frames) return ASTRO_ERR_CAPACITY;
+  for (int j = 0; frames && j < n_frames; ++j)
+    if (frames[j] < 0 || frames[j] >= held) return ASTRO_ERR_SHAPE;
+  const long long frame_vecs = static_cast<long long>(d.tokens_per_frame) * d.head_dim / 8;
+  const long long pieces = (frame_vecs + kForkThreads * kForkVecsPerThread - 1) / (kForkThreads * kForkVecsPerThread);
+  const long long per_frame = 2ll * d.cache_batch * d.heads * pieces;
+  if (frame_vecs > 0x3fffffffLL || per_frame > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
+  if (n_frames > 0) {
+    astro_status_t s = check_arch();
+    if (s != ASTRO_OK) return s;
+    // as many frames per launch as the map and the grid take
+    const long long most = 0x7fffffffLL / per_frame;
+    const int step = most < kMaxFramesPerCopy ? static_cast<int>(most) : kMaxFramesPerCopy;
+    for (int f0 = 0; f0 < n_frames; f0 += step) {
+      ForkMap map;
+      map.n = n_frames - f0 < step ? n_frames - f0 : step;
+      for (int j = 0; j < map.n; ++j) {
+        const int f = frames ? frames[f0 + j] : f0 + j;
+        map.from[j] = f < src->sink_held ? f : a.sink_frames + (src->win_head + f - src->sink_held) % a.window_frames;
+        map.to[j] = f0 + j;   // an emptied cache fills its sink and then the window from ring index 0
+      }
+      cache_fork_kernel<<<static_cast<unsigned>(map.n * per_frame), kForkThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+          static_cast<const uint4*>(src->k), static_cast<const uint4*>(src->v), static_cast<uint4*>(dst->k),
+          static_cast<uint4*>(dst->v), parents, map, a.cache_batch, d.cache_batch, d.heads, static_cast<int>(frame_vecs),
+          static_cast<int>(pieces), a.sink_frames + a.window_frames, d.sink_frames + d.window_frames);
+    }
+    if ((s = launch_status()) != ASTRO_OK) return s;
+  }
+  dst->sink_held = n_frames < d.sink_frames ? n_frames : d.sink_frames;
+  dst->win_head = 0;
+  dst->win_held = n_frames - dst->sink_held;
+  dst->frames_seen = src->frames_seen > n_frames ? src->frames_seen : n_frames;
+  return ASTRO_OK;
+}
+
+// ---- rotary positions -------------------------------------------------------------------------------
+astro_status_t astro_rope_create(const astro_rope_desc_t* d, astro_rope_t** out) {
+  if (!d || !out) return ASTRO_ERR_NULL;
+  if (d->head_dim < 8 || d->head_dim > 2 * kRopeMaxPairs || d->head_dim % 8 || d->rot_dim < 2 || d->rot_dim % 2 ||
+      d->rot_dim > d->head_dim || d->axes < 1 || d->axes > 4)
+    return ASTRO_ERR_SHAPE;
+  if (d->layout != ASTRO_ROPE_INTERLEAVED && d->layout != ASTRO_ROPE_HALVES) return ASTRO_ERR_SHAPE;
+  if (d->scaling < ASTRO_ROPE_SCALE_NONE || d->scaling > ASTRO_ROPE_SCALE_RAMP) return ASTRO_ERR_SHAPE;
+  if (!(d->base > 0.0) || !std::isfinite(d->base) || !(d->magnitude >= 0.0) || !std::isfinite(d->magnitude))
+    return ASTRO_ERR_SHAPE;
+  if (d->scaling != ASTRO_ROPE_SCALE_NONE && (!(d->factor >= 1.0) || !std::isfinite(d->factor))) return ASTRO_ERR_SHAPE;
+  if (d->scaling == ASTRO_ROPE_SCALE_RAMP &&
+      (!(d->original_length > 0.0) || !std::isfinite(d->original_length) || !(d->ramp_low < d->ramp_high) ||
+       !std::isfinite(d->ramp_low) || !std::isfinite(d->ramp_high)))
+    return ASTRO_ERR_SHAPE;
+  long long sum = 0;
+  for (int a = 0; a < d->axes; ++a) {
+    if (d->axis_pairs[a] < 1) return ASTRO_ERR_SHAPE;
+    sum += d->axis_pairs[a];
+  }
+  if (sum != d->rot_dim / 2) return ASTRO_ERR_SHAPE;
+  astro_rope* r = new (std::nothrow) astro_rope();
+  if (!r) return ASTRO_ERR_CUDA;
+  r->d = *d;
+  const double two_pi = 6.283185307179586476925286766559;
+  int p = 0;
+  for (int a = 0; a < d->axes; ++a) {
+    const int n = d->axis_pairs[a];
+    const bool scaled = d->scaling != ASTRO_ROPE_SCALE_NONE && ((d->scaled_axes >> a) & 1);
+    double base = d->base;
+    if (scaled && d->scaling == ASTRO_ROPE_SCALE_BASE && n > 1) base *= std::pow(d->factor, static_cast<double>(n) / (n - 1));
+    for (int i = 0; i < n; ++i, ++p) {
+      double f = std::pow(base, -static_cast<double>(i) / n);
+      if (scaled && d->scaling == ASTRO_ROPE_SCALE_LINEAR) f /= d->factor;
+      if (scaled && d->scaling == ASTRO_ROPE_SCALE_RAMP) {
+        double g = (d->original_length * f / two_pi - d->ramp_low) / (d->ramp_high - d->ramp_low);
+        g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
+        f *= g + (1.0 - g) / d->factor;
+      }
+      r->frequency[p] = f;
+      r->table.turns[p] = f / two_pi;
+      r->table.axis[p] = static_cast<uint8_t>(a);
+    }
+  }
+  r->magnitude = d->magnitude > 0.0 ? d->magnitude
+                                    : d->scaling == ASTRO_ROPE_SCALE_RAMP ? 0.1 * std::log(d->factor) + 1.0 : 1.0;
+  r->table.size = static_cast<float>(r->magnitude);
+  r->table.pairs = p;
+  r->table.axes = d->axes;
+  *out = r;
+  return ASTRO_OK;
+}
+
+astro_status_t astro_rope_destroy(astro_rope_t* rope) {
+  if (!rope) return ASTRO_ERR_NULL;
+  delete rope;
+  return ASTRO_OK;
+}
+
+astro_status_t astro_rope_frequencies(const astro_rope_t* rope, double* frequencies, double* magnitude) {
+  if (!rope || !frequencies) return ASTRO_ERR_NULL;
+  std::memcpy(frequencies, rope->frequency, sizeof(double) * rope->table.pairs);
+  if (magnitude) *magnitude = rope->magnitude;
+  return ASTRO_OK;
+}
+
+astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const void* q, const void* k,
+                                const int32_t* positions, int positions_batch, int batch, int n_tokens, int heads_q,
+                                int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
+                                const astro_strides_t* out_strides, void* stream) {
+  if (!rope || (k != nullptr) != (k_out != nullptr)) return ASTRO_ERR_NULL;
+  if (batch < 1 || n_tokens < 0 || heads_q < 1 || (k && heads_k < 1) || (positions_batch != 1 && positions_batch != batch))
+    return ASTRO_ERR_SHAPE;
+  if (dtype != ASTRO_BF16 && dtype != ASTRO_F16 && dtype != ASTRO_F32) return ASTRO_ERR_SHAPE;
+  if (inverse != 0 && inverse != 1) return ASTRO_ERR_SHAPE;
+  if (static_cast<long long>(batch) * n_tokens > 0x7fffffffLL - kRopeMaxTokens || heads_q > 65535 || (k && heads_k > 65535))
+    return ASTRO_ERR_SHAPE;
+  if (n_tokens == 0) return ASTRO_OK;
+  if (!q || !q_out || !positions) return ASTRO_ERR_NULL;
+  const int size = dtype == ASTRO_F32 ? 4 : 2, per16 = 16 / size, D = rope->d.head_dim;
+  if (!aligned16(q) || !aligned16(q_out) || (k && (!aligned16(k) || !aligned16(k_out))) ||
+      (reinterpret_cast<uintptr_t>(positions) & 3u))
+    return ASTRO_ERR_ALIGN;
+  const int heads = k && heads_k > heads_q ? heads_k : heads_q;
+  RopeTensors x;
+  x.q = q; x.k = k; x.q_out = q_out; x.k_out = k_out;
+  x.heads_q = heads_q;
+  x.heads_k = k ? heads_k : 0;
+  // contiguous tensors of different head counts have different strides: those need two calls
+  if (k && heads_k != heads_q && (!in_strides || !out_strides)) return ASTRO_ERR_SHAPE;
+  const astro_strides_t dense = {static_cast<int64_t>(n_tokens) * heads_q * D, static_cast<int64_t>(heads_q) * D, D};
+  const astro_strides_t in = in_strides ? *in_strides : dense, to = out_strides ? *out_strides : dense;
+  const long long sizes[3] = {batch, n_tokens, heads}, is[3] = {in.batch, in.token, in.head}, os[3] = {to.batch, to.token, to.head};
+  const long long limit = 1ll << 40;   // elements: keeps every product of a stride and an index inside 64 bits
+  for (int i = 0; i < 3; ++i) {
+    if (sizes[i] <= 1) continue;
+    if (is[i] < 0 || os[i] < 0 || is[i] > limit || os[i] > limit) return ASTRO_ERR_SHAPE;
+    if (is[i] % per16 || os[i] % per16) return ASTRO_ERR_ALIGN;
+  }
+  if (overlaps_itself(sizes, os, D)) return ASTRO_ERR_SHAPE;
+  if (q_out == k_out || (k && (q_out == k || k_out == q))) return ASTRO_ERR_SHAPE;
+  if (q_out == q || (k && k_out == k))
+    for (int i = 0; i < 3; ++i)
+      if (sizes[i] > 1 && is[i] != os[i]) return ASTRO_ERR_SHAPE;
+  x.in_b = in.batch; x.in_t = in.token; x.in_h = in.head;
+  x.out_b = to.batch; x.out_t = to.token; x.out_h = to.head;
+  astro_status_t s = check_arch();
+  if (s != ASTRO_OK) return s;
+  const int total = batch * n_tokens, per_sample = positions_batch > 1 || batch == 1 ? 1 : 0;
+  const float sign = inverse ? -1.f : 1.f;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dtype == ASTRO_BF16) return launch_rope_typed<__nv_bfloat16>(rope, x, positions, per_sample, n_tokens, total, sign, st);
+  if (dtype == ASTRO_F16) return launch_rope_typed<__half>(rope, x, positions, per_sample, n_tokens, total, sign, st);
+  return launch_rope_typed<float>(rope, x, positions, per_sample, n_tokens, total, sign, st);
+}
+
+// ---- key blocks ---------------------------------------------------------------------------------------
+astro_status_t astro_block_count(const astro_kvcache_t* cache, int n_kc, int block_tokens, int* ctx_blocks,
+                                 int* chunk_blocks) {
+  KeyBlocks kb;
+  if (!block_tokens_ok(block_tokens) || n_kc < 0 || !build_key_blocks(cache, n_kc, block_tokens, &kb)) return ASTRO_ERR_SHAPE;
+  if (ctx_blocks) *ctx_blocks = kb.ctx;
+  if (chunk_blocks) *chunk_blocks = kb.total - kb.ctx;
+  return ASTRO_OK;
+}
+
+astro_status_t astro_block_pool(const astro_kvcache_t* c, int first_frame, int n_frames, int block_tokens, float* pooled,
+                                void* stream) {
+  if (!c || !pooled) return ASTRO_ERR_NULL;
+  KeyBlocks kb;
+  if (!block_tokens_ok(block_tokens) || !build_key_blocks(c, 0, block_tokens, &kb)) return ASTRO_ERR_SHAPE;
+  const int held = c->sink_held + c->win_held;
+  if (first_frame < 0 || n_frames < 0 || first_frame > held || n_frames > held - first_frame) return ASTRO_ERR_SHAPE;
+  if (!aligned16(pooled)) return ASTRO_ERR_ALIGN;
+  const auto& d = c->d;
+  if (d.heads > 65535 || d.cache_batch > 65535) return ASTRO_ERR_SHAPE;
+  if (n_frames == 0) return ASTRO_OK;
+  astro_status_t s = check_arch();
+  if (s != ASTRO_OK) return s;
+  const long long slots = d.sink_frames + d.window_frames;
+  PoolSource src;
+  src.base = static_cast<const __nv_bfloat16*>(c->k);
+  src.st = d.head_dim;
+  src.sh = slots * d.tokens_per_frame * d.head_dim;
+  src.sb = src.sh * d.heads;
+  src.out = pooled;
+  src.out_h = slots * kb.per_frame;
+  src.out_b = src.out_h * d.heads;
+  src.tokens = d.tokens_per_frame;
+  src.block = block_tokens;
+  src.blocks = n_frames * kb.per_frame;
+  dim3 grid(src.blocks, d.heads, d.cache_batch);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (d.head_dim == 128) block_pool_kernel<128><<<grid, kPoolThreads, 0, st>>>(src, src, src.blocks, kb, first_frame, 1);
+  else block_pool_kernel<64><<<grid, kPoolThreads, 0, st>>>(src, src, src.blocks, kb, first_frame, 1);
+  return launch_status();
+}
+
+size_t astro_block_select_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens) {
+  if (batch < 1 || heads < 1 || n_q < 1 || n_kc < 0 || (head_dim != 64 && head_dim != 128) || !block_tokens_ok(block_tokens))
+    return 0;
+  const size_t blocks = static_cast<size_t>((n_q - 1) / ASTRO_QUERY_BLOCK + 1) + (static_cast<size_t>(n_kc) + block_tokens - 1) / block_tokens;
+  return blocks * batch * heads * head_dim * sizeof(float);
+}
+
+astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* pooled, const void* q, const void* k_chunk,
+                                  int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens, int n_select,
+                                  int keep, int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !blocks || !workspace || (n_kc > 0 && !k_chunk)) return ASTRO_ERR_NULL;
+  const AttnArgs args{cache, batch, heads, head_dim, n_q, n_kc};
+  astro_status_t s = check_attn_args(args, 1.f);
+  if (s != ASTRO_OK) return s;
+  KeyBlocks kb;
+  if (!block_tokens_ok(block_tokens) || n_select < 1 || (keep & ~(ASTRO_KEEP_SINK | ASTRO_KEEP_CHUNK)) ||
+      !build_key_blocks(cache, n_kc, block_tokens, &kb) || kb.total > ASTRO_SELECT_MAX_BLOCKS)
+    return ASTRO_ERR_SHAPE;
+  if (kb.ctx > 0 && !pooled) return ASTRO_ERR_NULL;
+  if (!aligned16(q) || (n_kc > 0 && !aligned16(k_chunk)) || !aligned16(pooled) || !aligned16(workspace) ||
+      (reinterpret_cast<uintptr_t>(blocks) & 3u))
+    return ASTRO_ERR_ALIGN;
+  if (workspace_bytes < astro_block_select_workspace_bytes(batch, heads, head_dim, n_q, n_kc, block_tokens))
+    return ASTRO_ERR_CAPACITY;
+  if ((s = check_arch()) != ASTRO_OK) return s;
+  const long long row = static_cast<long long>(heads) * head_dim;
+  PoolSource qs, ks;
+  qs.base = static_cast<const __nv_bfloat16*>(q);
+  qs.st = row; qs.sh = head_dim; qs.sb = row * n_q;
+  qs.tokens = n_q;
+  qs.block = ASTRO_QUERY_BLOCK;
+  qs.blocks = (n_q - 1) / ASTRO_QUERY_BLOCK + 1;
+  qs.out = static_cast<float*>(workspace);
+  qs.out_h = qs.blocks;
+  qs.out_b = qs.out_h * heads;
+  ks = qs;
+  ks.base = static_cast<const __nv_bfloat16*>(k_chunk);
+  ks.sb = row * n_kc;
+  ks.tokens = n_kc;
+  ks.block = block_tokens;
+  ks.blocks = kb.total - kb.ctx;
+  ks.out = qs.out + qs.out_b * batch * head_dim;
+  ks.out_h = ks.blocks;
+  ks.out_b = ks.out_h * heads;
+  SelectArgs a;
+  a.pooled = pooled;
+  a.q_mean = qs.out;
+  a.kc_mean = ks.out;
+  a.blocks = blocks;
+  a.heads = heads;
+  a.q_blocks = qs.blocks;
+  a.n_select = n_select;
+  a.cache_shared = cache && cache->d.cache_batch == 1 && batch > 1;
+  a.keep_sink = keep & ASTRO_KEEP_SINK ? 1 : 0;
+  a.keep_chunk = keep & ASTRO_KEEP_CHUNK ? 1 : 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return head_dim == 128 ? launch_select_all<128>(qs, ks, a, kb, batch, st) : launch_select_all<64>(qs, ks, a, kb, batch, st);
 }
 
 astro_status_t astro_nft_loss(const void* v_theta, const void* v_old, const void* v_ref, const void* v_target,

@@ -53,4 +53,50 @@ ring_copy_kernel(uint4* __restrict__ k_user, uint4* __restrict__ v_user, uint4* 
     if (i < n) dst[static_cast<long long>(i) * dst_step] = val[i];
 }
 
+// Frames of one cache copied into another (fork): slot map.to[j] of sample b takes slot map.from[j] of sample
+// parents[b] (sample b, or sample 0 of a one-sample source, when parents is null).  The frame of one head is contiguous
+// on both sides, so the copy is plain 16-byte vectors.  The samples of a piece are neighbours in the grid: when several
+// continue one parent, its bytes come from HBM once and from L2 for the others.  A parent outside the source leaves
+// zeros, never an access out of range.
+constexpr int kForkThreads = 256;
+constexpr int kForkVecsPerThread = 8;
+
+struct ForkMap {
+  int n;
+  int from[kMaxFramesPerCopy], to[kMaxFramesPerCopy];
+};
+
+// grid.x = ((frame, head, piece) * 2 + (0: K, 1: V)) * batch + b
+__global__ void __launch_bounds__(kForkThreads)
+cache_fork_kernel(const uint4* __restrict__ k_src, const uint4* __restrict__ v_src, uint4* __restrict__ k_dst,
+                  uint4* __restrict__ v_dst, const int* __restrict__ parents, const ForkMap map, const int source_batch,
+                  const int batch, const int heads, const int frame_vecs, const int pieces, const int src_slots,
+                  const int dst_slots) {
+  unsigned i = blockIdx.x;
+  const int b = i % batch;
+  i /= batch;
+  const bool is_v = i & 1;
+  i >>= 1;
+  const int piece = i % pieces;
+  i /= pieces;
+  const int h = i % heads, j = i / heads;
+  const int parent = parents ? parents[b] : (source_batch == 1 ? 0 : b);
+  const bool there = parent >= 0 && parent < source_batch;
+  const uint4* src = (is_v ? v_src : k_src) +
+                     ((static_cast<long long>(there ? parent : 0) * heads + h) * src_slots + map.from[j]) * frame_vecs;
+  uint4* dst = (is_v ? v_dst : k_dst) + ((static_cast<long long>(b) * heads + h) * dst_slots + map.to[j]) * frame_vecs;
+  const int first = piece * (kForkThreads * kForkVecsPerThread) + threadIdx.x;
+  uint4 val[kForkVecsPerThread];
+#pragma unroll
+  for (int u = 0; u < kForkVecsPerThread; ++u) {
+    const int at = first + u * kForkThreads;
+    val[u] = there && at < frame_vecs ? src[at] : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int u = 0; u < kForkVecsPerThread; ++u) {
+    const int at = first + u * kForkThreads;
+    if (at < frame_vecs) dst[at] = val[u];
+  }
+}
+
 }  // namespace astro
