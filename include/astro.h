@@ -272,6 +272,18 @@ astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* poo
                                   int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens, int n_select,
                                   int keep, int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Forward of attention over chosen key blocks: astro_chunk_attn_fwd with the keys of query block i restricted to the
+ * blocks that its list names.  blocks: device int32 [batch, H, ceil(n_q / ASTRO_QUERY_BLOCK), n_select] in any order.  An
+ * entry outside [0, number of blocks) names none; a block named twice counts twice.  A query with no key (an empty list) gets
+ * O = 0 and LSE = -infinity.  The other arguments, layouts and errors are astro_chunk_attn_fwd's.
+ * workspace: device scratch, 16-byte aligned, at least astro_sparse_attn_fwd_workspace_bytes() (0 for all but a few
+ * queries: their lists are cut into ranges that run side by side; then it may be null). */
+size_t astro_sparse_attn_fwd_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_select, int block_tokens);
+astro_status_t astro_sparse_attn_fwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
+                                     const int32_t* blocks, int n_select, int block_tokens, int batch, int heads,
+                                     int head_dim, int n_q, int n_kc, float scale, void* o, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
 /* Eq. 1, Eq. 2 and the selective KL term of Sec. 3.4 (Algorithm 2, "Policy loss on window"), fused with
  * the gradient for the current policy, over the velocity tensors of the active window:
  *   v+ = (1-beta) v_old + beta v_theta;  v- = (1+beta) v_old - beta v_theta;

@@ -23,7 +23,8 @@ EXPORTED = ("astro_kvcache_key_segments", "astro_selftest_wait_timeout", "astro_
             "astro_chunk_attn_bwd_static", "astro_debug_forward_mode", "astro_debug_pair_flag",
             "astro_last_device_status", "astro_status_string", "astro_kvcache_fork", "astro_rope_create",
             "astro_rope_destroy", "astro_rope_frequencies", "astro_rope_apply", "astro_block_count", "astro_block_pool",
-            "astro_block_select_workspace_bytes", "astro_block_select")
+            "astro_block_select_workspace_bytes", "astro_block_select", "astro_sparse_attn_fwd_workspace_bytes",
+            "astro_sparse_attn_fwd")
 
 
 class AstroError(RuntimeError):
@@ -122,6 +123,10 @@ def lib():
     L.astro_block_select_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
     L.astro_block_select.restype = ci
     L.astro_block_select.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, vp, vp, sz, vp]
+    L.astro_sparse_attn_fwd_workspace_bytes.restype = sz
+    L.astro_sparse_attn_fwd_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
+    L.astro_sparse_attn_fwd.restype = ci
+    L.astro_sparse_attn_fwd.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp, vp, vp, sz, vp]
     L.astro_debug_forward_mode.restype = ci
     L.astro_debug_forward_mode.argtypes = [ci]
     L.astro_debug_pair_flag.restype = ci
@@ -190,6 +195,12 @@ def _chunk_shape(q, *chunk):
                 raise ValueError("chunk tensors must be [B, n_kc, H, D] like q")
             n_kc = t.shape[1]
     return n_kc
+
+
+def _sized(*pairs):
+    for t, n in pairs:
+        if t is not None and t.numel() != n:
+            raise ValueError("an output or saved tensor has %d elements, %d expected" % (t.numel(), n))
 
 
 def _numel(shape):
@@ -587,6 +598,50 @@ def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: i
                                   workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "astro_block_select")
     return blocks
+
+
+def astro_sparse_attn_fwd_workspace_bytes(batch, heads, head_dim, n_q, n_select, block_tokens) -> int:
+    return int(lib().astro_sparse_attn_fwd_workspace_bytes(int(batch), int(heads), int(head_dim), int(n_q), int(n_select),
+                                                           int(block_tokens)))
+
+
+def _lists_shape(q, blocks):
+    """n_select of blocks [B, H, query blocks, n_select], which must fit q."""
+    B, n_q, H, _ = q.shape
+    if blocks.dim() != 4 or tuple(blocks.shape[:3]) != (B, H, -(-n_q // QUERY_BLOCK)):
+        raise ValueError("blocks must be [B, H, query blocks, n_select]")
+    return blocks.shape[3]
+
+
+def astro_sparse_attn_fwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int, scale: float, o=None, lse=None, workspace=None,
+                          stream=None):
+    """Attention of every query block over the key blocks its list names (blocks: int32 [B, H, ceil(n_q / QUERY_BLOCK),
+    n_select] on the device, -1 for none); returns (O bf16, LSE fp32 [B, H, n_q]); a query without a key gets 0 and
+    -infinity."""
+    import torch
+    B, n_q, H, D = q.shape
+    n_kc, n_select = _chunk_shape(q, k_chunk, v_chunk), _lists_shape(q, blocks)
+    fresh = []
+    if o is None:
+        o = torch.empty_like(q); fresh.append(o)
+    if lse is None:
+        lse = torch.empty((B, H, n_q), dtype=torch.float32, device=q.device); fresh.append(lse)
+    need = astro_sparse_attn_fwd_workspace_bytes(B, H, D, n_q, n_select, block_tokens)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _typed("int32", blocks)
+    _typed("float32", lse)
+    _typed("bfloat16", q, k_chunk, v_chunk, o)
+    _contiguous(q, k_chunk, v_chunk, blocks, o, lse, workspace)
+    _here(stream, q, k_chunk, v_chunk, blocks, o, lse, workspace, None if cache is None else cache.k_storage)
+    _sized((o, q.numel()), (lse, B * H * n_q))
+    _used_on(stream, *fresh)
+    st = lib().astro_sparse_attn_fwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk), _ptr(blocks),
+                                     n_select, int(block_tokens), B, H, D, n_q, n_kc, float(scale), _ptr(o), _ptr(lse),
+                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                     _stream(stream))
+    _check(st, "astro_sparse_attn_fwd")
+    return o, lse
 
 
 def astro_nft_loss(v_theta, v_old, v_ref, v_target, r_tilde, beta: float, w_policy=None, w_kl=None, grad=True,

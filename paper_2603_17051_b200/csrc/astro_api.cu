@@ -18,6 +18,7 @@
 #include "kv_ring.cuh"
 #include "nft_loss.cuh"
 #include "rope.cuh"
+#include "sparse_fwd.cuh"
 
 using namespace astro;
 
@@ -456,6 +457,126 @@ astro_status_t launch_select_all(const PoolSource& q, const PoolSource& kc, Sele
   const bool four = 4ll * kb.total <= ASTRO_SELECT_MAX_BLOCKS &&
                     static_cast<long long>((a.q_blocks + 3) / 4) * a.heads * batch * 2 >= sms;
   return four ? launch_select<D, 4>(a, kb, batch, st) : launch_select<D, 1>(a, kb, batch, st);
+}
+
+// ---- attention over lists of key blocks ---------------------------------------------------------------------
+// bf16 tensor seen as {d, token, slot, head, batch}: rows from `tokens` on read as zeros in every slot.
+astro_status_t make_tmap5(CUtensorMap* out, const void* base, int head_dim, long long tokens, int slots, int heads, int batch,
+                          unsigned long long st_tok, unsigned long long st_slot, unsigned long long st_head,
+                          unsigned long long st_batch, int box_rows) {
+  encode_tiled_fn fn = get_encode_fn();
+  if (!fn) return ASTRO_ERR_CUDA;
+  cuuint64_t dims[5] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(tokens), static_cast<cuuint64_t>(slots),
+                        static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(batch)};
+  cuuint64_t strides[4] = {st_tok, st_slot, st_head, st_batch};
+  cuuint32_t box[5] = {64, static_cast<cuuint32_t>(box_rows), 1, 1, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? ASTRO_OK : ASTRO_ERR_CUDA;
+}
+
+struct SparseCall {
+  AttnArgs a;
+  const void *q, *k_chunk, *v_chunk;
+  const int32_t* blocks;
+  int n_select, block_tokens;
+};
+
+astro_status_t check_sparse(const SparseCall& c, float scale, SparseGeom* g) {
+  astro_status_t s = check_attn_args(c.a, scale);
+  if (s != ASTRO_OK) return s;
+  if (!block_tokens_ok(c.block_tokens) || c.n_select < 1 || c.n_select > (1 << 30) ||
+      !build_key_blocks(c.a.cache, c.a.n_kc, c.block_tokens, &g->kb))
+    return ASTRO_ERR_SHAPE;
+  g->pad = sparse_pad(c.block_tokens);
+  g->per_tile = kTile / g->pad;
+  g->chunk_fill = g->kb.ctx == 0 ? 1 : 0;
+  return ASTRO_OK;
+}
+
+astro_status_t sparse_maps(const SparseCall& c, const SparseGeom& g, SparseMaps* m) {
+  std::memset(m, 0, sizeof(*m));
+  astro_status_t s = ASTRO_OK;
+  const unsigned long long row = static_cast<unsigned long long>(c.a.head_dim) * 2;
+  if (c.a.n_kc > 0) {
+    const unsigned long long all = row * c.a.heads * c.a.n_kc;
+    for (int i = 0; i < 2 && s == ASTRO_OK; ++i)
+      s = make_tmap5(i ? &m->vc : &m->kc, i ? c.v_chunk : c.k_chunk, c.a.head_dim, c.a.n_kc, 1, c.a.heads, c.a.batch,
+                     row * c.a.heads, all, row, all, g.kb.block);
+  }
+  if (g.kb.ctx > 0 && s == ASTRO_OK) {
+    const auto& d = c.a.cache->d;
+    const int slots = d.sink_frames + d.window_frames;
+    const unsigned long long frame = row * d.tokens_per_frame;
+    for (int i = 0; i < 2 && s == ASTRO_OK; ++i)
+      s = make_tmap5(i ? &m->vx : &m->kx, i ? c.a.cache->v : c.a.cache->k, d.head_dim, d.tokens_per_frame, slots, d.heads,
+                     d.cache_batch, row, frame, frame * slots, frame * slots * d.heads, g.kb.block);
+  }
+  return s;
+}
+
+// Into how many ranges a unit's list is cut, and how many entries a range has.  With fewer units than half the SMs of a B200
+// (148) most of it would idle while a few CTAs walk over long lists; a range keeps at least two tiles.
+struct SparseSplit {
+  int splits, entries;
+};
+SparseSplit sparse_split(int batch, int heads, int n_q, int n_select, int block_tokens) {
+  constexpr int kSms = 148;
+  const long long units = static_cast<long long>((n_q - 1) / kTile + 1) * heads * batch;
+  const int per_tile = kTile / sparse_pad(block_tokens);
+  const int tiles = (n_select - 1) / per_tile + 1;
+  SparseSplit r{1, n_select};
+  if (units * 2 > kSms || tiles < 4) return r;
+  int want = static_cast<int>(kSms / units);
+  if (want > tiles / 2) want = tiles / 2;
+  const int each = (tiles - 1) / want + 1;   // tiles of a range
+  r.splits = (tiles - 1) / each + 1;
+  r.entries = each * per_tile;
+  return r;
+}
+
+template <int D>
+astro_status_t launch_sparse_fwd(const SparseCall& c, const SparseGeom& g, float scale, void* o, float* lse, void* workspace,
+                                 cudaStream_t st) {
+  SparseMaps maps;
+  astro_status_t s = sparse_maps(c, g, &maps);
+  if (s != ASTRO_OK) return s;
+  static std::atomic<int> done[kMaxDevices];
+  if ((s = set_smem_once(sparse_attn_fwd_kernel<D>, SparseFwdSmem<D>::kTotal, done)) != ASTRO_OK) return s;
+  const SparseSplit split = sparse_split(c.a.batch, c.a.heads, c.a.n_q, c.n_select, c.block_tokens);
+  const long long rows = static_cast<long long>(c.a.batch) * c.a.heads * c.a.n_q;
+  SparseFwdArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(c.q);
+  a.blocks = c.blocks;
+  a.o = static_cast<__nv_bfloat16*>(o);
+  a.lse = lse;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_lse = a.part_o + (split.splits > 1 ? split.splits * rows * D : 0);
+  a.batch = c.a.batch; a.heads = c.a.heads; a.n_q = c.a.n_q;
+  a.scale_log2 = scale * kLog2e;
+  a.careful = g_fwd_mode.load(std::memory_order_relaxed) == 1 ? 1 : 0;
+  SparseUnits u;
+  u.q_tiles = (c.a.n_q - 1) / kTile + 1;
+  u.cache_shared = (c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1) ? 1 : 0;
+  u.dim_y = u.cache_shared ? c.a.batch : c.a.heads;
+  u.splits = split.splits;
+  u.entries = split.entries;
+  u.n_select = c.n_select;
+  u.first = 0; u.stride = 0;
+  const long long units = static_cast<long long>(u.q_tiles) * c.a.heads * c.a.batch * split.splits;
+  const int sms = sm_count();
+  if (sms <= 0) return ASTRO_ERR_CUDA;
+  if (units > 0x3fffffffLL) return ASTRO_ERR_SHAPE;
+  u.total = static_cast<int>(units);
+  long long ctas = units < sms ? units : sms;
+  if (units > ctas * kFwdMaxUnits) ctas = sms * ((units + static_cast<long long>(sms) * kFwdMaxUnits - 1) / (static_cast<long long>(sms) * kFwdMaxUnits));
+  sparse_attn_fwd_kernel<D><<<static_cast<unsigned>(ctas), kFwdThreads, SparseFwdSmem<D>::kTotal, st>>>(maps, a, g, u);
+  if ((s = launch_status()) != ASTRO_OK || split.splits == 1) return s;
+  sparse_combine_kernel<D><<<static_cast<unsigned>((rows + 7) / 8), 256, 0, st>>>(a.part_o, a.part_lse, split.splits, rows, c.a.n_q,
+                                                                             c.a.heads, a.o, lse);
+  return launch_status();
 }
 
 }  // namespace
@@ -1018,6 +1139,34 @@ astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* poo
   a.keep_chunk = keep & ASTRO_KEEP_CHUNK ? 1 : 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return head_dim == 128 ? launch_select_all<128>(qs, ks, a, kb, batch, st) : launch_select_all<64>(qs, ks, a, kb, batch, st);
+}
+
+size_t astro_sparse_attn_fwd_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_select, int block_tokens) {
+  if (batch < 1 || heads < 1 || n_q < 1 || n_select < 1 || (head_dim != 64 && head_dim != 128) || !block_tokens_ok(block_tokens))
+    return 0;
+  const SparseSplit sp = sparse_split(batch, heads, n_q, n_select, block_tokens);
+  return sp.splits == 1 ? 0 : static_cast<size_t>(sp.splits) * batch * heads * n_q * (head_dim + 1) * sizeof(float);
+}
+
+astro_status_t astro_sparse_attn_fwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
+                                     const int32_t* blocks, int n_select, int block_tokens, int batch, int heads,
+                                     int head_dim, int n_q, int n_kc, float scale, void* o, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  if (!q || !o || !blocks || (n_kc > 0 && (!k_chunk || !v_chunk))) return ASTRO_ERR_NULL;
+  const SparseCall c{{cache, batch, heads, head_dim, n_q, n_kc}, q, k_chunk, v_chunk, blocks, n_select, block_tokens};
+  SparseGeom g;
+  astro_status_t s = check_sparse(c, scale, &g);
+  if (s != ASTRO_OK) return s;
+  const size_t need = astro_sparse_attn_fwd_workspace_bytes(batch, heads, head_dim, n_q, n_select, block_tokens);
+  if (need > 0 && !workspace) return ASTRO_ERR_NULL;
+  if (!aligned16(q) || !aligned16(o) || (n_kc > 0 && (!aligned16(k_chunk) || !aligned16(v_chunk))) ||
+      (need > 0 && !aligned16(workspace)) || (reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(blocks) & 3u))
+    return ASTRO_ERR_ALIGN;
+  if (workspace_bytes < need) return ASTRO_ERR_CAPACITY;
+  if ((s = check_arch()) != ASTRO_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return head_dim == 128 ? launch_sparse_fwd<128>(c, g, scale, o, lse, workspace, st)
+                         : launch_sparse_fwd<64>(c, g, scale, o, lse, workspace, st);
 }
 
 astro_status_t astro_nft_loss(const void* v_theta, const void* v_old, const void* v_ref, const void* v_target,

@@ -1,0 +1,634 @@
+// Forward of attention over lists of key blocks: O and LSE.
+//   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - LSE_i),  j over the tokens of the blocks listed for i's query block
+//
+// The work of a listed block is that of a block of dense attention, so the kernel is built like the dense forward: one
+// CTA per SM walks over its share of the units (a 128-query tile of one head of one sample), the key tiles of all its
+// units form one stream, four softmax groups of 128 threads, one thread that issues every tcgen05 MMA, one
+// warp that follows the lists and issues every TMA load, eight warps that bring Q and take O out.  What the dense
+// kernel knows beforehand (how many tiles a unit has, which keys of a tile exist) is here data: the producer warp writes a
+// descriptor per tile, two tiles ahead, and the other roles act on it.  Tensor-memory layout, the S look-ahead, the rings and
+// the one-wait, one-commit rhythm of the issuing thread are the dense kernel's.
+//
+// Precision: bf16 products, fp32 sums.  P is rounded to bf16 for P V (2^-9 of each weight), the row sum is taken from the
+// fp32 values.  Fast pass: each row keeps the maximum of its unit's first tile as its one reference; exp2(s - m) is exact for
+// any reference as long as nothing overflows.  A unit with a row sum beyond 2^100, an infinity or a NaN is done
+// again by the careful pass: a plain loop, tile by tile, with the running maximum of the textbook.
+//
+// Few units: a unit's list is cut into up to `splits` ranges that run as units of their own and leave O (fp32, normalised)
+// and LSE of their part; sparse_combine_kernel joins them.
+#pragma once
+#include "attn_fwd.cuh"
+#include "sparse_common.cuh"
+
+namespace astro {
+
+struct SparseUnits {
+  int q_tiles, dim_y, cache_shared, splits, entries, n_select;   // entries: list entries per split
+  int first, stride, total;
+};
+// Unit id -> (query tile, head, sample, split); query tiles fastest, then (y, z) = (head, sample), or (sample, head) when one
+// stored prefix serves every sample (see the dense kernel), splits slowest.
+struct SparseUnit {
+  int qt, h, b, split;
+  __device__ SparseUnit(const SparseUnits& s, int unit, int heads, int batch) {
+    qt = unit % s.q_tiles;
+    int x = unit / s.q_tiles;
+    const int y = x % s.dim_y;
+    x /= s.dim_y;
+    const int dim_z = s.cache_shared ? heads : batch;
+    const int z = x % dim_z;
+    split = x / dim_z;
+    h = s.cache_shared ? z : y;
+    b = s.cache_shared ? y : z;
+  }
+};
+
+struct SparseFwdArgs {
+  const __nv_bfloat16* q;
+  const int* blocks;       // [B][H][q_tiles][n_select]
+  __nv_bfloat16* o;
+  float* lse;              // may be null
+  float* part_o;           // [split][B][H][n_q][D] when splits > 1
+  float* part_lse;         // [split][B][H][n_q]
+  int batch, heads, n_q;
+  float scale_log2;
+  int careful;             // 1: careful pass only
+};
+
+template <int D> struct SparseFwdSmem {
+  static constexpr int kK = FwdSmem<D>::kK;
+  static constexpr int kV = FwdSmem<D>::kV;
+  static constexpr int kMax = FwdSmem<D>::kMax;
+  static constexpr int kBars = FwdSmem<D>::kBars;                            // 48 barriers, holder and abort flag
+  static constexpr int kDesc = kBars + 48 * 8 + 16;
+  static constexpr int kSource = kDesc + kSpDescs * static_cast<int>(sizeof(TileDesc));
+  static constexpr int kRedo = kSource + kSpDescs * static_cast<int>(sizeof(TileSource));
+  static constexpr int kTotal = kRedo + kFwdMaxUnits / 8 + 1024;
+};
+
+// Everything a role needs.
+template <int D> struct SparseCta {
+  uint8_t *sK, *sV;
+  float* smax;
+  TileDesc* desc;
+  TileSource* source;
+  uint32_t* redo;
+  volatile int* abort_flag;
+  uint32_t tmem_base;
+};
+
+// The units of a CTA as one stream of tiles (producer warp, all lanes).
+struct SparseStream {
+  ListWalker w;
+  int unit, h, b, bx;
+  bool opens;
+  __device__ void open(const SparseGeom& g, const SparseUnits& s, const SparseFwdArgs& a, int lane) {
+    const SparseUnit u(s, unit, a.heads, a.batch);
+    h = u.h;
+    b = u.b;
+    bx = s.cache_shared ? 0 : u.b;
+    const int from = u.split * s.entries;
+    const int* list = a.blocks + ((static_cast<long long>(b) * a.heads + h) * s.q_tiles + u.qt) * s.n_select + from;
+    w.open(g, list, max(0, min(s.entries, s.n_select - from)), lane);
+    opens = true;
+  }
+  // tile J: descriptor and source (lane 0 writes them); false when the stream is over
+  __device__ bool next(const SparseGeom& g, const SparseUnits& s, const SparseFwdArgs& a, int J, TileDesc* desc,
+                       TileSource* source, int lane) {
+    if (unit >= s.total) {
+      if (lane == 0) desc[J % kSpDescs].flags = 0;
+      return false;
+    }
+    uint32_t valid;
+    const bool last = next_tile(g, w, h, b, bx, source + J % kSpDescs, valid);
+    const bool end = last && unit + s.stride >= s.total;
+    if (lane == 0) {
+      desc[J % kSpDescs].valid = valid;
+      desc[J % kSpDescs].flags = kTileThere | (opens ? kTileFirst : 0u) | (last ? kTileLast : 0u) | (end ? kTileEnd : 0u);
+    }
+    opens = false;
+    if (last) {
+      unit += s.stride;
+      if (unit < s.total) open(g, s, a, lane);
+    }
+    return true;
+  }
+};
+
+// The dense fast pass's barriers and one per warp quarter for the first tile's row maxima: every meeting of the
+// fast pass is an mbarrier with a bounded wait, so a role that gives up leaves none of the others behind.
+struct SparseBars : FwdFastBars {
+  uint64_t* max_full;   // [4], 32 * kFwdGroups arrivals
+  __device__ explicit SparseBars(uint64_t* b) : FwdFastBars(b), max_full(b + 23) {}
+  __device__ void init(int q_count) const {
+    FwdFastBars::init(q_count);
+    for (int i = 0; i < 4; ++i) mbar_init(max_full + i, 32 * kFwdGroups);
+  }
+};
+
+// O (+)= P V: P of 16 keys = 8 packed columns; group g's pairs start at its own S columns.  One thread.
+template <int D>
+__device__ __forceinline__ void sparse_pv(uint32_t tmem_base, uint32_t pcol, uint32_t v_smem, uint32_t onto) {
+  constexpr uint32_t idesc = make_idesc_bf16(kTile, D, false, true);
+  const uint64_t v_desc = desc_mnmajor(v_smem, TileGeom<D>::kBlockBytes);
+#pragma unroll
+  for (int kb = 0; kb < kTile / 16; ++kb) {
+    const uint32_t p = pcol + (kb * 16 / kFwdCols) * kFwdCols + (kb * 16 % kFwdCols) / 2;
+    mma_ts(tmem_base + kFwdColO, p, desc_step(v_desc, kb * 2048), idesc, kb > 0 ? 1u : onto);
+  }
+}
+// S = Q K^T of one tile into the S buffer at column `scol`.  One thread.
+template <int D>
+__device__ __forceinline__ void sparse_s(uint32_t scol, uint32_t qcol, uint64_t k_desc) {
+  constexpr uint32_t idesc = make_idesc_bf16(kTile, kTile, false, false);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)   // 16 elements of the head dimension = 8 packed Q columns
+    mma_ts(scol, qcol + k * 8, desc_step(k_desc, (k >> 2) * TileGeom<D>::kBlockBytes + (k & 3) * 32), idesc, k > 0);
+}
+
+// ---------------------------------------------------------------------------------- producer warp, fast pass
+template <int D>
+__device__ __forceinline__ void sparse_produce(const SparseCta<D>& c, const SparseGeom& g, const SparseUnits& s,
+                                               const SparseFwdArgs& a, const SparseMaps& maps, const SparseBars& bar, int lane) {
+  SparseStream st;
+  st.unit = s.first;
+  st.open(g, s, a, lane);
+  const uint32_t bytes = sparse_tile_bytes<D>(g);
+  auto load = [&](int J, bool is_k, uint64_t* full) {
+    load_sparse_tile<D>((is_k ? c.sK + (J % kFwdKStages) * TileGeom<D>::kBytes : c.sV + (J % kFwdVStages) * TileGeom<D>::kBytes),
+                        is_k ? &maps.kx : &maps.vx, is_k ? &maps.kc : &maps.vc, full, c.source + J % kSpDescs, g);
+  };
+  st.next(g, s, a, 0, c.desc, c.source, lane);
+  bool more = st.next(g, s, a, 1, c.desc, c.source, lane);   // whether tile J + 1 exists
+  if (lane == 0) {
+    mbar_arrive_expect_tx(bar.k01, (more ? 2 : 1) * bytes);
+    load(0, true, bar.k01);
+    if (more) load(1, true, bar.k01);
+  }
+  for (int J = 0;; ++J) {
+    // S(J-1) done: the K stage of tile J+2 (that of tile J-1) and the V stage of tile J (that of tile J-3) are free, and no
+    // role still reads the descriptor that tile J+2 overwrites (that of tile J-6)
+    if (J >= 1 && !mbar_wait(bar.sdone + (J - 1) % 4, ((J - 1) / 4) & 1, c.abort_flag)) break;
+    const bool ahead = st.next(g, s, a, J + 2, c.desc, c.source, lane);
+    if (lane == 0) {
+      uint64_t* full = bar.ready + J % 4;
+      mbar_arrive_expect_tx(full, (ahead ? 2 : 1) * bytes);
+      load(J, false, full);
+      if (ahead) load(J + 2, true, full);
+    }
+    __syncwarp();
+    if (!more) break;
+    more = ahead;
+  }
+}
+
+// ---------------------------------------------------------------------------------- MMA issuer, fast pass (one thread)
+template <int D>
+__device__ __forceinline__ void sparse_issue(const SparseCta<D>& c, const SparseBars& bar) {
+  const uint64_t k_desc0 = desc_kmajor(smem_u32(c.sK));
+  const uint32_t sV_addr = smem_u32(c.sV);
+  const uint32_t tmem_base = c.tmem_base;
+  volatile int* abort_flag = c.abort_flag;
+  uint64_t *q_full = bar.q_full, *ready = bar.ready, *sdone = bar.sdone, *o_full = bar.o_full, *o_free = bar.o_free;
+  const volatile TileDesc* desc = c.desc;
+  auto issue_s = [&](int J, int qbuf) {
+    sparse_s<D>(tmem_base + kFwdColS + (J % kFwdSBufs) * 128, tmem_base + kFwdColQ + qbuf * kFwdQCols,
+                desc_step(k_desc0, (J % kFwdKStages) * TileGeom<D>::kBytes));
+    mma_commit(sdone + J % 4);
+  };
+  int s_n = 0;   // unit (counted within the CTA) of the last S issued
+  auto wait_q = [&]() {
+    mbar_wait_spin(q_full + (s_n & 1), (s_n >> 1) & 1, abort_flag);
+    tc_fence_after_sync();
+  };
+  mbar_wait_spin(bar.k01, 0, abort_flag);
+  uint32_t now = desc[0].flags, next = desc[1].flags;
+  wait_q();
+  issue_s(0, 0);
+  if (next & kTileThere) {
+    if (next & kTileFirst) { ++s_n; wait_q(); }
+    issue_s(1, s_n & 1);
+  }
+  int n = 0;
+  for (int J = 0;; ++J) {
+    mbar_wait_spin(ready + J % 4, (J / 4) & 1, abort_flag);
+    if ((now & kTileFirst) && n > 0) mbar_wait_spin(o_free, (n - 1) & 1, abort_flag);   // the previous unit's O is out
+    tc_fence_after_sync();
+    const uint32_t later = desc[(J + 2) % kSpDescs].flags;   // written before the bytes of tile J were asked for
+    sparse_pv<D>(tmem_base, tmem_base + kFwdColS + (J % kFwdSBufs) * 128, sV_addr + (J % kFwdVStages) * TileGeom<D>::kBytes,
+                 (now & kTileFirst) ? 0u : 1u);
+    if (now & kTileLast) { mma_commit(o_full); ++n; }
+    if (later & kTileThere) {
+      if (later & kTileFirst) { ++s_n; wait_q(); }
+      issue_s(J + 2, s_n & 1);
+    }
+    if ((now & kTileEnd) || *abort_flag) break;
+    now = next;
+    next = later;
+  }
+}
+
+// ---------------------------------------------------------------------------------- softmax groups, fast pass
+// exp2(s * scale_log2 - m) of a group's 32 keys of which the first `valid` exist, as bf16 pairs; returns their sum.
+// `valid` is the same for the whole warp, so full groups of eight keys need no test per key.
+__device__ __forceinline__ float sparse_exp32(const uint32_t (&s)[32], int valid, float scale_log2, float neg_m,
+                                              uint32_t (&pk)[16]) {
+  float unused = 0.f;
+  if (valid >= 32) return fwd_exp32(s, 32, scale_log2, neg_m, pk, unused);
+  const uint64_t sc2 = f32x2(scale_log2, scale_log2), nm2 = f32x2(neg_m, neg_m);
+  float sum = 0.f;
+#pragma unroll
+  for (int c8 = 0; c8 < 32; c8 += 8) {
+    if (valid >= c8 + 8) {
+#pragma unroll
+      for (int c = c8; c < c8 + 8; c += 2) {
+        float x0, x1;
+        f32x2_split(fma2(f32x2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sc2, nm2), x0, x1);
+        const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+        sum += p0 + p1;
+        pk[c >> 1] = pack_bf16(p0, p1);
+      }
+    } else {
+#pragma unroll
+      for (int c = c8; c < c8 + 8; c += 2) {
+        float p0 = 0.f, p1 = 0.f;
+        if (c < valid) p0 = fast_exp2(fmaf(__uint_as_float(s[c]), scale_log2, neg_m));
+        if (c + 1 < valid) p1 = fast_exp2(fmaf(__uint_as_float(s[c + 1]), scale_log2, neg_m));
+        sum += p0 + p1;
+        pk[c >> 1] = pack_bf16(p0, p1);
+      }
+    }
+  }
+  return sum;
+}
+
+__device__ __forceinline__ float row_max(const uint32_t (&s)[32], int valid) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 32; ++k)
+    if (k < valid) mx = fmaxf(mx, __uint_as_float(s[k]));
+  return mx;
+}
+
+template <int D>
+__device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const SparseBars& bar, int warp, int r, float scale_log2) {
+  const int g = warp >> 2;
+  const FwdStats<D> stats{c.smax};
+  const uint32_t lane_s = c.tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kFwdColS + g * kFwdCols;
+  volatile int* abort_flag = c.abort_flag;
+  const volatile TileDesc* desc = c.desc;
+  float m_ref = 0.f, l_run = 0.f;
+  int n = 0;
+  for (int J = 0;; ++J) {
+    // the descriptor of tile J was written before the producer asked for the bytes that tile J-2 (J = 0, 1: the first
+    // two S) waited for; that barrier's phase is over by now, the wait on it is for the order of memory alone
+    mbar_wait(bar.sdone + J % 4, (J / 4) & 1, abort_flag);
+    mbar_wait_spin(J < 2 ? bar.k01 : bar.ready + (J - 2) % 4, J < 2 ? 0 : ((J - 2) / 4) & 1, abort_flag);
+    __syncwarp();
+    tc_fence_after_sync();
+    const uint32_t flags = desc[J % kSpDescs].flags;
+    const int valid = (desc[J % kSpDescs].valid >> (8 * g)) & 0xff;
+    const uint32_t colS = lane_s + (J % kFwdSBufs) * 128;
+    uint32_t s[32], pk[16];
+    tmem_ld32(colS, s);
+    tmem_wait_ld();
+    if (flags & kTileFirst) {
+      float* slot = stats.maxima(n);   // alternates: a fast thread may be a unit ahead of the others
+      float mx = row_max(s, valid);
+      slot[g * kTile + r] = mx;
+      mbar_arrive(bar.max_full + (warp & 3));
+      mbar_wait(bar.max_full + (warp & 3), n & 1, abort_flag);
+#pragma unroll
+      for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
+      m_ref = mx == -INFINITY ? 0.f : mx * scale_log2;   // no key in an empty list's tile
+      l_run = 0.f;
+    }
+    l_run += sparse_exp32(s, valid, scale_log2, -m_ref, pk);
+    tmem_st16(colS, pk);   // in place: this thread has read all of its S columns
+    tmem_wait_st();
+    tc_fence_before_sync();
+    mbar_arrive(bar.ready + J % 4);
+    if (flags & kTileLast) {
+      // the slots of unit n - 2 are free: the epilogue warps read them before they let go of that unit's O, which the
+      // first P V of unit n - 1 waited for
+      stats.sums(n)[g * kTile + r] = l_run;
+      if (g == 0) stats.refs(n)[r] = m_ref;
+      if (!(l_run < kFastSumLimit)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));   // true for inf and NaN too
+      mbar_arrive(bar.stats_full + (n & 1));
+      ++n;
+    }
+    if ((flags & kTileEnd) || *abort_flag) break;
+  }
+}
+
+// ---------------------------------------------------------------------------------- results of a unit
+// Where a lane's row goes: bf16 rows of O (its quad's rows together) and LSE, or the fp32 parts of a split.
+template <int D> struct SparseRow {
+  bool in_range;
+  float *lse_dst, *part;
+  QuadRows out, q_rows;
+  __device__ SparseRow(const SparseUnits& s, const SparseUnit& u, const SparseFwdArgs& a, int r) {
+    const int row = u.qt * kTile + r;
+    in_range = row < a.n_q;
+    const size_t at = (static_cast<size_t>(u.b) * a.heads + u.h) * a.n_q + (in_range ? row : 0);
+    const size_t rows = static_cast<size_t>(a.batch) * a.heads * a.n_q;
+    lse_dst = s.splits > 1 ? a.part_lse + u.split * rows + at : a.lse ? a.lse + at : nullptr;
+    part = s.splits > 1 ? a.part_o + (u.split * rows + at) * D : nullptr;
+    out = quad_rows(a.o, u.b, u.h, a.n_q, a.heads, D, row);
+    q_rows = quad_rows(a.q, u.b, u.h, a.n_q, a.heads, D, row);
+  }
+  // 32 accumulator columns from col0 on, times 1 / l
+  __device__ void store(const uint32_t (&acc)[32], float inv, uint64_t& chk2, int col0, int lane) const {
+    if (part == nullptr) {
+      fwd_store_slice(acc, f32x2(inv, inv), chk2, out, col0, lane);
+      return;
+    }
+    float4* dst = reinterpret_cast<float4*>(part + col0);
+#pragma unroll
+    for (int c = 0; c < 32; c += 4) {
+      const float4 v = make_float4(__uint_as_float(acc[c]) * inv, __uint_as_float(acc[c + 1]) * inv,
+                                   __uint_as_float(acc[c + 2]) * inv, __uint_as_float(acc[c + 3]) * inv);
+      chk2 = fma2(f32x2(v.x, v.y), f32x2(0.f, 0.f), chk2);
+      chk2 = fma2(f32x2(v.z, v.w), f32x2(0.f, 0.f), chk2);
+      if (in_range) dst[c / 4] = v;
+    }
+  }
+  __device__ void store_lse(float m, float l) const {
+    if (in_range && lse_dst != nullptr) *lse_dst = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  }
+  __device__ void stage_q(uint32_t tmem_q, int part64, int lane) const {
+    uint32_t qr[32];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      uint4 ch[4];
+      load_quad_rows(ch, q_rows, part64 * 64 + half * 32, lane);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        qr[16 * half + 4 * v] = ch[v].x; qr[16 * half + 4 * v + 1] = ch[v].y;
+        qr[16 * half + 4 * v + 2] = ch[v].z; qr[16 * half + 4 * v + 3] = ch[v].w;
+      }
+    }
+    tmem_st32(tmem_q + part64 * 32, qr);
+    tmem_wait_st();
+  }
+};
+
+template <int D>
+__device__ __forceinline__ void sparse_epilogue(const SparseCta<D>& c, const SparseUnits& s, const SparseFwdArgs& a,
+                                                const SparseBars& bar, int warp, int lane) {
+  constexpr int kSlices = D / 32, kOwn = kSlices / 2;
+  constexpr int kMmaWarp = 4 * kFwdGroups;
+  const FwdStats<D> stats{c.smax};
+  const int half = (warp - kMmaWarp - 2) >> 2;
+  const int r = (warp & 3) * 32 + lane;
+  const uint32_t tmem_lane = c.tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  auto stage_q = [&](int unit, int buf) {
+    if (half >= D / 64 || unit >= s.total) return;
+    SparseRow<D>(s, SparseUnit(s, unit, a.heads, a.batch), a, r).stage_q(tmem_lane + kFwdColQ + buf * kFwdQCols, half, lane);
+    tc_fence_before_sync();
+    mbar_arrive(bar.q_full + buf);
+  };
+  stage_q(s.first, 0);
+  if (s.total - s.first > s.stride) stage_q(s.first + s.stride, 1);
+  int n = 0;
+  for (int unit = s.first; unit < s.total; unit += s.stride, ++n) {
+    const SparseRow<D> row(s, SparseUnit(s, unit, a.heads, a.batch), a, r);
+    mbar_wait_relaxed(bar.stats_full + (n & 1), (n >> 1) & 1, c.abort_flag);
+    float l = 0.f;
+#pragma unroll
+    for (int g = 0; g < kFwdGroups; ++g) l += stats.sums(n)[g * kTile + r];
+    const float m = stats.refs(n)[r];
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint64_t chk2 = f32x2(0.f, 0.f);
+    mbar_wait(bar.o_full, n & 1, c.abort_flag);
+    tc_fence_after_sync();
+    uint32_t acc[kOwn][32];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) tmem_ld32(tmem_lane + kFwdColO + (half * kOwn + i) * 32, acc[i]);
+    tmem_wait_ld();
+    tc_fence_before_sync();
+    mbar_arrive(bar.o_free);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) row.store(acc[i], inv, chk2, (half * kOwn + i) * 32, lane);
+    if (half == 0) row.store_lse(m, l);
+    if (!fwd_all_finite(chk2)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));
+    if (s.total - unit > 2 * s.stride) stage_q(unit + 2 * s.stride, n & 1);
+  }
+}
+
+// ---------------------------------------------------------------------------------- careful pass
+// One unit, tile by tile, nothing overlapped: load, S, running maximum, P, P V.  All threads of the CTA call it;
+// `tick` counts the tiles this CTA has done in this pass (the phases of its three barriers).
+template <int D>
+__device__ __noinline__ void sparse_careful_unit(const SparseCta<D>& c, const SparseGeom& g, const SparseUnits& s,
+                                                 const SparseFwdArgs& a, const SparseMaps* maps, uint64_t* bars, int unit,
+                                                 int warp, int lane, int& tick) {
+  constexpr int kMmaWarp = 4 * kFwdGroups, kTmaWarp = 4 * kFwdGroups + 1;
+  uint64_t *kv_full = bars, *s_done = bars + 1, *pv_done = bars + 2;
+  const SparseUnit u(s, unit, a.heads, a.batch);
+  const int grp = warp >> 2, r = (warp & 3) * 32 + lane;
+  const bool softmax = warp < kMmaWarp;
+  const uint32_t tmem_lane = c.tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  const SparseRow<D> row(s, u, a, r);
+  SparseStream st;
+  if (warp == kTmaWarp) {
+    st.unit = unit;
+    st.open(g, s, a, lane);
+  }
+  if (softmax && grp < D / 64) row.stage_q(tmem_lane + kFwdColQ, grp, lane);
+  float m_run = -INFINITY, l_run = 0.f;
+  float* slot = c.smax;
+  for (bool first = true;; first = false, ++tick) {
+    bool last = false;
+    if (warp == kTmaWarp) {
+      uint32_t valid;
+      last = next_tile(g, st.w, st.h, st.b, st.bx, c.source, valid);
+      if (lane == 0) {
+        c.desc[0].valid = valid;
+        c.desc[0].flags = last ? kTileLast : 0u;
+        if (!*c.abort_flag) {
+          mbar_arrive_expect_tx(kv_full, 2 * sparse_tile_bytes<D>(g));
+          load_sparse_tile<D>(c.sK, &maps->kx, &maps->kc, kv_full, c.source, g);
+          load_sparse_tile<D>(c.sV, &maps->vx, &maps->vc, kv_full, c.source, g);
+        }
+      }
+    }
+    tc_fence_before_sync();
+    __syncthreads();   // descriptor written; Q staged; the tile before is done with S and P
+    tc_fence_after_sync();
+    last = reinterpret_cast<const volatile TileDesc*>(c.desc)->flags & kTileLast;
+    const uint32_t valid4 = reinterpret_cast<const volatile TileDesc*>(c.desc)->valid;
+    if (warp == kMmaWarp && lane == 0) {
+      mbar_wait_spin(kv_full, tick & 1, c.abort_flag);
+      tc_fence_after_sync();
+      sparse_s<D>(c.tmem_base + kFwdColS, c.tmem_base + kFwdColQ, desc_kmajor(smem_u32(c.sK)));
+      mma_commit(s_done);
+    }
+    if (softmax) {
+      const int valid = (valid4 >> (8 * grp)) & 0xff;
+      const uint32_t colS = tmem_lane + kFwdColS + grp * kFwdCols;
+      mbar_wait(s_done, tick & 1, c.abort_flag);
+      tc_fence_after_sync();
+      uint32_t sv[32], pk[16];
+      tmem_ld32(colS, sv);
+      tmem_wait_ld();
+      float mx = row_max(sv, valid);
+      slot[grp * kTile + r] = mx;
+      named_barrier_sync(1 + (warp & 3), 32 * kFwdGroups);
+#pragma unroll
+      for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
+      const float m_new = fmaxf(m_run, mx * a.scale_log2);   // -inf while no key has a finite score
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_use);
+      m_run = m_new;
+      l_run = l_run * alpha + sparse_exp32(sv, valid, a.scale_log2, -m_use, pk);
+      tmem_st16(colS, pk);
+      if (!first) {   // O is at rest: the P V of the tile before was awaited
+#pragma unroll
+        for (int c4 = 0; c4 < D / 32; ++c4) {
+          if (c4 % kFwdGroups != grp) continue;
+          tmem_ld32(tmem_lane + kFwdColO + c4 * 32, sv);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) * alpha);
+          tmem_st32(tmem_lane + kFwdColO + c4 * 32, sv);
+        }
+      }
+      tmem_wait_st();
+    }
+    tc_fence_before_sync();
+    __syncthreads();   // P and the rescaled O are in tensor memory
+    tc_fence_after_sync();
+    if (warp == kMmaWarp && lane == 0) {
+      sparse_pv<D>(c.tmem_base, c.tmem_base + kFwdColS, smem_u32(c.sV), first ? 0u : 1u);
+      mma_commit(pv_done);
+    }
+    mbar_wait(pv_done, tick & 1, c.abort_flag);   // K, V, S, P and the descriptor may be overwritten
+    tc_fence_after_sync();
+    if (last) { ++tick; break; }   // the same for every thread; after a wait has run out the others return at once
+  }
+  __syncthreads();
+  if (softmax) {
+    slot[grp * kTile + r] = l_run;
+    named_barrier_sync(1 + (warp & 3), 32 * kFwdGroups);
+    float l = 0.f;
+#pragma unroll
+    for (int og = 0; og < kFwdGroups; ++og) l += slot[og * kTile + r];
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint64_t chk2 = f32x2(0.f, 0.f);
+    for (int c4 = grp; c4 < D / 32; c4 += kFwdGroups) {
+      uint32_t acc[32];
+      tmem_ld32(tmem_lane + kFwdColO + c4 * 32, acc);
+      tmem_wait_ld();
+      row.store(acc, inv, chk2, c4 * 32, lane);
+    }
+    if (grp == 0) row.store_lse(m_run, l);
+  }
+  tc_fence_before_sync();
+  __syncthreads();   // the exchange slots and O may be overwritten
+  tc_fence_after_sync();
+}
+
+// ---------------------------------------------------------------------------------- kernel
+// grid.x CTAs share the units (at most kFwdMaxUnits each): CTA i takes units i, i + grid.x, ...
+template <int D>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_constant__ SparseFwdArgs a,
+                       const __grid_constant__ SparseGeom g, const __grid_constant__ SparseUnits units_in) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = align_1024(smem_raw);
+  uint64_t* bar_mem = reinterpret_cast<uint64_t*>(smem + SparseFwdSmem<D>::kBars);
+  const SparseBars bar(bar_mem);
+  uint64_t* careful_bars = bar_mem + kFwdBarSlots;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bar_mem + 48);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  constexpr uint32_t kTmemCols = 512;
+  constexpr int kMmaWarp = 4 * kFwdGroups, kTmaWarp = 4 * kFwdGroups + 1;
+
+  SparseCta<D> c;
+  c.sK = smem + SparseFwdSmem<D>::kK;
+  c.sV = smem + SparseFwdSmem<D>::kV;
+  c.smax = reinterpret_cast<float*>(smem + SparseFwdSmem<D>::kMax);
+  c.desc = reinterpret_cast<TileDesc*>(smem + SparseFwdSmem<D>::kDesc);
+  c.source = reinterpret_cast<TileSource*>(smem + SparseFwdSmem<D>::kSource);
+  c.redo = reinterpret_cast<uint32_t*>(smem + SparseFwdSmem<D>::kRedo);
+  c.abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  SparseUnits s = units_in;
+  s.first = blockIdx.x;
+  s.stride = gridDim.x;
+
+  if (tid == 0) {
+    bar.init(128 * (D / 64));
+    for (int i = 0; i < 3; ++i) mbar_init(careful_bars + i, 1);
+    *c.abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (tid < kFwdMaxUnits / 32) c.redo[tid] = 0;
+  zero_uncovered_rows<D>(c.sK, kFwdKStages, g, tid, kFwdThreads);
+  zero_uncovered_rows<D>(c.sV, kFwdVStages, g, tid, kFwdThreads);
+  fence_proxy_async_smem();
+  if (warp == kMmaWarp) {
+    tmem_alloc(tmem_holder, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  c.tmem_base = *tmem_holder;
+
+  if (!a.careful) {
+    if (warp == kTmaWarp) sparse_produce<D>(c, g, s, a, maps, bar, lane);
+    else if (warp == kMmaWarp) { if (lane == 0) sparse_issue<D>(c, bar); }
+    else if (warp < kMmaWarp) sparse_softmax<D>(c, bar, warp, tid & 127, a.scale_log2);
+    else sparse_epilogue<D>(c, s, a, bar, warp, lane);
+  }
+  // every MMA of the fast pass has finished by now: the epilogue warps waited for the last one
+  int n = 0, tick = 0;
+  for (int unit = s.first; unit < s.total; unit += s.stride, ++n) {
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (*c.abort_flag) break;
+    if (!a.careful && !((c.redo[n >> 5] >> (n & 31)) & 1u)) continue;
+    sparse_careful_unit<D>(c, g, s, a, &maps, careful_bars, unit, warp, lane, tick);
+  }
+  settle_after_abort(c.abort_flag);
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == kMmaWarp) tmem_dealloc(c.tmem_base, kTmemCols);
+}
+
+// Joins the parts of split units: weights exp(LSE_s - LSE), a warp per (sample, head, query) row.  Bandwidth: the parts are
+// read once.
+template <int D>
+__global__ void __launch_bounds__(256)
+sparse_combine_kernel(const float* __restrict__ part_o, const float* __restrict__ part_lse, const int splits,
+                      const long long rows, const int n_q, const int heads, __nv_bfloat16* __restrict__ o,
+                      float* __restrict__ lse) {
+  constexpr int kPer = D / 32;
+  const long long at = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
+  const int lane = threadIdx.x & 31;
+  if (at >= rows) return;
+  float top = -INFINITY;
+  for (int i = 0; i < splits; ++i) top = fmaxf(top, part_lse[i * rows + at]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float total = 0.f, acc[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) acc[e] = 0.f;
+  for (int i = 0; i < splits; ++i) {
+    const float w = expf(part_lse[i * rows + at] - ref);   // 0 for a part without keys
+    total += w;
+    const float* src = part_o + (i * rows + at) * D + lane * kPer;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) acc[e] = fmaf(w, src[e], acc[e]);
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const long long bh = at / n_q;
+  const int i = static_cast<int>(at - bh * n_q), h = static_cast<int>(bh % heads);
+  __nv_bfloat16* dst = o + (((bh / heads) * n_q + i) * heads + h) * D + lane * kPer;
+#pragma unroll
+  for (int e = 0; e < kPer; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+  if (lane == 0 && lse != nullptr) lse[at] = total == 0.f ? -INFINITY : ref + logf(total);
+}
+
+}  // namespace astro
