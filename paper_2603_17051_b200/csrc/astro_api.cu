@@ -572,7 +572,7 @@ astro_status_t launch_sparse_fwd(const SparseCall& c, const SparseGeom& g, float
   u.total = static_cast<int>(units);
   long long ctas = units < sms ? units : sms;
   if (units > ctas * kFwdMaxUnits) ctas = sms * ((units + static_cast<long long>(sms) * kFwdMaxUnits - 1) / (static_cast<long long>(sms) * kFwdMaxUnits));
-  sparse_attn_fwd_kernel<D><<<static_cast<unsigned>(ctas), kFwdThreads, SparseFwdSmem<D>::kTotal, st>>>(maps, a, g, u);
+  sparse_attn_fwd_kernel<D><<<static_cast<unsigned>(ctas), kSparseThreads, SparseFwdSmem<D>::kTotal, st>>>(maps, a, g, u);
   if ((s = launch_status()) != ASTRO_OK || split.splits == 1) return s;
   sparse_combine_kernel<D><<<static_cast<unsigned>((rows + 7) / 8), 256, 0, st>>>(a.part_o, a.part_lse, split.splits, rows, c.a.n_q,
                                                                              c.a.heads, a.o, lse);

@@ -4,9 +4,9 @@
 // The work of a listed block is that of a block of dense attention, so the kernel is built like the dense forward: one
 // CTA per SM walks over its share of the units (a 128-query tile of one head of one sample), the key tiles of all its
 // units form one stream, four softmax groups of 128 threads, one thread that issues every tcgen05 MMA, one
-// warp that follows the lists and issues every TMA load, eight warps that bring Q and take O out.  What the dense
+// warp that follows the lists, a thread each for the loads of K and V, eight warps that bring Q and take O out.  What the dense
 // kernel knows beforehand (how many tiles a unit has, which keys of a tile exist) is here data: the producer warp writes a
-// descriptor per tile, two tiles ahead, and the other roles act on it.  Tensor-memory layout, the S look-ahead, the rings and
+// descriptor per tile, a few tiles ahead, and the other roles act on it.  Tensor-memory layout, the S look-ahead, the rings and
 // the one-wait, one-commit rhythm of the issuing thread are the dense kernel's.
 //
 // Precision: bf16 products, fp32 sums.  P is rounded to bf16 for P V (2^-9 of each weight), the row sum is taken from the
@@ -115,16 +115,30 @@ struct SparseStream {
   }
 };
 
-// The dense fast pass's barriers and one per warp quarter for the first tile's row maxima: every meeting of the
-// fast pass is an mbarrier with a bounded wait, so a role that gives up leaves none of the others behind.
+// The dense fast pass's barriers, one per descriptor (written), and one per warp quarter for the first tile's row maxima:
+// every meeting of the fast pass is an mbarrier with a bounded wait, so a role that gives up leaves none of the others
+// behind.  ready[J % 4] takes two arrivals with byte counts, V(J)'s and K(J+2)'s.
 struct SparseBars : FwdFastBars {
-  uint64_t* max_full;   // [4], 32 * kFwdGroups arrivals
-  __device__ explicit SparseBars(uint64_t* b) : FwdFastBars(b), max_full(b + 23) {}
+  uint64_t *max_full, *listed;   // [4], 32 * kFwdGroups arrivals; [kSpDescs]
+  __device__ explicit SparseBars(uint64_t* b) : FwdFastBars(b), max_full(b + 23), listed(b + 27) {}
   __device__ void init(int q_count) const {
-    FwdFastBars::init(q_count);
-    for (int i = 0; i < 4; ++i) mbar_init(max_full + i, 32 * kFwdGroups);
+    mbar_init(q_full, q_count);
+    mbar_init(q_full + 1, q_count);
+    mbar_init(k01, 1);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(ready + i, 2 + 128 * kFwdGroups);
+      mbar_init(sdone + i, 1);
+      mbar_init(max_full + i, 32 * kFwdGroups);
+    }
+    mbar_init(o_full, 1);
+    mbar_init(o_free, 32 * kFwdEpiWarps);
+    mbar_init(stats_full, 128 * kFwdGroups);
+    mbar_init(stats_full + 1, 128 * kFwdGroups);
+    for (int i = 0; i < kSpDescs; ++i) mbar_init(listed + i, 1);
   }
 };
+constexpr int kSparseBarSlots = 36;
+constexpr int kSparseThreads = kFwdThreads + 64;   // the dense kernel's warps and two for the loads of K and V
 
 // O (+)= P V: P of 16 keys = 8 packed columns; group g's pairs start at its own S columns.  One thread.
 template <int D>
@@ -146,39 +160,73 @@ __device__ __forceinline__ void sparse_s(uint32_t scol, uint32_t qcol, uint64_t 
     mma_ts(scol, qcol + k * 8, desc_step(k_desc, (k >> 2) * TileGeom<D>::kBlockBytes + (k & 3) * 32), idesc, k > 0);
 }
 
-// ---------------------------------------------------------------------------------- producer warp, fast pass
+// ---------------------------------------------------------------------------------- producers, fast pass
+// Three warps: one follows the lists and writes descriptors and sources, up to four tiles ahead of S; one thread loads K, one
+// V.  A single producer needed about 1700 clocks per tile for both jobs, with the loads behind each other in front of an
+// MMA that takes 1024 (a 7680-key list per query block, layer shape: 244 us against 217 with the three).
+
+// The list walker.  Tile J overwrites what was written for tile J-8; S(J-4) done means that every P(J-6) has arrived.
+// (The wait names the barrier that S(J) will use next, so its phase cannot run ahead of it.)
 template <int D>
-__device__ __forceinline__ void sparse_produce(const SparseCta<D>& c, const SparseGeom& g, const SparseUnits& s,
-                                               const SparseFwdArgs& a, const SparseMaps& maps, const SparseBars& bar, int lane) {
+__device__ __forceinline__ void sparse_walk(const SparseCta<D>& c, const SparseGeom& g, const SparseUnits& s, const SparseFwdArgs& a,
+                                            const SparseBars& bar, int lane) {
   SparseStream st;
   st.unit = s.first;
   st.open(g, s, a, lane);
-  const uint32_t bytes = sparse_tile_bytes<D>(g);
-  auto load = [&](int J, bool is_k, uint64_t* full) {
-    load_sparse_tile<D>((is_k ? c.sK + (J % kFwdKStages) * TileGeom<D>::kBytes : c.sV + (J % kFwdVStages) * TileGeom<D>::kBytes),
-                        is_k ? &maps.kx : &maps.vx, is_k ? &maps.kc : &maps.vc, full, c.source + J % kSpDescs, g);
-  };
-  st.next(g, s, a, 0, c.desc, c.source, lane);
-  bool more = st.next(g, s, a, 1, c.desc, c.source, lane);   // whether tile J + 1 exists
-  if (lane == 0) {
-    mbar_arrive_expect_tx(bar.k01, (more ? 2 : 1) * bytes);
-    load(0, true, bar.k01);
-    if (more) load(1, true, bar.k01);
+  int behind = 0;   // descriptors behind the last tile: the issuer looks two ahead
+  for (int J = 0; behind < 2; ++J) {
+    if (J >= 4 && !mbar_wait(bar.sdone + J % 4, ((J - 4) / 4) & 1, c.abort_flag)) break;
+    if (!st.next(g, s, a, J, c.desc, c.source, lane)) ++behind;
+    if (lane == 0) mbar_arrive(bar.listed + J % kSpDescs);
   }
-  for (int J = 0;; ++J) {
-    // S(J-1) done: the K stage of tile J+2 (that of tile J-1) and the V stage of tile J (that of tile J-3) are free, and no
-    // role still reads the descriptor that tile J+2 overwrites (that of tile J-6)
-    if (J >= 1 && !mbar_wait(bar.sdone + (J - 1) % 4, ((J - 1) / 4) & 1, c.abort_flag)) break;
-    const bool ahead = st.next(g, s, a, J + 2, c.desc, c.source, lane);
-    if (lane == 0) {
-      uint64_t* full = bar.ready + J % 4;
-      mbar_arrive_expect_tx(full, (ahead ? 2 : 1) * bytes);
-      load(J, false, full);
-      if (ahead) load(J + 2, true, full);
+}
+
+// K of tiles 0 and 1, then K(J+2) as soon as S(J-1) has freed its stage.  One thread.
+template <int D>
+__device__ __forceinline__ void sparse_load_k(const SparseCta<D>& c, const SparseGeom& g, const SparseMaps& maps,
+                                              const SparseBars& bar) {
+  const uint32_t bytes = sparse_tile_bytes<D>(g);
+  const volatile TileDesc* desc = c.desc;
+  auto listed = [&](int J) { return mbar_wait_spin(bar.listed + J % kSpDescs, (J / kSpDescs) & 1, c.abort_flag); };
+  auto load = [&](int J, uint64_t* full) {
+    load_sparse_tile<D>(c.sK + (J % kFwdKStages) * TileGeom<D>::kBytes, &maps.kx, &maps.kc, full, c.source + J % kSpDescs, g);
+  };
+  if (!listed(0) || !listed(1)) return;
+  const bool two = desc[1].flags & kTileThere;
+  mbar_arrive_expect_tx(bar.k01, (two ? 2 : 1) * bytes);
+  load(0, bar.k01);
+  if (two) load(1, bar.k01);
+  uint32_t now = desc[0].flags, next = desc[1].flags;
+  for (int J = 0; now & kTileThere; ++J) {
+    if (!listed(J + 2)) break;
+    const uint32_t later = desc[(J + 2) % kSpDescs].flags;
+    uint64_t* full = bar.ready + J % 4;
+    if (later & kTileThere) {
+      if (J >= 1 && !mbar_wait_spin(bar.sdone + (J - 1) % 4, ((J - 1) / 4) & 1, c.abort_flag)) break;
+      mbar_arrive_expect_tx(full, bytes);
+      load(J + 2, full);
+    } else {
+      mbar_arrive(full);
     }
-    __syncwarp();
-    if (!more) break;
-    more = ahead;
+    now = next;
+    next = later;
+  }
+}
+
+// V(J) as soon as S(J-1) is done, and with it P V of tile J-3, which used its stage.  One thread.
+template <int D>
+__device__ __forceinline__ void sparse_load_v(const SparseCta<D>& c, const SparseGeom& g, const SparseMaps& maps,
+                                              const SparseBars& bar) {
+  const uint32_t bytes = sparse_tile_bytes<D>(g);
+  const volatile TileDesc* desc = c.desc;
+  for (int J = 0;; ++J) {
+    if (!mbar_wait_spin(bar.listed + J % kSpDescs, (J / kSpDescs) & 1, c.abort_flag)) break;
+    const uint32_t flags = desc[J % kSpDescs].flags;
+    if (J >= 3 && !mbar_wait_spin(bar.sdone + (J - 1) % 4, ((J - 1) / 4) & 1, c.abort_flag)) break;
+    uint64_t* full = bar.ready + J % 4;
+    mbar_arrive_expect_tx(full, bytes);
+    load_sparse_tile<D>(c.sV + (J % kFwdVStages) * TileGeom<D>::kBytes, &maps.vx, &maps.vc, full, c.source + J % kSpDescs, g);
+    if (flags & kTileEnd) break;
   }
 }
 
@@ -211,10 +259,10 @@ __device__ __forceinline__ void sparse_issue(const SparseCta<D>& c, const Sparse
   }
   int n = 0;
   for (int J = 0;; ++J) {
-    mbar_wait_spin(ready + J % 4, (J / 4) & 1, abort_flag);
+    if (!mbar_wait_spin(ready + J % 4, (J / 4) & 1, abort_flag)) break;
     if ((now & kTileFirst) && n > 0) mbar_wait_spin(o_free, (n - 1) & 1, abort_flag);   // the previous unit's O is out
     tc_fence_after_sync();
-    const uint32_t later = desc[(J + 2) % kSpDescs].flags;   // written before the bytes of tile J were asked for
+    const uint32_t later = desc[(J + 2) % kSpDescs].flags;   // its writing was awaited by the K loader's arrival for tile J
     sparse_pv<D>(tmem_base, tmem_base + kFwdColS + (J % kFwdSBufs) * 128, sV_addr + (J % kFwdVStages) * TileGeom<D>::kBytes,
                  (now & kTileFirst) ? 0u : 1u);
     if (now & kTileLast) { mma_commit(o_full); ++n; }
@@ -222,7 +270,7 @@ __device__ __forceinline__ void sparse_issue(const SparseCta<D>& c, const Sparse
       if (later & kTileFirst) { ++s_n; wait_q(); }
       issue_s(J + 2, s_n & 1);
     }
-    if ((now & kTileEnd) || *abort_flag) break;
+    if (now & kTileEnd) break;
     now = next;
     next = later;
   }
@@ -270,54 +318,110 @@ __device__ __forceinline__ float row_max(const uint32_t (&s)[32], int valid) {
   return mx;
 }
 
+// Shared-memory addresses (32 bits) that the softmax loop works with, for one group.
+struct SparseLoop {
+  uint32_t lane_s, sdone, ready, listed, desc, abort_flag;
+  int g;
+};
+__device__ __forceinline__ TileDesc load_desc(uint32_t desc, int J) {
+  TileDesc d;
+  asm volatile("ld.volatile.shared::cta.v2.u32 {%0, %1}, [%2];"
+               : "=r"(d.valid), "=r"(d.flags)
+               : "r"(desc + (J % kSpDescs) * static_cast<uint32_t>(sizeof(TileDesc)))
+               : "memory");
+  return d;
+}
+__device__ __forceinline__ TileDesc await_desc(const SparseLoop& c, int J) {
+  mbar_wait_at(c.listed + 8 * (J % kSpDescs), (J / kSpDescs) & 1, c.abort_flag);
+  return load_desc(c.desc, J);
+}
+
+struct SparseRun {
+  float l_run;
+  int J;
+  TileDesc d;   // of tile J
+  bool ok;
+};
+// The tiles of a unit behind its first, from tile J (descriptor d) to the unit's last: the loop in which the kernel spends
+// its time.  Out of line and handed plain values, so that its code does not depend on the bookkeeping around it.
+__device__ __noinline__ SparseRun sparse_run(SparseLoop c, float scale_log2, float neg_m, float l_run, int J, TileDesc d) {
+  static_assert(kFwdCols == 32, "one 32-column load per thread and tile");
+  bool ok = true;
+  while (true) {
+    const uint32_t colS = c.lane_s + (J % kFwdSBufs) * 128;
+    const int valid = (d.valid >> (8 * c.g)) & 0xff;
+    ok = mbar_wait_at(c.sdone + 8 * (J % 4), (J / 4) & 1, c.abort_flag);
+    tc_fence_after_sync();
+    uint32_t sv[32], pk[16];
+    tmem_ld32(colS, sv);
+    const TileDesc next = d.flags & kTileLast ? d : await_desc(c, J + 1);   // long written; in the shadow of the load
+    tmem_wait_ld();
+    l_run += sparse_exp32(sv, valid, scale_log2, neg_m, pk);
+    tmem_st16(colS, pk);   // in place: this thread has read all of its S columns
+    tmem_wait_st();
+    tc_fence_before_sync();
+    mbar_arrive_at(c.ready + 8 * (J % 4));
+    if ((d.flags & kTileLast) || !ok) break;
+    d = next;
+    ++J;
+  }
+  return SparseRun{l_run, J, d, ok};
+}
+
 template <int D>
 __device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const SparseBars& bar, int warp, int r, float scale_log2) {
   const int g = warp >> 2;
   const FwdStats<D> stats{c.smax};
-  const uint32_t lane_s = c.tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kFwdColS + g * kFwdCols;
   volatile int* abort_flag = c.abort_flag;
-  const volatile TileDesc* desc = c.desc;
-  float m_ref = 0.f, l_run = 0.f;
-  int n = 0;
-  for (int J = 0;; ++J) {
-    // the descriptor of tile J was written before the producer asked for the bytes that tile J-2 (J = 0, 1: the first
-    // two S) waited for; that barrier's phase is over by now, the wait on it is for the order of memory alone
-    mbar_wait(bar.sdone + J % 4, (J / 4) & 1, abort_flag);
-    mbar_wait_spin(J < 2 ? bar.k01 : bar.ready + (J - 2) % 4, J < 2 ? 0 : ((J - 2) / 4) & 1, abort_flag);
-    __syncwarp();
+  SparseLoop lp;
+  lp.lane_s = c.tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kFwdColS + g * kFwdCols;
+  lp.sdone = smem_u32(bar.sdone); lp.ready = smem_u32(bar.ready); lp.listed = smem_u32(bar.listed);
+  lp.desc = smem_u32(c.desc);
+  lp.abort_flag = smem_u32(const_cast<int*>(abort_flag));
+  lp.g = g;
+  TileDesc d = await_desc(lp, 0);
+  int J = 0;
+  for (int n = 0;; ++n) {
+    // the unit's first tile fixes the rows' reference
+    const int valid = (d.valid >> (8 * g)) & 0xff;
+    const uint32_t colS = lp.lane_s + (J % kFwdSBufs) * 128;
+    bool ok = mbar_wait_at(lp.sdone + 8 * (J % 4), (J / 4) & 1, lp.abort_flag);
     tc_fence_after_sync();
-    const uint32_t flags = desc[J % kSpDescs].flags;
-    const int valid = (desc[J % kSpDescs].valid >> (8 * g)) & 0xff;
-    const uint32_t colS = lane_s + (J % kFwdSBufs) * 128;
     uint32_t s[32], pk[16];
     tmem_ld32(colS, s);
     tmem_wait_ld();
-    if (flags & kTileFirst) {
-      float* slot = stats.maxima(n);   // alternates: a fast thread may be a unit ahead of the others
-      float mx = row_max(s, valid);
-      slot[g * kTile + r] = mx;
-      mbar_arrive(bar.max_full + (warp & 3));
-      mbar_wait(bar.max_full + (warp & 3), n & 1, abort_flag);
+    float* slot = stats.maxima(n);   // alternates: a fast thread may be a unit ahead of the others
+    float mx = row_max(s, valid);
+    slot[g * kTile + r] = mx;
+    mbar_arrive(bar.max_full + (warp & 3));
+    ok = mbar_wait(bar.max_full + (warp & 3), n & 1, abort_flag) && ok;
 #pragma unroll
-      for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
-      m_ref = mx == -INFINITY ? 0.f : mx * scale_log2;   // no key in an empty list's tile
-      l_run = 0.f;
-    }
-    l_run += sparse_exp32(s, valid, scale_log2, -m_ref, pk);
-    tmem_st16(colS, pk);   // in place: this thread has read all of its S columns
+    for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
+    const float m_ref = mx == -INFINITY ? 0.f : mx * scale_log2;   // no key in an empty list's tile
+    float l_run = sparse_exp32(s, valid, scale_log2, -m_ref, pk);
+    tmem_st16(colS, pk);
     tmem_wait_st();
     tc_fence_before_sync();
-    mbar_arrive(bar.ready + J % 4);
-    if (flags & kTileLast) {
-      // the slots of unit n - 2 are free: the epilogue warps read them before they let go of that unit's O, which the
-      // first P V of unit n - 1 waited for
-      stats.sums(n)[g * kTile + r] = l_run;
-      if (g == 0) stats.refs(n)[r] = m_ref;
-      if (!(l_run < kFastSumLimit)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));   // true for inf and NaN too
-      mbar_arrive(bar.stats_full + (n & 1));
-      ++n;
+    mbar_arrive_at(lp.ready + 8 * (J % 4));
+    uint32_t flags = d.flags;
+    TileDesc next = await_desc(lp, J + 1);
+    if (ok && !(flags & kTileLast)) {
+      const SparseRun run = sparse_run(lp, scale_log2, -m_ref, l_run, J + 1, next);
+      l_run = run.l_run;
+      J = run.J;
+      flags = run.d.flags;
+      ok = run.ok;
+      next = await_desc(lp, J + 1);
     }
-    if ((flags & kTileEnd) || *abort_flag) break;
+    // the slots of unit n - 2 are free: the epilogue warps read them before they let go of that unit's O, which the
+    // first P V of unit n - 1 waited for
+    stats.sums(n)[g * kTile + r] = l_run;
+    if (g == 0) stats.refs(n)[r] = m_ref;
+    if (!(l_run < kFastSumLimit)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));   // true for inf and NaN too
+    mbar_arrive(bar.stats_full + (n & 1));
+    if ((flags & kTileEnd) || !ok) break;
+    d = next;
+    ++J;
   }
 }
 
@@ -532,18 +636,19 @@ __device__ __noinline__ void sparse_careful_unit(const SparseCta<D>& c, const Sp
 // ---------------------------------------------------------------------------------- kernel
 // grid.x CTAs share the units (at most kFwdMaxUnits each): CTA i takes units i, i + grid.x, ...
 template <int D>
-__global__ void __launch_bounds__(kFwdThreads, 1)
+__global__ void __launch_bounds__(kSparseThreads, 1)
 sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_constant__ SparseFwdArgs a,
                        const __grid_constant__ SparseGeom g, const __grid_constant__ SparseUnits units_in) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = align_1024(smem_raw);
   uint64_t* bar_mem = reinterpret_cast<uint64_t*>(smem + SparseFwdSmem<D>::kBars);
   const SparseBars bar(bar_mem);
-  uint64_t* careful_bars = bar_mem + kFwdBarSlots;
+  uint64_t* careful_bars = bar_mem + kSparseBarSlots;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bar_mem + 48);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr uint32_t kTmemCols = 512;
-  constexpr int kMmaWarp = 4 * kFwdGroups, kTmaWarp = 4 * kFwdGroups + 1;
+  constexpr int kMmaWarp = 4 * kFwdGroups, kTmaWarp = 4 * kFwdGroups + 1;   // kTmaWarp: lists
+  constexpr int kKWarp = kSparseThreads / 32 - 2, kVWarp = kSparseThreads / 32 - 1;
 
   SparseCta<D> c;
   c.sK = smem + SparseFwdSmem<D>::kK;
@@ -564,8 +669,8 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
     fence_mbar_init();
   }
   if (tid < kFwdMaxUnits / 32) c.redo[tid] = 0;
-  zero_uncovered_rows<D>(c.sK, kFwdKStages, g, tid, kFwdThreads);
-  zero_uncovered_rows<D>(c.sV, kFwdVStages, g, tid, kFwdThreads);
+  zero_uncovered_rows<D>(c.sK, kFwdKStages, g, tid, kSparseThreads);
+  zero_uncovered_rows<D>(c.sV, kFwdVStages, g, tid, kSparseThreads);
   fence_proxy_async_smem();
   if (warp == kMmaWarp) {
     tmem_alloc(tmem_holder, kTmemCols);
@@ -577,7 +682,9 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
   c.tmem_base = *tmem_holder;
 
   if (!a.careful) {
-    if (warp == kTmaWarp) sparse_produce<D>(c, g, s, a, maps, bar, lane);
+    if (warp == kTmaWarp) sparse_walk<D>(c, g, s, a, bar, lane);
+    else if (warp == kKWarp) { if (lane == 0) sparse_load_k<D>(c, g, maps, bar); }
+    else if (warp == kVWarp) { if (lane == 0) sparse_load_v<D>(c, g, maps, bar); }
     else if (warp == kMmaWarp) { if (lane == 0) sparse_issue<D>(c, bar); }
     else if (warp < kMmaWarp) sparse_softmax<D>(c, bar, warp, tid & 127, a.scale_log2);
     else sparse_epilogue<D>(c, s, a, bar, warp, lane);
