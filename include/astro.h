@@ -284,6 +284,19 @@ astro_status_t astro_sparse_attn_fwd(const astro_kvcache_t* cache, const void* q
                                      int head_dim, int n_q, int n_kc, float scale, void* o, float* lse, void* workspace,
                                      size_t workspace_bytes, void* stream);
 
+/* Its backward, the cached context detached as in astro_chunk_attn_bwd: from dO and the forward's O and LSE (same lists),
+ * dQ over the listed keys, dK and dV of the chunk's own tokens.  A query without a key has dQ = 0; a chunk block that no
+ * list names has dK = dV = 0; a block named twice counts twice here too.  All sums have one fixed order: the same call
+ * gives the same bits.  Other arguments as for astro_chunk_attn_bwd; workspace: device scratch, 16-byte aligned, at least
+ * astro_sparse_attn_bwd_workspace_bytes(). */
+size_t astro_sparse_attn_bwd_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_kc, int n_select,
+                                             int block_tokens);
+astro_status_t astro_sparse_attn_bwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
+                                     const int32_t* blocks, int n_select, int block_tokens, const void* o, const float* lse,
+                                     const void* d_o, int batch, int heads, int head_dim, int n_q, int n_kc, float scale,
+                                     void* dq, void* dk_chunk, void* dv_chunk, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
 /* Eq. 1, Eq. 2 and the selective KL term of Sec. 3.4 (Algorithm 2, "Policy loss on window"), fused with
  * the gradient for the current policy, over the velocity tensors of the active window:
  *   v+ = (1-beta) v_old + beta v_theta;  v- = (1+beta) v_old - beta v_theta;

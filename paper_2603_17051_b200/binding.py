@@ -24,7 +24,7 @@ EXPORTED = ("astro_kvcache_key_segments", "astro_selftest_wait_timeout", "astro_
             "astro_last_device_status", "astro_status_string", "astro_kvcache_fork", "astro_rope_create",
             "astro_rope_destroy", "astro_rope_frequencies", "astro_rope_apply", "astro_block_count", "astro_block_pool",
             "astro_block_select_workspace_bytes", "astro_block_select", "astro_sparse_attn_fwd_workspace_bytes",
-            "astro_sparse_attn_fwd")
+            "astro_sparse_attn_fwd", "astro_sparse_attn_bwd_workspace_bytes", "astro_sparse_attn_bwd")
 
 
 class AstroError(RuntimeError):
@@ -127,6 +127,10 @@ def lib():
     L.astro_sparse_attn_fwd_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
     L.astro_sparse_attn_fwd.restype = ci
     L.astro_sparse_attn_fwd.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp, vp, vp, sz, vp]
+    L.astro_sparse_attn_bwd_workspace_bytes.restype = sz
+    L.astro_sparse_attn_bwd_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci, ci]
+    L.astro_sparse_attn_bwd.restype = ci
+    L.astro_sparse_attn_bwd.argtypes = [vp, vp, vp, vp, vp, ci, ci, vp, vp, vp, ci, ci, ci, ci, ci, cf, vp, vp, vp, vp, sz, vp]
     L.astro_debug_forward_mode.restype = ci
     L.astro_debug_forward_mode.argtypes = [ci]
     L.astro_debug_pair_flag.restype = ci
@@ -642,6 +646,43 @@ def astro_sparse_attn_fwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
                                      _stream(stream))
     _check(st, "astro_sparse_attn_fwd")
     return o, lse
+
+
+def astro_sparse_attn_bwd_workspace_bytes(batch, heads, head_dim, n_q, n_kc, n_select, block_tokens) -> int:
+    return int(lib().astro_sparse_attn_bwd_workspace_bytes(int(batch), int(heads), int(head_dim), int(n_q), int(n_kc),
+                                                           int(n_select), int(block_tokens)))
+
+
+def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int, o, lse, d_o, scale: float, dq=None, dk_chunk=None,
+                          dv_chunk=None, workspace=None, stream=None):
+    """Returns (dQ, dK_chunk, dV_chunk), bf16, of astro_sparse_attn_fwd with the same lists; the cached context receives no
+    gradient."""
+    import torch
+    B, n_q, H, D = q.shape
+    n_kc, n_select = _chunk_shape(q, k_chunk, v_chunk), _lists_shape(q, blocks)
+    fresh = []
+    if dq is None:
+        dq = torch.empty_like(q); fresh.append(dq)
+    if n_kc and dk_chunk is None:
+        dk_chunk = torch.empty_like(k_chunk); fresh.append(dk_chunk)
+    if n_kc and dv_chunk is None:
+        dv_chunk = torch.empty_like(v_chunk); fresh.append(dv_chunk)
+    if workspace is None:
+        need = astro_sparse_attn_bwd_workspace_bytes(B, H, D, n_q, n_kc, n_select, block_tokens)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _typed("int32", blocks)
+    _typed("float32", lse)
+    _typed("bfloat16", q, k_chunk, v_chunk, o, d_o, dq, dk_chunk, dv_chunk)
+    _contiguous(q, k_chunk, v_chunk, blocks, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace)
+    _here(stream, q, k_chunk, v_chunk, blocks, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, None if cache is None else cache.k_storage)
+    _sized((o, q.numel()), (d_o, q.numel()), (dq, q.numel()), (lse, B * H * n_q), (dk_chunk, B * n_kc * H * D), (dv_chunk, B * n_kc * H * D))
+    _used_on(stream, *fresh)
+    st = lib().astro_sparse_attn_bwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk), _ptr(blocks),
+                                     n_select, int(block_tokens), _ptr(o), _ptr(lse), _ptr(d_o), B, H, D, n_q, n_kc, float(scale),
+                                     _ptr(dq), _ptr(dk_chunk), _ptr(dv_chunk), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "astro_sparse_attn_bwd")
+    return dq, dk_chunk, dv_chunk
 
 
 def astro_nft_loss(v_theta, v_old, v_ref, v_target, r_tilde, beta: float, w_policy=None, w_kl=None, grad=True,

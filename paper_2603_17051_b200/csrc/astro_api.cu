@@ -18,6 +18,7 @@
 #include "kv_ring.cuh"
 #include "nft_loss.cuh"
 #include "rope.cuh"
+#include "sparse_bwd.cuh"
 #include "sparse_fwd.cuh"
 
 using namespace astro;
@@ -576,6 +577,68 @@ astro_status_t launch_sparse_fwd(const SparseCall& c, const SparseGeom& g, float
   if ((s = launch_status()) != ASTRO_OK || split.splits == 1) return s;
   sparse_combine_kernel<D><<<static_cast<unsigned>((rows + 7) / 8), 256, 0, st>>>(a.part_o, a.part_lse, split.splits, rows, c.a.n_q,
                                                                              c.a.heads, a.o, lse);
+  return launch_status();
+}
+
+// Scratch of the backward: delta, then how often every query tile names every chunk block.
+struct SparseBwdScratch {
+  size_t delta, counts;   // bytes
+};
+SparseBwdScratch sparse_bwd_scratch(int batch, int heads, int n_q, int n_kc, int block_tokens) {
+  const size_t q_tiles = (n_q - 1) / kTile + 1, blocks = (static_cast<size_t>(n_kc) + block_tokens - 1) / block_tokens;
+  SparseBwdScratch s;
+  s.delta = (static_cast<size_t>(batch) * heads * n_q * sizeof(float) + 255) & ~static_cast<size_t>(255);
+  s.counts = static_cast<size_t>(batch) * heads * blocks * q_tiles * sizeof(int);
+  return s;
+}
+
+template <int D>
+astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float scale, const void* o, const float* lse,
+                                 const void* d_o, void* dq, void* dk, void* dv, void* workspace, cudaStream_t st) {
+  SparseMaps maps;
+  astro_status_t s = sparse_maps(c, g, &maps);
+  if (s != ASTRO_OK) return s;
+  CUtensorMap tq, tdo;
+  if ((s = make_tmap_user(&tq, c.q, D, c.a.n_q, c.a.heads, c.a.batch)) != ASTRO_OK) return s;
+  if ((s = make_tmap_user(&tdo, d_o, D, c.a.n_q, c.a.heads, c.a.batch)) != ASTRO_OK) return s;
+  static std::atomic<int> done_q[kMaxDevices], done_kv[kMaxDevices];
+  if ((s = set_smem_once(sparse_attn_bwd_dq_kernel<D>, SdqSmem<D>::kTotal, done_q)) != ASTRO_OK) return s;
+  if ((s = set_smem_once(sparse_attn_bwd_dkv_kernel<D>, DkvSmem<D>::kTotal, done_kv)) != ASTRO_OK) return s;
+  const SparseBwdScratch need = sparse_bwd_scratch(c.a.batch, c.a.heads, c.a.n_q, c.a.n_kc, c.block_tokens);
+  float* delta = static_cast<float*>(workspace);
+  int* counts = reinterpret_cast<int*>(static_cast<char*>(workspace) + need.delta);
+  const int q_tiles = (c.a.n_q - 1) / kTile + 1, chunk_blocks = g.kb.total - g.kb.ctx;
+  if ((s = launch_bwd_delta<D>(o, d_o, c.a.batch, c.a.heads, c.a.n_q, delta, st)) != ASTRO_OK) return s;
+  SparseBwdArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(c.q);
+  a.blocks = c.blocks;
+  a.lse = lse;
+  a.delta = delta;
+  a.batch = c.a.batch; a.heads = c.a.heads; a.n_q = c.a.n_q;
+  a.q_tiles = q_tiles;
+  a.n_select = c.n_select;
+  a.cache_shared = (c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1) ? 1 : 0;
+  a.scale = scale;
+  dim3 grid_q(q_tiles, a.cache_shared ? c.a.batch : c.a.heads, a.cache_shared ? c.a.heads : c.a.batch);
+  sparse_attn_bwd_dq_kernel<D><<<grid_q, kSdqThreads, SdqSmem<D>::kTotal, st>>>(maps, tdo, g, a, static_cast<__nv_bfloat16*>(dq));
+  if ((s = launch_status()) != ASTRO_OK || chunk_blocks == 0) return s;
+  if (cudaMemsetAsync(counts, 0, need.counts, st) != cudaSuccess) return ASTRO_ERR_CUDA;
+  const long long entries = static_cast<long long>(c.a.batch) * c.a.heads * q_tiles * c.n_select;
+  sparse_count_kernel<<<static_cast<unsigned>((entries + 255) / 256), 256, 0, st>>>(c.blocks, counts, entries, c.n_select, q_tiles,
+                                                                               g.kb.ctx, chunk_blocks);
+  if ((s = launch_status()) != ASTRO_OK) return s;
+  SparseDkvArgs k;
+  k.counts = counts;
+  k.lse = lse;
+  k.delta = delta;
+  k.heads = c.a.heads; k.n_q = c.a.n_q; k.n_kc = c.a.n_kc;
+  k.q_tiles = q_tiles;
+  k.block = c.block_tokens;
+  k.chunk_blocks = chunk_blocks;
+  k.scale = scale;
+  dim3 grid_k(chunk_blocks, c.a.heads, c.a.batch);
+  sparse_attn_bwd_dkv_kernel<D><<<grid_k, kDkvThreads, DkvSmem<D>::kTotal, st>>>(
+      tq, tdo, maps.kc, maps.vc, k, static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv));
   return launch_status();
 }
 
@@ -1167,6 +1230,41 @@ astro_status_t astro_sparse_attn_fwd(const astro_kvcache_t* cache, const void* q
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return head_dim == 128 ? launch_sparse_fwd<128>(c, g, scale, o, lse, workspace, st)
                          : launch_sparse_fwd<64>(c, g, scale, o, lse, workspace, st);
+}
+
+size_t astro_sparse_attn_bwd_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_kc, int n_select,
+                                             int block_tokens) {
+  if (batch < 1 || heads < 1 || n_q < 1 || n_kc < 0 || n_select < 1 || (head_dim != 64 && head_dim != 128) ||
+      !block_tokens_ok(block_tokens))
+    return 0;
+  const SparseBwdScratch s = sparse_bwd_scratch(batch, heads, n_q, n_kc, block_tokens);
+  return s.delta + s.counts;
+}
+
+astro_status_t astro_sparse_attn_bwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
+                                     const int32_t* blocks, int n_select, int block_tokens, const void* o, const float* lse,
+                                     const void* d_o, int batch, int heads, int head_dim, int n_q, int n_kc, float scale,
+                                     void* dq, void* dk_chunk, void* dv_chunk, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  if (!q || !blocks || !o || !lse || !d_o || !dq || !workspace) return ASTRO_ERR_NULL;
+  if (n_kc > 0 && (!k_chunk || !v_chunk || !dk_chunk || !dv_chunk)) return ASTRO_ERR_NULL;
+  const SparseCall c{{cache, batch, heads, head_dim, n_q, n_kc}, q, k_chunk, v_chunk, blocks, n_select, block_tokens};
+  SparseGeom g;
+  astro_status_t s = check_sparse(c, scale, &g);
+  if (s != ASTRO_OK) return s;
+  const long long q_tiles = (n_q - 1) / kTile + 1;
+  // the tiles of a block are counted in 32 bits, the grid of the entries too
+  if (q_tiles * n_select > 0x3fffffffLL || q_tiles * n_select * heads > 0x7fffffffLL * 256 / batch) return ASTRO_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(o) || !aligned16(d_o) || !aligned16(dq) || !aligned16(workspace) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(blocks) & 3u) ||
+      (n_kc > 0 && (!aligned16(k_chunk) || !aligned16(v_chunk) || !aligned16(dk_chunk) || !aligned16(dv_chunk))))
+    return ASTRO_ERR_ALIGN;
+  if (workspace_bytes < astro_sparse_attn_bwd_workspace_bytes(batch, heads, head_dim, n_q, n_kc, n_select, block_tokens))
+    return ASTRO_ERR_CAPACITY;
+  if ((s = check_arch()) != ASTRO_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return head_dim == 128 ? launch_sparse_bwd<128>(c, g, scale, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, st)
+                         : launch_sparse_bwd<64>(c, g, scale, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, st);
 }
 
 astro_status_t astro_nft_loss(const void* v_theta, const void* v_old, const void* v_ref, const void* v_target,
