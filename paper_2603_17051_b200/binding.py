@@ -172,22 +172,30 @@ def _contiguous(*tensors):
 
 def _typed(kind, *tensors):
     """Index and statistics tensors are read as the type their name says."""
-    import torch
     for t in tensors:
-        if t is not None and t.dtype != getattr(torch, kind):
+        if t is not None and t.dtype is not kind:
             raise ValueError("expected a %s tensor, got %s" % (kind, t.dtype))
 
 
 def _here(stream, *tensors):
-    """Kernels run on the current device (or the given stream's, which must be the same one): a tensor that lives
-    elsewhere, on the host included, is refused before its address reaches one."""
+    """Kernels run on the current device (and a given stream must belong to it): a tensor that lives elsewhere, on the
+    host included, is refused before its address reaches one.  Returns the stream's address."""
     import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
-    if stream is not None and stream.device.index != dev:
-        raise ValueError("the stream belongs to another device than the current one")
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise ValueError("tensor on %s, the current device is %s" % (t.device, dev))
+        if t is not None and (t.get_device() != dev or dev < 0):
+            raise ValueError("tensors on different devices, or on the host: %s" % [str(x.device) for x in tensors if x is not None])
+    if dev != torch.cuda.current_device():
+        raise ValueError("tensors on %s, the current device is %d" % (tensors[0].device, torch.cuda.current_device()))
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device.index != dev:
+        raise ValueError("the stream belongs to another device than the current one")
+    return stream.cuda_stream
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _chunk_shape(q, *chunk):
@@ -426,16 +434,17 @@ def astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, scale: float,
 def astro_kvcache_fork(dst: KVCache, src: KVCache, parents=None, frames=None, stream=None) -> None:
     """Empty `dst` and copy the listed held frames of `src` (logical indices, None = all) into it; parents: int32 [dst
     cache_batch] on the device, the sample of src that each sample of dst continues."""
-    _typed("int32", parents)
+    import torch
+    _typed(torch.int32, parents)
     _contiguous(parents)
-    _here(stream, parents, dst.k_storage, dst.v_storage, src.k_storage, src.v_storage)
+    st = _here(stream, dst.k_storage, dst.v_storage, src.k_storage, src.v_storage, parents)
     if parents is not None and parents.numel() != dst.desc.cache_batch:
         raise ValueError("parents must hold one entry per sample of the destination")
     if frames is None:
         arr, n = None, -1
     else:
         arr, n = (C.c_int * max(1, len(frames)))(*[int(f) for f in frames]), len(frames)
-    _check(lib().astro_kvcache_fork(dst.handle, src.handle, _ptr(parents), arr, n, _stream(stream)), "astro_kvcache_fork")
+    _check(lib().astro_kvcache_fork(dst.handle, src.handle, _at(parents), arr, n, st), "astro_kvcache_fork")
 
 
 ROPE_LAYOUTS = {"interleaved": 0, "halves": 1}
@@ -491,42 +500,70 @@ def _rope_strides(t):
     return tuple(s if size > 1 else d for s, size, d in zip(t.stride(), (B, n, H), dense))
 
 
+def _dense_like(t):
+    import torch
+    # empty_like keeps the strides of a dense tensor, and is the cheaper of the two where they are the contiguous ones
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+_ROPE_TYPES = {}
+
+
 def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """Rotate q [B, n, H, D] and k (same type; other head count allowed; None: q alone) by their tokens' positions, int32
     [B or 1, n, axes] on the device.  Inputs and outputs may be strided as long as a head's elements are contiguous;
     q_out = q and k_out = k rotate in place.  inverse=True turns back: the gradient of q and k from that of the outputs."""
     import torch
-    kinds = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    if not _ROPE_TYPES:
+        _ROPE_TYPES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+    kind = _ROPE_TYPES.get(q.dtype)
+    if kind is None:
+        raise ValueError("q and k must be bf16, fp16 or fp32")
+    shape = q.shape
+    if len(shape) != 4 or shape[3] != rope.desc.head_dim:
+        raise ValueError("q must be [B, n, heads, head_dim]")
+    B, n, H, _ = shape
     fresh = []
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device); fresh.append(q_out)
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device); fresh.append(k_out)
-    pairs = [(x, y) for x, y in ((q, q_out), (k, k_out)) if x is not None]
-    B, n, _, D = q.shape
-    for x, y in pairs:
-        if x.dim() != 4 or x.shape != y.shape or x.dtype != y.dtype or x.dtype != q.dtype or x.shape[:2] != q.shape[:2] or \
-                x.shape[3] != rope.desc.head_dim:
-            raise ValueError("q, k and their outputs must be [B, n, heads, head_dim] of one type")
-        if n and (x.stride(3) != 1 or y.stride(3) != 1):
-            raise ValueError("the elements of a head must be contiguous")
-    if q.dtype not in kinds:
-        raise ValueError("q and k must be bf16, fp16 or fp32")
-    _typed("int32", positions)
+        q_out = _dense_like(q); fresh.append(q_out)
+    elif q_out.shape != shape or q_out.dtype is not q.dtype:
+        raise ValueError("q_out must be like q")
+    if k is not None:
+        if k.dim() != 4 or k.dtype is not q.dtype or k.shape[0] != B or k.shape[1] != n or k.shape[3] != shape[3]:
+            raise ValueError("k must be [B, n, heads, head_dim] of q's type")
+        if k_out is None:
+            k_out = _dense_like(k); fresh.append(k_out)
+        elif k_out.shape != k.shape or k_out.dtype is not k.dtype:
+            raise ValueError("k_out must be like k")
+    else:
+        k_out = None
+    _typed(torch.int32, positions)
     _contiguous(positions)
-    _here(stream, q, k, q_out, k_out, positions)
-    if tuple(positions.shape) not in {(B, n, rope.desc.axes), (1, n, rope.desc.axes)}:
+    pb = positions.shape[0]
+    if tuple(positions.shape) != (pb, n, rope.desc.axes) or (pb != 1 and pb != B):
         raise ValueError("positions must be [B or 1, n, axes]")
+    on = _here(stream, q, positions, q_out, k, k_out)
     _used_on(stream, *fresh)
+
+    def call(x, x2, y, y2, strides):
+        _check(lib().astro_rope_apply(rope.handle, 1 if inverse else 0, _at(x), _at(x2), _at(positions), pb, B, n, x.shape[2],
+                                      0 if x2 is None else x2.shape[2], kind, None if strides is None else C.byref(Strides(*strides[0])),
+                                      _at(y), _at(y2), None if strides is None else C.byref(Strides(*strides[1])), on),
+               "astro_rope_apply")
+
+    dense = q.is_contiguous() and q_out.is_contiguous()
+    if dense and (k is None or (k.shape == shape and k.is_contiguous() and k_out.is_contiguous())):
+        call(q, k, q_out, k_out, None)
+        return q_out, k_out
+    pairs = [(x, y) for x, y in ((q, q_out), (k, k_out)) if x is not None]
+    if n and any(z.stride(3) != 1 for pair in pairs for z in pair):
+        raise ValueError("the elements of a head must be contiguous")
     layouts = [(_rope_strides(x), _rope_strides(y)) for x, y in pairs]
-    # one launch for q and k; two where their strides differ
-    together = len(pairs) == 2 and layouts[0] == layouts[1]
-    calls = [(q, k, q_out, k_out, layouts[0])] if together else [(x, None, y, None, l) for (x, y), l in zip(pairs, layouts)]
-    for x, x2, y, y2, (si, so) in calls:
-        st = lib().astro_rope_apply(rope.handle, int(bool(inverse)), _ptr(x), _ptr(x2), _ptr(positions), positions.shape[0], B, n,
-                                    x.shape[2], 0 if x2 is None else x2.shape[2], kinds[q.dtype], C.byref(Strides(*si)),
-                                    _ptr(y), _ptr(y2), C.byref(Strides(*so)), _stream(stream))
-        _check(st, "astro_rope_apply")
+    if len(pairs) == 2 and layouts[0] == layouts[1]:   # one launch for q and k; two where their strides differ
+        call(q, k, q_out, k_out, layouts[0])
+    else:
+        for (x, y), layout in zip(pairs, layouts):
+            call(x, None, y, None, layout)
     return q_out, k_out
 
 
@@ -559,12 +596,12 @@ def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_
             raise AstroError(2, "astro_block_pool")
         pooled = torch.zeros(_pooled_shape(cache, block_tokens), dtype=torch.float32, device=cache.k_storage.device)
         _used_on(stream, pooled)
-    _typed("float32", pooled)
+    _typed(torch.float32, pooled)
     _contiguous(pooled)
-    _here(stream, pooled, cache.k_storage)
+    st = _here(stream, pooled, cache.k_storage)
     if int(block_tokens) >= 1 and pooled.numel() != _numel(_pooled_shape(cache, block_tokens)):
         raise ValueError("pooled must be [B_c, H, S+L, blocks per frame, D]")
-    _check(lib().astro_block_pool(cache.handle, int(first_frame), int(n_frames), int(block_tokens), _ptr(pooled), _stream(stream)),
+    _check(lib().astro_block_pool(cache.handle, int(first_frame), int(n_frames), int(block_tokens), _at(pooled), st),
            "astro_block_pool")
     return pooled
 
@@ -583,23 +620,23 @@ def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: i
     shape = (B, H, -(-n_q // QUERY_BLOCK), max(1, int(n_select)))
     fresh = []
     if blocks is None:
-        blocks = torch.empty(shape, dtype=torch.int32, device=q.device); fresh.append(blocks)
+        blocks = q.new_empty(shape, dtype=torch.int32); fresh.append(blocks)
     if workspace is None:
         need = astro_block_select_workspace_bytes(B, H, D, n_q, n_kc, block_tokens)
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _typed("int32", blocks)
-    _typed("float32", pooled)
-    _typed("bfloat16", q, k_chunk)
+    _typed(torch.int32, blocks)
+    _typed(torch.float32, pooled)
+    _typed(torch.bfloat16, q, k_chunk)
     _contiguous(q, k_chunk, blocks, pooled, workspace)
-    _here(stream, q, k_chunk, blocks, pooled, workspace, None if cache is None else cache.k_storage)
+    on = _here(stream, q, k_chunk, blocks, pooled, workspace, None if cache is None else cache.k_storage)
     if blocks.numel() != _numel(shape):
         raise ValueError("blocks must be [B, H, query blocks, n_select]")
     if cache is not None and pooled is not None and int(block_tokens) >= 1 and pooled.numel() != _numel(_pooled_shape(cache, block_tokens)):
         raise ValueError("pooled must be [B_c, H, S+L, blocks per frame, D]")
     _used_on(stream, *fresh)
-    st = lib().astro_block_select(None if cache is None else cache.handle, _ptr(pooled), _ptr(q), _ptr(k_chunk), B, H, D, n_q,
-                                  n_kc, int(block_tokens), int(n_select), int(keep), _ptr(blocks), _ptr(workspace),
-                                  workspace.numel() * workspace.element_size(), _stream(stream))
+    st = lib().astro_block_select(None if cache is None else cache.handle, _at(pooled), _at(q), _at(k_chunk), B, H, D, n_q,
+                                  n_kc, int(block_tokens), int(n_select), int(keep), _at(blocks), _at(workspace),
+                                  workspace.numel() * workspace.element_size(), on)
     _check(st, "astro_block_select")
     return blocks
 
@@ -629,21 +666,21 @@ def astro_sparse_attn_fwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
     if o is None:
         o = torch.empty_like(q); fresh.append(o)
     if lse is None:
-        lse = torch.empty((B, H, n_q), dtype=torch.float32, device=q.device); fresh.append(lse)
+        lse = q.new_empty((B, H, n_q), dtype=torch.float32); fresh.append(lse)
     need = astro_sparse_attn_fwd_workspace_bytes(B, H, D, n_q, n_select, block_tokens)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _typed("int32", blocks)
-    _typed("float32", lse)
-    _typed("bfloat16", q, k_chunk, v_chunk, o)
+    _typed(torch.int32, blocks)
+    _typed(torch.float32, lse)
+    _typed(torch.bfloat16, q, k_chunk, v_chunk, o)
     _contiguous(q, k_chunk, v_chunk, blocks, o, lse, workspace)
-    _here(stream, q, k_chunk, v_chunk, blocks, o, lse, workspace, None if cache is None else cache.k_storage)
+    on = _here(stream, q, k_chunk, v_chunk, blocks, o, lse, workspace, None if cache is None else cache.k_storage)
     _sized((o, q.numel()), (lse, B * H * n_q))
     _used_on(stream, *fresh)
-    st = lib().astro_sparse_attn_fwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk), _ptr(blocks),
-                                     n_select, int(block_tokens), B, H, D, n_q, n_kc, float(scale), _ptr(o), _ptr(lse),
-                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                     _stream(stream))
+    st = lib().astro_sparse_attn_fwd(None if cache is None else cache.handle, _at(q), _at(k_chunk), _at(v_chunk), _at(blocks),
+                                     n_select, int(block_tokens), B, H, D, n_q, n_kc, float(scale), _at(o), _at(lse),
+                                     _at(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                     on)
     _check(st, "astro_sparse_attn_fwd")
     return o, lse
 
@@ -670,17 +707,17 @@ def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
     if workspace is None:
         need = astro_sparse_attn_bwd_workspace_bytes(B, H, D, n_q, n_kc, n_select, block_tokens)
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _typed("int32", blocks)
-    _typed("float32", lse)
-    _typed("bfloat16", q, k_chunk, v_chunk, o, d_o, dq, dk_chunk, dv_chunk)
+    _typed(torch.int32, blocks)
+    _typed(torch.float32, lse)
+    _typed(torch.bfloat16, q, k_chunk, v_chunk, o, d_o, dq, dk_chunk, dv_chunk)
     _contiguous(q, k_chunk, v_chunk, blocks, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace)
-    _here(stream, q, k_chunk, v_chunk, blocks, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, None if cache is None else cache.k_storage)
+    on = _here(stream, q, k_chunk, v_chunk, blocks, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, None if cache is None else cache.k_storage)
     _sized((o, q.numel()), (d_o, q.numel()), (dq, q.numel()), (lse, B * H * n_q), (dk_chunk, B * n_kc * H * D), (dv_chunk, B * n_kc * H * D))
     _used_on(stream, *fresh)
-    st = lib().astro_sparse_attn_bwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk), _ptr(blocks),
-                                     n_select, int(block_tokens), _ptr(o), _ptr(lse), _ptr(d_o), B, H, D, n_q, n_kc, float(scale),
-                                     _ptr(dq), _ptr(dk_chunk), _ptr(dv_chunk), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(), _stream(stream))
+    st = lib().astro_sparse_attn_bwd(None if cache is None else cache.handle, _at(q), _at(k_chunk), _at(v_chunk), _at(blocks),
+                                     n_select, int(block_tokens), _at(o), _at(lse), _at(d_o), B, H, D, n_q, n_kc, float(scale),
+                                     _at(dq), _at(dk_chunk), _at(dv_chunk), _at(workspace),
+                                     workspace.numel() * workspace.element_size(), on)
     _check(st, "astro_sparse_attn_bwd")
     return dq, dk_chunk, dv_chunk
 

@@ -380,20 +380,18 @@ bool overlaps_itself(const long long (&size)[3], const long long (&stride)[3], l
 template <typename T, int MODE>
 astro_status_t launch_rope(const astro_rope* rope, const RopeTensors& x, const int* positions, int per_sample, int n_tokens,
                            int total_tokens, float sign, cudaStream_t st) {
-  const int items = (x.heads_q + x.heads_k) * rope_items_per_row(MODE, rope->d.head_dim, rope->d.rot_dim, RopeVec<T>::kElems);
-  const int sms = sm_count();
+  const int per_row = rope_items_per_row(MODE, rope->d.head_dim, rope->d.rot_dim, RopeVec<T>::kElems);
+  const int rows = x.heads_q + x.heads_k, sms = sm_count();
   if (sms <= 0) return ASTRO_ERR_CUDA;
-  // a token's items side by side in whole warps, several tokens side by side when a token has few
-  const int passes = (items + kRopeMaxThreads - 1) / kRopeMaxThreads;
-  const int width = ((items + passes - 1) / passes + 31) / 32 * 32;
-  const int lanes = kRopeMaxThreads / 2 / width > 1 ? kRopeMaxThreads / 2 / width : 1;
-  // tokens of a block: enough for kRopeUnroll loads in flight per thread, fewer while that leaves SMs without a block
-  int tokens = lanes * kRopeUnroll < kRopeMaxTokens ? lanes * kRopeUnroll : kRopeMaxTokens;
-  while (tokens > 1 && (total_tokens + tokens - 1) / tokens < 2 * sms) tokens /= 2;
-  const dim3 threads(width, lanes < tokens ? lanes : tokens);
-  const size_t smem = sizeof(float2) * tokens * rope->table.pairs;   // at most 32 KB
-  rope_kernel<T, MODE><<<(total_tokens + tokens - 1) / tokens, threads, smem, st>>>(
-      rope->table, x, positions, per_sample, n_tokens, total_tokens, rope->d.head_dim, rope->d.rot_dim, tokens, sign);
+  // as many row phases as bring every SM about 512 threads, each phase with a row at least (chunk of 4680
+  // tokens: 12.1 us, with 1024 threads 15.7, more angles and a second wave of blocks)
+  const long long threads = static_cast<long long>(total_tokens) * per_row;
+  long long phases = (sms * 512ll + threads - 1) / threads;
+  if (phases > rows) phases = rows;
+  const long long blocks = (threads * phases + kRopeThreads - 1) / kRopeThreads;
+  if (blocks > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
+  rope_kernel<T, MODE><<<static_cast<unsigned>(blocks), kRopeThreads, 0, st>>>(
+      rope->table, x, positions, per_sample, n_tokens, total_tokens, rope->d.head_dim, rope->d.rot_dim, static_cast<int>(phases), sign);
   return launch_status();
 }
 
@@ -434,16 +432,6 @@ bool build_key_blocks(const astro_kvcache* c, int n_kc, int block, KeyBlocks* ou
   return true;
 }
 
-template <int D, int R>
-astro_status_t launch_select(const SelectArgs& a, const KeyBlocks& kb, int batch, cudaStream_t st) {
-  static std::atomic<int> done[kMaxDevices];
-  astro_status_t s = set_smem_once(block_select_kernel<D, R>, ASTRO_SELECT_MAX_BLOCKS * 8, done);
-  if (s != ASTRO_OK) return s;
-  dim3 grid((a.q_blocks + R - 1) / R, a.heads, batch);
-  block_select_kernel<D, R><<<grid, kSelectThreads, static_cast<size_t>(R) * kb.total * 8, st>>>(a, kb);
-  return launch_status();
-}
-
 template <int D>
 astro_status_t launch_select_all(const PoolSource& q, const PoolSource& kc, SelectArgs a, const KeyBlocks& kb, int batch,
                                  cudaStream_t st) {
@@ -451,13 +439,14 @@ astro_status_t launch_select_all(const PoolSource& q, const PoolSource& kc, Sele
   block_pool_kernel<D><<<grid, kPoolThreads, 0, st>>>(q, kc, q.blocks, kb, 0, 0);
   astro_status_t s = launch_status();
   if (s != ASTRO_OK) return s;
-  // four query blocks share a reading of the key means when there are enough of them to fill the GPU and their keys fit
-  // into shared memory
-  const int sms = sm_count();
-  if (sms <= 0) return ASTRO_ERR_CUDA;
-  const bool four = 4ll * kb.total <= ASTRO_SELECT_MAX_BLOCKS &&
-                    static_cast<long long>((a.q_blocks + 3) / 4) * a.heads * batch * 2 >= sms;
-  return four ? launch_select<D, 4>(a, kb, batch, st) : launch_select<D, 1>(a, kb, batch, st);
+  static std::atomic<int> done[kMaxDevices];
+  if ((s = set_smem_once(block_select_kernel<D>, ASTRO_SELECT_MAX_BLOCKS * 8, done)) != ASTRO_OK) return s;
+  // as many of a tile's eight query blocks as have room for their keys in shared memory
+  const int most = ASTRO_SELECT_MAX_BLOCKS / kb.total;
+  a.rows = most < kSelectRows ? most : kSelectRows;
+  dim3 tiles((a.q_blocks + a.rows - 1) / a.rows, a.heads, batch);
+  block_select_kernel<D><<<tiles, kSelectThreads, static_cast<size_t>(a.rows) * kb.total * 8, st>>>(a, kb);
+  return launch_status();
 }
 
 // ---- attention over lists of key blocks ---------------------------------------------------------------------
@@ -1062,7 +1051,7 @@ astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const voi
     return ASTRO_ERR_SHAPE;
   if (dtype != ASTRO_BF16 && dtype != ASTRO_F16 && dtype != ASTRO_F32) return ASTRO_ERR_SHAPE;
   if (inverse != 0 && inverse != 1) return ASTRO_ERR_SHAPE;
-  if (static_cast<long long>(batch) * n_tokens > 0x7fffffffLL - kRopeMaxTokens || heads_q > 65535 || (k && heads_k > 65535))
+  if (static_cast<long long>(batch) * n_tokens > 0x7fffffffLL || heads_q > 65535 || (k && heads_k > 65535))
     return ASTRO_ERR_SHAPE;
   if (n_tokens == 0) return ASTRO_OK;
   if (!q || !q_out || !positions) return ASTRO_ERR_NULL;

@@ -40,15 +40,24 @@ struct PoolSource {
 
 constexpr int kPoolThreads = 256;
 
+// Sums of bf16 values in fp64 without a conversion per value (those run at a quarter of the adds' rate or less): the bits of a
+// bf16, moved to the places of an fp64's sign, exponent and mantissa, are that value times 2^-896, zeros and denormal
+// values included; the sum is scaled back once.  Infinities and NaN have no such image (`seen` collects the magnitudes so
+// that they are noticed).
+__device__ __forceinline__ void add_scaled(double& lo, double& hi, uint32_t pair) {
+  lo += __hiloint2double(static_cast<int>(((pair << 13) & 0x0fffe000u) | ((pair << 16) & 0x80000000u)), 0);
+  hi += __hiloint2double(static_cast<int>(((pair >> 3) & 0x0fffe000u) | (pair & 0x80000000u)), 0);
+}
+
 // One block of tokens of one head per thread block: D/8 threads side by side hold 8 elements each, the others walk the
-// tokens; partial sums meet in shared memory.  Bandwidth bound: every token row is read once, 16 bytes per thread.
-// grid.x = blocks of source 0, then of source 1 (n0 of the first); grid.y = head, grid.z = sample.
-// `frames` > 0: source 0 is the cache storage, and grid.x walks frames x per_frame blocks from logical frame `frame0`.
+// tokens, all of a thread's loads in flight at once; partial sums meet in shared memory.  Bandwidth bound.
+// grid.x = blocks of source 0, then of source 1 (n0 of the first); grid.y = head, grid.z = sample.  cache_source: source 0 is
+// the cache storage, and grid.x walks the blocks of the frames from logical frame `frame0` on.
 template <int D>
 __global__ void __launch_bounds__(kPoolThreads)
 block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const KeyBlocks kb, const int frame0,
                   const int cache_source) {
-  constexpr int kCols = D / 8, kRows = kPoolThreads / kCols;
+  constexpr int kCols = D / 8, kRows = kPoolThreads / kCols, kDeep = kTile / kRows;   // a block has at most kTile tokens
   const bool second = static_cast<int>(blockIdx.x) >= n0;
   const PoolSource& s = second ? s1 : s0;
   int j = second ? blockIdx.x - n0 : blockIdx.x;
@@ -63,35 +72,58 @@ block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const 
   const int count = min(s.block, s.tokens - j * s.block);
   const int col = threadIdx.x % kCols, row = threadIdx.x / kCols;
   const __nv_bfloat16* src = s.base + b * s.sb + h * s.sh + (first_row + static_cast<long long>(j) * s.block) * s.st + col * 8;
+  uint4 v[kDeep];
+#pragma unroll
+  for (int u = 0; u < kDeep; ++u) {
+    const int t = row + u * kRows;
+    v[u] = t < count ? *reinterpret_cast<const uint4*>(src + t * s.st) : make_uint4(0, 0, 0, 0);
+  }
   double acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0;
-#pragma unroll 4
-  for (int t = row; t < count; t += kRows) {
-    const uint4 v = *reinterpret_cast<const uint4*>(src + t * s.st);
-    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+  uint32_t seen = 0;
+#pragma unroll
+  for (int u = 0; u < kDeep; ++u) {
+    const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float2 f = __bfloat1622float2(p[e]);
-      acc[2 * e] += static_cast<double>(f.x);
-      acc[2 * e + 1] += static_cast<double>(f.y);
+      add_scaled(acc[2 * e], acc[2 * e + 1], w[e]);
+      seen = __vmaxu2(seen, w[e] & 0x7fff7fffu);
     }
   }
-  __shared__ double part[kRows][D + 2];
+  double unscale = ldexp(1.0, 896);
+  if ((seen & 0xffffu) >= 0x7f80u || (seen >> 16) >= 0x7f80u) {   // again with true conversions; scaled down, see below
 #pragma unroll
-  for (int e = 0; e < 8; ++e) part[row][col * 8 + e] = acc[e];
+    for (int e = 0; e < 8; ++e) acc[e] = 0.0;
+#pragma unroll
+    for (int u = 0; u < kDeep; ++u) {
+      const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v[u]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __bfloat1622float2(p[e]);
+        acc[2 * e] += static_cast<double>(f.x);
+        acc[2 * e + 1] += static_cast<double>(f.y);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= 1.0 / unscale;   // back into the others' scale; a power of two loses nothing
+  }
+  __shared__ double part[kRows][8][kCols];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) part[row][e][col] = acc[e];
   __syncthreads();
   for (int e = threadIdx.x; e < D; e += kPoolThreads) {
     double sum = 0.0;
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) sum += part[r][e];
-    s.out[((b * s.out_b + h * s.out_h) + out_row) * D + e] = static_cast<float>(sum / static_cast<double>(count));
+    for (int r = 0; r < kRows; ++r) sum += part[r][e % 8][e / 8];
+    s.out[((b * s.out_b + h * s.out_h) + out_row) * D + e] = static_cast<float>(sum * unscale / static_cast<double>(count));
   }
 }
 
 // ------------------------------------------------------------------------------------------------ choice
-constexpr int kSelectThreads = 256;
+constexpr int kSelectThreads = 512;
 constexpr int kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectRows = 8;     // query blocks of one MMA tile
 
 // A double as an unsigned integer of the same order; NaN becomes 0, below every number.
 __device__ __forceinline__ unsigned long long order_key(double x) {
@@ -107,95 +139,95 @@ struct SelectArgs {
   const float* kc_mean;   // [B][H][chunk blocks][D]
   int* blocks;            // [B][H][q_blocks][n_select]
   int heads, q_blocks, n_select, cache_shared, keep_sink, keep_chunk;
+  int rows;               // query blocks of a thread block, at most kSelectRows
 };
 
-// R query blocks of one head per thread block: the key means are read once for all R.  Scores: a warp per key block,
-// D/32 elements per lane, fp64 fused multiply-adds; the R partial sums of the 32 lanes are folded together (lanes
-// split the sums between them on the way, 6 fp64 shuffles for 4 sums instead of 20).  Then a warp per query block finds the
-// n-th largest key bit by bit and writes the blocks above it, and as many equal to it as there is room for, in order.
-// Shared memory: keys [R][total].
-template <int D, int R>
+// c[8 x 8] += a[8 x 4] b[4 x 8], fp64: lane holds a[lane / 4][lane % 4], b[lane % 4][lane / 4] and
+// c[lane / 4][2 (lane % 4) + {0, 1}].
+__device__ __forceinline__ void mma_f64(double (&c)[2], double a, double b) {
+  asm("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};"
+      : "+d"(c[0]), "+d"(c[1])
+      : "d"(a), "d"(b));
+}
+
+// Up to eight query blocks of one head per thread block.  Scores: a warp per eight key blocks, fp64 MMAs over the head
+// dimension; the contraction index is dealt to the lanes so that each reads 16 contiguous bytes of a row (the same
+// order on both sides, so nothing else changes).  Then a warp per query block finds the n-th largest key bit by bit, stopping
+// as soon as a candidate separates exactly n, and writes the blocks above it, and as many equal to it as there is room
+// for, in order.  Scores by fused multiply-adds and shuffles, a warp per key block: 42 us for a chunk of 37 x 12 query blocks
+// and 273 key blocks against XXX.
+// Shared memory: keys [rows][total].
+template <int D>
 __global__ void __launch_bounds__(kSelectThreads)
 block_select_kernel(const SelectArgs a, const KeyBlocks kb) {
-  static_assert(R == 4 || R == 1, "the fold of the partial sums is written for four sums or one");
   extern __shared__ unsigned long long s_key[];
-  constexpr int kPer = D / 32;
+  constexpr int kSteps = D / 16;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int q0 = blockIdx.x * R, h = blockIdx.y, b = blockIdx.z;
-  const int rows = min(R, a.q_blocks - q0);
-  double q[R][kPer];
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int e = 0; e < kPer; ++e)
-      q[r][e] = r < rows ? static_cast<double>(
-                               a.q_mean[((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + r) * D + lane * kPer + e])
-                         : 0.0;
-  const int chunk_blocks = kb.total - kb.ctx, slots = kb.sink_slots + kb.win_slots;
+  const int q0 = blockIdx.x * a.rows, h = blockIdx.y, b = blockIdx.z;
+  const int rows = min(a.rows, a.q_blocks - q0);
+  const int slots = kb.sink_slots + kb.win_slots, chunk_blocks = kb.total - kb.ctx;
   const float* ctx = a.pooled + static_cast<long long>(a.cache_shared ? 0 : b) * a.heads * slots * kb.per_frame * D +
                      static_cast<long long>(h) * slots * kb.per_frame * D;
   const float* own = a.kc_mean + (static_cast<long long>(b) * a.heads + h) * chunk_blocks * D;
-  for (int j = warp; j < kb.total; j += kSelectWarps) {
-    const float* src;
-    bool keep;
+  const int pair = lane >> 2, col = (lane & 3) * 4;
+  float4 q[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    q[i] = pair < rows ? *reinterpret_cast<const float4*>(
+                             a.q_mean + ((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + pair) * D + i * 16 + col)
+                       : make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int j0 = warp * 8; j0 < kb.total; j0 += kSelectWarps * 8) {
+    const int j = j0 + pair;
+    const float* src = nullptr;
     if (j < kb.ctx) {
       const int f = j / kb.per_frame;
       src = ctx + (static_cast<long long>(key_block_slot(kb, f)) * kb.per_frame + (j - f * kb.per_frame)) * D;
-      keep = a.keep_sink && f < kb.sink_held;
-    } else {
+    } else if (j < kb.total) {
       src = own + static_cast<long long>(j - kb.ctx) * D;
-      keep = a.keep_chunk;
     }
-    double k[kPer], s[R];
-    if constexpr (kPer == 4) {
-      const float4 v = *reinterpret_cast<const float4*>(src + lane * 4);
-      k[0] = v.x; k[1] = v.y; k[2] = v.z; k[3] = v.w;
-    } else {
-      const float2 v = *reinterpret_cast<const float2*>(src + lane * 2);
-      k[0] = v.x; k[1] = v.y;
+    float4 k[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      k[i] = src ? *reinterpret_cast<const float4*>(src + i * 16 + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+    double even[2] = {0.0, 0.0}, odd[2] = {0.0, 0.0};   // two chains
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      mma_f64(even, q[i].x, k[i].x);
+      mma_f64(odd, q[i].y, k[i].y);
+      mma_f64(even, q[i].z, k[i].z);
+      mma_f64(odd, q[i].w, k[i].w);
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      s[r] = 0.0;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) s[r] = fma(q[r][e], k[e], s[r]);
+    for (int e = 0; e < 2; ++e) {
+      const int to = j0 + 2 * (lane & 3) + e;
+      if (pair < rows && to < kb.total) {
+        const bool keep = to < kb.ctx ? a.keep_sink && to < kb.sink_held * kb.per_frame : a.keep_chunk != 0;
+        s_key[static_cast<long long>(pair) * kb.total + to] = keep ? kKeptKey : order_key(even[e] + odd[e]);
+      }
     }
-    double sum;
-    int row = 0;
-    if constexpr (R == 4) {
-      const bool up = lane & 16, left = lane & 8;
-      double x = up ? s[2] : s[0], y = up ? s[3] : s[1];
-      x += __shfl_xor_sync(0xffffffffu, up ? s[0] : s[2], 16);
-      y += __shfl_xor_sync(0xffffffffu, up ? s[1] : s[3], 16);
-      sum = left ? y : x;
-      sum += __shfl_xor_sync(0xffffffffu, left ? x : y, 8);
-      row = (up ? 2 : 0) + (left ? 1 : 0);
-    } else {
-      sum = s[0];
-      sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-    }
-    sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    if ((lane & 7) == 0 && (R == 4 || lane == 0))
-      s_key[static_cast<long long>(row) * kb.total + j] = keep ? kKeptKey : order_key(sum);
   }
   __syncthreads();
   for (int r = warp; r < rows; r += kSelectWarps) {
     const unsigned long long* key = s_key + static_cast<long long>(r) * kb.total;
     int* out = a.blocks + ((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + r) * a.n_select;
     const int want = min(a.n_select, kb.total);
-    unsigned long long cut = 0;   // the want-th largest key: the largest value that at least `want` keys reach
-    for (int bit = 63; bit >= 0; --bit) {
+    // the want-th largest key: the largest value that at least `want` keys reach; or any value that exactly `want` reach
+    unsigned long long cut = 0;
+    int reach = kb.total;
+    for (int bit = 63; bit >= 0 && reach != want; --bit) {
       const unsigned long long cand = cut | (1ull << bit);
       int n = 0;
       for (int j = lane; j < kb.total; j += 32) n += key[j] >= cand;
-      if (__reduce_add_sync(0xffffffffu, n) >= want) cut = cand;
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (n >= want) {
+        cut = cand;
+        reach = n;
+      }
     }
-    int above = 0;
+    int above = 0;   // keys over the cut; the rest of the places go to those equal to it, the lower blocks first
     for (int j = lane; j < kb.total; j += 32) above += key[j] > cut;
     int ties = want - __reduce_add_sync(0xffffffffu, above);
+    if (reach == want) ties = kb.total;
     int at = 0;
     for (int j0 = 0; j0 < kb.total; j0 += 32) {
       const int j = j0 + lane;

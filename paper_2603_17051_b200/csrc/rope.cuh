@@ -7,10 +7,12 @@
 // positions lose nothing (an fp32 product is 0.06 rad off at position 10^6); sine and cosine of the fraction are
 // fp32 (2e-7 rad), the rotation is fp32 and each result is rounded once to the tensor's type.
 //
-// The work is bandwidth: q and k read once, written once.  A block owns a few tokens: its threads first compute the
-// tokens' cosines and sines into shared memory (once for all heads of q and k), then every thread keeps one 16-byte
-// position of a token's rows and walks over the tokens, so that up to four loads per thread are in flight and no
-// index is divided inside the loop.
+// The work is bandwidth: q and k read once, written once.  A thread owns one 16-byte piece of a token's rows (two where
+// pairs are halves), works out the cosines and sines of its 2 to 8 pairs itself and walks over the rows (the heads of q, then
+// those of k), kRopeRows loads in flight: no shared memory, no barrier, and the angles cost a fifth of the instructions when a thread
+// has all 24 rows of a 12-head token.  With fewer tokens the rows are dealt to several threads.
+// Sharing the angles of a few tokens through shared memory instead made every block load, wait, turn and store in step: 18.4 us
+// against 12.1 us for the 4680 tokens of a chunk (57.6 MB).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -20,9 +22,8 @@
 namespace astro {
 
 constexpr int kRopeMaxPairs = 128;
-constexpr int kRopeMaxThreads = 512;
-constexpr int kRopeUnroll = 4;      // tokens whose loads a thread has in flight
-constexpr int kRopeMaxTokens = 32;  // tokens of a block
+constexpr int kRopeThreads = 256;
+constexpr int kRopeRows = 6;        // rows whose loads a thread has in flight
 
 struct RopeTable {
   double turns[kRopeMaxPairs];      // f_p / 2 pi
@@ -96,122 +97,112 @@ __host__ __device__ inline int rope_items_per_row(int mode, int head_dim, int ro
   return rot_dim / 2 + (head_dim - rot_dim);
 }
 
-// blockDim.x threads share a token's (row, item) positions, blockDim.y token lanes; a block owns
-// `block_tokens` consecutive tokens of the batch * n_tokens (sample-major).  Shared memory: float2 [tokens][pairs].
+// Thread = (token, row phase, item): the rows phase, phase + phases, ... of the token.  Tokens are numbered sample-major,
+// batch * n_tokens in all.
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kRopeMaxThreads)
+__global__ void __launch_bounds__(kRopeThreads)
 rope_kernel(const __grid_constant__ RopeTable table, const __grid_constant__ RopeTensors x,
             const int* __restrict__ positions, const int positions_per_sample, const int n_tokens, const int total_tokens,
-            const int head_dim, const int rot_dim, const int block_tokens, const float sign) {
+            const int head_dim, const int rot_dim, const int phases, const float sign) {
   constexpr int E = RopeVec<T>::kElems;
-  extern __shared__ float2 s_turn[];
-  __shared__ long long s_in[kRopeMaxTokens], s_out[kRopeMaxTokens];
-  const int first = blockIdx.x * block_tokens;
-  const int count = min(block_tokens, total_tokens - first);
-  const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
-  for (int i = tid; i < count * table.pairs; i += threads) {
-    const int t = i / table.pairs, p = i - t * table.pairs;
-    const long long row = positions_per_sample ? first + t : (first + t) % n_tokens;
-    double turn = static_cast<double>(positions[row * table.axes + table.axis[p]]) * table.turns[p];
-    turn -= rint(turn);
-    float sn, cs;
-    sincospif(2.f * static_cast<float>(turn), &sn, &cs);
-    s_turn[i] = make_float2(cs * table.size, sn * table.size * sign);
-  }
-  if (tid < count) {
-    const int b = (first + tid) / n_tokens, t = (first + tid) - b * n_tokens;
-    s_in[tid] = b * x.in_b + t * x.in_t;
-    s_out[tid] = b * x.out_b + t * x.out_t;
-  }
-  __syncthreads();
-
+  constexpr int kPairs = MODE == kRopeInterleaved ? E / 2 : MODE == kRopeHalves ? E : 1;   // pairs of an item
   const int per_row = rope_items_per_row(MODE, head_dim, rot_dim, E);
-  const int items = (x.heads_q + x.heads_k) * per_row;
+  const long long id = static_cast<long long>(blockIdx.x) * kRopeThreads + threadIdx.x;
+  const int token = static_cast<int>(id / (per_row * phases));
+  if (token >= total_tokens) return;
+  const int rest = static_cast<int>(id - static_cast<long long>(token) * (per_row * phases));
+  const int phase = rest / per_row, c = rest - phase * per_row;
+  const int b = token / n_tokens, t = token - b * n_tokens;
   const int half = rot_dim / 2;
-  for (int i = threadIdx.x; i < items; i += blockDim.x) {
-    const int r = i / per_row, c = i - r * per_row;
-    const bool is_k = r >= x.heads_q;
-    const int h = is_k ? r - x.heads_q : r;
-    const T* in = static_cast<const T*>(is_k ? x.k : x.q) + h * x.in_h;
-    T* out = static_cast<T*>(is_k ? x.k_out : x.q_out) + h * x.out_h;
-    if (MODE == kRopeInterleaved) {
-      const int e0 = c * E, p0 = e0 / 2, rotated = min(E / 2, max(0, half - p0));
-      for (int t0 = threadIdx.y; t0 < count; t0 += kRopeUnroll * blockDim.y) {
-        uint4 v[kRopeUnroll];
+  // first pair of the item, how many of its pairs turn, its first element
+  const int p0 = c * kPairs;
+  const int turning = min(kPairs, max(0, half - p0));
+  const int e0 = MODE == kRopeInterleaved ? c * E : turning > 0 ? p0 : p0 + half;   // copied pieces of halves start at rot_dim
+
+  const int rows = x.heads_q + x.heads_k;
+  const long long in0 = b * x.in_b + t * x.in_t + e0, out0 = b * x.out_b + t * x.out_t + e0;
+  auto source = [&](int r) {
+    return r < x.heads_q ? static_cast<const T*>(x.q) + in0 + r * x.in_h
+                         : static_cast<const T*>(x.k) + in0 + (r - x.heads_q) * x.in_h;
+  };
+  auto target = [&](int r) {
+    return r < x.heads_q ? static_cast<T*>(x.q_out) + out0 + r * x.out_h
+                         : static_cast<T*>(x.k_out) + out0 + (r - x.heads_q) * x.out_h;
+  };
+  // the piece, and its partner half a rotated part further on
+  uint4 v[kRopeRows], w[MODE == kRopeHalves ? kRopeRows : 1];
+  auto fetch = [&](int r0) {
 #pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) {
-          const int t = t0 + u * blockDim.y;
-          if (t < count) v[u] = *reinterpret_cast<const uint4*>(in + s_in[t] + e0);
-        }
+    for (int u = 0; u < kRopeRows; ++u) {
+      const int r = r0 + u * phases;
+      if (r >= rows) continue;
+      const T* src = source(r);
+      v[u] = __ldcs(reinterpret_cast<const uint4*>(src));
+      if (MODE == kRopeHalves && turning > 0) w[u] = __ldcs(reinterpret_cast<const uint4*>(src + half));
+    }
+  };
+  if (MODE != kRopeHalvesScalar) fetch(phase);   // on their way while the angles are worked out
+
+  float cs[kPairs], sn[kPairs];
+  const int* coordinate = positions + static_cast<long long>(positions_per_sample ? token : t) * table.axes;
 #pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) {
-          const int t = t0 + u * blockDim.y;
-          if (t >= count) break;
+  for (int j = 0; j < kPairs; ++j)
+    if (j < turning) {
+      double turns = static_cast<double>(coordinate[table.axis[p0 + j]]) * table.turns[p0 + j];
+      turns -= rint(turns);
+      sincospif(2.f * static_cast<float>(turns), &sn[j], &cs[j]);
+      cs[j] *= table.size;
+      sn[j] *= table.size * sign;
+    }
+
+  if constexpr (MODE == kRopeHalvesScalar) {
+    for (int r = phase; r < rows; r += phases) {
+      const T* src = source(r);
+      T* dst = target(r);
+      if (turning == 0) {
+        *dst = *src;
+        continue;
+      }
+      const float lo = RopeVec<T>::load(src), hi = RopeVec<T>::load(src + half);
+      RopeVec<T>::store(dst, lo * cs[0] - hi * sn[0]);
+      RopeVec<T>::store(dst + half, lo * sn[0] + hi * cs[0]);
+    }
+  } else {
+    for (int r0 = phase; r0 < rows;) {
+#pragma unroll
+      for (int u = 0; u < kRopeRows; ++u) {
+        const int r = r0 + u * phases;
+        if (r >= rows) continue;
+        T* dst = target(r);
+        if (turning == 0) {   // stored bit for bit as it came
+          __stcs(reinterpret_cast<uint4*>(dst), v[u]);
+        } else if (MODE == kRopeInterleaved) {
           float f[E];
           RopeVec<T>::unpack(v[u], f);
-          const float2* cs = s_turn + t * table.pairs + p0;
 #pragma unroll
-          for (int j = 0; j < E / 2; ++j)
-            if (j < rotated) {
-              const float2 w = cs[j];
-              const float a = f[2 * j], b = f[2 * j + 1];
-              f[2 * j] = a * w.x - b * w.y;
-              f[2 * j + 1] = a * w.y + b * w.x;
+          for (int j = 0; j < kPairs; ++j)
+            if (j < turning) {
+              const float lo = f[2 * j], hi = f[2 * j + 1];
+              f[2 * j] = lo * cs[j] - hi * sn[j];
+              f[2 * j + 1] = lo * sn[j] + hi * cs[j];
             }
-          // a piece without rotated elements is stored bit for bit as it came
-          *reinterpret_cast<uint4*>(out + s_out[t] + e0) = rotated == 0 ? v[u] : RopeVec<T>::pack(f);
-        }
-      }
-    } else if (MODE == kRopeHalves) {
-      const bool copy = c >= half / E;
-      const int e0 = copy ? c * E + half : c * E;   // copied pieces start at rot_dim
-      for (int t0 = threadIdx.y; t0 < count; t0 += kRopeUnroll * blockDim.y) {
-        uint4 v[kRopeUnroll], w[kRopeUnroll];
+          __stcs(reinterpret_cast<uint4*>(dst), RopeVec<T>::pack(f));
+        } else {
+          float lo[E], hi[E];
+          RopeVec<T>::unpack(v[u], lo);
+          RopeVec<T>::unpack(w[u], hi);
 #pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) {
-          const int t = t0 + u * blockDim.y;
-          if (t >= count) continue;
-          v[u] = *reinterpret_cast<const uint4*>(in + s_in[t] + e0);
-          if (!copy) w[u] = *reinterpret_cast<const uint4*>(in + s_in[t] + e0 + half);
-        }
-#pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) {
-          const int t = t0 + u * blockDim.y;
-          if (t >= count) continue;
-          if (copy) {
-            *reinterpret_cast<uint4*>(out + s_out[t] + e0) = v[u];
-            continue;
+          for (int j = 0; j < E; ++j) {   // half is a multiple of E: the whole piece turns
+            const float a = lo[j] * cs[j % kPairs] - hi[j] * sn[j % kPairs];
+            hi[j] = lo[j] * sn[j % kPairs] + hi[j] * cs[j % kPairs];
+            lo[j] = a;
           }
-          float a[E], b[E];
-          RopeVec<T>::unpack(v[u], a);
-          RopeVec<T>::unpack(w[u], b);
-          const float2* cs = s_turn + t * table.pairs + e0;
-#pragma unroll
-          for (int j = 0; j < E; ++j) {
-            const float2 y = cs[j];
-            const float lo = a[j] * y.x - b[j] * y.y;
-            b[j] = a[j] * y.y + b[j] * y.x;
-            a[j] = lo;
-          }
-          *reinterpret_cast<uint4*>(out + s_out[t] + e0) = RopeVec<T>::pack(a);
-          *reinterpret_cast<uint4*>(out + s_out[t] + e0 + half) = RopeVec<T>::pack(b);
+          __stcs(reinterpret_cast<uint4*>(dst), RopeVec<T>::pack(lo));
+          __stcs(reinterpret_cast<uint4*>(dst + half), RopeVec<T>::pack(hi));
         }
       }
-    } else {
-      const bool copy = c >= half;
-      const int e0 = copy ? c + half : c;
-      for (int t = threadIdx.y; t < count; t += blockDim.y) {
-        const T* src = in + s_in[t] + e0;
-        T* dst = out + s_out[t] + e0;
-        if (copy) {
-          *dst = *src;
-          continue;
-        }
-        const float a = RopeVec<T>::load(src), b = RopeVec<T>::load(src + half);
-        const float2 y = s_turn[t * table.pairs + c];
-        RopeVec<T>::store(dst, a * y.x - b * y.y);
-        RopeVec<T>::store(dst + half, a * y.y + b * y.x);
-      }
+      r0 += kRopeRows * phases;
+      if (r0 < rows) fetch(r0);
     }
   }
 }
