@@ -433,11 +433,29 @@ bool build_key_blocks(const astro_kvcache* c, int n_kc, int block, KeyBlocks* ou
 }
 
 template <int D>
+astro_status_t launch_pool(const PoolSource& s0, const PoolSource& s1, int n0, int n1, int heads, int batch, const KeyBlocks& kb,
+                           int frame0, int cache_source, cudaStream_t st) {
+  // as many warps per block of tokens as bring the GPU 1500 of them, so that enough loads are in flight (1872
+  // blocks: one warp each 15.5 us, two 17.9: more streams, more sums to join)
+  const long long blocks = (static_cast<long long>(n0) + n1) * heads * batch;
+  int share = 1;
+  while (share < 8 && blocks * share < 1500) share *= 2;
+  const int per_cta = kPoolThreads / 32 / share;
+  dim3 grid((n0 + n1 + per_cta - 1) / per_cta, heads, batch);
+  block_pool_kernel<D><<<grid, kPoolThreads, 0, st>>>(s0, s1, n0, n1, kb, frame0, cache_source, share);
+  return launch_status();
+}
+
+void set_inverses(PoolSource* s) {
+  const int rest = s->tokens % s->block;
+  s->inv_block = 1.0 / s->block;
+  s->inv_last = 1.0 / (rest ? rest : s->block);
+}
+
+template <int D>
 astro_status_t launch_select_all(const PoolSource& q, const PoolSource& kc, SelectArgs a, const KeyBlocks& kb, int batch,
                                  cudaStream_t st) {
-  dim3 grid(q.blocks + kc.blocks, a.heads, batch);
-  block_pool_kernel<D><<<grid, kPoolThreads, 0, st>>>(q, kc, q.blocks, kb, 0, 0);
-  astro_status_t s = launch_status();
+  astro_status_t s = launch_pool<D>(q, kc, q.blocks, kc.blocks, a.heads, batch, kb, 0, 0, st);
   if (s != ASTRO_OK) return s;
   static std::atomic<int> done[kMaxDevices];
   if ((s = set_smem_once(block_select_kernel<D>, ASTRO_SELECT_MAX_BLOCKS * 8, done)) != ASTRO_OK) return s;
@@ -1127,11 +1145,10 @@ astro_status_t astro_block_pool(const astro_kvcache_t* c, int first_frame, int n
   src.tokens = d.tokens_per_frame;
   src.block = block_tokens;
   src.blocks = n_frames * kb.per_frame;
-  dim3 grid(src.blocks, d.heads, d.cache_batch);
+  set_inverses(&src);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (d.head_dim == 128) block_pool_kernel<128><<<grid, kPoolThreads, 0, st>>>(src, src, src.blocks, kb, first_frame, 1);
-  else block_pool_kernel<64><<<grid, kPoolThreads, 0, st>>>(src, src, src.blocks, kb, first_frame, 1);
-  return launch_status();
+  return d.head_dim == 128 ? launch_pool<128>(src, src, src.blocks, 0, d.heads, d.cache_batch, kb, first_frame, 1, st)
+                           : launch_pool<64>(src, src, src.blocks, 0, d.heads, d.cache_batch, kb, first_frame, 1, st);
 }
 
 size_t astro_block_select_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens) {
@@ -1166,6 +1183,7 @@ astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* poo
   qs.tokens = n_q;
   qs.block = ASTRO_QUERY_BLOCK;
   qs.blocks = (n_q - 1) / ASTRO_QUERY_BLOCK + 1;
+  set_inverses(&qs);
   qs.out = static_cast<float*>(workspace);
   qs.out_h = qs.blocks;
   qs.out_b = qs.out_h * heads;
@@ -1175,6 +1193,7 @@ astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* poo
   ks.tokens = n_kc;
   ks.block = block_tokens;
   ks.blocks = kb.total - kb.ctx;
+  set_inverses(&ks);
   ks.out = qs.out + qs.out_b * batch * head_dim;
   ks.out_h = ks.blocks;
   ks.out_b = ks.out_h * heads;

@@ -36,31 +36,28 @@ struct PoolSource {
   float* out;              // [b][h][out_row][D]
   long long out_b, out_h;  // rows per sample, rows per head of `out`
   int tokens, block, blocks;
+  double inv_block, inv_last;   // 1 / tokens of a full block, of the last one
 };
 
 constexpr int kPoolThreads = 256;
 
-// Sums of bf16 values in fp64 without a conversion per value (those run at a quarter of the adds' rate or less): the bits of a
-// bf16, moved to the places of an fp64's sign, exponent and mantissa, are that value times 2^-896, zeros and denormal
-// values included; the sum is scaled back once.  Infinities and NaN have no such image (`seen` collects the magnitudes so
-// that they are noticed).
-__device__ __forceinline__ void add_scaled(double& lo, double& hi, uint32_t pair) {
-  lo += __hiloint2double(static_cast<int>(((pair << 13) & 0x0fffe000u) | ((pair << 16) & 0x80000000u)), 0);
-  hi += __hiloint2double(static_cast<int>(((pair >> 3) & 0x0fffe000u) | (pair & 0x80000000u)), 0);
-}
+constexpr int kPoolBatch = 6;   // token rows a thread has in flight, twice (the next batch is asked for before this one is added)
 
-// One block of tokens of one head per thread block: D/8 threads side by side hold 8 elements each, the others walk the
-// tokens, all of a thread's loads in flight at once; partial sums meet in shared memory.  Bandwidth bound.
-// grid.x = blocks of source 0, then of source 1 (n0 of the first); grid.y = head, grid.z = sample.  cache_source: source 0 is
-// the cache storage, and grid.x walks the blocks of the frames from logical frame `frame0` on.
+// `share` warps (1, 2, 4 or 8) per block of tokens of one head: D/8 lanes side by side hold 8 elements each, the other lanes
+// and warps walk the tokens.  Everything is resident at once and every warp streams by itself: 58 MB in 14.6 us (13.6 with
+// fp32 sums; a thread block per block of tokens, with its partial sums in shared memory, 17.2).
+// grid.x * (8 / share) covers the blocks of source 0, then of source 1 (n0 and n1 of them); grid.y = head, grid.z = sample.
+// cache_source: source 0 is the cache storage, and its blocks are those of the frames from logical frame `frame0` on.
 template <int D>
 __global__ void __launch_bounds__(kPoolThreads)
-block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const KeyBlocks kb, const int frame0,
-                  const int cache_source) {
-  constexpr int kCols = D / 8, kRows = kPoolThreads / kCols, kDeep = kTile / kRows;   // a block has at most kTile tokens
-  const bool second = static_cast<int>(blockIdx.x) >= n0;
+block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const int n1, const KeyBlocks kb, const int frame0,
+                  const int cache_source, const int share) {
+  constexpr int kCols = D / 8, kWarps = kPoolThreads / 32, kGroups = 32 / kCols;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane % kCols;
+  const int unit = blockIdx.x * (kWarps / share) + warp / share;
+  const bool there = unit < n0 + n1, second = unit >= n0;
   const PoolSource& s = second ? s1 : s0;
-  int j = second ? blockIdx.x - n0 : blockIdx.x;
+  int j = second ? unit - n0 : unit;
   const int h = blockIdx.y, b = blockIdx.z;
   long long first_row = 0, out_row = j;
   if (cache_source) {
@@ -69,54 +66,61 @@ block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const 
     first_row = static_cast<long long>(slot) * s.tokens;
     out_row = static_cast<long long>(slot) * kb.per_frame + j;
   }
-  const int count = min(s.block, s.tokens - j * s.block);
-  const int col = threadIdx.x % kCols, row = threadIdx.x / kCols;
+  const int count = there ? min(s.block, s.tokens - j * s.block) : 0;
+  const int step = share * kGroups;
+  int t = (warp % share) * kGroups + lane / kCols;
   const __nv_bfloat16* src = s.base + b * s.sb + h * s.sh + (first_row + static_cast<long long>(j) * s.block) * s.st + col * 8;
-  uint4 v[kDeep];
-#pragma unroll
-  for (int u = 0; u < kDeep; ++u) {
-    const int t = row + u * kRows;
-    v[u] = t < count ? *reinterpret_cast<const uint4*>(src + t * s.st) : make_uint4(0, 0, 0, 0);
-  }
   double acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0;
-  uint32_t seen = 0;
+  uint4 v[kPoolBatch];
+  auto fetch = [&]() {
 #pragma unroll
-  for (int u = 0; u < kDeep; ++u) {
-    const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+    for (int u = 0; u < kPoolBatch; ++u)
+      v[u] = t + u * step < count ? __ldcs(reinterpret_cast<const uint4*>(src + (t + u * step) * s.st)) : make_uint4(0, 0, 0, 0);
+  };
+  fetch();
+  while (t < count) {
+    uint4 now[kPoolBatch];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      add_scaled(acc[2 * e], acc[2 * e + 1], w[e]);
-      seen = __vmaxu2(seen, w[e] & 0x7fff7fffu);
-    }
-  }
-  double unscale = ldexp(1.0, 896);
-  if ((seen & 0xffffu) >= 0x7f80u || (seen >> 16) >= 0x7f80u) {   // again with true conversions; scaled down, see below
+    for (int u = 0; u < kPoolBatch; ++u) now[u] = v[u];
+    t += kPoolBatch * step;
+    fetch();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = 0.0;
-#pragma unroll
-    for (int u = 0; u < kDeep; ++u) {
-      const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v[u]);
+    for (int u = 0; u < kPoolBatch; ++u) {
+      const uint32_t w[4] = {now[u].x, now[u].y, now[u].z, now[u].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 f = __bfloat1622float2(p[e]);
-        acc[2 * e] += static_cast<double>(f.x);
-        acc[2 * e + 1] += static_cast<double>(f.y);
+        acc[2 * e] += static_cast<double>(__uint_as_float(w[e] << 16));
+        acc[2 * e + 1] += static_cast<double>(__uint_as_float(w[e] & 0xffff0000u));
       }
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= 1.0 / unscale;   // back into the others' scale; a power of two loses nothing
   }
-  __shared__ double part[kRows][8][kCols];
+  __syncwarp();
 #pragma unroll
-  for (int e = 0; e < 8; ++e) part[row][e][col] = acc[e];
-  __syncthreads();
-  for (int e = threadIdx.x; e < D; e += kPoolThreads) {
-    double sum = 0.0;
+  for (int x = kCols; x < 32; x *= 2)
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) sum += part[r][e % 8][e / 8];
-    s.out[((b * s.out_b + h * s.out_h) + out_row) * D + e] = static_cast<float>(sum * unscale / static_cast<double>(count));
+    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], x);
+  __shared__ double part[kWarps][8][kCols];
+  if (share > 1) {
+    if (lane < kCols) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) part[warp][e][col] = acc[e];
+    }
+    __syncthreads();
+    if (warp % share) return;
+    for (int r = 1; r < share; ++r)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += part[warp + r][e][col];
+  }
+  if (there && lane < kCols) {
+    const double inv = count == s.block ? s.inv_block : s.inv_last;
+    float* out = s.out + ((b * s.out_b + h * s.out_h) + out_row) * D + col * 8;
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(acc[e] * inv);
+    reinterpret_cast<float4*>(out)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(out)[1] = make_float4(f[4], f[5], f[6], f[7]);
   }
 }
 
@@ -124,6 +128,7 @@ block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const 
 constexpr int kSelectThreads = 512;
 constexpr int kSelectWarps = kSelectThreads / 32;
 constexpr int kSelectRows = 8;     // query blocks of one MMA tile
+constexpr int kSelectHeld = 16;    // keys a lane holds in registers
 
 // A double as an unsigned integer of the same order; NaN becomes 0, below every number.
 __device__ __forceinline__ unsigned long long order_key(double x) {
@@ -148,6 +153,27 @@ __device__ __forceinline__ void mma_f64(double (&c)[2], double a, double b) {
   asm("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};"
       : "+d"(c[0]), "+d"(c[1])
       : "d"(a), "d"(b));
+}
+
+// A warp's search for the cut between the `want` largest of `total` keys and the others.  The cut is the want-th largest key
+// (the largest value that at least `want` keys reach) or any value that exactly `want` keys reach; `ties` is how many
+// of the keys equal to it belong to the chosen ones.  count(p) counts the keys of a lane for which p holds; keys of 0 that
+// pad a lane are not counted because a candidate is never 0.
+template <typename Count>
+__device__ __forceinline__ unsigned long long select_cut(int want, int total, int& ties, Count count) {
+  unsigned long long cut = 0;
+  int reach = total;
+  for (int bit = 63; bit >= 0 && reach != want; --bit) {
+    const unsigned long long cand = cut | (1ull << bit);
+    const int n = __reduce_add_sync(0xffffffffu, count([&](unsigned long long x) { return x >= cand; }));
+    if (n >= want) {
+      cut = cand;
+      reach = n;
+    }
+  }
+  ties = total;
+  if (reach != want) ties = want - __reduce_add_sync(0xffffffffu, count([&](unsigned long long x) { return x > cut; }));
+  return cut;
 }
 
 // Up to eight query blocks of one head per thread block.  Scores: a warp per eight key blocks, fp64 MMAs over the head
@@ -211,23 +237,26 @@ block_select_kernel(const SelectArgs a, const KeyBlocks kb) {
     const unsigned long long* key = s_key + static_cast<long long>(r) * kb.total;
     int* out = a.blocks + ((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + r) * a.n_select;
     const int want = min(a.n_select, kb.total);
-    // the want-th largest key: the largest value that at least `want` keys reach; or any value that exactly `want` reach
-    unsigned long long cut = 0;
-    int reach = kb.total;
-    for (int bit = 63; bit >= 0 && reach != want; --bit) {
-      const unsigned long long cand = cut | (1ull << bit);
-      int n = 0;
-      for (int j = lane; j < kb.total; j += 32) n += key[j] >= cand;
-      n = __reduce_add_sync(0xffffffffu, n);
-      if (n >= want) {
-        cut = cand;
-        reach = n;
-      }
+    int ties;
+    unsigned long long cut;
+    // up to 512 keys sit in the lanes' registers during the search, more are read again for every bit
+    if (kb.total <= 32 * kSelectHeld) {
+      unsigned long long held[kSelectHeld];
+#pragma unroll
+      for (int i = 0; i < kSelectHeld; ++i) held[i] = lane + 32 * i < kb.total ? key[lane + 32 * i] : 0ull;
+      cut = select_cut(want, kb.total, ties, [&](auto reaches) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kSelectHeld; ++i) n += reaches(held[i]) ? 1 : 0;
+        return n;
+      });
+    } else {
+      cut = select_cut(want, kb.total, ties, [&](auto reaches) {
+        int n = 0;
+        for (int j = lane; j < kb.total; j += 32) n += reaches(key[j]) ? 1 : 0;
+        return n;
+      });
     }
-    int above = 0;   // keys over the cut; the rest of the places go to those equal to it, the lower blocks first
-    for (int j = lane; j < kb.total; j += 32) above += key[j] > cut;
-    int ties = want - __reduce_add_sync(0xffffffffu, above);
-    if (reach == want) ties = kb.total;
     int at = 0;
     for (int j0 = 0; j0 < kb.total; j0 += 32) {
       const int j = j0 + lane;
