@@ -215,6 +215,23 @@ template <typename K> astro_status_t set_smem_once(K kernel, int bytes, std::ato
 
 astro_status_t launch_status() { return cudaGetLastError() == cudaSuccess ? ASTRO_OK : ASTRO_ERR_CUDA; }
 
+// Launches a kernel as the dependent of the one launched just before it on the stream: it may start while that one
+// drains, and waits for it itself (dependency_wait).
+template <typename... Params, typename... Args>
+astro_status_t launch_dependent(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...) == cudaSuccess ? launch_status() : ASTRO_ERR_CUDA;
+}
+
 struct AttnArgs {
   const astro_kvcache* cache;
   int batch, heads, head_dim, n_q, n_kc;
@@ -463,8 +480,7 @@ astro_status_t launch_select_all(const PoolSource& q, const PoolSource& kc, Sele
   const int most = ASTRO_SELECT_MAX_BLOCKS / kb.total;
   a.rows = most < kSelectRows ? most : kSelectRows;
   dim3 tiles((a.q_blocks + a.rows - 1) / a.rows, a.heads, batch);
-  block_select_kernel<D><<<tiles, kSelectThreads, static_cast<size_t>(a.rows) * kb.total * 8, st>>>(a, kb);
-  return launch_status();
+  return launch_dependent(block_select_kernel<D>, tiles, kSelectThreads, static_cast<size_t>(a.rows) * kb.total * 8, st, a, kb);
 }
 
 // ---- attention over lists of key blocks ---------------------------------------------------------------------
@@ -526,7 +542,8 @@ astro_status_t sparse_maps(const SparseCall& c, const SparseGeom& g, SparseMaps*
 }
 
 // Into how many ranges a unit's list is cut, and how many entries a range has.  With fewer units than half the SMs of a B200
-// (148) most of it would idle while a few CTAs walk over long lists; a range keeps at least two tiles.
+// (148) most of it would idle while a few CTAs walk over long lists.  Joining the parts costs about 4 us, a tile about 0.7: lists
+// of 12 tiles and more are cut, into ranges of 4 tiles and more.
 struct SparseSplit {
   int splits, entries;
 };
@@ -536,9 +553,9 @@ SparseSplit sparse_split(int batch, int heads, int n_q, int n_select, int block_
   const int per_tile = kTile / sparse_pad(block_tokens);
   const int tiles = (n_select - 1) / per_tile + 1;
   SparseSplit r{1, n_select};
-  if (units * 2 > kSms || tiles < 4) return r;
+  if (units * 2 > kSms || tiles < 12) return r;
   int want = static_cast<int>(kSms / units);
-  if (want > tiles / 2) want = tiles / 2;
+  if (want > tiles / 4) want = tiles / 4;
   const int each = (tiles - 1) / want + 1;   // tiles of a range
   r.splits = (tiles - 1) / each + 1;
   r.entries = each * per_tile;
@@ -582,9 +599,8 @@ astro_status_t launch_sparse_fwd(const SparseCall& c, const SparseGeom& g, float
   if (units > ctas * kFwdMaxUnits) ctas = sms * ((units + static_cast<long long>(sms) * kFwdMaxUnits - 1) / (static_cast<long long>(sms) * kFwdMaxUnits));
   sparse_attn_fwd_kernel<D><<<static_cast<unsigned>(ctas), kSparseThreads, SparseFwdSmem<D>::kTotal, st>>>(maps, a, g, u);
   if ((s = launch_status()) != ASTRO_OK || split.splits == 1) return s;
-  sparse_combine_kernel<D><<<static_cast<unsigned>((rows + 7) / 8), 256, 0, st>>>(a.part_o, a.part_lse, split.splits, rows, c.a.n_q,
-                                                                             c.a.heads, a.o, lse);
-  return launch_status();
+  return launch_dependent(sparse_combine_kernel<D>, dim3(static_cast<unsigned>((rows + 7) / 8)), 256, 0, st, a.part_o, a.part_lse,
+                          split.splits, rows, c.a.n_q, c.a.heads, a.o, lse);
 }
 
 // Scratch of the backward: delta, then how often every query tile names every chunk block.
@@ -615,7 +631,26 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
   float* delta = static_cast<float*>(workspace);
   int* counts = reinterpret_cast<int*>(static_cast<char*>(workspace) + need.delta);
   const int q_tiles = (c.a.n_q - 1) / kTile + 1, chunk_blocks = g.kb.total - g.kb.ctx;
-  if ((s = launch_bwd_delta<D>(o, d_o, c.a.batch, c.a.heads, c.a.n_q, delta, st)) != ASTRO_OK) return s;
+  SparsePrepArgs p;
+  p.o = static_cast<const __nv_bfloat16*>(o);
+  p.d_o = static_cast<const __nv_bfloat16*>(d_o);
+  p.blocks = c.blocks;
+  p.delta = delta;
+  p.counts = counts;
+  p.rows = static_cast<long long>(c.a.batch) * c.a.n_q * c.a.heads;
+  p.lists = static_cast<long long>(c.a.batch) * c.a.heads * q_tiles;
+  p.heads = c.a.heads; p.n_q = c.a.n_q;
+  p.q_tiles = q_tiles;
+  p.n_select = c.n_select;
+  p.ctx_blocks = g.kb.ctx;
+  p.chunk_blocks = chunk_blocks;
+  p.spans = (chunk_blocks + kCountSpan - 1) / kCountSpan;
+  p.count_blocks = (p.lists * p.spans + kPrepThreads / 32 - 1) / (kPrepThreads / 32);
+  const long long per_block = static_cast<long long>(kPrepThreads) * 8 / D * kDeltaRows;
+  const long long prep_blocks = p.count_blocks + (p.rows + per_block - 1) / per_block;
+  if (prep_blocks > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
+  sparse_bwd_prep_kernel<D><<<static_cast<unsigned>(prep_blocks), kPrepThreads, 0, st>>>(p);
+  if ((s = launch_status()) != ASTRO_OK) return s;
   SparseBwdArgs a;
   a.q = static_cast<const __nv_bfloat16*>(c.q);
   a.blocks = c.blocks;
@@ -627,13 +662,9 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
   a.cache_shared = (c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1) ? 1 : 0;
   a.scale = scale;
   dim3 grid_q(q_tiles, a.cache_shared ? c.a.batch : c.a.heads, a.cache_shared ? c.a.heads : c.a.batch);
-  sparse_attn_bwd_dq_kernel<D><<<grid_q, kSdqThreads, SdqSmem<D>::kTotal, st>>>(maps, tdo, g, a, static_cast<__nv_bfloat16*>(dq));
-  if ((s = launch_status()) != ASTRO_OK || chunk_blocks == 0) return s;
-  if (cudaMemsetAsync(counts, 0, need.counts, st) != cudaSuccess) return ASTRO_ERR_CUDA;
-  const long long entries = static_cast<long long>(c.a.batch) * c.a.heads * q_tiles * c.n_select;
-  sparse_count_kernel<<<static_cast<unsigned>((entries + 255) / 256), 256, 0, st>>>(c.blocks, counts, entries, c.n_select, q_tiles,
-                                                                               g.kb.ctx, chunk_blocks);
-  if ((s = launch_status()) != ASTRO_OK) return s;
+  s = launch_dependent(sparse_attn_bwd_dq_kernel<D>, grid_q, kSdqThreads, SdqSmem<D>::kTotal, st, maps, tdo, g, a,
+                       static_cast<__nv_bfloat16*>(dq));
+  if (s != ASTRO_OK || chunk_blocks == 0) return s;
   SparseDkvArgs k;
   k.counts = counts;
   k.lse = lse;
@@ -644,9 +675,8 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
   k.chunk_blocks = chunk_blocks;
   k.scale = scale;
   dim3 grid_k(chunk_blocks, c.a.heads, c.a.batch);
-  sparse_attn_bwd_dkv_kernel<D><<<grid_k, kDkvThreads, DkvSmem<D>::kTotal, st>>>(
-      tq, tdo, maps.kc, maps.vc, k, static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv));
-  return launch_status();
+  return launch_dependent(sparse_attn_bwd_dkv_kernel<D>, grid_k, kDkvThreads, DkvSmem<D>::kTotal, st, tq, tdo, maps.kc, maps.vc, k,
+                          static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv));
 }
 
 }  // namespace
@@ -1261,8 +1291,7 @@ astro_status_t astro_sparse_attn_bwd(const astro_kvcache_t* cache, const void* q
   astro_status_t s = check_sparse(c, scale, &g);
   if (s != ASTRO_OK) return s;
   const long long q_tiles = (n_q - 1) / kTile + 1;
-  // the tiles of a block are counted in 32 bits, the grid of the entries too
-  if (q_tiles * n_select > 0x3fffffffLL || q_tiles * n_select * heads > 0x7fffffffLL * 256 / batch) return ASTRO_ERR_SHAPE;
+  if (q_tiles * n_select > 0x3fffffffLL) return ASTRO_ERR_SHAPE;   // the tiles of a block are counted in 32 bits
   if (!aligned16(q) || !aligned16(o) || !aligned16(d_o) || !aligned16(dq) || !aligned16(workspace) ||
       (reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(blocks) & 3u) ||
       (n_kc > 0 && (!aligned16(k_chunk) || !aligned16(v_chunk) || !aligned16(dk_chunk) || !aligned16(dv_chunk))))

@@ -70,6 +70,7 @@ block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const 
   const int step = share * kGroups;
   int t = (warp % share) * kGroups + lane / kCols;
   const __nv_bfloat16* src = s.base + b * s.sb + h * s.sh + (first_row + static_cast<long long>(j) * s.block) * s.st + col * 8;
+  dependents_may_start();
   double acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0;
@@ -196,6 +197,7 @@ block_select_kernel(const SelectArgs a, const KeyBlocks kb) {
                      static_cast<long long>(h) * slots * kb.per_frame * D;
   const float* own = a.kc_mean + (static_cast<long long>(b) * a.heads + h) * chunk_blocks * D;
   const int pair = lane >> 2, col = (lane & 3) * 4;
+  dependency_wait();   // the means of the queries and of the chunk
   float4 q[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)

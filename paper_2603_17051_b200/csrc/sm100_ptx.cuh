@@ -157,6 +157,12 @@ __device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint
   return ok;
 }
 
+// A kernel launched as the dependent of the one before it (programmatic launch) may start while that one drains.  The
+// dependent waits here before it touches anything the other has written: everything is then complete and visible.  The other may
+// say early that its dependent can be brought in.
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Barrier among `threads` threads of the CTA (a multiple of 32) that all name the same id (1..15).
 __device__ __forceinline__ void named_barrier_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");

@@ -1,6 +1,6 @@
 // Backward of attention over lists of key blocks, the cached context detached.
 //   dQ kernel     a query tile stationary, over the key tiles of its list:  dQ = scale * sum dS K
-//   dK/dV kernel  a chunk key block stationary, over the query tiles whose lists name it (sparse_count_kernel turns the
+//   dK/dV kernel  a chunk key block stationary, over the query tiles whose lists name it (sparse_bwd_prep_kernel turns the
 //                 lists around): dV = sum P^T dO, dK = scale * sum dS^T Q
 // with P = exp(S - LSE), dS = P o (dP - delta), as in the dense kernels, whose tensor-memory layouts, operand forms and
 // hand-offs these two have: see there.  No atomics touch a sum: the counts that turn the lists around are whole numbers
@@ -12,16 +12,81 @@
 
 namespace astro {
 
-// counts[b][h][chunk block][query tile] += times that the query tile's list names the block.  A thread per list entry.
-__global__ void __launch_bounds__(256)
-sparse_count_kernel(const int* __restrict__ blocks, int* __restrict__ counts, const long long entries, const int n_select,
-                    const int q_tiles, const int ctx_blocks, const int chunk_blocks) {
-  const long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (i >= entries) return;
-  const int id = blocks[i];
-  if (id < ctx_blocks || id - ctx_blocks >= chunk_blocks) return;
-  const long long row = i / n_select, bh = row / q_tiles;
-  atomicAdd(counts + (bh * chunk_blocks + (id - ctx_blocks)) * q_tiles + (row - bh * q_tiles), 1);
+// What both kernels need, in one launch.
+//   delta[b][h][i] = dO_i . O_i, fp32: D/8 lanes per row, 16 bytes of both tensors each; bandwidth
+//   counts[b][h][chunk block][query tile] = times that the query tile's list names the block: a warp per list and 1024 chunk
+//   blocks counts them in shared memory and writes every count, zeros included
+// The first `count_blocks` thread blocks count, the others take 256 * kDeltaRows * 8 / D rows each.
+constexpr int kPrepThreads = 256, kDeltaRows = 4, kCountSpan = 1024;
+
+struct SparsePrepArgs {
+  const __nv_bfloat16 *o, *d_o;
+  const int* blocks;
+  float* delta;
+  int* counts;
+  long long rows;    // batch * n_q * heads
+  long long lists;   // batch * heads * q_tiles
+  long long count_blocks;
+  int heads, n_q, q_tiles, n_select, ctx_blocks, chunk_blocks, spans;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kPrepThreads)
+sparse_bwd_prep_kernel(const SparsePrepArgs a) {
+  __shared__ int hist[kPrepThreads / 32][kCountSpan];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  dependents_may_start();
+  if (blockIdx.x < a.count_blocks) {
+    const long long job = static_cast<long long>(blockIdx.x) * (kPrepThreads / 32) + warp;   // (list, span)
+    if (job >= a.lists * a.spans) return;
+    const long long list = job / a.spans;
+    const int first = static_cast<int>(job - list * a.spans) * kCountSpan, n = min(kCountSpan, a.chunk_blocks - first);
+    int* own = hist[warp];
+    for (int i = lane; i < n; i += 32) own[i] = 0;
+    __syncwarp();
+    const int* ids = a.blocks + list * a.n_select;
+    for (int i = lane; i < a.n_select; i += 32) {
+      const int id = ids[i];
+      if (id >= a.ctx_blocks && id - a.ctx_blocks >= first && id - a.ctx_blocks < first + n)
+        atomicAdd(own + (id - a.ctx_blocks - first), 1);
+    }
+    __syncwarp();
+    const long long bh = list / a.q_tiles, qt = list - bh * a.q_tiles;
+    for (int i = lane; i < n; i += 32) a.counts[(bh * a.chunk_blocks + first + i) * a.q_tiles + qt] = own[i];
+    return;
+  }
+  constexpr int kLanes = D / 8, kPerPass = kPrepThreads / kLanes;
+  const int part = threadIdx.x % kLanes;
+  const long long row0 = (static_cast<long long>(blockIdx.x) - a.count_blocks) * (kPerPass * kDeltaRows) + threadIdx.x / kLanes;
+  uint4 x[kDeltaRows], y[kDeltaRows];
+#pragma unroll
+  for (int u = 0; u < kDeltaRows; ++u) {
+    const long long row = row0 + u * kPerPass;
+    if (row < a.rows) {
+      x[u] = *reinterpret_cast<const uint4*>(a.o + row * D + part * 8);
+      y[u] = *reinterpret_cast<const uint4*>(a.d_o + row * D + part * 8);
+    } else {
+      x[u] = y[u] = make_uint4(0, 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kDeltaRows; ++u) {
+    const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162*>(&x[u]), *q = reinterpret_cast<const __nv_bfloat162*>(&y[u]);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = __bfloat1622float2(p[e]), g = __bfloat1622float2(q[e]);
+      sum = fmaf(f.x, g.x, sum);
+      sum = fmaf(f.y, g.y, sum);
+    }
+#pragma unroll
+    for (int s = kLanes / 2; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    const long long row = row0 + u * kPerPass;
+    if (part == 0 && row < a.rows) {
+      const long long bi = row / a.heads, b = bi / a.n_q;
+      a.delta[(b * a.heads + (row - bi * a.heads)) * a.n_q + (bi - b * a.n_q)] = sum;
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------ dQ
@@ -70,6 +135,14 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
   constexpr uint32_t kColS = 0, kColdP = 128, kColdS = 256, kColQ = 320, kColdQ = 384;
   constexpr int kMmaWarp = 4 * kDqGroups, kTmaWarp = kMmaWarp + 1, kListWarp = kMmaWarp + 2;
 
+  // the list's first entries are on their way while barriers and tensor memory are set up
+  const int* list = a.blocks + ((static_cast<long long>(b) * a.heads + h) * a.q_tiles + qt) * a.n_select;
+  int first_entries = -1;
+  if (warp == kListWarp) first_entries = ListWalker::first_entries(list, a.n_select, lane);
+  if (warp == kTmaWarp && lane == 0) {
+    tma_prefetch_desc(&maps.kx); tma_prefetch_desc(&maps.vx); tma_prefetch_desc(&maps.kc); tma_prefetch_desc(&maps.vc);
+    tma_prefetch_desc(&tm_do);
+  }
   if (tid == 0) {
     mbar_init(kv0_full, 1);
     mbar_init(qt_full, 128 * (D / 64));
@@ -93,12 +166,13 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_holder;
+  dependents_may_start();
   // a descriptor's reading, and its return (a warp's readers return it together)
   auto await_listed = [&](int j) { return mbar_wait_spin(listed + j % kSpDescs, (j / kSpDescs) & 1, abort_flag); };
 
   if (warp == kListWarp) {
     ListWalker w;
-    w.open(geom, a.blocks + ((static_cast<long long>(b) * a.heads + h) * a.q_tiles + qt) * a.n_select, a.n_select, lane);
+    w.open(geom, list, a.n_select, lane, first_entries);
     for (int j = 0;; ++j) {
       if (!mbar_wait(unlisted + j % kSpDescs, ((j / kSpDescs) & 1) ^ 1, abort_flag)) break;
       uint32_t valid;
@@ -191,10 +265,12 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
     const int row = q0 + r;
     const bool in_range = row < a.n_q;
     const size_t stat_idx = (static_cast<size_t>(b) * a.heads + h) * a.n_q + (in_range ? row : 0);
+    dependency_wait();   // delta
     const float lse2 = in_range ? a.lse[stat_idx] * kLog2e : 0.f;
     const float delta_r = in_range ? a.delta[stat_idx] : 0.f;
     const float scale_log2 = a.scale * kLog2e;
     const uint64_t sc2 = f32x2(scale_log2, scale_log2), nl2 = f32x2(-lse2, -lse2), nd2 = f32x2(-delta_r, -delta_r);
+    const bool idle = q0 + (warp & 3) * 32 >= a.n_q;   // no query among the warp's rows: it only keeps the hand-offs going
     if (g * 64 < D) {   // Q row -> tensor memory: group g writes elements [64g, 64g+64) of its row as 32 packed columns
       uint32_t qr[32];
       const QuadRows q_rows = quad_rows(a.q, b, h, a.n_q, a.heads, D, row);
@@ -222,6 +298,13 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
       if (lane == 0) mbar_arrive(unlisted + j % kSpDescs);
       ok = mbar_wait(s_full, j & 1, abort_flag) && ok;
       tc_fence_after_sync();
+      if (idle) {   // rows of an MMA do not mix: what dS holds here ends in rows of dQ that nobody stores
+        mbar_arrive(rs + j % 4);
+        ok = mbar_wait(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
+        mbar_arrive(rb + j % 4);
+        if ((flags & kTileLast) || !__all_sync(0xffffffffu, ok)) break;
+        continue;
+      }
       uint32_t s[2][32];
       tmem_ld32(tmem_lane + kColS + g * kDqCols, s[0]);
       tmem_ld32(tmem_lane + kColS + g * kDqCols + 32, s[1]);
@@ -345,6 +428,7 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
   geom.per_tile = 1;
   zero_uncovered_rows<D>(sK, 2, geom, tid, kDkvThreads);   // K and V of the block follow each other
   fence_proxy_async_smem();
+  dependency_wait();   // counts and delta
   if (warp == kTmaWarp) {
     int n = 0;
     for (int t = lane; t < a.q_tiles; t += 32) n += counts[t];

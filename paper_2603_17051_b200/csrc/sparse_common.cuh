@@ -51,7 +51,8 @@ struct TileDesc {
   uint32_t flags;
 };
 constexpr uint32_t kTileThere = 1u, kTileFirst = 2u, kTileLast = 4u, kTileEnd = 8u;   // first / last of its unit; last of all
-constexpr uint32_t kTileFull = 0x20202020u;
+constexpr int kTileLiveShift = 8;   // bits 8..10: quarters (32 rows) of the query tile that hold a query, 1..4
+__device__ __forceinline__ uint32_t live_quarters(int n_q, int qt) { return (min(kTile, n_q - qt * kTile) + 31) / 32; }
 
 // Where the producer finds the blocks of a tile.
 struct TileSource {
@@ -76,15 +77,17 @@ struct ListWalker {
       if (ok) ref = block_ref(g, id);
     }
   }
-  __device__ void open(const SparseGeom& g, const int* entries, int count, int lane_) {
+  // Opens a list whose first 32 entries have been asked for before (first_entries).
+  __device__ void open(const SparseGeom& g, const int* entries, int count, int lane_, int first) {
     list = entries;
     n = count;
     pos = 0;
     lane = lane_;
     mask = 0;
-    ahead = lane < n ? list[lane] : -1;
+    ahead = first;
     fetch(g);
   }
+  static __device__ int first_entries(const int* entries, int count, int lane) { return lane < count ? entries[lane] : -1; }
   __device__ bool done() const { return mask == 0; }
   __device__ BlockRef take(const SparseGeom& g) {
     const int from = __ffs(mask) - 1;

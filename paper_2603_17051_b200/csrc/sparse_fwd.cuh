@@ -77,41 +77,38 @@ template <int D> struct SparseCta {
   uint32_t tmem_base;
 };
 
-// The units of a CTA as one stream of tiles (producer warp, all lanes).
+// The units of a CTA as one stream of tiles (list warp, all lanes).  The first entries of the next unit's list are
+// asked for when a unit is opened.
 struct SparseStream {
   ListWalker w;
-  int unit, h, b, bx;
+  const int* list;        // of the unit to open next
+  int unit, count, first; // its id, length and first entries
+  int h, b, bx;           // of the open unit
+  uint32_t live;
   bool opens;
+  // `unit` is the one to open next: where its list is, and its first entries
+  __device__ void look_up(const SparseUnits& s, const SparseFwdArgs& a, int lane) {
+    if (unit >= s.total) return;
+    const SparseUnit u(s, unit, a.heads, a.batch);
+    const int from = u.split * s.entries;
+    list = a.blocks + ((static_cast<long long>(u.b) * a.heads + u.h) * s.q_tiles + u.qt) * s.n_select + from;
+    count = max(0, min(s.entries, s.n_select - from));
+    first = ListWalker::first_entries(list, count, lane);
+  }
+  __device__ void start(const SparseUnits& s, const SparseFwdArgs& a, int unit_, int lane) {
+    unit = unit_;
+    look_up(s, a, lane);
+  }
   __device__ void open(const SparseGeom& g, const SparseUnits& s, const SparseFwdArgs& a, int lane) {
     const SparseUnit u(s, unit, a.heads, a.batch);
     h = u.h;
     b = u.b;
     bx = s.cache_shared ? 0 : u.b;
-    const int from = u.split * s.entries;
-    const int* list = a.blocks + ((static_cast<long long>(b) * a.heads + h) * s.q_tiles + u.qt) * s.n_select + from;
-    w.open(g, list, max(0, min(s.entries, s.n_select - from)), lane);
+    live = live_quarters(a.n_q, u.qt) << kTileLiveShift;
+    w.open(g, list, count, lane, first);
     opens = true;
-  }
-  // tile J: descriptor and source (lane 0 writes them); false when the stream is over
-  __device__ bool next(const SparseGeom& g, const SparseUnits& s, const SparseFwdArgs& a, int J, TileDesc* desc,
-                       TileSource* source, int lane) {
-    if (unit >= s.total) {
-      if (lane == 0) desc[J % kSpDescs].flags = 0;
-      return false;
-    }
-    uint32_t valid;
-    const bool last = next_tile(g, w, h, b, bx, source + J % kSpDescs, valid);
-    const bool end = last && unit + s.stride >= s.total;
-    if (lane == 0) {
-      desc[J % kSpDescs].valid = valid;
-      desc[J % kSpDescs].flags = kTileThere | (opens ? kTileFirst : 0u) | (last ? kTileLast : 0u) | (end ? kTileEnd : 0u);
-    }
-    opens = false;
-    if (last) {
-      unit += s.stride;
-      if (unit < s.total) open(g, s, a, lane);
-    }
-    return true;
+    unit += s.stride;
+    look_up(s, a, lane);
   }
 };
 
@@ -124,7 +121,7 @@ struct SparseBars : FwdFastBars {
   __device__ void init(int q_count) const {
     mbar_init(q_full, q_count);
     mbar_init(q_full + 1, q_count);
-    mbar_init(k01, 1);
+    mbar_init(k01, 2);
     for (int i = 0; i < 4; ++i) {
       mbar_init(ready + i, 2 + 128 * kFwdGroups);
       mbar_init(sdone + i, 1);
@@ -169,15 +166,34 @@ __device__ __forceinline__ void sparse_s(uint32_t scol, uint32_t qcol, uint64_t 
 // (The wait names the barrier that S(J) will use next, so its phase cannot run ahead of it.)
 template <int D>
 __device__ __forceinline__ void sparse_walk(const SparseCta<D>& c, const SparseGeom& g, const SparseUnits& s, const SparseFwdArgs& a,
-                                            const SparseBars& bar, int lane) {
-  SparseStream st;
-  st.unit = s.first;
-  st.open(g, s, a, lane);
-  int behind = 0;   // descriptors behind the last tile: the issuer looks two ahead
-  for (int J = 0; behind < 2; ++J) {
-    if (J >= 4 && !mbar_wait(bar.sdone + J % 4, ((J - 4) / 4) & 1, c.abort_flag)) break;
-    if (!st.next(g, s, a, J, c.desc, c.source, lane)) ++behind;
-    if (lane == 0) mbar_arrive(bar.listed + J % kSpDescs);
+                                            const SparseBars& bar, SparseStream& st, int lane) {
+  int J = 0;
+  bool over = false;
+  // a slot of the rings; false once a wait has run out
+  auto slot = [&]() { return J < 4 || mbar_wait(bar.sdone + J % 4, ((J - 4) / 4) & 1, c.abort_flag); };
+  while (!over) {
+    st.open(g, s, a, lane);
+    const bool last_unit = st.unit >= s.total;
+    for (bool last = false; !last; ++J) {
+      if (!slot()) return;
+      uint32_t valid;
+      last = next_tile(g, st.w, st.h, st.b, st.bx, c.source + J % kSpDescs, valid);
+      if (lane == 0) {
+        c.desc[J % kSpDescs].valid = valid;
+        c.desc[J % kSpDescs].flags = kTileThere | (st.opens ? kTileFirst : 0u) | (last ? kTileLast : 0u) |
+                                     (last && last_unit ? kTileEnd : 0u) | st.live;
+        mbar_arrive(bar.listed + J % kSpDescs);
+      }
+      st.opens = false;
+    }
+    over = last_unit;
+  }
+  for (int behind = 0; behind < 2; ++behind, ++J) {   // behind the last tile: the issuer looks two ahead
+    if (!slot()) return;
+    if (lane == 0) {
+      c.desc[J % kSpDescs].flags = 0;
+      mbar_arrive(bar.listed + J % kSpDescs);
+    }
   }
 }
 
@@ -191,12 +207,18 @@ __device__ __forceinline__ void sparse_load_k(const SparseCta<D>& c, const Spars
   auto load = [&](int J, uint64_t* full) {
     load_sparse_tile<D>(c.sK + (J % kFwdKStages) * TileGeom<D>::kBytes, &maps.kx, &maps.kc, full, c.source + J % kSpDescs, g);
   };
-  if (!listed(0) || !listed(1)) return;
-  const bool two = desc[1].flags & kTileThere;
-  mbar_arrive_expect_tx(bar.k01, (two ? 2 : 1) * bytes);
+  if (!listed(0)) return;
+  uint32_t now = desc[0].flags, next = 0;
+  mbar_arrive_expect_tx(bar.k01, bytes);
   load(0, bar.k01);
-  if (two) load(1, bar.k01);
-  uint32_t now = desc[0].flags, next = desc[1].flags;
+  if (!listed(1)) return;
+  next = desc[1].flags;
+  if (next & kTileThere) {
+    mbar_arrive_expect_tx(bar.k01, bytes);
+    load(1, bar.k01);
+  } else {
+    mbar_arrive(bar.k01);
+  }
   for (int J = 0; now & kTileThere; ++J) {
     if (!listed(J + 2)) break;
     const uint32_t later = desc[(J + 2) % kSpDescs].flags;
@@ -368,6 +390,20 @@ __device__ __noinline__ SparseRun sparse_run(SparseLoop c, float scale_log2, flo
   return SparseRun{l_run, J, d, ok};
 }
 
+// The whole of a unit for a warp whose quarter of the query tile holds no query: it keeps the hand-offs going and leaves S
+// where P would be.  Rows of an MMA do not mix, so what comes of it stays in rows that nobody stores.
+__device__ __noinline__ SparseRun sparse_idle(SparseLoop c, int J, TileDesc d) {
+  bool ok = true;
+  while (true) {
+    ok = mbar_wait_at(c.sdone + 8 * (J % 4), (J / 4) & 1, c.abort_flag);
+    mbar_arrive_at(c.ready + 8 * (J % 4));
+    if ((d.flags & kTileLast) || !ok) break;
+    ++J;
+    d = await_desc(c, J);
+  }
+  return SparseRun{1.f, J, d, ok};
+}
+
 template <int D>
 __device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const SparseBars& bar, int warp, int r, float scale_log2) {
   const int g = warp >> 2;
@@ -381,11 +417,24 @@ __device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const Spar
   lp.g = g;
   TileDesc d = await_desc(lp, 0);
   int J = 0;
+  int maxima = 0;   // units for which this warp has met the other groups over the row maxima
   for (int n = 0;; ++n) {
+    float m_ref = 0.f, l_run;
+    uint32_t flags = d.flags;
+    bool ok;
+    TileDesc next;
+    if ((flags >> kTileLiveShift & 7u) <= static_cast<uint32_t>(warp & 3)) {
+      const SparseRun run = sparse_idle(lp, J, d);
+      l_run = run.l_run;
+      J = run.J;
+      flags = run.d.flags;
+      ok = run.ok;
+      next = await_desc(lp, J + 1);
+    } else {
     // the unit's first tile fixes the rows' reference
     const int valid = (d.valid >> (8 * g)) & 0xff;
     const uint32_t colS = lp.lane_s + (J % kFwdSBufs) * 128;
-    bool ok = mbar_wait_at(lp.sdone + 8 * (J % 4), (J / 4) & 1, lp.abort_flag);
+    ok = mbar_wait_at(lp.sdone + 8 * (J % 4), (J / 4) & 1, lp.abort_flag);
     tc_fence_after_sync();
     uint32_t s[32], pk[16];
     tmem_ld32(colS, s);
@@ -394,17 +443,17 @@ __device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const Spar
     float mx = row_max(s, valid);
     slot[g * kTile + r] = mx;
     mbar_arrive(bar.max_full + (warp & 3));
-    ok = mbar_wait(bar.max_full + (warp & 3), n & 1, abort_flag) && ok;
+    ok = mbar_wait(bar.max_full + (warp & 3), maxima & 1, abort_flag) && ok;
+    ++maxima;
 #pragma unroll
     for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
-    const float m_ref = mx == -INFINITY ? 0.f : mx * scale_log2;   // no key in an empty list's tile
-    float l_run = sparse_exp32(s, valid, scale_log2, -m_ref, pk);
+    m_ref = mx == -INFINITY ? 0.f : mx * scale_log2;   // no key in an empty list's tile
+    l_run = sparse_exp32(s, valid, scale_log2, -m_ref, pk);
     tmem_st16(colS, pk);
     tmem_wait_st();
     tc_fence_before_sync();
     mbar_arrive_at(lp.ready + 8 * (J % 4));
-    uint32_t flags = d.flags;
-    TileDesc next = await_desc(lp, J + 1);
+    next = await_desc(lp, J + 1);
     if (ok && !(flags & kTileLast)) {
       const SparseRun run = sparse_run(lp, scale_log2, -m_ref, l_run, J + 1, next);
       l_run = run.l_run;
@@ -412,6 +461,7 @@ __device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const Spar
       flags = run.d.flags;
       ok = run.ok;
       next = await_desc(lp, J + 1);
+    }
     }
     // the slots of unit n - 2 are free: the epilogue warps read them before they let go of that unit's O, which the
     // first P V of unit n - 1 waited for
@@ -515,7 +565,7 @@ __device__ __forceinline__ void sparse_epilogue(const SparseCta<D>& c, const Spa
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) row.store(acc[i], inv, chk2, (half * kOwn + i) * 32, lane);
     if (half == 0) row.store_lse(m, l);
-    if (!fwd_all_finite(chk2)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));
+    if (row.in_range && !fwd_all_finite(chk2)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));
     if (s.total - unit > 2 * s.stride) stage_q(unit + 2 * s.stride, n & 1);
   }
 }
@@ -536,7 +586,7 @@ __device__ __noinline__ void sparse_careful_unit(const SparseCta<D>& c, const Sp
   const SparseRow<D> row(s, u, a, r);
   SparseStream st;
   if (warp == kTmaWarp) {
-    st.unit = unit;
+    st.start(s, a, unit, lane);
     st.open(g, s, a, lane);
   }
   if (softmax && grp < D / 64) row.stage_q(tmem_lane + kFwdColQ, grp, lane);
@@ -662,6 +712,12 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
   s.first = blockIdx.x;
   s.stride = gridDim.x;
 
+  // the first list's entries are on their way while barriers and tensor memory are set up
+  SparseStream stream;
+  if (warp == kTmaWarp) stream.start(s, a, s.first, lane);
+  if (warp == kKWarp && lane == 0) {
+    tma_prefetch_desc(&maps.kx); tma_prefetch_desc(&maps.vx); tma_prefetch_desc(&maps.kc); tma_prefetch_desc(&maps.vc);
+  }
   if (tid == 0) {
     bar.init(128 * (D / 64));
     for (int i = 0; i < 3; ++i) mbar_init(careful_bars + i, 1);
@@ -680,9 +736,10 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
   __syncthreads();
   tc_fence_after_sync();
   c.tmem_base = *tmem_holder;
+  dependents_may_start();
 
   if (!a.careful) {
-    if (warp == kTmaWarp) sparse_walk<D>(c, g, s, a, bar, lane);
+    if (warp == kTmaWarp) sparse_walk<D>(c, g, s, a, bar, stream, lane);
     else if (warp == kKWarp) { if (lane == 0) sparse_load_k<D>(c, g, maps, bar); }
     else if (warp == kVWarp) { if (lane == 0) sparse_load_v<D>(c, g, maps, bar); }
     else if (warp == kMmaWarp) { if (lane == 0) sparse_issue<D>(c, bar); }
@@ -713,6 +770,7 @@ sparse_combine_kernel(const float* __restrict__ part_o, const float* __restrict_
                       const long long rows, const int n_q, const int heads, __nv_bfloat16* __restrict__ o,
                       float* __restrict__ lse) {
   constexpr int kPer = D / 32;
+  dependency_wait();
   const long long at = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
   if (at >= rows) return;
