@@ -145,8 +145,8 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
   }
   if (tid == 0) {
     mbar_init(kv0_full, 1);
-    mbar_init(qt_full, 128 * (D / 64));
-    for (int i = 0; i < 4; ++i) { mbar_init(rs + i, 1 + kDqSoftmaxThreads); mbar_init(rb + i, 1 + kDqSoftmaxThreads); }
+    mbar_init(qt_full, 4 * (D / 64));
+    for (int i = 0; i < 4; ++i) { mbar_init(rs + i, 1 + 4 * kDqGroups); mbar_init(rb + i, 1 + 4 * kDqGroups); }   // bytes, warps
     mbar_init(s_full, 1);
     mbar_init(b_done, 1);
     mbar_init(b_done + 1, 1);
@@ -287,7 +287,7 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
       tmem_st32(tmem_lane + kColQ + g * 32, qr);
       tmem_wait_st();
       tc_fence_before_sync();
-      mbar_arrive(qt_full);
+      warp_arrive(qt_full, lane);
     }
     static_assert(kDqCols == 64, "two 32-key pieces per thread and tile");
     for (int j = 0;; ++j) {
@@ -299,9 +299,9 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
       ok = mbar_wait(s_full, j & 1, abort_flag) && ok;
       tc_fence_after_sync();
       if (idle) {   // rows of an MMA do not mix: what dS holds here ends in rows of dQ that nobody stores
-        mbar_arrive(rs + j % 4);
+        warp_arrive(rs + j % 4, lane);
         ok = mbar_wait(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
-        mbar_arrive(rb + j % 4);
+        warp_arrive(rb + j % 4, lane);
         if ((flags & kTileLast) || !__all_sync(0xffffffffu, ok)) break;
         continue;
       }
@@ -310,7 +310,7 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
       tmem_ld32(tmem_lane + kColS + g * kDqCols + 32, s[1]);
       tmem_wait_ld();
       tc_fence_before_sync();
-      mbar_arrive(rs + j % 4);
+      warp_arrive(rs + j % 4, lane);
       uint64_t p2[2][16];
 #pragma unroll
       for (int c2 = 0; c2 < 2; ++c2)
@@ -349,7 +349,7 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
       }
       tmem_wait_st();
       tc_fence_before_sync();
-      mbar_arrive(rb + j % 4);   // dS(j) stored; dP(j) was read before it, so its buffer is free as well
+      warp_arrive(rb + j % 4, lane);   // dS(j) stored; dP(j) was read before it, so its buffer is free as well
       if ((flags & kTileLast) || !__all_sync(0xffffffffu, ok)) break;
     }
     mbar_wait(dq_full, 0, abort_flag);
@@ -416,8 +416,8 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     for (int i = 0; i < kDkvStages; ++i) { mbar_init(q_full + i, 2); mbar_init(q_empty + i, 1); }
     mbar_init(s_full, 1);
     mbar_init(dp_full, 1);
-    mbar_init(p_full, 256);
-    mbar_init(ds_full, 256);
+    mbar_init(p_full, 8);    // one arrival per warp
+    mbar_init(ds_full, 8);
     mbar_init(acc_full, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -561,7 +561,7 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
       tmem_st32(tmem_lane + kColSt + g * 64, pt);
       tmem_wait_st();
       tc_fence_before_sync();
-      mbar_arrive(p_full);
+      warp_arrive(p_full, lane);
 
       mbar_wait(dp_full, i & 1, abort_flag);
       tc_fence_after_sync();
@@ -582,7 +582,7 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
       }
       tmem_wait_st();
       tc_fence_before_sync();
-      mbar_arrive(ds_full);
+      warp_arrive(ds_full, lane);
     }
     // the rows of a quad that are keys of this block
     auto rows_of = [&](__nv_bfloat16* base) {
