@@ -19,6 +19,7 @@
 #include "nft_loss.cuh"
 #include "rope.cuh"
 #include "sparse_bwd.cuh"
+#include "sparse_decode.cuh"
 #include "sparse_fwd.cuh"
 
 using namespace astro;
@@ -553,7 +554,7 @@ SparseSplit sparse_split(int batch, int heads, int n_q, int n_select, int block_
   const int per_tile = kTile / sparse_pad(block_tokens);
   const int tiles = (n_select - 1) / per_tile + 1;
   SparseSplit r{1, n_select};
-  if (units * 2 > kSms || tiles < 12) return r;
+  if (n_q <= kDecodeMaxQueries || units * 2 > kSms || tiles < 12) return r;   // one or two queries: a kernel of their own
   int want = static_cast<int>(kSms / units);
   if (want > tiles / 4) want = tiles / 4;
   const int each = (tiles - 1) / want + 1;   // tiles of a range
@@ -562,9 +563,70 @@ SparseSplit sparse_split(int batch, int heads, int n_q, int n_select, int block_
   return r;
 }
 
+// One or two queries per sample: a cluster of CTAs per list (3 and more queries go to the MMA kernel: every query costs this
+// one as much arithmetic as the first).  Clusters do not straddle the GPU's processing clusters, so fewer fit than the
+// number of SMs says (48 of three CTAs do not): the size is chosen from what the runtime says fits at a time, to need the
+// least rounds * (tiles of a CTA + 8, a CTA's start and end being worth about 8 tiles).
+template <int D, int R>
+astro_status_t launch_sparse_decode(const SparseCall& c, const SparseGeom& g, float scale, void* o, float* lse, cudaStream_t st) {
+  SparseMaps maps;
+  astro_status_t s = sparse_maps(c, g, &maps);
+  if (s != ASTRO_OK) return s;
+  static std::atomic<int> done[kMaxDevices];
+  constexpr int kSmem = DecodeSmem<D, R>::kTotal, kThreads = DecodeShape<R>::kThreads;
+  if ((s = set_smem_once(sparse_decode_kernel<D, R>, kSmem, done)) != ASTRO_OK) return s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  static std::atomic<int> fits[kMaxDevices][kDecodeMaxCluster + 1];   // clusters of a size at a time, + 1
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return ASTRO_ERR_CUDA;
+  const long long lists = static_cast<long long>(c.a.batch) * c.a.heads;
+  const int tiles = (c.n_select - 1) / g.per_tile + 1;
+  int parts = 1;
+  long long least = 0;
+  for (int p = 1; p <= kDecodeMaxCluster && p <= tiles; ++p) {
+    int n = fits[dev][p].load(std::memory_order_acquire) - 1;
+    if (n < 0) {
+      attr.val.clusterDim.x = p;
+      cfg.gridDim = dim3(p, 1, 1);
+      if (cudaOccupancyMaxActiveClusters(&n, sparse_decode_kernel<D, R>, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        n = 0;
+      }
+      fits[dev][p].store(n + 1, std::memory_order_release);
+    }
+    if (n < 1) continue;
+    const long long cost = ((lists + n - 1) / n) * ((tiles + p - 1) / p + 8);
+    if (p == 1 || cost < least) { parts = p; least = cost; }
+  }
+  DecodeArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(c.q);
+  a.blocks = c.blocks;
+  a.o = static_cast<__nv_bfloat16*>(o);
+  a.lse = lse;
+  a.batch = c.a.batch; a.heads = c.a.heads;
+  a.n_select = c.n_select;
+  a.entries = (tiles + parts - 1) / parts * g.per_tile;
+  a.cache_shared = (c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1) ? 1 : 0;
+  a.scale_log2 = scale * kLog2e;
+  attr.val.clusterDim.x = static_cast<unsigned>(parts);
+  cfg.gridDim = dim3(static_cast<unsigned>(parts), c.a.heads, c.a.batch);
+  return cudaLaunchKernelEx(&cfg, sparse_decode_kernel<D, R>, maps, a, g) == cudaSuccess ? launch_status() : ASTRO_ERR_CUDA;
+}
+
 template <int D>
 astro_status_t launch_sparse_fwd(const SparseCall& c, const SparseGeom& g, float scale, void* o, float* lse, void* workspace,
                                  cudaStream_t st) {
+  const bool careful = g_fwd_mode.load(std::memory_order_relaxed) == 1;   // reaches the MMA kernel's careful pass
+  if (c.a.n_q == 1 && !careful) return launch_sparse_decode<D, 1>(c, g, scale, o, lse, st);
+  if (c.a.n_q == 2 && !careful) return launch_sparse_decode<D, 2>(c, g, scale, o, lse, st);
   SparseMaps maps;
   astro_status_t s = sparse_maps(c, g, &maps);
   if (s != ASTRO_OK) return s;
@@ -581,7 +643,7 @@ astro_status_t launch_sparse_fwd(const SparseCall& c, const SparseGeom& g, float
   a.part_lse = a.part_o + (split.splits > 1 ? split.splits * rows * D : 0);
   a.batch = c.a.batch; a.heads = c.a.heads; a.n_q = c.a.n_q;
   a.scale_log2 = scale * kLog2e;
-  a.careful = g_fwd_mode.load(std::memory_order_relaxed) == 1 ? 1 : 0;
+  a.careful = careful ? 1 : 0;
   SparseUnits u;
   u.q_tiles = (c.a.n_q - 1) / kTile + 1;
   u.cache_shared = (c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1) ? 1 : 0;

@@ -83,6 +83,11 @@ SHAPES = [  # Bc, B, H, D, T, S, L, evicted, held, n_q, n_kc, block, n_select
     (1, 1, 3, 64, 130, 0, 4, 1, 3, 200, 77, 40, 14),
     (1, 4, 12, 128, 61, 0, 30, 5, 28, 3, 2, 32, 57),
     (1, 1, 1, 64, 1, 0, 40, 7, 33, 1, 0, 128, 33),
+    (1, 3, 2, 128, 70, 1, 5, 2, 6, 2, 1, 64, 13),
+    (2, 2, 5, 64, 97, 0, 12, 4, 12, 1, 1, 96, 20),
+    (1, 1, 1, 128, 50, 0, 30, 3, 30, 2, 0, 8, 200),
+    (1, 5, 33, 64, 31, 0, 4, 1, 4, 1, 3, 32, 5),
+    (1, 1, 2, 128, 80, 2, 9, 3, 11, 5, 4, 40, 22),
 ]
 
 
@@ -180,10 +185,10 @@ def test_refusals_of_the_forward():
             run(**bad)
         assert e.value.status == status
     few = torch.zeros(1, 2, 1, 40, dtype=torch.int32, device="cuda")
-    need = A.astro_sparse_attn_fwd_workspace_bytes(1, 2, 64, 1, 40, 64)
-    assert need > 0
+    need = A.astro_sparse_attn_fwd_workspace_bytes(1, 2, 64, 5, 40, 64)
+    assert need > 0 and A.astro_sparse_attn_fwd_workspace_bytes(1, 2, 64, 1, 40, 64) == 0
     with pytest.raises(A.AstroError) as e:
-        run(q=q[:, :1].contiguous(), blocks=few, workspace=torch.empty(need - 4, dtype=torch.uint8, device="cuda"))
+        run(q=q[:, :5].contiguous(), blocks=few, workspace=torch.empty(need - 4, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 4
 
 
