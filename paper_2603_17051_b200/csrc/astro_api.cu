@@ -686,9 +686,8 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
   CUtensorMap tq, tdo;
   if ((s = make_tmap_user(&tq, c.q, D, c.a.n_q, c.a.heads, c.a.batch)) != ASTRO_OK) return s;
   if ((s = make_tmap_user(&tdo, d_o, D, c.a.n_q, c.a.heads, c.a.batch)) != ASTRO_OK) return s;
-  static std::atomic<int> done_q[kMaxDevices], done_kv[kMaxDevices];
-  if ((s = set_smem_once(sparse_attn_bwd_dq_kernel<D>, SdqSmem<D>::kTotal, done_q)) != ASTRO_OK) return s;
-  if ((s = set_smem_once(sparse_attn_bwd_dkv_kernel<D>, DkvSmem<D>::kTotal, done_kv)) != ASTRO_OK) return s;
+  static std::atomic<int> done[kMaxDevices];
+  if ((s = set_smem_once(sparse_attn_bwd_kernel<D>, sparse_bwd_smem<D>(), done)) != ASTRO_OK) return s;
   const SparseBwdScratch need = sparse_bwd_scratch(c.a.batch, c.a.heads, c.a.n_q, c.a.n_kc, c.block_tokens);
   float* delta = static_cast<float*>(workspace);
   int* counts = reinterpret_cast<int*>(static_cast<char*>(workspace) + need.delta);
@@ -710,7 +709,8 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
   p.count_blocks = (p.lists * p.spans + kPrepThreads / 32 - 1) / (kPrepThreads / 32);
   const long long per_block = static_cast<long long>(kPrepThreads) * 8 / D * kDeltaRows;
   const long long prep_blocks = p.count_blocks + (p.rows + per_block - 1) / per_block;
-  if (prep_blocks > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
+  const long long heads = static_cast<long long>(c.a.batch) * c.a.heads, ctas = heads * (q_tiles + chunk_blocks);
+  if (prep_blocks > 0x7fffffffLL || ctas > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
   sparse_bwd_prep_kernel<D><<<static_cast<unsigned>(prep_blocks), kPrepThreads, 0, st>>>(p);
   if ((s = launch_status()) != ASTRO_OK) return s;
   SparseBwdArgs a;
@@ -718,15 +718,12 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
   a.blocks = c.blocks;
   a.lse = lse;
   a.delta = delta;
+  a.dq = static_cast<__nv_bfloat16*>(dq);
   a.batch = c.a.batch; a.heads = c.a.heads; a.n_q = c.a.n_q;
   a.q_tiles = q_tiles;
   a.n_select = c.n_select;
   a.cache_shared = (c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1) ? 1 : 0;
   a.scale = scale;
-  dim3 grid_q(q_tiles, a.cache_shared ? c.a.batch : c.a.heads, a.cache_shared ? c.a.heads : c.a.batch);
-  s = launch_dependent(sparse_attn_bwd_dq_kernel<D>, grid_q, kSdqThreads, SdqSmem<D>::kTotal, st, maps, tdo, g, a,
-                       static_cast<__nv_bfloat16*>(dq));
-  if (s != ASTRO_OK || chunk_blocks == 0) return s;
   SparseDkvArgs k;
   k.counts = counts;
   k.lse = lse;
@@ -736,9 +733,10 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
   k.block = c.block_tokens;
   k.chunk_blocks = chunk_blocks;
   k.scale = scale;
-  dim3 grid_k(chunk_blocks, c.a.heads, c.a.batch);
-  return launch_dependent(sparse_attn_bwd_dkv_kernel<D>, grid_k, kDkvThreads, DkvSmem<D>::kTotal, st, tq, tdo, maps.kc, maps.vc, k,
-                          static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv));
+  k.dk = static_cast<__nv_bfloat16*>(dk);
+  k.dv = static_cast<__nv_bfloat16*>(dv);
+  return launch_dependent(sparse_attn_bwd_kernel<D>, dim3(static_cast<unsigned>(ctas)), kSparseBwdThreads, sparse_bwd_smem<D>(), st,
+                          maps, tq, tdo, g, a, k, static_cast<int>(heads * q_tiles));
 }
 
 }  // namespace

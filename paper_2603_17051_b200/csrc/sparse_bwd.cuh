@@ -94,13 +94,14 @@ struct SparseBwdArgs {
   const __nv_bfloat16* q;
   const int* blocks;
   const float *lse, *delta;
+  __nv_bfloat16* dq;
   int batch, heads, n_q, q_tiles, n_select, cache_shared;
   float scale;
 };
 
 // A warp of its own follows the list and describes the tiles to come in a ring (listed: written; unlisted: everyone has
 // read it).  The rest is the dense dQ kernel with `last` read out of the descriptors.
-constexpr int kSdqThreads = kDqSoftmaxThreads + 96;   // MMA, loads, list
+constexpr int kSparseBwdThreads = kDqSoftmaxThreads + 96;   // MMA, loads, list
 
 template <int D> struct SdqSmem {
   static constexpr int kBars = DqSmem<D>::kBars;
@@ -110,11 +111,8 @@ template <int D> struct SdqSmem {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kSdqThreads, 1)
-sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_constant__ CUtensorMap tm_do,
-                          const __grid_constant__ SparseGeom geom, const __grid_constant__ SparseBwdArgs a,
-                          __nv_bfloat16* __restrict__ dq) {
-  extern __shared__ uint8_t smem_raw[];
+__device__ __forceinline__ void sparse_bwd_dq(uint8_t* smem_raw, const SparseMaps& maps, const CUtensorMap& tm_do,
+                                              const SparseGeom& geom, const SparseBwdArgs& a, const int qt, const int h, const int b) {
   uint8_t* smem = align_1024(smem_raw);
   uint8_t* sdO = smem + DqSmem<D>::kdO;
   uint8_t* sK = smem + DqSmem<D>::kK;
@@ -128,8 +126,7 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
   TileSource* source = reinterpret_cast<TileSource*>(smem + SdqSmem<D>::kSource);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int qt = blockIdx.x, q0 = qt * kTile;
-  const int h = a.cache_shared ? blockIdx.z : blockIdx.y, b = a.cache_shared ? blockIdx.y : blockIdx.z;
+  const int q0 = qt * kTile;
   const int bx = a.cache_shared ? 0 : b;
   constexpr uint32_t kTmemCols = 512;
   constexpr uint32_t kColS = 0, kColdP = 128, kColdS = 256, kColQ = 320, kColdQ = 384;
@@ -155,8 +152,8 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
     *abort_flag = 0;
     fence_mbar_init();
   }
-  zero_uncovered_rows<D>(sK, kDqKStages, geom, tid, kSdqThreads);
-  zero_uncovered_rows<D>(sV, kDqVStages, geom, tid, kSdqThreads);
+  zero_uncovered_rows<D>(sK, kDqKStages, geom, tid, kSparseBwdThreads);
+  zero_uncovered_rows<D>(sV, kDqVStages, geom, tid, kSparseBwdThreads);
   fence_proxy_async_smem();
   if (warp == kMmaWarp) {
     tmem_alloc(tmem_holder, kTmemCols);
@@ -354,7 +351,7 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
     }
     mbar_wait(dq_full, 0, abort_flag);
     tc_fence_after_sync();
-    store_rows_from_tmem<D / 2>(tmem_lane + kColdQ + g * (D / 2), a.scale, quad_rows(dq, b, h, a.n_q, a.heads, D, row),
+    store_rows_from_tmem<D / 2>(tmem_lane + kColdQ + g * (D / 2), a.scale, quad_rows(a.dq, b, h, a.n_q, a.heads, D, row),
                                 g * (D / 2), lane);
   }
 
@@ -367,6 +364,7 @@ sparse_attn_bwd_dq_kernel(const __grid_constant__ SparseMaps maps, const __grid_
 // ------------------------------------------------------------------------------------------ dK, dV
 struct SparseDkvArgs {
   const int* counts;     // [B][H][chunk blocks][q_tiles]
+  __nv_bfloat16 *dk, *dv;
   const float *lse, *delta;
   int heads, n_q, n_kc, q_tiles, block, chunk_blocks;
   float scale;
@@ -377,12 +375,9 @@ struct SparseDkvArgs {
 // list names gets zeros.  Blocks of fewer than 128 tokens leave rows of the key tile empty (zeros in shared memory): blocks of 64
 // cost twice the work, which a tile of several blocks could save only for query tiles that name all of them.
 template <int D>
-__global__ void __launch_bounds__(kDkvThreads, 1)
-sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do,
-                           const __grid_constant__ CUtensorMap tm_kc, const __grid_constant__ CUtensorMap tm_vc,
-                           const __grid_constant__ SparseDkvArgs a, __nv_bfloat16* __restrict__ dk,
-                           __nv_bfloat16* __restrict__ dv) {
-  extern __shared__ uint8_t smem_raw[];
+__device__ __forceinline__ void sparse_bwd_dkv(uint8_t* smem_raw, const CUtensorMap& tm_q, const CUtensorMap& tm_do,
+                                               const CUtensorMap& tm_kc, const CUtensorMap& tm_vc, const SparseDkvArgs& a,
+                                               const int cb, const int h, const int b) {
   uint8_t* smem = align_1024(smem_raw);
   uint8_t* sK = smem + DkvSmem<D>::kK;
   uint8_t* sV = smem + DkvSmem<D>::kV;
@@ -403,7 +398,6 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
   volatile int* tiles_holder = reinterpret_cast<volatile int*>(tmem_holder + 2);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int cb = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const int k0 = cb * a.block, keys = min(a.block, a.n_kc - k0);
   constexpr uint32_t kTmemCols = 512;
   constexpr uint32_t kColSt = 0, kColdPt = 128, kColdK = 256, kColdV = 384;
@@ -426,7 +420,7 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
   geom.kb.block = a.block;
   geom.pad = kTile;
   geom.per_tile = 1;
-  zero_uncovered_rows<D>(sK, 2, geom, tid, kDkvThreads);   // K and V of the block follow each other
+  zero_uncovered_rows<D>(sK, 2, geom, tid, kSparseBwdThreads);   // K and V of the block follow each other
   fence_proxy_async_smem();
   dependency_wait();   // counts and delta
   if (warp == kTmaWarp) {
@@ -524,7 +518,7 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
       }
       mma_commit(acc_full);
     }
-  } else {
+  } else if (warp < kMmaWarp) {
     const int g = warp >> 2;
     const int r = tid & 127;  // key row inside the tile = TMEM lane
     const uint32_t tmem_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -596,14 +590,14 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
     if (n_tiles > 0) {
       mbar_wait(acc_full, 0, abort_flag);
       tc_fence_after_sync();
-      store_rows_from_tmem<D / 2>(tmem_lane + kColdK + g * (D / 2), a.scale, rows_of(dk), g * (D / 2), lane);
-      store_rows_from_tmem<D / 2>(tmem_lane + kColdV + g * (D / 2), 1.f, rows_of(dv), g * (D / 2), lane);
+      store_rows_from_tmem<D / 2>(tmem_lane + kColdK + g * (D / 2), a.scale, rows_of(a.dk), g * (D / 2), lane);
+      store_rows_from_tmem<D / 2>(tmem_lane + kColdV + g * (D / 2), 1.f, rows_of(a.dv), g * (D / 2), lane);
     } else {
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
         uint4 zero[4] = {};
-        store_quad_rows(zero, rows_of(dk), g * (D / 2) + c * 32, lane);
-        store_quad_rows(zero, rows_of(dv), g * (D / 2) + c * 32, lane);
+        store_quad_rows(zero, rows_of(a.dk), g * (D / 2) + c * 32, lane);
+        store_quad_rows(zero, rows_of(a.dv), g * (D / 2) + c * 32, lane);
       }
     }
   }
@@ -612,6 +606,32 @@ sparse_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __gri
   tc_fence_before_sync();
   __syncthreads();
   if (warp == kMmaWarp) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+// Both in one launch: the first CTAs take the query tiles (the longer job), the others the chunk blocks.  Neither needs the
+// other, and one launch leaves no SM idle between them.
+template <int D>
+__global__ void __launch_bounds__(kSparseBwdThreads, 1)
+sparse_attn_bwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_constant__ CUtensorMap tm_q,
+                       const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ SparseGeom geom,
+                       const __grid_constant__ SparseBwdArgs a, const __grid_constant__ SparseDkvArgs k, const int q_ctas) {
+  extern __shared__ uint8_t smem_raw[];
+  int i = blockIdx.x;
+  if (i < q_ctas) {
+    const int qt = i % a.q_tiles;
+    i /= a.q_tiles;
+    // with one stored prefix for every sample, the samples of a head run next to each other (see the dense kernel)
+    const int inner = a.cache_shared ? a.batch : a.heads, y = i % inner, z = i / inner;
+    sparse_bwd_dq<D>(smem_raw, maps, tm_do, geom, a, qt, a.cache_shared ? z : y, a.cache_shared ? y : z);
+  } else {
+    i -= q_ctas;
+    const int cb = i % k.chunk_blocks;
+    i /= k.chunk_blocks;
+    sparse_bwd_dkv<D>(smem_raw, tm_q, tm_do, maps.kc, maps.vc, k, cb, i % k.heads, i / k.heads);
+  }
+}
+template <int D> constexpr int sparse_bwd_smem() {
+  return SdqSmem<D>::kTotal > DkvSmem<D>::kTotal ? SdqSmem<D>::kTotal : DkvSmem<D>::kTotal;
 }
 
 }  // namespace astro
