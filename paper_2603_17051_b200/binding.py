@@ -170,56 +170,71 @@ def _contiguous(*tensors):
             raise ValueError("tensor arguments must be contiguous")
 
 
-def _typed(kind, *tensors):
-    """Index and statistics tensors are read as the type their name says."""
-    for t in tensors:
-        if t is not None and t.dtype is not kind:
-            raise ValueError("expected a %s tensor, got %s" % (kind, t.dtype))
-
-
-def _here(stream, *tensors):
-    """Kernels run on the current device (and a given stream must belong to it): a tensor that lives elsewhere, on the
-    host included, is refused before its address reaches one.  Returns the stream's address."""
+def _where(stream, q):
+    """(device, stream address) of a call on q.  Kernels run on the current device, and a given stream must belong to it: a
+    tensor that lives elsewhere, on the host included, is refused before its address reaches one."""
     import torch
-    dev = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and (t.get_device() != dev or dev < 0):
-            raise ValueError("tensors on different devices, or on the host: %s" % [str(x.device) for x in tensors if x is not None])
-    if dev != torch.cuda.current_device():
-        raise ValueError("tensors on %s, the current device is %d" % (tensors[0].device, torch.cuda.current_device()))
+    dev = q.get_device()
+    if dev < 0:
+        raise ValueError("tensors must be on the GPU")
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError("tensors on cuda:%d, the current device is %d" % (dev, torch._C._cuda_getDevice()))
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev)
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
     if stream.device.index != dev:
         raise ValueError("the stream belongs to another device than the current one")
-    return stream.cuda_stream
+    return dev, stream.cuda_stream
+
+
+def _like(shape, kind, dev, *tensors):
+    """Tensors (None passes) that a kernel reads as contiguous ones of this shape and type on this device."""
+    for t in tensors:
+        if t is not None and (t.dtype is not kind or t.get_device() != dev or not t.is_contiguous() or t.shape != shape):
+            raise ValueError("expected a contiguous %s tensor %s on cuda:%d, got %s %s on %s%s" % (
+                kind, tuple(shape), dev, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
+
+
+def _scratch(workspace, dev):
+    """(address, bytes) of a workspace tensor."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous and on cuda:%d" % dev)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _handle(cache, dev):
+    if cache is None:
+        return None
+    if cache.k_storage.get_device() != dev or cache.v_storage.get_device() != dev:
+        raise ValueError("the cache is on %s, the call on cuda:%d" % (cache.k_storage.device, dev))
+    return cache.handle
 
 
 def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _chunk_shape(q, *chunk):
+def _chunk(q, dev, k_chunk, v_chunk, *others):
     """n_kc of the chunk tensors, which must fit q [B, n_q, H, D]."""
-    n_kc = 0
-    for t in chunk:
-        if t is not None:
-            if t.dim() != 4 or (t.shape[0], t.shape[2], t.shape[3]) != (q.shape[0], q.shape[2], q.shape[3]) or (n_kc and t.shape[1] != n_kc):
-                raise ValueError("chunk tensors must be [B, n_kc, H, D] like q")
-            n_kc = t.shape[1]
-    return n_kc
+    first = k_chunk if k_chunk is not None else v_chunk
+    if first is None:
+        return 0
+    s, (B, _, H, D) = first.shape, q.shape
+    if len(s) != 4 or s[0] != B or s[2] != H or s[3] != D:
+        raise ValueError("chunk tensors must be [B, n_kc, H, D] like q")
+    _like(s, q.dtype, dev, k_chunk, v_chunk, *others)
+    return s[1]
 
 
-def _sized(*pairs):
-    for t, n in pairs:
-        if t is not None and t.numel() != n:
-            raise ValueError("an output or saved tensor has %d elements, %d expected" % (t.numel(), n))
-
-
-def _numel(shape):
-    n = 1
-    for s in shape:
-        n *= s
-    return n
+def _lists(q, dev, blocks):
+    """n_select of blocks [B, H, query blocks, n_select], which must fit q."""
+    import torch
+    s, (B, n_q, H, _) = blocks.shape, q.shape
+    if len(s) != 4 or s[0] != B or s[1] != H or s[2] != (n_q + QUERY_BLOCK - 1) // QUERY_BLOCK:
+        raise ValueError("blocks must be [B, H, query blocks, n_select]")
+    _like(s, torch.int32, dev, blocks)
+    return s[3]
 
 
 def _used_on(stream, *tensors):
@@ -435,16 +450,15 @@ def astro_kvcache_fork(dst: KVCache, src: KVCache, parents=None, frames=None, st
     """Empty `dst` and copy the listed held frames of `src` (logical indices, None = all) into it; parents: int32 [dst
     cache_batch] on the device, the sample of src that each sample of dst continues."""
     import torch
-    _typed(torch.int32, parents)
-    _contiguous(parents)
-    st = _here(stream, dst.k_storage, dst.v_storage, src.k_storage, src.v_storage, parents)
-    if parents is not None and parents.numel() != dst.desc.cache_batch:
-        raise ValueError("parents must hold one entry per sample of the destination")
+    dev, on = _where(stream, dst.k_storage)
+    if parents is not None:
+        _like((dst.desc.cache_batch,), torch.int32, dev, parents)
     if frames is None:
         arr, n = None, -1
     else:
-        arr, n = (C.c_int * max(1, len(frames)))(*[int(f) for f in frames]), len(frames)
-    _check(lib().astro_kvcache_fork(dst.handle, src.handle, _at(parents), arr, n, st), "astro_kvcache_fork")
+        n = len(frames)
+        arr = (C.c_int * max(1, n))(*frames)
+    _check(lib().astro_kvcache_fork(_handle(dst, dev), _handle(src, dev), _at(parents), arr, n, on), "astro_kvcache_fork")
 
 
 ROPE_LAYOUTS = {"interleaved": 0, "halves": 1}
@@ -523,26 +537,25 @@ def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=N
     if len(shape) != 4 or shape[3] != rope.desc.head_dim:
         raise ValueError("q must be [B, n, heads, head_dim]")
     B, n, H, _ = shape
+    dev, on = _where(stream, q)
     fresh = []
     if q_out is None:
         q_out = _dense_like(q); fresh.append(q_out)
-    elif q_out.shape != shape or q_out.dtype is not q.dtype:
+    elif q_out.shape != shape or q_out.dtype is not q.dtype or q_out.get_device() != dev:
         raise ValueError("q_out must be like q")
     if k is not None:
-        if k.dim() != 4 or k.dtype is not q.dtype or k.shape[0] != B or k.shape[1] != n or k.shape[3] != shape[3]:
-            raise ValueError("k must be [B, n, heads, head_dim] of q's type")
+        if k.dim() != 4 or k.dtype is not q.dtype or k.shape[0] != B or k.shape[1] != n or k.shape[3] != shape[3] or k.get_device() != dev:
+            raise ValueError("k must be [B, n, heads, head_dim] of q's type, beside it")
         if k_out is None:
             k_out = _dense_like(k); fresh.append(k_out)
-        elif k_out.shape != k.shape or k_out.dtype is not k.dtype:
+        elif k_out.shape != k.shape or k_out.dtype is not k.dtype or k_out.get_device() != dev:
             raise ValueError("k_out must be like k")
     else:
         k_out = None
-    _typed(torch.int32, positions)
-    _contiguous(positions)
     pb = positions.shape[0]
-    if tuple(positions.shape) != (pb, n, rope.desc.axes) or (pb != 1 and pb != B):
+    if pb != 1 and pb != B:
         raise ValueError("positions must be [B or 1, n, axes]")
-    on = _here(stream, q, positions, q_out, k, k_out)
+    _like((pb, n, rope.desc.axes), torch.int32, dev, positions)
     _used_on(stream, *fresh)
 
     def call(x, x2, y, y2, strides):
@@ -591,17 +604,16 @@ def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_
     if n_frames is None:
         sink, win, _ = astro_kvcache_query(cache)
         n_frames = sink + win - int(first_frame)
+    dev, on = _where(stream, cache.k_storage)
+    if int(block_tokens) < 1:
+        raise AstroError(2, "astro_block_pool")
+    shape = _pooled_shape(cache, block_tokens)
     if pooled is None:
-        if int(block_tokens) < 1:
-            raise AstroError(2, "astro_block_pool")
-        pooled = torch.zeros(_pooled_shape(cache, block_tokens), dtype=torch.float32, device=cache.k_storage.device)
+        pooled = torch.zeros(shape, dtype=torch.float32, device=cache.k_storage.device)
         _used_on(stream, pooled)
-    _typed(torch.float32, pooled)
-    _contiguous(pooled)
-    st = _here(stream, pooled, cache.k_storage)
-    if int(block_tokens) >= 1 and pooled.numel() != _numel(_pooled_shape(cache, block_tokens)):
-        raise ValueError("pooled must be [B_c, H, S+L, blocks per frame, D]")
-    _check(lib().astro_block_pool(cache.handle, int(first_frame), int(n_frames), int(block_tokens), _at(pooled), st),
+    else:
+        _like(shape, torch.float32, dev, pooled)
+    _check(lib().astro_block_pool(_handle(cache, dev), int(first_frame), int(n_frames), int(block_tokens), _at(pooled), on),
            "astro_block_pool")
     return pooled
 
@@ -615,28 +627,24 @@ def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: i
     """int32 [B, H, ceil(n_q / QUERY_BLOCK), n_select]: per query block the key blocks of the highest scores, ascending,
     -1 behind them.  pooled: astro_block_pool's means of every held frame (None without a cache)."""
     import torch
+    dev, on = _where(stream, q)
     B, n_q, H, D = q.shape
-    n_kc = _chunk_shape(q, k_chunk)
-    shape = (B, H, -(-n_q // QUERY_BLOCK), max(1, int(n_select)))
+    _like(q.shape, torch.bfloat16, dev, q)
+    n_kc = _chunk(q, dev, k_chunk, None)
+    shape = (B, H, (n_q + QUERY_BLOCK - 1) // QUERY_BLOCK, max(1, int(n_select)))
     fresh = []
     if blocks is None:
         blocks = q.new_empty(shape, dtype=torch.int32); fresh.append(blocks)
+    else:
+        _like(shape, torch.int32, dev, blocks)
     if workspace is None:
         need = astro_block_select_workspace_bytes(B, H, D, n_q, n_kc, block_tokens)
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _typed(torch.int32, blocks)
-    _typed(torch.float32, pooled)
-    _typed(torch.bfloat16, q, k_chunk)
-    _contiguous(q, k_chunk, blocks, pooled, workspace)
-    on = _here(stream, q, k_chunk, blocks, pooled, workspace, None if cache is None else cache.k_storage)
-    if blocks.numel() != _numel(shape):
-        raise ValueError("blocks must be [B, H, query blocks, n_select]")
-    if cache is not None and pooled is not None and int(block_tokens) >= 1 and pooled.numel() != _numel(_pooled_shape(cache, block_tokens)):
-        raise ValueError("pooled must be [B_c, H, S+L, blocks per frame, D]")
+    if pooled is not None and cache is not None and int(block_tokens) >= 1:
+        _like(_pooled_shape(cache, block_tokens), torch.float32, dev, pooled)
     _used_on(stream, *fresh)
-    st = lib().astro_block_select(None if cache is None else cache.handle, _at(pooled), _at(q), _at(k_chunk), B, H, D, n_q,
-                                  n_kc, int(block_tokens), int(n_select), int(keep), _at(blocks), _at(workspace),
-                                  workspace.numel() * workspace.element_size(), on)
+    st = lib().astro_block_select(_handle(cache, dev), _at(pooled), _at(q), _at(k_chunk), B, H, D, n_q, n_kc, int(block_tokens),
+                                  int(n_select), int(keep), _at(blocks), *_scratch(workspace, dev), on)
     _check(st, "astro_block_select")
     return blocks
 
@@ -646,41 +654,32 @@ def astro_sparse_attn_fwd_workspace_bytes(batch, heads, head_dim, n_q, n_select,
                                                            int(block_tokens)))
 
 
-def _lists_shape(q, blocks):
-    """n_select of blocks [B, H, query blocks, n_select], which must fit q."""
-    B, n_q, H, _ = q.shape
-    if blocks.dim() != 4 or tuple(blocks.shape[:3]) != (B, H, -(-n_q // QUERY_BLOCK)):
-        raise ValueError("blocks must be [B, H, query blocks, n_select]")
-    return blocks.shape[3]
-
-
 def astro_sparse_attn_fwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int, scale: float, o=None, lse=None, workspace=None,
                           stream=None):
     """Attention of every query block over the key blocks its list names (blocks: int32 [B, H, ceil(n_q / QUERY_BLOCK),
     n_select] on the device, -1 for none); returns (O bf16, LSE fp32 [B, H, n_q]); a query without a key gets 0 and
     -infinity."""
     import torch
-    B, n_q, H, D = q.shape
-    n_kc, n_select = _chunk_shape(q, k_chunk, v_chunk), _lists_shape(q, blocks)
+    dev, on = _where(stream, q)
+    shape = q.shape
+    B, n_q, H, D = shape
+    _like(shape, torch.bfloat16, dev, q, o)
+    n_kc, n_select = _chunk(q, dev, k_chunk, v_chunk), _lists(q, dev, blocks)
     fresh = []
     if o is None:
         o = torch.empty_like(q); fresh.append(o)
     if lse is None:
         lse = q.new_empty((B, H, n_q), dtype=torch.float32); fresh.append(lse)
-    need = astro_sparse_attn_fwd_workspace_bytes(B, H, D, n_q, n_select, block_tokens)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _typed(torch.int32, blocks)
-    _typed(torch.float32, lse)
-    _typed(torch.bfloat16, q, k_chunk, v_chunk, o)
-    _contiguous(q, k_chunk, v_chunk, blocks, o, lse, workspace)
-    on = _here(stream, q, k_chunk, v_chunk, blocks, o, lse, workspace, None if cache is None else cache.k_storage)
-    _sized((o, q.numel()), (lse, B * H * n_q))
+    else:
+        _like((B, H, n_q), torch.float32, dev, lse)
+    if workspace is None:
+        need = astro_sparse_attn_fwd_workspace_bytes(B, H, D, n_q, n_select, block_tokens)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
     _used_on(stream, *fresh)
-    st = lib().astro_sparse_attn_fwd(None if cache is None else cache.handle, _at(q), _at(k_chunk), _at(v_chunk), _at(blocks),
-                                     n_select, int(block_tokens), B, H, D, n_q, n_kc, float(scale), _at(o), _at(lse),
-                                     _at(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                     on)
+    st = lib().astro_sparse_attn_fwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), _at(blocks), n_select,
+                                     int(block_tokens), B, H, D, n_q, n_kc, float(scale), _at(o), _at(lse),
+                                     *_scratch(workspace, dev), on)
     _check(st, "astro_sparse_attn_fwd")
     return o, lse
 
@@ -695,8 +694,12 @@ def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
     """Returns (dQ, dK_chunk, dV_chunk), bf16, of astro_sparse_attn_fwd with the same lists; the cached context receives no
     gradient."""
     import torch
-    B, n_q, H, D = q.shape
-    n_kc, n_select = _chunk_shape(q, k_chunk, v_chunk), _lists_shape(q, blocks)
+    dev, on = _where(stream, q)
+    shape = q.shape
+    B, n_q, H, D = shape
+    _like(shape, torch.bfloat16, dev, q, o, d_o, dq)
+    _like((B, H, n_q), torch.float32, dev, lse)
+    n_kc, n_select = _chunk(q, dev, k_chunk, v_chunk, dk_chunk, dv_chunk), _lists(q, dev, blocks)
     fresh = []
     if dq is None:
         dq = torch.empty_like(q); fresh.append(dq)
@@ -707,17 +710,10 @@ def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
     if workspace is None:
         need = astro_sparse_attn_bwd_workspace_bytes(B, H, D, n_q, n_kc, n_select, block_tokens)
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _typed(torch.int32, blocks)
-    _typed(torch.float32, lse)
-    _typed(torch.bfloat16, q, k_chunk, v_chunk, o, d_o, dq, dk_chunk, dv_chunk)
-    _contiguous(q, k_chunk, v_chunk, blocks, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace)
-    on = _here(stream, q, k_chunk, v_chunk, blocks, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, None if cache is None else cache.k_storage)
-    _sized((o, q.numel()), (d_o, q.numel()), (dq, q.numel()), (lse, B * H * n_q), (dk_chunk, B * n_kc * H * D), (dv_chunk, B * n_kc * H * D))
     _used_on(stream, *fresh)
-    st = lib().astro_sparse_attn_bwd(None if cache is None else cache.handle, _at(q), _at(k_chunk), _at(v_chunk), _at(blocks),
-                                     n_select, int(block_tokens), _at(o), _at(lse), _at(d_o), B, H, D, n_q, n_kc, float(scale),
-                                     _at(dq), _at(dk_chunk), _at(dv_chunk), _at(workspace),
-                                     workspace.numel() * workspace.element_size(), on)
+    st = lib().astro_sparse_attn_bwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), _at(blocks), n_select,
+                                     int(block_tokens), _at(o), _at(lse), _at(d_o), B, H, D, n_q, n_kc, float(scale), _at(dq),
+                                     _at(dk_chunk), _at(dv_chunk), *_scratch(workspace, dev), on)
     _check(st, "astro_sparse_attn_bwd")
     return dq, dk_chunk, dv_chunk
 
