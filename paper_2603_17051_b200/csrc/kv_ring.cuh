@@ -59,7 +59,7 @@ ring_copy_kernel(uint4* __restrict__ k_user, uint4* __restrict__ v_user, uint4* 
 // continue one parent, its bytes come from HBM once and from L2 for the others.  A parent outside the source leaves
 // zeros, never an access out of range.
 constexpr int kForkThreads = 256;
-constexpr int kForkVecsPerThread = 8;
+constexpr int kForkVecsPerThread = 4;
 
 struct ForkMap {
   int n;
@@ -95,7 +95,7 @@ cache_fork_kernel(const uint4* __restrict__ k_src, const uint4* __restrict__ v_s
 #pragma unroll
   for (int u = 0; u < kForkVecsPerThread; ++u) {
     const int at = first + u * kForkThreads;
-    if (at < frame_vecs) dst[at] = val[u];
+    if (at < frame_vecs) __stcs(dst + at, val[u]);   // nobody reads it soon: leaves L2 to the source
   }
 }
 

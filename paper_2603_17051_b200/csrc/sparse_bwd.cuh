@@ -140,18 +140,12 @@ __device__ __forceinline__ void sparse_bwd_dq(uint8_t* smem_raw, const SparseMap
     tma_prefetch_desc(&maps.kx); tma_prefetch_desc(&maps.vx); tma_prefetch_desc(&maps.kc); tma_prefetch_desc(&maps.vc);
     tma_prefetch_desc(&tm_do);
   }
-  if (tid == 0) {
-    mbar_init(kv0_full, 1);
-    mbar_init(qt_full, 4 * (D / 64));
-    for (int i = 0; i < 4; ++i) { mbar_init(rs + i, 1 + 4 * kDqGroups); mbar_init(rb + i, 1 + 4 * kDqGroups); }   // bytes, warps
-    mbar_init(s_full, 1);
-    mbar_init(b_done, 1);
-    mbar_init(b_done + 1, 1);
-    mbar_init(dq_full, 1);
-    for (int i = 0; i < kSpDescs; ++i) { mbar_init(listed + i, 1); mbar_init(unlisted + i, 4 * kDqGroups + 2); }
-    *abort_flag = 0;
+  if (tid < 14 + 2 * kSpDescs) {   // every barrier is set up by a thread of its own
+    // qt_full: one arrival per warp and 64 elements; rs, rb: bytes and warps; unlisted: the list's readers
+    mbar_init(bars + tid, tid == 1 ? 4 * (D / 64) : tid >= 2 && tid < 10 ? 1 + 4 * kDqGroups : tid < 14 + kSpDescs ? 1 : 4 * kDqGroups + 2);
     fence_mbar_init();
   }
+  if (tid == 0) *abort_flag = 0;
   zero_uncovered_rows<D>(sK, kDqKStages, geom, tid, kSparseBwdThreads);
   zero_uncovered_rows<D>(sV, kDqVStages, geom, tid, kSparseBwdThreads);
   fence_proxy_async_smem();

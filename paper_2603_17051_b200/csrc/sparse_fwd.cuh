@@ -118,20 +118,15 @@ struct SparseStream {
 struct SparseBars : FwdFastBars {
   uint64_t *max_full, *listed;   // [4], kFwdGroups arrivals; [kSpDescs]
   __device__ explicit SparseBars(uint64_t* b) : FwdFastBars(b), max_full(b + 23), listed(b + 27) {}
-  __device__ void init(int q_count) const {
-    mbar_init(q_full, q_count);
-    mbar_init(q_full + 1, q_count);
-    mbar_init(k01, 2);
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(ready + i, 2 + 4 * kFwdGroups);   // two loads, one arrival per softmax warp
-      mbar_init(sdone + i, 1);
-      mbar_init(max_full + i, kFwdGroups);
-    }
-    mbar_init(o_full, 1);
-    mbar_init(o_free, kFwdEpiWarps);
-    mbar_init(stats_full, 4 * kFwdGroups);
-    mbar_init(stats_full + 1, 4 * kFwdGroups);
-    for (int i = 0; i < kSpDescs; ++i) mbar_init(listed + i, 1);
+  // Arrivals of the barrier in slot i (0: none there); every barrier is set up by a thread of its own.
+  static __device__ int arrivals(int i, int q_count) {
+    if (i < 2) return q_count;
+    if (i == 2) return 2;                                     // k01: two loads
+    if (i >= 3 && i < 7) return 2 + 4 * kFwdGroups;           // ready: two loads, one arrival per softmax warp
+    if (i == 20) return kFwdEpiWarps;                         // o_free
+    if (i == 21 || i == 22) return 4 * kFwdGroups;            // stats_full
+    if (i >= 23 && i < 27) return kFwdGroups;                 // max_full
+    return (i >= 11 && i < 15) || i == 19 || (i >= 27 && i < 27 + kSpDescs) ? 1 : 0;   // sdone, o_full, listed
   }
 };
 constexpr int kSparseBarSlots = 36;
@@ -396,8 +391,9 @@ __device__ __noinline__ SparseRun sparse_idle(SparseLoop c, int J, TileDesc d) {
   return SparseRun{1.f, J, d, ok};
 }
 
+// Returns whether this thread asked for a unit to be done again.
 template <int D>
-__device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const SparseBars& bar, int warp, int r, float scale_log2) {
+__device__ __forceinline__ bool sparse_softmax(const SparseCta<D>& c, const SparseBars& bar, int warp, int r, float scale_log2) {
   const int g = warp >> 2, lane = r & 31;
   const FwdStats<D> stats{c.smax};
   volatile int* abort_flag = c.abort_flag;
@@ -409,6 +405,7 @@ __device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const Spar
   lp.g = g;
   TileDesc d = await_desc(lp, 0);
   int J = 0;
+  bool asked = false;
   int maxima = 0;   // units for which this warp has met the other groups over the row maxima
   for (int n = 0;; ++n) {
     float m_ref = 0.f, l_run;
@@ -459,12 +456,16 @@ __device__ __forceinline__ void sparse_softmax(const SparseCta<D>& c, const Spar
     // first P V of unit n - 1 waited for
     stats.sums(n)[g * kTile + r] = l_run;
     if (g == 0) stats.refs(n)[r] = m_ref;
-    if (!(l_run < kFastSumLimit)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));   // true for inf and NaN too
+    if (!(l_run < kFastSumLimit)) {   // true for inf and NaN too
+      atomicOr(c.redo + (n >> 5), 1u << (n & 31));
+      asked = true;
+    }
     warp_arrive(bar.stats_full + (n & 1), lane);
     if ((flags & kTileEnd) || !ok) break;
     d = next;
     ++J;
   }
+  return asked;
 }
 
 // ---------------------------------------------------------------------------------- results of a unit
@@ -520,7 +521,7 @@ template <int D> struct SparseRow {
 };
 
 template <int D>
-__device__ __forceinline__ void sparse_epilogue(const SparseCta<D>& c, const SparseUnits& s, const SparseFwdArgs& a,
+__device__ __forceinline__ bool sparse_epilogue(const SparseCta<D>& c, const SparseUnits& s, const SparseFwdArgs& a,
                                                 const SparseBars& bar, int warp, int lane) {
   constexpr int kSlices = D / 32, kOwn = kSlices / 2;
   constexpr int kMmaWarp = 4 * kFwdGroups;
@@ -536,6 +537,7 @@ __device__ __forceinline__ void sparse_epilogue(const SparseCta<D>& c, const Spa
   };
   stage_q(s.first, 0);
   if (s.total - s.first > s.stride) stage_q(s.first + s.stride, 1);
+  bool asked = false;
   int n = 0;
   for (int unit = s.first; unit < s.total; unit += s.stride, ++n) {
     const SparseRow<D> row(s, SparseUnit(s, unit, a.heads, a.batch), a, r);
@@ -557,9 +559,13 @@ __device__ __forceinline__ void sparse_epilogue(const SparseCta<D>& c, const Spa
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) row.store(acc[i], inv, chk2, (half * kOwn + i) * 32, lane);
     if (half == 0) row.store_lse(m, l);
-    if (row.in_range && !fwd_all_finite(chk2)) atomicOr(c.redo + (n >> 5), 1u << (n & 31));
+    if (row.in_range && !fwd_all_finite(chk2)) {
+      atomicOr(c.redo + (n >> 5), 1u << (n & 31));
+      asked = true;
+    }
     if (s.total - unit > 2 * s.stride) stage_q(unit + 2 * s.stride, n & 1);
   }
+  return asked;
 }
 
 // ---------------------------------------------------------------------------------- careful pass
@@ -710,12 +716,12 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
   if (warp == kKWarp && lane == 0) {
     tma_prefetch_desc(&maps.kx); tma_prefetch_desc(&maps.vx); tma_prefetch_desc(&maps.kc); tma_prefetch_desc(&maps.vc);
   }
-  if (tid == 0) {
-    bar.init(4 * (D / 64));   // q_full: one arrival per warp and 64-element part
-    for (int i = 0; i < 3; ++i) mbar_init(careful_bars + i, 1);
-    *c.abort_flag = 0;
+  if (tid < kSparseBarSlots + 3) {   // the three of the careful pass behind them
+    const int arrivals = tid < kSparseBarSlots ? SparseBars::arrivals(tid, 4 * (D / 64)) : 1;   // q_full: a warp and 64 elements
+    if (arrivals > 0) mbar_init(bar_mem + tid, arrivals);
     fence_mbar_init();
   }
+  if (tid == 0) *c.abort_flag = 0;
   if (tid < kFwdMaxUnits / 32) c.redo[tid] = 0;
   zero_uncovered_rows<D>(c.sK, kFwdKStages, g, tid, kSparseThreads);
   zero_uncovered_rows<D>(c.sV, kFwdVStages, g, tid, kSparseThreads);
@@ -730,23 +736,27 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
   c.tmem_base = *tmem_holder;
   dependents_may_start();
 
+  bool asked = a.careful != 0;
   if (!a.careful) {
     if (warp == kTmaWarp) sparse_walk<D>(c, g, s, a, bar, stream, lane);
     else if (warp == kKWarp) { if (lane == 0) sparse_load_k<D>(c, g, maps, bar); }
     else if (warp == kVWarp) { if (lane == 0) sparse_load_v<D>(c, g, maps, bar); }
     else if (warp == kMmaWarp) { if (lane == 0) sparse_issue<D>(c, bar); }
-    else if (warp < kMmaWarp) sparse_softmax<D>(c, bar, warp, tid & 127, a.scale_log2);
-    else sparse_epilogue<D>(c, s, a, bar, warp, lane);
+    else if (warp < kMmaWarp) asked = sparse_softmax<D>(c, bar, warp, tid & 127, a.scale_log2);
+    else asked = sparse_epilogue<D>(c, s, a, bar, warp, lane);
   }
   // every MMA of the fast pass has finished by now: the epilogue warps waited for the last one
-  int n = 0, tick = 0;
-  for (int unit = s.first; unit < s.total; unit += s.stride, ++n) {
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
-    if (*c.abort_flag) break;
-    if (!a.careful && !((c.redo[n >> 5] >> (n & 31)) & 1u)) continue;
-    sparse_careful_unit<D>(c, g, s, a, &maps, careful_bars, unit, warp, lane, tick);
+  tc_fence_before_sync();
+  if (__syncthreads_or(asked)) {
+    int n = 0, tick = 0;
+    for (int unit = s.first; unit < s.total; unit += s.stride, ++n) {
+      tc_fence_before_sync();
+      __syncthreads();
+      tc_fence_after_sync();
+      if (*c.abort_flag) break;
+      if (!a.careful && !((c.redo[n >> 5] >> (n & 31)) & 1u)) continue;
+      sparse_careful_unit<D>(c, g, s, a, &maps, careful_bars, unit, warp, lane, tick);
+    }
   }
   settle_after_abort(c.abort_flag);
   tc_fence_before_sync();
