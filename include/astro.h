@@ -177,7 +177,7 @@ astro_status_t astro_chunk_attn_bwd_dkv(const void* q, const void* k_chunk, cons
 /* Continue a cache as another one: empties `dst` and copies frames of `src` into it, as if they had been appended to it
  * in the order of `frames` (its first S_dst frames become the sink).  frames: HOST array of n_frames logical frame
  * indices of src (0 = oldest: sink frames, then the window oldest to newest; repeats allowed); null with
- * n_frames = -1 takes every held frame.  So the call copies, forks (one shared prefix, cache_batch 1, into one cache per
+ * n_frames = -1 takes every held frame, n_frames = 0 none.  So the call copies, forks (one shared prefix, cache_batch 1, into one cache per
  * candidate), reorders and compacts.
  * parents: device int32 [dst cache_batch], the sample of src that each sample of dst continues; null: sample b
  * continues sample b, or sample 0 of a one-sample src.  A parent outside src leaves zeros in the copied frames.
@@ -246,6 +246,8 @@ astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const voi
  * ASTRO_QUERY_BLOCK neighbouring queries share one list of key blocks; a query block that is shorter (the last one,
  * or a single query) has its list to itself. */
 #define ASTRO_QUERY_BLOCK 128
+/* Longest list of a query block (n_select): the bounded waits inside the kernels are laid out for lists of that length. */
+#define ASTRO_MAX_SELECT 65536
 /* Host only: number of cache blocks and of chunk blocks (HOST pointers, either may be null). */
 astro_status_t astro_block_count(const astro_kvcache_t* cache, int n_kc, int block_tokens, int* ctx_blocks,
                                  int* chunk_blocks);
@@ -263,8 +265,11 @@ astro_status_t astro_block_pool(const astro_kvcache_t* cache, int first_frame, i
  * scores go to the lower block; NaN ranks below every number.  keep: blocks that come before every other one
  * whatever their score (the lower ones first), ASTRO_KEEP_SINK those of the sink frames, ASTRO_KEEP_CHUNK the chunk's.
  * pooled: the means of every held frame (may be null if the cache is null or empty); k_chunk null when n_kc = 0.
- * workspace: device scratch, 16-byte aligned, at least astro_block_select_workspace_bytes().
- * ASTRO_ERR_SHAPE as for the attention calls, and for more than ASTRO_SELECT_MAX_BLOCKS blocks. */
+ * workspace: device scratch, 16-byte aligned, at least astro_block_select_workspace_bytes().  Like every workspace here it
+ * is written and read by the call's kernels only: calls that may overlap on the GPU (other streams, replayed graphs) need
+ * one each.
+ * ASTRO_ERR_SHAPE as for the attention calls, for more than ASTRO_SELECT_MAX_BLOCKS blocks and for an n_select outside
+ * 1..ASTRO_MAX_SELECT. */
 #define ASTRO_SELECT_MAX_BLOCKS 24576
 enum { ASTRO_KEEP_SINK = 1, ASTRO_KEEP_CHUNK = 2 };
 size_t astro_block_select_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens);
@@ -275,7 +280,7 @@ astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* poo
 /* Forward of attention over chosen key blocks: astro_chunk_attn_fwd with the keys of query block i restricted to the
  * blocks that its list names.  blocks: device int32 [batch, H, ceil(n_q / ASTRO_QUERY_BLOCK), n_select] in any order.  An
  * entry outside [0, number of blocks) names none; a block named twice counts twice.  A query with no key (an empty list) gets
- * O = 0 and LSE = -infinity.  The other arguments, layouts and errors are astro_chunk_attn_fwd's.
+ * O = 0 and LSE = -infinity.  The other arguments, layouts and errors are astro_chunk_attn_fwd's; n_select is 1..ASTRO_MAX_SELECT.
  * workspace: device scratch, 16-byte aligned, at least astro_sparse_attn_fwd_workspace_bytes() (0 for all but a few
  * queries: their lists are cut into ranges that run side by side; then it may be null). */
 size_t astro_sparse_attn_fwd_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_select, int block_tokens);
@@ -350,7 +355,8 @@ astro_status_t astro_selftest_wait_timeout(void* stream);
  * query row keeps the maximum of its first key tile as its one reference exponent, and repeats a 128-query
  * tile with a running reference (the "safe pass") only if a row sum left the range fp32 can hold.
  *   mode 0  normal operation;
- *   mode 1  every later astro_chunk_attn_fwd of this process runs the safe pass only;
+ *   mode 1  every later astro_chunk_attn_fwd of this process runs the safe pass only (astro_sparse_attn_fwd likewise its
+ *           own pass with a running reference);
  *   mode 2  head_dim 128 calls run the CTA-pair kernel (two query tiles share every K/V tile through one
  *           tcgen05 cta_group::2 MMA); it has no safe pass of its own: a call whose rows would need one leaves
  *           a flag that astro_debug_pair_flag reads (and clears) after synchronising the device.

@@ -512,7 +512,7 @@ struct SparseCall {
 astro_status_t check_sparse(const SparseCall& c, float scale, SparseGeom* g) {
   astro_status_t s = check_attn_args(c.a, scale);
   if (s != ASTRO_OK) return s;
-  if (!block_tokens_ok(c.block_tokens) || c.n_select < 1 || c.n_select > (1 << 30) ||
+  if (!block_tokens_ok(c.block_tokens) || c.n_select < 1 || c.n_select > ASTRO_MAX_SELECT ||
       !build_key_blocks(c.a.cache, c.a.n_kc, c.block_tokens, &g->kb))
     return ASTRO_ERR_SHAPE;
   g->pad = sparse_pad(c.block_tokens);
@@ -1034,10 +1034,10 @@ astro_status_t astro_chunk_attn_bwd(const astro_kvcache_t* cache, const void* q,
 
 astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* src, const int32_t* parents,
                                   const int* frames, int n_frames, void* stream) {
-  if (!dst || !src || (!frames && n_frames >= 0)) return ASTRO_ERR_NULL;
+  if (!dst || !src || (!frames && n_frames > 0)) return ASTRO_ERR_NULL;
   const auto &a = src->d, &d = dst->d;
   const int held = src->sink_held + src->win_held;
-  if (!frames) n_frames = held;
+  if (!frames && n_frames == -1) n_frames = held;
   if (n_frames < 0 || dst == src || a.heads != d.heads || a.head_dim != d.head_dim ||
       a.tokens_per_frame != d.tokens_per_frame)
     return ASTRO_ERR_SHAPE;
@@ -1256,7 +1256,7 @@ astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* poo
   astro_status_t s = check_attn_args(args, 1.f);
   if (s != ASTRO_OK) return s;
   KeyBlocks kb;
-  if (!block_tokens_ok(block_tokens) || n_select < 1 || (keep & ~(ASTRO_KEEP_SINK | ASTRO_KEEP_CHUNK)) ||
+  if (!block_tokens_ok(block_tokens) || n_select < 1 || n_select > ASTRO_MAX_SELECT || (keep & ~(ASTRO_KEEP_SINK | ASTRO_KEEP_CHUNK)) ||
       !build_key_blocks(cache, n_kc, block_tokens, &kb) || kb.total > ASTRO_SELECT_MAX_BLOCKS)
     return ASTRO_ERR_SHAPE;
   if (kb.ctx > 0 && !pooled) return ASTRO_ERR_NULL;
