@@ -450,17 +450,19 @@ bool build_key_blocks(const astro_kvcache* c, int n_kc, int block, KeyBlocks* ou
   return true;
 }
 
-template <int D>
-astro_status_t launch_pool(const PoolSource& s0, const PoolSource& s1, int n0, int n1, int heads, int batch, const KeyBlocks& kb,
-                           int frame0, int cache_source, cudaStream_t st) {
-  // as many warps per block of tokens as bring the GPU 1500 of them, so that enough loads are in flight (1872
-  // blocks: one warp each 15.5 us, two 17.9: more streams, more sums to join)
-  const long long blocks = (static_cast<long long>(n0) + n1) * heads * batch;
+// As many warps per block of tokens as bring the GPU about 1500 of them, so that enough loads are in flight (1872
+// blocks: one warp each 15.5 us, two 17.9: more streams, more sums to join).
+int pool_share(long long blocks) {
   int share = 1;
   while (share < 8 && blocks * share < 1500) share *= 2;
-  const int per_cta = kPoolThreads / 32 / share;
-  dim3 grid((n0 + n1 + per_cta - 1) / per_cta, heads, batch);
-  block_pool_kernel<D><<<grid, kPoolThreads, 0, st>>>(s0, s1, n0, n1, kb, frame0, cache_source, share);
+  return share;
+}
+
+template <int D>
+astro_status_t launch_pool(const PoolSource& s, int heads, int batch, const KeyBlocks& kb, int frame0, cudaStream_t st) {
+  const int share = pool_share(static_cast<long long>(s.blocks) * heads * batch), per_cta = kPoolThreads / 32 / share;
+  dim3 grid((s.blocks + per_cta - 1) / per_cta, heads, batch);
+  block_pool_kernel<D><<<grid, kPoolThreads, 0, st>>>(s, kb, frame0, share);
   return launch_status();
 }
 
@@ -471,17 +473,40 @@ void set_inverses(PoolSource* s) {
 }
 
 template <int D>
-astro_status_t launch_select_all(const PoolSource& q, const PoolSource& kc, SelectArgs a, const KeyBlocks& kb, int batch,
-                                 cudaStream_t st) {
-  astro_status_t s = launch_pool<D>(q, kc, q.blocks, kc.blocks, a.heads, batch, kb, 0, 0, st);
-  if (s != ASTRO_OK) return s;
+astro_status_t launch_select(const PoolSource& q, const PoolSource& kc, SelectArgs a, const KeyBlocks& kb, int batch,
+                             cudaStream_t st) {
   static std::atomic<int> done[kMaxDevices];
-  if ((s = set_smem_once(block_select_kernel<D>, ASTRO_SELECT_MAX_BLOCKS * 8, done)) != ASTRO_OK) return s;
-  // as many of a tile's eight query blocks as have room for their keys in shared memory
-  const int most = ASTRO_SELECT_MAX_BLOCKS / kb.total;
-  a.rows = most < kSelectRows ? most : kSelectRows;
-  dim3 tiles((a.q_blocks + a.rows - 1) / a.rows, a.heads, batch);
-  return launch_dependent(block_select_kernel<D>, tiles, kSelectThreads, static_cast<size_t>(a.rows) * kb.total * 8, st, a, kb);
+  astro_status_t s = set_smem_once(block_select_kernel<D>, ASTRO_SELECT_MAX_BLOCKS * 8, done);
+  if (s != ASTRO_OK) return s;
+  const long long units = static_cast<long long>(q.blocks) + kc.blocks;
+  const bool fused = units <= kSelectWarps;   // a warp for every mean (both sides measured: see the kernel)
+  // thread blocks of a head: a tile's eight query blocks each, or as many as have room for their keys in shared memory
+  const int room = ASTRO_SELECT_MAX_BLOCKS / kb.total;
+  a.rows = room < kSelectRows ? room : kSelectRows;
+  int size = (a.q_blocks + a.rows - 1) / a.rows;
+  if (!fused) {
+    const int share = pool_share(units * a.heads * batch), per_cta = kPoolThreads / 32 / share;
+    dim3 grid(static_cast<unsigned>((units + per_cta - 1) / per_cta), a.heads, batch);
+    block_mean_kernel<D><<<grid, kPoolThreads, 0, st>>>(q, kc, share);
+    if ((s = launch_status()) != ASTRO_OK) return s;
+    return launch_dependent(block_select_kernel<D>, dim3(size, a.heads, batch), kSelectThreads,
+                            static_cast<size_t>(a.rows) * kb.total * 8, st, a, kb, q, kc, 0);
+  }
+  if (size > 8) size = 8;
+  int share = 1;
+  while (units * share * 2 <= kSelectWarps) share *= 2;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = static_cast<unsigned>(size);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(size), a.heads, batch);
+  cfg.blockDim = dim3(kSelectThreads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(a.rows) * kb.total * 8;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, block_select_kernel<D>, a, kb, q, kc, share) == cudaSuccess ? launch_status() : ASTRO_ERR_CUDA;
 }
 
 // ---- attention over lists of key blocks ---------------------------------------------------------------------
@@ -1237,8 +1262,8 @@ astro_status_t astro_block_pool(const astro_kvcache_t* c, int first_frame, int n
   src.blocks = n_frames * kb.per_frame;
   set_inverses(&src);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return d.head_dim == 128 ? launch_pool<128>(src, src, src.blocks, 0, d.heads, d.cache_batch, kb, first_frame, 1, st)
-                           : launch_pool<64>(src, src, src.blocks, 0, d.heads, d.cache_batch, kb, first_frame, 1, st);
+  return d.head_dim == 128 ? launch_pool<128>(src, d.heads, d.cache_batch, kb, first_frame, st)
+                           : launch_pool<64>(src, d.heads, d.cache_batch, kb, first_frame, st);
 }
 
 size_t astro_block_select_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_kc, int block_tokens) {
@@ -1299,7 +1324,7 @@ astro_status_t astro_block_select(const astro_kvcache_t* cache, const float* poo
   a.keep_sink = keep & ASTRO_KEEP_SINK ? 1 : 0;
   a.keep_chunk = keep & ASTRO_KEEP_CHUNK ? 1 : 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return head_dim == 128 ? launch_select_all<128>(qs, ks, a, kb, batch, st) : launch_select_all<64>(qs, ks, a, kb, batch, st);
+  return head_dim == 128 ? launch_select<128>(qs, ks, a, kb, batch, st) : launch_select<64>(qs, ks, a, kb, batch, st);
 }
 
 size_t astro_sparse_attn_fwd_workspace_bytes(int batch, int heads, int head_dim, int n_q, int n_select, int block_tokens) {

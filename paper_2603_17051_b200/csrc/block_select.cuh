@@ -40,45 +40,19 @@ struct PoolSource {
 };
 
 constexpr int kPoolThreads = 256;
-
 constexpr int kPoolBatch = 6;   // token rows a thread has in flight, twice (the next batch is asked for before this one is added)
 
-// `share` warps (1, 2, 4 or 8) per block of tokens of one head: D/8 lanes side by side hold 8 elements each, the other lanes
-// and warps walk the tokens.  Everything is resident at once and every warp streams by itself: 58 MB in 14.6 us (13.6 with
-// fp32 sums; a thread block per block of tokens, with its partial sums in shared memory, 17.2).
-// grid.x * (8 / share) covers the blocks of source 0, then of source 1 (n0 and n1 of them); grid.y = head, grid.z = sample.
-// cache_source: source 0 is the cache storage, and its blocks are those of the frames from logical frame `frame0` on.
+// A warp's part of the sum over the rows of one block: D/8 lanes side by side hold 8 elements each; the warp's lane groups
+// take rows t, t + step, ...  On return every lane of a column has the warp's sum.
 template <int D>
-__global__ void __launch_bounds__(kPoolThreads)
-block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const int n1, const KeyBlocks kb, const int frame0,
-                  const int cache_source, const int share) {
-  constexpr int kCols = D / 8, kWarps = kPoolThreads / 32, kGroups = 32 / kCols;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane % kCols;
-  const int unit = blockIdx.x * (kWarps / share) + warp / share;
-  const bool there = unit < n0 + n1, second = unit >= n0;
-  const PoolSource& s = second ? s1 : s0;
-  int j = second ? unit - n0 : unit;
-  const int h = blockIdx.y, b = blockIdx.z;
-  long long first_row = 0, out_row = j;
-  if (cache_source) {
-    const int f = j / kb.per_frame, slot = key_block_slot(kb, frame0 + f);
-    j -= f * kb.per_frame;
-    first_row = static_cast<long long>(slot) * s.tokens;
-    out_row = static_cast<long long>(slot) * kb.per_frame + j;
-  }
-  const int count = there ? min(s.block, s.tokens - j * s.block) : 0;
-  const int step = share * kGroups;
-  int t = (warp % share) * kGroups + lane / kCols;
-  const __nv_bfloat16* src = s.base + b * s.sb + h * s.sh + (first_row + static_cast<long long>(j) * s.block) * s.st + col * 8;
-  dependents_may_start();
-  double acc[8];
+__device__ __forceinline__ void pool_rows(const __nv_bfloat16* src, long long st, int count, int t, int step, double (&acc)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0;
   uint4 v[kPoolBatch];
   auto fetch = [&]() {
 #pragma unroll
     for (int u = 0; u < kPoolBatch; ++u)
-      v[u] = t + u * step < count ? __ldcs(reinterpret_cast<const uint4*>(src + (t + u * step) * s.st)) : make_uint4(0, 0, 0, 0);
+      v[u] = t + u * step < count ? __ldcs(reinterpret_cast<const uint4*>(src + (t + u * step) * st)) : make_uint4(0, 0, 0, 0);
   };
   fetch();
   while (t < count) {
@@ -99,30 +73,77 @@ block_pool_kernel(const PoolSource s0, const PoolSource s1, const int n0, const 
   }
   __syncwarp();
 #pragma unroll
-  for (int x = kCols; x < 32; x *= 2)
+  for (int x = D / 8; x < 32; x *= 2)
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], x);
-  __shared__ double part[kWarps][8][kCols];
+}
+__device__ __forceinline__ void store_mean(float* out, const double (&acc)[8], double inv) {
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(acc[e] * inv);
+  reinterpret_cast<float4*>(out)[0] = make_float4(f[0], f[1], f[2], f[3]);
+  reinterpret_cast<float4*>(out)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+
+// The mean of one block by `share` neighbouring warps of a thread block: their
+// partial sums are joined in shared memory by the first of them.  All threads of the thread block together.
+template <int D>
+__device__ __forceinline__ void pool_shared(const __nv_bfloat16* src, long long st, int count, bool there, int share, float* out,
+                                            double inv, double (*part)[8][D / 8]) {
+  constexpr int kCols = D / 8, kGroups = 32 / kCols;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane % kCols;
+  double acc[8];
+  pool_rows<D>(src + col * 8, st, count, (warp % share) * kGroups + lane / kCols, share * kGroups, acc);
   if (share > 1) {
-    if (lane < kCols) {
+    if (lane < kCols && warp % share) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) part[warp][e][col] = acc[e];
     }
     __syncthreads();
-    if (warp % share) return;
-    for (int r = 1; r < share; ++r)
+    if (warp % share == 0)
+      for (int r = 1; r < share; ++r)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += part[warp + r][e][col];
+        for (int e = 0; e < 8; ++e) acc[e] += part[warp + r][e][col];
   }
-  if (there && lane < kCols) {
-    const double inv = count == s.block ? s.inv_block : s.inv_last;
-    float* out = s.out + ((b * s.out_b + h * s.out_h) + out_row) * D + col * 8;
-    float f[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(acc[e] * inv);
-    reinterpret_cast<float4*>(out)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4*>(out)[1] = make_float4(f[4], f[5], f[6], f[7]);
-  }
+  if (there && lane < kCols && warp % share == 0) store_mean(out + col * 8, acc, inv);
+}
+
+// The means of cached blocks: `share` warps (1, 2, 4 or 8) per block of one head.  Everything is resident at once and every
+// warp streams by itself: 58 MB in 14.6 us (13.6 with fp32 sums; a thread block per block, all its partial sums joined in
+// shared memory, 17.2).
+// grid.x * (8 / share) covers the `blocks` blocks of the frames from logical frame `frame0` on; grid.y = head, grid.z = sample.
+template <int D>
+__global__ void __launch_bounds__(kPoolThreads)
+block_pool_kernel(const PoolSource s, const KeyBlocks kb, const int frame0, const int share) {
+  constexpr int kWarps = kPoolThreads / 32;
+  const int unit = blockIdx.x * (kWarps / share) + (threadIdx.x >> 5) / share;
+  const int f = unit / kb.per_frame, j = unit - f * kb.per_frame;
+  const int h = blockIdx.y, b = blockIdx.z;
+  const bool there = unit < s.blocks;
+  const int slot = there ? key_block_slot(kb, frame0 + f) : 0;
+  const int count = there ? min(s.block, s.tokens - j * s.block) : 0;
+  __shared__ double part[kWarps][8][D / 8];
+  pool_shared<D>(
+      s.base + b * s.sb + h * s.sh + (static_cast<long long>(slot) * s.tokens + static_cast<long long>(j) * s.block) * s.st, s.st,
+      count, there, share, s.out + (b * s.out_b + h * s.out_h + static_cast<long long>(slot) * kb.per_frame + j) * D,
+      count == s.block ? s.inv_block : s.inv_last, part);
+}
+
+// The same for the blocks of two contiguous tensors (queries, chunk keys), numbered one after the other.
+template <int D>
+__global__ void __launch_bounds__(kPoolThreads)
+block_mean_kernel(const PoolSource s0, const PoolSource s1, const int share) {
+  constexpr int kWarps = kPoolThreads / 32;
+  dependents_may_start();
+  const int unit = blockIdx.x * (kWarps / share) + (threadIdx.x >> 5) / share;
+  const int h = blockIdx.y, b = blockIdx.z;
+  const bool second = unit >= s0.blocks, there = unit < s0.blocks + s1.blocks;
+  const PoolSource& s = second ? s1 : s0;
+  const int j = second ? unit - s0.blocks : unit;
+  const int count = there ? min(s.block, s.tokens - j * s.block) : 0;
+  __shared__ double part[kWarps][8][D / 8];
+  pool_shared<D>(s.base + b * s.sb + h * s.sh + static_cast<long long>(j) * s.block * s.st, s.st, count, there, share,
+                               s.out + (b * s.out_b + h * s.out_h + j) * D, count == s.block ? s.inv_block : s.inv_last, part);
 }
 
 // ------------------------------------------------------------------------------------------------ choice
@@ -177,101 +198,125 @@ __device__ __forceinline__ unsigned long long select_cut(int want, int total, in
   return cut;
 }
 
-// Up to eight query blocks of one head per thread block.  Scores: a warp per eight key blocks, fp64 MMAs over the head
-// dimension; the contraction index is dealt to the lanes so that each reads 16 contiguous bytes of a row (the same
-// order on both sides, so nothing else changes).  Then a warp per query block finds the n-th largest key bit by bit, stopping
-// as soon as a candidate separates exactly n, and writes the blocks above it, and as many equal to it as there is room
-// for, in order.  Scores by fused multiply-adds and shuffles, a warp per key block: 42 us for a chunk of 37 x 12 query blocks
-// and 273 key blocks against XXX.
-// Shared memory: keys [rows][total].
+// The thread blocks of grid.x share the query blocks of one head of one sample, `rows` (up to eight) at a time.  Scores: a
+// warp per eight key blocks, fp64 MMAs over the head dimension; the contraction index is dealt to the lanes so that each
+// reads 16 contiguous bytes of a row (the same order on both sides, so nothing else changes).  Then a warp per query block
+// finds the n-th largest key bit by bit, stopping as soon as a candidate separates exactly n, and writes the blocks above
+// it, and as many equal to it as there is room for, in order.  Scores by fused multiply-adds and shuffles, a warp per key
+// block, took 42 us for a chunk of 37 x 12 query blocks and 273 key blocks; by MMAs 8.
+// share > 0: the kernel first works out the means of the head's query blocks and chunk blocks itself, `share` warps each, and
+// grid.x is one cluster, whose barrier makes them known.  For the single query this saves a launch (13.2 us against
+// 16.3); the 76 blocks of a chunk's queries and keys want more SMs than the clusters have (26.4 us against 24.6), so there
+// they come from block_mean_kernel, and this kernel is launched as its dependent with share = 0.
+// Dynamic shared memory: keys [rows][total].
 template <int D>
 __global__ void __launch_bounds__(kSelectThreads)
-block_select_kernel(const SelectArgs a, const KeyBlocks kb) {
+block_select_kernel(const SelectArgs a, const KeyBlocks kb, const PoolSource qs, const PoolSource ks, const int share) {
   extern __shared__ unsigned long long s_key[];
   constexpr int kSteps = D / 16;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int q0 = blockIdx.x * a.rows, h = blockIdx.y, b = blockIdx.z;
-  const int rows = min(a.rows, a.q_blocks - q0);
+  const int h = blockIdx.y, b = blockIdx.z, rank = blockIdx.x, size = gridDim.x;
+  if (share == 0) {
+    dependency_wait();
+  } else {
+    __shared__ double part[kSelectWarps][8][D / 8];
+    const int per_pass = kSelectWarps / share, units = qs.blocks + ks.blocks;
+    for (int u0 = rank * per_pass; u0 < units; u0 += size * per_pass) {   // the same for the whole thread block
+      const int unit = u0 + warp / share;
+      const bool there = unit < units, second = unit >= qs.blocks;
+      const PoolSource& s = second ? ks : qs;
+      const int j = second ? unit - qs.blocks : unit;
+      const int count = there ? min(s.block, s.tokens - j * s.block) : 0;
+      pool_shared<D>(s.base + b * s.sb + h * s.sh + static_cast<long long>(j) * s.block * s.st, s.st, count, there, share,
+                                     s.out + (b * s.out_b + h * s.out_h + j) * D, count == s.block ? s.inv_block : s.inv_last, part);
+      __syncthreads();   // the parts have been read
+    }
+    __syncwarp();
+    cluster_sync_all();
+  }
   const int slots = kb.sink_slots + kb.win_slots, chunk_blocks = kb.total - kb.ctx;
   const float* ctx = a.pooled + static_cast<long long>(a.cache_shared ? 0 : b) * a.heads * slots * kb.per_frame * D +
                      static_cast<long long>(h) * slots * kb.per_frame * D;
   const float* own = a.kc_mean + (static_cast<long long>(b) * a.heads + h) * chunk_blocks * D;
   const int pair = lane >> 2, col = (lane & 3) * 4;
-  dependency_wait();   // the means of the queries and of the chunk
-  float4 q[kSteps];
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i)
-    q[i] = pair < rows ? *reinterpret_cast<const float4*>(
-                             a.q_mean + ((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + pair) * D + i * 16 + col)
-                       : make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j0 = warp * 8; j0 < kb.total; j0 += kSelectWarps * 8) {
-    const int j = j0 + pair;
-    const float* src = nullptr;
-    if (j < kb.ctx) {
-      const int f = j / kb.per_frame;
-      src = ctx + (static_cast<long long>(key_block_slot(kb, f)) * kb.per_frame + (j - f * kb.per_frame)) * D;
-    } else if (j < kb.total) {
-      src = own + static_cast<long long>(j - kb.ctx) * D;
-    }
-    float4 k[kSteps];
+  for (int q0 = rank * a.rows; q0 < a.q_blocks; q0 += size * a.rows) {
+    const int rows = min(a.rows, a.q_blocks - q0);
+    float4 q[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
-      k[i] = src ? *reinterpret_cast<const float4*>(src + i * 16 + col) : make_float4(0.f, 0.f, 0.f, 0.f);
-    double even[2] = {0.0, 0.0}, odd[2] = {0.0, 0.0};   // two chains
+      q[i] = pair < rows ? *reinterpret_cast<const float4*>(
+                               a.q_mean + ((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + pair) * D + i * 16 + col)
+                         : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int j0 = warp * 8; j0 < kb.total; j0 += kSelectWarps * 8) {
+      const int j = j0 + pair;
+      const float* src = nullptr;
+      if (j < kb.ctx) {
+        const int f = j / kb.per_frame;
+        src = ctx + (static_cast<long long>(key_block_slot(kb, f)) * kb.per_frame + (j - f * kb.per_frame)) * D;
+      } else if (j < kb.total) {
+        src = own + static_cast<long long>(j - kb.ctx) * D;
+      }
+      float4 k[kSteps];
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      mma_f64(even, q[i].x, k[i].x);
-      mma_f64(odd, q[i].y, k[i].y);
-      mma_f64(even, q[i].z, k[i].z);
-      mma_f64(odd, q[i].w, k[i].w);
-    }
+      for (int i = 0; i < kSteps; ++i)
+        k[i] = src ? *reinterpret_cast<const float4*>(src + i * 16 + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+      double even[2] = {0.0, 0.0}, odd[2] = {0.0, 0.0};   // two chains
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int to = j0 + 2 * (lane & 3) + e;
-      if (pair < rows && to < kb.total) {
-        const bool keep = to < kb.ctx ? a.keep_sink && to < kb.sink_held * kb.per_frame : a.keep_chunk != 0;
-        s_key[static_cast<long long>(pair) * kb.total + to] = keep ? kKeptKey : order_key(even[e] + odd[e]);
+      for (int i = 0; i < kSteps; ++i) {
+        mma_f64(even, q[i].x, k[i].x);
+        mma_f64(odd, q[i].y, k[i].y);
+        mma_f64(even, q[i].z, k[i].z);
+        mma_f64(odd, q[i].w, k[i].w);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int to = j0 + 2 * (lane & 3) + e;
+        if (pair < rows && to < kb.total) {
+          const bool keep = to < kb.ctx ? a.keep_sink && to < kb.sink_held * kb.per_frame : a.keep_chunk != 0;
+          s_key[static_cast<long long>(pair) * kb.total + to] = keep ? kKeptKey : order_key(even[e] + odd[e]);
+        }
       }
     }
-  }
-  __syncthreads();
-  for (int r = warp; r < rows; r += kSelectWarps) {
-    const unsigned long long* key = s_key + static_cast<long long>(r) * kb.total;
-    int* out = a.blocks + ((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + r) * a.n_select;
-    const int want = min(a.n_select, kb.total);
-    int ties;
-    unsigned long long cut;
-    // up to 512 keys sit in the lanes' registers during the search, more are read again for every bit
-    if (kb.total <= 32 * kSelectHeld) {
-      unsigned long long held[kSelectHeld];
+    __syncthreads();
+    for (int r = warp; r < rows; r += kSelectWarps) {
+      const unsigned long long* key = s_key + static_cast<long long>(r) * kb.total;
+      int* out = a.blocks + ((static_cast<long long>(b) * a.heads + h) * a.q_blocks + q0 + r) * a.n_select;
+      const int want = min(a.n_select, kb.total);
+      int ties;
+      unsigned long long cut;
+      // up to 512 keys sit in the lanes' registers during the search, more are read again for every bit
+      if (kb.total <= 32 * kSelectHeld) {
+        unsigned long long held[kSelectHeld];
 #pragma unroll
-      for (int i = 0; i < kSelectHeld; ++i) held[i] = lane + 32 * i < kb.total ? key[lane + 32 * i] : 0ull;
-      cut = select_cut(want, kb.total, ties, [&](auto reaches) {
-        int n = 0;
+        for (int i = 0; i < kSelectHeld; ++i) held[i] = lane + 32 * i < kb.total ? key[lane + 32 * i] : 0ull;
+        cut = select_cut(want, kb.total, ties, [&](auto reaches) {
+          int n = 0;
 #pragma unroll
-        for (int i = 0; i < kSelectHeld; ++i) n += reaches(held[i]) ? 1 : 0;
-        return n;
-      });
-    } else {
-      cut = select_cut(want, kb.total, ties, [&](auto reaches) {
-        int n = 0;
-        for (int j = lane; j < kb.total; j += 32) n += reaches(key[j]) ? 1 : 0;
-        return n;
-      });
+          for (int i = 0; i < kSelectHeld; ++i) n += reaches(held[i]) ? 1 : 0;
+          return n;
+        });
+      } else {
+        cut = select_cut(want, kb.total, ties, [&](auto reaches) {
+          int n = 0;
+          for (int j = lane; j < kb.total; j += 32) n += reaches(key[j]) ? 1 : 0;
+          return n;
+        });
+      }
+      int at = 0;
+      for (int j0 = 0; j0 < kb.total; j0 += 32) {
+        const int j = j0 + lane;
+        const unsigned long long x = j < kb.total ? key[j] : 0ull;
+        const bool equal = j < kb.total && x == cut;
+        const unsigned eq = __ballot_sync(0xffffffffu, equal);
+        const bool take = (j < kb.total && x > cut) || (equal && __popc(eq & ((1u << lane) - 1u)) < ties);
+        ties = max(0, ties - __popc(eq));
+        const unsigned mask = __ballot_sync(0xffffffffu, take);
+        if (take) out[at + __popc(mask & ((1u << lane) - 1u))] = j;
+        at += __popc(mask);
+      }
+      for (int i = want + lane; i < a.n_select; i += 32) out[i] = -1;
     }
-    int at = 0;
-    for (int j0 = 0; j0 < kb.total; j0 += 32) {
-      const int j = j0 + lane;
-      const unsigned long long x = j < kb.total ? key[j] : 0ull;
-      const bool equal = j < kb.total && x == cut;
-      const unsigned eq = __ballot_sync(0xffffffffu, equal);
-      const bool take = (j < kb.total && x > cut) || (equal && __popc(eq & ((1u << lane) - 1u)) < ties);
-      ties = max(0, ties - __popc(eq));
-      const unsigned mask = __ballot_sync(0xffffffffu, take);
-      if (take) out[at + __popc(mask & ((1u << lane) - 1u))] = j;
-      at += __popc(mask);
-    }
-    for (int i = want + lane; i < a.n_select; i += 32) out[i] = -1;
+    __syncthreads();   // the keys have been read
   }
 }
 
