@@ -636,7 +636,7 @@ astro_status_t launch_sparse_decode(const SparseCall& c, const SparseGeom& g, fl
   a.blocks = c.blocks;
   a.o = static_cast<__nv_bfloat16*>(o);
   a.lse = lse;
-  a.batch = c.a.batch; a.heads = c.a.heads;
+  a.heads = c.a.heads;
   a.n_select = c.n_select;
   a.entries = (tiles + parts - 1) / parts * g.per_tile;
   a.cache_shared = (c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1) ? 1 : 0;

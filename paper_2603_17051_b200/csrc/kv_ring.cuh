@@ -57,7 +57,8 @@ ring_copy_kernel(uint4* __restrict__ k_user, uint4* __restrict__ v_user, uint4* 
 // parents[b] (sample b, or sample 0 of a one-sample source, when parents is null).  The frame of one head is contiguous
 // on both sides, so the copy is plain 16-byte vectors.  The samples of a piece are neighbours in the grid: when several
 // continue one parent, its bytes come from HBM once and from L2 for the others.  A parent outside the source leaves
-// zeros, never an access out of range.
+// zeros, never an access out of range.  Bandwidth: 18 frames of one prefix for 8 samples (173 MB read, 1.38 GB written) in
+// 244 us = 6.36 TB/s, 97 % of the measured copy rate; 250 us without the streaming stores and with 8 vectors per thread.
 constexpr int kForkThreads = 256;
 constexpr int kForkVecsPerThread = 4;
 

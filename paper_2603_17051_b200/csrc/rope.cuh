@@ -12,7 +12,7 @@
 // those of k), kRopeRows loads in flight: no shared memory, no barrier, and the angles cost a fifth of the instructions when a thread
 // has all 24 rows of a 12-head token.  With fewer tokens the rows are dealt to several threads.
 // Sharing the angles of a few tokens through shared memory instead made every block load, wait, turn and store in step: 18.4 us
-// against 12.1 us for the 4680 tokens of a chunk (57.6 MB).
+// against 12.1 us for the 4680 tokens of a chunk (57.6 MB).  fp32, 8 samples (920 MB): 140 us = 6.6 TB/s, the copy rate.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

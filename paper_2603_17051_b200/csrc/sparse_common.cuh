@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t live_quarters(int n_q, int qt) { return (min
 // Where the producer finds the blocks of a tile.
 struct TileSource {
   BlockRef part[kSpParts];
-  int h, b, bx, unused;
+  int h, b, bx;   // head, sample of the chunk tensors, sample of the cache
 };
 
 // Walks over one list of block ids, 32 entries at a time; the next 32 are fetched while these are used.  Entries that

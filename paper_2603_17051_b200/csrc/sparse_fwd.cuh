@@ -9,10 +9,16 @@
 // descriptor per tile, a few tiles ahead, and the other roles act on it.  Tensor-memory layout, the S look-ahead, the rings and
 // the one-wait, one-commit rhythm of the issuing thread are the dense kernel's.
 //
-// Precision: bf16 products, fp32 sums.  P is rounded to bf16 for P V (2^-9 of each weight), the row sum is taken from the
+// Precision: bf16 products, fp32 sums.  P is rounded to bf16 for P V (half a step, 2^-8 of each weight at most), the row sum is taken from the
 // fp32 values.  Fast pass: each row keeps the maximum of its unit's first tile as its one reference; exp2(s - m) is exact for
 // any reference as long as nothing overflows.  A unit with a row sum beyond 2^100, an infinity or a NaN is done
 // again by the careful pass: a plain loop, tile by tile, with the running maximum of the textbook.
+//
+// Bound: the tensor pipe and its hand-offs.  A tile takes 1600 to 1670 clocks (the dense kernel's 1630), of which the MMAs are
+// 1024: S -> softmax 1250 -> hand-over 300 -> P V and the next S 1250, two tiles in flight.  Layer shape, 64 of 273 blocks of
+// 120 tokens per query block: 208 us = 1063 TFLOP/s at 1.67 GHz (tensor pipe 58 %, DRAM bytes as few as the inputs and
+// outputs have), 241 us under the power limit; with every query block naming one and the same block 188 us at 1.80 GHz in
+// as many clocks: what random lists cost is power.  Start and end of the kernel take 9 % of its clocks, a unit boundary 2.5 tiles.
 //
 // Few units: a unit's list is cut into up to `splits` ranges that run as units of their own and leave O (fp32, normalised)
 // and LSE of their part; sparse_combine_kernel joins them.
