@@ -485,9 +485,10 @@ astro_status_t launch_select(const PoolSource& q, const PoolSource& kc, SelectAr
   a.rows = room < kSelectRows ? room : kSelectRows;
   int size = (a.q_blocks + a.rows - 1) / a.rows;
   if (!fused) {
-    const int share = pool_share(units * a.heads * batch), per_cta = kPoolThreads / 32 / share;
+    // four warps per thread block where that is enough: spreads 912 means better over the SMs (23.5 us against 24.8 in all)
+    const int share = pool_share(units * a.heads * batch), warps = share > 4 ? share : 4, per_cta = warps / share;
     dim3 grid(static_cast<unsigned>((units + per_cta - 1) / per_cta), a.heads, batch);
-    block_mean_kernel<D><<<grid, kPoolThreads, 0, st>>>(q, kc, share);
+    block_mean_kernel<D><<<grid, 32 * warps, 0, st>>>(q, kc, share);
     if ((s = launch_status()) != ASTRO_OK) return s;
     return launch_dependent(block_select_kernel<D>, dim3(size, a.heads, batch), kSelectThreads,
                             static_cast<size_t>(a.rows) * kb.total * 8, st, a, kb, q, kc, 0);

@@ -115,14 +115,13 @@ __device__ __forceinline__ void pool_shared(const __nv_bfloat16* src, long long 
 template <int D>
 __global__ void __launch_bounds__(kPoolThreads)
 block_pool_kernel(const PoolSource s, const KeyBlocks kb, const int frame0, const int share) {
-  constexpr int kWarps = kPoolThreads / 32;
-  const int unit = blockIdx.x * (kWarps / share) + (threadIdx.x >> 5) / share;
+  const int unit = blockIdx.x * (blockDim.x / 32 / share) + (threadIdx.x >> 5) / share;
   const int f = unit / kb.per_frame, j = unit - f * kb.per_frame;
   const int h = blockIdx.y, b = blockIdx.z;
   const bool there = unit < s.blocks;
   const int slot = there ? key_block_slot(kb, frame0 + f) : 0;
   const int count = there ? min(s.block, s.tokens - j * s.block) : 0;
-  __shared__ double part[kWarps][8][D / 8];
+  __shared__ double part[kPoolThreads / 32][8][D / 8];
   pool_shared<D>(
       s.base + b * s.sb + h * s.sh + (static_cast<long long>(slot) * s.tokens + static_cast<long long>(j) * s.block) * s.st, s.st,
       count, there, share, s.out + (b * s.out_b + h * s.out_h + static_cast<long long>(slot) * kb.per_frame + j) * D,
@@ -133,15 +132,14 @@ block_pool_kernel(const PoolSource s, const KeyBlocks kb, const int frame0, cons
 template <int D>
 __global__ void __launch_bounds__(kPoolThreads)
 block_mean_kernel(const PoolSource s0, const PoolSource s1, const int share) {
-  constexpr int kWarps = kPoolThreads / 32;
   dependents_may_start();
-  const int unit = blockIdx.x * (kWarps / share) + (threadIdx.x >> 5) / share;
+  const int unit = blockIdx.x * (blockDim.x / 32 / share) + (threadIdx.x >> 5) / share;
   const int h = blockIdx.y, b = blockIdx.z;
   const bool second = unit >= s0.blocks, there = unit < s0.blocks + s1.blocks;
   const PoolSource& s = second ? s1 : s0;
   const int j = second ? unit - s0.blocks : unit;
   const int count = there ? min(s.block, s.tokens - j * s.block) : 0;
-  __shared__ double part[kWarps][8][D / 8];
+  __shared__ double part[kPoolThreads / 32][8][D / 8];
   pool_shared<D>(s.base + b * s.sb + h * s.sh + static_cast<long long>(j) * s.block * s.st, s.st, count, there, share,
                                s.out + (b * s.out_b + h * s.out_h + j) * D, count == s.block ? s.inv_block : s.inv_last, part);
 }
