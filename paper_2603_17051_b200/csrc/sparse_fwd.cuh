@@ -125,8 +125,8 @@ struct SparseBars : FwdFastBars {
   uint64_t *max_full, *listed;   // [4], kFwdGroups arrivals; [kSpDescs]
   __device__ explicit SparseBars(uint64_t* b) : FwdFastBars(b), max_full(b + 23), listed(b + 27) {}
   // Arrivals of the barrier in slot i (0: none there); every barrier is set up by a thread of its own.
-  static __device__ int arrivals(int i, int q_count) {
-    if (i < 2) return q_count;
+  static __device__ int arrivals(int i) {
+    if (i < 2) return kFwdEpiWarps;                           // q_full
     if (i == 2) return 2;                                     // k01: two loads
     if (i >= 3 && i < 7) return 2 + 4 * kFwdGroups;           // ready: two loads, one arrival per softmax warp
     if (i == 20) return kFwdEpiWarps;                         // o_free
@@ -458,8 +458,7 @@ __device__ __forceinline__ bool sparse_softmax(const SparseCta<D>& c, const Spar
       next = await_desc(lp, J + 1);
     }
     }
-    // the slots of unit n - 2 are free: the epilogue warps read them before they let go of that unit's O, which the
-    // first P V of unit n - 1 waited for
+    // the slots of unit n - 2 are free: the epilogue warps brought Q of unit n after they had read them
     stats.sums(n)[g * kTile + r] = l_run;
     if (g == 0) stats.refs(n)[r] = m_ref;
     if (!(l_run < kFastSumLimit)) {   // true for inf and NaN too
@@ -535,9 +534,12 @@ __device__ __forceinline__ bool sparse_epilogue(const SparseCta<D>& c, const Spa
   const int half = (warp - kMmaWarp - 2) >> 2;
   const int r = (warp & 3) * 32 + lane;
   const uint32_t tmem_lane = c.tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  // Every warp arrives, those without a share of Q too: Q of unit n then says that all of them have read the row sums of unit
+  // n - 2, whose slots the softmax threads write next.
   auto stage_q = [&](int unit, int buf) {
-    if (half >= D / 64 || unit >= s.total) return;
-    SparseRow<D>(s, SparseUnit(s, unit, a.heads, a.batch), a, r).stage_q(tmem_lane + kFwdColQ + buf * kFwdQCols, half, lane);
+    if (unit >= s.total) return;
+    if (D / 64 == 2 || half == 0)
+      SparseRow<D>(s, SparseUnit(s, unit, a.heads, a.batch), a, r).stage_q(tmem_lane + kFwdColQ + buf * kFwdQCols, half, lane);
     tc_fence_before_sync();
     warp_arrive(bar.q_full + buf, lane);
   };
@@ -723,7 +725,7 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
     tma_prefetch_desc(&maps.kx); tma_prefetch_desc(&maps.vx); tma_prefetch_desc(&maps.kc); tma_prefetch_desc(&maps.vc);
   }
   if (tid < kSparseBarSlots + 3) {   // the three of the careful pass behind them
-    const int arrivals = tid < kSparseBarSlots ? SparseBars::arrivals(tid, 4 * (D / 64)) : 1;   // q_full: a warp and 64 elements
+    const int arrivals = tid < kSparseBarSlots ? SparseBars::arrivals(tid) : 1;
     if (arrivals > 0) mbar_init(bar_mem + tid, arrivals);
     fence_mbar_init();
   }

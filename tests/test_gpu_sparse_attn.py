@@ -156,6 +156,32 @@ def test_many_short_lists_per_cta_and_single_tile_units():
     check_forward(o, lse, ref, o_abs, qf, 0.125, D, "short lists")
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_single_tile_units_with_and_without_queries_in_every_quarter(D):
+    """A CTA meets full and nearly empty query blocks in turn, one key tile each: what one unit leaves for the epilogue must
+    not be overwritten by the unit after the next."""
+    import torch
+    from paper_2603_17051_b200 import binding as A
+    B, H, n_q, n_kc, block = 8, 40, 128 * 2 + 5, 96, 32
+    bits = [synth.normal_bf16(60 + i, (B, n, H, D)) for i, n in enumerate((n_q, n_kc, n_kc))]
+    qf, kf, vf = (bf16_bits_to_f64(x) for x in bits)
+    ranges = orc.key_blocks(0, 1, n_kc, block)
+    blocks = lists(np.random.default_rng(8), B, H, 3, len(ranges), 3, "odd")
+    none = np.zeros((1, 0, H, D))
+    scale = D ** -0.5
+    ref, o_abs = reference(qf, kf, vf, none, none, blocks, ranges, scale, 0)
+    q, k, v = (dev_bf16(x) for x in bits)
+    tb = torch.from_numpy(blocks).cuda()
+    first = None
+    for _ in range(5):
+        o, lse = A.astro_sparse_attn_fwd(None, q, k, v, tb, block, scale)
+        A.astro_last_device_status()
+        if first is None:
+            first = o.clone()
+            check_forward(o, lse, ref, o_abs, qf, scale, D, "single tiles")
+        assert torch.equal(o, first)
+
+
 def test_every_block_chosen_is_dense_attention():
     import torch
     from paper_2603_17051_b200 import binding as A
