@@ -42,6 +42,49 @@ struct PoolSource {
 constexpr int kPoolThreads = 256;
 constexpr int kPoolBatch = 6;   // token rows a thread has in flight, twice (the next batch is asked for before this one is added)
 
+// Adds N rows of 8 bf16 values to the sums.  Conversions to fp64 are what a pool spends most of its issue time on (14.6 us with
+// one per value, 11.7 without the sums): two rows are added in fp32 first and converted together, 13.5.  Where that sum s = a + b is not exact the two are added one by one; it is exact
+// if s - a gives b and s - b gives a back (the error term of the two-sum algorithm is then zero; an infinity or a NaN never
+// gives both back, -0 does not always).  With exponents less than 16 apart it always is; of pairs of normal deviates one in
+// 10^5 is not.
+template <int N>
+__device__ __forceinline__ void pool_add(const uint4 (&v)[N], double (&acc)[8]) {
+  static_assert(N % 2 == 0, "pairs of rows");
+  const uint64_t minus = f32x2(-1.f, -1.f);
+#pragma unroll
+  for (int u = 0; u < N; u += 2) {
+    const uint32_t a[4] = {v[u].x, v[u].y, v[u].z, v[u].w}, b[4] = {v[u + 1].x, v[u + 1].y, v[u + 1].z, v[u + 1].w};
+    float s[8];
+    uint32_t off = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float a0 = __uint_as_float(a[e] << 16), a1 = __uint_as_float(a[e] & 0xffff0000u);
+      const float b0 = __uint_as_float(b[e] << 16), b1 = __uint_as_float(b[e] & 0xffff0000u);
+      const uint64_t a2 = f32x2(a0, a1), b2 = f32x2(b0, b1), s2 = add2(a2, b2);
+      float x0, x1, y0, y1;
+      f32x2_split(fma2(a2, minus, s2), x0, x1);
+      f32x2_split(fma2(b2, minus, s2), y0, y1);
+      f32x2_split(s2, s[2 * e], s[2 * e + 1]);
+      off |= __float_as_uint(x0) ^ __float_as_uint(b0);
+      off |= __float_as_uint(x1) ^ __float_as_uint(b1);
+      off |= __float_as_uint(y0) ^ __float_as_uint(a0);
+      off |= __float_as_uint(y1) ^ __float_as_uint(a1);
+    }
+    if (off == 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += static_cast<double>(s[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[2 * e] += static_cast<double>(__uint_as_float(a[e] << 16));
+        acc[2 * e] += static_cast<double>(__uint_as_float(b[e] << 16));
+        acc[2 * e + 1] += static_cast<double>(__uint_as_float(a[e] & 0xffff0000u));
+        acc[2 * e + 1] += static_cast<double>(__uint_as_float(b[e] & 0xffff0000u));
+      }
+    }
+  }
+}
+
 // A warp's part of the sum over the rows of one block: D/8 lanes side by side hold 8 elements each; the warp's lane groups
 // take rows t, t + step, ...  On return every lane of a column has the warp's sum.
 template <int D>
@@ -61,15 +104,7 @@ __device__ __forceinline__ void pool_rows(const __nv_bfloat16* src, long long st
     for (int u = 0; u < kPoolBatch; ++u) now[u] = v[u];
     t += kPoolBatch * step;
     fetch();
-#pragma unroll
-    for (int u = 0; u < kPoolBatch; ++u) {
-      const uint32_t w[4] = {now[u].x, now[u].y, now[u].z, now[u].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        acc[2 * e] += static_cast<double>(__uint_as_float(w[e] << 16));
-        acc[2 * e + 1] += static_cast<double>(__uint_as_float(w[e] & 0xffff0000u));
-      }
-    }
+    pool_add(now, acc);
   }
   __syncwarp();
 #pragma unroll
@@ -109,8 +144,8 @@ __device__ __forceinline__ void pool_shared(const __nv_bfloat16* src, long long 
 }
 
 // The means of cached blocks: `share` warps (1, 2, 4 or 8) per block of one head.  Everything is resident at once and every
-// warp streams by itself: 58 MB in 14.6 us (13.6 with fp32 sums; a thread block per block, all its partial sums joined in
-// shared memory, 17.2).
+// warp streams by itself: 58 MB in 13.5 us (a thread block per block, all its partial sums joined in shared memory, 17.2;
+// bulk copies into a ring of pieces per warp, twice the bytes in flight, 14.6).
 // grid.x * (8 / share) covers the `blocks` blocks of the frames from logical frame `frame0` on; grid.y = head, grid.z = sample.
 template <int D>
 __global__ void __launch_bounds__(kPoolThreads)
@@ -204,7 +239,7 @@ __device__ __forceinline__ unsigned long long select_cut(int want, int total, in
 // block, took 42 us for a chunk of 37 x 12 query blocks and 273 key blocks; by MMAs 8.
 // share > 0: the kernel first works out the means of the head's query blocks and chunk blocks itself, `share` warps each, and
 // grid.x is one cluster, whose barrier makes them known.  For the single query this saves a launch (13.2 us against
-// 16.3); the 76 blocks of a chunk's queries and keys want more SMs than the clusters have (26.4 us against 24.6), so there
+// 16.3); the 76 blocks of a chunk's queries and keys want more SMs than the clusters have (23.9 us against 21.9), so there
 // they come from block_mean_kernel, and this kernel is launched as its dependent with share = 0.
 // Dynamic shared memory: keys [rows][total].
 template <int D>

@@ -87,6 +87,43 @@ def test_means_of_new_frames_only_and_their_slots():
             assert (np.abs(got[:, :, slot, i] - want) <= 2.0 ** -24 * np.abs(want) + 1e-16).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("block", [8, 24, 120])
+def test_means_of_values_far_apart_and_beyond_fp32(D, block):
+    """Sums in fp64 whatever the exponents: neighbours 2^80 apart, terms that cancel, a sum beyond fp32's range, denormals,
+    negative zeros, infinities and NaN."""
+    import math
+    import torch
+    from paper_2603_17051_b200 import binding as A
+    T = 121
+    g = np.random.default_rng(block + D)
+    x = torch.from_numpy(np.ldexp(g.standard_normal((1, T, 2, D)), g.integers(-40, 41, (1, T, 2, D)))).bfloat16()
+    x[:, 1::2, :, 1] = -x[:, 0:-1:2, :, 1]                     # every pair cancels
+    x[:, :, :, 2] = torch.finfo(torch.bfloat16).max            # two of them overflow fp32, their mean does not
+    x[:, :, :, 3] = 2.0 ** -133                                # the smallest denormal
+    x[:, :, :, 4] = -0.0
+    x[:, 5, :, 5] = float("inf")
+    x[:, 2, :, 6], x[:, 3, :, 6] = float("inf"), float("-inf")
+    x[:, 7, :, 7] = float("nan")
+    cache = A.astro_kvcache_create(1, 2, D, T, 0, 1)
+    A.astro_kvcache_append(cache, x.cuda(), x.cuda(), 1)
+    got = f64(A.astro_block_pool(cache, block))[0, :, 0]
+    want_all = x.double().numpy()[0]
+    for h in range(2):
+        for i, a in enumerate(range(0, T, block)):
+            rows = want_all[a:a + block, h]
+            for d in range(D):
+                col = rows[:, d]
+                if not np.isfinite(col).all():
+                    want = col.sum()
+                    assert np.isnan(got[h, i, d]) if np.isnan(want) else got[h, i, d] == want, (h, i, d)
+                    continue
+                want = math.fsum(col) / len(col)
+                # each addition in fp64, the product with the rounded inverse, one rounding to fp32 (denormals: 2^-150)
+                bound = (len(col) + 2) * 2.0 ** -53 * math.fsum(np.abs(col)) / len(col) + 2.0 ** -24 * abs(want) + 2.0 ** -150
+                assert abs(got[h, i, d] - want) <= bound * (1 + 1e-6), (h, i, d, got[h, i, d], want)
+
+
 def test_ties_take_the_lower_block_and_nan_comes_last():
     import torch
     from paper_2603_17051_b200 import binding as A
