@@ -43,9 +43,9 @@ constexpr int kPoolThreads = 256;
 constexpr int kPoolBatch = 6;   // token rows a thread has in flight, twice (the next batch is asked for before this one is added)
 
 // Adds N rows of 8 bf16 values to the sums.  Conversions to fp64 are what a pool spends most of its issue time on (14.6 us with
-// one per value, 11.7 without the sums): two rows are added in fp32 first and converted together, 13.5.  Where that sum s = a + b is not exact the two are added one by one; it is exact
-// if s - a gives b and s - b gives a back (the error term of the two-sum algorithm is then zero; an infinity or a NaN never
-// gives both back, -0 does not always).  With exponents less than 16 apart it always is; of pairs of normal deviates one in
+// one per value, 11.7 without the sums): two rows are added in fp32 first and converted together, 13.5.  Where that sum
+// s = a + b is not exact the two are added one by one; it is exact if s - a gives b and s - b gives a back (the error term of
+// the two-sum algorithm is then zero; an infinity or a NaN never gives both back, -0 does not always).  With exponents less than 16 apart it always is; of pairs of normal deviates one in
 // 10^5 is not.
 template <int N>
 __device__ __forceinline__ void pool_add(const uint4 (&v)[N], double (&acc)[8]) {
