@@ -699,8 +699,9 @@ __device__ __forceinline__ void fwd_softmax_fast(const FwdUnit<D>& u, const FwdS
       }
       if (rest) { fwd_fast_tile<false>(c, Jr, rest - kFwdCols * g, m_ref, l_run, poly_max); ++Jr; }
     }
-    // The slots of unit n - 2 are free: the epilogue warps read them before they let go of that unit's O, which the
-    // first P V of unit n - 1 waited for.
+    // The slots of unit n - 2 are free: every epilogue warp answered for Q of unit n, which the S of this unit waited for,
+    // after it had read them.  (Their letting go of unit n - 2's O says so only behind the first P V of unit n - 1, and where
+    // units have a single tile the S of unit n is issued before that.)
     stats.sums(n)[g * kTile + r] = l_run;
     if (g == 0) stats.refs(n)[r] = m_ref;
     if (!((l_run < kFastSumLimit) && !(poly_max > kPolyArgLimit)))   // true for inf and NaN too
@@ -725,14 +726,16 @@ __device__ __forceinline__ void fwd_epilogue_fast(const FwdUnit<D>& u, const Fwd
   const int half = (warp - kMmaWarp - 2) >> 2;          // 0: columns [0, D/2), 1: the others
   const int r = (warp & 3) * 32 + lane;
   const uint32_t tmem_lane = u.tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-  const bool stages_q = half < D / 64;                  // part `half` of the Q rows
+  // Part `half` of the Q rows.  Every warp arrives, those without a part too (head_dim 64): Q of unit n then says that all of
+  // them have read the row sums of unit n - 2, whose slots the softmax threads write next.
   auto stage_q = [&](const FwdPos& pos, int buf) {
-    if (!stages_q) return;
-    const FwdRow<D> row(sch, pos, r, q, n_q, heads, o, lse);
-    uint32_t qr[32];
-    row.load_q(qr, half, lane);
-    tmem_st32(tmem_lane + kFwdColQ + buf * kFwdQCols + half * 32, qr);
-    tmem_wait_st();
+    if (half < D / 64) {
+      const FwdRow<D> row(sch, pos, r, q, n_q, heads, o, lse);
+      uint32_t qr[32];
+      row.load_q(qr, half, lane);
+      tmem_st32(tmem_lane + kFwdColQ + buf * kFwdQCols + half * 32, qr);
+      tmem_wait_st();
+    }
     tc_fence_before_sync();
     mbar_arrive(bar.q_full + buf);
   };
@@ -940,7 +943,7 @@ chunk_attn_fwd_kernel(const __nv_bfloat16* __restrict__ q, const __grid_constant
     tma_prefetch_desc(&tm_kc); tma_prefetch_desc(&tm_vc); tma_prefetch_desc(&tm_kx); tma_prefetch_desc(&tm_vx0);
   }
   if (tid == 0) {
-    bar_fast.init(128 * (D / 64));   // q_full: one arrival per row and 64-element part
+    bar_fast.init(32 * kFwdEpiWarps);   // q_full: every thread of the epilogue warps
     bar_safe.init(1, 128);
     *abort_flag = 0;
     fence_mbar_init();
