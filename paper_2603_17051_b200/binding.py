@@ -609,8 +609,13 @@ def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_
         raise AstroError(2, "astro_block_pool")
     shape = _pooled_shape(cache, block_tokens)
     if pooled is None:
-        pooled = torch.zeros(shape, dtype=torch.float32, device=cache.k_storage.device)
+        pooled = torch.empty(shape, dtype=torch.float32, device=cache.k_storage.device)
         _used_on(stream, pooled)
+        if stream is None:
+            pooled.zero_()
+        else:
+            with torch.cuda.stream(stream):   # the means go there: cleared elsewhere, they could be wiped
+                pooled.zero_()
     else:
         _like(shape, torch.float32, dev, pooled)
     _check(lib().astro_block_pool(_handle(cache, dev), int(first_frame), int(n_frames), int(block_tokens), _at(pooled), on),
