@@ -348,7 +348,8 @@ astro_status_t astro_last_device_status(uint32_t* detail);
 /* Self-test of that mechanism (the paper has no counterpart): enqueues a one-warp kernel that waits about a
  * millisecond on a barrier nothing will ever complete.  The kernel gives up, ends normally and leaves the
  * time-out in the status word, so the next astro_last_device_status returns ASTRO_ERR_TIMEOUT and the
- * context stays usable.  Nothing faults or hangs. */
+ * context stays usable.  Nothing faults or hangs.  The wait runs out for one lane of the warp only: were the others to go
+ * on without it, bit 1 of the raw word would be set as well. */
 astro_status_t astro_selftest_wait_timeout(void* stream);
 
 /* Diagnostic switch (the paper has no counterpart).  The forward kernel first runs a fast pass in which a

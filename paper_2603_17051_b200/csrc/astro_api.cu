@@ -49,17 +49,24 @@ struct astro_rope {
 namespace astro {
 // Self-test of the bounded wait: one warp waits on an mbarrier that nothing will ever complete.  The wait
 // gives up after `cycle_limit` clocks, records the time-out in the device status word and the kernel ends
-// normally, which is exactly the path a broken hand-off in the attention kernels would take.
+// normally, which is exactly the path a broken hand-off in the attention kernels would take.  Only the first lane waits on
+// that barrier, the others on one that is complete: every form of the wait has to tell all of them that it failed.
 __global__ void wait_timeout_selftest_kernel(long long cycle_limit) {
-  __shared__ uint64_t bar;
+  __shared__ uint64_t never, done;
   __shared__ int abort_flag;
   if (threadIdx.x == 0) {
-    mbar_init(&bar, 1);
+    mbar_init(&never, 1);
+    mbar_init(&done, 1);
     abort_flag = 0;
     fence_mbar_init();
+    mbar_arrive(&done);
   }
   __syncthreads();
-  mbar_wait_spin(&bar, 0, &abort_flag, cycle_limit);
+  uint64_t* bar = threadIdx.x == 0 ? &never : &done;
+  bool went_on = mbar_wait(bar, 0, &abort_flag, cycle_limit);
+  went_on = mbar_wait_relaxed(bar, 0, &abort_flag) || went_on;   // these two return at once: the flag is up
+  went_on = mbar_wait_at(smem_u32(bar), 0, smem_u32(&abort_flag)) || went_on;
+  if (went_on) atomicOr(&g_device_status, kStatusWarpParted);
 }
 }  // namespace astro
 

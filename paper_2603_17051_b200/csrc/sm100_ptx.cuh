@@ -12,6 +12,7 @@ namespace astro {
 __device__ uint32_t g_device_status = 0;
 
 constexpr uint32_t kStatusWaitTimeout = 1u;
+constexpr uint32_t kStatusWarpParted = 2u;   // self-test: the lanes of a warp got different answers from one wait
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
@@ -87,11 +88,12 @@ __device__ __forceinline__ void settle_after_abort(volatile int* abort_flag) {
   }
 }
 
-// The warp re-converges after the wait so that warp-collective tcgen05 instructions may follow.
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  const bool ok = mbar_wait_spin(bar, parity, abort_flag);
-  __syncwarp();
-  return ok;
+// The waits of whole warps.  The lanes come together behind the wait, so that warp-collective tcgen05 instructions may
+// follow, and all get the same answer: a wait can run out for some lanes in the moment in which it completes for the others, and a
+// warp whose lanes part there would stand against itself at its next barrier.
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                          long long cycle_limit = kWaitCycleLimit) {
+  return __all_sync(0xffffffffu, mbar_wait_spin(bar, parity, abort_flag, cycle_limit));
 }
 
 // For warps that wait long and are in nobody's way when they wake up a little late: sleeps between the polls, so
@@ -113,8 +115,7 @@ __device__ __forceinline__ bool mbar_wait_relaxed(uint64_t* bar, uint32_t parity
       }
     }
   }
-  __syncwarp();
-  return ok;
+  return __all_sync(0xffffffffu, ok);
 }
 
 // The same waits and arrivals on 32-bit shared-memory addresses (of the barrier and of the abort flag): for code
@@ -153,8 +154,7 @@ __device__ __forceinline__ bool mbar_wait_at(uint32_t bar, uint32_t parity, uint
       }
     }
   }
-  __syncwarp();
-  return ok;
+  return __all_sync(0xffffffffu, ok);
 }
 
 // A kernel launched as the dependent of the one before it (programmatic launch) may start while that one drains.  The

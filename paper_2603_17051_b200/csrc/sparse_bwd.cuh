@@ -489,27 +489,32 @@ __device__ __forceinline__ void sparse_bwd_dkv(uint8_t* smem_raw, const CUtensor
     if (lane == 0 && n_tiles > 0) {
       auto q_tile = [&](int i) { return smem_u32(sQ + (i % kDkvStages) * TileGeom<D>::kBytes); };
       auto do_tile = [&](int i) { return smem_u32(sdO + (i % kDkvStages) * TileGeom<D>::kBytes); };
+      // once a wait has run out no more MMAs are issued: their operands may never have been loaded
+      bool ok = true;
       auto wait_q = [&](int i) {
-        mbar_wait_spin(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
+        ok = ok && mbar_wait_spin(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
         tc_fence_after_sync();
       };
-      mbar_wait_spin(kv_full, 0, abort_flag);
+      ok = mbar_wait_spin(kv_full, 0, abort_flag);
       wait_q(0);
-      mma_abT<D>(tmem_base + kColSt, smem_u32(sK), q_tile(0));
-      mma_commit(s_full);
-      mma_abT<D>(tmem_base + kColdPt, smem_u32(sV), do_tile(0));
-      mma_commit(dp_full);
-      for (int i = 0; i < n_tiles; ++i) {
-        mbar_wait_spin(p_full, i & 1, abort_flag);
+      if (ok) {
+        mma_abT<D>(tmem_base + kColSt, smem_u32(sK), q_tile(0));
+        mma_commit(s_full);
+        mma_abT<D>(tmem_base + kColdPt, smem_u32(sV), do_tile(0));
+        mma_commit(dp_full);
+      }
+      for (int i = 0; ok && i < n_tiles; ++i) {
+        if (!mbar_wait_spin(p_full, i & 1, abort_flag)) break;
         tc_fence_after_sync();
         mma_pb<D, 64>(tmem_base + kColdV, tmem_base + kColSt, do_tile(i), i > 0);
         mma_pb<D, 64>(tmem_base + kColdV, tmem_base + kColSt + 64, do_tile(i) + kHalfBytes, true);
         if (i + 1 < n_tiles) {
           wait_q(i + 1);
+          if (!ok) break;
           mma_abT<D>(tmem_base + kColSt, smem_u32(sK), q_tile(i + 1));
           mma_commit(s_full);
         }
-        mbar_wait_spin(ds_full, i & 1, abort_flag);
+        if (!mbar_wait_spin(ds_full, i & 1, abort_flag)) break;
         tc_fence_after_sync();
         mma_pb<D, 64>(tmem_base + kColdK, tmem_base + kColdPt, q_tile(i), i > 0);
         mma_pb<D, 64>(tmem_base + kColdK, tmem_base + kColdPt + 64, q_tile(i) + kHalfBytes, true);
@@ -529,8 +534,9 @@ __device__ __forceinline__ void sparse_bwd_dkv(uint8_t* smem_raw, const CUtensor
     const uint64_t sc2 = f32x2(scale_log2, scale_log2);
     for (int i = 0; i < n_tiles; ++i) {
       const float* stat = sStat + (i % kDkvStages) * 2 * kTile + g * 64;
-      mbar_wait(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
-      mbar_wait(s_full, i & 1, abort_flag);
+      bool ok = mbar_wait(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
+      ok = mbar_wait(s_full, i & 1, abort_flag) && ok;
+      if (!ok) break;
       tc_fence_after_sync();
       uint32_t s[2][32], pt[32];
       tmem_ld32(tmem_lane + kColSt + g * 64, s[0]);
@@ -560,7 +566,7 @@ __device__ __forceinline__ void sparse_bwd_dkv(uint8_t* smem_raw, const CUtensor
       tc_fence_before_sync();
       warp_arrive(p_full, lane);
 
-      mbar_wait(dp_full, i & 1, abort_flag);
+      if (!mbar_wait(dp_full, i & 1, abort_flag)) break;
       tc_fence_after_sync();
 #pragma unroll
       for (int c2 = 0; c2 < 2; ++c2) {

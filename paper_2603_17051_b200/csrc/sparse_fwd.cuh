@@ -549,14 +549,14 @@ __device__ __forceinline__ bool sparse_epilogue(const SparseCta<D>& c, const Spa
   int n = 0;
   for (int unit = s.first; unit < s.total; unit += s.stride, ++n) {
     const SparseRow<D> row(s, SparseUnit(s, unit, a.heads, a.batch), a, r);
-    mbar_wait_relaxed(bar.stats_full + (n & 1), (n >> 1) & 1, c.abort_flag);
+    if (!mbar_wait_relaxed(bar.stats_full + (n & 1), (n >> 1) & 1, c.abort_flag)) break;
     float l = 0.f;
 #pragma unroll
     for (int g = 0; g < kFwdGroups; ++g) l += stats.sums(n)[g * kTile + r];
     const float m = stats.refs(n)[r];
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint64_t chk2 = f32x2(0.f, 0.f);
-    mbar_wait(bar.o_full, n & 1, c.abort_flag);
+    if (!mbar_wait(bar.o_full, n & 1, c.abort_flag)) break;
     tc_fence_after_sync();
     uint32_t acc[kOwn][32];
 #pragma unroll
@@ -614,7 +614,8 @@ __device__ __noinline__ void sparse_careful_unit(const SparseCta<D>& c, const Sp
       }
     }
     tc_fence_before_sync();
-    __syncthreads();   // descriptor written; Q staged; the tile before is done with S and P
+    // descriptor written; Q staged; the tile before is done with S and P.  Once a wait has run out, all leave together.
+    if (__syncthreads_or(*c.abort_flag)) break;
     tc_fence_after_sync();
     last = reinterpret_cast<const volatile TileDesc*>(c.desc)->flags & kTileLast;
     const uint32_t valid4 = reinterpret_cast<const volatile TileDesc*>(c.desc)->valid;
@@ -665,7 +666,7 @@ __device__ __noinline__ void sparse_careful_unit(const SparseCta<D>& c, const Sp
     }
     mbar_wait(pv_done, tick & 1, c.abort_flag);   // K, V, S, P and the descriptor may be overwritten
     tc_fence_after_sync();
-    if (last) { ++tick; break; }   // the same for every thread; after a wait has run out the others return at once
+    if (last) { ++tick; break; }   // the same for every thread
   }
   __syncthreads();
   if (softmax) {
