@@ -774,12 +774,12 @@ sparse_attn_fwd_kernel(const __grid_constant__ SparseMaps maps, const __grid_con
 }
 
 // Joins the parts of split units: weights exp(LSE_s - LSE), a warp per (sample, head, query) row.  Bandwidth: the parts are
-// read once.
+// read once.  This kernel may be running while the one that writes the parts still does, so they are no read-only data to it:
+// no const __restrict__, which would allow loads ahead of dependency_wait.
 template <int D>
 __global__ void __launch_bounds__(256)
-sparse_combine_kernel(const float* __restrict__ part_o, const float* __restrict__ part_lse, const int splits,
-                      const long long rows, const int n_q, const int heads, __nv_bfloat16* __restrict__ o,
-                      float* __restrict__ lse) {
+sparse_combine_kernel(const float* part_o, const float* part_lse, const int splits, const long long rows, const int n_q,
+                      const int heads, __nv_bfloat16* o, float* lse) {
   constexpr int kPer = D / 32;
   dependency_wait();
   const long long at = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
