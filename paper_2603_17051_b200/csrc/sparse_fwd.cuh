@@ -11,8 +11,8 @@
 //
 // Precision: bf16 products, fp32 sums.  P is rounded to bf16 for P V (half a step, 2^-8 of each weight at most), the row sum is taken from the
 // fp32 values.  Fast pass: each row keeps the maximum of its unit's first tile as its one reference; exp2(s - m) is exact for
-// any reference as long as nothing overflows.  A unit with a row sum beyond 2^100, an infinity or a NaN is done
-// again by the careful pass: a plain loop, tile by tile, with the running maximum of the textbook.
+// any reference as long as nothing overflows.  A unit with a row sum beyond 2^100, an infinity or a NaN, or whose first tile gives
+// a row no finite score, is done again by the careful pass: a plain loop, tile by tile, with the running maximum of the textbook.
 //
 // Bound: the tensor pipe and its hand-offs.  A tile takes 1600 to 1670 clocks (the dense kernel's 1630), of which the MMAs are
 // 1024: S -> softmax 1250 -> hand-over 300 -> P V and the next S 1250, two tiles in flight.  Layer shape, 64 of 273 blocks of
@@ -442,7 +442,9 @@ __device__ __forceinline__ bool sparse_softmax(const SparseCta<D>& c, const Spar
     ++maxima;
 #pragma unroll
     for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
-    m_ref = mx == -INFINITY ? 0.f : mx * scale_log2;   // no key in an empty list's tile
+    // 0 for the empty list's tile alone.  Keys whose scores are all -infinity leave -infinity, and with it an infinite or NaN row
+    // sum: 0 would be no reference for the tiles to come, whose scores may lie far below it.
+    m_ref = d.valid == 0u ? 0.f : mx * scale_log2;
     l_run = sparse_exp32(s, valid, scale_log2, -m_ref, pk);
     tmem_st16(colS, pk);
     tmem_wait_st();
