@@ -63,9 +63,9 @@ __global__ void wait_timeout_selftest_kernel(long long cycle_limit) {
   }
   __syncthreads();
   uint64_t* bar = threadIdx.x == 0 ? &never : &done;
-  bool went_on = mbar_wait(bar, 0, &abort_flag, cycle_limit);
-  went_on = mbar_wait_relaxed(bar, 0, &abort_flag) || went_on;   // these two return at once: the flag is up
-  went_on = mbar_wait_at(smem_u32(bar), 0, smem_u32(&abort_flag)) || went_on;
+  bool went_on = mbar_wait_ok(bar, 0, &abort_flag, cycle_limit);
+  went_on = mbar_wait_relaxed_ok(bar, 0, &abort_flag) || went_on;   // these two return at once: the flag is up
+  went_on = mbar_wait_at_ok(smem_u32(bar), 0, smem_u32(&abort_flag)) || went_on;
   if (went_on) atomicOr(&g_device_status, kStatusWarpParted);
 }
 }  // namespace astro

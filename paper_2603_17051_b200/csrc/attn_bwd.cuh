@@ -416,7 +416,7 @@ chunk_attn_bwd_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid
     }
     for (int i = 0; i < n_tiles; ++i) {
       const int st = i % kDkvStages;
-      const bool go = mbar_wait(q_empty + st, ((i / kDkvStages) & 1) ^ 1, abort_flag);
+      const bool go = mbar_wait_ok(q_empty + st, ((i / kDkvStages) & 1) ^ 1, abort_flag);
       if (lane == 0 && go) {   // no copies once a wait has run out
         mbar_arrive_expect_tx(q_full + st, 2 * TileGeom<D>::kBytes);
         tma_load_tile<D>(sQ + st * TileGeom<D>::kBytes, &tm_q, q_full + st, i * kTile, h, b);

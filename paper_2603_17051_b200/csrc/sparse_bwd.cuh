@@ -174,7 +174,7 @@ __device__ __forceinline__ void sparse_bwd_dq(uint8_t* smem_raw, const SparseMap
     ListWalker w;
     w.open(geom, list, a.n_select, lane, first_entries);
     for (int j = 0;; ++j) {
-      if (!mbar_wait(unlisted + j % kSpDescs, ((j / kSpDescs) & 1) ^ 1, abort_flag)) break;
+      if (!mbar_wait_ok(unlisted + j % kSpDescs, ((j / kSpDescs) & 1) ^ 1, abort_flag)) break;
       uint32_t valid;
       const bool last = next_tile(geom, w, h, b, bx, source + j % kSpDescs, valid);
       if (lane == 0) {
@@ -296,11 +296,11 @@ __device__ __forceinline__ void sparse_bwd_dq(uint8_t* smem_raw, const SparseMap
       const uint32_t valid = reinterpret_cast<volatile TileDesc*>(desc + j % kSpDescs)->valid >> (16 * g);   // two bytes
       __syncwarp();
       if (lane == 0) mbar_arrive(unlisted + j % kSpDescs);
-      ok = mbar_wait(s_full, j & 1, abort_flag) && ok;
+      ok = mbar_wait_ok(s_full, j & 1, abort_flag) && ok;
       tc_fence_after_sync();
       if (idle) {   // rows of an MMA do not mix: what dS holds here ends in rows of dQ that nobody stores
         warp_arrive(rs + j % 4, lane);
-        ok = mbar_wait(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
+        ok = mbar_wait_ok(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
         warp_arrive(rb + j % 4, lane);
         if ((flags & kTileLast) || !__all_sync(0xffffffffu, ok)) break;
         continue;
@@ -321,7 +321,7 @@ __device__ __forceinline__ void sparse_bwd_dq(uint8_t* smem_raw, const SparseMap
           p2[c2][c >> 1] = f32x2(fast_exp2(x0), fast_exp2(x1));
         }
       // commit j+1 of b_done: dP(j) is there, and dQ(j-1) has consumed the one dS buffer
-      ok = mbar_wait(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
+      ok = mbar_wait_ok(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
       tc_fence_after_sync();
       uint32_t dp[2][32], ds[2][16];
       tmem_ld32(tmem_lane + kColdP + g * kDqCols, dp[0]);
@@ -468,7 +468,7 @@ __device__ __forceinline__ void sparse_bwd_dkv(uint8_t* smem_raw, const CUtensor
       }
       --times;
       const int st = i % kDkvStages;
-      const bool go = mbar_wait(q_empty + st, ((i / kDkvStages) & 1) ^ 1, abort_flag);
+      const bool go = mbar_wait_ok(q_empty + st, ((i / kDkvStages) & 1) ^ 1, abort_flag);
       if (!go) break;   // no copies once a wait has run out
       if (lane == 0) {
         mbar_arrive_expect_tx(q_full + st, 2 * TileGeom<D>::kBytes);
@@ -534,8 +534,8 @@ __device__ __forceinline__ void sparse_bwd_dkv(uint8_t* smem_raw, const CUtensor
     const uint64_t sc2 = f32x2(scale_log2, scale_log2);
     for (int i = 0; i < n_tiles; ++i) {
       const float* stat = sStat + (i % kDkvStages) * 2 * kTile + g * 64;
-      bool ok = mbar_wait(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
-      ok = mbar_wait(s_full, i & 1, abort_flag) && ok;
+      bool ok = mbar_wait_ok(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
+      ok = mbar_wait_ok(s_full, i & 1, abort_flag) && ok;
       if (!ok) break;
       tc_fence_after_sync();
       uint32_t s[2][32], pt[32];
@@ -566,7 +566,7 @@ __device__ __forceinline__ void sparse_bwd_dkv(uint8_t* smem_raw, const CUtensor
       tc_fence_before_sync();
       warp_arrive(p_full, lane);
 
-      if (!mbar_wait(dp_full, i & 1, abort_flag)) break;
+      if (!mbar_wait_ok(dp_full, i & 1, abort_flag)) break;
       tc_fence_after_sync();
 #pragma unroll
       for (int c2 = 0; c2 < 2; ++c2) {

@@ -129,7 +129,7 @@ sparse_decode_kernel(const __grid_constant__ SparseMaps maps, const __grid_const
       const int st = j % kDecodeStages;
       uint32_t valid;
       const bool last = next_tile(g, w, h, b, a.cache_shared ? 0 : b, source, valid);   // before the wait for the stage
-      if (!mbar_wait(empty + st, ((j / kDecodeStages) & 1) ^ 1, abort_flag)) break;
+      if (!mbar_wait_ok(empty + st, ((j / kDecodeStages) & 1) ^ 1, abort_flag)) break;
       if (lane == 0) {
         if (is_k) {   // the readers of the stage's last descriptor have returned its K
           desc[st].valid = valid;
@@ -162,7 +162,7 @@ sparse_decode_kernel(const __grid_constant__ SparseMaps maps, const __grid_const
     for (int j = 0;; ++j) {
       const int st = j % kDecodeStages;
       const uint32_t phase = (j / kDecodeStages) & 1;
-      bool ok = mbar_wait(k_full + st, phase, abort_flag);
+      bool ok = mbar_wait_ok(k_full + st, phase, abort_flag);
       const uint32_t flags = reinterpret_cast<volatile TileDesc*>(desc + st)->flags;
       const uint32_t valid4 = reinterpret_cast<volatile TileDesc*>(desc + st)->valid;
       const int valid = static_cast<int>((valid4 >> (8 * (warp * kKeys / 32))) & 0xff) - warp * kKeys % 32;   // of this warp's keys
@@ -201,7 +201,7 @@ sparse_decode_kernel(const __grid_constant__ SparseMaps maps, const __grid_const
         }
       }
       warp_arrive(k_empty + st, lane);
-      ok = mbar_wait(v_full + st, phase, abort_flag) && ok;
+      ok = mbar_wait_ok(v_full + st, phase, abort_flag) && ok;
       if (valid > 0) {
 #pragma unroll
         for (int i = 0; i < kPerGroup; ++i) {

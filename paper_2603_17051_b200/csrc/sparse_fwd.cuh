@@ -171,7 +171,7 @@ __device__ __forceinline__ void sparse_walk(const SparseCta<D>& c, const SparseG
   int J = 0;
   bool over = false;
   // a slot of the rings; false once a wait has run out
-  auto slot = [&]() { return J < 4 || mbar_wait(bar.sdone + J % 4, ((J - 4) / 4) & 1, c.abort_flag); };
+  auto slot = [&]() { return J < 4 || mbar_wait_ok(bar.sdone + J % 4, ((J - 4) / 4) & 1, c.abort_flag); };
   while (!over) {
     st.open(g, s, a, lane);
     const bool last_unit = st.unit >= s.total;
@@ -364,7 +364,7 @@ __device__ __noinline__ SparseRun sparse_run(SparseLoop c, float scale_log2, flo
   while (true) {
     const uint32_t colS = c.lane_s + (J % kFwdSBufs) * 128;
     const int valid = (d.valid >> (8 * c.g)) & 0xff;
-    ok = mbar_wait_at(c.sdone + 8 * (J % 4), (J / 4) & 1, c.abort_flag);
+    ok = mbar_wait_at_ok(c.sdone + 8 * (J % 4), (J / 4) & 1, c.abort_flag);
     tc_fence_after_sync();
     uint32_t sv[32], pk[16];
     tmem_ld32(colS, sv);
@@ -388,7 +388,7 @@ __device__ __noinline__ SparseRun sparse_idle(SparseLoop c, int J, TileDesc d) {
   const int lane = threadIdx.x & 31;
   bool ok = true;
   while (true) {
-    ok = mbar_wait_at(c.sdone + 8 * (J % 4), (J / 4) & 1, c.abort_flag);
+    ok = mbar_wait_at_ok(c.sdone + 8 * (J % 4), (J / 4) & 1, c.abort_flag);
     warp_arrive_at(c.ready + 8 * (J % 4), lane);
     if ((d.flags & kTileLast) || !ok) break;
     ++J;
@@ -429,7 +429,7 @@ __device__ __forceinline__ bool sparse_softmax(const SparseCta<D>& c, const Spar
     // the unit's first tile fixes the rows' reference
     const int valid = (d.valid >> (8 * g)) & 0xff;
     const uint32_t colS = lp.lane_s + (J % kFwdSBufs) * 128;
-    ok = mbar_wait_at(lp.sdone + 8 * (J % 4), (J / 4) & 1, lp.abort_flag);
+    ok = mbar_wait_at_ok(lp.sdone + 8 * (J % 4), (J / 4) & 1, lp.abort_flag);
     tc_fence_after_sync();
     uint32_t s[32], pk[16];
     tmem_ld32(colS, s);
@@ -438,7 +438,7 @@ __device__ __forceinline__ bool sparse_softmax(const SparseCta<D>& c, const Spar
     float mx = row_max(s, valid);
     slot[g * kTile + r] = mx;
     warp_arrive(bar.max_full + (warp & 3), lane);
-    ok = mbar_wait(bar.max_full + (warp & 3), maxima & 1, abort_flag) && ok;
+    ok = mbar_wait_ok(bar.max_full + (warp & 3), maxima & 1, abort_flag) && ok;
     ++maxima;
 #pragma unroll
     for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
@@ -551,14 +551,14 @@ __device__ __forceinline__ bool sparse_epilogue(const SparseCta<D>& c, const Spa
   int n = 0;
   for (int unit = s.first; unit < s.total; unit += s.stride, ++n) {
     const SparseRow<D> row(s, SparseUnit(s, unit, a.heads, a.batch), a, r);
-    if (!mbar_wait_relaxed(bar.stats_full + (n & 1), (n >> 1) & 1, c.abort_flag)) break;
+    if (!mbar_wait_relaxed_ok(bar.stats_full + (n & 1), (n >> 1) & 1, c.abort_flag)) break;
     float l = 0.f;
 #pragma unroll
     for (int g = 0; g < kFwdGroups; ++g) l += stats.sums(n)[g * kTile + r];
     const float m = stats.refs(n)[r];
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint64_t chk2 = f32x2(0.f, 0.f);
-    if (!mbar_wait(bar.o_full, n & 1, c.abort_flag)) break;
+    if (!mbar_wait_ok(bar.o_full, n & 1, c.abort_flag)) break;
     tc_fence_after_sync();
     uint32_t acc[kOwn][32];
 #pragma unroll
