@@ -478,26 +478,28 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // 2^x for a pair on the FMA and integer pipes instead of the special-function unit: round x to the
 // nearest integer n with the 1.5*2^23 trick, evaluate a cubic for 2^(x-n) on [-0.5, 0.5] (relative error
-// 7.6e-5, far below the 2^-9 of the bf16 rounding that follows) and add n to the exponent field.
-// x is clamped to >= -126 so the exponent field cannot wrap.
+// 7.6e-5, far below the 2^-9 of the bf16 rounding that follows) and multiply by 2^n, whose exponent field the rounded number's last
+// bits are (127 is added with the constant).  x is clamped to >= -126 so that the field cannot wrap.  NaN passes the clamp and
+// the product; added to the exponent field as an integer, n would have made a number of it.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ void exp2_poly_pair(uint64_t x2, float& p0, float& p1) {
   float x0, x1;
   f32x2_split(x2, x0, x1);
-  x0 = fmaxf(x0, -126.f);
-  x1 = fmaxf(x1, -126.f);
-  const uint64_t xc = f32x2(x0, x1);
-  const uint64_t t2 = add2(xc, f32x2(12582912.f, 12582912.f));
-  const uint64_t n2 = add2(t2, f32x2(-12582912.f, -12582912.f));
+  const uint64_t xc = f32x2(max_nan(x0, -126.f), max_nan(x1, -126.f));
+  const uint64_t t2 = add2(xc, f32x2(12583039.f, 12583039.f));   // 1.5 * 2^23 + 127
+  const uint64_t n2 = add2(t2, f32x2(-12583039.f, -12583039.f));
   const uint64_t f2 = fma2(n2, f32x2(-1.f, -1.f), xc);
   uint64_t q2 = fma2(f2, f32x2(0.055205512791872025f, 0.055205512791872025f),
                      f32x2(0.24261389672756195f, 0.24261389672756195f));
   q2 = fma2(q2, f2, f32x2(0.6932547688484192f, 0.6932547688484192f));
   q2 = fma2(q2, f2, f32x2(0.9999276995658875f, 0.9999276995658875f));
-  float q0, q1, t0, t1;
-  f32x2_split(q2, q0, q1);
+  float t0, t1;
   f32x2_split(t2, t0, t1);
-  p0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
-  p1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
+  f32x2_split(mul2(q2, f32x2(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23))), p0, p1);
 }
 
 }  // namespace astro
