@@ -7,6 +7,7 @@ device memory and the current stream, nothing else.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 from . import build as _build
@@ -237,14 +238,26 @@ def _lists(q, dev, blocks):
     return s[3]
 
 
-def _used_on(stream, *tensors):
-    """Tensors this wrapper allocated are used by kernels on `stream`: tell torch's caching allocator, so that
-    a block dropped by the caller is not handed out again (on the allocating stream) while they still run."""
+_HERE = contextlib.nullcontext()
+
+
+def _owned_by(stream):
+    """Context in which a wrapper allocates: what its kernels use on `stream` comes out of that stream's memory.  torch hands
+    out memory whose last use may still be queued on the stream that it belongs to, and on that one alone."""
+    import torch
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
+def _used_here(stream, *tensors):
+    """Tensors a wrapper allocated for `stream` are for the caller, who may be on another: tell torch's caching allocator, so that
+    a block that the caller drops is not handed out again on `stream` while the caller's work still uses it."""
     if stream is None:
         return
+    import torch
+    here = torch.cuda.current_stream(stream.device)
     for t in tensors:
         if t is not None:
-            t.record_stream(stream)
+            t.record_stream(here)
 
 
 def _desc(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames):
@@ -345,8 +358,10 @@ def astro_kvcache_export(cache: KVCache, stream=None):
     sink, win, _ = astro_kvcache_query(cache)
     d = cache.desc
     shape = (d.cache_batch, (sink + win) * d.tokens_per_frame, d.heads, d.head_dim)
-    k = torch.empty(shape, dtype=torch.bfloat16, device=cache.k_storage.device)
-    v = torch.empty_like(k)
+    with _owned_by(stream):
+        k = torch.empty(shape, dtype=torch.bfloat16, device=cache.k_storage.device)
+        v = torch.empty_like(k)
+    _used_here(stream, k, v)
     if sink + win:
         _check(lib().astro_kvcache_export(cache.handle, _ptr(k), _ptr(v), _stream(stream)), "astro_kvcache_export")
     return k, v
@@ -358,12 +373,13 @@ def astro_chunk_attn_fwd(cache, q, k_chunk, v_chunk, scale: float, o=None, lse=N
     B, n_q, H, D = q.shape
     n_kc = 0 if k_chunk is None else k_chunk.shape[1]
     fresh = []
-    if o is None:
-        o = torch.empty_like(q); fresh.append(o)
-    if lse is None:
-        lse = torch.empty((B, H, n_q), dtype=torch.float32, device=q.device); fresh.append(lse)
+    with _owned_by(stream):
+        if o is None:
+            o = torch.empty_like(q); fresh.append(o)
+        if lse is None:
+            lse = torch.empty((B, H, n_q), dtype=torch.float32, device=q.device); fresh.append(lse)
     _contiguous(q, k_chunk, v_chunk, o, lse)
-    _used_on(stream, *fresh)
+    _used_here(stream, *fresh)
     st = lib().astro_chunk_attn_fwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
                                     B, H, D, n_q, n_kc, float(scale), _ptr(o), _ptr(lse), _stream(stream))
     _check(st, "astro_chunk_attn_fwd")
@@ -381,17 +397,18 @@ def astro_chunk_attn_bwd(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: float, 
     B, n_q, H, D = q.shape
     n_kc = 0 if k_chunk is None else k_chunk.shape[1]
     fresh = []
-    if dq is None:
-        dq = torch.empty_like(q); fresh.append(dq)
-    if n_kc and dk_chunk is None:
-        dk_chunk = torch.empty_like(k_chunk); fresh.append(dk_chunk)
-    if n_kc and dv_chunk is None:
-        dv_chunk = torch.empty_like(v_chunk); fresh.append(dv_chunk)
-    need = astro_chunk_attn_bwd_workspace_bytes(B, H, n_q, D)
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    with _owned_by(stream):
+        if dq is None:
+            dq = torch.empty_like(q); fresh.append(dq)
+        if n_kc and dk_chunk is None:
+            dk_chunk = torch.empty_like(k_chunk); fresh.append(dk_chunk)
+        if n_kc and dv_chunk is None:
+            dv_chunk = torch.empty_like(v_chunk); fresh.append(dv_chunk)
+        if workspace is None:
+            need = astro_chunk_attn_bwd_workspace_bytes(B, H, n_q, D)
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
     _contiguous(q, k_chunk, v_chunk, o, lse, d_o, dq, dk_chunk, dv_chunk)
-    _used_on(stream, *fresh)
+    _used_here(stream, *fresh)
     st = lib().astro_chunk_attn_bwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
                                     _ptr(o), _ptr(lse), _ptr(d_o), B, H, D, n_q, n_kc, float(scale), _ptr(dq),
                                     _ptr(dk_chunk), _ptr(dv_chunk), _ptr(workspace),
@@ -405,8 +422,9 @@ def astro_chunk_attn_bwd_delta(o, d_o, delta=None, stream=None):
     import torch
     B, n_q, H, D = o.shape
     if delta is None:
-        delta = torch.empty((B, H, n_q), dtype=torch.float32, device=o.device)
-        _used_on(stream, delta)
+        with _owned_by(stream):
+            delta = torch.empty((B, H, n_q), dtype=torch.float32, device=o.device)
+        _used_here(stream, delta)
     _contiguous(o, d_o, delta)
     _check(lib().astro_chunk_attn_bwd_delta(_ptr(o), _ptr(d_o), B, H, D, n_q, _ptr(delta), _stream(stream)),
            "astro_chunk_attn_bwd_delta")
@@ -418,8 +436,9 @@ def astro_chunk_attn_bwd_dq(cache, q, k_chunk, v_chunk, lse, delta, d_o, scale: 
     B, n_q, H, D = q.shape
     n_kc = 0 if k_chunk is None else k_chunk.shape[1]
     if dq is None:
-        dq = torch.empty_like(q)
-        _used_on(stream, dq)
+        with _owned_by(stream):
+            dq = torch.empty_like(q)
+        _used_here(stream, dq)
     _contiguous(q, k_chunk, v_chunk, lse, delta, d_o, dq)
     st = lib().astro_chunk_attn_bwd_dq(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
                                        _ptr(lse), _ptr(delta), _ptr(d_o), B, H, D, n_q, n_kc, float(scale), _ptr(dq),
@@ -433,12 +452,13 @@ def astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, scale: float,
     import torch
     B, n_q, H, D = q.shape
     n_kc = k_chunk.shape[1]
-    if dk_chunk is None:
-        dk_chunk = torch.empty_like(k_chunk)
-        _used_on(stream, dk_chunk)
-    if dv_chunk is None:
-        dv_chunk = torch.empty_like(v_chunk)
-        _used_on(stream, dv_chunk)
+    fresh = []
+    with _owned_by(stream):
+        if dk_chunk is None:
+            dk_chunk = torch.empty_like(k_chunk); fresh.append(dk_chunk)
+        if dv_chunk is None:
+            dv_chunk = torch.empty_like(v_chunk); fresh.append(dv_chunk)
+    _used_here(stream, *fresh)
     _contiguous(q, k_chunk, v_chunk, lse, delta, d_o, dk_chunk, dv_chunk)
     st = lib().astro_chunk_attn_bwd_dkv(_ptr(q), _ptr(k_chunk), _ptr(v_chunk), _ptr(lse), _ptr(delta), _ptr(d_o), B, H,
                                         D, n_q, n_kc, float(scale), _ptr(dk_chunk), _ptr(dv_chunk), _stream(stream))
@@ -540,14 +560,16 @@ def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=N
     dev, on = _where(stream, q)
     fresh = []
     if q_out is None:
-        q_out = _dense_like(q); fresh.append(q_out)
+        with _owned_by(stream):
+            q_out = _dense_like(q); fresh.append(q_out)
     elif q_out.shape != shape or q_out.dtype is not q.dtype or q_out.get_device() != dev:
         raise ValueError("q_out must be like q")
     if k is not None:
         if k.dim() != 4 or k.dtype is not q.dtype or k.shape[0] != B or k.shape[1] != n or k.shape[3] != shape[3] or k.get_device() != dev:
             raise ValueError("k must be [B, n, heads, head_dim] of q's type, beside it")
         if k_out is None:
-            k_out = _dense_like(k); fresh.append(k_out)
+            with _owned_by(stream):
+                k_out = _dense_like(k); fresh.append(k_out)
         elif k_out.shape != k.shape or k_out.dtype is not k.dtype or k_out.get_device() != dev:
             raise ValueError("k_out must be like k")
     else:
@@ -556,7 +578,7 @@ def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=N
     if pb != 1 and pb != B:
         raise ValueError("positions must be [B or 1, n, axes]")
     _like((pb, n, rope.desc.axes), torch.int32, dev, positions)
-    _used_on(stream, *fresh)
+    _used_here(stream, *fresh)
 
     def call(x, x2, y, y2, strides):
         _check(lib().astro_rope_apply(rope.handle, 1 if inverse else 0, _at(x), _at(x2), _at(positions), pb, B, n, x.shape[2],
@@ -609,13 +631,9 @@ def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_
         raise AstroError(2, "astro_block_pool")
     shape = _pooled_shape(cache, block_tokens)
     if pooled is None:
-        pooled = torch.empty(shape, dtype=torch.float32, device=cache.k_storage.device)
-        _used_on(stream, pooled)
-        if stream is None:
-            pooled.zero_()
-        else:
-            with torch.cuda.stream(stream):   # the means go there: cleared elsewhere, they could be wiped
-                pooled.zero_()
+        with _owned_by(stream):   # and cleared there too: on another stream the clearing could wipe the means
+            pooled = torch.zeros(shape, dtype=torch.float32, device=cache.k_storage.device)
+        _used_here(stream, pooled)
     else:
         _like(shape, torch.float32, dev, pooled)
     _check(lib().astro_block_pool(_handle(cache, dev), int(first_frame), int(n_frames), int(block_tokens), _at(pooled), on),
@@ -637,17 +655,18 @@ def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: i
     _like(q.shape, torch.bfloat16, dev, q)
     n_kc = _chunk(q, dev, k_chunk, None)
     shape = (B, H, (n_q + QUERY_BLOCK - 1) // QUERY_BLOCK, max(1, int(n_select)))
-    fresh = []
-    if blocks is None:
-        blocks = q.new_empty(shape, dtype=torch.int32); fresh.append(blocks)
-    else:
+    if blocks is not None:
         _like(shape, torch.int32, dev, blocks)
-    if workspace is None:
-        need = astro_block_select_workspace_bytes(B, H, D, n_q, n_kc, block_tokens)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    fresh = []
+    with _owned_by(stream):
+        if blocks is None:
+            blocks = q.new_empty(shape, dtype=torch.int32); fresh.append(blocks)
+        if workspace is None:
+            need = astro_block_select_workspace_bytes(B, H, D, n_q, n_kc, block_tokens)
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
     if pooled is not None and cache is not None and int(block_tokens) >= 1:
         _like(_pooled_shape(cache, block_tokens), torch.float32, dev, pooled)
-    _used_on(stream, *fresh)
+    _used_here(stream, *fresh)
     st = lib().astro_block_select(_handle(cache, dev), _at(pooled), _at(q), _at(k_chunk), B, H, D, n_q, n_kc, int(block_tokens),
                                   int(n_select), int(keep), _at(blocks), *_scratch(workspace, dev), on)
     _check(st, "astro_block_select")
@@ -670,18 +689,19 @@ def astro_sparse_attn_fwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
     B, n_q, H, D = shape
     _like(shape, torch.bfloat16, dev, q, o)
     n_kc, n_select = _chunk(q, dev, k_chunk, v_chunk), _lists(q, dev, blocks)
-    fresh = []
-    if o is None:
-        o = torch.empty_like(q); fresh.append(o)
-    if lse is None:
-        lse = q.new_empty((B, H, n_q), dtype=torch.float32); fresh.append(lse)
-    else:
+    if lse is not None:
         _like((B, H, n_q), torch.float32, dev, lse)
-    if workspace is None:
-        need = astro_sparse_attn_fwd_workspace_bytes(B, H, D, n_q, n_select, block_tokens)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _used_on(stream, *fresh)
+    fresh = []
+    with _owned_by(stream):
+        if o is None:
+            o = torch.empty_like(q); fresh.append(o)
+        if lse is None:
+            lse = q.new_empty((B, H, n_q), dtype=torch.float32); fresh.append(lse)
+        if workspace is None:
+            need = astro_sparse_attn_fwd_workspace_bytes(B, H, D, n_q, n_select, block_tokens)
+            if need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _used_here(stream, *fresh)
     st = lib().astro_sparse_attn_fwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), _at(blocks), n_select,
                                      int(block_tokens), B, H, D, n_q, n_kc, float(scale), _at(o), _at(lse),
                                      *_scratch(workspace, dev), on)
@@ -706,16 +726,17 @@ def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
     _like((B, H, n_q), torch.float32, dev, lse)
     n_kc, n_select = _chunk(q, dev, k_chunk, v_chunk, dk_chunk, dv_chunk), _lists(q, dev, blocks)
     fresh = []
-    if dq is None:
-        dq = torch.empty_like(q); fresh.append(dq)
-    if n_kc and dk_chunk is None:
-        dk_chunk = torch.empty_like(k_chunk); fresh.append(dk_chunk)
-    if n_kc and dv_chunk is None:
-        dv_chunk = torch.empty_like(v_chunk); fresh.append(dv_chunk)
-    if workspace is None:
-        need = astro_sparse_attn_bwd_workspace_bytes(B, H, D, n_q, n_kc, n_select, block_tokens)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    _used_on(stream, *fresh)
+    with _owned_by(stream):
+        if dq is None:
+            dq = torch.empty_like(q); fresh.append(dq)
+        if n_kc and dk_chunk is None:
+            dk_chunk = torch.empty_like(k_chunk); fresh.append(dk_chunk)
+        if n_kc and dv_chunk is None:
+            dv_chunk = torch.empty_like(v_chunk); fresh.append(dv_chunk)
+        if workspace is None:
+            need = astro_sparse_attn_bwd_workspace_bytes(B, H, D, n_q, n_kc, n_select, block_tokens)
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _used_here(stream, *fresh)
     st = lib().astro_sparse_attn_bwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), _at(blocks), n_select,
                                      int(block_tokens), _at(o), _at(lse), _at(d_o), B, H, D, n_q, n_kc, float(scale), _at(dq),
                                      _at(dk_chunk), _at(dv_chunk), *_scratch(workspace, dev), on)
@@ -735,10 +756,11 @@ def astro_nft_loss(v_theta, v_old, v_ref, v_target, r_tilde, beta: float, w_poli
     if out is not None:
         policy, kl, g = out
     else:
-        policy = torch.empty(B, dtype=torch.float32, device=v_theta.device)
-        kl = None if v_ref is None else torch.empty(B, dtype=torch.float32, device=v_theta.device)
-        g = torch.empty_like(v_theta) if grad else None
-        _used_on(stream, policy, kl, g)
+        with _owned_by(stream):
+            policy = torch.empty(B, dtype=torch.float32, device=v_theta.device)
+            kl = None if v_ref is None else torch.empty(B, dtype=torch.float32, device=v_theta.device)
+            g = torch.empty_like(v_theta) if grad else None
+        _used_here(stream, policy, kl, g)
     _contiguous(v_theta, v_old, v_ref, v_target, g)
     st = lib().astro_nft_loss(_ptr(v_theta), _ptr(v_old), _ptr(v_ref), _ptr(v_target), _ptr(r_tilde), _ptr(w_policy),
                               _ptr(w_kl), B, elems, float(beta), _ptr(policy), _ptr(kl), _ptr(g), _stream(stream))
