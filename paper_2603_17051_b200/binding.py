@@ -204,12 +204,21 @@ def _scratch(workspace, dev):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+def _cache(cache):
+    """Handle of a cache or None for none.  One that has been destroyed is refused: as a null handle it would be no context."""
+    if cache is None:
+        return None
+    if cache.handle is None:
+        raise ValueError("the cache has been destroyed")
+    return cache.handle
+
+
 def _handle(cache, dev):
     if cache is None:
         return None
     if cache.k_storage.get_device() != dev or cache.v_storage.get_device() != dev:
         raise ValueError("the cache is on %s, the call on cuda:%d" % (cache.k_storage.device, dev))
-    return cache.handle
+    return _cache(cache)
 
 
 def _at(t):
@@ -347,7 +356,7 @@ def astro_kvcache_key_segments(cache, n_kc: int):
     """List of (first_token, token_count, from_chunk) the attention kernels would walk (host only)."""
     n = C.c_int()
     a, b, c = (C.c_int * 3)(), (C.c_int * 3)(), (C.c_int * 3)()
-    _check(lib().astro_kvcache_key_segments(None if cache is None else cache.handle, int(n_kc), C.byref(n), a, b, c),
+    _check(lib().astro_kvcache_key_segments(_cache(cache), int(n_kc), C.byref(n), a, b, c),
            "astro_kvcache_key_segments")
     return [(a[i], b[i], c[i]) for i in range(n.value)]
 
@@ -380,7 +389,7 @@ def astro_chunk_attn_fwd(cache, q, k_chunk, v_chunk, scale: float, o=None, lse=N
             lse = torch.empty((B, H, n_q), dtype=torch.float32, device=q.device); fresh.append(lse)
     _contiguous(q, k_chunk, v_chunk, o, lse)
     _used_here(stream, *fresh)
-    st = lib().astro_chunk_attn_fwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
+    st = lib().astro_chunk_attn_fwd(_cache(cache), _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
                                     B, H, D, n_q, n_kc, float(scale), _ptr(o), _ptr(lse), _stream(stream))
     _check(st, "astro_chunk_attn_fwd")
     return o, lse
@@ -409,7 +418,7 @@ def astro_chunk_attn_bwd(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: float, 
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
     _contiguous(q, k_chunk, v_chunk, o, lse, d_o, dq, dk_chunk, dv_chunk)
     _used_here(stream, *fresh)
-    st = lib().astro_chunk_attn_bwd(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
+    st = lib().astro_chunk_attn_bwd(_cache(cache), _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
                                     _ptr(o), _ptr(lse), _ptr(d_o), B, H, D, n_q, n_kc, float(scale), _ptr(dq),
                                     _ptr(dk_chunk), _ptr(dv_chunk), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _stream(stream))
@@ -440,7 +449,7 @@ def astro_chunk_attn_bwd_dq(cache, q, k_chunk, v_chunk, lse, delta, d_o, scale: 
             dq = torch.empty_like(q)
         _used_here(stream, dq)
     _contiguous(q, k_chunk, v_chunk, lse, delta, d_o, dq)
-    st = lib().astro_chunk_attn_bwd_dq(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
+    st = lib().astro_chunk_attn_bwd_dq(_cache(cache), _ptr(q), _ptr(k_chunk), _ptr(v_chunk),
                                        _ptr(lse), _ptr(delta), _ptr(d_o), B, H, D, n_q, n_kc, float(scale), _ptr(dq),
                                        _stream(stream))
     _check(st, "astro_chunk_attn_bwd_dq")
@@ -609,7 +618,7 @@ KEEP_SINK, KEEP_CHUNK = 1, 2
 def astro_block_count(cache, n_kc: int, block_tokens: int):
     """(cache blocks, chunk blocks) that a call numbers (host only)."""
     a, b = C.c_int(), C.c_int()
-    _check(lib().astro_block_count(None if cache is None else cache.handle, int(n_kc), int(block_tokens), C.byref(a), C.byref(b)),
+    _check(lib().astro_block_count(_cache(cache), int(n_kc), int(block_tokens), C.byref(a), C.byref(b)),
            "astro_block_count")
     return a.value, b.value
 
@@ -780,7 +789,7 @@ def astro_chunk_attn_bwd_static(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: 
     B, n_q, H, D = q.shape
     n_kc = 0 if k_chunk is None else k_chunk.shape[1]
     _contiguous(q, k_chunk, v_chunk, o, lse, d_o, dq, dk_chunk, dv_chunk)
-    st = lib().astro_chunk_attn_bwd_static(None if cache is None else cache.handle, _ptr(q), _ptr(k_chunk),
+    st = lib().astro_chunk_attn_bwd_static(_cache(cache), _ptr(q), _ptr(k_chunk),
                                            _ptr(v_chunk), _ptr(o), _ptr(lse), _ptr(d_o), B, H, D, n_q, n_kc,
                                            float(scale), _ptr(dq), _ptr(dk_chunk), _ptr(dv_chunk), _stream(stream))
     _check(st, "astro_chunk_attn_bwd_static")
