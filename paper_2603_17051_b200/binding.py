@@ -155,6 +155,13 @@ def _check(status: int, where: str) -> None:
         raise AstroError(status, where)
 
 
+def _int(x):
+    """A whole number for a C int.  ctypes would cut off the bits behind the 32nd; a number that has any becomes one that every
+    call refuses."""
+    x = int(x)
+    return x if -0x80000000 <= x <= 0x7fffffff else -0x80000000
+
+
 def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
@@ -270,8 +277,8 @@ def _used_here(stream, *tensors):
 
 
 def _desc(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames):
-    return KVCacheDesc(int(cache_batch), int(heads), int(head_dim), int(tokens_per_frame), int(sink_frames),
-                       int(window_frames))
+    return KVCacheDesc(_int(cache_batch), _int(heads), _int(head_dim), _int(tokens_per_frame), _int(sink_frames),
+                       _int(window_frames))
 
 
 def astro_kvcache_storage_bytes(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames) -> int:
@@ -327,12 +334,12 @@ def astro_kvcache_reset(cache: KVCache) -> None:
 
 def astro_kvcache_append(cache: KVCache, k, v, n_frames: int, stream=None) -> None:
     """k, v: bf16 [B_c, n_frames*T, H, D] on the device."""
-    _check(lib().astro_kvcache_append(cache.handle, _ptr(k), _ptr(v), int(n_frames), _stream(stream)),
+    _check(lib().astro_kvcache_append(cache.handle, _ptr(k), _ptr(v), _int(n_frames), _stream(stream)),
            "astro_kvcache_append")
 
 
 def astro_kvcache_evict(cache: KVCache, n_frames: int, stream=None) -> None:
-    _check(lib().astro_kvcache_evict(cache.handle, int(n_frames), None), "astro_kvcache_evict")
+    _check(lib().astro_kvcache_evict(cache.handle, _int(n_frames), None), "astro_kvcache_evict")
 
 
 def astro_kvcache_query(cache: KVCache):
@@ -356,7 +363,7 @@ def astro_kvcache_key_segments(cache, n_kc: int):
     """List of (first_token, token_count, from_chunk) the attention kernels would walk (host only)."""
     n = C.c_int()
     a, b, c = (C.c_int * 3)(), (C.c_int * 3)(), (C.c_int * 3)()
-    _check(lib().astro_kvcache_key_segments(_cache(cache), int(n_kc), C.byref(n), a, b, c),
+    _check(lib().astro_kvcache_key_segments(_cache(cache), _int(n_kc), C.byref(n), a, b, c),
            "astro_kvcache_key_segments")
     return [(a[i], b[i], c[i]) for i in range(n.value)]
 
@@ -396,7 +403,7 @@ def astro_chunk_attn_fwd(cache, q, k_chunk, v_chunk, scale: float, o=None, lse=N
 
 
 def astro_chunk_attn_bwd_workspace_bytes(batch, heads, n_q, head_dim) -> int:
-    return int(lib().astro_chunk_attn_bwd_workspace_bytes(int(batch), int(heads), int(n_q), int(head_dim)))
+    return int(lib().astro_chunk_attn_bwd_workspace_bytes(_int(batch), _int(heads), _int(n_q), _int(head_dim)))
 
 
 def astro_chunk_attn_bwd(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: float, dq=None, dk_chunk=None,
@@ -475,6 +482,14 @@ def astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, scale: float,
     return dk_chunk, dv_chunk
 
 
+def _frame_list(frames):
+    """(C array, count) of a list of frame indices, (None, -1) for all."""
+    if frames is None:
+        return None, -1
+    n = len(frames)
+    return (C.c_int * max(1, n))(*[_int(f) for f in frames]), n
+
+
 def astro_kvcache_fork(dst: KVCache, src: KVCache, parents=None, frames=None, stream=None) -> None:
     """Empty `dst` and copy the listed held frames of `src` (logical indices, None = all) into it; parents: int32 [dst
     cache_batch] on the device, the sample of src that each sample of dst continues."""
@@ -482,11 +497,7 @@ def astro_kvcache_fork(dst: KVCache, src: KVCache, parents=None, frames=None, st
     dev, on = _where(stream, dst.k_storage)
     if parents is not None:
         _like((dst.desc.cache_batch,), torch.int32, dev, parents)
-    if frames is None:
-        arr, n = None, -1
-    else:
-        n = len(frames)
-        arr = (C.c_int * max(1, n))(*frames)
+    arr, n = _frame_list(frames)
     _check(lib().astro_kvcache_fork(_handle(dst, dev), _handle(src, dev), _at(parents), arr, n, on), "astro_kvcache_fork")
 
 
@@ -515,7 +526,7 @@ def astro_rope_create(head_dim, rot_dim, layout, axis_pairs, base=10000.0, scali
     if len(axis_pairs) > 4:
         raise AstroError(2, "astro_rope_create")
     axes = range(len(axis_pairs)) if scaled_axes is None else scaled_axes
-    d = RopeDesc(int(head_dim), int(rot_dim), ROPE_LAYOUTS[layout], len(axis_pairs), (C.c_int * 4)(*[int(p) for p in axis_pairs]),
+    d = RopeDesc(_int(head_dim), _int(rot_dim), ROPE_LAYOUTS[layout], len(axis_pairs), (C.c_int * 4)(*[_int(p) for p in axis_pairs]),
                  float(base), ROPE_SCALINGS[scaling], sum(1 << int(a) for a in axes), float(factor), float(original_length),
                  float(ramp_low), float(ramp_high), float(magnitude))
     out = C.c_void_p()
@@ -590,7 +601,7 @@ def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=N
     _used_here(stream, *fresh)
 
     def call(x, x2, y, y2, strides):
-        _check(lib().astro_rope_apply(rope.handle, 1 if inverse else 0, _at(x), _at(x2), _at(positions), pb, B, n, x.shape[2],
+        _check(lib().astro_rope_apply(rope.handle, 1 if inverse else 0, _at(x), _at(x2), _at(positions), pb, B, _int(n), x.shape[2],
                                       0 if x2 is None else x2.shape[2], kind, None if strides is None else C.byref(Strides(*strides[0])),
                                       _at(y), _at(y2), None if strides is None else C.byref(Strides(*strides[1])), on),
                "astro_rope_apply")
@@ -618,14 +629,14 @@ KEEP_SINK, KEEP_CHUNK = 1, 2
 def astro_block_count(cache, n_kc: int, block_tokens: int):
     """(cache blocks, chunk blocks) that a call numbers (host only)."""
     a, b = C.c_int(), C.c_int()
-    _check(lib().astro_block_count(_cache(cache), int(n_kc), int(block_tokens), C.byref(a), C.byref(b)),
+    _check(lib().astro_block_count(_cache(cache), _int(n_kc), _int(block_tokens), C.byref(a), C.byref(b)),
            "astro_block_count")
     return a.value, b.value
 
 
 def _pooled_shape(cache, block_tokens):
     d = cache.desc
-    return (d.cache_batch, d.heads, d.sink_frames + d.window_frames, -(-d.tokens_per_frame // int(block_tokens)), d.head_dim)
+    return (d.cache_batch, d.heads, d.sink_frames + d.window_frames, -(-d.tokens_per_frame // _int(block_tokens)), d.head_dim)
 
 
 def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_frames=None, pooled=None, stream=None):
@@ -634,9 +645,9 @@ def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_
     import torch
     if n_frames is None:
         sink, win, _ = astro_kvcache_query(cache)
-        n_frames = sink + win - int(first_frame)
+        n_frames = sink + win - _int(first_frame)
     dev, on = _where(stream, cache.k_storage)
-    if int(block_tokens) < 1:
+    if _int(block_tokens) < 1:
         raise AstroError(2, "astro_block_pool")
     shape = _pooled_shape(cache, block_tokens)
     if pooled is None:
@@ -645,13 +656,13 @@ def astro_block_pool(cache: KVCache, block_tokens: int, first_frame: int = 0, n_
         _used_here(stream, pooled)
     else:
         _like(shape, torch.float32, dev, pooled)
-    _check(lib().astro_block_pool(_handle(cache, dev), int(first_frame), int(n_frames), int(block_tokens), _at(pooled), on),
+    _check(lib().astro_block_pool(_handle(cache, dev), _int(first_frame), _int(n_frames), _int(block_tokens), _at(pooled), on),
            "astro_block_pool")
     return pooled
 
 
 def astro_block_select_workspace_bytes(batch, heads, head_dim, n_q, n_kc, block_tokens) -> int:
-    return int(lib().astro_block_select_workspace_bytes(int(batch), int(heads), int(head_dim), int(n_q), int(n_kc), int(block_tokens)))
+    return int(lib().astro_block_select_workspace_bytes(_int(batch), _int(heads), _int(head_dim), _int(n_q), _int(n_kc), _int(block_tokens)))
 
 
 def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: int, keep: int = 0, blocks=None, workspace=None,
@@ -663,7 +674,7 @@ def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: i
     B, n_q, H, D = q.shape
     _like(q.shape, torch.bfloat16, dev, q)
     n_kc = _chunk(q, dev, k_chunk, None)
-    shape = (B, H, (n_q + QUERY_BLOCK - 1) // QUERY_BLOCK, max(1, int(n_select)))
+    shape = (B, H, (n_q + QUERY_BLOCK - 1) // QUERY_BLOCK, max(1, _int(n_select)))
     if blocks is not None:
         _like(shape, torch.int32, dev, blocks)
     fresh = []
@@ -673,18 +684,18 @@ def astro_block_select(cache, pooled, q, k_chunk, block_tokens: int, n_select: i
         if workspace is None:
             need = astro_block_select_workspace_bytes(B, H, D, n_q, n_kc, block_tokens)
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
-    if pooled is not None and cache is not None and int(block_tokens) >= 1:
+    if pooled is not None and cache is not None and _int(block_tokens) >= 1:
         _like(_pooled_shape(cache, block_tokens), torch.float32, dev, pooled)
     _used_here(stream, *fresh)
-    st = lib().astro_block_select(_handle(cache, dev), _at(pooled), _at(q), _at(k_chunk), B, H, D, n_q, n_kc, int(block_tokens),
-                                  int(n_select), int(keep), _at(blocks), *_scratch(workspace, dev), on)
+    st = lib().astro_block_select(_handle(cache, dev), _at(pooled), _at(q), _at(k_chunk), B, H, D, n_q, n_kc, _int(block_tokens),
+                                  _int(n_select), _int(keep), _at(blocks), *_scratch(workspace, dev), on)
     _check(st, "astro_block_select")
     return blocks
 
 
 def astro_sparse_attn_fwd_workspace_bytes(batch, heads, head_dim, n_q, n_select, block_tokens) -> int:
-    return int(lib().astro_sparse_attn_fwd_workspace_bytes(int(batch), int(heads), int(head_dim), int(n_q), int(n_select),
-                                                           int(block_tokens)))
+    return int(lib().astro_sparse_attn_fwd_workspace_bytes(_int(batch), _int(heads), _int(head_dim), _int(n_q), _int(n_select),
+                                                           _int(block_tokens)))
 
 
 def astro_sparse_attn_fwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int, scale: float, o=None, lse=None, workspace=None,
@@ -712,15 +723,15 @@ def astro_sparse_attn_fwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
                 workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
     _used_here(stream, *fresh)
     st = lib().astro_sparse_attn_fwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), _at(blocks), n_select,
-                                     int(block_tokens), B, H, D, n_q, n_kc, float(scale), _at(o), _at(lse),
+                                     _int(block_tokens), B, H, D, n_q, n_kc, float(scale), _at(o), _at(lse),
                                      *_scratch(workspace, dev), on)
     _check(st, "astro_sparse_attn_fwd")
     return o, lse
 
 
 def astro_sparse_attn_bwd_workspace_bytes(batch, heads, head_dim, n_q, n_kc, n_select, block_tokens) -> int:
-    return int(lib().astro_sparse_attn_bwd_workspace_bytes(int(batch), int(heads), int(head_dim), int(n_q), int(n_kc),
-                                                           int(n_select), int(block_tokens)))
+    return int(lib().astro_sparse_attn_bwd_workspace_bytes(_int(batch), _int(heads), _int(head_dim), _int(n_q), _int(n_kc),
+                                                           _int(n_select), _int(block_tokens)))
 
 
 def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int, o, lse, d_o, scale: float, dq=None, dk_chunk=None,
@@ -747,7 +758,7 @@ def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
     _used_here(stream, *fresh)
     st = lib().astro_sparse_attn_bwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), _at(blocks), n_select,
-                                     int(block_tokens), _at(o), _at(lse), _at(d_o), B, H, D, n_q, n_kc, float(scale), _at(dq),
+                                     _int(block_tokens), _at(o), _at(lse), _at(d_o), B, H, D, n_q, n_kc, float(scale), _at(dq),
                                      _at(dk_chunk), _at(dv_chunk), *_scratch(workspace, dev), on)
     _check(st, "astro_sparse_attn_bwd")
     return dq, dk_chunk, dv_chunk
@@ -802,7 +813,7 @@ FWD_MODE_NORMAL, FWD_MODE_SAFE_ONLY, FWD_MODE_PAIR = 0, 1, 2
 def astro_debug_forward_mode(mode: int) -> None:
     """Diagnostic switch: 0 normal operation, 1 every later forward runs its safe pass only, 2 head_dim 128
     forwards run the CTA-pair kernel."""
-    _check(lib().astro_debug_forward_mode(int(mode)), "astro_debug_forward_mode")
+    _check(lib().astro_debug_forward_mode(_int(mode)), "astro_debug_forward_mode")
 
 
 def astro_debug_pair_flag() -> int:

@@ -27,3 +27,26 @@ def test_a_destroyed_cache_is_not_an_empty_context():
         with pytest.raises(ValueError):
             call()
     A.astro_kvcache_destroy(cache)                         # again: nothing left to do
+
+
+def test_whole_numbers_beyond_the_c_types_are_refused_not_cut():
+    far = 2 ** 32
+    for n_kc, block in ((100, far + 64), (far + 100, 64), (100, -far + 64)):
+        with pytest.raises(A.AstroError) as e:
+            A.astro_block_count(None, n_kc, block)
+        assert e.value.status == SHAPE
+    for f in ([0, far], [far + 1], [-far]):
+        assert min(A._frame_list(f)[0]) < 0                # no frame, which the call refuses
+    arr, n = A._frame_list([3, 0, 2 ** 31 - 1])
+    assert n == 3 and list(arr)[:3] == [3, 0, 2 ** 31 - 1]
+    assert A._frame_list(None) == (None, -1) and A._frame_list([])[1] == 0
+    for size in (A.astro_block_select_workspace_bytes(1, 2, 64, 300, 40, far + 16), A.astro_sparse_attn_fwd_workspace_bytes(1, 2, 64, 5, far + 64, 128),
+                 A.astro_sparse_attn_bwd_workspace_bytes(1, 2, 64, 300, 40, 4, far + 16)):
+        assert size == 0                                   # as for every size that the calls refuse
+
+
+def test_rotary_descriptions_beyond_the_c_types():
+    for bad in (dict(head_dim=2 ** 32 + 64), dict(rot_dim=2 ** 32 + 64), dict(axis_pairs=(2 ** 32 + 32,))):
+        with pytest.raises(A.AstroError) as e:
+            A.astro_rope_create(**{**dict(head_dim=64, rot_dim=64, layout="halves", axis_pairs=(32,), scaling="linear", factor=2.0), **bad})
+        assert e.value.status == SHAPE
