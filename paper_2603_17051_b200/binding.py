@@ -525,9 +525,11 @@ def astro_rope_create(head_dim, rot_dim, layout, axis_pairs, base=10000.0, scali
     (None = all); magnitude 0 = the scaling's own."""
     if len(axis_pairs) > 4:
         raise AstroError(2, "astro_rope_create")
-    axes = range(len(axis_pairs)) if scaled_axes is None else scaled_axes
+    axes = range(len(axis_pairs)) if scaled_axes is None else [int(a) for a in scaled_axes]
+    if any(not 0 <= a < len(axis_pairs) for a in axes):
+        raise AstroError(2, "astro_rope_create")
     d = RopeDesc(_int(head_dim), _int(rot_dim), ROPE_LAYOUTS[layout], len(axis_pairs), (C.c_int * 4)(*[_int(p) for p in axis_pairs]),
-                 float(base), ROPE_SCALINGS[scaling], sum(1 << int(a) for a in axes), float(factor), float(original_length),
+                 float(base), ROPE_SCALINGS[scaling], sum({1 << a for a in axes}), float(factor), float(original_length),
                  float(ramp_low), float(ramp_high), float(magnitude))
     out = C.c_void_p()
     _check(lib().astro_rope_create(C.byref(d), C.byref(out)), "astro_rope_create")

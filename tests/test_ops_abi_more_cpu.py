@@ -1,11 +1,9 @@
 """Refusals that need no device: handles that are gone, whole numbers beyond the C types, strides beyond any memory, frequencies
 that are no numbers."""
-import ctypes as C
-
 import pytest
 
 from paper_2603_17051_b200 import binding as A
-from test_ops_abi_cpu import SHAPE, desc
+from test_ops_abi_cpu import SHAPE
 
 
 def host_cache(**kw):
@@ -50,3 +48,16 @@ def test_rotary_descriptions_beyond_the_c_types():
         with pytest.raises(A.AstroError) as e:
             A.astro_rope_create(**{**dict(head_dim=64, rot_dim=64, layout="halves", axis_pairs=(32,), scaling="linear", factor=2.0), **bad})
         assert e.value.status == SHAPE
+
+
+@pytest.mark.parametrize("axes", [(1,), (0, 40), (-1,), [2 ** 32]])
+def test_scaled_axes_that_are_not_there(axes):
+    with pytest.raises(A.AstroError) as e:
+        A.astro_rope_create(64, 64, "halves", (32,), scaling="linear", factor=2.0, scaled_axes=axes)
+    assert e.value.status == SHAPE
+
+
+def test_scaled_axes_may_come_from_an_iterator_and_name_any_axis():
+    rope = A.astro_rope_create(64, 64, "halves", (16, 16), scaling="linear", factor=2.0, scaled_axes=iter((1,)))
+    f = A.astro_rope_frequencies(rope)[0]
+    assert f[0] == 1.0 and f[16] == 0.5
