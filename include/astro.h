@@ -199,7 +199,8 @@ astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* s
  *   BASE    base replaced by base * factor^(n/(n-1)): the fastest pair is left alone, the slowest divided by factor
  *   RAMP    with r = original_length f_i / 2 pi turns over the trained length and g = (r - ramp_low) /
  *           (ramp_high - ramp_low) clamped to [0, 1]:  f_i (g + (1 - g) / factor)
- * magnitude multiplies cosines and sines; 0 means 1, or 0.1 ln(factor) + 1 for RAMP. */
+ * magnitude multiplies cosines and sines; 0 means 1, or 0.1 ln(factor) + 1 for RAMP.  ASTRO_ERR_SHAPE for a table whose
+ * frequencies are not all positive finite doubles or whose magnitude is no positive finite float. */
 typedef struct astro_rope astro_rope_t; /* opaque, host side, owns no device memory */
 enum { ASTRO_ROPE_INTERLEAVED = 0, ASTRO_ROPE_HALVES = 1 };       /* pairs (2p, 2p+1) or (p, p + rot_dim/2) */
 enum { ASTRO_ROPE_SCALE_NONE = 0, ASTRO_ROPE_SCALE_LINEAR = 1, ASTRO_ROPE_SCALE_BASE = 2, ASTRO_ROPE_SCALE_RAMP = 3 };

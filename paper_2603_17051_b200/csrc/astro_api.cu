@@ -1143,6 +1143,7 @@ astro_status_t astro_rope_create(const astro_rope_desc_t* d, astro_rope_t** out)
   r->d = *d;
   const double two_pi = 6.283185307179586476925286766559;
   int p = 0;
+  bool numbers = true;   // an infinite or vanished frequency turns positions, 0 among them, into NaN or into none
   for (int a = 0; a < d->axes; ++a) {
     const int n = d->axis_pairs[a];
     const bool scaled = d->scaling != ASTRO_ROPE_SCALE_NONE && ((d->scaled_axes >> a) & 1);
@@ -1156,6 +1157,7 @@ astro_status_t astro_rope_create(const astro_rope_desc_t* d, astro_rope_t** out)
         g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
         f *= g + (1.0 - g) / d->factor;
       }
+      numbers = numbers && f > 0.0 && std::isfinite(f) && std::isfinite(base);
       r->frequency[p] = f;
       r->table.turns[p] = f / two_pi;
       r->table.axis[p] = static_cast<uint8_t>(a);
@@ -1164,6 +1166,10 @@ astro_status_t astro_rope_create(const astro_rope_desc_t* d, astro_rope_t** out)
   r->magnitude = d->magnitude > 0.0 ? d->magnitude
                                     : d->scaling == ASTRO_ROPE_SCALE_RAMP ? 0.1 * std::log(d->factor) + 1.0 : 1.0;
   r->table.size = static_cast<float>(r->magnitude);
+  if (!numbers || !(r->table.size > 0.f) || !std::isfinite(r->table.size)) {
+    delete r;
+    return ASTRO_ERR_SHAPE;
+  }
   r->table.pairs = p;
   r->table.axes = d->axes;
   *out = r;

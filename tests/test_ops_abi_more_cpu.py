@@ -1,9 +1,11 @@
 """Refusals that need no device: handles that are gone, whole numbers beyond the C types, strides beyond any memory, frequencies
 that are no numbers."""
+import ctypes as C
+
 import pytest
 
 from paper_2603_17051_b200 import binding as A
-from test_ops_abi_cpu import SHAPE
+from test_ops_abi_cpu import SHAPE, desc
 
 
 def host_cache(**kw):
@@ -61,3 +63,19 @@ def test_scaled_axes_may_come_from_an_iterator_and_name_any_axis():
     rope = A.astro_rope_create(64, 64, "halves", (16, 16), scaling="linear", factor=2.0, scaled_axes=iter((1,)))
     f = A.astro_rope_frequencies(rope)[0]
     assert f[0] == 1.0 and f[16] == 0.5
+
+
+@pytest.mark.parametrize("bad", [dict(base=5e-324), dict(base=1e-300, scaling=2, factor=1e300), dict(magnitude=1e39), dict(magnitude=1e-46),
+                                 dict(scaling=2, base=1e200, factor=1e200)])
+def test_tables_that_are_no_numbers_are_refused(bad):
+    """Frequencies or a magnitude that overflow would turn every position, 0 included, into NaN."""
+    import math
+    out = C.c_void_p()
+    status = A.lib().astro_rope_create(C.byref(desc(**{**dict(scaled_axes=1), **bad})), C.byref(out))
+    if status == 0:                                        # what is accepted is a table of numbers
+        f, m = (C.c_double * 32)(), C.c_double()
+        assert A.lib().astro_rope_frequencies(out, f, C.byref(m)) == 0
+        assert all(0.0 < x < math.inf for x in f) and 0 < C.c_float(m.value).value < math.inf
+        A.lib().astro_rope_destroy(out)
+    else:
+        assert status == SHAPE and not out.value
