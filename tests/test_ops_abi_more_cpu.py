@@ -79,3 +79,17 @@ def test_tables_that_are_no_numbers_are_refused(bad):
         A.lib().astro_rope_destroy(out)
     else:
         assert status == SHAPE and not out.value
+
+
+def test_strides_whose_products_pass_64_bits():
+    """Output rows 2^40 elements apart, 2^29 of them: the second sample starts inside the first whatever 64-bit products say."""
+    keep = A.astro_rope_create(64, 64, "halves", (32,))
+    p = C.c_void_p
+    strides = lambda *x: C.byref(A.Strides(*x))  # noqa: E731
+    run = lambda si, so: A.lib().astro_rope_apply(keep.handle, 0, p(0x10000), None, p(0x30000), 1, 2, 1 << 29, 4, 0, 0, strides(*si),  # noqa: E731
+                                                  p(0x40000), None, strides(*so), None)
+    dense = ((1 << 29) * 256, 256, 64)
+    assert run(dense, (1 << 40, 1 << 40, 64)) == SHAPE
+    assert run(dense, (1 << 40, 1 << 39, 64)) == SHAPE
+    assert run((1 << 40, 1 << 40, 64), dense) == SHAPE     # no memory holds such an input either
+    assert run((dense[0], dense[1], (1 << 40) + 8), dense) == SHAPE
