@@ -1216,7 +1216,7 @@ astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const voi
   const astro_strides_t dense = {static_cast<int64_t>(n_tokens) * heads_q * D, static_cast<int64_t>(heads_q) * D, D};
   const astro_strides_t in = in_strides ? *in_strides : dense, to = out_strides ? *out_strides : dense;
   const long long sizes[3] = {batch, n_tokens, heads}, is[3] = {in.batch, in.token, in.head}, os[3] = {to.batch, to.token, to.head};
-  const long long limit = 1ll << 44;   // elements from the first row to the last along an axis: beyond any memory, sums of three inside 64 bits
+  const long long limit = 1ll << 40;   // elements from the first row to the last along an axis: beyond any memory, sums inside 64 bits
   for (int i = 0; i < 3; ++i) {
     if (sizes[i] <= 1) continue;
     const long long most = limit / (sizes[i] - 1);
