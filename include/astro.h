@@ -240,6 +240,13 @@ astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const voi
                                 int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
                                 const astro_strides_t* out_strides, void* stream);
 
+/* Host only: what astro_rope_apply would answer to these arguments before it launches anything.  For callers that rotate q and
+ * k in two calls (different strides) and want neither if one of them is refused. */
+astro_status_t astro_rope_apply_check(const astro_rope_t* rope, int inverse, const void* q, const void* k,
+                                      const int32_t* positions, int positions_batch, int batch, int n_tokens, int heads_q,
+                                      int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
+                                      const astro_strides_t* out_strides);
+
 /* ---- attention over chosen key blocks ---------------------------------------------------------------------------
  * The keys of a call are cut into blocks of block_tokens tokens (a multiple of 8, 8..128): every held cache frame, in
  * logical order, into ceil(T / block_tokens) blocks, then the chunk's n_kc tokens into ceil(n_kc / block_tokens).

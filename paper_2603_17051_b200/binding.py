@@ -23,7 +23,7 @@ EXPORTED = ("astro_kvcache_key_segments", "astro_selftest_wait_timeout", "astro_
             "astro_chunk_attn_bwd_delta", "astro_chunk_attn_bwd_dq", "astro_chunk_attn_bwd_dkv",
             "astro_chunk_attn_bwd_static", "astro_debug_forward_mode", "astro_debug_pair_flag",
             "astro_last_device_status", "astro_status_string", "astro_kvcache_fork", "astro_rope_create",
-            "astro_rope_destroy", "astro_rope_frequencies", "astro_rope_apply", "astro_block_count", "astro_block_pool",
+            "astro_rope_destroy", "astro_rope_frequencies", "astro_rope_apply", "astro_rope_apply_check", "astro_block_count", "astro_block_pool",
             "astro_block_select_workspace_bytes", "astro_block_select", "astro_sparse_attn_fwd_workspace_bytes",
             "astro_sparse_attn_fwd", "astro_sparse_attn_bwd_workspace_bytes", "astro_sparse_attn_bwd")
 
@@ -116,6 +116,8 @@ def lib():
     L.astro_rope_apply.restype = ci
     L.astro_rope_apply.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, ci, ci, ci, C.POINTER(Strides), vp, vp,
                                    C.POINTER(Strides), vp]
+    L.astro_rope_apply_check.restype = ci
+    L.astro_rope_apply_check.argtypes = L.astro_rope_apply.argtypes[:-1]
     L.astro_block_count.restype = ci
     L.astro_block_count.argtypes = [vp, ci, ci, C.POINTER(ci), C.POINTER(ci)]
     L.astro_block_pool.restype = ci
@@ -602,11 +604,13 @@ def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=N
     _like((pb, n, rope.desc.axes), torch.int32, dev, positions)
     _used_here(stream, *fresh)
 
-    def call(x, x2, y, y2, strides):
-        _check(lib().astro_rope_apply(rope.handle, 1 if inverse else 0, _at(x), _at(x2), _at(positions), pb, B, _int(n), x.shape[2],
-                                      0 if x2 is None else x2.shape[2], kind, None if strides is None else C.byref(Strides(*strides[0])),
-                                      _at(y), _at(y2), None if strides is None else C.byref(Strides(*strides[1])), on),
-               "astro_rope_apply")
+    def arguments(x, x2, y, y2, strides):
+        return (rope.handle, 1 if inverse else 0, _at(x), _at(x2), _at(positions), pb, B, _int(n), x.shape[2],
+                0 if x2 is None else x2.shape[2], kind, None if strides is None else C.byref(Strides(*strides[0])), _at(y), _at(y2),
+                None if strides is None else C.byref(Strides(*strides[1])))
+
+    def call(*of):
+        _check(lib().astro_rope_apply(*arguments(*of), on), "astro_rope_apply")
 
     dense = q.is_contiguous() and q_out.is_contiguous()
     if dense and (k is None or (k.shape == shape and k.is_contiguous() and k_out.is_contiguous())):
@@ -619,6 +623,12 @@ def astro_rope_apply(rope: Rope, q, k, positions, inverse: bool = False, q_out=N
     if len(pairs) == 2 and layouts[0] == layouts[1]:   # one launch for q and k; two where their strides differ
         call(q, k, q_out, k_out, layouts[0])
     else:
+        if len(pairs) == 2:                            # neither if one is refused, and none reads what the other has written
+            if q_out.data_ptr() in (k.data_ptr(), k_out.data_ptr()) or k_out.data_ptr() == q.data_ptr():
+                if n:
+                    raise AstroError(2, "astro_rope_apply")
+            for (x, y), layout in zip(pairs, layouts):
+                _check(lib().astro_rope_apply_check(*arguments(x, None, y, None, layout)), "astro_rope_apply")
         for (x, y), layout in zip(pairs, layouts):
             call(x, None, y, None, layout)
     return q_out, k_out

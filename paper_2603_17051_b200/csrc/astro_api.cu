@@ -1189,10 +1189,10 @@ astro_status_t astro_rope_frequencies(const astro_rope_t* rope, double* frequenc
   return ASTRO_OK;
 }
 
-astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const void* q, const void* k,
-                                const int32_t* positions, int positions_batch, int batch, int n_tokens, int heads_q,
-                                int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
-                                const astro_strides_t* out_strides, void* stream) {
+static astro_status_t check_rope(const astro_rope_t* rope, int inverse, const void* q, const void* k, const int32_t* positions,
+                                 int positions_batch, int batch, int n_tokens, int heads_q, int heads_k, int dtype,
+                                 const astro_strides_t* in_strides, void* q_out, void* k_out, const astro_strides_t* out_strides,
+                                 RopeTensors* x) {
   if (!rope || (k != nullptr) != (k_out != nullptr)) return ASTRO_ERR_NULL;
   if (batch < 1 || n_tokens < 0 || heads_q < 1 || (k && heads_k < 1) || (positions_batch != 1 && positions_batch != batch))
     return ASTRO_ERR_SHAPE;
@@ -1207,10 +1207,6 @@ astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const voi
       (reinterpret_cast<uintptr_t>(positions) & 3u))
     return ASTRO_ERR_ALIGN;
   const int heads = k && heads_k > heads_q ? heads_k : heads_q;
-  RopeTensors x;
-  x.q = q; x.k = k; x.q_out = q_out; x.k_out = k_out;
-  x.heads_q = heads_q;
-  x.heads_k = k ? heads_k : 0;
   // contiguous tensors of different head counts have different strides: those need two calls
   if (k && heads_k != heads_q && (!in_strides || !out_strides)) return ASTRO_ERR_SHAPE;
   const astro_strides_t dense = {static_cast<int64_t>(n_tokens) * heads_q * D, static_cast<int64_t>(heads_q) * D, D};
@@ -1228,10 +1224,32 @@ astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const voi
   if (q_out == q || (k && k_out == k))
     for (int i = 0; i < 3; ++i)
       if (sizes[i] > 1 && is[i] != os[i]) return ASTRO_ERR_SHAPE;
-  x.in_b = in.batch; x.in_t = in.token; x.in_h = in.head;
-  x.out_b = to.batch; x.out_t = to.token; x.out_h = to.head;
-  astro_status_t s = check_arch();
-  if (s != ASTRO_OK) return s;
+  x->q = q; x->k = k; x->q_out = q_out; x->k_out = k_out;
+  x->heads_q = heads_q;
+  x->heads_k = k ? heads_k : 0;
+  x->in_b = in.batch; x->in_t = in.token; x->in_h = in.head;
+  x->out_b = to.batch; x->out_t = to.token; x->out_h = to.head;
+  return ASTRO_OK;
+}
+
+astro_status_t astro_rope_apply_check(const astro_rope_t* rope, int inverse, const void* q, const void* k,
+                                      const int32_t* positions, int positions_batch, int batch, int n_tokens, int heads_q,
+                                      int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
+                                      const astro_strides_t* out_strides) {
+  RopeTensors x;
+  return check_rope(rope, inverse, q, k, positions, positions_batch, batch, n_tokens, heads_q, heads_k, dtype, in_strides, q_out,
+                    k_out, out_strides, &x);
+}
+
+astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const void* q, const void* k,
+                                const int32_t* positions, int positions_batch, int batch, int n_tokens, int heads_q,
+                                int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
+                                const astro_strides_t* out_strides, void* stream) {
+  RopeTensors x;
+  astro_status_t s = check_rope(rope, inverse, q, k, positions, positions_batch, batch, n_tokens, heads_q, heads_k, dtype,
+                                in_strides, q_out, k_out, out_strides, &x);
+  if (s != ASTRO_OK || n_tokens == 0) return s;
+  if ((s = check_arch()) != ASTRO_OK) return s;
   const int total = batch * n_tokens, per_sample = positions_batch > 1 || batch == 1 ? 1 : 0;
   const float sign = inverse ? -1.f : 1.f;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

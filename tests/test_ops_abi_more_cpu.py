@@ -93,3 +93,16 @@ def test_strides_whose_products_pass_64_bits():
     assert run(dense, (1 << 40, 1 << 39, 64)) == SHAPE
     assert run((1 << 40, 1 << 40, 64), dense) == SHAPE     # no memory holds such an input either
     assert run((dense[0], dense[1], (1 << 40) + 8), dense) == SHAPE
+
+
+def test_the_check_of_a_rotary_call_answers_as_the_call_does():
+    keep = A.astro_rope_create(64, 64, "halves", (32,))
+    p = lambda x: C.c_void_p(x) if x else None  # noqa: E731
+
+    def check(q=0x10000, qo=0x40000, pos=0x30000, B=2, n=8, dtype=0, so=None):
+        return A.lib().astro_rope_apply_check(keep.handle, 0, p(q), None, p(pos), 1, B, n, 4, 0, dtype, None, p(qo), None,
+                                              None if so is None else C.byref(A.Strides(*so)))
+
+    assert check() == 0 and check(n=0, q=0, qo=0, pos=0) == 0
+    assert check(q=0) == 1 and check(B=0) == SHAPE and check(dtype=3) == SHAPE and check(q=0x10002) == 3 and check(so=(0, 256, 64)) == SHAPE
+    assert A.lib().astro_rope_apply_check(None, 0, p(1 << 16), None, p(1 << 17), 1, 1, 1, 1, 0, 0, None, p(1 << 18), None, None) == 1
