@@ -181,7 +181,8 @@ astro_status_t astro_chunk_attn_bwd_dkv(const void* q, const void* k_chunk, cons
  * candidate), reorders and compacts.
  * parents: device int32 [dst cache_batch], the sample of src that each sample of dst continues; null: sample b
  * continues sample b, or sample 0 of a one-sample src.  A parent outside src leaves zeros in the copied frames.
- * dst's frames_seen becomes src's.  ASTRO_ERR_SHAPE: other heads, head_dim or tokens_per_frame; parents null and
+ * dst's frames_seen becomes src's, or the number of copied frames where repeats make that larger (a cache has seen at least
+ * the frames it holds).  ASTRO_ERR_SHAPE: other heads, head_dim or tokens_per_frame; parents null and
  * cache batches that are neither equal nor 1; a frame index that src does not hold; storage of dst that overlaps src's.
  * ASTRO_ERR_CAPACITY: more frames than dst holds.  Calls on dst and src obey the rules of calls that change a cache
  * (dst) and of calls that take it as const (src). */
