@@ -2,9 +2,11 @@
 //   mean_j  = (sum over the tokens t of block j of k_t) / (tokens of block j), summed in fp64, kept in fp32
 //   score_ij = mean of query block i . mean_j, in fp64
 // and per query block the n_select largest scores.  A choice is a comparison: two scores that are equal or nearly so
-// must come out in the same order whatever the order of the sums, so sums and products are fp64 (the sum of a block
-// of bf16 values is exact there) and only the means are rounded, once, to fp32.  Equal scores go to the lower block,
-// NaN ranks below everything.
+// should come out in the same order whatever the order of the sums, so sums and products are fp64 and only the means are rounded,
+// once, to fp32.  The fp64 sum of a block of up to 128 bf16 values is exact while their exponents lie within 38 binades (53 bits,
+// less the 8 of a value and 7 of carries).  Values further apart leave rounding in its last bits, which depends on how many warps
+// share a block, that is on the size of the launch: the fp32 mean can then differ by its last bit between a launch over a few
+// frames and one over all.  Equal scores go to the lower block, NaN ranks below everything.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

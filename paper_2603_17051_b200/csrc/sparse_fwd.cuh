@@ -16,9 +16,12 @@
 //
 // Bound: the tensor pipe and its hand-offs.  A tile takes 1600 to 1670 clocks (the dense kernel's 1630), of which the MMAs are
 // 1024: S -> softmax 1250 -> hand-over 300 -> P V and the next S 1250, two tiles in flight.  Layer shape, 64 of 273 blocks of
-// 120 tokens per query block: 208 us = 1063 TFLOP/s at 1.67 GHz (tensor pipe 58 %, DRAM bytes as few as the inputs and
-// outputs have), 241 us under the power limit; with every query block naming one and the same block 188 us at 1.80 GHz in
-// as many clocks: what random lists cost is power.  Start and end of the kernel take 9 % of its clocks, a unit boundary 2.5 tiles.
+// 120 tokens per query block: 203 to 210 us in short bursts = 1050 to 1090 TFLOP/s (tensor pipe 58 %, DRAM bytes as few as the inputs
+// and outputs have), 242 us in a loop under the power limit (993 W, 1.53 GHz, 370k clocks).  With every query block naming one and the
+// same block 205 us, and 218 us in the loop (992 W, 1.66 GHz, 362k clocks): random lists cost 2 % in clocks and, where power is
+// the limit, 8 % in clock rate.  Start and end of the kernel take 9 % of its clocks, a unit boundary 2.5 tiles.
+// Registers: 72 per thread (27 warps); the softmax loop spills nothing, the other roles' code 212 bytes, 11 local accesses per key tile of
+// 3600 warp instructions.
 //
 // Few units: a unit's list is cut into up to `splits` ranges that run as units of their own and leave O (fp32, normalised)
 // and LSE of their part; sparse_combine_kernel joins them.
