@@ -233,8 +233,8 @@ astro_status_t astro_rope_frequencies(const astro_rope_t* rope, double* frequenc
  * positions: device int32 [positions_batch, n_tokens, axes], positions_batch = batch or 1 (the same for every
  * sample); any int32 value, angles keep their accuracy to the far end of it.
  * in_strides (of q and k alike) and out_strides (of q_out and k_out): null = contiguous.  Pointers and strides must be
- * multiples of 16 bytes (ASTRO_ERR_ALIGN).  An input stride may be 0 (a broadcast input); outputs must not overlap
- * themselves (ASTRO_ERR_SHAPE).  q_out = q (and k_out = k) rotates in place, with equal strides; otherwise outputs
+ * multiples of 16 bytes (ASTRO_ERR_ALIGN).  An input stride may be 0 (a broadcast input, whose gradient is the sum of the
+ * copies' gradients: the caller's to take); outputs must not overlap themselves (ASTRO_ERR_SHAPE).  q_out = q (and k_out = k) rotates in place, with equal strides; otherwise outputs
  * must not overlap inputs.  n_tokens = 0 is an empty call. */
 astro_status_t astro_rope_apply(const astro_rope_t* rope, int inverse, const void* q, const void* k,
                                 const int32_t* positions, int positions_batch, int batch, int n_tokens, int heads_q,
