@@ -95,3 +95,30 @@ def test_what_a_call_returns_stays_whole_while_either_stream_uses_it():
             torch.empty_like(copy).zero_()
     torch.cuda.synchronize()
     assert torch.equal(copy, want)
+
+
+def test_calls_on_a_stream_that_joined_a_capture():
+    """Inside a captured graph, on a stream forked from the capturing one, with results dropped along the way."""
+    import torch
+    from paper_2603_17051_b200 import binding as A
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v, d_o = (torch.randn((1, n, 2, 64), generator=g, device="cuda").bfloat16() for n in (300, 256, 256, 300))
+    blocks = torch.tensor([0, 2, 3], dtype=torch.int32, device="cuda").expand(1, 2, 3, 3).contiguous()
+
+    def whole(stream):
+        o, lse = A.astro_sparse_attn_fwd(None, q, k, v, blocks, 64, 0.125, stream=stream)
+        return (o, lse) + A.astro_sparse_attn_bwd(None, q, k, v, blocks, 64, o, lse, d_o, 0.125, stream=stream)
+
+    want = [x.clone() for x in whole(None)]
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        for _ in range(3):
+            out = whole(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    A.astro_last_device_status()
+    assert all(torch.equal(x, y) for x, y in zip(want, out))
