@@ -248,6 +248,47 @@ astro_status_t astro_rope_apply_check(const astro_rope_t* rope, int inverse, con
                                       int heads_k, int dtype, const astro_strides_t* in_strides, void* q_out, void* k_out,
                                       const astro_strides_t* out_strides);
 
+/* ---- the cache in 8 bits ------------------------------------------------------------------------------------------
+ * A rolling cache that takes 8 bits per element and 8 per row (the head_dim elements of one head and token): half the memory
+ * of astro_kvcache_create's, so twice the frames or samples.  A row x is held as
+ *   e = the smallest whole number with max |x_d| <= 448 * 2^e over the row's finite elements, -124 at least, and
+ *   e4m3(x_d * 2^-e) for every element, rounded to nearest even; an infinity or NaN becomes NaN, the others are not touched by it.
+ * (Elements of 248 * 2^120 and more, which would round beyond the largest float, are held as 240 * 2^120.)
+ * What it stands for, e4m3 value times 2^e, is a bf16 number exactly: reading it back in bf16 or fp32 rounds nothing.
+ * The handle is an astro_kvcache_t: destroy, reset, evict, query, get_state, set_state, key_segments, export and append (which takes
+ * bf16) do for it what they do for the other kind.  The calls that read a 16-bit cache's rows (astro_chunk_attn_fwd and _bwd,
+ * astro_block_pool, astro_block_select, astro_sparse_attn_*, astro_kvcache_fork) answer ASTRO_ERR_SHAPE to it, and the calls below
+ * to a 16-bit one. */
+/* Bytes for K (and the same again for V); 0 for an invalid descriptor. */
+size_t astro_kvcache8_storage_bytes(const astro_kvcache_desc_t* desc);
+/* As astro_kvcache_create; the layout inside the storage is private. */
+astro_status_t astro_kvcache8_create(const astro_kvcache_desc_t* desc, void* k_storage, void* v_storage, size_t bytes_each,
+                                     astro_kvcache_t** out);
+/* As astro_kvcache_append, the rows being quantised on the way.  k, v: device [B_c, n_frames * T, H, D] of type dtype, strides
+ * (of both, null = contiguous) and pointers multiples of 16 bytes. */
+astro_status_t astro_kvcache8_append(astro_kvcache_t* cache, const void* k, const void* v, int n_frames, int dtype,
+                                     const astro_strides_t* strides, void* stream);
+/* What the n_frames held frames from logical frame first_frame on stand for, in logical order: k_out, v_out device
+ * [B_c, n_frames * T, H, D], contiguous, of type dtype (in fp16 values are rounded, and infinite beyond its range).
+ * n_frames = 0 is an empty call. */
+astro_status_t astro_kvcache8_read(const astro_kvcache_t* cache, int first_frame, int n_frames, int dtype, void* k_out, void* v_out,
+                                   void* stream);
+
+/* astro_chunk_attn_fwd over a cache in 8 bits: the keys and values of the cached tokens are what their rows stand for, the
+ * chunk's are bf16.  Same layouts, results and errors; cache may be null.  workspace: device scratch, 16-byte aligned, at least
+ * astro_chunk_attn8_fwd_workspace_bytes() for the frames that the cache holds at the time of the call (it may be null where that is 0).  Many
+ * queries: the held rows in bf16; few: the parts of lists that several CTAs share. */
+size_t astro_chunk_attn8_fwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc);
+astro_status_t astro_chunk_attn8_fwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk, int batch,
+                                     int heads, int head_dim, int n_q, int n_kc, float scale, void* o, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+/* astro_chunk_attn_bwd over a cache in 8 bits, the cached context detached: dQ over all keys, dK and dV of the chunk's own. */
+size_t astro_chunk_attn8_bwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc);
+astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
+                                     const void* o, const float* lse, const void* d_o, int batch, int heads, int head_dim, int n_q,
+                                     int n_kc, float scale, void* dq, void* dk_chunk, void* dv_chunk, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
 /* ---- attention over chosen key blocks ---------------------------------------------------------------------------
  * The keys of a call are cut into blocks of block_tokens tokens (a multiple of 8, 8..128): every held cache frame, in
  * logical order, into ceil(T / block_tokens) blocks, then the chunk's n_kc tokens into ceil(n_kc / block_tokens).

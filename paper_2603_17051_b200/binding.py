@@ -25,7 +25,10 @@ EXPORTED = ("astro_kvcache_key_segments", "astro_selftest_wait_timeout", "astro_
             "astro_last_device_status", "astro_status_string", "astro_kvcache_fork", "astro_rope_create",
             "astro_rope_destroy", "astro_rope_frequencies", "astro_rope_apply", "astro_rope_apply_check", "astro_block_count", "astro_block_pool",
             "astro_block_select_workspace_bytes", "astro_block_select", "astro_sparse_attn_fwd_workspace_bytes",
-            "astro_sparse_attn_fwd", "astro_sparse_attn_bwd_workspace_bytes", "astro_sparse_attn_bwd")
+            "astro_sparse_attn_fwd", "astro_sparse_attn_bwd_workspace_bytes", "astro_sparse_attn_bwd",
+            "astro_kvcache8_storage_bytes", "astro_kvcache8_create", "astro_kvcache8_append", "astro_kvcache8_read",
+            "astro_chunk_attn8_fwd_workspace_bytes", "astro_chunk_attn8_fwd", "astro_chunk_attn8_bwd_workspace_bytes",
+            "astro_chunk_attn8_bwd")
 
 
 class AstroError(RuntimeError):
@@ -134,6 +137,22 @@ def lib():
     L.astro_sparse_attn_bwd_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci, ci]
     L.astro_sparse_attn_bwd.restype = ci
     L.astro_sparse_attn_bwd.argtypes = [vp, vp, vp, vp, vp, ci, ci, vp, vp, vp, ci, ci, ci, ci, ci, cf, vp, vp, vp, vp, sz, vp]
+    L.astro_kvcache8_storage_bytes.restype = sz
+    L.astro_kvcache8_storage_bytes.argtypes = [C.POINTER(KVCacheDesc)]
+    L.astro_kvcache8_create.restype = ci
+    L.astro_kvcache8_create.argtypes = [C.POINTER(KVCacheDesc), vp, vp, sz, C.POINTER(vp)]
+    L.astro_kvcache8_append.restype = ci
+    L.astro_kvcache8_append.argtypes = [vp, vp, vp, ci, ci, C.POINTER(Strides), vp]
+    L.astro_kvcache8_read.restype = ci
+    L.astro_kvcache8_read.argtypes = [vp, ci, ci, ci, vp, vp, vp]
+    L.astro_chunk_attn8_fwd_workspace_bytes.restype = sz
+    L.astro_chunk_attn8_fwd_workspace_bytes.argtypes = [vp, ci, ci, ci, ci, ci]
+    L.astro_chunk_attn8_fwd.restype = ci
+    L.astro_chunk_attn8_fwd.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, cf, vp, vp, vp, sz, vp]
+    L.astro_chunk_attn8_bwd_workspace_bytes.restype = sz
+    L.astro_chunk_attn8_bwd_workspace_bytes.argtypes = [vp, ci, ci, ci, ci, ci]
+    L.astro_chunk_attn8_bwd.restype = ci
+    L.astro_chunk_attn8_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, cf, vp, vp, vp, vp, sz, vp]
     L.astro_debug_forward_mode.restype = ci
     L.astro_debug_forward_mode.argtypes = [ci]
     L.astro_debug_pair_flag.restype = ci
@@ -289,9 +308,10 @@ def astro_kvcache_storage_bytes(cache_batch, heads, head_dim, tokens_per_frame, 
 
 
 class KVCache:
-    """Handle of one layer's rolling cache plus the torch tensors that back its storage."""
+    """Handle of one layer's rolling cache plus the torch tensors that back its storage; bits: 16, or 8 (astro_kvcache8_create)."""
 
-    def __init__(self, handle, desc, k_storage, v_storage):
+    def __init__(self, handle, desc, k_storage, v_storage, bits=16):
+        self.bits = bits
         self.handle = handle
         self.desc = desc
         self.k_storage = k_storage
@@ -307,21 +327,25 @@ class KVCache:
 def astro_kvcache_create(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames,
                          k_storage=None, v_storage=None, device="cuda") -> KVCache:
     """Bind storage (torch uint8/bf16 tensors; allocated here with torch when not given) to a new cache."""
-    import torch
     d = _desc(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames)
-    nbytes = int(lib().astro_kvcache_storage_bytes(C.byref(d)))
+    return _create(16, "astro_kvcache", d, k_storage, v_storage, device)
+
+
+def _create(bits, family, d, k_storage, v_storage, device):
+    import torch
+    nbytes = int(getattr(lib(), family + "_storage_bytes")(C.byref(d)))
     if nbytes == 0:
-        raise AstroError(2, "astro_kvcache_storage_bytes")
+        raise AstroError(2, family + "_storage_bytes")
     if k_storage is None:
         k_storage = torch.empty(nbytes, dtype=torch.uint8, device=device)
     if v_storage is None:
         v_storage = torch.empty(nbytes, dtype=torch.uint8, device=device)
     out = C.c_void_p()
-    st = lib().astro_kvcache_create(C.byref(d), _ptr(k_storage), _ptr(v_storage),
-                                    min(k_storage.numel() * k_storage.element_size(),
-                                        v_storage.numel() * v_storage.element_size()), C.byref(out))
-    _check(st, "astro_kvcache_create")
-    return KVCache(out, d, k_storage, v_storage)
+    st = getattr(lib(), family + "_create")(C.byref(d), _ptr(k_storage), _ptr(v_storage),
+                                            min(k_storage.numel() * k_storage.element_size(),
+                                                v_storage.numel() * v_storage.element_size()), C.byref(out))
+    _check(st, family + "_create")
+    return KVCache(out, d, k_storage, v_storage, bits)
 
 
 def astro_kvcache_destroy(cache: KVCache) -> None:
@@ -773,6 +797,143 @@ def astro_sparse_attn_bwd(cache, q, k_chunk, v_chunk, blocks, block_tokens: int,
                                      _int(block_tokens), _at(o), _at(lse), _at(d_o), B, H, D, n_q, n_kc, float(scale), _at(dq),
                                      _at(dk_chunk), _at(dv_chunk), *_scratch(workspace, dev), on)
     _check(st, "astro_sparse_attn_bwd")
+    return dq, dk_chunk, dv_chunk
+
+
+def astro_kvcache8_storage_bytes(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames) -> int:
+    d = _desc(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames)
+    return int(lib().astro_kvcache8_storage_bytes(C.byref(d)))
+
+
+def astro_kvcache8_create(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames, k_storage=None, v_storage=None,
+                          device="cuda") -> KVCache:
+    """A rolling cache that holds its rows in 8 bits (see include/astro.h); storage as for astro_kvcache_create."""
+    d = _desc(cache_batch, heads, head_dim, tokens_per_frame, sink_frames, window_frames)
+    return _create(8, "astro_kvcache8", d, k_storage, v_storage, device)
+
+
+def _kind(dtype):
+    """ASTRO_BF16, ASTRO_F16 or ASTRO_F32."""
+    import torch
+    if not _ROPE_TYPES:
+        _ROPE_TYPES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+    kind = _ROPE_TYPES.get(dtype)
+    if kind is None:
+        raise ValueError("the type must be bf16, fp16 or fp32")
+    return kind
+
+
+def astro_kvcache8_append(cache: KVCache, k, v, n_frames: int, stream=None) -> None:
+    """Quantise and store new frames: k, v [B_c, n_frames*T, H, D] in bf16, fp16 or fp32 on the device; they may be strided alike
+    as long as a head's elements are contiguous."""
+    d = cache.desc
+    shape = (d.cache_batch, _int(n_frames) * d.tokens_per_frame, d.heads, d.head_dim)
+    dev, on = _where(stream, k)
+    kind = _kind(k.dtype)
+    if k.shape != shape or v.shape != shape or v.dtype is not k.dtype or v.get_device() != dev:
+        raise ValueError("k and v must be [B_c, n_frames*T, H, D] of one type, beside each other")
+    strides = None
+    if not (k.is_contiguous() and v.is_contiguous()):
+        strides = _rope_strides(k)
+        if k.stride(3) != 1 or v.stride(3) != 1 or strides != _rope_strides(v):
+            raise ValueError("k and v must have the same strides and contiguous heads")
+    _check(lib().astro_kvcache8_append(_handle(cache, dev), _at(k), _at(v), _int(n_frames), kind,
+                                       None if strides is None else C.byref(Strides(*strides)), on), "astro_kvcache8_append")
+
+
+def astro_kvcache8_read(cache: KVCache, first_frame: int = 0, n_frames=None, dtype=None, k_out=None, v_out=None, stream=None):
+    """What held frames stand for (n_frames None: all from first_frame on), in logical order: two tensors [B_c, n_frames*T, H, D]
+    of type dtype (None: k_out's, or bf16)."""
+    import torch
+    if n_frames is None:
+        sink, win, _ = astro_kvcache_query(cache)
+        n_frames = sink + win - _int(first_frame)
+    if dtype is None:
+        dtype = torch.bfloat16 if k_out is None else k_out.dtype
+    kind = _kind(dtype)
+    dev, on = _where(stream, cache.k_storage)
+    d = cache.desc
+    shape = (d.cache_batch, max(0, _int(n_frames)) * d.tokens_per_frame, d.heads, d.head_dim)
+    _like(shape, dtype, dev, k_out, v_out)
+    fresh = []
+    with _owned_by(stream):
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dtype, device=cache.k_storage.device); fresh.append(k_out)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=dtype, device=cache.k_storage.device); fresh.append(v_out)
+    _used_here(stream, *fresh)
+    _check(lib().astro_kvcache8_read(_handle(cache, dev), _int(first_frame), _int(n_frames), kind, _at(k_out), _at(v_out), on),
+           "astro_kvcache8_read")
+    return k_out, v_out
+
+
+def _workspace8(which, cache, batch, n_q, n_kc, heads, head_dim):
+    d = None if cache is None else cache.desc
+    return int(getattr(lib(), which)(_cache(cache), _int(batch), _int(d.heads if heads is None else heads),
+                                     _int(d.head_dim if head_dim is None else head_dim), _int(n_q), _int(n_kc)))
+
+
+def astro_chunk_attn8_fwd_workspace_bytes(cache, batch, n_q, n_kc, heads=None, head_dim=None) -> int:
+    """For the frames that the cache holds now; heads and head_dim are the cache's unless there is none."""
+    return _workspace8("astro_chunk_attn8_fwd_workspace_bytes", cache, batch, n_q, n_kc, heads, head_dim)
+
+
+def astro_chunk_attn8_fwd(cache, q, k_chunk, v_chunk, scale: float, o=None, lse=None, workspace=None, stream=None):
+    """astro_chunk_attn_fwd over a cache in 8 bits; returns (O bf16, LSE fp32 [B, H, n_q])."""
+    import torch
+    dev, on = _where(stream, q)
+    shape = q.shape
+    B, n_q, H, D = shape
+    _like(shape, torch.bfloat16, dev, q, o)
+    n_kc = _chunk(q, dev, k_chunk, v_chunk)
+    if lse is not None:
+        _like((B, H, n_q), torch.float32, dev, lse)
+    fresh = []
+    with _owned_by(stream):
+        if o is None:
+            o = torch.empty_like(q); fresh.append(o)
+        if lse is None:
+            lse = q.new_empty((B, H, n_q), dtype=torch.float32); fresh.append(lse)
+        if workspace is None:
+            need = astro_chunk_attn8_fwd_workspace_bytes(cache, B, n_q, n_kc, H, D)
+            if need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _used_here(stream, *fresh)
+    st = lib().astro_chunk_attn8_fwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), B, H, D, n_q, n_kc, float(scale), _at(o),
+                                     _at(lse), *_scratch(workspace, dev), on)
+    _check(st, "astro_chunk_attn8_fwd")
+    return o, lse
+
+
+def astro_chunk_attn8_bwd_workspace_bytes(cache, batch, n_q, n_kc, heads=None, head_dim=None) -> int:
+    return _workspace8("astro_chunk_attn8_bwd_workspace_bytes", cache, batch, n_q, n_kc, heads, head_dim)
+
+
+def astro_chunk_attn8_bwd(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: float, dq=None, dk_chunk=None, dv_chunk=None, workspace=None,
+                          stream=None):
+    """Returns (dQ, dK_chunk, dV_chunk), bf16, of astro_chunk_attn8_fwd; the cached context receives no gradient."""
+    import torch
+    dev, on = _where(stream, q)
+    shape = q.shape
+    B, n_q, H, D = shape
+    _like(shape, torch.bfloat16, dev, q, o, d_o, dq)
+    _like((B, H, n_q), torch.float32, dev, lse)
+    n_kc = _chunk(q, dev, k_chunk, v_chunk, dk_chunk, dv_chunk)
+    fresh = []
+    with _owned_by(stream):
+        if dq is None:
+            dq = torch.empty_like(q); fresh.append(dq)
+        if n_kc and dk_chunk is None:
+            dk_chunk = torch.empty_like(k_chunk); fresh.append(dk_chunk)
+        if n_kc and dv_chunk is None:
+            dv_chunk = torch.empty_like(v_chunk); fresh.append(dv_chunk)
+        if workspace is None:
+            need = astro_chunk_attn8_bwd_workspace_bytes(cache, B, n_q, n_kc, H, D)
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _used_here(stream, *fresh)
+    st = lib().astro_chunk_attn8_bwd(_handle(cache, dev), _at(q), _at(k_chunk), _at(v_chunk), _at(o), _at(lse), _at(d_o), B, H, D, n_q,
+                                     n_kc, float(scale), _at(dq), _at(dk_chunk), _at(dv_chunk), *_scratch(workspace, dev), on)
+    _check(st, "astro_chunk_attn8_bwd")
     return dq, dk_chunk, dv_chunk
 
 

@@ -11,10 +11,12 @@
 #include <mutex>
 #include <new>
 
+#include "attn8.cuh"
 #include "attn_bwd.cuh"
 #include "attn_fwd.cuh"
 #include "attn_fwd_pair.cuh"
 #include "block_select.cuh"
+#include "kv_quant.cuh"
 #include "kv_ring.cuh"
 #include "nft_loss.cuh"
 #include "rope.cuh"
@@ -26,6 +28,7 @@ using namespace astro;
 
 struct astro_kvcache {
   astro_kvcache_desc_t d;
+  int bits;        // 16, or 8: rows in 8 bits with an exponent each
   void* k;
   void* v;
   int sink_held;   // frames in sink slots [0, S)
@@ -245,7 +248,8 @@ struct AttnArgs {
   int batch, heads, head_dim, n_q, n_kc;
 };
 
-astro_status_t check_attn_args(const AttnArgs& a, float scale) {
+// `bits`: the kind of cache that the call reads.
+astro_status_t check_attn_args(const AttnArgs& a, float scale, int bits = 16) {
   if (a.batch < 1 || a.heads < 1 || a.n_q < 1 || a.n_kc < 0) return ASTRO_ERR_SHAPE;
   if (a.head_dim != 64 && a.head_dim != 128) return ASTRO_ERR_SHAPE;
   if (!(scale >= 0.f) || !(scale < 3.0e38f)) return ASTRO_ERR_SHAPE;
@@ -253,7 +257,7 @@ astro_status_t check_attn_args(const AttnArgs& a, float scale) {
   int held = 0;
   if (a.cache) {
     const auto& d = a.cache->d;
-    if (d.heads != a.heads || d.head_dim != a.head_dim) return ASTRO_ERR_SHAPE;
+    if (a.cache->bits != bits || d.heads != a.heads || d.head_dim != a.head_dim) return ASTRO_ERR_SHAPE;
     if (d.cache_batch != a.batch && d.cache_batch != 1) return ASTRO_ERR_SHAPE;
     held = a.cache->sink_held + a.cache->win_held;
   }
@@ -772,6 +776,174 @@ astro_status_t launch_sparse_bwd(const SparseCall& c, const SparseGeom& g, float
                           maps, tq, tdo, g, a, k, static_cast<int>(heads * q_tiles));
 }
 
+// ---- the cache in 8 bits ------------------------------------------------------------------------------------
+size_t codes_bytes(const astro_kvcache_desc_t& d) {
+  return static_cast<size_t>(d.cache_batch) * d.heads * (d.sink_frames + d.window_frames) * d.tokens_per_frame * d.head_dim;
+}
+
+// Everything about the storage but the caller's tensors; `base`: one of the two storages.
+QuantTensors quant_tensors(const astro_kvcache* c, int n_frames) {
+  const auto& d = c->d;
+  QuantTensors x;
+  x.k = x.v = nullptr;
+  x.k_store = static_cast<uint8_t*>(c->k);
+  x.v_store = static_cast<uint8_t*>(c->v);
+  x.k_exp = x.k_store + codes_bytes(d);      // a multiple of 64 bytes
+  x.v_exp = x.v_store + codes_bytes(d);
+  x.slot_tokens = static_cast<long long>(d.sink_frames + d.window_frames) * d.tokens_per_frame;
+  x.heads = d.heads;
+  x.tokens_per_frame = d.tokens_per_frame;
+  x.n_tokens = n_frames * d.tokens_per_frame;   // at most the storage's, which create keeps below 2^31
+  x.in_h = d.head_dim;
+  x.in_t = static_cast<long long>(d.heads) * d.head_dim;
+  x.in_b = x.in_t * x.n_tokens;
+  return x;
+}
+
+struct QuantGrid {
+  dim3 grid;
+  int threads;
+};
+bool quant_grid(const QuantTensors& x, int batch, int head_dim, QuantGrid* g) {
+  const long long positions = static_cast<long long>(x.heads) * head_dim / 8;
+  g->threads = positions >= kQuantThreads ? kQuantThreads : static_cast<int>((positions + 31) / 32 * 32);
+  const long long y = (positions + g->threads - 1) / g->threads;
+  if (batch > 32767 || y > 65535) return false;
+  g->grid = dim3(static_cast<unsigned>((x.n_tokens + kQuantTokens - 1) / kQuantTokens), static_cast<unsigned>(y), 2u * batch);
+  return true;
+}
+
+template <typename T, bool Write>
+astro_status_t launch_quant(const QuantTensors& x, const FrameSlots& slots, int batch, int head_dim, cudaStream_t st) {
+  QuantGrid g;
+  if (!quant_grid(x, batch, head_dim, &g)) return ASTRO_ERR_SHAPE;
+  if constexpr (Write) {
+    if (head_dim == 128) cache8_append_kernel<T, 128><<<g.grid, g.threads, 0, st>>>(x, slots);
+    else cache8_append_kernel<T, 64><<<g.grid, g.threads, 0, st>>>(x, slots);
+  } else {
+    if (head_dim == 128) cache8_read_kernel<T, 128><<<g.grid, g.threads, 0, st>>>(x, slots);
+    else cache8_read_kernel<T, 64><<<g.grid, g.threads, 0, st>>>(x, slots);
+  }
+  return launch_status();
+}
+template <bool Write>
+astro_status_t launch_quant_typed(int dtype, const QuantTensors& x, const FrameSlots& slots, int batch, int head_dim, cudaStream_t st) {
+  if (dtype == ASTRO_BF16) return launch_quant<__nv_bfloat16, Write>(x, slots, batch, head_dim, st);
+  if (dtype == ASTRO_F16) return launch_quant<__half, Write>(x, slots, batch, head_dim, st);
+  return launch_quant<float, Write>(x, slots, batch, head_dim, st);
+}
+
+// Up to this many queries per sample take the kernel that reads the codes themselves.
+constexpr int kFewMaxQueries = 64;
+
+int held_tokens(const astro_kvcache* c) { return c ? (c->sink_held + c->win_held) * c->d.tokens_per_frame : 0; }
+
+// CTAs (one per SM) that share a list of keys: as many as fill a B200's 148 SMs once, each with two steps of every warp at least.
+int few_splits(int batch, int heads, int n_q, long long keys) {
+  const int per_cta = n_q <= 8 ? 8 : 16;
+  const long long units = static_cast<long long>(batch) * heads * ((n_q - 1) / per_cta + 1);
+  const long long most = keys / (2 * kFewStep * (128 / per_cta)) + 1;
+  long long want = 148 / units;
+  if (want > most) want = most;
+  return want < 1 ? 1 : static_cast<int>(want);
+}
+
+struct Attn8Call {
+  AttnArgs a;
+  const void *q, *k_chunk, *v_chunk;
+};
+
+template <int D, int NT>
+astro_status_t launch_few(const Attn8Call& c, float scale, void* o, float* lse, void* workspace, cudaStream_t st) {
+  using S = FewShape<D, NT>;
+  constexpr int kSmem = few_smem_bytes<D, NT>();
+  static std::atomic<int> done[kMaxDevices];
+  astro_status_t s = set_smem_once(attn8_few_kernel<D, NT>, kSmem, done);
+  if (s != ASTRO_OK) return s;
+  FewArgs f;
+  std::memset(&f, 0, sizeof(f));
+  f.q = static_cast<const __nv_bfloat16*>(c.q);
+  f.kc = static_cast<const __nv_bfloat16*>(c.k_chunk);
+  f.vc = static_cast<const __nv_bfloat16*>(c.v_chunk);
+  f.o = static_cast<__nv_bfloat16*>(o);
+  f.lse = lse;
+  f.n_ctx = held_tokens(c.a.cache);
+  f.n_kc = c.a.n_kc;
+  if (f.n_ctx > 0) {
+    const QuantTensors x = quant_tensors(c.a.cache, 0);
+    f.k = x.k_store; f.v = x.v_store; f.k_exp = x.k_exp; f.v_exp = x.v_exp;
+    f.slot_tokens = x.slot_tokens;
+    const KeySegs segs = build_segments(c.a.cache, 0);
+    f.start0 = segs.start[0];
+    f.count0 = segs.count[0];
+    f.start1 = segs.n > 1 ? segs.start[1] : 0;
+  }
+  f.batch = c.a.batch; f.heads = c.a.heads; f.n_q = c.a.n_q;
+  f.q_tiles = (c.a.n_q - 1) / (8 * NT) + 1;
+  f.cache_shared = c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1 ? 1 : 0;
+  f.splits = few_splits(c.a.batch, c.a.heads, c.a.n_q, static_cast<long long>(f.n_ctx) + f.n_kc);
+  f.scale_log2 = scale * kLog2e;
+  const long long rows = static_cast<long long>(c.a.batch) * c.a.heads * c.a.n_q;
+  if (f.splits > 1) {
+    f.part_o = static_cast<float*>(workspace);
+    f.part_lse = f.part_o + f.splits * rows * D;
+  }
+  const dim3 grid(static_cast<unsigned>(f.q_tiles * f.splits), f.cache_shared ? c.a.batch : c.a.heads, f.cache_shared ? c.a.heads : c.a.batch);
+  attn8_few_kernel<D, NT><<<grid, S::kThreads, kSmem, st>>>(f);
+  if ((s = launch_status()) != ASTRO_OK || f.splits == 1) return s;
+  return launch_dependent(sparse_combine_kernel<D>, dim3(static_cast<unsigned>((rows + 7) / 8)), 256, 0, st, f.part_o, f.part_lse,
+                          f.splits, rows, c.a.n_q, c.a.heads, f.o, lse);
+}
+
+// Bytes of the held rows in bf16, K or V.
+size_t expanded_bytes(const astro_kvcache* c) {
+  return c ? static_cast<size_t>(c->d.cache_batch) * c->d.heads * held_tokens(c) * c->d.head_dim * 2 : 0;
+}
+
+// The held rows into bf16 [B_c, H, n, D], K and then V, and the maps of them; `segs`: what the dense kernels walk.
+struct Expanded {
+  CUtensorMap k, v;
+  KeySegs segs;
+};
+astro_status_t expand_context(const Attn8Call& c, void* workspace, Expanded* out, cudaStream_t st) {
+  std::memset(out, 0, sizeof(*out));
+  const int n = held_tokens(c.a.cache);
+  if (n > 0) {
+    const auto& d = c.a.cache->d;
+    const QuantTensors x = quant_tensors(c.a.cache, 0);
+    const KeySegs segs = build_segments(c.a.cache, 0);
+    Expand8 e;
+    e.k = x.k_store; e.v = x.v_store; e.k_exp = x.k_exp; e.v_exp = x.v_exp;
+    e.k_out = static_cast<__nv_bfloat16*>(workspace);
+    e.v_out = reinterpret_cast<__nv_bfloat16*>(static_cast<char*>(workspace) + expanded_bytes(c.a.cache));
+    e.slot_tokens = x.slot_tokens;
+    e.start0 = segs.start[0];
+    e.count0 = segs.count[0];
+    e.start1 = segs.n > 1 ? segs.start[1] : 0;
+    e.n = n;
+    const int per_block = kExpandThreads * 8 / d.head_dim * kExpandRows;
+    const long long lists = static_cast<long long>(d.cache_batch) * d.heads;
+    if (lists > 65535) return ASTRO_ERR_SHAPE;
+    const dim3 grid(static_cast<unsigned>((n + per_block - 1) / per_block), static_cast<unsigned>(lists), 2);
+    const unsigned long long row = static_cast<unsigned long long>(d.head_dim) * 2;
+    for (int i = 0; i < 2; ++i) {
+      astro_status_t s = make_tmap(i ? &out->v : &out->k, i ? e.v_out : e.k_out, d.head_dim, n, d.heads, d.cache_batch, row, row * n,
+                                   row * n * d.heads);
+      if (s != ASTRO_OK) return s;
+    }
+    if (d.head_dim == 128) expand8_kernel<128><<<grid, kExpandThreads, 0, st>>>(e);
+    else expand8_kernel<64><<<grid, kExpandThreads, 0, st>>>(e);
+    astro_status_t s = launch_status();
+    if (s != ASTRO_OK) return s;
+    out->segs.count[out->segs.n++] = n;
+  }
+  if (c.a.n_kc > 0) {
+    out->segs.count[out->segs.n] = c.a.n_kc;
+    out->segs.from_chunk[out->segs.n++] = 1;
+  }
+  return ASTRO_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -782,28 +954,34 @@ size_t astro_kvcache_storage_bytes(const astro_kvcache_desc_t* d) {
          d->tokens_per_frame * d->head_dim * 2;
 }
 
-astro_status_t astro_kvcache_create(const astro_kvcache_desc_t* desc, void* k_storage, void* v_storage,
-                                    size_t bytes_each, astro_kvcache_t** out) {
+static astro_status_t create_cache(const astro_kvcache_desc_t* desc, int bits, void* k_storage, void* v_storage, size_t bytes_each,
+                                   astro_kvcache_t** out) {
   if (!desc || !k_storage || !v_storage || !out) return ASTRO_ERR_NULL;
   if (!desc_ok(desc)) return ASTRO_ERR_SHAPE;
   if (!aligned16(k_storage) || !aligned16(v_storage)) return ASTRO_ERR_ALIGN;
-  if (bytes_each < astro_kvcache_storage_bytes(desc)) return ASTRO_ERR_CAPACITY;
+  if (bytes_each < (bits == 8 ? astro_kvcache8_storage_bytes(desc) : astro_kvcache_storage_bytes(desc))) return ASTRO_ERR_CAPACITY;
   const long long tok = static_cast<long long>(desc->sink_frames + desc->window_frames) * desc->tokens_per_frame;
   if (tok >= (1ll << 31) - kTile) return ASTRO_ERR_SHAPE;
   astro_kvcache* c = new (std::nothrow) astro_kvcache();
   if (!c) return ASTRO_ERR_CUDA;
   c->d = *desc;
+  c->bits = bits;
   c->k = k_storage;
   c->v = v_storage;
   c->sink_held = c->win_head = c->win_held = 0;
   c->frames_seen = 0;
   c->maps_status = ASTRO_ERR_CUDA;
-  if (get_encode_fn() != nullptr) {   // a driver is present: build the maps now, so attention calls only read them
+  if (bits == 16 && get_encode_fn() != nullptr) {   // a driver is present: build the maps now, so attention calls only read them
     const astro_status_t ms = cache_maps(c);
     if (ms != ASTRO_OK) { delete c; return ms; }
   }
   *out = c;
   return ASTRO_OK;
+}
+
+astro_status_t astro_kvcache_create(const astro_kvcache_desc_t* desc, void* k_storage, void* v_storage,
+                                    size_t bytes_each, astro_kvcache_t** out) {
+  return create_cache(desc, 16, k_storage, v_storage, bytes_each, out);
 }
 
 astro_status_t astro_kvcache_destroy(astro_kvcache_t* cache) {
@@ -826,6 +1004,7 @@ astro_status_t astro_kvcache_append(astro_kvcache_t* c, const void* k, const voi
   const int S = c->d.sink_frames, L = c->d.window_frames;
   const int room = (S - c->sink_held) + (L - c->win_held);
   if (n_frames > room) return ASTRO_ERR_CAPACITY;
+  if (c->bits == 8) return astro_kvcache8_append(c, k, v, n_frames, ASTRO_BF16, nullptr, stream);
   if (n_frames == 0) return ASTRO_OK;
   astro_status_t s = check_arch();
   if (s != ASTRO_OK) return s;
@@ -907,6 +1086,7 @@ astro_status_t astro_kvcache_export(const astro_kvcache_t* c, void* k_out, void*
   if (!aligned16(k_out) || !aligned16(v_out)) return ASTRO_ERR_ALIGN;
   const int n = c->sink_held + c->win_held;
   if (n == 0) return ASTRO_OK;
+  if (c->bits == 8) return astro_kvcache8_read(c, 0, n, ASTRO_BF16, k_out, v_out, stream);
   astro_status_t s = check_arch();
   if (s != ASTRO_OK) return s;
   int* slots = new (std::nothrow) int[n];
@@ -1071,7 +1251,7 @@ astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* s
   const auto &a = src->d, &d = dst->d;
   const int held = src->sink_held + src->win_held;
   if (!frames && n_frames == -1) n_frames = held;
-  if (n_frames < 0 || dst == src || a.heads != d.heads || a.head_dim != d.head_dim ||
+  if (n_frames < 0 || dst == src || src->bits != 16 || dst->bits != 16 || a.heads != d.heads || a.head_dim != d.head_dim ||
       a.tokens_per_frame != d.tokens_per_frame)
     return ASTRO_ERR_SHAPE;
   if (!parents && a.cache_batch != 1 && a.cache_batch != d.cache_batch) return ASTRO_ERR_SHAPE;
@@ -1271,6 +1451,7 @@ astro_status_t astro_block_count(const astro_kvcache_t* cache, int n_kc, int blo
 astro_status_t astro_block_pool(const astro_kvcache_t* c, int first_frame, int n_frames, int block_tokens, float* pooled,
                                 void* stream) {
   if (!c || !pooled) return ASTRO_ERR_NULL;
+  if (c->bits != 16) return ASTRO_ERR_SHAPE;
   KeyBlocks kb;
   if (!block_tokens_ok(block_tokens) || !build_key_blocks(c, 0, block_tokens, &kb)) return ASTRO_ERR_SHAPE;
   const int held = c->sink_held + c->win_held;
@@ -1420,6 +1601,159 @@ astro_status_t astro_sparse_attn_bwd(const astro_kvcache_t* cache, const void* q
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return head_dim == 128 ? launch_sparse_bwd<128>(c, g, scale, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, st)
                          : launch_sparse_bwd<64>(c, g, scale, o, lse, d_o, dq, dk_chunk, dv_chunk, workspace, st);
+}
+
+// ---- the cache in 8 bits ------------------------------------------------------------------------------
+size_t astro_kvcache8_storage_bytes(const astro_kvcache_desc_t* d) {
+  if (!desc_ok(d)) return 0;
+  const size_t codes = codes_bytes(*d);
+  return codes + (codes / d->head_dim + 15) / 16 * 16;
+}
+
+astro_status_t astro_kvcache8_create(const astro_kvcache_desc_t* desc, void* k_storage, void* v_storage, size_t bytes_each,
+                                     astro_kvcache_t** out) {
+  return create_cache(desc, 8, k_storage, v_storage, bytes_each, out);
+}
+
+astro_status_t astro_kvcache8_append(astro_kvcache_t* c, const void* k, const void* v, int n_frames, int dtype,
+                                     const astro_strides_t* strides, void* stream) {
+  if (!c || !k || !v) return ASTRO_ERR_NULL;
+  if (c->bits != 8 || n_frames < 0 || (dtype != ASTRO_BF16 && dtype != ASTRO_F16 && dtype != ASTRO_F32)) return ASTRO_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v)) return ASTRO_ERR_ALIGN;
+  const auto& d = c->d;
+  const int S = d.sink_frames, L = d.window_frames;
+  if (n_frames > static_cast<long long>(S - c->sink_held) + (L - c->win_held)) return ASTRO_ERR_CAPACITY;
+  if (n_frames == 0) return ASTRO_OK;
+  QuantTensors x = quant_tensors(c, n_frames);
+  x.k = const_cast<void*>(k);
+  x.v = const_cast<void*>(v);
+  if (strides) {
+    const long long sizes[3] = {d.cache_batch, x.n_tokens, d.heads}, given[3] = {strides->batch, strides->token, strides->head};
+    const int per16 = dtype == ASTRO_F32 ? 4 : 8;
+    for (int i = 0; i < 3; ++i) {
+      if (sizes[i] <= 1) continue;
+      if (given[i] < 0 || given[i] > (1ll << 40) / (sizes[i] - 1)) return ASTRO_ERR_SHAPE;
+      if (given[i] % per16) return ASTRO_ERR_ALIGN;
+    }
+    x.in_b = d.cache_batch > 1 ? strides->batch : 0;
+    x.in_t = x.n_tokens > 1 ? strides->token : 0;
+    x.in_h = d.heads > 1 ? strides->head : 0;
+  }
+  QuantGrid g;
+  if (!quant_grid(x, d.cache_batch, d.head_dim, &g)) return ASTRO_ERR_SHAPE;
+  astro_status_t s = check_arch();
+  if (s != ASTRO_OK) return s;
+  const int to_sink = n_frames < S - c->sink_held ? n_frames : S - c->sink_held;
+  const FrameSlots slots{c->sink_held + c->win_held, S, c->sink_held + to_sink, c->win_head, L};
+  s = launch_quant_typed<true>(dtype, x, slots, d.cache_batch, d.head_dim, static_cast<cudaStream_t>(stream));
+  if (s != ASTRO_OK) return s;
+  c->sink_held += to_sink;
+  c->win_held += n_frames - to_sink;
+  c->frames_seen += n_frames;
+  return ASTRO_OK;
+}
+
+astro_status_t astro_kvcache8_read(const astro_kvcache_t* c, int first_frame, int n_frames, int dtype, void* k_out, void* v_out,
+                                   void* stream) {
+  if (!c) return ASTRO_ERR_NULL;
+  const int held = c->sink_held + c->win_held;
+  if (c->bits != 8 || first_frame < 0 || n_frames < 0 || first_frame > held || n_frames > held - first_frame ||
+      (dtype != ASTRO_BF16 && dtype != ASTRO_F16 && dtype != ASTRO_F32))
+    return ASTRO_ERR_SHAPE;
+  if (n_frames == 0) return ASTRO_OK;
+  if (!k_out || !v_out) return ASTRO_ERR_NULL;
+  if (!aligned16(k_out) || !aligned16(v_out)) return ASTRO_ERR_ALIGN;
+  QuantTensors x = quant_tensors(c, n_frames);
+  x.k = k_out;
+  x.v = v_out;
+  QuantGrid g;
+  if (!quant_grid(x, c->d.cache_batch, c->d.head_dim, &g)) return ASTRO_ERR_SHAPE;
+  astro_status_t s = check_arch();
+  if (s != ASTRO_OK) return s;
+  const FrameSlots slots{first_frame, c->d.sink_frames, c->sink_held, c->win_head, c->d.window_frames};
+  return launch_quant_typed<false>(dtype, x, slots, c->d.cache_batch, c->d.head_dim, static_cast<cudaStream_t>(stream));
+}
+
+size_t astro_chunk_attn8_fwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
+  if (check_attn_args(AttnArgs{cache, batch, heads, head_dim, n_q, n_kc}, 1.f, 8) != ASTRO_OK) return 0;
+  if (n_q > kFewMaxQueries) return 2 * expanded_bytes(cache);
+  const int splits = few_splits(batch, heads, n_q, static_cast<long long>(held_tokens(cache)) + n_kc);
+  return splits == 1 ? 0 : static_cast<size_t>(splits) * batch * heads * n_q * (head_dim + 1) * sizeof(float);
+}
+
+astro_status_t astro_chunk_attn8_fwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk, int batch,
+                                     int heads, int head_dim, int n_q, int n_kc, float scale, void* o, float* lse, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  if (!q || !o || (n_kc > 0 && (!k_chunk || !v_chunk))) return ASTRO_ERR_NULL;
+  const Attn8Call c{{cache, batch, heads, head_dim, n_q, n_kc}, q, k_chunk, v_chunk};
+  astro_status_t s = check_attn_args(c.a, scale, 8);
+  if (s != ASTRO_OK) return s;
+  const size_t need = astro_chunk_attn8_fwd_workspace_bytes(cache, batch, heads, head_dim, n_q, n_kc);
+  if (need > 0 && !workspace) return ASTRO_ERR_NULL;
+  if (!aligned16(q) || !aligned16(o) || (n_kc > 0 && (!aligned16(k_chunk) || !aligned16(v_chunk))) ||
+      (need > 0 && !aligned16(workspace)) || (reinterpret_cast<uintptr_t>(lse) & 3u))
+    return ASTRO_ERR_ALIGN;
+  if (workspace_bytes < need) return ASTRO_ERR_CAPACITY;
+  if ((s = check_arch()) != ASTRO_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (n_q <= kFewMaxQueries) {
+    if (head_dim == 128)
+      return n_q <= 8 ? launch_few<128, 1>(c, scale, o, lse, workspace, st) : launch_few<128, 2>(c, scale, o, lse, workspace, st);
+    return n_q <= 8 ? launch_few<64, 1>(c, scale, o, lse, workspace, st) : launch_few<64, 2>(c, scale, o, lse, workspace, st);
+  }
+  CUtensorMap tkc, tvc;
+  std::memset(&tkc, 0, sizeof(tkc)); std::memset(&tvc, 0, sizeof(tvc));
+  if (n_kc > 0) {
+    if ((s = make_tmap_user(&tkc, k_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
+    if ((s = make_tmap_user(&tvc, v_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
+  }
+  Expanded x;
+  if ((s = expand_context(c, workspace, &x, st)) != ASTRO_OK) return s;
+  const CUtensorMap tvx[2] = {x.v, x.v};
+  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(q);
+  return head_dim == 128 ? launch_fwd<128>(c.a, qp, tkc, tvc, x.k, tvx, x.segs, scale, o, lse, st)
+                         : launch_fwd<64>(c.a, qp, tkc, tvc, x.k, tvx, x.segs, scale, o, lse, st);
+}
+
+size_t astro_chunk_attn8_bwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
+  if (check_attn_args(AttnArgs{cache, batch, heads, head_dim, n_q, n_kc}, 1.f, 8) != ASTRO_OK) return 0;
+  return 2 * expanded_bytes(cache) + astro_chunk_attn_bwd_workspace_bytes(batch, heads, n_q, head_dim);
+}
+
+astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
+                                     const void* o, const float* lse, const void* d_o, int batch, int heads, int head_dim, int n_q,
+                                     int n_kc, float scale, void* dq, void* dk_chunk, void* dv_chunk, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  if (!q || !o || !lse || !d_o || !dq || !workspace) return ASTRO_ERR_NULL;
+  if (n_kc > 0 && (!k_chunk || !v_chunk || !dk_chunk || !dv_chunk)) return ASTRO_ERR_NULL;
+  const Attn8Call c{{cache, batch, heads, head_dim, n_q, n_kc}, q, k_chunk, v_chunk};
+  astro_status_t s = check_attn_args(c.a, scale, 8);
+  if (s != ASTRO_OK) return s;
+  if (!aligned16(q) || !aligned16(o) || !aligned16(d_o) || !aligned16(dq) || !aligned16(workspace) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u) ||
+      (n_kc > 0 && (!aligned16(k_chunk) || !aligned16(v_chunk) || !aligned16(dk_chunk) || !aligned16(dv_chunk))))
+    return ASTRO_ERR_ALIGN;
+  if (workspace_bytes < astro_chunk_attn8_bwd_workspace_bytes(cache, batch, heads, head_dim, n_q, n_kc)) return ASTRO_ERR_CAPACITY;
+  if ((s = check_arch()) != ASTRO_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  CUtensorMap tdo, tkc, tvc;
+  std::memset(&tkc, 0, sizeof(tkc)); std::memset(&tvc, 0, sizeof(tvc));
+  if ((s = make_tmap_user(&tdo, d_o, head_dim, n_q, heads, batch)) != ASTRO_OK) return s;
+  if (n_kc > 0) {
+    if ((s = make_tmap_user(&tkc, k_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
+    if ((s = make_tmap_user(&tvc, v_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
+  }
+  float* delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * expanded_bytes(cache));
+  if ((s = astro_chunk_attn_bwd_delta(o, d_o, batch, heads, head_dim, n_q, delta, stream)) != ASTRO_OK) return s;
+  Expanded x;
+  if ((s = expand_context(c, workspace, &x, st)) != ASTRO_OK) return s;
+  const CUtensorMap tkx[2] = {x.k, x.k};
+  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(q);
+  s = head_dim == 128 ? launch_bwd_dq<128>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st)
+                      : launch_bwd_dq<64>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st);
+  if (s != ASTRO_OK || n_kc == 0) return s;
+  return astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, batch, heads, head_dim, n_q, n_kc, scale, dk_chunk, dv_chunk,
+                                  stream);
 }
 
 astro_status_t astro_nft_loss(const void* v_theta, const void* v_old, const void* v_ref, const void* v_target,

@@ -1,0 +1,216 @@
+// The rolling cache in 8 bits.  A row x (the D elements of one head and token) is held as one exponent e and D codes:
+//   e = the smallest whole number with max |x_d| <= 448 * 2^e over the row's finite elements, at least -124;
+//   code_d = e4m3(x_d * 2^-e), rounded to nearest even; an infinity or NaN becomes e4m3's NaN and touches no other element.
+//   (Of rows that reach 2^127 e is 120, and elements that would round to 256 * 2^120, beyond every finite float, are held as 240.)
+// The factor is a power of two, so that what a code stands for, code * 2^e, has 4 significant bits and a step of 2^-133 or
+// more: it is a bf16 number exactly, and attention over it needs no rounding beyond the one that the write made (half a step
+// of e4m3, 2^-4 of the element, or 2^(e-10) where that is larger).
+// Storage: codes [B_c, H, slot * T + t, D], then, from the next multiple of 16 bytes on, e + 127 as a byte for every row.
+// Everything here is bandwidth work: a thread owns 8 neighbouring elements (16 bytes of bf16, 8 of codes) of one head and walks
+// kQuantTokens tokens, all of them in flight, so that a warp reads 512 contiguous bytes of the caller's tensor and writes whole rows.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+namespace astro {
+
+constexpr int kQuantTokens = 8;
+constexpr int kQuantThreads = 256;
+constexpr int kQuantLowestExp = -124;
+
+// Where the frames of a call sit: frame j of the call is the cache's logical frame first + j; the sink's frames sit in their
+// own slots, the window's in the ring behind them.
+struct FrameSlots {
+  int first, sink_frames, sink_held, win_head, win_slots;
+  __host__ __device__ int slot(int j) const {
+    const int f = first + j;
+    if (f < sink_held) return f;
+    const unsigned at = static_cast<unsigned>(win_head) + static_cast<unsigned>(f - sink_held);   // less than two rounds
+    return sink_frames + static_cast<int>(at < static_cast<unsigned>(win_slots) ? at : at - win_slots);
+  }
+};
+
+struct QuantTensors {
+  void *k, *v;                       // the caller's
+  uint8_t *k_store, *v_store;        // codes
+  uint8_t *k_exp, *v_exp;
+  long long in_b, in_t, in_h;        // strides of the caller's tensors in elements
+  long long slot_tokens;             // tokens of the storage per (sample, head)
+  int heads, tokens_per_frame, n_tokens;
+};
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      float2 f;
+      if constexpr (std::is_same<T, __half>::value) f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      else f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    } else {
+      x[i] = __uint_as_float(w[i]);
+    }
+  }
+  if constexpr (sizeof(T) == 4) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p + 4);
+    x[4] = __uint_as_float(u.x); x[5] = __uint_as_float(u.y); x[6] = __uint_as_float(u.z); x[7] = __uint_as_float(u.w);
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (std::is_same<T, __half>::value) {
+        const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// Two floats of at most 448 in magnitude (or NaN) -> two e4m3 codes, `lo` in the low byte.
+__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// Two codes in the low 16 bits -> two fp16, which hold every e4m3 number (and its NaN).
+__device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t codes) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(codes)));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3_to_floats(uint32_t codes) {
+  const uint32_t h = e4m3_to_half2(codes);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+// 2^e of a stored exponent byte (3..247): its own exponent field.
+__device__ __forceinline__ float exp_byte_to_float(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// grid.x: token chunks, grid.y: head * D/8 positions, grid.z = 2 * b + (0: K, 1: V).  Lanes without a position stay for the
+// shuffles.
+template <typename T, int D>
+__global__ void __launch_bounds__(kQuantThreads) cache8_append_kernel(const QuantTensors x, const FrameSlots slots) {
+  constexpr int kLanes = D / 8;                         // lanes of a row
+  const int hv = blockIdx.y * blockDim.x + threadIdx.x;
+  const bool there = hv < x.heads * kLanes;
+  const int h = there ? hv / kLanes : 0, part = hv % kLanes;
+  const int b = blockIdx.z >> 1;
+  const bool is_v = blockIdx.z & 1;
+  const int t0 = blockIdx.x * kQuantTokens;
+  const int n = there ? min(kQuantTokens, x.n_tokens - t0) : 0;
+  const T* src = static_cast<const T*>(is_v ? x.v : x.k) + b * x.in_b + t0 * x.in_t + h * x.in_h + part * 8;
+  float f[kQuantTokens][8];
+#pragma unroll
+  for (int i = 0; i < kQuantTokens; ++i) {
+    if (i < n) {
+      load8(src + i * x.in_t, f[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[i][e] = 0.f;
+    }
+  }
+  const long long row_base = (static_cast<long long>(b) * x.heads + h) * x.slot_tokens;
+  uint8_t* codes = is_v ? x.v_store : x.k_store;
+  uint8_t* exps = is_v ? x.v_exp : x.k_exp;
+  int frame = t0 / x.tokens_per_frame, in_frame = t0 - frame * x.tokens_per_frame;
+  long long slot_row = row_base + static_cast<long long>(slots.slot(frame)) * x.tokens_per_frame;
+#pragma unroll
+  for (int i = 0; i < kQuantTokens; ++i) {
+    uint32_t top = 0;                                   // bits of the largest finite magnitude: ordered like the numbers
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t m = __float_as_uint(f[i][e]) & 0x7fffffffu;
+      top = max(top, m < 0x7f800000u ? m : 0u);
+    }
+#pragma unroll
+    for (int s = kLanes / 2; s > 0; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+    // top = 1.f * 2^k <= 1.75 * 2^(e + 8)
+    const int k = static_cast<int>(top >> 23) - 127;
+    const int e = max(kQuantLowestExp, k - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0));
+    const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // 2^-e: -e is 124 at most, -120 at least
+    const float most = e == 120 ? 240.f : 448.f;
+    uint32_t w[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      float y[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float v = f[i][4 * p + c];
+        y[c] = fabsf(v) < INFINITY ? fminf(fmaxf(v * inv, -most), most) : __uint_as_float(0x7fffffffu);
+      }
+      w[p] = e4m3_pair(y[0], y[1]) | e4m3_pair(y[2], y[3]) << 16;
+    }
+    if (i < n) {
+      const long long row = slot_row + in_frame;
+      *reinterpret_cast<uint2*>(codes + row * D + part * 8) = make_uint2(w[0], w[1]);
+      if (part == 0) exps[row] = static_cast<uint8_t>(e + 127);
+      if (++in_frame == x.tokens_per_frame) {
+        in_frame = 0;
+        slot_row = row_base + static_cast<long long>(slots.slot(++frame)) * x.tokens_per_frame;
+      }
+    }
+  }
+}
+
+// The reverse, into contiguous rows at strides of the caller's (in_b, in_t, in_h).  The same grid.
+template <typename T, int D>
+__global__ void __launch_bounds__(kQuantThreads) cache8_read_kernel(const QuantTensors x, const FrameSlots slots) {
+  constexpr int kLanes = D / 8;
+  const int hv = blockIdx.y * blockDim.x + threadIdx.x;
+  if (hv >= x.heads * kLanes) return;
+  const int h = hv / kLanes, part = hv % kLanes;
+  const int b = blockIdx.z >> 1;
+  const bool is_v = blockIdx.z & 1;
+  const int t0 = blockIdx.x * kQuantTokens;
+  const int n = min(kQuantTokens, x.n_tokens - t0);
+  const long long row_base = (static_cast<long long>(b) * x.heads + h) * x.slot_tokens;
+  const uint8_t* codes = is_v ? x.v_store : x.k_store;
+  const uint8_t* exps = is_v ? x.v_exp : x.k_exp;
+  int frame = t0 / x.tokens_per_frame, in_frame = t0 - frame * x.tokens_per_frame;
+  long long slot_row = row_base + static_cast<long long>(slots.slot(frame)) * x.tokens_per_frame;
+  uint2 w[kQuantTokens];
+  uint32_t e[kQuantTokens];
+#pragma unroll
+  for (int i = 0; i < kQuantTokens; ++i) {
+    if (i >= n) continue;
+    const long long row = slot_row + in_frame;
+    w[i] = *reinterpret_cast<const uint2*>(codes + row * D + part * 8);
+    e[i] = exps[row];
+    if (++in_frame == x.tokens_per_frame) {
+      in_frame = 0;
+      if (i + 1 < n) slot_row = row_base + static_cast<long long>(slots.slot(++frame)) * x.tokens_per_frame;
+    }
+  }
+  T* dst = static_cast<T*>(is_v ? x.v : x.k) + b * x.in_b + t0 * x.in_t + h * x.in_h + part * 8;
+#pragma unroll
+  for (int i = 0; i < kQuantTokens; ++i) {
+    if (i >= n) continue;
+    const float s = exp_byte_to_float(e[i]);
+    const float2 p[4] = {e4m3_to_floats(w[i].x), e4m3_to_floats(w[i].x >> 16), e4m3_to_floats(w[i].y), e4m3_to_floats(w[i].y >> 16)};
+    float f[8];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      f[2 * c] = p[c].x * s;
+      f[2 * c + 1] = p[c].y * s;
+    }
+    store8(dst + i * x.in_t, f);
+  }
+}
+
+}  // namespace astro

@@ -1,0 +1,183 @@
+"""Attention over a cache in 8 bits on the GPU, against attention in 64 bits over what the cache holds (attn_bounds.py)."""
+import pytest
+
+from attn_bounds import check, head
+
+pytestmark = pytest.mark.gpu
+
+
+def modules():
+    import torch
+    from paper_2603_17051_b200 import binding as A
+    return torch, A
+
+
+def filled(torch, A, Bc, H, D, T, S, L, held, head_at, seed, spread=0.5):
+    """A cache of `held` frames whose window starts at ring slot head_at."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    cache = A.astro_kvcache8_create(Bc, H, D, T, S, L)
+    for s in (cache.k_storage, cache.v_storage):
+        s.fill_(0x7f)                                        # NaN in every row that is not written
+    sink = min(S, held)
+    size = torch.exp(spread * torch.randn(2, H, D, generator=g, device="cuda"))
+    k, v = ((torch.randn(Bc, held * T, H, D, generator=g, device="cuda") * size[i]).bfloat16() for i in range(2))
+    cut = lambda x, a, b: x[:, a * T:b * T].contiguous()  # noqa: E731
+    if sink:
+        A.astro_kvcache8_append(cache, cut(k, 0, sink), cut(v, 0, sink), sink)
+    if held > sink:
+        A.astro_kvcache_set_state(cache, A.KVCacheState(sink, head_at, 1, sink + 1))    # an empty window starts at 0: hold one,
+        A.astro_kvcache_evict(cache, 0)
+        if held - sink > 1:
+            A.astro_kvcache8_append(cache, cut(k, sink + 1, held), cut(v, sink + 1, held), held - sink - 1)
+        A.astro_kvcache_set_state(cache, A.KVCacheState(sink, (head_at - 1) % L, 1, sink + 1))  # and write it last
+        if L > 1:
+            A.astro_kvcache8_append(cache, cut(k, sink, sink + 1), cut(v, sink, sink + 1), 1)
+        else:
+            A.astro_kvcache_set_state(cache, A.KVCacheState(sink, 0, 0, sink))
+            A.astro_kvcache8_append(cache, cut(k, sink, sink + 1), cut(v, sink, sink + 1), 1)
+        A.astro_kvcache_set_state(cache, A.KVCacheState(sink, head_at, held - sink, held))
+    return cache
+
+
+def compare(torch, A, cache, q, kc, vc, scale, d_o=None, tag="", rows=None, heads=None):
+    B, n_q, H, D = q.shape
+    o, lse = A.astro_chunk_attn8_fwd(cache, q, kc, vc, scale)
+    grads = None if d_o is None else A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, scale)
+    A.astro_last_device_status()
+    if cache is not None:
+        k8, v8 = (x.double() for x in A.astro_kvcache8_read(cache, dtype=torch.float32))
+        n_ctx = k8.shape[1]
+    else:
+        n_ctx = 0
+    for b in range(B):
+        for h in range(H) if heads is None else heads:
+            parts = []
+            for x, y in ((k8 if n_ctx else None, kc), (v8 if n_ctx else None, vc)):
+                got = ([x[b if x.shape[0] > 1 else 0, :, h]] if n_ctx else []) + ([] if y is None else [y[b, :, h].double()])
+                parts.append(torch.cat(got))
+            want = head(q[b, :, h].double(), *parts, scale, d_o=None if d_o is None else d_o[b, :, h].double())
+            name = "%s sample %d head %d " % (tag, b, h)
+            check(o[b, :, h], want["o"], name + "O")
+            check(lse[b, h], want["lse"], name + "LSE")
+            if d_o is not None:
+                check(grads[0][b, :, h], want["dq"], name + "dQ")
+                if kc is not None:
+                    check(grads[1][b, :, h], tuple(x[n_ctx:] for x in want["dk"]), name + "dK")
+                    check(grads[2][b, :, h], tuple(x[n_ctx:] for x in want["dv"]), name + "dV")
+    return o, lse
+
+
+def tensors(torch, B, n_q, n_kc, H, D, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    make = lambda n: torch.randn(B, n, H, D, generator=g, device="cuda").bfloat16() if n else None  # noqa: E731
+    return make(n_q), make(n_kc), make(n_kc), make(n_q)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q", [1, 2, 7, 8, 9, 16, 17, 63, 64, 65, 130])
+def test_numbers_of_queries(D, n_q):
+    torch, A = modules()
+    cache = filled(torch, A, 2, 3, D, 37, 1, 6, 6, 4, n_q)
+    q, kc, vc, d_o = tensors(torch, 2, n_q, 11, 3, D, n_q + 100)
+    compare(torch, A, cache, q, kc, vc, D ** -0.5, d_o)
+
+
+@pytest.mark.parametrize("n_q", [1, 12, 100])
+@pytest.mark.parametrize("T,S,L,held,at", [(1, 0, 1, 1, 0), (1, 4, 600, 530, 590), (1, 4, 20, 3, 0), (15, 0, 1, 1, 0), (16, 1, 3, 4, 2), (17, 2, 5, 6, 3),
+                                           (129, 0, 4, 3, 3), (500, 3, 3, 5, 1)])
+@pytest.mark.parametrize("n_kc", [0, 1, 16, 45])
+def test_lengths_and_places_of_the_context(n_q, T, S, L, held, at, n_kc):
+    torch, A = modules()
+    for Bc in (1, 2):
+        cache = filled(torch, A, Bc, 2, 64, T, S, L, held, at, T + n_kc)
+        q, kc, vc, d_o = tensors(torch, 2, n_q, n_kc, 2, 64, held)
+        compare(torch, A, cache, q, kc, vc, 0.125, d_o if n_q > 1 else None, "cache batch %d" % Bc)
+
+
+def test_without_a_context():
+    torch, A = modules()
+    empty = A.astro_kvcache8_create(1, 2, 128, 4, 1, 2)
+    for n_q in (1, 20, 70):
+        q, kc, vc, d_o = tensors(torch, 2, n_q, 33, 2, 128, n_q)
+        for cache in (None, empty):
+            o, lse = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.1)
+            want = A.astro_chunk_attn_fwd(None, q, kc, vc, 0.1)
+            if n_q > 64:
+                assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+        compare(torch, A, None, q, kc, vc, 0.1, d_o)
+
+
+@pytest.mark.parametrize("n_q", [1, 3, 40, 300])
+def test_large_scores_and_large_values(n_q):
+    """Scores of several hundred, rising along the keys; values and keys of very different sizes from row to row."""
+    torch, A = modules()
+    B, H, D, T, L = 1, 2, 128, 64, 8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    cache = A.astro_kvcache8_create(B, H, D, T, 0, L)
+    n = T * L
+    ramp = torch.linspace(0.1, 4.0, n, device="cuda").view(1, n, 1, 1)
+    size = torch.exp2(torch.randint(-40, 40, (B, n, H, 1), generator=g, device="cuda").float())
+    k = (torch.randn(B, n, H, D, generator=g, device="cuda") * ramp).bfloat16()
+    v = (torch.randn(B, n, H, D, generator=g, device="cuda") * size).bfloat16()
+    A.astro_kvcache8_append(cache, k, v, L)
+    q, kc, vc, _ = tensors(torch, B, n_q, 5, H, D, 4)
+    compare(torch, A, cache, q * 3, kc, vc, 1.0)
+
+
+@pytest.mark.parametrize("n_q", [1, 20, 100])
+def test_nan_in_one_element_of_a_value_reaches_that_element_alone(n_q):
+    torch, A = modules()
+    cache = A.astro_kvcache8_create(1, 1, 64, 40, 0, 2)
+    q, k, v, _ = tensors(torch, 1, max(n_q, 80), 80, 1, 64, 5)
+    q = q[:, :n_q].contiguous()
+    v[0, 41, 0, 7] = float("inf")
+    A.astro_kvcache8_append(cache, k, v, 2)
+    o, lse = A.astro_chunk_attn8_fwd(cache, q, None, None, 0.125)
+    bad = o.isnan()
+    assert bad[..., 7].all() and bad.sum() == n_q and lse.isfinite().all()
+
+
+@pytest.mark.parametrize("shape", ["rollout", "update"])
+def test_layer_size(shape):
+    torch, A = modules()
+    B, n_q, S, L, held = (4, 1, 3, 12, 12) if shape == "rollout" else (1, 4680, 3, 18, 18)
+    cache = filled(torch, A, B, 12, 128, 1560, S, L, held, 1, 6)
+    q, kc, vc, d_o = tensors(torch, B, n_q, n_q, 12, 128, 7)
+    heads = range(12) if n_q == 1 else (0, 11)
+    if n_q == 1:
+        compare(torch, A, cache, q, kc, vc, 128 ** -0.5, heads=heads)
+        return
+    o, lse = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 128 ** -0.5)
+    dense = A.astro_kvcache_create(1, 12, 128, 1560, S, L)
+    A.astro_kvcache_append(dense, *A.astro_kvcache8_read(cache), held)
+    want, want_lse = A.astro_chunk_attn_fwd(dense, q, kc, vc, 128 ** -0.5)     # the same rows in 16 bits, tiles cut elsewhere
+    assert (o.float() - want.float()).abs().max() <= 2.0 ** -8 * 2 and (lse - want_lse).abs().max() <= 1e-5
+    got, ref = (f(c, q, kc, vc, o, lse, d_o, 128 ** -0.5) for f, c in ((A.astro_chunk_attn8_bwd, cache), (A.astro_chunk_attn_bwd, dense)))
+    for a, r in zip(got, ref):
+        assert (a.float() - r.float()).norm() <= 2.0 ** -8 * r.float().norm()
+    assert torch.equal(got[1], ref[1]) and torch.equal(got[2], ref[2])
+
+
+def test_a_captured_call_and_one_on_another_stream():
+    torch, A = modules()
+    cache = filled(torch, A, 2, 2, 128, 50, 1, 4, 5, 2, 8)
+    for n_q in (1, 9, 100):
+        q, kc, vc, d_o = tensors(torch, 2, n_q, 7, 2, 128, 9)
+        want = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.1)
+        grads = A.astro_chunk_attn8_bwd(cache, q, kc, vc, *want, d_o, 0.1)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.1, stream=side)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            inside = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.1)
+            inside_grads = A.astro_chunk_attn8_bwd(cache, q, kc, vc, *inside, d_o, 0.1)
+        for x in (*inside, *inside_grads):
+            x.zero_()
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((*want, *grads), (*inside, *inside_grads)))
+        del graph
