@@ -352,6 +352,38 @@ astro_status_t astro_sparse_attn_bwd(const astro_kvcache_t* cache, const void* q
                                      void* dq, void* dk_chunk, void* dv_chunk, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
+/* ---- sliding window with sinks over whole sequences ---------------------------------------------------------------
+ * The attention of the streaming scheme for all the blocks of a sequence at once, as it is trained or as a prompt is taken in:
+ * with c = i / block_tokens, query i sees key j iff
+ *     j < min(len, (c + 1) * block_tokens)  and  (j < sink_tokens or j >= (c + 1) * block_tokens - window_tokens),
+ * its own block whole, the window_tokens - block_tokens tokens in front of it, and the sink.  (A cache of S + L frames from which a caller
+ * evicts down to S + L - c frames before every chunk of c frames of T tokens shows a chunk the same keys with block_tokens = c T,
+ * sink_tokens = S T, window_tokens = L T.)  block_tokens = 1 is the sliding window of single tokens; a window_tokens of n_tokens +
+ * block_tokens and more shows every token in front.  heads / kv_heads neighbouring heads share a head of k and v.
+ *   q, o [batch, n_tokens, heads, head_dim], k, v [batch, n_tokens, kv_heads, head_dim], bf16, LSE fp32 [batch, heads, n_tokens].
+ *   q_strides, k_strides, v_strides: null = contiguous; multiples of 16 bytes, no stride of 0.  o is contiguous.
+ *   lengths: device int32 [batch], tokens of each sample (values outside 0..n_tokens count as the nearer end); null: n_tokens each.  What k, v and q
+ *   hold from there on does not matter, NaN included; those queries get O = 0 and LSE = -infinity.
+ * A NaN or infinity reaches the queries that see it and no others.  lse may be null.  n_tokens = 0 is an empty call.
+ * ASTRO_ERR_SHAPE: head_dim not 64 or 128, heads not a multiple of kv_heads, window_tokens < block_tokens, n_tokens > 2^29, a scale that
+ * is negative or not finite.  bf16 products, fp32 accumulation and softmax. */
+typedef struct {
+  int batch, n_tokens, heads, kv_heads, head_dim;
+  int block_tokens, window_tokens, sink_tokens;
+} astro_window_desc_t;
+astro_status_t astro_window_attn_fwd(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,
+                                     const astro_strides_t* k_strides, const void* v, const astro_strides_t* v_strides,
+                                     const int32_t* lengths, float scale, void* o, float* lse, void* stream);
+/* Its backward, nothing detached: dQ, and dK and dV of every token, summed over the heads that share it, from dO and the forward's
+ * O and LSE (all contiguous, as are dq, dk and dv).  Queries and keys from a sequence's length on get zeros, and what o, lse and d_o hold there does not
+ * matter.  workspace: device scratch, 16-byte aligned, at least astro_window_attn_bwd_workspace_bytes().  All sums have one
+ * fixed order: the same call gives the same bits. */
+size_t astro_window_attn_bwd_workspace_bytes(int batch, int heads, int n_tokens, int head_dim);
+astro_status_t astro_window_attn_bwd(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,
+                                     const astro_strides_t* k_strides, const void* v, const astro_strides_t* v_strides,
+                                     const int32_t* lengths, const void* o, const float* lse, const void* d_o, float scale, void* dq,
+                                     void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Eq. 1, Eq. 2 and the selective KL term of Sec. 3.4 (Algorithm 2, "Policy loss on window"), fused with
  * the gradient for the current policy, over the velocity tensors of the active window:
  *   v+ = (1-beta) v_old + beta v_theta;  v- = (1+beta) v_old - beta v_theta;

@@ -28,7 +28,7 @@ EXPORTED = ("astro_kvcache_key_segments", "astro_selftest_wait_timeout", "astro_
             "astro_sparse_attn_fwd", "astro_sparse_attn_bwd_workspace_bytes", "astro_sparse_attn_bwd",
             "astro_kvcache8_storage_bytes", "astro_kvcache8_create", "astro_kvcache8_append", "astro_kvcache8_read",
             "astro_chunk_attn8_fwd_workspace_bytes", "astro_chunk_attn8_fwd", "astro_chunk_attn8_bwd_workspace_bytes",
-            "astro_chunk_attn8_bwd")
+            "astro_chunk_attn8_bwd", "astro_window_attn_fwd", "astro_window_attn_bwd_workspace_bytes", "astro_window_attn_bwd")
 
 
 class AstroError(RuntimeError):
@@ -53,6 +53,11 @@ class RopeDesc(C.Structure):
                 ("axis_pairs", C.c_int * 4), ("base", C.c_double), ("scaling", C.c_int), ("scaled_axes", C.c_int),
                 ("factor", C.c_double), ("original_length", C.c_double), ("ramp_low", C.c_double),
                 ("ramp_high", C.c_double), ("magnitude", C.c_double)]
+
+
+class WindowDesc(C.Structure):
+    _fields_ = [("batch", C.c_int), ("n_tokens", C.c_int), ("heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("block_tokens", C.c_int), ("window_tokens", C.c_int), ("sink_tokens", C.c_int)]
 
 
 class Strides(C.Structure):
@@ -153,6 +158,13 @@ def lib():
     L.astro_chunk_attn8_bwd_workspace_bytes.argtypes = [vp, ci, ci, ci, ci, ci]
     L.astro_chunk_attn8_bwd.restype = ci
     L.astro_chunk_attn8_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, cf, vp, vp, vp, vp, sz, vp]
+    rows = [vp, C.POINTER(Strides)]
+    L.astro_window_attn_fwd.restype = ci
+    L.astro_window_attn_fwd.argtypes = [C.POINTER(WindowDesc), *rows, *rows, *rows, vp, cf, vp, vp, vp]
+    L.astro_window_attn_bwd_workspace_bytes.restype = sz
+    L.astro_window_attn_bwd_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    L.astro_window_attn_bwd.restype = ci
+    L.astro_window_attn_bwd.argtypes = [C.POINTER(WindowDesc), *rows, *rows, *rows, vp, vp, vp, vp, cf, vp, vp, vp, vp, sz, vp]
     L.astro_debug_forward_mode.restype = ci
     L.astro_debug_forward_mode.argtypes = [ci]
     L.astro_debug_pair_flag.restype = ci
@@ -935,6 +947,83 @@ def astro_chunk_attn8_bwd(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: float,
                                      n_kc, float(scale), _at(dq), _at(dk_chunk), _at(dv_chunk), *_scratch(workspace, dev), on)
     _check(st, "astro_chunk_attn8_bwd")
     return dq, dk_chunk, dv_chunk
+
+
+def _window_call(q, k, v, block_tokens, window_tokens, sink_tokens, lengths, dev):
+    """(descriptor, [address and strides of q, k, v], address of lengths) of a call on whole sequences."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k and v must be [B, n, heads, head_dim]")
+    B, n, H, D = q.shape
+    rows = []
+    for x, heads in ((q, H), (k, k.shape[2]), (v, k.shape[2])):
+        if x.dtype is not torch.bfloat16 or x.get_device() != dev or x.shape != (B, n, heads, D):
+            raise ValueError("q, k and v must be bf16 [B, n, heads, head_dim] beside each other, k and v of the same heads")
+        if x.is_contiguous():
+            rows += [x.data_ptr(), None]
+            continue
+        if x.stride(3) != 1:
+            raise ValueError("the elements of a head must be contiguous")
+        rows += [x.data_ptr(), C.byref(Strides(*_rope_strides(x)))]
+    if lengths is not None:
+        _like((B,), torch.int32, dev, lengths)
+    window = 0x7fffffff if window_tokens is None else _int(window_tokens)
+    d = WindowDesc(B, _int(n), H, k.shape[2], D, _int(block_tokens), window, _int(sink_tokens))
+    return d, rows, _at(lengths)
+
+
+def astro_window_attn_fwd(q, k, v, scale: float, block_tokens: int = 1, window_tokens=None, sink_tokens: int = 0, lengths=None, o=None,
+                          lse=None, stream=None):
+    """Attention of whole sequences with a sliding window and sinks (see include/astro.h): q [B, n, H, D], k and v [B, n, KVH, D], bf16,
+    strided as long as a head's elements are contiguous; window_tokens None: everything in front; lengths: int32 [B] on the
+    device or None.  Returns (O bf16 [B, n, H, D], LSE fp32 [B, H, n])."""
+    import torch
+    dev, on = _where(stream, q)
+    d, rows, lens = _window_call(q, k, v, block_tokens, window_tokens, sink_tokens, lengths, dev)
+    B, n, H, D = shape = q.shape
+    _like(shape, torch.bfloat16, dev, o)
+    if lse is not None:
+        _like((B, H, n), torch.float32, dev, lse)
+    fresh = []
+    with _owned_by(stream):
+        if o is None:
+            o = torch.empty(shape, dtype=q.dtype, device=q.device); fresh.append(o)
+        if lse is None:
+            lse = q.new_empty((B, H, n), dtype=torch.float32); fresh.append(lse)
+    _used_here(stream, *fresh)
+    _check(lib().astro_window_attn_fwd(C.byref(d), *rows, lens, float(scale), _at(o), _at(lse), on), "astro_window_attn_fwd")
+    return o, lse
+
+
+def astro_window_attn_bwd_workspace_bytes(batch, heads, n_tokens, head_dim) -> int:
+    return int(lib().astro_window_attn_bwd_workspace_bytes(_int(batch), _int(heads), _int(n_tokens), _int(head_dim)))
+
+
+def astro_window_attn_bwd(q, k, v, o, lse, d_o, scale: float, block_tokens: int = 1, window_tokens=None, sink_tokens: int = 0,
+                          lengths=None, dq=None, dk=None, dv=None, workspace=None, stream=None):
+    """Returns (dQ, dK, dV), bf16 and contiguous, of astro_window_attn_fwd with the same arguments."""
+    import torch
+    dev, on = _where(stream, q)
+    d, rows, lens = _window_call(q, k, v, block_tokens, window_tokens, sink_tokens, lengths, dev)
+    B, n, H, D = shape = q.shape
+    _like(shape, torch.bfloat16, dev, o, d_o, dq)
+    _like(k.shape, torch.bfloat16, dev, dk, dv)
+    _like((B, H, n), torch.float32, dev, lse)
+    fresh = []
+    with _owned_by(stream):
+        if dq is None:
+            dq = torch.empty(shape, dtype=q.dtype, device=q.device); fresh.append(dq)
+        if dk is None:
+            dk = torch.empty(k.shape, dtype=q.dtype, device=q.device); fresh.append(dk)
+        if dv is None:
+            dv = torch.empty(k.shape, dtype=q.dtype, device=q.device); fresh.append(dv)
+        if workspace is None:
+            need = astro_window_attn_bwd_workspace_bytes(B, H, n, D)
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
+    _used_here(stream, *fresh)
+    _check(lib().astro_window_attn_bwd(C.byref(d), *rows, lens, _at(o), _at(lse), _at(d_o), float(scale), _at(dq), _at(dk), _at(dv),
+                                       *_scratch(workspace, dev), on), "astro_window_attn_bwd")
+    return dq, dk, dv
 
 
 def astro_nft_loss(v_theta, v_old, v_ref, v_target, r_tilde, beta: float, w_policy=None, w_kl=None, grad=True,

@@ -23,6 +23,8 @@
 #include "sparse_bwd.cuh"
 #include "sparse_decode.cuh"
 #include "sparse_fwd.cuh"
+#include "window_bwd.cuh"
+#include "window_fwd.cuh"
 
 using namespace astro;
 
@@ -944,6 +946,139 @@ astro_status_t expand_context(const Attn8Call& c, void* workspace, Expanded* out
   return ASTRO_OK;
 }
 
+// ---- sliding window with sinks over whole sequences ---------------------------------------------------------
+// A tensor [batch, n, heads, D] of the caller's: contiguous where `given` is null.  ASTRO_ERR_SHAPE for strides that leave 64 bits
+// or let rows fall onto one another (a tensor map has no stride of 0).
+astro_status_t window_strides(const astro_window_desc_t& d, int heads, const astro_strides_t* given, WinStrides* out) {
+  const long long row = d.head_dim;
+  *out = WinStrides{row * heads * d.n_tokens, row * heads, row};
+  if (!given) return ASTRO_OK;
+  const long long sizes[3] = {d.batch, d.n_tokens, heads}, s[3] = {given->batch, given->token, given->head};
+  for (int i = 0; i < 3; ++i) {
+    if (sizes[i] <= 1) continue;
+    if (s[i] < 1 || s[i] > (1ll << 38) / (sizes[i] - 1)) return ASTRO_ERR_SHAPE;
+    if (s[i] % 8) return ASTRO_ERR_ALIGN;
+  }
+  if (overlaps_itself(sizes, s, row)) return ASTRO_ERR_SHAPE;
+  if (d.batch > 1) out->b = s[0];
+  if (d.n_tokens > 1) out->t = s[1];
+  if (heads > 1) out->h = s[2];
+  return ASTRO_OK;
+}
+
+astro_status_t check_window(const astro_window_desc_t& d) {
+  if (d.batch < 1 || d.n_tokens < 0 || d.n_tokens > (1 << 29) || d.heads < 1 || d.kv_heads < 1 || d.heads % d.kv_heads ||
+      (d.head_dim != 64 && d.head_dim != 128) || d.block_tokens < 1 || d.window_tokens < d.block_tokens || d.sink_tokens < 0 ||
+      d.batch > 65535 || d.heads > 65535)
+    return ASTRO_ERR_SHAPE;
+  const long long tiles = (static_cast<long long>(d.n_tokens) + kTile - 1) / kTile;
+  return tiles * d.batch * d.heads > 0x3fffffffLL ? ASTRO_ERR_SHAPE : ASTRO_OK;
+}
+
+WinMask window_mask(const astro_window_desc_t& d, const int32_t* lengths) {
+  WinMask m;
+  m.n = d.n_tokens;
+  m.block = d.block_tokens < d.n_tokens ? d.block_tokens : d.n_tokens;
+  // a window that reaches to the first token from the end of any block shows everything in front (a block longer than the
+  // sequence is the sequence)
+  const int most = d.n_tokens + m.block;
+  m.window = d.block_tokens > d.n_tokens || d.window_tokens > most ? most : d.window_tokens;
+  m.sink = d.sink_tokens < d.n_tokens ? d.sink_tokens : d.n_tokens;
+  m.lengths = lengths;
+  return m;
+}
+
+astro_status_t make_tmap_strided(CUtensorMap* out, const void* base, int head_dim, int n, int heads, int batch, const WinStrides& s) {
+  return make_tmap(out, base, head_dim, n, heads, batch, 2ull * s.t, 2ull * s.h, 2ull * s.b);
+}
+
+struct WindowCall {
+  astro_window_desc_t d;
+  const void *q, *k, *v;
+  WinStrides qs, ks, vs;
+  const int32_t* lengths;
+};
+
+astro_status_t check_window_call(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,
+                                 const astro_strides_t* k_strides, const void* v, const astro_strides_t* v_strides,
+                                 const int32_t* lengths, float scale, WindowCall* c) {
+  c->d = *desc;
+  c->q = q; c->k = k; c->v = v;
+  c->lengths = lengths;
+  astro_status_t s = check_window(*desc);
+  if (s != ASTRO_OK) return s;
+  if (!(scale >= 0.f) || !(scale < 3.0e38f)) return ASTRO_ERR_SHAPE;
+  if ((s = window_strides(*desc, desc->heads, q_strides, &c->qs)) != ASTRO_OK) return s;
+  if ((s = window_strides(*desc, desc->kv_heads, k_strides, &c->ks)) != ASTRO_OK) return s;
+  if ((s = window_strides(*desc, desc->kv_heads, v_strides, &c->vs)) != ASTRO_OK) return s;
+  if (desc->n_tokens > 0 && (!aligned16(q) || !aligned16(k) || !aligned16(v) || (reinterpret_cast<uintptr_t>(lengths) & 3u)))
+    return ASTRO_ERR_ALIGN;
+  return ASTRO_OK;
+}
+
+template <int D>
+astro_status_t launch_window_fwd(const WindowCall& c, float scale, void* o, float* lse, cudaStream_t st) {
+  static std::atomic<int> done[kMaxDevices];
+  astro_status_t s = set_smem_once(window_attn_fwd_kernel<D>, WinFwdSmem<D>::kTotal, done);
+  if (s != ASTRO_OK) return s;
+  CUtensorMap tk, tv;
+  if ((s = make_tmap_strided(&tk, c.k, D, c.d.n_tokens, c.d.kv_heads, c.d.batch, c.ks)) != ASTRO_OK) return s;
+  if ((s = make_tmap_strided(&tv, c.v, D, c.d.n_tokens, c.d.kv_heads, c.d.batch, c.vs)) != ASTRO_OK) return s;
+  WinFwdArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(c.q);
+  a.k = static_cast<const __nv_bfloat16*>(c.k);
+  a.v = static_cast<const __nv_bfloat16*>(c.v);
+  a.qs = c.qs; a.ks = c.ks; a.vs = c.vs;
+  a.o = static_cast<__nv_bfloat16*>(o);
+  a.lse = lse;
+  a.mask = window_mask(c.d, c.lengths);
+  a.heads = c.d.heads;
+  a.group = c.d.heads / c.d.kv_heads;
+  a.lists = c.d.batch * c.d.heads;
+  a.q_tiles = (c.d.n_tokens + kTile - 1) / kTile;
+  a.scale = scale;
+  a.scale_log2 = scale * kLog2e;
+  a.careful = g_fwd_mode.load(std::memory_order_relaxed) == 1 ? 1 : 0;
+  window_attn_fwd_kernel<D><<<static_cast<unsigned>(a.lists) * a.q_tiles, kWinThreads, WinFwdSmem<D>::kTotal, st>>>(tk, tv, a);
+  return launch_status();
+}
+
+template <int D>
+astro_status_t launch_window_bwd(const WindowCall& c, const void* o, const float* lse, const void* d_o, float scale, void* dq, void* dk,
+                                 void* dv, void* workspace, cudaStream_t st) {
+  static std::atomic<int> done[kMaxDevices];
+  astro_status_t s = set_smem_once(window_attn_bwd_kernel<D>, window_bwd_smem<D>(), done);
+  if (s != ASTRO_OK) return s;
+  const auto& d = c.d;
+  CUtensorMap tq, tdo, tk, tv;
+  if ((s = make_tmap_strided(&tq, c.q, D, d.n_tokens, d.heads, d.batch, c.qs)) != ASTRO_OK) return s;
+  if ((s = make_tmap_user(&tdo, d_o, D, d.n_tokens, d.heads, d.batch)) != ASTRO_OK) return s;
+  if ((s = make_tmap_strided(&tk, c.k, D, d.n_tokens, d.kv_heads, d.batch, c.ks)) != ASTRO_OK) return s;
+  if ((s = make_tmap_strided(&tv, c.v, D, d.n_tokens, d.kv_heads, d.batch, c.vs)) != ASTRO_OK) return s;
+  WinBwdArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(c.q);
+  a.k = static_cast<const __nv_bfloat16*>(c.k);
+  a.v = static_cast<const __nv_bfloat16*>(c.v);
+  a.d_o = static_cast<const __nv_bfloat16*>(d_o);
+  a.qs = c.qs; a.ks = c.ks; a.vs = c.vs;
+  a.lse = lse;
+  a.delta = static_cast<const float*>(workspace);
+  a.dq = static_cast<__nv_bfloat16*>(dq);
+  a.dk = static_cast<__nv_bfloat16*>(dk);
+  a.dv = static_cast<__nv_bfloat16*>(dv);
+  a.mask = window_mask(d, c.lengths);
+  a.heads = d.heads;
+  a.kv_heads = d.kv_heads;
+  a.group = d.heads / d.kv_heads;
+  a.lists = d.batch * d.heads;
+  a.kv_lists = d.batch * d.kv_heads;
+  a.tiles = (d.n_tokens + kTile - 1) / kTile;
+  a.scale = scale;
+  if ((s = launch_bwd_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, static_cast<float*>(workspace), st)) != ASTRO_OK) return s;
+  return launch_dependent(window_attn_bwd_kernel<D>, dim3(static_cast<unsigned>(a.lists + a.kv_lists) * a.tiles), kWinBwdThreads,
+                          window_bwd_smem<D>(), st, tq, tdo, tk, tv, a);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1754,6 +1889,43 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
   if (s != ASTRO_OK || n_kc == 0) return s;
   return astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, batch, heads, head_dim, n_q, n_kc, scale, dk_chunk, dv_chunk,
                                   stream);
+}
+
+// ---- sliding window with sinks over whole sequences ---------------------------------------------------
+astro_status_t astro_window_attn_fwd(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,
+                                     const astro_strides_t* k_strides, const void* v, const astro_strides_t* v_strides,
+                                     const int32_t* lengths, float scale, void* o, float* lse, void* stream) {
+  if (!desc || (desc->n_tokens > 0 && (!q || !k || !v || !o))) return ASTRO_ERR_NULL;
+  WindowCall c;
+  astro_status_t s = check_window_call(desc, q, q_strides, k, k_strides, v, v_strides, lengths, scale, &c);
+  if (s != ASTRO_OK || desc->n_tokens == 0) return s;
+  if (!aligned16(o) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return ASTRO_ERR_ALIGN;
+  if ((s = check_arch()) != ASTRO_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return desc->head_dim == 128 ? launch_window_fwd<128>(c, scale, o, lse, st) : launch_window_fwd<64>(c, scale, o, lse, st);
+}
+
+size_t astro_window_attn_bwd_workspace_bytes(int batch, int heads, int n_tokens, int head_dim) {
+  return astro_chunk_attn_bwd_workspace_bytes(batch, heads, n_tokens, head_dim);
+}
+
+astro_status_t astro_window_attn_bwd(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,
+                                     const astro_strides_t* k_strides, const void* v, const astro_strides_t* v_strides,
+                                     const int32_t* lengths, const void* o, const float* lse, const void* d_o, float scale, void* dq,
+                                     void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!desc || (desc->n_tokens > 0 && (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv || !workspace))) return ASTRO_ERR_NULL;
+  WindowCall c;
+  astro_status_t s = check_window_call(desc, q, q_strides, k, k_strides, v, v_strides, lengths, scale, &c);
+  if (s != ASTRO_OK || desc->n_tokens == 0) return s;
+  if (!aligned16(o) || !aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(workspace) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u))
+    return ASTRO_ERR_ALIGN;
+  if (workspace_bytes < astro_window_attn_bwd_workspace_bytes(desc->batch, desc->heads, desc->n_tokens, desc->head_dim))
+    return ASTRO_ERR_CAPACITY;
+  if ((s = check_arch()) != ASTRO_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return desc->head_dim == 128 ? launch_window_bwd<128>(c, o, lse, d_o, scale, dq, dk, dv, workspace, st)
+                               : launch_window_bwd<64>(c, o, lse, d_o, scale, dq, dk, dv, workspace, st);
 }
 
 astro_status_t astro_nft_loss(const void* v_theta, const void* v_old, const void* v_ref, const void* v_target,

@@ -1,0 +1,684 @@
+// Backward of attention with a sliding window and sinks (window_common.cuh), nothing detached.
+//   dQ     a query tile stationary, over the key tiles that it sees:    dQ = scale * sum dS K
+//   dK/dV  a key tile stationary, over the query tiles of all the heads that share it and see it:
+//          dV = sum P^T dO, dK = scale * sum dS^T Q
+// with P = exp(S - LSE), dS = P o (dP - delta), as in the dense kernels (attn_bwd.cuh), whose tensor-memory layouts, operand
+// forms and hand-offs these two have: see there.  Both in one launch, a CTA per tile, the query tiles first; within each the long
+// ones come first.  Tiles of which a row sees only a part are masked bit by bit, P and dS by selection, so that what a masked
+// place holds, NaN included, ends there; rows behind a sequence's end are cleared in shared memory where they are operands.
+// Inside a sequence a NaN or infinity in K, Q or dO would still reach the rows of a masked tile that do not see it (0 * NaN):
+// a tile whose gradients are not finite is done again by the formula, on the ordinary cores (slow and rare).
+// Every accumulator belongs to one CTA: results do not depend on the order of anything.
+// Precision: bf16 products, fp32 sums; P and dS are rounded to bf16 (half a step, 2^-8 of each term at most) as operands of the
+// second products.
+#pragma once
+#include "attn_bwd.cuh"
+#include "sparse_common.cuh"
+#include "window_fwd.cuh"
+
+namespace astro {
+
+struct WinBwdArgs {
+  const __nv_bfloat16 *q, *k, *v, *d_o;
+  WinStrides qs, ks, vs;
+  const float *lse, *delta;       // [B, H, n]
+  __nv_bfloat16 *dq, *dk, *dv;    // [B, n, H or KVH, D]
+  WinMask mask;
+  int heads, kv_heads, group, lists, kv_lists, tiles;   // lists = batch * heads, kv_lists = batch * kv_heads
+  float scale;
+};
+constexpr int kWinBwdThreads = kDqSoftmaxThreads + 64;   // MMA, loads
+static_assert(kWinBwdThreads == kDkvThreads, "both kinds of CTA have the same warps");
+
+// 32 accumulator columns of the lane's row times `mult`, zeros where the row is not live, as bf16; whether all are finite.
+__device__ __forceinline__ bool win_store_row32(uint32_t taddr, float mult, bool live, const QuadRows& rows, int col0, int lane) {
+  uint32_t r[32];
+  tmem_ld32(taddr, r);
+  tmem_wait_ld();
+  uint64_t chk2 = f32x2(0.f, 0.f);
+  win_store_slice(r, mult, live, chk2, rows, col0, lane);
+  return !live || fwd_all_finite(chk2);
+}
+
+// ------------------------------------------------------------------------------------------ dQ
+// One row of dQ by the formula: eight lanes per key, four keys at a time.
+template <int D>
+__device__ __noinline__ void win_careful_dq(const WinBwdArgs& a, int qt, int h, int b, int warp, int lane) {
+  constexpr int kPer = D / 8;
+  const int len = a.mask.length(b), part = lane & 7, slot = lane >> 3;
+  for (int r = warp; r < kTile; r += kWinBwdThreads / 32) {
+    const int row = qt * kTile + r;
+    if (row >= len) break;
+    const size_t stat = (static_cast<size_t>(b) * a.heads + h) * a.mask.n + row;
+    const float lse2 = a.lse[stat] * kLog2e, delta = a.delta[stat], scale_log2 = a.scale * kLog2e;
+    const __nv_bfloat16* qp = a.q + b * a.qs.b + row * a.qs.t + h * a.qs.h + part * kPer;
+    const size_t at = ((static_cast<size_t>(b) * a.mask.n + row) * a.heads + h) * D + part * kPer;
+    float acc[kPer], q[kPer], g[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      acc[e] = 0.f;
+      q[e] = __bfloat162float(qp[e]);
+      g[e] = __bfloat162float(a.d_o[at + e]);
+    }
+    int lo, hi;
+    a.mask.keys_of(row, len, lo, hi);
+    const int sink = min(min(a.mask.sink, hi), lo), keys = sink + hi - lo;
+    const __nv_bfloat16* kb = a.k + b * a.ks.b + (h / a.group) * a.ks.h + part * kPer;
+    const __nv_bfloat16* vb = a.v + b * a.vs.b + (h / a.group) * a.vs.h + part * kPer;
+    for (int x = 0; x < keys; x += 4) {
+      const bool there = x + slot < keys;
+      const int y = there ? x + slot : keys - 1, j = y < sink ? y : lo + y - sink;
+      float s = 0.f, dp = 0.f;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        s = fmaf(q[e], __bfloat162float(kb[j * a.ks.t + e]), s);
+        dp = fmaf(g[e], __bfloat162float(vb[j * a.vs.t + e]), dp);
+      }
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) {
+        s += __shfl_xor_sync(0xffffffffu, s, d);
+        dp += __shfl_xor_sync(0xffffffffu, dp, d);
+      }
+      if (there) {
+        const float ds = fast_exp2(s * scale_log2 - lse2) * (dp - delta);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(ds, __bfloat162float(kb[j * a.ks.t + e]), acc[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+#pragma unroll
+      for (int d = 8; d < 32; d *= 2) acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], d);
+      if (slot == 0) a.dq[at + e] = __float2bfloat16_rn(acc[e] * a.scale);
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CUtensorMap& tm_do,
+                                           const WinBwdArgs& a, const int qt, const int h, const int b) {
+  uint8_t* smem = align_1024(smem_raw);
+  uint8_t* sdO = smem + DqSmem<D>::kdO;
+  uint8_t* sK = smem + DqSmem<D>::kK;
+  uint8_t* sV = smem + DqSmem<D>::kV;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + DqSmem<D>::kBars);
+  uint64_t *kv0_full = bars, *qt_full = bars + 1, *rs = bars + 2, *rb = bars + 6, *s_full = bars + 10, *b_done = bars + 11,
+           *dq_full = bars + 13, *landed = bars + 14;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bars + 15);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int q0 = qt * kTile, len = a.mask.length(b), kvh = h / a.group;
+  constexpr uint32_t kTmemCols = 512;
+  constexpr uint32_t kColS = 0, kColdP = 128, kColdS = 256, kColQ = 320, kColdQ = 384;
+  constexpr int kMmaWarp = 4 * kDqGroups, kTmaWarp = kMmaWarp + 1;
+
+  if (q0 >= len) {   // nothing but zeros, the same for the whole CTA
+    dependency_wait();
+    if (warp < kMmaWarp) {
+      const QuadRows rows = quad_rows(a.dq, b, h, a.mask.n, a.heads, D, q0 + (tid & 127));
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        uint4 zero[4] = {};
+        store_quad_rows(zero, rows, (warp >> 2) * (D / 2) + c * 32, lane);
+      }
+    }
+    return;
+  }
+  WinTiles tiles;
+  tiles.set(a.mask, q0, len);
+  const int n_tiles = tiles.count();
+
+  if (warp == kTmaWarp && lane == 0) { tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v); tma_prefetch_desc(&tm_do); }
+  if (tid < 15) {
+    // qt_full: one arrival per warp and 64 elements; rs, rb: bytes and warps
+    mbar_init(bars + tid, tid == 1 ? 4 * (D / 64) : tid >= 2 && tid < 10 ? 1 + 4 * kDqGroups : 1);
+    fence_mbar_init();
+  }
+  if (tid == 0) *abort_flag = 0;
+  fence_proxy_async_smem();
+  if (warp == kMmaWarp) {
+    tmem_alloc(tmem_holder, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_holder;
+  bool redo = false;
+
+  if (warp == kTmaWarp) {
+    int kt = tiles.first();
+    // K of a tile that straddles the sequence's end: its rows behind it are cleared before anyone is told (dS is 0 there, but
+    // 0 * NaN would reach dQ).  It is the last tile, so at most once.
+    auto load_kv = [&](int t, uint64_t* k_bar, uint64_t* v_bar, bool k_counted) {
+      uint8_t *k_dst = sK + (t % kDqKStages) * TileGeom<D>::kBytes, *v_dst = sV + (t % kDqVStages) * TileGeom<D>::kBytes;
+      const bool straddles = kt * kTile + kTile > len && len < a.mask.n;
+      bool ok = true;
+      if (lane == 0) tma_load_tile<D>(v_dst, &tm_v, v_bar, kt * kTile, kvh, b);
+      if (straddles) {
+        if (lane == 0) {
+          mbar_arrive_expect_tx(landed, TileGeom<D>::kBytes);
+          tma_load_tile<D>(k_dst, &tm_k, landed, kt * kTile, kvh, b);
+        }
+        ok = mbar_wait_ok(landed, 0, abort_flag);
+        zero_rows_by_warp<D>(k_dst, len - kt * kTile, lane);
+        if (lane == 0 && k_counted) mbar_arrive(k_bar);
+      } else if (lane == 0) {
+        if (k_counted) mbar_arrive_expect_tx(k_bar, TileGeom<D>::kBytes);
+        tma_load_tile<D>(k_dst, &tm_k, k_bar, kt * kTile, kvh, b);
+      }
+      kt = tiles.next(kt);
+      return ok;
+    };
+    const bool k0_straddles = kt * kTile + kTile > len && len < a.mask.n;
+    // kv0_full counts one arrival: it comes with the bytes, or behind the clearing where there is any
+    if (lane == 0) {
+      if (!k0_straddles) mbar_arrive_expect_tx(kv0_full, 3 * TileGeom<D>::kBytes);
+      else asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(kv0_full)), "r"(2 * TileGeom<D>::kBytes) : "memory");
+      tma_load_tile<D>(sdO, &tm_do, kv0_full, q0, h, b);
+    }
+    __syncwarp();
+    bool ok = load_kv(0, kv0_full, kv0_full, false);
+    if (k0_straddles && lane == 0) mbar_arrive(kv0_full);
+    for (int t = 1; ok && t <= n_tiles; ++t) {
+      // commit t-1 of b_done: dQ(t-3) and dP(t-2) are done, the K stage and the V stage of tile t are free
+      if (t >= 2 && !mbar_wait_ok(b_done + ((t - 1) & 1), ((t - 2) >> 1) & 1, abort_flag)) break;
+      if (t < n_tiles) {
+        if (lane == 0) mbar_arrive_expect_tx(rb + (t - 1) % 4, TileGeom<D>::kBytes);
+        __syncwarp();
+        ok = load_kv(t, rs + (t - 1) % 4, rb + (t - 1) % 4, true);
+      } else if (lane == 0) {
+        mbar_arrive(rb + (t - 1) % 4);   // the last tile's burst waits for no bytes (its rs is never awaited)
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    if (lane == 0) {
+      constexpr uint32_t idesc_s = make_idesc_bf16(kTile, kTile, false, false);
+      const uint64_t k_desc0 = desc_kmajor(smem_u32(sK));
+      auto issue_s = [&](int j) {
+        const uint64_t k_desc = desc_step(k_desc0, (j % kDqKStages) * TileGeom<D>::kBytes);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          mma_ts(tmem_base + kColS, tmem_base + kColQ + k * 8,
+                 desc_step(k_desc, (k >> 2) * TileGeom<D>::kBlockBytes + (k & 3) * 32), idesc_s, k > 0);
+        mma_commit(s_full);
+      };
+      auto issue_dp = [&](int j) {
+        mma_abT<D>(tmem_base + kColdP, smem_u32(sdO), smem_u32(sV + (j % kDqVStages) * TileGeom<D>::kBytes));
+      };
+      bool ok = mbar_wait_spin(qt_full, 0, abort_flag);
+      ok = mbar_wait_spin(kv0_full, 0, abort_flag) && ok;
+      tc_fence_after_sync();
+      if (ok) {
+        issue_s(0);
+        issue_dp(0);
+        mma_commit(b_done + 1);                       // commit 1
+      }
+      for (int j = 0; ok && j < n_tiles; ++j) {
+        const bool more = j + 1 < n_tiles;
+        if (more) {
+          if (!mbar_wait_spin(rs + j % 4, (j / 4) & 1, abort_flag)) break;
+          tc_fence_after_sync();
+          issue_s(j + 1);
+        }
+        if (!mbar_wait_spin(rb + j % 4, (j / 4) & 1, abort_flag)) break;
+        tc_fence_after_sync();
+        if (more) issue_dp(j + 1);
+        mma_pb<D, kTile>(tmem_base + kColdQ, tmem_base + kColdS, smem_u32(sK + (j % kDqKStages) * TileGeom<D>::kBytes), j > 0);
+        mma_commit(b_done + (j & 1));                 // commit j + 2
+      }
+      mma_commit(dq_full);
+    }
+  } else {
+    const int g = warp >> 2;
+    const int r = tid & 127;
+    const uint32_t tmem_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const int row = q0 + r;
+    const bool live = row < len;
+    const size_t stat_idx = (static_cast<size_t>(b) * a.heads + h) * a.mask.n + (live ? row : 0);
+    {   // Q row -> tensor memory: group g writes elements [64g, 64g+64) of its row as 32 packed columns
+      if (g * 64 < D) {
+        uint32_t qr[32];
+        const QuadRows q_rows = quad_rows_strided(a.q, a.qs, b, h, a.mask.n, row);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint4 ch[4];
+          load_quad_rows(ch, q_rows, g * 64 + half * 32, lane);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            qr[16 * half + 4 * v] = ch[v].x; qr[16 * half + 4 * v + 1] = ch[v].y;
+            qr[16 * half + 4 * v + 2] = ch[v].z; qr[16 * half + 4 * v + 3] = ch[v].w;
+          }
+        }
+        tmem_st32(tmem_lane + kColQ + g * 32, qr);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        warp_arrive(qt_full, lane);
+      }
+    }
+    dependency_wait();   // delta
+    const float lse2 = live ? a.lse[stat_idx] * kLog2e : 0.f;
+    const float delta_r = live ? a.delta[stat_idx] : 0.f;
+    const float scale_log2 = a.scale * kLog2e;
+    const uint64_t sc2 = f32x2(scale_log2, scale_log2), nl2 = f32x2(-lse2, -lse2), nd2 = f32x2(-delta_r, -delta_r);
+    int lo = 0, hi = 0;
+    if (live) a.mask.keys_of(row, len, lo, hi);
+    const int sink = min(a.mask.sink, hi);
+    int kt = tiles.first();
+    for (int j = 0; j < n_tiles; ++j, kt = tiles.next(kt)) {
+      bool ok = mbar_wait_ok(s_full, j & 1, abort_flag);
+      tc_fence_after_sync();
+      uint32_t s[2][32];
+      tmem_ld32(tmem_lane + kColS + g * kDqCols, s[0]);
+      tmem_ld32(tmem_lane + kColS + g * kDqCols + 32, s[1]);
+      tmem_wait_ld();
+      tc_fence_before_sync();
+      warp_arrive(rs + j % 4, lane);
+      uint64_t p2[2][16];
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          float x0, x1;
+          f32x2_split(fma2(f32x2(__uint_as_float(s[c2][c]), __uint_as_float(s[c2][c + 1])), sc2, nl2), x0, x1);
+          p2[c2][c >> 1] = f32x2(fast_exp2(x0), fast_exp2(x1));
+        }
+      // commit j+1 of b_done: dP(j) is there, and dQ(j-1) has consumed the one dS buffer
+      ok = mbar_wait_ok(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
+      tc_fence_after_sync();
+      uint32_t dp[2][32], ds[2][16];
+      tmem_ld32(tmem_lane + kColdP + g * kDqCols, dp[0]);
+      tmem_ld32(tmem_lane + kColdP + g * kDqCols + 32, dp[1]);
+      tmem_wait_ld();
+      if (tiles.full(kt)) {
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            float d0, d1;
+            f32x2_split(mul2(p2[c2][c >> 1], add2(f32x2(__uint_as_float(dp[c2][c]), __uint_as_float(dp[c2][c + 1])), nd2)), d0, d1);
+            ds[c2][c >> 1] = pack_bf16(d0, d1);
+          }
+      } else {
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2) {
+          const int base = kt * kTile + g * kDqCols + c2 * 32;
+          const uint32_t see = bits_below(sink, base) | (bits_below(hi, base) & ~bits_below(lo, base));
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            float d0, d1;
+            f32x2_split(mul2(p2[c2][c >> 1], add2(f32x2(__uint_as_float(dp[c2][c]), __uint_as_float(dp[c2][c + 1])), nd2)), d0, d1);
+            ds[c2][c >> 1] = pack_bf16((see >> c) & 1u ? d0 : 0.f, (see >> (c + 1)) & 1u ? d1 : 0.f);
+          }
+        }
+      }
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2) tmem_st16(tmem_lane + kColdS + g * (kDqCols / 2) + c2 * 16, ds[c2]);
+      tmem_wait_st();
+      tc_fence_before_sync();
+      warp_arrive(rb + j % 4, lane);   // dS(j) stored; dP(j) was read before it, so its buffer is free as well
+      if (!ok) break;
+    }
+    mbar_wait(dq_full, 0, abort_flag);
+    tc_fence_after_sync();
+    const QuadRows rows = quad_rows(a.dq, b, h, a.mask.n, a.heads, D, row);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+      redo = !win_store_row32(tmem_lane + kColdQ + g * (D / 2) + c * 32, a.scale, live, rows, g * (D / 2) + c * 32, lane) || redo;
+  }
+
+  settle_after_abort(abort_flag);
+  tc_fence_before_sync();
+  if (__syncthreads_or(redo) && !*abort_flag) win_careful_dq<D>(a, qt, h, b, warp, lane);
+  if (warp == kMmaWarp) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+// ------------------------------------------------------------------------------------------ dK, dV
+// One row each of dK and dV by the formula: eight lanes per query, four queries at a time.
+template <int D>
+__device__ __noinline__ void win_careful_dkv(const WinBwdArgs& a, int kt, int kvh, int b, int warp, int lane) {
+  constexpr int kPer = D / 8;
+  const int len = a.mask.length(b), part = lane & 7, slot = lane >> 3;
+  for (int r = warp; r < kTile; r += kWinBwdThreads / 32) {
+    const int row = kt * kTile + r;
+    if (row >= len) break;
+    const float scale_log2 = a.scale * kLog2e;
+    const __nv_bfloat16 *kp = a.k + b * a.ks.b + row * a.ks.t + kvh * a.ks.h + part * kPer,
+                        *vp = a.v + b * a.vs.b + row * a.vs.t + kvh * a.vs.h + part * kPer;
+    float dk[kPer], dv[kPer], k[kPer], v[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      dk[e] = dv[e] = 0.f;
+      k[e] = __bfloat162float(kp[e]);
+      v[e] = __bfloat162float(vp[e]);
+    }
+    int first, last;
+    a.mask.queries_of(row, len, first, last);
+    for (int h = kvh * a.group; h < (kvh + 1) * a.group; ++h) {
+      const size_t stat = (static_cast<size_t>(b) * a.heads + h) * a.mask.n;
+      const __nv_bfloat16* qb = a.q + b * a.qs.b + h * a.qs.h + part * kPer;
+      const __nv_bfloat16* gb = a.d_o + (static_cast<size_t>(b) * a.mask.n * a.heads + h) * D + part * kPer;
+      const long long g_row = static_cast<long long>(a.heads) * D;
+      for (int x = first; x < last; x += 4) {
+        const bool there = x + slot < last;
+        const int i = there ? x + slot : last - 1;
+        float s = 0.f, dp = 0.f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          s = fmaf(k[e], __bfloat162float(qb[i * a.qs.t + e]), s);
+          dp = fmaf(v[e], __bfloat162float(gb[i * g_row + e]), dp);
+        }
+#pragma unroll
+        for (int d = 1; d < 8; d *= 2) {
+          s += __shfl_xor_sync(0xffffffffu, s, d);
+          dp += __shfl_xor_sync(0xffffffffu, dp, d);
+        }
+        if (there) {
+          const float p = fast_exp2(s * scale_log2 - a.lse[stat + i] * kLog2e), ds = p * (dp - a.delta[stat + i]);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) {
+            dk[e] = fmaf(ds, __bfloat162float(qb[i * a.qs.t + e]), dk[e]);
+            dv[e] = fmaf(p, __bfloat162float(gb[i * g_row + e]), dv[e]);
+          }
+        }
+      }
+    }
+    const size_t at = ((static_cast<size_t>(b) * a.mask.n + row) * a.kv_heads + kvh) * D + part * kPer;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+#pragma unroll
+      for (int d = 8; d < 32; d *= 2) {
+        dk[e] += __shfl_xor_sync(0xffffffffu, dk[e], d);
+        dv[e] += __shfl_xor_sync(0xffffffffu, dv[e], d);
+      }
+      if (slot == 0) {
+        a.dk[at + e] = __float2bfloat16_rn(dk[e] * a.scale);
+        a.dv[at + e] = __float2bfloat16_rn(dv[e]);
+      }
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap& tm_q, const CUtensorMap& tm_do, const CUtensorMap& tm_k,
+                                            const CUtensorMap& tm_v, const WinBwdArgs& a, const int kt, const int kvh, const int b) {
+  uint8_t* smem = align_1024(smem_raw);
+  uint8_t* sK = smem + DkvSmem<D>::kK;
+  uint8_t* sV = smem + DkvSmem<D>::kV;
+  uint8_t* sQ = smem + DkvSmem<D>::kQ;
+  uint8_t* sdO = smem + DkvSmem<D>::kdO;
+  float* sStat = reinterpret_cast<float*>(smem + DkvSmem<D>::kStats);   // [stage][-LSE*log2e | -delta][128 queries]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + DkvSmem<D>::kBars);
+  uint64_t* kv_full = bars;
+  uint64_t* q_full = bars + 1;
+  uint64_t* q_empty = q_full + kDkvStages;
+  uint64_t* s_full = q_empty + kDkvStages;
+  uint64_t* dp_full = s_full + 1;
+  uint64_t* p_full = dp_full + 1;
+  uint64_t* ds_full = p_full + 1;
+  uint64_t* acc_full = ds_full + 1;
+  uint64_t* landed = acc_full + 1;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(landed + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int k0 = kt * kTile, len = a.mask.length(b);
+  constexpr uint32_t kTmemCols = 512;
+  constexpr uint32_t kColSt = 0, kColdPt = 128, kColdK = 256, kColdV = 384;
+  constexpr int kMmaWarp = 8, kTmaWarp = 9;
+  constexpr int kHalfBytes = 64 * 128;
+  const int g = warp >> 2, r = tid & 127;
+
+  if (k0 >= len) {
+    dependency_wait();
+    if (warp < kMmaWarp) {
+      const QuadRows dk_rows = quad_rows(a.dk, b, kvh, a.mask.n, a.kv_heads, D, k0 + r), dv_rows = quad_rows(a.dv, b, kvh, a.mask.n, a.kv_heads, D, k0 + r);
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        uint4 zero[4] = {};
+        store_quad_rows(zero, dk_rows, g * (D / 2) + c * 32, lane);
+        store_quad_rows(zero, dv_rows, g * (D / 2) + c * 32, lane);
+      }
+    }
+    return;
+  }
+  // the query tiles [t0, t0 + per_head) of every head of the group; full: those within [full_first, full_last)
+  int first, last, full_first, full_last;
+  {
+    const int k_last = min(k0 + kTile, len) - 1;
+    int x, y;
+    a.mask.queries_of(k0, len, first, last);
+    a.mask.queries_of(k_last, len, full_first, y);
+    if (y > last) last = y;
+    full_last = len;
+    if (k_last >= a.mask.sink) a.mask.queries_of(max(k0, a.mask.sink), len, x, full_last);
+  }
+  const int t0 = first / kTile, per_head = (last - 1) / kTile + 1 - t0, n_tiles = per_head * a.group;
+
+  if (tid == 0) {
+    mbar_init(kv_full, 1);
+    for (int i = 0; i < kDkvStages; ++i) { mbar_init(q_full + i, 2); mbar_init(q_empty + i, 1); }
+    mbar_init(s_full, 1);
+    mbar_init(dp_full, 1);
+    mbar_init(p_full, 8);    // one arrival per warp
+    mbar_init(ds_full, 8);
+    mbar_init(acc_full, 1);
+    mbar_init(landed, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(tmem_holder, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_holder;
+  bool redo = false;
+
+  if (warp == kTmaWarp) {
+    if (lane == 0) {
+      mbar_arrive_expect_tx(kv_full, 2 * TileGeom<D>::kBytes);
+      tma_load_tile<D>(sK, &tm_k, kv_full, k0, kvh, b);
+      tma_load_tile<D>(sV, &tm_v, kv_full, k0, kvh, b);
+    }
+    dependency_wait();   // delta
+    int h = kvh * a.group, qt = t0, fixes = 0;
+    for (int i = 0; i < n_tiles; ++i) {
+      const int st = i % kDkvStages;
+      if (!mbar_wait_ok(q_empty + st, ((i / kDkvStages) & 1) ^ 1, abort_flag)) break;   // no copies once a wait has run out
+      uint8_t *q_dst = sQ + st * TileGeom<D>::kBytes, *do_dst = sdO + st * TileGeom<D>::kBytes;
+      const bool straddles = qt * kTile + kTile > len && len < a.mask.n;   // rows of Q and dO behind the end are cleared: 0 * NaN
+      uint64_t* bar = straddles ? landed : q_full + st;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(bar, 2 * TileGeom<D>::kBytes);
+        tma_load_tile<D>(q_dst, &tm_q, bar, qt * kTile, h, b);
+        tma_load_tile<D>(do_dst, &tm_do, bar, qt * kTile, h, b);
+      }
+      const size_t stat_base = (static_cast<size_t>(b) * a.heads + h) * a.mask.n;
+      float* stat = sStat + st * 2 * kTile;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int qi = qt * kTile + lane * 4 + e;
+        stat[lane * 4 + e] = qi < len ? -a.lse[stat_base + qi] * kLog2e : -INFINITY;
+        stat[kTile + lane * 4 + e] = qi < len ? -a.delta[stat_base + qi] : 0.f;
+      }
+      if (straddles) {
+        if (!mbar_wait_ok(landed, fixes & 1, abort_flag)) break;
+        ++fixes;
+        zero_rows_by_warp<D>(q_dst, len - qt * kTile, lane);
+        zero_rows_by_warp<D>(do_dst, len - qt * kTile, lane);
+        if (lane == 0) mbar_arrive(q_full + st);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full + st);
+      if (++qt == t0 + per_head) { qt = t0; ++h; }
+    }
+  } else if (warp == kMmaWarp) {
+    if (lane == 0) {
+      auto q_tile = [&](int i) { return smem_u32(sQ + (i % kDkvStages) * TileGeom<D>::kBytes); };
+      auto do_tile = [&](int i) { return smem_u32(sdO + (i % kDkvStages) * TileGeom<D>::kBytes); };
+      // once a wait has run out no more MMAs are issued: their operands may never have been loaded
+      bool ok = true;
+      auto wait_q = [&](int i) {
+        ok = ok && mbar_wait_spin(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
+        tc_fence_after_sync();
+      };
+      ok = mbar_wait_spin(kv_full, 0, abort_flag);
+      wait_q(0);
+      if (ok) {
+        mma_abT<D>(tmem_base + kColSt, smem_u32(sK), q_tile(0));
+        mma_commit(s_full);
+        mma_abT<D>(tmem_base + kColdPt, smem_u32(sV), do_tile(0));
+        mma_commit(dp_full);
+      }
+      for (int i = 0; ok && i < n_tiles; ++i) {
+        if (!mbar_wait_spin(p_full, i & 1, abort_flag)) break;
+        tc_fence_after_sync();
+        mma_pb<D, 64>(tmem_base + kColdV, tmem_base + kColSt, do_tile(i), i > 0);
+        mma_pb<D, 64>(tmem_base + kColdV, tmem_base + kColSt + 64, do_tile(i) + kHalfBytes, true);
+        if (i + 1 < n_tiles) {
+          wait_q(i + 1);
+          if (!ok) break;
+          mma_abT<D>(tmem_base + kColSt, smem_u32(sK), q_tile(i + 1));
+          mma_commit(s_full);
+        }
+        if (!mbar_wait_spin(ds_full, i & 1, abort_flag)) break;
+        tc_fence_after_sync();
+        mma_pb<D, 64>(tmem_base + kColdK, tmem_base + kColdPt, q_tile(i), i > 0);
+        mma_pb<D, 64>(tmem_base + kColdK, tmem_base + kColdPt + 64, q_tile(i) + kHalfBytes, true);
+        mma_commit(q_empty + i % kDkvStages);
+        if (i + 1 < n_tiles) {
+          mma_abT<D>(tmem_base + kColdPt, smem_u32(sV), do_tile(i + 1));
+          mma_commit(dp_full);
+        }
+      }
+      mma_commit(acc_full);
+    }
+  } else {
+    const uint32_t tmem_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const float scale_log2 = a.scale * kLog2e;
+    const uint64_t sc2 = f32x2(scale_log2, scale_log2);
+    const int key = k0 + r;
+    const bool live = key < len;
+    int q_first = 0, q_last = 0;
+    if (live) a.mask.queries_of(key, len, q_first, q_last);
+    int qt = t0;
+    for (int i = 0; i < n_tiles; ++i) {
+      const float* stat = sStat + (i % kDkvStages) * 2 * kTile + g * 64;
+      const bool full = qt * kTile >= full_first && qt * kTile + kTile <= full_last;
+      uint32_t see[2];
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2) {
+        const int base = qt * kTile + g * 64 + c2 * 32;
+        see[c2] = full ? 0xffffffffu : bits_below(q_last, base) & ~bits_below(q_first, base);
+      }
+      if (++qt == t0 + per_head) qt = t0;
+      bool ok = mbar_wait_ok(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
+      ok = mbar_wait_ok(s_full, i & 1, abort_flag) && ok;
+      if (!ok) break;
+      tc_fence_after_sync();
+      uint32_t s[2][32], pt[32];
+      tmem_ld32(tmem_lane + kColSt + g * 64, s[0]);
+      tmem_ld32(tmem_lane + kColSt + g * 64 + 32, s[1]);
+      tmem_wait_ld();
+      uint64_t p2[2][16];
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          const uint64_t nl2 = *reinterpret_cast<const uint64_t*>(stat + c2 * 32 + c);
+          const uint64_t x2 = fma2(f32x2(__uint_as_float(s[c2][c]), __uint_as_float(s[c2][c + 1])), sc2, nl2);
+          float p0, p1;
+          if (((c >> 1) & 7) < kDkvPolyOf8) {
+            exp2_poly_pair(x2, p0, p1);
+          } else {
+            float x0, x1;
+            f32x2_split(x2, x0, x1);
+            p0 = fast_exp2(x0);
+            p1 = fast_exp2(x1);
+          }
+          p2[c2][c >> 1] = f32x2(p0, p1);
+          pt[c2 * 16 + (c >> 1)] = pack_bf16(p0, p1);
+        }
+      if (!full) {
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            const uint32_t keep = ((see[c2] >> c) & 1u ? 0x0000ffffu : 0u) | ((see[c2] >> (c + 1)) & 1u ? 0xffff0000u : 0u);
+            pt[c2 * 16 + (c >> 1)] &= keep;
+          }
+      }
+      tmem_st32(tmem_lane + kColSt + g * 64, pt);
+      tmem_wait_st();
+      tc_fence_before_sync();
+      warp_arrive(p_full, lane);
+
+      if (!mbar_wait_ok(dp_full, i & 1, abort_flag)) break;
+      tc_fence_after_sync();
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2) {
+        uint32_t dp[32], ds[16];
+        tmem_ld32(tmem_lane + kColdPt + g * 64 + c2 * 32, dp);
+        tmem_wait_ld();
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          const uint64_t nd2 = *reinterpret_cast<const uint64_t*>(stat + kTile + c2 * 32 + c);
+          const uint64_t d2 = mul2(p2[c2][c >> 1], add2(f32x2(__uint_as_float(dp[c]), __uint_as_float(dp[c + 1])), nd2));
+          float d0, d1;
+          f32x2_split(d2, d0, d1);
+          ds[c >> 1] = pack_bf16(d0, d1);
+        }
+        if (!full) {
+#pragma unroll
+          for (int c = 0; c < 32; c += 2)
+            ds[c >> 1] &= ((see[c2] >> c) & 1u ? 0x0000ffffu : 0u) | ((see[c2] >> (c + 1)) & 1u ? 0xffff0000u : 0u);
+        }
+        tmem_st16(tmem_lane + kColdPt + g * 64 + c2 * 16, ds);
+      }
+      tmem_wait_st();
+      tc_fence_before_sync();
+      warp_arrive(ds_full, lane);
+    }
+    mbar_wait(acc_full, 0, abort_flag);
+    tc_fence_after_sync();
+    const QuadRows dk_rows = quad_rows(a.dk, b, kvh, a.mask.n, a.kv_heads, D, key), dv_rows = quad_rows(a.dv, b, kvh, a.mask.n, a.kv_heads, D, key);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const int col = g * (D / 2) + c * 32;
+      redo = !win_store_row32(tmem_lane + kColdK + col, a.scale, live, dk_rows, col, lane) || redo;
+      redo = !win_store_row32(tmem_lane + kColdV + col, 1.f, live, dv_rows, col, lane) || redo;
+    }
+  }
+
+  settle_after_abort(abort_flag);
+  tc_fence_before_sync();
+  if (__syncthreads_or(redo) && !*abort_flag) win_careful_dkv<D>(a, kt, kvh, b, warp, lane);
+  if (warp == kMmaWarp) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kWinBwdThreads, 1)
+window_attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do,
+                       const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                       const __grid_constant__ WinBwdArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  int i = blockIdx.x;
+  if (i < a.lists * a.tiles) {   // query tiles backwards: the later ones see more keys
+    const int back = i / a.lists, bh = i - back * a.lists;
+    win_bwd_dq<D>(smem_raw, tm_k, tm_v, tm_do, a, a.tiles - 1 - back, bh % a.heads, bh / a.heads);
+  } else {                       // key tiles forwards: the sinks are seen by every query
+    i -= a.lists * a.tiles;
+    const int kt = i / a.kv_lists, bh = i - kt * a.kv_lists;
+    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, kt, bh % a.kv_heads, bh / a.kv_heads);
+  }
+}
+template <int D> constexpr int window_bwd_smem() {
+  return DqSmem<D>::kTotal > DkvSmem<D>::kTotal ? DqSmem<D>::kTotal : DkvSmem<D>::kTotal;
+}
+
+}  // namespace astro

@@ -1,0 +1,101 @@
+// Attention of whole sequences in which a query sees its own block of tokens, a window in front of it and the first tokens
+// (sinks): what the kernels share about who sees whom.
+//
+// With c = i / block, query i sees key j < len iff j < min(len, (c+1) block) and (j < sink or j >= (c+1) block - window).
+// window >= block, so every query sees itself.  Queries from len on see nothing.
+//
+// Queries and keys are cut into tiles of 128 on one grid.  A query tile's keys are the tiles [0, a1) of the sinks and [w0, w1)
+// of the window (a1 = w0 = 0 where they meet); its own tile, the diagonal one, lies in the second.  A pair of tiles is full when every
+// live row sees every key; the others are masked bit by bit.
+#pragma once
+#include "attn_common.cuh"
+
+namespace astro {
+
+struct WinMask {
+  int n, block, window, sink;   // block <= n, window <= n + block, sink <= n
+  const int* lengths;           // may be null: n each
+  __host__ __device__ __forceinline__ int length(int b) const { return lengths == nullptr ? n : max(0, min(n, lengths[b])); }
+  // the keys of query i of a sequence of `len`: [0, sink) below hi, and [lo, hi)
+  __host__ __device__ __forceinline__ void keys_of(int i, int len, int& lo, int& hi) const {
+    const int end = (i / block + 1) * block;
+    lo = max(0, end - window);
+    hi = min(len, end);
+  }
+  // the queries of key j: [first, last)
+  __host__ __device__ __forceinline__ void queries_of(int j, int len, int& first, int& last) const {
+    first = j / block * block;
+    last = j < sink ? len : min(len, (j + window) / block * block);
+  }
+};
+
+// 32 columns from `base` on: the bits of those below `end` (or all, or none).
+__host__ __device__ __forceinline__ uint32_t bits_below(int end, int base) {
+  const int x = end - base;
+  return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u;
+}
+
+// The key tiles of a query tile.
+struct WinTiles {
+  int a1, w0, w1;        // [0, a1) and [w0, w1)
+  int full_sink, full_lo, full_hi;   // full: tiles below full_sink, and [full_lo, full_hi)
+  // a query tile that starts at row i0 < len
+  __host__ __device__ __forceinline__ void set(const WinMask& m, int i0, int len) {
+    int lo_min, lo_max, hi_min, hi_max;
+    m.keys_of(i0, len, lo_min, hi_min);
+    m.keys_of(min(i0 + kTile, len) - 1, len, lo_max, hi_max);
+    w0 = lo_min / kTile;
+    w1 = (hi_max + kTile - 1) / kTile;
+    a1 = (min(m.sink, hi_max) + kTile - 1) / kTile;
+    if (a1 >= w0) a1 = w0 = 0;
+    const int sink_min = min(m.sink, hi_min);
+    full_sink = sink_min / kTile;
+    full_lo = lo_max <= sink_min ? 0 : (lo_max + kTile - 1) / kTile;
+    full_hi = hi_min / kTile;
+  }
+  __host__ __device__ __forceinline__ void set_dead(int tile) {   // one tile, of which nothing is seen
+    a1 = 0;
+    w0 = tile;
+    w1 = tile + 1;
+    full_sink = full_lo = full_hi = 0;
+  }
+  __host__ __device__ __forceinline__ int count() const { return a1 + w1 - w0; }
+  __host__ __device__ __forceinline__ int first() const { return a1 > 0 ? 0 : w0; }
+  __host__ __device__ __forceinline__ int next(int tile) const { return tile + 1 == a1 ? w0 : tile + 1; }   // from w1 on: none left
+  __host__ __device__ __forceinline__ bool full(int tile) const { return tile < full_sink || (tile >= full_lo && tile < full_hi); }
+  // where the run of full tiles that `tile` is in ends
+  __host__ __device__ __forceinline__ int run_end(int tile) const {
+    int e = full_hi;
+    if (tile < full_sink && !(full_lo <= full_sink && full_hi > full_sink)) e = full_sink;
+    return tile < a1 ? min(e, a1) : min(e, w1);
+  }
+};
+
+struct WinStrides {
+  long long b, t, h;     // in elements
+};
+
+// The four rows of a lane's quad in a strided tensor (see QuadRows).
+__device__ __forceinline__ QuadRows quad_rows_strided(const __nv_bfloat16* base, const WinStrides& s, int b, int h, int n_rows,
+                                                      int own_row) {
+  QuadRows q;
+  const int row_first = own_row & ~3;
+  q.stride = static_cast<size_t>(s.t);
+  q.first = const_cast<__nv_bfloat16*>(base) + b * s.b + row_first * s.t + h * s.h;
+  q.valid = n_rows - row_first;
+  return q;
+}
+
+// Rows [first_row, 128) of a tile that a bulk copy has brought become zeros.  A whole warp, behind its wait for the copy.
+template <int D>
+__device__ __forceinline__ void zero_rows_by_warp(uint8_t* smem_tile, int first_row, int lane) {
+  const int pieces = (kTile - first_row) * 8 * TileGeom<D>::kBlocks;
+  for (int i = lane; i < pieces; i += 32) {
+    const int blk = i % TileGeom<D>::kBlocks, x = i / TileGeom<D>::kBlocks;
+    *reinterpret_cast<uint4*>(smem_tile + blk * TileGeom<D>::kBlockBytes + first_row * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+
+}  // namespace astro
