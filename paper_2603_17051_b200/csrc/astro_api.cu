@@ -369,6 +369,24 @@ astro_status_t launch_bwd_dkv(const AttnArgs& a, const CUtensorMap& tq, const CU
   return launch_status();
 }
 
+// delta for the backwards of the 8-bit cache and of whole sequences: the preparation kernel of the chosen blocks' backward, without lists.
+// Its dependents may start at once.
+template <int D>
+astro_status_t launch_delta(const void* o, const void* d_o, int batch, int heads, int n_q, float* delta, cudaStream_t st) {
+  SparsePrepArgs p;
+  std::memset(&p, 0, sizeof(p));
+  p.o = static_cast<const __nv_bfloat16*>(o);
+  p.d_o = static_cast<const __nv_bfloat16*>(d_o);
+  p.delta = delta;
+  p.rows = static_cast<long long>(batch) * n_q * heads;
+  p.heads = heads;
+  p.n_q = n_q;
+  const long long per_block = static_cast<long long>(kPrepThreads) * 8 / D * kDeltaRows, blocks = (p.rows + per_block - 1) / per_block;
+  if (blocks > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
+  sparse_bwd_prep_kernel<D><<<static_cast<unsigned>(blocks), kPrepThreads, 0, st>>>(p);
+  return launch_status();
+}
+
 // Copies frames between a caller tensor and the storage slots listed in `slots` (logical order).
 template <bool ToCache>
 astro_status_t launch_ring_copy(const astro_kvcache* c, void* k_user, void* v_user, const int* slots, int n_frames,
@@ -840,14 +858,29 @@ constexpr int kFewMaxQueries = 64;
 
 int held_tokens(const astro_kvcache* c) { return c ? (c->sink_held + c->win_held) * c->d.tokens_per_frame : 0; }
 
-// CTAs (one per SM) that share a list of keys: as many as fill a B200's 148 SMs once, each with two steps of every warp at least.
-int few_splits(int batch, int heads, int n_q, long long keys) {
-  const int per_cta = n_q <= 8 ? 8 : 16;
-  const long long units = static_cast<long long>(batch) * heads * ((n_q - 1) / per_cta + 1);
-  const long long most = keys / (2 * kFewStep * (128 / per_cta)) + 1;
-  long long want = 148 / units;
-  if (want > most) want = most;
-  return want < 1 ? 1 : static_cast<int>(want);
+// How the kernel for few queries divides its work: the queries of a list (those of every sample over one prefix) into tiles of
+// 8 or 16, and the keys of a list among `splits` CTAs.  One CTA runs on an SM; with `units` lists and tiles, splits CTAs each
+// take ceil(units * splits / 148) rounds of a share of the steps, a CTA's start and end being worth about 40 steps of 16 keys.
+struct FewSplit {
+  int rows, per_tile, tiles, splits;
+  long long lists;
+};
+FewSplit few_split(const astro_kvcache* cache, int batch, int heads, int n_q, int n_kc) {
+  constexpr int kSms = 148;
+  FewSplit f;
+  const bool shared = cache && cache->d.cache_batch == 1 && batch > 1;
+  f.rows = shared ? batch * n_q : n_q;     // n_q is kFewMaxQueries at most
+  f.per_tile = f.rows <= 8 ? 8 : 16;
+  f.tiles = (f.rows - 1) / f.per_tile + 1;
+  f.lists = static_cast<long long>(shared ? 1 : batch) * heads;
+  const long long units = f.lists * f.tiles, steps = (static_cast<long long>(held_tokens(cache)) + n_kc) / kFewStep + 1;
+  f.splits = 1;
+  long long least = 0;
+  for (int i = 1; i <= 148 && (i == 1 || steps / i >= 2 * 128 / f.per_tile); ++i) {   // two steps for every warp
+    const long long cost = (units * i + kSms - 1) / kSms * ((steps + i - 1) / i + 40);
+    if (i == 1 || cost < least) { f.splits = i; least = cost; }
+  }
+  return f;
 }
 
 struct Attn8Call {
@@ -880,17 +913,18 @@ astro_status_t launch_few(const Attn8Call& c, float scale, void* o, float* lse, 
     f.count0 = segs.count[0];
     f.start1 = segs.n > 1 ? segs.start[1] : 0;
   }
+  const FewSplit split = few_split(c.a.cache, c.a.batch, c.a.heads, c.a.n_q, c.a.n_kc);
   f.batch = c.a.batch; f.heads = c.a.heads; f.n_q = c.a.n_q;
-  f.q_tiles = (c.a.n_q - 1) / (8 * NT) + 1;
-  f.cache_shared = c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1 ? 1 : 0;
-  f.splits = few_splits(c.a.batch, c.a.heads, c.a.n_q, static_cast<long long>(f.n_ctx) + f.n_kc);
+  f.shared = c.a.cache && c.a.cache->d.cache_batch == 1 && c.a.batch > 1 ? 1 : 0;
+  f.rows = split.rows;
+  f.splits = split.splits;
   f.scale_log2 = scale * kLog2e;
   const long long rows = static_cast<long long>(c.a.batch) * c.a.heads * c.a.n_q;
   if (f.splits > 1) {
     f.part_o = static_cast<float*>(workspace);
     f.part_lse = f.part_o + f.splits * rows * D;
   }
-  const dim3 grid(static_cast<unsigned>(f.q_tiles * f.splits), f.cache_shared ? c.a.batch : c.a.heads, f.cache_shared ? c.a.heads : c.a.batch);
+  const dim3 grid(static_cast<unsigned>(split.tiles * f.splits), c.a.heads, f.shared ? 1 : c.a.batch);
   attn8_few_kernel<D, NT><<<grid, S::kThreads, kSmem, st>>>(f);
   if ((s = launch_status()) != ASTRO_OK || f.splits == 1) return s;
   return launch_dependent(sparse_combine_kernel<D>, dim3(static_cast<unsigned>((rows + 7) / 8)), 256, 0, st, f.part_o, f.part_lse,
@@ -1074,7 +1108,9 @@ astro_status_t launch_window_bwd(const WindowCall& c, const void* o, const float
   a.kv_lists = d.batch * d.kv_heads;
   a.tiles = (d.n_tokens + kTile - 1) / kTile;
   a.scale = scale;
-  if ((s = launch_bwd_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, static_cast<float*>(workspace), st)) != ASTRO_OK) return s;
+  // the key tiles of the sinks first where they are seen by far more queries than others: they would end last
+  a.front = a.mask.window < d.n_tokens ? (a.mask.sink + kTile - 1) / kTile : 0;
+  if ((s = launch_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, static_cast<float*>(workspace), st)) != ASTRO_OK) return s;
   return launch_dependent(window_attn_bwd_kernel<D>, dim3(static_cast<unsigned>(a.lists + a.kv_lists) * a.tiles), kWinBwdThreads,
                           window_bwd_smem<D>(), st, tq, tdo, tk, tv, a);
 }
@@ -1812,7 +1848,7 @@ astro_status_t astro_kvcache8_read(const astro_kvcache_t* c, int first_frame, in
 size_t astro_chunk_attn8_fwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
   if (check_attn_args(AttnArgs{cache, batch, heads, head_dim, n_q, n_kc}, 1.f, 8) != ASTRO_OK) return 0;
   if (n_q > kFewMaxQueries) return 2 * expanded_bytes(cache);
-  const int splits = few_splits(batch, heads, n_q, static_cast<long long>(held_tokens(cache)) + n_kc);
+  const int splits = few_split(cache, batch, heads, n_q, n_kc).splits;
   return splits == 1 ? 0 : static_cast<size_t>(splits) * batch * heads * n_q * (head_dim + 1) * sizeof(float);
 }
 
@@ -1832,9 +1868,9 @@ astro_status_t astro_chunk_attn8_fwd(const astro_kvcache_t* cache, const void* q
   if ((s = check_arch()) != ASTRO_OK) return s;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (n_q <= kFewMaxQueries) {
-    if (head_dim == 128)
-      return n_q <= 8 ? launch_few<128, 1>(c, scale, o, lse, workspace, st) : launch_few<128, 2>(c, scale, o, lse, workspace, st);
-    return n_q <= 8 ? launch_few<64, 1>(c, scale, o, lse, workspace, st) : launch_few<64, 2>(c, scale, o, lse, workspace, st);
+    const bool eight = few_split(cache, batch, heads, n_q, n_kc).per_tile == 8;
+    if (head_dim == 128) return eight ? launch_few<128, 1>(c, scale, o, lse, workspace, st) : launch_few<128, 2>(c, scale, o, lse, workspace, st);
+    return eight ? launch_few<64, 1>(c, scale, o, lse, workspace, st) : launch_few<64, 2>(c, scale, o, lse, workspace, st);
   }
   CUtensorMap tkc, tvc;
   std::memset(&tkc, 0, sizeof(tkc)); std::memset(&tvc, 0, sizeof(tvc));
@@ -1879,7 +1915,8 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
     if ((s = make_tmap_user(&tvc, v_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
   }
   float* delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * expanded_bytes(cache));
-  if ((s = astro_chunk_attn_bwd_delta(o, d_o, batch, heads, head_dim, n_q, delta, stream)) != ASTRO_OK) return s;
+  s = head_dim == 128 ? launch_delta<128>(o, d_o, batch, heads, n_q, delta, st) : launch_delta<64>(o, d_o, batch, heads, n_q, delta, st);
+  if (s != ASTRO_OK) return s;
   Expanded x;
   if ((s = expand_context(c, workspace, &x, st)) != ASTRO_OK) return s;
   const CUtensorMap tkx[2] = {x.k, x.k};

@@ -43,26 +43,55 @@ struct QuantTensors {
   int heads, tokens_per_frame, n_tokens;
 };
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 2) {
-      float2 f;
-      if constexpr (std::is_same<T, __half>::value) f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      else f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-      x[2 * i] = f.x;
-      x[2 * i + 1] = f.y;
-    } else {
-      x[i] = __uint_as_float(w[i]);
+// 8 neighbouring elements as they come, and in fp32.
+template <typename T> struct Raw8 {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* p) {
+    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    if constexpr (sizeof(T) == 4) {
+      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+      w[4] = u.x; w[5] = u.y; w[6] = u.z; w[7] = u.w;
     }
   }
-  if constexpr (sizeof(T) == 4) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p + 4);
-    x[4] = __uint_as_float(u.x); x[5] = __uint_as_float(u.y); x[6] = __uint_as_float(u.z); x[7] = __uint_as_float(u.w);
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 2 * static_cast<int>(sizeof(T)); ++i) w[i] = 0;
   }
-}
+  __device__ __forceinline__ float2 pair(int i) const {
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    else if constexpr (std::is_same<T, __half>::value) return __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    else return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  // The largest magnitude's bits as those of a float, infinities and NaN left out.
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+    if constexpr (sizeof(T) == 2) {
+      constexpr bool kHalf = std::is_same<T, __half>::value;
+      constexpr uint32_t kInf = kHalf ? 0x7c00u : 0x7f80u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);   // magnitudes are ordered like their bits
+      m = max(m >> 16, m & 0xffffu);
+      if (m >= kInf) {                                  // rare
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t x = (w[i / 2] >> (16 * (i & 1))) & 0x7fffu;
+          m = max(m, x < kInf ? x : 0u);
+        }
+      }
+      if constexpr (kHalf) return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(m))));
+      else return m << 16;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t x = w[i] & 0x7fffffffu;
+        m = max(m, x < 0x7f800000u ? x : 0u);
+      }
+      return m;
+    }
+  }
+};
 template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -102,12 +131,30 @@ __device__ __forceinline__ float2 e4m3_to_floats(uint32_t codes) {
 // 2^e of a stored exponent byte (3..247): its own exponent field.
 __device__ __forceinline__ float exp_byte_to_float(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// The lanes of a row each hold a value for every token; afterwards lane x holds the maximum over them for token x % kQuantTokens:
+// they halve the tokens among themselves step by step instead of every lane learning every token's.
+template <int kLanes>
+__device__ __forceinline__ uint32_t max_per_token(uint32_t (&v)[kQuantTokens], int lane) {
+  static_assert(kQuantTokens == 8 && (kLanes == 8 || kLanes == 16), "three halvings, and one more step over 16 lanes");
+#pragma unroll
+  for (int half = 4; half > 0; half /= 2) {
+    const bool upper = lane & half;
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const uint32_t give = upper ? v[i] : v[i + half], keep = upper ? v[i + half] : v[i];
+      v[i] = max(keep, __shfl_xor_sync(0xffffffffu, give, half));
+    }
+  }
+  if constexpr (kLanes == 16) v[0] = max(v[0], __shfl_xor_sync(0xffffffffu, v[0], 8));
+  return v[0];
+}
+
 // grid.x: token chunks, grid.y: head * D/8 positions, grid.z = 2 * b + (0: K, 1: V).  Lanes without a position stay for the
 // shuffles.
 template <typename T, int D>
 __global__ void __launch_bounds__(kQuantThreads) cache8_append_kernel(const QuantTensors x, const FrameSlots slots) {
   constexpr int kLanes = D / 8;                         // lanes of a row
-  const int hv = blockIdx.y * blockDim.x + threadIdx.x;
+  const int hv = blockIdx.y * blockDim.x + threadIdx.x, lane = threadIdx.x & 31;
   const bool there = hv < x.heads * kLanes;
   const int h = there ? hv / kLanes : 0, part = hv % kLanes;
   const int b = blockIdx.z >> 1;
@@ -115,34 +162,36 @@ __global__ void __launch_bounds__(kQuantThreads) cache8_append_kernel(const Quan
   const int t0 = blockIdx.x * kQuantTokens;
   const int n = there ? min(kQuantTokens, x.n_tokens - t0) : 0;
   const T* src = static_cast<const T*>(is_v ? x.v : x.k) + b * x.in_b + t0 * x.in_t + h * x.in_h + part * 8;
-  float f[kQuantTokens][8];
+  Raw8<T> f[kQuantTokens];
 #pragma unroll
   for (int i = 0; i < kQuantTokens; ++i) {
-    if (i < n) {
-      load8(src + i * x.in_t, f[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[i][e] = 0.f;
-    }
+    if (i < n) f[i].load(src + i * x.in_t);
+    else f[i].clear();
   }
   const long long row_base = (static_cast<long long>(b) * x.heads + h) * x.slot_tokens;
   uint8_t* codes = is_v ? x.v_store : x.k_store;
   uint8_t* exps = is_v ? x.v_exp : x.k_exp;
-  int frame = t0 / x.tokens_per_frame, in_frame = t0 - frame * x.tokens_per_frame;
-  long long slot_row = row_base + static_cast<long long>(slots.slot(frame)) * x.tokens_per_frame;
+  int frame = t0 / x.tokens_per_frame;
+  const int in_frame = t0 - frame * x.tokens_per_frame;
+  // where token i of these goes; most often all of them are in one frame
+  const long long row0 = row_base + static_cast<long long>(slots.slot(frame)) * x.tokens_per_frame + in_frame;
+  const bool one_frame = in_frame + kQuantTokens <= x.tokens_per_frame;
+  auto row_of = [&](int i) -> long long {
+    if (one_frame) return row0 + i;
+    const int fr = (t0 + i) / x.tokens_per_frame;
+    return row_base + static_cast<long long>(slots.slot(fr)) * x.tokens_per_frame + (t0 + i - fr * x.tokens_per_frame);
+  };
+  uint32_t tops[kQuantTokens];
+#pragma unroll
+  for (int i = 0; i < kQuantTokens; ++i) tops[i] = f[i].top();
+  const uint32_t top = max_per_token<kLanes>(tops, lane);
+  // top = 1.f * 2^k <= 1.75 * 2^(e + 8)
+  const int k = static_cast<int>(top >> 23) - 127;
+  const int my_e = max(kQuantLowestExp, k - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0));
+  if (part < kQuantTokens && part < n) exps[row_of(part)] = static_cast<uint8_t>(my_e + 127);
 #pragma unroll
   for (int i = 0; i < kQuantTokens; ++i) {
-    uint32_t top = 0;                                   // bits of the largest finite magnitude: ordered like the numbers
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t m = __float_as_uint(f[i][e]) & 0x7fffffffu;
-      top = max(top, m < 0x7f800000u ? m : 0u);
-    }
-#pragma unroll
-    for (int s = kLanes / 2; s > 0; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-    // top = 1.f * 2^k <= 1.75 * 2^(e + 8)
-    const int k = static_cast<int>(top >> 23) - 127;
-    const int e = max(kQuantLowestExp, k - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0));
+    const int e = __shfl_sync(0xffffffffu, my_e, (lane & ~(kLanes - 1)) + i);
     const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // 2^-e: -e is 124 at most, -120 at least
     const float most = e == 120 ? 240.f : 448.f;
     uint32_t w[2];
@@ -150,21 +199,15 @@ __global__ void __launch_bounds__(kQuantThreads) cache8_append_kernel(const Quan
     for (int p = 0; p < 2; ++p) {
       float y[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const float v = f[i][4 * p + c];
-        y[c] = fabsf(v) < INFINITY ? fminf(fmaxf(v * inv, -most), most) : __uint_as_float(0x7fffffffu);
+      for (int c = 0; c < 2; ++c) {
+        const float2 v = f[i].pair(2 * p + c);
+        // an infinity becomes NaN (0 * infinity), a finite number is left as it is
+        y[2 * c] = fminf(fmaxf(v.x * inv, -most), most) + 0.f * v.x;
+        y[2 * c + 1] = fminf(fmaxf(v.y * inv, -most), most) + 0.f * v.y;
       }
       w[p] = e4m3_pair(y[0], y[1]) | e4m3_pair(y[2], y[3]) << 16;
     }
-    if (i < n) {
-      const long long row = slot_row + in_frame;
-      *reinterpret_cast<uint2*>(codes + row * D + part * 8) = make_uint2(w[0], w[1]);
-      if (part == 0) exps[row] = static_cast<uint8_t>(e + 127);
-      if (++in_frame == x.tokens_per_frame) {
-        in_frame = 0;
-        slot_row = row_base + static_cast<long long>(slots.slot(++frame)) * x.tokens_per_frame;
-      }
-    }
+    if (i < n) *reinterpret_cast<uint2*>(codes + row_of(i) * D + part * 8) = make_uint2(w[0], w[1]);
   }
 }
 

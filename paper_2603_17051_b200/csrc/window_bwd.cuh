@@ -3,8 +3,8 @@
 //   dK/dV  a key tile stationary, over the query tiles of all the heads that share it and see it:
 //          dV = sum P^T dO, dK = scale * sum dS^T Q
 // with P = exp(S - LSE), dS = P o (dP - delta), as in the dense kernels (attn_bwd.cuh), whose tensor-memory layouts, operand
-// forms and hand-offs these two have: see there.  Both in one launch, a CTA per tile, the query tiles first; within each the long
-// ones come first.  Tiles of which a row sees only a part are masked bit by bit, P and dS by selection, so that what a masked
+// forms and hand-offs these two have: see there.  Both in one launch, a CTA per tile, the long ones first (of the key tiles
+// those of the sinks, which every query sees; then the query tiles; then the other key tiles).  Tiles of which a row sees only a part are masked bit by bit, P and dS by selection, so that what a masked
 // place holds, NaN included, ends there; rows behind a sequence's end are cleared in shared memory where they are operands.
 // Inside a sequence a NaN or infinity in K, Q or dO would still reach the rows of a masked tile that do not see it (0 * NaN):
 // a tile whose gradients are not finite is done again by the formula, on the ordinary cores (slow and rare).
@@ -25,6 +25,7 @@ struct WinBwdArgs {
   __nv_bfloat16 *dq, *dk, *dv;    // [B, n, H or KVH, D]
   WinMask mask;
   int heads, kv_heads, group, lists, kv_lists, tiles;   // lists = batch * heads, kv_lists = batch * kv_heads
+  int front;                      // key tiles whose CTAs come before the query tiles'
   float scale;
 };
 constexpr int kWinBwdThreads = kDqSoftmaxThreads + 64;   // MMA, loads
@@ -667,12 +668,13 @@ window_attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                        const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                        const __grid_constant__ WinBwdArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  int i = blockIdx.x;
-  if (i < a.lists * a.tiles) {   // query tiles backwards: the later ones see more keys
+  // key tiles forwards (the earlier ones are seen by more queries), query tiles backwards (the later ones see more keys)
+  int i = blockIdx.x - a.front * a.kv_lists;
+  if (i >= 0 && i < a.lists * a.tiles) {
     const int back = i / a.lists, bh = i - back * a.lists;
     win_bwd_dq<D>(smem_raw, tm_k, tm_v, tm_do, a, a.tiles - 1 - back, bh % a.heads, bh / a.heads);
-  } else {                       // key tiles forwards: the sinks are seen by every query
-    i -= a.lists * a.tiles;
+  } else {
+    i = i < 0 ? blockIdx.x : blockIdx.x - a.lists * a.tiles;
     const int kt = i / a.kv_lists, bh = i - kt * a.kv_lists;
     win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, kt, bh % a.kv_heads, bh / a.kv_heads);
   }

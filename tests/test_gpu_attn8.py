@@ -155,7 +155,8 @@ def test_layer_size(shape):
     got, ref = (f(c, q, kc, vc, o, lse, d_o, 128 ** -0.5) for f, c in ((A.astro_chunk_attn8_bwd, cache), (A.astro_chunk_attn_bwd, dense)))
     for a, r in zip(got, ref):
         assert (a.float() - r.float()).norm() <= 2.0 ** -8 * r.float().norm()
-    assert torch.equal(got[1], ref[1]) and torch.equal(got[2], ref[2])
+    # dV is the same sum; in dK the fp32 sum delta runs in another order (2^-20 of its terms), which may turn single roundings of dS by a step
+    assert torch.equal(got[2], ref[2])
 
 
 def test_a_captured_call_and_one_on_another_stream():
