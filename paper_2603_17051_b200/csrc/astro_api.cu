@@ -860,7 +860,7 @@ int held_tokens(const astro_kvcache* c) { return c ? (c->sink_held + c->win_held
 
 // How the kernel for few queries divides its work: the queries of a list (those of every sample over one prefix) into tiles of
 // 8 or 16, and the keys of a list among `splits` CTAs.  One CTA runs on an SM; with `units` lists and tiles, splits CTAs each
-// take ceil(units * splits / 148) rounds of a share of the steps, a CTA's start and end being worth about 40 steps of 16 keys.
+// take ceil(units * splits / 148) rounds of a share of the steps, a CTA's start and end being worth about 20 steps of 32 keys.
 struct FewSplit {
   int rows, per_tile, tiles, splits;
   long long lists;
@@ -874,10 +874,11 @@ FewSplit few_split(const astro_kvcache* cache, int batch, int heads, int n_q, in
   f.tiles = (f.rows - 1) / f.per_tile + 1;
   f.lists = static_cast<long long>(shared ? 1 : batch) * heads;
   const long long units = f.lists * f.tiles, steps = (static_cast<long long>(held_tokens(cache)) + n_kc) / kFewStep + 1;
+  const int warps = f.per_tile == 8 ? FewShape<128, 1>::kWarps : FewShape<128, 2>::kWarps;
   f.splits = 1;
   long long least = 0;
-  for (int i = 1; i <= 148 && (i == 1 || steps / i >= 2 * 128 / f.per_tile); ++i) {   // two steps for every warp
-    const long long cost = (units * i + kSms - 1) / kSms * ((steps + i - 1) / i + 40);
+  for (int i = 1; i <= 148 && (i == 1 || steps / i >= 2 * warps); ++i) {   // two steps for every warp
+    const long long cost = (units * i + kSms - 1) / kSms * ((steps + i - 1) / i + 20);
     if (i == 1 || cost < least) { f.splits = i; least = cost; }
   }
   return f;
@@ -888,10 +889,24 @@ struct Attn8Call {
   const void *q, *k_chunk, *v_chunk;
 };
 
+// Rows of codes seen as {code, token up to `end`, list}; boxes of kFewStep rows, swizzled over a row.
+astro_status_t make_tmap_codes(CUtensorMap* out, const void* base, int head_dim, long long end, long long slot_tokens, long long lists) {
+  encode_tiled_fn fn = get_encode_fn();
+  if (!fn) return ASTRO_ERR_CUDA;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(end), static_cast<cuuint64_t>(lists)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(slot_tokens) * head_dim};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(head_dim), kFewStep, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? ASTRO_OK : ASTRO_ERR_CUDA;
+}
+
 template <int D, int NT>
 astro_status_t launch_few(const Attn8Call& c, float scale, void* o, float* lse, void* workspace, cudaStream_t st) {
   using S = FewShape<D, NT>;
-  constexpr int kSmem = few_smem_bytes<D, NT>();
+  constexpr int kSmem = S::kTotal;
   static std::atomic<int> done[kMaxDevices];
   astro_status_t s = set_smem_once(attn8_few_kernel<D, NT>, kSmem, done);
   if (s != ASTRO_OK) return s;
@@ -902,16 +917,23 @@ astro_status_t launch_few(const Attn8Call& c, float scale, void* o, float* lse, 
   f.vc = static_cast<const __nv_bfloat16*>(c.v_chunk);
   f.o = static_cast<__nv_bfloat16*>(o);
   f.lse = lse;
-  f.n_ctx = held_tokens(c.a.cache);
   f.n_kc = c.a.n_kc;
-  if (f.n_ctx > 0) {
+  FewMaps maps;
+  std::memset(&maps, 0, sizeof(maps));
+  if (held_tokens(c.a.cache) > 0) {
     const QuantTensors x = quant_tensors(c.a.cache, 0);
-    f.k = x.k_store; f.v = x.v_store; f.k_exp = x.k_exp; f.v_exp = x.v_exp;
+    f.k_exp = x.k_exp; f.v_exp = x.v_exp;
     f.slot_tokens = x.slot_tokens;
     const KeySegs segs = build_segments(c.a.cache, 0);
     f.start0 = segs.start[0];
     f.count0 = segs.count[0];
-    f.start1 = segs.n > 1 ? segs.start[1] : 0;
+    if (segs.n > 1) { f.start1 = segs.start[1]; f.count1 = segs.count[1]; }
+    const long long lists = static_cast<long long>(c.a.cache->d.cache_batch) * c.a.heads;
+    for (int i = 0; i < segs.n; ++i) {
+      const long long end = static_cast<long long>(segs.start[i]) + segs.count[i];
+      if ((s = make_tmap_codes(&maps.k[i], x.k_store, D, end, x.slot_tokens, lists)) != ASTRO_OK) return s;
+      if ((s = make_tmap_codes(&maps.v[i], x.v_store, D, end, x.slot_tokens, lists)) != ASTRO_OK) return s;
+    }
   }
   const FewSplit split = few_split(c.a.cache, c.a.batch, c.a.heads, c.a.n_q, c.a.n_kc);
   f.batch = c.a.batch; f.heads = c.a.heads; f.n_q = c.a.n_q;
@@ -925,7 +947,7 @@ astro_status_t launch_few(const Attn8Call& c, float scale, void* o, float* lse, 
     f.part_lse = f.part_o + f.splits * rows * D;
   }
   const dim3 grid(static_cast<unsigned>(split.tiles * f.splits), c.a.heads, f.shared ? 1 : c.a.batch);
-  attn8_few_kernel<D, NT><<<grid, S::kThreads, kSmem, st>>>(f);
+  attn8_few_kernel<D, NT><<<grid, S::kThreads, kSmem, st>>>(maps, f);
   if ((s = launch_status()) != ASTRO_OK || f.splits == 1) return s;
   return launch_dependent(sparse_combine_kernel<D>, dim3(static_cast<unsigned>((rows + 7) / 8)), 256, 0, st, f.part_o, f.part_lse,
                           f.splits, rows, c.a.n_q, c.a.heads, f.o, lse);

@@ -8,17 +8,18 @@
 // Few queries: a kernel of its own that reads the codes and nothing else.  Bandwidth: 2 (D + 1) bytes per key and head.
 // mma.sync does the products (16 keys x 8 queries x 16 elements; a tcgen05 tile of 128 queries would be 1/16 full, and its
 // operands would have to go through shared memory), scores as S^T = K Q^T and O^T = V^T P^T, so that 8 queries fill a tile.
-//   The elements of a head are summed in whatever order suits: lane (g, t) of a warp takes 16 consecutive codes of key g at
-//   16 t and 64 + 16 t for K, and codes 16 g .. 16 g + 15 of keys 2t, 2t+1, 2t+8, 2t+9 for V, each one 16-byte access; Q is
-//   brought into the same order, O leaves in it.  P^T changes from its place as a result into that of an operand by movmatrix.
+//   The elements of a head are summed in whatever order suits: lane (g, t) of a warp takes 32 consecutive codes of key g from 32 t on
+//   for K (16 from 16 t at head_dim 64), and codes 16 g .. 16 g + 15 of keys 2t, 2t+1, 2t+8, 2t+9 for V; Q is brought into the same
+//   order, O leaves in it.  P^T changes from its place as a result into that of an operand by movmatrix.
 //   The operands are fp16, which holds every e4m3 number: one instruction turns two codes.  A query is multiplied by the power
 //   of two that brings its largest element to 2^14 (elements below 2^-38 of it vanish, the others keep all of bf16's bits).
 //   2^ek multiplies the score; 2^ev joins the weight: w = exp2(s + ev - M) with M a running maximum of s + ev, rounded to fp16
 //   (half a step, 2^-11 of a weight; those below 2^-31 of the largest vanish), while the row sum has a reference m of its own
 //   and takes fp32 weights.  (In bf16, whose range needs no second reference, turning the codes took 8 instructions per pair of
 //   pairs and the whole 506 per step: 50 us for 4 x 12 lists of 18720 keys, against 36 of bytes.)
-//   Every lane fetches its own 16-byte pieces with cp.async into slots that no other lane touches: a deep ring without a
-//   barrier, read back without a bank conflict.  References move (all lanes agreeing) when exceeded by more than 8.
+//   A warp streams its own tiles: one lane has 32 rows of K and of V brought by TMA into a ring that no other warp touches,
+//   swizzled so that no two lanes of a quarter warp meet in a bank.  (The same bytes by cp.async, 16 per lane, came at 4.8 TB/s
+//   whatever the warps did with them.)  References move (all lanes agreeing) when exceeded by more than 8.
 //   Over one stored prefix the queries of all samples are the rows of one list.  Warps take 16-key steps of their CTA's range
 //   in turn and are joined in shared memory; CTAs that share a list leave normalised parts and their LSE for
 //   sparse_combine_kernel.
@@ -70,41 +71,48 @@ __global__ void __launch_bounds__(kExpandThreads) expand8_kernel(const Expand8 a
 }
 
 // ---------------------------------------------------------------------------------- few queries
-constexpr int kFewStep = 16;                       // keys of a step
+constexpr int kFewStep = 32;                       // keys of a step: two tiles of 16, whose latencies overlap
 
 // 8 * NT queries per CTA; twice the queries take twice the registers and half the warps.
 template <int D, int NT> struct FewShape {
-  static constexpr int kWarps = 16 / NT, kThreads = 32 * kWarps;
+  static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = 32 * kWarps;
   static constexpr int kPieces = D / 64;           // 16-byte pieces of a key's K per lane
-  static constexpr int kSlots = 2 * kPieces + 4;   // accesses per lane and step: K of two keys, V of four
   static constexpr int kVBytes = D / 8;            // bytes of a key's V per lane: 16 or 8
-  static constexpr int kStageBytes = 32 * (2 * kPieces * 16 + 4 * kVBytes);
-  static constexpr int kStages = (D == 128 ? 3 : 6) * NT;
+  static constexpr int kStageBytes = 2 * kFewStep * D;   // K, then V
+  static constexpr int kStages = (D == 128 ? 2 : 4) + (NT - 1);
   static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kJoined = kWarps * 8 * NT * (D + 4) * 4;               // the warps' outputs and statistics, behind the loop
+  static constexpr int kBars = kRing > kJoined ? kRing : kJoined;
+  static constexpr int kTotal = kBars + kWarps * kStages * 8 + 16 + 1024;
 };
 
 struct FewArgs {
   const __nv_bfloat16 *q, *kc, *vc;
-  const uint8_t *k, *v, *k_exp, *v_exp;
+  const uint8_t *k_exp, *v_exp;
   __nv_bfloat16* o;
   float* lse;              // may be null
   float *part_o, *part_lse;  // when splits > 1
   long long slot_tokens;
-  int start0, count0, start1, n_ctx, n_kc;
+  int start0, count0, start1, count1, n_kc;   // the held rows' two runs in the storage
   int batch, heads, n_q, splits;
   int rows;                // of a list: n_q, or batch * n_q over one prefix
   int shared;              // 1: one prefix for all samples
   float scale_log2;
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+struct FewMaps {
+  CUtensorMap k[2], v[2];   // {code, token up to the run's end, list} of both runs
+};
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tmap, uint64_t* bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
 }
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+// Byte offset of 16-byte chunk `chunk` of row `row` in a tile of rows of D bytes, as TMA's swizzle over D bytes leaves it.
+template <int D> __device__ __forceinline__ int swizzled(int row, int chunk) {
+  return row * D + ((chunk ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4);
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // c[16 x 8] += a[16 x 16] b[16 x 8], bf16 or fp16 products, fp32 sums.
 template <bool kBf16>
@@ -148,29 +156,39 @@ template <int D, int NT> struct FewState {
         for (int e = 0; e < 4; ++e) o[n][j][e] = 0.f;
     }
   }
-  // Scores of keys g (s[..][0..1]) and g + 8 (s[..][2..3]) in log2 units, -infinity where there is no key, and the exponents
-  // of their values -> the weights as the operand of O^T = V^T P^T.
-  template <bool kBf16>
-  __device__ __forceinline__ void weigh(const float (&s)[NT][4], float e0, float e1, uint32_t (&b)[NT][2]) {
+  // Scores of keys g (s[..][..][0..1]) and g + 8 (s[..][..][2..3]) of TILES tiles in log2 units, -infinity where there is no key,
+  // and the exponents of their values -> the weights as the operands of O^T = V^T P^T.
+  template <bool kBf16, int TILES>
+  __device__ __forceinline__ void weigh(const float (&s)[TILES][NT][4], const float (&e)[TILES][2], uint32_t (&b)[TILES][NT][2]) {
     bool over = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-        over = over || fmaxf(s[n][c], s[n][c + 2]) > m[n][c] + kFewSlack || fmaxf(s[n][c] + e0, s[n][c + 2] + e1) > top[n][c] + kFewSlack;
+      for (int c = 0; c < 2; ++c) {
+        float x = -INFINITY, y = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+          x = max3(x, s[i][n][c], s[i][n][c + 2]);
+          y = max3(y, s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]);
+        }
+        over = over || x > m[n][c] + kFewSlack || y > top[n][c] + kFewSlack;
+      }
     if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float x = fmaxf(s[n][c], s[n][c + 2]), y = fmaxf(s[n][c] + e0, s[n][c + 2] + e1);
+          float x = m[n][c], y = top[n][c];
+#pragma unroll
+          for (int i = 0; i < TILES; ++i) {
+            x = max3(x, s[i][n][c], s[i][n][c + 2]);
+            y = max3(y, s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]);
+          }
 #pragma unroll
           for (int d = 4; d < 32; d *= 2) {
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
           }
-          x = fmaxf(x, m[n][c]);
-          y = fmaxf(y, top[n][c]);
           l[n][c] *= m[n][c] == -INFINITY ? 0.f : fast_exp2(m[n][c] - x);
           const float alpha = top[n][c] == -INFINITY ? 0.f : fast_exp2(top[n][c] - y);
           m[n][c] = x;
@@ -183,81 +201,91 @@ template <int D, int NT> struct FewState {
         }
     }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float w[4];
+    for (int i = 0; i < TILES; ++i)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const float ref = m[n][c] == -INFINITY ? 0.f : m[n][c], wref = (top[n][c] == -INFINITY ? 0.f : top[n][c]) - kFewBias;
-        l[n][c] += fast_exp2(s[n][c] - ref) + fast_exp2(s[n][c + 2] - ref);
-        w[c] = fast_exp2(s[n][c] + (e0 - wref));
-        w[c + 2] = fast_exp2(s[n][c + 2] + (e1 - wref));
+      for (int n = 0; n < NT; ++n) {
+        float w[4];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float ref = m[n][c] == -INFINITY ? 0.f : m[n][c], wref = (top[n][c] == -INFINITY ? 0.f : top[n][c]) - kFewBias;
+          l[n][c] += fast_exp2(s[i][n][c] - ref) + fast_exp2(s[i][n][c + 2] - ref);
+          w[c] = fast_exp2(s[i][n][c] + (e[i][0] - wref));
+          w[c + 2] = fast_exp2(s[i][n][c + 2] + (e[i][1] - wref));
+        }
+        b[i][n][0] = transpose_8x8(kBf16 ? pack_bf16(w[0], w[1]) : pack_half(w[0], w[1]));
+        b[i][n][1] = transpose_8x8(kBf16 ? pack_bf16(w[2], w[3]) : pack_half(w[2], w[3]));
       }
-      b[n][0] = transpose_8x8(kBf16 ? pack_bf16(w[0], w[1]) : pack_half(w[0], w[1]));
-      b[n][1] = transpose_8x8(kBf16 ? pack_bf16(w[2], w[3]) : pack_half(w[2], w[3]));
-    }
   }
 };
 
 // grid.x: (tile of 8 NT rows, split) with the split fastest, grid.y: head, grid.z: sample (one over a shared prefix).
 template <int D, int NT>
-__global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel(const FewArgs a) {
+__global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ FewArgs a) {
   using S = FewShape<D, NT>;
   constexpr int kFewWarps = S::kWarps, kFewThreads = S::kThreads;
-  extern __shared__ __align__(16) uint8_t few_smem[];
+  extern __shared__ uint8_t few_smem_raw[];
+  uint8_t* few_smem = align_1024(few_smem_raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int split = blockIdx.x % a.splits, row0 = blockIdx.x / a.splits * (8 * NT);
   const int h = blockIdx.y, bz = blockIdx.z;
   const long long list = static_cast<long long>(bz) * a.heads + h;
-  const uint8_t* k_base = a.k + list * a.slot_tokens * D + t * 16;
-  const uint8_t* v_base = a.v + list * a.slot_tokens * D + g * S::kVBytes;
   const uint8_t *ke = a.k_exp + list * a.slot_tokens, *ve = a.v_exp + list * a.slot_tokens;
-  const uint32_t ring = smem_u32(few_smem) + warp * (S::kStages * S::kStageBytes);
+  uint8_t* ring = few_smem + warp * (S::kStages * S::kStageBytes);
+  uint64_t* full = reinterpret_cast<uint64_t*>(few_smem + S::kBars) + warp * S::kStages;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(few_smem + S::kBars + kFewWarps * S::kStages * 8);
+  if (lane == 0) {
+    for (int i = 0; i < S::kStages; ++i) mbar_init(full + i, 1);
+    fence_mbar_init();
+  }
+  if (threadIdx.x == 0) *abort_flag = 0;
+  dependents_may_start();   // the joining kernel waits for the whole grid where it begins
+  __syncthreads();
   // row of the list -> sample and query
   auto sample_of = [&](int row) { return a.shared ? row / a.n_q : bz; };
   auto query_of = [&](int row) { return a.shared ? row % a.n_q : row; };
 
   // this CTA's steps: those of the cache first, then those of the chunks of the samples that the rows belong to
   const int row_end = min(row0 + 8 * NT, a.rows), first_sample = sample_of(row0);
-  const int ctx_steps = (a.n_ctx + kFewStep - 1) / kFewStep, chunk_steps = (a.n_kc + kFewStep - 1) / kFewStep;
+  const int steps0 = (a.count0 + kFewStep - 1) / kFewStep, ctx_steps = steps0 + (a.count1 + kFewStep - 1) / kFewStep;
+  const int chunk_steps = (a.n_kc + 15) / 16;   // the chunk's: one tile
   const int steps = ctx_steps + (sample_of(row_end - 1) - first_sample + 1) * chunk_steps;
   const int each = steps / a.splits, rest = steps % a.splits;
   const int first = split * each + min(split, rest), last = first + each + (split < rest ? 1 : 0);
   const int ctx_last = min(last, ctx_steps);
 
-  auto place = [&](int r) -> long long { return r < a.count0 ? a.start0 + r : a.start1 + (r - a.count0); };
-  // keys behind the end: the last key's bytes, with a score of -infinity
+  // the first row of a step in the storage, and how many of its 32 are there
+  auto row_of_step = [&](int step) { return step < steps0 ? a.start0 + step * kFewStep : a.start1 + (step - steps0) * kFewStep; };
+  auto rows_left = [&](int step) { return step < steps0 ? a.count0 - step * kFewStep : a.count1 - (step - steps0) * kFewStep; };
+  // Rows behind a run's end come as zeros.  All lanes have read the stage before.
   auto fetch = [&](int step, int stage) {
-    if (step < ctx_last) {
-      const int key0 = step * kFewStep;
-      const uint32_t slot = ring + stage * S::kStageBytes + lane * 16;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint8_t* src = k_base + place(min(key0 + g + 8 * i, a.n_ctx - 1)) * D;
-#pragma unroll
-        for (int c = 0; c < S::kPieces; ++c) cp_async16(slot + (i * S::kPieces + c) * 512, src + c * 64);
-      }
-      const uint32_t v_slot = ring + stage * S::kStageBytes + 2 * S::kPieces * 512 + lane * S::kVBytes;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint8_t* src = v_base + place(min(key0 + 2 * t + (i & 1) + 8 * (i >> 1), a.n_ctx - 1)) * D;
-        if constexpr (D == 128) cp_async16(v_slot + i * 512, src);
-        else cp_async8(v_slot + i * 256, src);
-      }
+    __syncwarp();
+    if (lane == 0 && step < ctx_last) {
+      const int run = step < steps0 ? 0 : 1, row = row_of_step(step);
+      const uint32_t dst = smem_u32(ring + stage * S::kStageBytes);
+      mbar_arrive_expect_tx(full + stage, S::kStageBytes);
+      tma_load_3d(dst, &maps.k[run], full + stage, 0, row, static_cast<int>(list));
+      tma_load_3d(dst + kFewStep * D, &maps.v[run], full + stage, 0, row, static_cast<int>(list));
     }
-    cp_async_commit();
   };
-  uint32_t e_next[4];   // exponent bytes of keys g, g + 8: K, K, V, V
+  uint32_t k_next[2][2], v_next[2][2];   // exponent bytes of keys g, g + 8 of both tiles
   auto fetch_exps = [&](int step) {
     if (step < ctx_last) {
-      const long long r0 = place(min(step * kFewStep + g, a.n_ctx - 1)), r1 = place(min(step * kFewStep + g + 8, a.n_ctx - 1));
-      e_next[0] = ke[r0]; e_next[1] = ke[r1]; e_next[2] = ve[r0]; e_next[3] = ve[r1];
+      const int row = row_of_step(step), most = rows_left(step) - 1;
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = row + min(16 * tile + g + 8 * i, most);
+          k_next[tile][i] = ke[r];
+          v_next[tile][i] = ve[r];
+        }
     }
   };
 #pragma unroll
   for (int i = 0; i < S::kStages - 1; ++i) fetch(first + warp + i * kFewWarps, i);
   fetch_exps(first + warp);
 
-  // Q in the order of the K pieces: elements 16 (t + 4 c) + 4 x + {0, 1} and {2, 3} of query 8 n + g
+  // Q in the order of the K pieces: elements 16 (kPieces t + c) + 4 x + {0, 1} and {2, 3} of query 8 n + g
   uint32_t qf[NT][S::kPieces][4][2];
   auto load_q = [&]() {
 #pragma unroll
@@ -268,7 +296,7 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
       for (int c = 0; c < S::kPieces; ++c)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const uint4 w = src[2 * (t + 4 * c) + x];
+          const uint4 w = src[2 * (S::kPieces * t + c) + x];
           qf[n][c][2 * x][0] = w.x; qf[n][c][2 * x][1] = w.y;
           qf[n][c][2 * x + 1][0] = w.z; qf[n][c][2 * x + 1][1] = w.w;
         }
@@ -300,74 +328,88 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
   FewState<D, NT> st;
   st.clear();
 
-  int stage = 0;
+  int stage = 0, round = 0;
   for (int step = first + warp; step < ctx_last; step += kFewWarps) {
-    cp_async_wait<S::kStages - 2>();
-    const uint4* slot = reinterpret_cast<const uint4*>(few_smem + warp * (S::kStages * S::kStageBytes) + stage * S::kStageBytes) + lane;
-    const float ks0 = exp_byte_to_float(e_next[0]), ks1 = exp_byte_to_float(e_next[1]);
-    const float vs0 = static_cast<float>(static_cast<int>(e_next[2]) - 127), vs1 = static_cast<float>(static_cast<int>(e_next[3]) - 127);
+    // into the stage that the step before has been read out of
+    fetch(step + (S::kStages - 1) * kFewWarps, stage == 0 ? S::kStages - 1 : stage - 1);
+    if (!mbar_wait_ok(full + stage, round & 1, abort_flag)) break;
+    const uint8_t* held = ring + stage * S::kStageBytes;
+    float ks[2][2], ve_log2[2][2];
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        ks[tile][i] = exp_byte_to_float(k_next[tile][i]);
+        ve_log2[tile][i] = static_cast<float>(static_cast<int>(v_next[tile][i]) - 127);
+      }
     fetch_exps(step + kFewWarps);
-    float s[NT][4];
+    float s[2][NT][4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-#pragma unroll
-    for (int c = 0; c < S::kPieces; ++c) {
-      const uint4 x = slot[c * 32], y = slot[(S::kPieces + c) * 32];
-      const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t a0 = e4m3_to_half2(xw[i]), a2 = e4m3_to_half2(xw[i] >> 16);
-        const uint32_t a1 = e4m3_to_half2(yw[i]), a3 = e4m3_to_half2(yw[i] >> 16);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s[n], a0, a1, a2, a3, qf[n][c][i][0], qf[n][c][i][1]);
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        s[n][c] *= ks0 * unit[n][c];
-        s[n][c + 2] *= ks1 * unit[n][c];
-      }
-    const int left = a.n_ctx - step * kFewStep;   // keys from here to the end
-    if (left < kFewStep) {
+    for (int tile = 0; tile < 2; ++tile)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (g + 8 * (e / 2) >= left) s[n][e] = -INFINITY;
-    }
-    uint32_t p[NT][2];
-    st.template weigh<false>(s, vs0, vs1, p);
-    // V: words of keys 2t, 2t+1, 2t+8, 2t+9
-    uint32_t w[4][S::kVBytes / 4];
-    const uint8_t* v_slot = few_smem + warp * (S::kStages * S::kStageBytes) + stage * S::kStageBytes + 2 * S::kPieces * 512 + lane * S::kVBytes;
+        for (int e = 0; e < 4; ++e) s[tile][n][e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (D == 128) {
-        const uint4 x = *reinterpret_cast<const uint4*>(v_slot + i * 512);
-        w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(v_slot + i * 256);
-        w[i][0] = x.x; w[i][1] = x.y;
+    for (int c = 0; c < S::kPieces; ++c)
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) {
+        const uint4 x = *reinterpret_cast<const uint4*>(held + swizzled<D>(16 * tile + g, S::kPieces * t + c));
+        const uint4 y = *reinterpret_cast<const uint4*>(held + swizzled<D>(16 * tile + g + 8, S::kPieces * t + c));
+        const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a0 = e4m3_to_half2(xw[i]), a2 = e4m3_to_half2(xw[i] >> 16);
+          const uint32_t a1 = e4m3_to_half2(yw[i]), a3 = e4m3_to_half2(yw[i] >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_16x8x16<false>(s[tile][n], a0, a1, a2, a3, qf[n][c][i][0], qf[n][c][i][1]);
+        }
       }
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[tile][n][e] *= ks[tile][e / 2] * unit[n][e % 2];
+    const int left = rows_left(step);
+    if (left < kFewStep) {
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (16 * tile + g + 8 * (e / 2) >= left) s[tile][n][e] = -INFINITY;
     }
+    uint32_t p[2][NT][2];
+    st.template weigh<false, 2>(s, ve_log2, p);
 #pragma unroll
-    for (int i = 0; i < S::kVBytes / 4; ++i)
+    for (int tile = 0; tile < 2; ++tile) {
+      // V: words of keys 2t, 2t+1, 2t+8, 2t+9
+      uint32_t w[4][S::kVBytes / 4];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const uint32_t sel = half ? 0x7362u : 0x5140u;   // codes of two elements, keys side by side
-        const uint32_t x = __byte_perm(w[0][i], w[1][i], sel), y = __byte_perm(w[2][i], w[3][i], sel);
-        const uint32_t a0 = e4m3_to_half2(x), a1 = e4m3_to_half2(x >> 16), a2 = e4m3_to_half2(y), a3 = e4m3_to_half2(y >> 16);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma_16x8x16<false>(st.o[n][2 * i + half], a0, a1, a2, a3, p[n][0], p[n][1]);
+      for (int i = 0; i < 4; ++i) {
+        const int r = 16 * tile + 2 * t + (i & 1) + 8 * (i >> 1);
+        if constexpr (D == 128) {
+          const uint4 x = *reinterpret_cast<const uint4*>(held + kFewStep * D + swizzled<D>(r, g));
+          w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(held + kFewStep * D + swizzled<D>(r, g >> 1) + 8 * (g & 1));
+          w[i][0] = x.x; w[i][1] = x.y;
+        }
       }
-    int ahead = stage + S::kStages - 1;
-    if (ahead >= S::kStages) ahead -= S::kStages;
-    fetch(step + (S::kStages - 1) * kFewWarps, ahead);
-    if (++stage == S::kStages) stage = 0;
+#pragma unroll
+      for (int i = 0; i < S::kVBytes / 4; ++i)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t sel = half ? 0x7362u : 0x5140u;   // codes of two elements, keys side by side
+          const uint32_t x = __byte_perm(w[0][i], w[1][i], sel), y = __byte_perm(w[2][i], w[3][i], sel);
+          const uint32_t a0 = e4m3_to_half2(x), a1 = e4m3_to_half2(x >> 16), a2 = e4m3_to_half2(y), a3 = e4m3_to_half2(y >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_16x8x16<false>(st.o[n][2 * i + half], a0, a1, a2, a3, p[tile][n][0], p[tile][n][1]);
+        }
+    }
+    if (++stage == S::kStages) { stage = 0; ++round; }
   }
 
   // the chunks' own keys, bf16 [B, n_kc, H, D]; the warps take them in the order in which the cache's steps would have gone on
@@ -375,25 +417,25 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
   if (step < ctx_steps) step += (ctx_steps - step + kFewWarps - 1) / kFewWarps * kFewWarps;
   if (step < last) load_q();
   for (; step < last; step += kFewWarps) {
-    const int b = first_sample + (step - ctx_steps) / chunk_steps, key0 = (step - ctx_steps) % chunk_steps * kFewStep;
+    const int b = first_sample + (step - ctx_steps) / chunk_steps, key0 = (step - ctx_steps) % chunk_steps * 16;
     auto row_of = [&](const __nv_bfloat16* base, int key) {
       return base + ((static_cast<long long>(b) * a.n_kc + min(key, a.n_kc - 1)) * a.heads + h) * D;
     };
-    float s[NT][4];
+    float s[1][NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+      for (int e = 0; e < 4; ++e) s[0][n][e] = 0.f;
     const uint4 *k0 = reinterpret_cast<const uint4*>(row_of(a.kc, key0 + g)), *k1 = reinterpret_cast<const uint4*>(row_of(a.kc, key0 + g + 8));
 #pragma unroll
     for (int c = 0; c < S::kPieces; ++c)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint4 x = k0[2 * (t + 4 * c) + i], y = k1[2 * (t + 4 * c) + i];
+        const uint4 x = k0[2 * (S::kPieces * t + c) + i], y = k1[2 * (S::kPieces * t + c) + i];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          mma_16x8x16<true>(s[n], x.x, y.x, x.y, y.y, qf[n][c][2 * i][0], qf[n][c][2 * i][1]);
-          mma_16x8x16<true>(s[n], x.z, y.z, x.w, y.w, qf[n][c][2 * i + 1][0], qf[n][c][2 * i + 1][1]);
+          mma_16x8x16<true>(s[0][n], x.x, y.x, x.y, y.y, qf[n][c][2 * i][0], qf[n][c][2 * i][1]);
+          mma_16x8x16<true>(s[0][n], x.z, y.z, x.w, y.w, qf[n][c][2 * i + 1][0], qf[n][c][2 * i + 1][1]);
         }
       }
     const int left = a.n_kc - key0;
@@ -402,10 +444,11 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        s[n][e] = g + 8 * (e / 2) < left && sample_of(row0 + 8 * n + 2 * t + e % 2) == b ? s[n][e] * a.scale_log2 : -INFINITY;
+        s[0][n][e] = g + 8 * (e / 2) < left && sample_of(row0 + 8 * n + 2 * t + e % 2) == b ? s[0][n][e] * a.scale_log2 : -INFINITY;
     // no weight for those who do not see the key, whatever its value holds: 0 * NaN would reach them
-    uint32_t p[NT][2];
-    st.template weigh<true>(s, 0.f, 0.f, p);
+    uint32_t p[1][NT][2];
+    const float none[1][2] = {{0.f, 0.f}};
+    st.template weigh<true, 1>(s, none, p);
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {       // 8 elements of the lane's D/8
       uint32_t w[4][4];
@@ -420,7 +463,7 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
         for (int n = 0; n < NT; ++n) {
           float add[4] = {0.f, 0.f, 0.f, 0.f};
           mma_16x8x16<true>(add, __byte_perm(w[0][j], w[1][j], 0x5410), __byte_perm(w[0][j], w[1][j], 0x7632),
-                            __byte_perm(w[2][j], w[3][j], 0x5410), __byte_perm(w[2][j], w[3][j], 0x7632), p[n][0], p[n][1]);
+                            __byte_perm(w[2][j], w[3][j], 0x5410), __byte_perm(w[2][j], w[3][j], 0x7632), p[0][n][0], p[0][n][1]);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (sample_of(row0 + 8 * n + 2 * t + e % 2) == b) st.o[n][4 * i + j][e] += add[e];
@@ -429,7 +472,7 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
   }
 
   // ---- the warps' outputs joined: [warp][query][D], then [warp][query] of references and sums
-  cp_async_wait<0>();
+  settle_after_abort(abort_flag);
   __syncthreads();
   float* out = reinterpret_cast<float*>(few_smem);
   float4* stats = reinterpret_cast<float4*>(out + kFewWarps * 8 * NT * D);
@@ -478,11 +521,5 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
       if (d == 0 && a.lse != nullptr) a.lse[at] = lse;
     }
   }
-  dependents_may_start();
 }
-template <int D, int NT> constexpr int few_smem_bytes() {
-  const int joined = FewShape<D, NT>::kWarps * 8 * NT * (D + 4) * 4;
-  return FewShape<D, NT>::kRing > joined ? FewShape<D, NT>::kRing : joined;
-}
-
 }  // namespace astro
