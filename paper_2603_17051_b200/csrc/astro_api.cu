@@ -1090,13 +1090,45 @@ astro_status_t launch_window_fwd(const WindowCall& c, float scale, void* o, floa
   a.mask = window_mask(c.d, c.lengths);
   a.heads = c.d.heads;
   a.group = c.d.heads / c.d.kv_heads;
-  a.lists = c.d.batch * c.d.heads;
-  a.q_tiles = (c.d.n_tokens + kTile - 1) / kTile;
+  a.order.set(c.d.batch * c.d.heads, (c.d.n_tokens + kTile - 1) / kTile);
   a.scale = scale;
   a.scale_log2 = scale * kLog2e;
   a.careful = g_fwd_mode.load(std::memory_order_relaxed) == 1 ? 1 : 0;
-  window_attn_fwd_kernel<D><<<static_cast<unsigned>(a.lists) * a.q_tiles, kWinThreads, WinFwdSmem<D>::kTotal, st>>>(tk, tv, a);
+  window_attn_fwd_kernel<D><<<static_cast<unsigned>(a.order.lists) * a.order.tiles, kWinThreads, WinFwdSmem<D>::kTotal, st>>>(tk, tv, a);
   return launch_status();
+}
+
+// Where the window hides the other key tiles from most queries, the sinks' are seen by all of them.  Where one of them alone would
+// take longer than an SM's share of all the work (its list of tiles against all lists over a B200's 148 SMs), it is divided
+// among CTAs, whose parts are joined; at most kWinPartSlots of them, the workspace's.  (12 heads over one of keys, 32760
+// tokens, a window of 1024, 4 sinks: 6200 us with a CTA to a key tile, 840 divided.  2 x 4097 tokens, 12 heads over 4: 198 and 204, not divided.)
+constexpr int kWinPartSlots = 296;
+struct WinShares {
+  int front, shares;
+};
+int window_part_slots(int batch, int heads, int n) {
+  const long long most = 8ll * batch * heads;
+  return n < 16 * kTile ? 0 : static_cast<int>(most < kWinPartSlots ? most : kWinPartSlots);
+}
+WinShares window_shares(const astro_window_desc_t& d) {
+  WinShares w{0, 1};
+  const WinMask m = window_mask(d, nullptr);
+  if (m.window >= d.n_tokens) return w;
+  w.front = (m.sink + kTile - 1) / kTile;
+  if (w.front == 0) return w;
+  const long long tiles = (d.n_tokens + kTile - 1) / kTile, group = d.heads / d.kv_heads;
+  long long usual = (m.window + m.block) / kTile + 2;       // tiles that a tile behind the sinks meets, about
+  if (usual > tiles) usual = tiles;
+  const long long longest = tiles * group, lists = static_cast<long long>(d.batch) * d.heads;
+  const long long all = 2 * lists * tiles * usual + lists * w.front * tiles;   // dQ's and dK/dV's
+  const long long fair = all / 148;
+  if (longest <= fair) return w;
+  const long long part = fair / 2 < 8 ? 8 : fair / 2;
+  long long shares = (longest + part - 1) / part;
+  const long long slots = window_part_slots(d.batch, d.heads, d.n_tokens) / (static_cast<long long>(w.front) * d.batch * d.kv_heads);
+  if (shares > slots) shares = slots;
+  if (shares > 1) w.shares = static_cast<int>(shares);
+  return w;
 }
 
 template <int D>
@@ -1130,11 +1162,19 @@ astro_status_t launch_window_bwd(const WindowCall& c, const void* o, const float
   a.kv_lists = d.batch * d.kv_heads;
   a.tiles = (d.n_tokens + kTile - 1) / kTile;
   a.scale = scale;
-  // the key tiles of the sinks first where they are seen by far more queries than others: they would end last
-  a.front = a.mask.window < d.n_tokens ? (a.mask.sink + kTile - 1) / kTile : 0;
+  const WinShares w = window_shares(d);
+  a.front = w.front;
+  a.q_order.set(a.lists, a.tiles);
+  a.k_order.set(a.kv_lists, a.tiles - a.front);
+  a.shares = w.shares;
+  a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + astro_chunk_attn_bwd_workspace_bytes(d.batch, d.heads, d.n_tokens, D));
   if ((s = launch_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, static_cast<float*>(workspace), st)) != ASTRO_OK) return s;
-  return launch_dependent(window_attn_bwd_kernel<D>, dim3(static_cast<unsigned>(a.lists + a.kv_lists) * a.tiles), kWinBwdThreads,
-                          window_bwd_smem<D>(), st, tq, tdo, tk, tv, a);
+  const long long ctas = static_cast<long long>(a.front) * a.kv_lists * a.shares + static_cast<long long>(a.lists) * a.tiles +
+                         static_cast<long long>(a.kv_lists) * (a.tiles - a.front);
+  s = launch_dependent(window_attn_bwd_kernel<D>, dim3(static_cast<unsigned>(ctas)), kWinBwdThreads, window_bwd_smem<D>(), st, tq, tdo, tk,
+                       tv, a);
+  if (s != ASTRO_OK || a.shares == 1) return s;
+  return launch_dependent(win_join_kernel<D>, dim3(static_cast<unsigned>(a.front * a.kv_lists), kTile / kJoinRows), kWinBwdThreads, 0, st, a);
 }
 
 }  // namespace
@@ -1965,7 +2005,9 @@ astro_status_t astro_window_attn_fwd(const astro_window_desc_t* desc, const void
 }
 
 size_t astro_window_attn_bwd_workspace_bytes(int batch, int heads, int n_tokens, int head_dim) {
-  return astro_chunk_attn_bwd_workspace_bytes(batch, heads, n_tokens, head_dim);
+  const size_t delta = astro_chunk_attn_bwd_workspace_bytes(batch, heads, n_tokens, head_dim);
+  if (delta == 0) return 0;
+  return delta + static_cast<size_t>(window_part_slots(batch, heads, n_tokens)) * 2 * kTile * head_dim * sizeof(float);
 }
 
 astro_status_t astro_window_attn_bwd(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,

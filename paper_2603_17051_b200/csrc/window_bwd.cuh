@@ -3,8 +3,9 @@
 //   dK/dV  a key tile stationary, over the query tiles of all the heads that share it and see it:
 //          dV = sum P^T dO, dK = scale * sum dS^T Q
 // with P = exp(S - LSE), dS = P o (dP - delta), as in the dense kernels (attn_bwd.cuh), whose tensor-memory layouts, operand
-// forms and hand-offs these two have: see there.  Both in one launch, a CTA per tile, the long ones first (of the key tiles
-// those of the sinks, which every query sees; then the query tiles; then the other key tiles).  Tiles of which a row sees only a part are masked bit by bit, P and dS by selection, so that what a masked
+// forms and hand-offs these two have: see there.  Both in one launch, a CTA per tile, the long jobs first:
+// the key tiles of the sinks, which every query sees (several CTAs to a tile where it would take longer than everything
+// else), the other key tiles, the query tiles.  Tiles of which a row sees only a part are masked bit by bit, P and dS by selection, so that what a masked
 // place holds, NaN included, ends there; rows behind a sequence's end are cleared in shared memory where they are operands.
 // Inside a sequence a NaN or infinity in K, Q or dO would still reach the rows of a masked tile that do not see it (0 * NaN):
 // a tile whose gradients are not finite is done again by the formula, on the ordinary cores (slow and rare).
@@ -25,11 +26,14 @@ struct WinBwdArgs {
   __nv_bfloat16 *dq, *dk, *dv;    // [B, n, H or KVH, D]
   WinMask mask;
   int heads, kv_heads, group, lists, kv_lists, tiles;   // lists = batch * heads, kv_lists = batch * kv_heads
-  int front;                      // key tiles whose CTAs come before the query tiles'
+  WinOrder q_order, k_order;      // of the query tiles and of the key tiles behind the front ones
+  int front;                      // key tiles of the sinks, where they come first
+  int shares;                     // CTAs that share each of them
+  float* parts;                   // [front][list][share][dK | dV][128][D] when shares > 1
   float scale;
 };
-constexpr int kWinBwdThreads = kDqSoftmaxThreads + 64;   // MMA, loads
-static_assert(kWinBwdThreads == kDkvThreads, "both kinds of CTA have the same warps");
+constexpr int kWinGroups = 2;                             // softmax groups of 128 threads, 32 columns of a tile each
+constexpr int kWinBwdThreads = 128 * kWinGroups + 64;     // + MMA, loads
 
 // 32 accumulator columns of the lane's row times `mult`, zeros where the row is not live, as bf16; whether all are finite.
 __device__ __forceinline__ bool win_store_row32(uint32_t taddr, float mult, bool live, const QuadRows& rows, int col0, int lane) {
@@ -112,11 +116,11 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
   const int q0 = qt * kTile, len = a.mask.length(b), kvh = h / a.group;
   constexpr uint32_t kTmemCols = 512;
   constexpr uint32_t kColS = 0, kColdP = 128, kColdS = 256, kColQ = 320, kColdQ = 384;
-  constexpr int kMmaWarp = 4 * kDqGroups, kTmaWarp = kMmaWarp + 1;
+  constexpr int kMmaWarp = 4 * kWinGroups, kTmaWarp = kMmaWarp + 1, kCols = kTile / kWinGroups, NL = kCols / 32;
 
   if (q0 >= len) {   // nothing but zeros, the same for the whole CTA
     dependency_wait();
-    if (warp < kMmaWarp) {
+    if (warp < 8) {
       const QuadRows rows = quad_rows(a.dq, b, h, a.mask.n, a.heads, D, q0 + (tid & 127));
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
@@ -133,7 +137,7 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
   if (warp == kTmaWarp && lane == 0) { tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v); tma_prefetch_desc(&tm_do); }
   if (tid < 15) {
     // qt_full: one arrival per warp and 64 elements; rs, rb: bytes and warps
-    mbar_init(bars + tid, tid == 1 ? 4 * (D / 64) : tid >= 2 && tid < 10 ? 1 + 4 * kDqGroups : 1);
+    mbar_init(bars + tid, tid == 1 ? 4 * (D / 64) : tid >= 2 && tid < 10 ? 1 + 4 * kWinGroups : 1);
     fence_mbar_init();
   }
   if (tid == 0) *abort_flag = 0;
@@ -270,15 +274,15 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
     for (int j = 0; j < n_tiles; ++j, kt = tiles.next(kt)) {
       bool ok = mbar_wait_ok(s_full, j & 1, abort_flag);
       tc_fence_after_sync();
-      uint32_t s[2][32];
-      tmem_ld32(tmem_lane + kColS + g * kDqCols, s[0]);
-      tmem_ld32(tmem_lane + kColS + g * kDqCols + 32, s[1]);
+      uint32_t s[NL][32];
+#pragma unroll
+      for (int c2 = 0; c2 < NL; ++c2) tmem_ld32(tmem_lane + kColS + g * kCols + c2 * 32, s[c2]);
       tmem_wait_ld();
       tc_fence_before_sync();
       warp_arrive(rs + j % 4, lane);
-      uint64_t p2[2][16];
+      uint64_t p2[NL][16];
 #pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2)
+      for (int c2 = 0; c2 < NL; ++c2)
 #pragma unroll
         for (int c = 0; c < 32; c += 2) {
           float x0, x1;
@@ -288,13 +292,13 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
       // commit j+1 of b_done: dP(j) is there, and dQ(j-1) has consumed the one dS buffer
       ok = mbar_wait_ok(b_done + ((j + 1) & 1), (j >> 1) & 1, abort_flag) && ok;
       tc_fence_after_sync();
-      uint32_t dp[2][32], ds[2][16];
-      tmem_ld32(tmem_lane + kColdP + g * kDqCols, dp[0]);
-      tmem_ld32(tmem_lane + kColdP + g * kDqCols + 32, dp[1]);
+      uint32_t dp[NL][32], ds[NL][16];
+#pragma unroll
+      for (int c2 = 0; c2 < NL; ++c2) tmem_ld32(tmem_lane + kColdP + g * kCols + c2 * 32, dp[c2]);
       tmem_wait_ld();
       if (tiles.full(kt)) {
 #pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2)
+        for (int c2 = 0; c2 < NL; ++c2)
 #pragma unroll
           for (int c = 0; c < 32; c += 2) {
             float d0, d1;
@@ -303,8 +307,8 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
           }
       } else {
 #pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2) {
-          const int base = kt * kTile + g * kDqCols + c2 * 32;
+        for (int c2 = 0; c2 < NL; ++c2) {
+          const int base = kt * kTile + g * kCols + c2 * 32;
           const uint32_t see = bits_below(sink, base) | (bits_below(hi, base) & ~bits_below(lo, base));
 #pragma unroll
           for (int c = 0; c < 32; c += 2) {
@@ -315,7 +319,7 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
         }
       }
 #pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) tmem_st16(tmem_lane + kColdS + g * (kDqCols / 2) + c2 * 16, ds[c2]);
+      for (int c2 = 0; c2 < NL; ++c2) tmem_st16(tmem_lane + kColdS + g * (kCols / 2) + c2 * 16, ds[c2]);
       tmem_wait_st();
       tc_fence_before_sync();
       warp_arrive(rb + j % 4, lane);   // dS(j) stored; dP(j) was read before it, so its buffer is free as well
@@ -325,8 +329,8 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
     tc_fence_after_sync();
     const QuadRows rows = quad_rows(a.dq, b, h, a.mask.n, a.heads, D, row);
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-      redo = !win_store_row32(tmem_lane + kColdQ + g * (D / 2) + c * 32, a.scale, live, rows, g * (D / 2) + c * 32, lane) || redo;
+    for (int c = 0; c < D / 32; ++c)
+      if (c % kWinGroups == g) redo = !win_store_row32(tmem_lane + kColdQ + c * 32, a.scale, live, rows, c * 32, lane) || redo;
   }
 
   settle_after_abort(abort_flag);
@@ -338,10 +342,10 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
 // ------------------------------------------------------------------------------------------ dK, dV
 // One row each of dK and dV by the formula: eight lanes per query, four queries at a time.
 template <int D>
-__device__ __noinline__ void win_careful_dkv(const WinBwdArgs& a, int kt, int kvh, int b, int warp, int lane) {
+__device__ __noinline__ void win_careful_dkv(const WinBwdArgs& a, int kt, int kvh, int b, int warp, int lane, int first_row, int end_row) {
   constexpr int kPer = D / 8;
   const int len = a.mask.length(b), part = lane & 7, slot = lane >> 3;
-  for (int r = warp; r < kTile; r += kWinBwdThreads / 32) {
+  for (int r = first_row + warp; r < end_row; r += kWinBwdThreads / 32) {
     const int row = kt * kTile + r;
     if (row >= len) break;
     const float scale_log2 = a.scale * kLog2e;
@@ -401,9 +405,21 @@ __device__ __noinline__ void win_careful_dkv(const WinBwdArgs& a, int kt, int kv
   }
 }
 
+// acc[128 x D] (+)= A[128 x 128] B[128 x D], A as the softmax groups leave it: bf16 pairs, group g's from its own first column on.
+template <int D>
+__device__ __forceinline__ void win_mma_groups(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_smem, bool accumulate) {
+  constexpr uint32_t idesc = make_idesc_bf16(kTile, D, false, true);
+  constexpr int kCols = kTile / kWinGroups;
+  const uint64_t b_desc = desc_mnmajor(b_smem, TileGeom<D>::kBlockBytes);
+#pragma unroll
+  for (int k = 0; k < kTile / 16; ++k)
+    mma_ts(d_tmem, a_tmem + (k * 16 / kCols) * kCols + (k * 16 % kCols) / 2, desc_step(b_desc, k * 2048), idesc, (accumulate || k > 0) ? 1u : 0u);
+}
+
 template <int D>
 __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap& tm_q, const CUtensorMap& tm_do, const CUtensorMap& tm_k,
-                                            const CUtensorMap& tm_v, const WinBwdArgs& a, const int kt, const int kvh, const int b) {
+                                            const CUtensorMap& tm_v, const WinBwdArgs& a, const int kt, const int kvh, const int b,
+                                            const int share, const int shares, float* part) {
   uint8_t* smem = align_1024(smem_raw);
   uint8_t* sK = smem + DkvSmem<D>::kK;
   uint8_t* sV = smem + DkvSmem<D>::kV;
@@ -427,26 +443,12 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
   const int k0 = kt * kTile, len = a.mask.length(b);
   constexpr uint32_t kTmemCols = 512;
   constexpr uint32_t kColSt = 0, kColdPt = 128, kColdK = 256, kColdV = 384;
-  constexpr int kMmaWarp = 8, kTmaWarp = 9;
-  constexpr int kHalfBytes = 64 * 128;
+  constexpr int kMmaWarp = 4 * kWinGroups, kTmaWarp = kMmaWarp + 1, kCols = kTile / kWinGroups, NL = kCols / 32;
   const int g = warp >> 2, r = tid & 127;
 
-  if (k0 >= len) {
-    dependency_wait();
-    if (warp < kMmaWarp) {
-      const QuadRows dk_rows = quad_rows(a.dk, b, kvh, a.mask.n, a.kv_heads, D, k0 + r), dv_rows = quad_rows(a.dv, b, kvh, a.mask.n, a.kv_heads, D, k0 + r);
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        uint4 zero[4] = {};
-        store_quad_rows(zero, dk_rows, g * (D / 2) + c * 32, lane);
-        store_quad_rows(zero, dv_rows, g * (D / 2) + c * 32, lane);
-      }
-    }
-    return;
-  }
   // the query tiles [t0, t0 + per_head) of every head of the group; full: those within [full_first, full_last)
-  int first, last, full_first, full_last;
-  {
+  int first = 0, last = 0, full_first = 0, full_last = 0, t0 = 0, per_head = 0, from = 0, n_tiles = 0;
+  if (k0 < len) {
     const int k_last = min(k0 + kTile, len) - 1;
     int x, y;
     a.mask.queries_of(k0, len, first, last);
@@ -454,16 +456,38 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     if (y > last) last = y;
     full_last = len;
     if (k_last >= a.mask.sink) a.mask.queries_of(max(k0, a.mask.sink), len, x, full_last);
+    t0 = first / kTile;
+    per_head = (last - 1) / kTile + 1 - t0;
+    // this CTA's share of the list of (head, query tile)
+    const int all = per_head * a.group;
+    from = static_cast<int>(static_cast<long long>(all) * share / shares);
+    n_tiles = static_cast<int>(static_cast<long long>(all) * (share + 1) / shares) - from;
   }
-  const int t0 = first / kTile, per_head = (last - 1) / kTile + 1 - t0, n_tiles = per_head * a.group;
+  if (n_tiles == 0) {   // the same for the whole CTA
+    dependency_wait();
+    if (warp < kMmaWarp) {
+      if (part != nullptr) {
+        for (int i = tid; i < 2 * kTile * D / 4; i += 32 * kMmaWarp) reinterpret_cast<float4*>(part)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      } else if (g < 2) {
+        const QuadRows dk_rows = quad_rows(a.dk, b, kvh, a.mask.n, a.kv_heads, D, k0 + r), dv_rows = quad_rows(a.dv, b, kvh, a.mask.n, a.kv_heads, D, k0 + r);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          uint4 zero[4] = {};
+          store_quad_rows(zero, dk_rows, g * (D / 2) + c * 32, lane);
+          store_quad_rows(zero, dv_rows, g * (D / 2) + c * 32, lane);
+        }
+      }
+    }
+    return;
+  }
 
   if (tid == 0) {
     mbar_init(kv_full, 1);
     for (int i = 0; i < kDkvStages; ++i) { mbar_init(q_full + i, 2); mbar_init(q_empty + i, 1); }
     mbar_init(s_full, 1);
     mbar_init(dp_full, 1);
-    mbar_init(p_full, 8);    // one arrival per warp
-    mbar_init(ds_full, 8);
+    mbar_init(p_full, kMmaWarp);    // one arrival per warp
+    mbar_init(ds_full, kMmaWarp);
     mbar_init(acc_full, 1);
     mbar_init(landed, 1);
     *abort_flag = 0;
@@ -487,7 +511,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
       tma_load_tile<D>(sV, &tm_v, kv_full, k0, kvh, b);
     }
     dependency_wait();   // delta
-    int h = kvh * a.group, qt = t0, fixes = 0;
+    int h = kvh * a.group + from / per_head, qt = t0 + from % per_head, fixes = 0;
     for (int i = 0; i < n_tiles; ++i) {
       const int st = i % kDkvStages;
       if (!mbar_wait_ok(q_empty + st, ((i / kDkvStages) & 1) ^ 1, abort_flag)) break;   // no copies once a wait has run out
@@ -539,8 +563,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
       for (int i = 0; ok && i < n_tiles; ++i) {
         if (!mbar_wait_spin(p_full, i & 1, abort_flag)) break;
         tc_fence_after_sync();
-        mma_pb<D, 64>(tmem_base + kColdV, tmem_base + kColSt, do_tile(i), i > 0);
-        mma_pb<D, 64>(tmem_base + kColdV, tmem_base + kColSt + 64, do_tile(i) + kHalfBytes, true);
+        win_mma_groups<D>(tmem_base + kColdV, tmem_base + kColSt, do_tile(i), i > 0);
         if (i + 1 < n_tiles) {
           wait_q(i + 1);
           if (!ok) break;
@@ -549,8 +572,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
         }
         if (!mbar_wait_spin(ds_full, i & 1, abort_flag)) break;
         tc_fence_after_sync();
-        mma_pb<D, 64>(tmem_base + kColdK, tmem_base + kColdPt, q_tile(i), i > 0);
-        mma_pb<D, 64>(tmem_base + kColdK, tmem_base + kColdPt + 64, q_tile(i) + kHalfBytes, true);
+        win_mma_groups<D>(tmem_base + kColdK, tmem_base + kColdPt, q_tile(i), i > 0);
         mma_commit(q_empty + i % kDkvStages);
         if (i + 1 < n_tiles) {
           mma_abT<D>(tmem_base + kColdPt, smem_u32(sV), do_tile(i + 1));
@@ -567,14 +589,14 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     const bool live = key < len;
     int q_first = 0, q_last = 0;
     if (live) a.mask.queries_of(key, len, q_first, q_last);
-    int qt = t0;
+    int qt = t0 + from % per_head;
     for (int i = 0; i < n_tiles; ++i) {
-      const float* stat = sStat + (i % kDkvStages) * 2 * kTile + g * 64;
+      const float* stat = sStat + (i % kDkvStages) * 2 * kTile + g * kCols;
       const bool full = qt * kTile >= full_first && qt * kTile + kTile <= full_last;
-      uint32_t see[2];
+      uint32_t see[NL];
 #pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) {
-        const int base = qt * kTile + g * 64 + c2 * 32;
+      for (int c2 = 0; c2 < NL; ++c2) {
+        const int base = qt * kTile + g * kCols + c2 * 32;
         see[c2] = full ? 0xffffffffu : bits_below(q_last, base) & ~bits_below(q_first, base);
       }
       if (++qt == t0 + per_head) qt = t0;
@@ -582,13 +604,13 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
       ok = mbar_wait_ok(s_full, i & 1, abort_flag) && ok;
       if (!ok) break;
       tc_fence_after_sync();
-      uint32_t s[2][32], pt[32];
-      tmem_ld32(tmem_lane + kColSt + g * 64, s[0]);
-      tmem_ld32(tmem_lane + kColSt + g * 64 + 32, s[1]);
-      tmem_wait_ld();
-      uint64_t p2[2][16];
+      uint32_t s[NL][32], pt[NL][16];
 #pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2)
+      for (int c2 = 0; c2 < NL; ++c2) tmem_ld32(tmem_lane + kColSt + g * kCols + c2 * 32, s[c2]);
+      tmem_wait_ld();
+      uint64_t p2[NL][16];
+#pragma unroll
+      for (int c2 = 0; c2 < NL; ++c2)
 #pragma unroll
         for (int c = 0; c < 32; c += 2) {
           const uint64_t nl2 = *reinterpret_cast<const uint64_t*>(stat + c2 * 32 + c);
@@ -603,18 +625,19 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
             p1 = fast_exp2(x1);
           }
           p2[c2][c >> 1] = f32x2(p0, p1);
-          pt[c2 * 16 + (c >> 1)] = pack_bf16(p0, p1);
+          pt[c2][c >> 1] = pack_bf16(p0, p1);
         }
       if (!full) {
 #pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2)
+        for (int c2 = 0; c2 < NL; ++c2)
 #pragma unroll
           for (int c = 0; c < 32; c += 2) {
             const uint32_t keep = ((see[c2] >> c) & 1u ? 0x0000ffffu : 0u) | ((see[c2] >> (c + 1)) & 1u ? 0xffff0000u : 0u);
-            pt[c2 * 16 + (c >> 1)] &= keep;
+            pt[c2][c >> 1] &= keep;
           }
       }
-      tmem_st32(tmem_lane + kColSt + g * 64, pt);
+#pragma unroll
+      for (int c2 = 0; c2 < NL; ++c2) tmem_st16(tmem_lane + kColSt + g * kCols + c2 * 16, pt[c2]);
       tmem_wait_st();
       tc_fence_before_sync();
       warp_arrive(p_full, lane);
@@ -622,9 +645,9 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
       if (!mbar_wait_ok(dp_full, i & 1, abort_flag)) break;
       tc_fence_after_sync();
 #pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) {
+      for (int c2 = 0; c2 < NL; ++c2) {
         uint32_t dp[32], ds[16];
-        tmem_ld32(tmem_lane + kColdPt + g * 64 + c2 * 32, dp);
+        tmem_ld32(tmem_lane + kColdPt + g * kCols + c2 * 32, dp);
         tmem_wait_ld();
 #pragma unroll
         for (int c = 0; c < 32; c += 2) {
@@ -639,7 +662,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
           for (int c = 0; c < 32; c += 2)
             ds[c >> 1] &= ((see[c2] >> c) & 1u ? 0x0000ffffu : 0u) | ((see[c2] >> (c + 1)) & 1u ? 0xffff0000u : 0u);
         }
-        tmem_st16(tmem_lane + kColdPt + g * 64 + c2 * 16, ds);
+        tmem_st16(tmem_lane + kColdPt + g * kCols + c2 * 16, ds);
       }
       tmem_wait_st();
       tc_fence_before_sync();
@@ -647,19 +670,67 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     }
     mbar_wait(acc_full, 0, abort_flag);
     tc_fence_after_sync();
-    const QuadRows dk_rows = quad_rows(a.dk, b, kvh, a.mask.n, a.kv_heads, D, key), dv_rows = quad_rows(a.dv, b, kvh, a.mask.n, a.kv_heads, D, key);
+    if (part != nullptr) {   // [dK | dV][128][D] in fp32, for win_join_kernel
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      const int col = g * (D / 2) + c * 32;
-      redo = !win_store_row32(tmem_lane + kColdK + col, a.scale, live, dk_rows, col, lane) || redo;
-      redo = !win_store_row32(tmem_lane + kColdV + col, 1.f, live, dv_rows, col, lane) || redo;
+      for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          if (c % kWinGroups != g) continue;
+          uint32_t x[32];
+          tmem_ld32(tmem_lane + (which ? kColdV : kColdK) + c * 32, x);
+          tmem_wait_ld();
+          float4* dst = reinterpret_cast<float4*>(part + (which * kTile + r) * D + c * 32);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            dst[e / 4] = make_float4(__uint_as_float(x[e]), __uint_as_float(x[e + 1]), __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
+        }
+    } else {
+      const QuadRows dk_rows = quad_rows(a.dk, b, kvh, a.mask.n, a.kv_heads, D, key), dv_rows = quad_rows(a.dv, b, kvh, a.mask.n, a.kv_heads, D, key);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        if (c % kWinGroups != g) continue;
+        redo = !win_store_row32(tmem_lane + kColdK + c * 32, a.scale, live, dk_rows, c * 32, lane) || redo;
+        redo = !win_store_row32(tmem_lane + kColdV + c * 32, 1.f, live, dv_rows, c * 32, lane) || redo;
+      }
     }
   }
 
   settle_after_abort(abort_flag);
   tc_fence_before_sync();
-  if (__syncthreads_or(redo) && !*abort_flag) win_careful_dkv<D>(a, kt, kvh, b, warp, lane);
+  if (__syncthreads_or(redo) && !*abort_flag) win_careful_dkv<D>(a, kt, kvh, b, warp, lane, 0, kTile);
   if (warp == kMmaWarp) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+// Joins the parts of the sinks' key tiles, in their order; rows whose sums are not finite are done again by the formula.  grid.x: (key
+// tile, list), grid.y: kJoinRows rows of it.
+constexpr int kJoinRows = 8;
+template <int D>
+__global__ void __launch_bounds__(kWinBwdThreads) win_join_kernel(const WinBwdArgs a) {
+  dependency_wait();
+  const int i = blockIdx.x, kt = i / a.kv_lists, list = i - kt * a.kv_lists, b = list / a.kv_heads, kvh = list - b * a.kv_heads;
+  const int len = a.mask.length(b), row0 = blockIdx.y * kJoinRows;
+  constexpr int kVecs = kJoinRows * D / 4;           // of dK, and as many of dV
+  const float4* parts = reinterpret_cast<const float4*>(a.parts) + static_cast<size_t>(i) * a.shares * (2 * kTile * D / 4) + row0 * (D / 4);
+  bool redo = false;
+  for (int x = threadIdx.x; x < 2 * kVecs; x += kWinBwdThreads) {
+    const int which = x / kVecs, in = x - which * kVecs;
+    const float4* src = parts + which * (kTile * D / 4) + in;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < a.shares; ++p) {
+      const float4 v = src[static_cast<size_t>(p) * (2 * kTile * D / 4)];
+      sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    }
+    const int key = kt * kTile + row0 + in / (D / 4), col = in % (D / 4) * 4;
+    if (key >= a.mask.n) continue;
+    const bool live = key < len;
+    const float m = which ? 1.f : a.scale;
+    const float chk = sum.x * m * 0.f + sum.y * m * 0.f + sum.z * m * 0.f + sum.w * m * 0.f;
+    redo = redo || (live && !(chk == 0.f));
+    const uint2 out = live ? make_uint2(pack_bf16(sum.x * m, sum.y * m), pack_bf16(sum.z * m, sum.w * m)) : make_uint2(0u, 0u);
+    *reinterpret_cast<uint2*>((which ? a.dv : a.dk) + ((static_cast<size_t>(b) * a.mask.n + key) * a.kv_heads + kvh) * D + col) = out;
+  }
+  if (__syncthreads_or(redo)) win_careful_dkv<D>(a, kt, kvh, b, threadIdx.x >> 5, threadIdx.x & 31, row0, row0 + kJoinRows);
 }
 
 template <int D>
@@ -668,15 +739,22 @@ window_attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                        const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                        const __grid_constant__ WinBwdArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  // key tiles forwards (the earlier ones are seen by more queries), query tiles backwards (the later ones see more keys)
-  int i = blockIdx.x - a.front * a.kv_lists;
-  if (i >= 0 && i < a.lists * a.tiles) {
-    const int back = i / a.lists, bh = i - back * a.lists;
-    win_bwd_dq<D>(smem_raw, tm_k, tm_v, tm_do, a, a.tiles - 1 - back, bh % a.heads, bh / a.heads);
+  // key tiles forwards (the earlier ones are seen by more queries), then query tiles backwards (the later ones see more keys)
+  const int front = a.front * a.kv_lists * a.shares;   // CTAs of the sinks' key tiles, `shares` to a tile
+  const int behind = a.kv_lists * (a.tiles - a.front);
+  int i = blockIdx.x;
+  if (i < front) {
+    const int share = i % a.shares, x = i / a.shares, kt = x / a.kv_lists, list = x - kt * a.kv_lists;
+    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, kt, list % a.kv_heads, list / a.kv_heads, share, a.shares,
+                   a.shares > 1 ? a.parts + static_cast<size_t>(i) * (2 * kTile * D) : nullptr);
+  } else if ((i -= front) < behind) {
+    int tile, list;
+    a.k_order.place(i, tile, list);
+    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, a.front + tile, list % a.kv_heads, list / a.kv_heads, 0, 1, nullptr);
   } else {
-    i = i < 0 ? blockIdx.x : blockIdx.x - a.lists * a.tiles;
-    const int kt = i / a.kv_lists, bh = i - kt * a.kv_lists;
-    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, kt, bh % a.kv_heads, bh / a.kv_heads);
+    int tile, list;
+    a.q_order.place(i - behind, tile, list);
+    win_bwd_dq<D>(smem_raw, tm_k, tm_v, tm_do, a, a.tiles - 1 - tile, list % a.heads, list / a.heads);
   }
 }
 template <int D> constexpr int window_bwd_smem() {

@@ -71,6 +71,30 @@ struct WinTiles {
   }
 };
 
+// Work in the order in which CTAs take it: `lists` (sample, head) lists of `tiles` tiles each.  Tile by tile over all lists the
+// long ones come first and the end is even; list by list the CTAs that run together share K and V in L2 (5 % on a video's 12 lists of
+// 256 tiles).  So: groups of lists of one size, one after the other, tile by tile within, eight rounds of 148 CTAs and more in each.
+struct WinOrder {
+  int lists, tiles, per_group;
+  __host__ void set(int lists_, int tiles_) {
+    lists = lists_;
+    tiles = tiles_;
+    const long long groups = static_cast<long long>(lists) * tiles / (8 * 148);
+    per_group = groups <= 1 ? lists : static_cast<int>((lists + groups - 1) / groups);
+  }
+  __device__ __forceinline__ void place(int i, int& tile, int& list) const {
+    int first = 0, here = lists;
+    if (per_group < lists) {
+      const int group = i / (per_group * tiles);
+      first = group * per_group;
+      i -= first * tiles;
+      here = min(per_group, lists - first);
+    }
+    tile = i / here;
+    list = first + i - tile * here;
+  }
+};
+
 struct WinStrides {
   long long b, t, h;     // in elements
 };

@@ -30,7 +30,7 @@ struct WinFwdArgs {
   float* lse;              // [B, H, n], may be null
   WinMask mask;
   int heads, group;        // group: heads that share K and V
-  int lists, q_tiles;      // lists = batch * heads
+  WinOrder order;
   float scale, scale_log2;
   int careful;             // 1: the second pass only
 };
@@ -55,14 +55,15 @@ template <int D> struct WinFwdSmem {
   static constexpr int kTotal = kRedo + kWinMaxUnits / 8 + 1024;
 };
 
-// Unit id -> query tile, head, sample.  Ids count the (sample, head) lists fastest and the query tiles backwards: the long ones first.
+// Unit id -> query tile, head, sample (WinOrder, the query tiles backwards: the long ones first).
 struct WinUnit {
   int qt, h, b;
   __device__ __forceinline__ WinUnit(const WinFwdArgs& a, int id) {
-    const int back = id / a.lists, bh = id - back * a.lists;
-    qt = a.q_tiles - 1 - back;
-    b = bh / a.heads;
-    h = bh - b * a.heads;
+    int tile, list;
+    a.order.place(id, tile, list);
+    qt = a.order.tiles - 1 - tile;
+    b = list / a.heads;
+    h = list - b * a.heads;
   }
 };
 
