@@ -182,7 +182,7 @@ astro_status_t astro_chunk_attn_bwd_dkv(const void* q, const void* k_chunk, cons
  * parents: device int32 [dst cache_batch], the sample of src that each sample of dst continues; null: sample b
  * continues sample b, or sample 0 of a one-sample src.  A parent outside src leaves zeros in the copied frames.
  * dst's frames_seen becomes src's, or the number of copied frames where repeats make that larger (a cache has seen at least
- * the frames it holds).  ASTRO_ERR_SHAPE: other heads, head_dim or tokens_per_frame; parents null and
+ * the frames it holds).  ASTRO_ERR_SHAPE: other heads, head_dim or tokens_per_frame, caches of different kinds (16 and 8 bits); parents null and
  * cache batches that are neither equal nor 1; a frame index that src does not hold; storage of dst that overlaps src's.
  * ASTRO_ERR_CAPACITY: more frames than dst holds.  Calls on dst and src obey the rules of calls that change a cache
  * (dst) and of calls that take it as const (src). */
@@ -255,10 +255,10 @@ astro_status_t astro_rope_apply_check(const astro_rope_t* rope, int inverse, con
  *   e4m3(x_d * 2^-e) for every element, rounded to nearest even; an infinity or NaN becomes NaN, the others are not touched by it.
  * (Elements of 248 * 2^120 and more, which would round beyond the largest float, are held as 240 * 2^120.)
  * What it stands for, e4m3 value times 2^e, is a bf16 number exactly: reading it back in bf16 or fp32 rounds nothing.
- * The handle is an astro_kvcache_t: destroy, reset, evict, query, get_state, set_state, key_segments, export and append (which takes
- * bf16) do for it what they do for the other kind.  The calls that read a 16-bit cache's rows (astro_chunk_attn_fwd and _bwd,
- * astro_block_pool, astro_block_select, astro_sparse_attn_*, astro_kvcache_fork) answer ASTRO_ERR_SHAPE to it, and the calls below
- * to a 16-bit one. */
+ * The handle is an astro_kvcache_t: destroy, reset, evict, query, get_state, set_state, key_segments, export, append (which takes
+ * bf16) and fork (from one such cache into another) do for it what they do for the other kind.  The calls that read a 16-bit
+ * cache's rows (astro_chunk_attn_*, astro_block_pool, astro_block_select, astro_sparse_attn_*) answer ASTRO_ERR_SHAPE to
+ * it, and the calls below to a 16-bit one. */
 /* Bytes for K (and the same again for V); 0 for an invalid descriptor. */
 size_t astro_kvcache8_storage_bytes(const astro_kvcache_desc_t* desc);
 /* As astro_kvcache_create; the layout inside the storage is private. */

@@ -1484,12 +1484,14 @@ astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* s
   const auto &a = src->d, &d = dst->d;
   const int held = src->sink_held + src->win_held;
   if (!frames && n_frames == -1) n_frames = held;
-  if (n_frames < 0 || dst == src || src->bits != 16 || dst->bits != 16 || a.heads != d.heads || a.head_dim != d.head_dim ||
+  if (n_frames < 0 || dst == src || src->bits != dst->bits || a.heads != d.heads || a.head_dim != d.head_dim ||
       a.tokens_per_frame != d.tokens_per_frame)
     return ASTRO_ERR_SHAPE;
   if (!parents && a.cache_batch != 1 && a.cache_batch != d.cache_batch) return ASTRO_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(parents) & 3u) return ASTRO_ERR_ALIGN;
-  const size_t src_bytes = astro_kvcache_storage_bytes(&a), dst_bytes = astro_kvcache_storage_bytes(&d);
+  const bool eight = src->bits == 8;
+  const size_t src_bytes = eight ? astro_kvcache8_storage_bytes(&a) : astro_kvcache_storage_bytes(&a);
+  const size_t dst_bytes = eight ? astro_kvcache8_storage_bytes(&d) : astro_kvcache_storage_bytes(&d);
   const uintptr_t from[2] = {reinterpret_cast<uintptr_t>(src->k), reinterpret_cast<uintptr_t>(src->v)};
   const uintptr_t to[2] = {reinterpret_cast<uintptr_t>(dst->k), reinterpret_cast<uintptr_t>(dst->v)};
   for (uintptr_t f : from)
@@ -1498,7 +1500,7 @@ astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* s
   if (n_frames > static_cast<long long>(d.sink_frames) + d.window_frames) return ASTRO_ERR_CAPACITY;
   for (int j = 0; frames && j < n_frames; ++j)
     if (frames[j] < 0 || frames[j] >= held) return ASTRO_ERR_SHAPE;
-  const long long frame_vecs = static_cast<long long>(d.tokens_per_frame) * d.head_dim / 8;
+  const long long frame_vecs = static_cast<long long>(d.tokens_per_frame) * d.head_dim / (eight ? 16 : 8);
   const long long pieces = (frame_vecs + kForkThreads * kForkVecsPerThread - 1) / (kForkThreads * kForkVecsPerThread);
   const long long per_frame = 2ll * d.cache_batch * d.heads * pieces;
   if (frame_vecs > 0x3fffffffLL || per_frame > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
@@ -1520,6 +1522,15 @@ astro_status_t astro_kvcache_fork(astro_kvcache_t* dst, const astro_kvcache_t* s
           static_cast<const uint4*>(src->k), static_cast<const uint4*>(src->v), static_cast<uint4*>(dst->k),
           static_cast<uint4*>(dst->v), parents, map, a.cache_batch, d.cache_batch, d.heads, static_cast<int>(frame_vecs),
           static_cast<int>(pieces), a.sink_frames + a.window_frames, d.sink_frames + d.window_frames);
+      if (eight) {
+        ForkSlots slots;
+        std::memcpy(slots.from, map.from, sizeof(int) * map.n);
+        slots.first_to = f0;
+        const QuantTensors x = quant_tensors(src, 0), y = quant_tensors(dst, 0);
+        cache8_fork_exps_kernel<<<static_cast<unsigned>(2ll * map.n * d.heads * d.cache_batch), 128, 0, static_cast<cudaStream_t>(stream)>>>(
+            x.k_exp, x.v_exp, y.k_exp, y.v_exp, parents, slots, a.cache_batch, d.cache_batch, d.heads, d.tokens_per_frame,
+            a.sink_frames + a.window_frames, d.sink_frames + d.window_frames);
+      }
     }
     if ((s = launch_status()) != ASTRO_OK) return s;
   }

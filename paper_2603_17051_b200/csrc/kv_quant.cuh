@@ -256,4 +256,29 @@ __global__ void __launch_bounds__(kQuantThreads) cache8_read_kernel(const QuantT
   }
 }
 
+// Exponent bytes of frames copied into another cache (fork; the codes go the way of every cache's bytes): frame first_to + j of
+// sample b takes slot from.slot[j] of sample parents[b].  A parent outside the source leaves zeros, whose rows stand for zeros.
+// grid.x = ((frame, head) * 2 + (0: K, 1: V)) * batch + b
+struct ForkSlots {
+  int from[32];
+  int first_to;
+};
+__global__ void __launch_bounds__(128)
+cache8_fork_exps_kernel(const uint8_t* __restrict__ k_src, const uint8_t* __restrict__ v_src, uint8_t* __restrict__ k_dst,
+                        uint8_t* __restrict__ v_dst, const int* __restrict__ parents, const ForkSlots slots, const int source_batch,
+                        const int batch, const int heads, const int tokens_per_frame, const int src_slots, const int dst_slots) {
+  unsigned i = blockIdx.x;
+  const int b = i % batch;
+  i /= batch;
+  const bool is_v = i & 1;
+  i >>= 1;
+  const int h = i % heads, j = i / heads;
+  const int parent = parents ? parents[b] : (source_batch == 1 ? 0 : b);
+  const bool there = parent >= 0 && parent < source_batch;
+  const uint8_t* src = (is_v ? v_src : k_src) +
+                       ((static_cast<long long>(there ? parent : 0) * heads + h) * src_slots + slots.from[j]) * tokens_per_frame;
+  uint8_t* dst = (is_v ? v_dst : k_dst) + ((static_cast<long long>(b) * heads + h) * dst_slots + slots.first_to + j) * tokens_per_frame;
+  for (int t = threadIdx.x; t < tokens_per_frame; t += 128) dst[t] = there ? src[t] : 0;
+}
+
 }  // namespace astro

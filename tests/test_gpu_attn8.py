@@ -182,3 +182,51 @@ def test_a_captured_call_and_one_on_another_stream():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((*want, *grads), (*inside, *inside_grads)))
         del graph
+
+
+@pytest.mark.parametrize("n_q,n_kc", [(1, 1), (3, 0), (5, 5), (17, 20), (64, 64)])
+@pytest.mark.parametrize("B", [2, 7, 33])
+def test_queries_of_many_samples_over_one_prefix(n_q, n_kc, B):
+    """They are rows of one list; a sample's chunk is its own, whatever the others' hold."""
+    torch, A = modules()
+    cache = filled(torch, A, 1, 2, 64, 1, 3, 400, 350, 100, B)
+    q, kc, vc, _ = tensors(torch, B, n_q, n_kc, 2, 64, n_q + B)
+    o, lse = compare(torch, A, cache, q, kc, vc, 0.125)
+    if n_kc:
+        kc, vc = kc.clone(), vc.clone()
+        kc[0] = float("nan")
+        vc[0] = float("inf")
+        bad, bad_lse = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.125)
+        assert bad[0].isnan().any() and torch.equal(bad[1:], o[1:]) and torch.equal(bad_lse[1:], lse[1:])
+
+
+def test_sizes_of_queries_keys_and_weights_that_fp16_does_not_hold():
+    """Queries of 2^-60 and 2^60, keys the other way round, one sample's scores far from another's."""
+    torch, A = modules()
+    g = torch.Generator(device="cuda").manual_seed(12)
+    cache = A.astro_kvcache8_create(1, 2, 128, 100, 0, 2)
+    up = torch.tensor([2.0 ** 60, 2.0 ** -60], device="cuda").view(1, 1, 2, 1)
+    k = (torch.randn(1, 200, 2, 128, generator=g, device="cuda") * up).bfloat16()
+    v = torch.randn(1, 200, 2, 128, generator=g, device="cuda").bfloat16()
+    A.astro_kvcache8_append(cache, k, v, 2)
+    for n_q in (1, 4, 9):
+        q = (torch.randn(2, n_q, 2, 128, generator=g, device="cuda") / up).bfloat16()
+        q[0, 0, 0, 5] = 0.0
+        compare(torch, A, cache, q, None, None, 0.09)
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of 2.4 million tokens of 2048 bytes."""
+    torch, A = modules()
+    H, D, L = 16, 128, 2400000
+    cache = A.astro_kvcache8_create(1, H, D, 1, 0, L)
+    n = 4000
+    A.astro_kvcache_set_state(cache, A.KVCacheState(0, L - n, 0, 0))
+    A.astro_kvcache_set_state(cache, A.KVCacheState(0, L - n, 1, 1))
+    g = torch.Generator(device="cuda").manual_seed(13)
+    k, v = (torch.randn(1, 2 * n, H, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    A.astro_kvcache8_append(cache, k[:, 1:].contiguous(), v[:, 1:].contiguous(), 2 * n - 1)
+    A.astro_kvcache_evict(cache, 1)                              # the slot that was never written
+    for n_q in (2, 70):
+        q, kc, vc, _ = tensors(torch, 1, n_q, 3, H, D, 14)
+        compare(torch, A, cache, q, kc, vc, D ** -0.5, heads=(0, 15))

@@ -143,3 +143,19 @@ def test_offsets_beyond_32_bits():
     got = A.astro_kvcache8_read(cache)
     assert same(got[0], want(k)) and same(got[1], want(v))
     A.astro_last_device_status()
+
+
+def test_forks_copy_rows_as_they_are():
+    torch, A = modules()
+    H, D, T = 3, 64, 7
+    src = A.astro_kvcache8_create(2, H, D, T, 1, 5)
+    k, v = (rows(torch, (2, 5 * T, H, D), torch.bfloat16, s) for s in (3, 4))
+    A.astro_kvcache8_append(src, k, v, 5)
+    dst = A.astro_kvcache8_create(4, H, D, T, 2, 40)
+    parents = torch.tensor([1, 0, 7, 1], dtype=torch.int32, device="cuda")
+    frames = [3, 0, 4] + [2] * 36                                # more than one launch takes
+    A.astro_kvcache_fork(dst, src, parents=parents, frames=frames)
+    at = torch.cat([torch.arange(f * T, (f + 1) * T) for f in frames])
+    for got, x in zip(A.astro_kvcache8_read(dst, dtype=torch.float32), (k, v)):
+        ref = want(x[:, at])
+        assert same(got[[0, 1, 3]], ref[[1, 0, 1]]) and not got[2].any()

@@ -272,3 +272,40 @@ def test_a_captured_call_one_on_another_stream_and_an_empty_one():
     none = q[:, :0].contiguous()
     o, lse = A.astro_window_attn_fwd(none, k[:, :0].contiguous(), v[:, :0].contiguous(), 0.1)
     assert o.shape == (2, 0, 4, 128) and lse.shape == (2, 4, 0)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lengths", [None, (4200,), (900,), (0,), (4195,)])
+def test_sinks_that_many_queries_of_many_heads_see(D, lengths):
+    """The sinks' key tiles are divided among CTAs and joined."""
+    torch, A = modules()
+    q, k, v, d_o = tensors(torch, 1, 4200, 12, 1, D, 15)
+    compare(torch, A, q, k, v, d_o, 1, 256, 100, lengths)
+
+
+def test_nan_in_a_divided_key_tile():
+    """In a query that the sinks' keys see, and in one that a key of the same tile does not see."""
+    torch, A = modules()
+    n, D = 4200, 64
+    q, k, v, d_o = tensors(torch, 1, n, 8, 1, D, 16)
+    form = dict(block_tokens=1, window_tokens=256, sink_tokens=40)
+    o, lse = A.astro_window_attn_fwd(q, k, v, 0.125, **form)
+    d_o[0, 3000, 2, 5] = float("nan")
+    _, dk, dv = A.astro_window_attn_bwd(q, k, v, o, lse, d_o, 0.125, **form)
+    A.astro_last_device_status()
+    i = torch.arange(n, device="cuda")
+    seen = (i < 40) | ((i > 3000 - 256) & (i <= 3000))
+    assert dk[0, seen].isnan().any(-1).all() and dk[0, ~seen].isfinite().all()
+    assert dv[0, seen][..., 5].isnan().all() and dv[0, ~seen].isfinite().all()
+
+
+def test_units_of_one_tile():
+    """A CTA's look-ahead spans several units: short sequences, many of them, dead ones among them."""
+    torch, A = modules()
+    B, n, H = 500, 100, 3
+    g = torch.Generator(device="cuda").manual_seed(17)
+    q, k, v, d_o = tensors(torch, B, n, H, 1, 64, 17)
+    lengths = torch.randint(0, n + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    lengths[::7] = 0
+    at = {(b, h) for b in range(0, B, 17) for h in range(H)} | {(b, h) for b in (7, 499) for h in range(H)}
+    compare(torch, A, q, k, v, d_o, 10, 30, 5, lengths.tolist(), at=at)
