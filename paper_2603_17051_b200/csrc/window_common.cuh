@@ -53,12 +53,6 @@ struct WinTiles {
     full_lo = lo_max <= sink_min ? 0 : (lo_max + kTile - 1) / kTile;
     full_hi = hi_min / kTile;
   }
-  __host__ __device__ __forceinline__ void set_dead(int tile) {   // one tile, of which nothing is seen
-    a1 = 0;
-    w0 = tile;
-    w1 = tile + 1;
-    full_sink = full_lo = full_hi = 0;
-  }
   __host__ __device__ __forceinline__ int count() const { return a1 + w1 - w0; }
   __host__ __device__ __forceinline__ int first() const { return a1 > 0 ? 0 : w0; }
   __host__ __device__ __forceinline__ int next(int tile) const { return tile + 1 == a1 ? w0 : tile + 1; }   // from w1 on: none left

@@ -35,7 +35,7 @@ struct WinFwdArgs {
   int careful;             // 1: the second pass only
 };
 
-constexpr int kWinMaxUnits = 1024;                       // of one CTA; it asks for no more
+constexpr int kWinMaxUnits = 1024;                       // of one CTA; it asks no more often
 constexpr int kWinThreads = 128 * kFwdGroups + 32 * (4 + kFwdEpiWarps);   // + MMA, units, K, V
 constexpr int kWinBarSlots = 40;
 
@@ -51,8 +51,8 @@ template <int D> struct WinFwdSmem {
   static constexpr int kHolder = kBars + kWinBarSlots * 8;                     // tensor memory's address, abort flag
   static constexpr int kAnswer = kHolder + 16;                                 // of the queue of units, 16 bytes
   static constexpr int kUnits = kAnswer + 16;
-  static constexpr int kRedo = kUnits + kWinMaxUnits * static_cast<int>(sizeof(WinUnitInfo));
-  static constexpr int kTotal = kRedo + kWinMaxUnits / 8 + 1024;
+  static constexpr int kRedo = kUnits + (kWinMaxUnits + 2) * static_cast<int>(sizeof(WinUnitInfo));
+  static constexpr int kTotal = kRedo + (kWinMaxUnits / 32 + 1) * 4 + 1024;
 };
 
 // Unit id -> query tile, head, sample (WinOrder, the query tiles backwards: the long ones first).
@@ -103,13 +103,13 @@ __device__ __forceinline__ bool win_await_unit(const WinCta<D>& c, const WinBars
   return u.id >= 0;
 }
 
+// A listed unit's tiles: it has a query.
 __device__ __forceinline__ void win_tiles(const WinFwdArgs& a, const WinUnit& u, int& len, WinTiles& t) {
   len = a.mask.length(u.b);
-  if (u.qt * kTile < len) t.set(a.mask, u.qt * kTile, len);
-  else t.set_dead(u.qt);
+  t.set(a.mask, u.qt * kTile, len);
 }
 
-// ---------------------------------------------------------------------------------- units (one thread)
+// ---------------------------------------------------------------------------------- units (a warp)
 // Asks the hardware for a CTA that has not been launched yet and takes its place.
 __device__ __forceinline__ void queue_ask(void* answer, uint64_t* bar) {
   asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)),
@@ -134,37 +134,65 @@ __device__ __forceinline__ int queue_answer(const void* answer) {
   return id;
 }
 
+// A unit without a query: zeros and -infinity.
 template <int D>
-__device__ __forceinline__ void win_take_units(const WinCta<D>& c, const WinFwdArgs& a, const WinBars& bar, void* answer) {
+__device__ __forceinline__ void win_clear_unit(const WinFwdArgs& a, const WinUnit& u, int lane) {
+  const int rows = min(kTile, a.mask.n - u.qt * kTile);
+  const size_t first = static_cast<size_t>(u.b) * a.mask.n + u.qt * kTile;
+  for (int i = lane; i < rows * (D / 8); i += 32)
+    *reinterpret_cast<uint4*>(a.o + ((first + i / (D / 8)) * a.heads + u.h) * D + i % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+  if (a.lse != nullptr)
+    for (int i = lane; i < rows; i += 32)
+      a.lse[(static_cast<size_t>(u.b) * a.heads + u.h) * a.mask.n + u.qt * kTile + i] = -INFINITY;
+}
+
+// The stream's units: the CTA's own, then what the queue gives; those without a query are dealt with here and never listed.
+template <int D>
+__device__ __forceinline__ void win_take_units(const WinCta<D>& c, const WinFwdArgs& a, const WinBars& bar, void* answer, int lane) {
   int tiles = 0;   // of the unit listed last
-  auto list = [&](int n, int id) {
-    tiles = 0;
-    if (id >= 0) {
-      int len;
-      WinTiles t;
-      win_tiles(a, WinUnit(a, id), len, t);
-      tiles = t.count();
-    }
-    c.units[n].id = id;
-    c.units[n].tiles = tiles;
-    mbar_arrive(bar.listed + n % 4);
-  };
-  list(0, blockIdx.x);
-  int done = 0;    // units known to be done
-  for (int n = 1;; ++n) {
-    // Unit n is asked for when unit n - 2 is done.  Where unit n - 1 is a single tile that would be too late: the last tile of
-    // unit n - 2 waits for the K of two tiles on, unit n's.
-    bool ok = true;
-    for (const int before = tiles == 1 ? n - 2 : n - 1; ok && done < before; ++done)
-      ok = mbar_wait_spin(bar.done + done % 4, (done / 4) & 1, c.abort_flag);
+  int asked = 0;
+  // the next unit of the queue, -1 if there is none
+  auto ask = [&]() {
+    if (asked == kWinMaxUnits) return -1;
     int id = -1;
-    if (ok && n < kWinMaxUnits - 1) {
+    if (lane == 0) {
       mbar_arrive_expect_tx(bar.answer, 16);
       queue_ask(answer, bar.answer);
-      if (mbar_wait_spin(bar.answer, (n - 1) & 1, c.abort_flag)) id = queue_answer(answer);
-      fence_proxy_async_smem();   // the next answer is written behind this reading
     }
-    list(n, id);
+    __syncwarp();
+    if (mbar_wait_ok(bar.answer, asked & 1, c.abort_flag)) id = queue_answer(answer);
+    fence_proxy_async_smem();   // the next answer is written behind this reading
+    __syncwarp();
+    ++asked;
+    return id;
+  };
+  int id = blockIdx.x, done = 0;   // done: units known to be
+  for (int n = 0;; ++n) {
+    if (n > 0) {
+      // Unit n is asked for when unit n - 2 is done.  Where unit n - 1 is a single tile that would be too late: the last tile of
+      // unit n - 2 waits for the K of two tiles on, unit n's.
+      bool ok = true;
+      for (const int before = tiles == 1 ? n - 2 : n - 1; ok && done < before; ++done)
+        ok = mbar_wait_ok(bar.done + done % 4, (done / 4) & 1, c.abort_flag);
+      id = ok ? ask() : -1;
+    }
+    for (; id >= 0; id = ask()) {
+      const WinUnit u(a, id);
+      if (u.qt * kTile < a.mask.length(u.b)) break;
+      win_clear_unit<D>(a, u, lane);
+    }
+    tiles = 0;
+    if (id >= 0) {
+      const WinUnit u(a, id);
+      WinTiles t;
+      t.set(a.mask, u.qt * kTile, a.mask.length(u.b));
+      tiles = t.count();
+    }
+    if (lane == 0) {
+      c.units[n].id = id;
+      c.units[n].tiles = tiles;
+      mbar_arrive(bar.listed + n % 4);
+    }
     if (id < 0) break;
   }
 }
@@ -644,7 +672,7 @@ window_attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
     fence_mbar_init();
   }
   if (tid == 0) *c.abort_flag = 0;
-  if (tid < kWinMaxUnits / 32) c.redo[tid] = 0;
+  if (tid <= kWinMaxUnits / 32) c.redo[tid] = 0;
   fence_proxy_async_smem();
   if (warp == kMmaWarp) {
     tmem_alloc(tmem_holder, kTmemCols);
@@ -658,7 +686,7 @@ window_attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
   bool asked = false;
   if (warp < kMmaWarp) asked = win_softmax<D>(c, a, bar, warp, tid & 127);
   else if (warp == kMmaWarp) { if (lane == 0) win_issue<D>(c, bar); }
-  else if (warp == kUnitWarp) { if (lane == 0) win_take_units<D>(c, a, bar, smem + WinFwdSmem<D>::kAnswer); }
+  else if (warp == kUnitWarp) win_take_units<D>(c, a, bar, smem + WinFwdSmem<D>::kAnswer, lane);
   else if (warp == kKWarp) { if (lane == 0) win_load_k<D>(c, a, &tm_k, bar); }
   else if (warp == kVWarp) win_load_v<D>(c, a, &tm_v, bar, lane);
   else asked = win_epilogue<D>(c, a, bar, warp, lane);
@@ -666,7 +694,7 @@ window_attn_fwd_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
   // every MMA has finished by now: the epilogue warps waited for the last one
   tc_fence_before_sync();
   if (__syncthreads_or(asked) && !*c.abort_flag) {
-    for (int n = 0; n < kWinMaxUnits && c.units[n].id >= 0; ++n)
+    for (int n = 0; c.units[n].id >= 0; ++n)
       if ((c.redo[n >> 5] >> (n & 31)) & 1u) win_careful_unit<D>(a, c.units[n].id, warp, lane);
   }
   settle_after_abort(c.abort_flag);
