@@ -416,33 +416,45 @@ __device__ __forceinline__ void win_mma_groups(uint32_t d_tmem, uint32_t a_tmem,
     mma_ts(d_tmem, a_tmem + (k * 16 / kCols) * kCols + (k * 16 % kCols) / 2, desc_step(b_desc, k * 2048), idesc, (accumulate || k > 0) ? 1u : 0u);
 }
 
+// The dense kernel's hand-offs (a tile takes 2750 clocks: P^T 1170, dV and the next S^T 1024 behind it, the rest on the way), and at
+// head_dim 64, where tensor memory has room, a second S^T buffer: S^T of the tile after the next is issued behind dV of this one, so
+// the softmax warps never wait for it.
+//   TMEM columns, head_dim 128:  S^T / P^T [0, 128)   dP^T / dS^T [128, 256)   dK [256, 384)   dV [384, 512)
+//                 head_dim 64:   S^T / P^T [0, 256)   dP^T / dS^T [256, 384)   dK [384, 448)   dV [448, 512)
+template <int D> struct WinDkvSmem {
+  static constexpr int kSBufs = D == 128 ? 1 : 2;
+  static constexpr int kStages = D == 128 ? 2 : 4;                        // of (Q, dO)
+  static constexpr int kK = 0;
+  static constexpr int kV = TileGeom<D>::kBytes;
+  static constexpr int kQ = 2 * TileGeom<D>::kBytes;
+  static constexpr int kdO = kQ + kStages * TileGeom<D>::kBytes;
+  static constexpr int kStats = kdO + kStages * TileGeom<D>::kBytes;      // float [stages][2][128]: -lse*log2e, -delta
+  static constexpr int kBars = kStats + kStages * 2 * kTile * 4;
+  static constexpr int kTotal = kBars + 256 + 1024;
+};
+
 template <int D>
 __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap& tm_q, const CUtensorMap& tm_do, const CUtensorMap& tm_k,
                                             const CUtensorMap& tm_v, const WinBwdArgs& a, const int kt, const int kvh, const int b,
                                             const int share, const int shares, float* part) {
+  using S = WinDkvSmem<D>;
+  constexpr int kStages = S::kStages, kSBufs = S::kSBufs;
   uint8_t* smem = align_1024(smem_raw);
-  uint8_t* sK = smem + DkvSmem<D>::kK;
-  uint8_t* sV = smem + DkvSmem<D>::kV;
-  uint8_t* sQ = smem + DkvSmem<D>::kQ;
-  uint8_t* sdO = smem + DkvSmem<D>::kdO;
-  float* sStat = reinterpret_cast<float*>(smem + DkvSmem<D>::kStats);   // [stage][-LSE*log2e | -delta][128 queries]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + DkvSmem<D>::kBars);
-  uint64_t* kv_full = bars;
-  uint64_t* q_full = bars + 1;
-  uint64_t* q_empty = q_full + kDkvStages;
-  uint64_t* s_full = q_empty + kDkvStages;
-  uint64_t* dp_full = s_full + 1;
-  uint64_t* p_full = dp_full + 1;
-  uint64_t* ds_full = p_full + 1;
-  uint64_t* acc_full = ds_full + 1;
-  uint64_t* landed = acc_full + 1;
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(landed + 1);
+  uint8_t* sK = smem + S::kK;
+  uint8_t* sV = smem + S::kV;
+  uint8_t* sQ = smem + S::kQ;
+  uint8_t* sdO = smem + S::kdO;
+  float* sStat = reinterpret_cast<float*>(smem + S::kStats);   // [stage][-LSE*log2e | -delta][128 queries]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBars);
+  uint64_t *kv_full = bars, *s_full = bars + 1 /* [2] */, *dp_full = bars + 3, *p_full = bars + 4, *ds_full = bars + 5, *acc_full = bars + 6,
+           *landed = bars + 7, *q_full = bars + 8, *q_empty = q_full + kStages;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(q_empty + kStages);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int k0 = kt * kTile, len = a.mask.length(b);
   constexpr uint32_t kTmemCols = 512;
-  constexpr uint32_t kColSt = 0, kColdPt = 128, kColdK = 256, kColdV = 384;
+  constexpr uint32_t kColSt = 0, kColdPt = 128 * kSBufs, kColdK = kColdPt + 128, kColdV = kColdK + D;
   constexpr int kMmaWarp = 4 * kWinGroups, kTmaWarp = kMmaWarp + 1, kCols = kTile / kWinGroups, NL = kCols / 32;
   const int g = warp >> 2, r = tid & 127;
 
@@ -481,19 +493,13 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     return;
   }
 
-  if (tid == 0) {
-    mbar_init(kv_full, 1);
-    for (int i = 0; i < kDkvStages; ++i) { mbar_init(q_full + i, 2); mbar_init(q_empty + i, 1); }
-    mbar_init(s_full, 1);
-    mbar_init(dp_full, 1);
-    mbar_init(p_full, kMmaWarp);    // one arrival per warp
-    mbar_init(ds_full, kMmaWarp);
-    mbar_init(acc_full, 1);
-    mbar_init(landed, 1);
-    *abort_flag = 0;
+  if (tid < 8 + 2 * kStages) {
+    // q_full: a stage's bytes and the constants of its queries; p_full, ds_full: one arrival per warp
+    mbar_init(bars + tid, tid >= 8 && tid < 8 + kStages ? 2 : tid == 4 || tid == 5 ? kMmaWarp : 1);
     fence_mbar_init();
-    fence_proxy_async_smem();
   }
+  if (tid == 0) *abort_flag = 0;
+  fence_proxy_async_smem();
   if (warp == kMmaWarp) {
     tmem_alloc(tmem_holder, kTmemCols);
     tmem_relinquish();
@@ -513,8 +519,8 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     dependency_wait();   // delta
     int h = kvh * a.group + from / per_head, qt = t0 + from % per_head, fixes = 0;
     for (int i = 0; i < n_tiles; ++i) {
-      const int st = i % kDkvStages;
-      if (!mbar_wait_ok(q_empty + st, ((i / kDkvStages) & 1) ^ 1, abort_flag)) break;   // no copies once a wait has run out
+      const int st = i % kStages;
+      if (!mbar_wait_ok(q_empty + st, ((i / kStages) & 1) ^ 1, abort_flag)) break;   // no copies once a wait has run out
       uint8_t *q_dst = sQ + st * TileGeom<D>::kBytes, *do_dst = sdO + st * TileGeom<D>::kBytes;
       const bool straddles = qt * kTile + kTile > len && len < a.mask.n;   // rows of Q and dO behind the end are cleared: 0 * NaN
       uint64_t* bar = straddles ? landed : q_full + st;
@@ -544,36 +550,40 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     }
   } else if (warp == kMmaWarp) {
     if (lane == 0) {
-      auto q_tile = [&](int i) { return smem_u32(sQ + (i % kDkvStages) * TileGeom<D>::kBytes); };
-      auto do_tile = [&](int i) { return smem_u32(sdO + (i % kDkvStages) * TileGeom<D>::kBytes); };
+      auto q_tile = [&](int i) { return smem_u32(sQ + (i % kStages) * TileGeom<D>::kBytes); };
+      auto do_tile = [&](int i) { return smem_u32(sdO + (i % kStages) * TileGeom<D>::kBytes); };
       // once a wait has run out no more MMAs are issued: their operands may never have been loaded
       bool ok = true;
       auto wait_q = [&](int i) {
-        ok = ok && mbar_wait_spin(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
+        ok = ok && mbar_wait_spin(q_full + i % kStages, (i / kStages) & 1, abort_flag);
         tc_fence_after_sync();
       };
+      // the next S^T to issue, if there is one
+      int s_next = 0;
+      auto issue_s = [&]() {
+        if (s_next >= n_tiles) return;
+        wait_q(s_next);
+        if (!ok) return;
+        mma_abT<D>(tmem_base + kColSt + (s_next % kSBufs) * 128, smem_u32(sK), q_tile(s_next));
+        mma_commit(s_full + s_next % kSBufs);
+        ++s_next;
+      };
       ok = mbar_wait_spin(kv_full, 0, abort_flag);
-      wait_q(0);
+      issue_s();
       if (ok) {
-        mma_abT<D>(tmem_base + kColSt, smem_u32(sK), q_tile(0));
-        mma_commit(s_full);
         mma_abT<D>(tmem_base + kColdPt, smem_u32(sV), do_tile(0));
         mma_commit(dp_full);
       }
+      if (kSBufs > 1) issue_s();
       for (int i = 0; ok && i < n_tiles; ++i) {
         if (!mbar_wait_spin(p_full, i & 1, abort_flag)) break;
         tc_fence_after_sync();
-        win_mma_groups<D>(tmem_base + kColdV, tmem_base + kColSt, do_tile(i), i > 0);
-        if (i + 1 < n_tiles) {
-          wait_q(i + 1);
-          if (!ok) break;
-          mma_abT<D>(tmem_base + kColSt, smem_u32(sK), q_tile(i + 1));
-          mma_commit(s_full);
-        }
-        if (!mbar_wait_spin(ds_full, i & 1, abort_flag)) break;
+        win_mma_groups<D>(tmem_base + kColdV, tmem_base + kColSt + (i % kSBufs) * 128, do_tile(i), i > 0);
+        issue_s();   // over P^T(i), behind the products that read it (MMAs run in order)
+        if (!ok || !mbar_wait_spin(ds_full, i & 1, abort_flag)) break;
         tc_fence_after_sync();
         win_mma_groups<D>(tmem_base + kColdK, tmem_base + kColdPt, q_tile(i), i > 0);
-        mma_commit(q_empty + i % kDkvStages);
+        mma_commit(q_empty + i % kStages);
         if (i + 1 < n_tiles) {
           mma_abT<D>(tmem_base + kColdPt, smem_u32(sV), do_tile(i + 1));
           mma_commit(dp_full);
@@ -591,7 +601,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     if (live) a.mask.queries_of(key, len, q_first, q_last);
     int qt = t0 + from % per_head;
     for (int i = 0; i < n_tiles; ++i) {
-      const float* stat = sStat + (i % kDkvStages) * 2 * kTile + g * kCols;
+      const float* stat = sStat + (i % kStages) * 2 * kTile + g * kCols;
       const bool full = qt * kTile >= full_first && qt * kTile + kTile <= full_last;
       uint32_t see[NL];
 #pragma unroll
@@ -600,13 +610,14 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
         see[c2] = full ? 0xffffffffu : bits_below(q_last, base) & ~bits_below(q_first, base);
       }
       if (++qt == t0 + per_head) qt = t0;
-      bool ok = mbar_wait_ok(q_full + i % kDkvStages, (i / kDkvStages) & 1, abort_flag);
-      ok = mbar_wait_ok(s_full, i & 1, abort_flag) && ok;
+      bool ok = mbar_wait_ok(q_full + i % kStages, (i / kStages) & 1, abort_flag);
+      ok = mbar_wait_ok(s_full + i % kSBufs, (i / kSBufs) & 1, abort_flag) && ok;
       if (!ok) break;
       tc_fence_after_sync();
+      const uint32_t col_s = tmem_lane + kColSt + (i % kSBufs) * 128 + g * kCols;
       uint32_t s[NL][32], pt[NL][16];
 #pragma unroll
-      for (int c2 = 0; c2 < NL; ++c2) tmem_ld32(tmem_lane + kColSt + g * kCols + c2 * 32, s[c2]);
+      for (int c2 = 0; c2 < NL; ++c2) tmem_ld32(col_s + c2 * 32, s[c2]);
       tmem_wait_ld();
       uint64_t p2[NL][16];
 #pragma unroll
@@ -637,7 +648,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
           }
       }
 #pragma unroll
-      for (int c2 = 0; c2 < NL; ++c2) tmem_st16(tmem_lane + kColSt + g * kCols + c2 * 16, pt[c2]);
+      for (int c2 = 0; c2 < NL; ++c2) tmem_st16(col_s + c2 * 16, pt[c2]);
       tmem_wait_st();
       tc_fence_before_sync();
       warp_arrive(p_full, lane);
@@ -758,7 +769,7 @@ window_attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   }
 }
 template <int D> constexpr int window_bwd_smem() {
-  return DqSmem<D>::kTotal > DkvSmem<D>::kTotal ? DqSmem<D>::kTotal : DkvSmem<D>::kTotal;
+  return DqSmem<D>::kTotal > WinDkvSmem<D>::kTotal ? DqSmem<D>::kTotal : WinDkvSmem<D>::kTotal;
 }
 
 }  // namespace astro
