@@ -853,9 +853,6 @@ astro_status_t launch_quant_typed(int dtype, const QuantTensors& x, const FrameS
   return launch_quant<float, Write>(x, slots, batch, head_dim, st);
 }
 
-// Up to this many queries per sample take the kernel that reads the codes themselves.
-constexpr int kFewMaxQueries = 64;
-
 int held_tokens(const astro_kvcache* c) { return c ? (c->sink_held + c->win_held) * c->d.tokens_per_frame : 0; }
 
 // How the kernel for few queries divides its work: the queries of a list (those of every sample over one prefix) into tiles of
@@ -869,7 +866,7 @@ FewSplit few_split(const astro_kvcache* cache, int batch, int heads, int n_q, in
   constexpr int kSms = 148;
   FewSplit f;
   const bool shared = cache && cache->d.cache_batch == 1 && batch > 1;
-  f.rows = shared ? batch * n_q : n_q;     // n_q is kFewMaxQueries at most
+  f.rows = shared ? batch * n_q : n_q;     // 2^20 at most, or 8 times the batch (see few_queries)
   f.per_tile = f.rows <= 8 ? 8 : 16;
   f.tiles = (f.rows - 1) / f.per_tile + 1;
   f.lists = static_cast<long long>(shared ? 1 : batch) * heads;
@@ -882,6 +879,24 @@ FewSplit few_split(const astro_kvcache* cache, int batch, int heads, int n_q, in
     if (i == 1 || cost < least) { f.splits = i; least = cost; }
   }
   return f;
+}
+
+// Whether the call goes to the kernel that reads the codes themselves, or has the rows turned into bf16 for the dense kernel.  The
+// first takes 0.2 us for a step of 32 keys and 16 queries (0.16 at head_dim 64) and CTA, the second 0.71 (0.64) for a tile of 128 keys in each
+// round of 148 query tiles, and the rows' bytes.  (Both measured, us, 28080 keys, head_dim 128, 12 heads: 67 and 211 for 64 queries,
+// 124 and 211 for 128, 238 and 212 for 256; one head: 90 and 174 for 1024, 162 and 175 for 2048; 2000 keys, 12 heads: 41 and 29 for 256.)
+bool few_queries(const astro_kvcache* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
+  if (n_q <= 8) return true;
+  if (static_cast<long long>(batch) * n_q > (1 << 20)) return false;
+  const bool wide = head_dim == 128;
+  const double keys = static_cast<double>(held_tokens(cache)) + n_kc;
+  const FewSplit f = few_split(cache, batch, heads, n_q, n_kc);
+  const double few_rounds = std::ceil(static_cast<double>(f.lists) * f.tiles * f.splits / 148.0);
+  const double few = 8.0 + few_rounds * (keys / kFewStep / f.splits + 20.0) * (wide ? 0.2 : 0.16) + (f.splits > 1 ? 4.0 : 0.0);
+  const double rounds = std::ceil(static_cast<double>((n_q - 1) / kTile + 1) * batch * heads / 148.0);
+  const double rows = cache ? static_cast<double>(cache->d.cache_batch) * heads * held_tokens(cache) : 0.0;
+  const double dense = 16.0 + rounds * std::ceil(keys / kTile) * (wide ? 0.71 : 0.64) + rows * head_dim * 6.0 / 6.0e6;
+  return few < dense;
 }
 
 struct Attn8Call {
@@ -1920,7 +1935,7 @@ astro_status_t astro_kvcache8_read(const astro_kvcache_t* c, int first_frame, in
 
 size_t astro_chunk_attn8_fwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
   if (check_attn_args(AttnArgs{cache, batch, heads, head_dim, n_q, n_kc}, 1.f, 8) != ASTRO_OK) return 0;
-  if (n_q > kFewMaxQueries) return 2 * expanded_bytes(cache);
+  if (!few_queries(cache, batch, heads, head_dim, n_q, n_kc)) return 2 * expanded_bytes(cache);
   const int splits = few_split(cache, batch, heads, n_q, n_kc).splits;
   return splits == 1 ? 0 : static_cast<size_t>(splits) * batch * heads * n_q * (head_dim + 1) * sizeof(float);
 }
@@ -1940,7 +1955,7 @@ astro_status_t astro_chunk_attn8_fwd(const astro_kvcache_t* cache, const void* q
   if (workspace_bytes < need) return ASTRO_ERR_CAPACITY;
   if ((s = check_arch()) != ASTRO_OK) return s;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (n_q <= kFewMaxQueries) {
+  if (few_queries(cache, batch, heads, head_dim, n_q, n_kc)) {
     const bool eight = few_split(cache, batch, heads, n_q, n_kc).per_tile == 8;
     if (head_dim == 128) return eight ? launch_few<128, 1>(c, scale, o, lse, workspace, st) : launch_few<128, 2>(c, scale, o, lse, workspace, st);
     return eight ? launch_few<64, 1>(c, scale, o, lse, workspace, st) : launch_few<64, 2>(c, scale, o, lse, workspace, st);

@@ -74,12 +74,20 @@ def tensors(torch, B, n_q, n_kc, H, D, seed):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("n_q", [1, 2, 7, 8, 9, 16, 17, 63, 64, 65, 130])
+@pytest.mark.parametrize("n_q", [1, 2, 7, 8, 9, 16, 17, 63, 64, 65, 130, 1000])
 def test_numbers_of_queries(D, n_q):
     torch, A = modules()
     cache = filled(torch, A, 2, 3, D, 37, 1, 6, 6, 4, n_q)
     q, kc, vc, d_o = tensors(torch, 2, n_q, 11, 3, D, n_q + 100)
     compare(torch, A, cache, q, kc, vc, D ** -0.5, d_o)
+
+
+@pytest.mark.parametrize("D,H,n_q", [(64, 40, 100), (64, 40, 300), (128, 40, 300), (128, 20, 1500)])
+def test_queries_on_both_sides_of_the_choice_between_the_kernels(D, H, n_q):
+    torch, A = modules()
+    cache = filled(torch, A, 1, H, D, 100, 1, 6, 7, 4, n_q)
+    q, kc, vc, d_o = tensors(torch, 1, n_q, 50, H, D, n_q)
+    compare(torch, A, cache, q, kc, vc, D ** -0.5, d_o, heads=(0, H - 1))
 
 
 @pytest.mark.parametrize("n_q", [1, 12, 100])
@@ -99,11 +107,9 @@ def test_without_a_context():
     empty = A.astro_kvcache8_create(1, 2, 128, 4, 1, 2)
     for n_q in (1, 20, 70):
         q, kc, vc, d_o = tensors(torch, 2, n_q, 33, 2, 128, n_q)
-        for cache in (None, empty):
-            o, lse = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.1)
-            want = A.astro_chunk_attn_fwd(None, q, kc, vc, 0.1)
-            if n_q > 64:
-                assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+        o, lse = compare(torch, A, empty, q, kc, vc, 0.1, d_o)
+        again = A.astro_chunk_attn8_fwd(None, q, kc, vc, 0.1)
+        assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
         compare(torch, A, None, q, kc, vc, 0.1, d_o)
 
 

@@ -88,10 +88,10 @@ def test_attention_over_the_cache_refusals(bits):
     c, empty = cache(bits=bits, held=3), cache(bits=bits)
     wrong = bits == 16
 
-    def fwd(cache=c, q=P, k=P, v=P, batch=1, heads=2, dim=64, n_q=100, n_kc=5, scale=0.1, o=P, lse=P, ws=P, nbytes=1 << 30):
+    def fwd(cache=c, q=P, k=P, v=P, batch=1, heads=2, dim=64, n_q=100000, n_kc=5, scale=0.1, o=P, lse=P, ws=P, nbytes=1 << 30):
         return L.astro_chunk_attn8_fwd(cache, q, k, v, batch, heads, dim, n_q, n_kc, scale, o, lse, ws, nbytes, None)
 
-    def bwd(cache=c, q=P, k=P, v=P, o=P, lse=P, d_o=P, batch=1, heads=2, dim=64, n_q=100, n_kc=5, scale=0.1, dq=P, dk=P, dv=P, ws=P, nbytes=1 << 30):
+    def bwd(cache=c, q=P, k=P, v=P, o=P, lse=P, d_o=P, batch=1, heads=2, dim=64, n_q=100000, n_kc=5, scale=0.1, dq=P, dk=P, dv=P, ws=P, nbytes=1 << 30):
         return L.astro_chunk_attn8_bwd(cache, q, k, v, o, lse, d_o, batch, heads, dim, n_q, n_kc, scale, dq, dk, dv, ws, nbytes, None)
 
     if wrong:
@@ -110,9 +110,9 @@ def test_attention_over_the_cache_refusals(bits):
         assert bad == "lse" or bwd(**{bad: ODD}) == ALIGN
     rows = 2 * 48 * 64 * 2                                       # K or V of the held frames in bf16
     size = L.astro_chunk_attn8_fwd_workspace_bytes
-    assert size(c, 1, 2, 64, 100, 5) == 2 * rows and size(None, 1, 2, 64, 100, 5) == 0
+    assert size(c, 1, 2, 64, 100000, 5) == 2 * rows and size(None, 1, 2, 64, 100, 5) == 0
     assert L.astro_chunk_attn8_bwd_workspace_bytes(c, 1, 2, 64, 100, 5) == 2 * rows + 1024
-    assert fwd(nbytes=2 * rows - 1) == CAPACITY and size(c, 1, 2, 64, 0, 5) == 0 and size(c, 1, 2, 65, 100, 5) == 0
+    assert fwd(n_q=100000, nbytes=2 * rows - 1) == CAPACITY and size(c, 1, 2, 64, 0, 5) == 0 and size(c, 1, 2, 65, 100, 5) == 0
 
 
 def window(fwd=True, q=P, qs=None, k=P, ks=None, v=P, vs=None, lens=None, o=P, lse=P, d_o=P, scale=0.1, dq=P, dk=P, dv=P, ws=P, nbytes=1 << 30,
