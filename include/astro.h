@@ -364,7 +364,8 @@ astro_status_t astro_sparse_attn_bwd(const astro_kvcache_t* cache, const void* q
  *   q_strides, k_strides, v_strides: null = contiguous; multiples of 16 bytes, no stride of 0.  o is contiguous.
  *   lengths: device int32 [batch], tokens of each sample (values outside 0..n_tokens count as the nearer end); null: n_tokens each.  What k, v and q
  *   hold from there on does not matter, NaN included; those queries get O = 0 and LSE = -infinity.
- * A NaN or infinity reaches the queries that see it and no others.  lse may be null.  n_tokens = 0 is an empty call.
+ * A NaN or infinity reaches the queries that see it and no others (a tile of 128 queries that is met by one goes key by key, which
+ * is slow).  lse may be null.  o must not overlap q, k or v.  n_tokens = 0 is an empty call.
  * ASTRO_ERR_SHAPE: head_dim not 64 or 128, heads not a multiple of kv_heads, window_tokens < block_tokens, n_tokens > 2^29, a scale that
  * is negative or not finite.  bf16 products, fp32 accumulation and softmax. */
 typedef struct {
@@ -376,7 +377,7 @@ astro_status_t astro_window_attn_fwd(const astro_window_desc_t* desc, const void
                                      const int32_t* lengths, float scale, void* o, float* lse, void* stream);
 /* Its backward, nothing detached: dQ, and dK and dV of every token, summed over the heads that share it, from dO and the forward's
  * O and LSE (all contiguous, as are dq, dk and dv).  Queries and keys from a sequence's length on get zeros, and what o, lse and d_o hold there does not
- * matter.  workspace: device scratch, 16-byte aligned, at least astro_window_attn_bwd_workspace_bytes().  All sums have one
+ * matter.  Outputs must not overlap inputs.  workspace: device scratch, 16-byte aligned, at least astro_window_attn_bwd_workspace_bytes().  All sums have one
  * fixed order: the same call gives the same bits. */
 size_t astro_window_attn_bwd_workspace_bytes(int batch, int heads, int n_tokens, int head_dim);
 astro_status_t astro_window_attn_bwd(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,

@@ -371,7 +371,9 @@ def astro_kvcache_reset(cache: KVCache) -> None:
 
 
 def astro_kvcache_append(cache: KVCache, k, v, n_frames: int, stream=None) -> None:
-    """k, v: bf16 [B_c, n_frames*T, H, D] on the device."""
+    """k, v: bf16 [B_c, n_frames*T, H, D] on the device (what astro_kvcache8_append takes, where the cache is one in 8 bits)."""
+    if cache.bits == 8:
+        return astro_kvcache8_append(cache, k, v, n_frames, stream=stream)
     _check(lib().astro_kvcache_append(cache.handle, _ptr(k), _ptr(v), _int(n_frames), _stream(stream)),
            "astro_kvcache_append")
 

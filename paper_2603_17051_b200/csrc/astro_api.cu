@@ -995,9 +995,10 @@ astro_status_t expand_context(const Attn8Call& c, void* workspace, Expanded* out
     e.start1 = segs.n > 1 ? segs.start[1] : 0;
     e.n = n;
     const int per_block = kExpandThreads * 8 / d.head_dim * kExpandRows;
-    const long long lists = static_cast<long long>(d.cache_batch) * d.heads;
-    if (lists > 65535) return ASTRO_ERR_SHAPE;
-    const dim3 grid(static_cast<unsigned>((n + per_block - 1) / per_block), static_cast<unsigned>(lists), 2);
+    e.pieces = (n + per_block - 1) / per_block;
+    const long long blocks = static_cast<long long>(d.cache_batch) * d.heads * e.pieces;
+    if (blocks > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
+    const dim3 grid(static_cast<unsigned>(blocks), 2);
     const unsigned long long row = static_cast<unsigned long long>(d.head_dim) * 2;
     for (int i = 0; i < 2; ++i) {
       astro_status_t s = make_tmap(i ? &out->v : &out->k, i ? e.v_out : e.k_out, d.head_dim, n, d.heads, d.cache_batch, row, row * n,
@@ -2003,10 +2004,10 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
     if ((s = make_tmap_user(&tvc, v_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
   }
   float* delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * expanded_bytes(cache));
-  s = head_dim == 128 ? launch_delta<128>(o, d_o, batch, heads, n_q, delta, st) : launch_delta<64>(o, d_o, batch, heads, n_q, delta, st);
-  if (s != ASTRO_OK) return s;
   Expanded x;
   if ((s = expand_context(c, workspace, &x, st)) != ASTRO_OK) return s;
+  s = head_dim == 128 ? launch_delta<128>(o, d_o, batch, heads, n_q, delta, st) : launch_delta<64>(o, d_o, batch, heads, n_q, delta, st);
+  if (s != ASTRO_OK) return s;
   const CUtensorMap tkx[2] = {x.k, x.k};
   const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(q);
   s = head_dim == 128 ? launch_bwd_dq<128>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st)

@@ -30,13 +30,13 @@
 namespace astro {
 
 // ---------------------------------------------------------------------------------- cached rows into bf16
-// grid.x: pieces of kQuantTokens * rows-per-block tokens, grid.y: (sample, head), grid.z: 0: K, 1: V.  The rows of a (sample,
-// head) are one or two runs of the storage and become one run of the output [B_c, H, n, D].
+// grid.x: ((sample, head), piece of its rows), pieces fastest, grid.y: 0: K, 1: V.  The rows of a (sample, head) are one or two
+// runs of the storage and become one run of the output [B_c, H, n, D].
 struct Expand8 {
   const uint8_t *k, *v, *k_exp, *v_exp;
   __nv_bfloat16 *k_out, *v_out;
   long long slot_tokens;
-  int start0, count0, start1, n;     // logical row r sits at start0 + r, or from count0 on at start1 + r - count0
+  int pieces, start0, count0, start1, n;     // logical row r sits at start0 + r, or from count0 on at start1 + r - count0
 };
 constexpr int kExpandThreads = 256, kExpandRows = 8;
 
@@ -45,10 +45,11 @@ __global__ void __launch_bounds__(kExpandThreads) expand8_kernel(const Expand8 a
   constexpr int kLanes = D / 8, kPerPass = kExpandThreads / kLanes;
   dependents_may_start();
   const int part = threadIdx.x % kLanes;
-  const int r0 = blockIdx.x * (kPerPass * kExpandRows) + threadIdx.x / kLanes;
-  const uint8_t* codes = (blockIdx.z ? a.v : a.k) + static_cast<long long>(blockIdx.y) * a.slot_tokens * D + part * 8;
-  const uint8_t* exps = (blockIdx.z ? a.v_exp : a.k_exp) + static_cast<long long>(blockIdx.y) * a.slot_tokens;
-  __nv_bfloat16* out = (blockIdx.z ? a.v_out : a.k_out) + static_cast<long long>(blockIdx.y) * a.n * D + part * 8;
+  const long long list = blockIdx.x / a.pieces;
+  const int r0 = (blockIdx.x - static_cast<int>(list) * a.pieces) * (kPerPass * kExpandRows) + threadIdx.x / kLanes;
+  const uint8_t* codes = (blockIdx.y ? a.v : a.k) + list * a.slot_tokens * D + part * 8;
+  const uint8_t* exps = (blockIdx.y ? a.v_exp : a.k_exp) + list * a.slot_tokens;
+  __nv_bfloat16* out = (blockIdx.y ? a.v_out : a.k_out) + list * a.n * D + part * 8;
   uint2 w[kExpandRows];
   uint32_t e[kExpandRows];
 #pragma unroll

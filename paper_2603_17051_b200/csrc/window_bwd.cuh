@@ -65,6 +65,7 @@ __device__ __noinline__ void win_careful_dq(const WinBwdArgs& a, int qt, int h, 
       q[e] = __bfloat162float(qp[e]);
       g[e] = __bfloat162float(a.d_o[at + e]);
     }
+    bool lost = false;
     int lo, hi;
     a.mask.keys_of(row, len, lo, hi);
     const int sink = min(min(a.mask.sink, hi), lo), keys = sink + hi - lo;
@@ -84,8 +85,10 @@ __device__ __noinline__ void win_careful_dq(const WinBwdArgs& a, int qt, int h, 
         s += __shfl_xor_sync(0xffffffffu, s, d);
         dp += __shfl_xor_sync(0xffffffffu, dp, d);
       }
+      if ((x & 127) == 0 && __any_sync(0xffffffffu, lost)) break;   // NaN in every element: nothing to add to that
       if (there) {
         const float ds = fast_exp2(s * scale_log2 - lse2) * (dp - delta);
+        lost = lost || isnan(ds);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) acc[e] = fmaf(ds, __bfloat162float(kb[j * a.ks.t + e]), acc[e]);
       }
@@ -378,6 +381,13 @@ __device__ __noinline__ void win_careful_dkv(const WinBwdArgs& a, int kt, int kv
         for (int d = 1; d < 8; d *= 2) {
           s += __shfl_xor_sync(0xffffffffu, s, d);
           dp += __shfl_xor_sync(0xffffffffu, dp, d);
+        }
+        if ((x - first & 127) == 0) {   // NaN in every element of both: nothing to add to that
+          bool lost = true;
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) lost = lost && isnan(dk[e]) && isnan(dv[e]);
+          const uint32_t lanes = __ballot_sync(0xffffffffu, lost);   // all eight lanes of a slot
+          if (((lanes & 0xffu) == 0xffu) || (lanes >> 8 & 0xffu) == 0xffu || (lanes >> 16 & 0xffu) == 0xffu || lanes >> 24 == 0xffu) break;
         }
         if (there) {
           const float p = fast_exp2(s * scale_log2 - a.lse[stat + i] * kLog2e), ds = p * (dp - a.delta[stat + i]);

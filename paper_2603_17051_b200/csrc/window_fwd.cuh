@@ -579,7 +579,7 @@ __device__ __forceinline__ bool win_epilogue(const WinCta<D>& c, const WinFwdArg
 
 // ---------------------------------------------------------------------------------- second pass
 // One unit by the formula, on the ordinary cores: a warp per row, eight lanes per key (D/8 elements each), four keys at a time, running
-// maximum.  About 10 ms for a unit of 32000 keys.
+// maximum.  About 10 ms for a unit of 32000 keys, less where all is NaN.
 template <int D>
 __device__ __noinline__ void win_careful_unit(const WinFwdArgs& a, int id, int warp, int lane) {
   constexpr int kPer = D / 8;
@@ -611,6 +611,8 @@ __device__ __noinline__ void win_careful_unit(const WinFwdArgs& a, int id, int w
 #pragma unroll
         for (int d = 1; d < 8; d *= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
         s *= a.scale_log2;
+        // a NaN score makes everything NaN: nothing to add to that
+        if ((x & 127) == 0 && __any_sync(0xffffffffu, isnan(l))) break;
         if (there) {
           const float top = fmaxf(m, s), ref = top == -INFINITY ? 0.f : top;
           const float alpha = fast_exp2(m - ref), p = fast_exp2(s - ref);

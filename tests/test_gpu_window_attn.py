@@ -309,3 +309,16 @@ def test_units_of_one_tile():
     lengths[::7] = 0
     at = {(b, h) for b in range(0, B, 17) for h in range(H)} | {(b, h) for b in (7, 499) for h in range(H)}
     compare(torch, A, q, k, v, d_o, 10, 30, 5, lengths.tolist(), at=at)
+
+
+def test_everything_nan():
+    """Sequences of which every result is NaN: every tile is done again, which ends as soon as a row is NaN throughout."""
+    torch, A = modules()
+    q, k, v, d_o = tensors(torch, 1, 8192, 12, 4, 128, 18)
+    form = dict(block_tokens=1, window_tokens=5000, sink_tokens=100)
+    o, lse = A.astro_window_attn_fwd(q, k, v, 0.1, **form)
+    nan = torch.full_like(q, float("nan"))
+    bad, bad_lse = A.astro_window_attn_fwd(nan, k, v, 0.1, **form)
+    grads = A.astro_window_attn_bwd(q, k, v, o, lse, nan, 0.1, **form)
+    A.astro_last_device_status()
+    assert bad.isnan().all() and bad_lse.isnan().all() and all(g.isnan().all() for g in grads)
