@@ -1184,7 +1184,13 @@ astro_status_t launch_window_bwd(const WindowCall& c, const void* o, const float
   a.k_order.set(a.kv_lists, a.tiles - a.front);
   a.shares = w.shares;
   a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + astro_chunk_attn_bwd_workspace_bytes(d.batch, d.heads, d.n_tokens, D));
-  if ((s = launch_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, static_cast<float*>(workspace), st)) != ASTRO_OK) return s;
+  if (d.n_tokens <= kWinShort) {
+    win_short_delta_kernel<D><<<static_cast<unsigned>((static_cast<long long>(a.lists) * d.n_tokens + 3) / 4), 128, 0, st>>>(a, static_cast<float*>(workspace));
+    s = launch_status();
+  } else {
+    s = launch_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, static_cast<float*>(workspace), st);
+  }
+  if (s != ASTRO_OK) return s;
   const long long ctas = static_cast<long long>(a.front) * a.kv_lists * a.shares + static_cast<long long>(a.lists) * a.tiles +
                          static_cast<long long>(a.kv_lists) * (a.tiles - a.front);
   s = launch_dependent(window_attn_bwd_kernel<D>, dim3(static_cast<unsigned>(ctas)), kWinBwdThreads, window_bwd_smem<D>(), st, tq, tdo, tk,

@@ -45,6 +45,52 @@ __device__ __forceinline__ bool win_store_row32(uint32_t taddr, float mult, bool
   return !live || fwd_all_finite(chk2);
 }
 
+// delta of short sequences from the weights, sum_j p_ij dO_i . v_j, instead of dO_i . O_i with the rounded O: a row of two or three keys
+// of which one has nearly all the weight has a dS far smaller than its delta, and half a step of O's (2^-8 of delta) is then per
+// cents of it.  Long sequences' gradients are made of other rows; in short ones such a row can be half of the result.
+// A warp per (sample, head, query); bandwidth and latency, a few microseconds.
+constexpr int kWinShort = 64;
+template <int D>
+__global__ void __launch_bounds__(128) win_short_delta_kernel(const WinBwdArgs a, float* delta) {
+  constexpr int kPer = D / 32;
+  dependents_may_start();
+  const int at = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;   // rows are fewer than 2^31
+  if (at >= a.lists * a.mask.n) return;
+  const int list = at / a.mask.n, row = at - list * a.mask.n, b = list / a.heads, h = list - b * a.heads, len = a.mask.length(b);
+  float sum = 0.f;
+  if (row < len) {
+    const __nv_bfloat16* qp = a.q + b * a.qs.b + row * a.qs.t + h * a.qs.h + lane * kPer;
+    const __nv_bfloat16* gp = a.d_o + ((static_cast<size_t>(b) * a.mask.n + row) * a.heads + h) * D + lane * kPer;
+    float q[kPer], g[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      q[e] = __bfloat162float(qp[e]);
+      g[e] = __bfloat162float(gp[e]);
+    }
+    int lo, hi;
+    a.mask.keys_of(row, len, lo, hi);
+    const float scale_log2 = a.scale * kLog2e, lse2 = a.lse[static_cast<size_t>(list) * a.mask.n + row] * kLog2e;
+    const __nv_bfloat16* kb = a.k + b * a.ks.b + (h / a.group) * a.ks.h + lane * kPer;
+    const __nv_bfloat16* vb = a.v + b * a.vs.b + (h / a.group) * a.vs.h + lane * kPer;
+    for (int j = 0; j < hi; ++j) {
+      if (j >= a.mask.sink && j < lo) continue;
+      float s = 0.f, dp = 0.f;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        s = fmaf(q[e], __bfloat162float(kb[j * a.ks.t + e]), s);
+        dp = fmaf(g[e], __bfloat162float(vb[j * a.vs.t + e]), dp);
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, d);
+        dp += __shfl_xor_sync(0xffffffffu, dp, d);
+      }
+      sum = fmaf(fast_exp2(s * scale_log2 - lse2), dp, sum);
+    }
+  }
+  if (lane == 0) delta[at] = sum;
+}
+
 // ------------------------------------------------------------------------------------------ dQ
 // One row of dQ by the formula: eight lanes per key, four keys at a time.
 template <int D>

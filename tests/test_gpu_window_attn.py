@@ -322,3 +322,36 @@ def test_everything_nan():
     grads = A.astro_window_attn_bwd(q, k, v, o, lse, nan, 0.1, **form)
     A.astro_last_device_status()
     assert bad.isnan().all() and bad_lse.isnan().all() and all(g.isnan().all() for g in grads)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [2, 3, 5, 64])
+def test_rows_of_which_one_key_has_nearly_all_the_weight(D, n):
+    """dS is far smaller than delta there: in short sequences delta comes from the weights, not from the rounded O.  Then every
+    error of dQ and dK is relative to dS itself: its rounding and the output's, 2^-8 of each term, beside fp32's."""
+    torch, A = modules()
+    q, k, v, d_o = tensors(torch, 3, n, 4, 2, D, 19)
+    k[:, 0] = (k[:, 0].float() + 5 * q[:, :, :1].float().mean(1) / D ** 0.5).bfloat16()
+    scale = 4.0 / D ** 0.5
+    o, lse = A.astro_window_attn_fwd(q, k, v, scale)
+    grads = A.astro_window_attn_bwd(q, k, v, o, lse, d_o, scale)
+    see = mask(torch, n, n, 1, 10 ** 9, 0)
+    h8 = 2.0 ** -8
+    for b in range(3):
+        for kv in range(2):
+            dk, dk_err = 0, 0
+            for h in (2 * kv, 2 * kv + 1):
+                qq, kk, vv, gg = (t[b, :, i].double() for t, i in ((q, h), (k, kv), (v, kv), (d_o, h)))
+                x = torch.where(see, scale * (qq @ kk.T), -torch.inf)
+                p = torch.softmax(x, 1)
+                dp = gg @ vv.T
+                ds = p * (dp - (p * dp).sum(1, keepdim=True))
+                # fp32: products of D terms and exp2 of arguments up to |x|, relative to the sizes that go into them
+                size = scale * (qq.abs() @ kk.abs().T) * see
+                fp32 = 2.0 ** -18 * (1 + size.amax(1, keepdim=True)) * p * (gg.abs() @ vv.abs().T).amax(1, keepdim=True)
+                err = h8 * ds.abs() + fp32
+                dq = scale * (ds @ kk)
+                check(grads[0][b, :, h], (dq, 1.1 * (scale * (err @ kk.abs()) + h8 * dq.abs()) + 1e-7), "dQ")
+                dk = dk + scale * (ds.T @ qq)
+                dk_err = dk_err + scale * (err.T @ qq.abs())
+            check(grads[1][b, :, kv], (dk, 1.1 * (dk_err + h8 * dk.abs()) + 1e-7), "dK")
