@@ -2012,15 +2012,42 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
   float* delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * expanded_bytes(cache));
   Expanded x;
   if ((s = expand_context(c, workspace, &x, st)) != ASTRO_OK) return s;
-  s = head_dim == 128 ? launch_delta<128>(o, d_o, batch, heads, n_q, delta, st) : launch_delta<64>(o, d_o, batch, heads, n_q, delta, st);
+  const long long keys = static_cast<long long>(held_tokens(cache)) + n_kc;
+  if (keys <= kShortKeys) {
+    ShortDelta8 f;
+    f.q = static_cast<const __nv_bfloat16*>(q);
+    f.d_o = static_cast<const __nv_bfloat16*>(d_o);
+    f.kx = static_cast<const __nv_bfloat16*>(workspace);
+    f.vx = reinterpret_cast<const __nv_bfloat16*>(static_cast<const char*>(workspace) + expanded_bytes(cache));
+    f.kc = static_cast<const __nv_bfloat16*>(k_chunk);
+    f.vc = static_cast<const __nv_bfloat16*>(v_chunk);
+    f.lse = lse;
+    f.delta = delta;
+    f.rows = static_cast<long long>(batch) * heads * n_q;
+    f.heads = heads; f.n_q = n_q;
+    f.n_ctx = held_tokens(cache);
+    f.n_kc = n_kc;
+    f.shared = cache && cache->d.cache_batch == 1 ? 1 : 0;
+    f.scale_log2 = scale * kLog2e;
+    const unsigned blocks = static_cast<unsigned>((f.rows + 3) / 4);
+    if (head_dim == 128) attn8_short_delta_kernel<128><<<blocks, 128, 0, st>>>(f);
+    else attn8_short_delta_kernel<64><<<blocks, 128, 0, st>>>(f);
+    s = launch_status();
+  } else {
+    s = head_dim == 128 ? launch_delta<128>(o, d_o, batch, heads, n_q, delta, st) : launch_delta<64>(o, d_o, batch, heads, n_q, delta, st);
+  }
   if (s != ASTRO_OK) return s;
   const CUtensorMap tkx[2] = {x.k, x.k};
   const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(q);
   s = head_dim == 128 ? launch_bwd_dq<128>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st)
                       : launch_bwd_dq<64>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st);
-  if (s != ASTRO_OK || n_kc == 0) return s;
-  return astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, batch, heads, head_dim, n_q, n_kc, scale, dk_chunk, dv_chunk,
-                                  stream);
+  if (s == ASTRO_OK && n_kc > 0)
+    s = astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, batch, heads, head_dim, n_q, n_kc, scale, dk_chunk, dv_chunk, stream);
+  if (s != ASTRO_OK || keys > 1) return s;
+  // A softmax over one key is constant: no gradient for queries and keys, where the kernels leave fp32's rounding of dP - delta.
+  const size_t row = static_cast<size_t>(batch) * heads * head_dim * 2;
+  if (cudaMemsetAsync(dq, 0, row * n_q, st) != cudaSuccess) return ASTRO_ERR_CUDA;
+  return n_kc == 0 || cudaMemsetAsync(dk_chunk, 0, row, st) == cudaSuccess ? ASTRO_OK : ASTRO_ERR_CUDA;
 }
 
 // ---- sliding window with sinks over whole sequences ---------------------------------------------------

@@ -71,6 +71,53 @@ __global__ void __launch_bounds__(kExpandThreads) expand8_kernel(const Expand8 a
   }
 }
 
+// delta over few keys from the weights, sum_j p_ij dO_i . v_j, instead of dO_i . O_i with the rounded O (window_bwd.cuh has the
+// reason: win_short_delta_kernel).  kx, vx: the expanded rows.  A warp per (sample, head, query).
+constexpr int kShortKeys = 64;
+struct ShortDelta8 {
+  const __nv_bfloat16 *q, *d_o, *kx, *vx, *kc, *vc;
+  const float* lse;
+  float* delta;
+  long long rows;
+  int heads, n_q, n_ctx, n_kc, shared;
+  float scale_log2;
+};
+template <int D>
+__global__ void __launch_bounds__(128) attn8_short_delta_kernel(const ShortDelta8 a) {
+  constexpr int kPer = D / 32;
+  const long long at = blockIdx.x * 4ll + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (at >= a.rows) return;
+  const long long bh = at / a.n_q, b = bh / a.heads;
+  const int i = static_cast<int>(at - bh * a.n_q), h = static_cast<int>(bh - b * a.heads);
+  const long long row = ((b * a.n_q + i) * a.heads + h) * D + lane * kPer;
+  float q[kPer], g[kPer], sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    q[e] = __bfloat162float(a.q[row + e]);
+    g[e] = __bfloat162float(a.d_o[row + e]);
+  }
+  const float lse2 = a.lse[at] * 1.4426950408889634f;
+  for (int j = 0; j < a.n_ctx + a.n_kc; ++j) {
+    const bool ctx = j < a.n_ctx;
+    const long long from = ctx ? (((a.shared ? 0 : b) * a.heads + h) * a.n_ctx + j) * D + lane * kPer
+                               : ((b * a.n_kc + (j - a.n_ctx)) * a.heads + h) * D + lane * kPer;
+    float s = 0.f, dp = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      s = fmaf(q[e], __bfloat162float((ctx ? a.kx : a.kc)[from + e]), s);
+      dp = fmaf(g[e], __bfloat162float((ctx ? a.vx : a.vc)[from + e]), dp);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, d);
+      dp += __shfl_xor_sync(0xffffffffu, dp, d);
+    }
+    sum = fmaf(fast_exp2(s * a.scale_log2 - lse2), dp, sum);
+  }
+  if (lane == 0) a.delta[at] = sum;
+}
+
 // ---------------------------------------------------------------------------------- few queries
 constexpr int kFewStep = 32;                       // keys of a step: two tiles of 16, whose latencies overlap
 

@@ -102,6 +102,7 @@ __device__ __noinline__ void win_careful_dq(const WinBwdArgs& a, int qt, int h, 
     if (row >= len) break;
     const size_t stat = (static_cast<size_t>(b) * a.heads + h) * a.mask.n + row;
     const float lse2 = a.lse[stat] * kLog2e, delta = a.delta[stat], scale_log2 = a.scale * kLog2e;
+    const bool alone = a.mask.one_key(row, len);
     const __nv_bfloat16* qp = a.q + b * a.qs.b + row * a.qs.t + h * a.qs.h + part * kPer;
     const size_t at = ((static_cast<size_t>(b) * a.mask.n + row) * a.heads + h) * D + part * kPer;
     float acc[kPer], q[kPer], g[kPer];
@@ -133,7 +134,8 @@ __device__ __noinline__ void win_careful_dq(const WinBwdArgs& a, int qt, int h, 
       }
       if ((x & 127) == 0 && __any_sync(0xffffffffu, lost)) break;   // NaN in every element: nothing to add to that
       if (there) {
-        const float ds = fast_exp2(s * scale_log2 - lse2) * (dp - delta);
+        float ds = fast_exp2(s * scale_log2 - lse2) * (dp - delta);
+        if (alone && fabsf(ds) < INFINITY) ds = 0.f;
         lost = lost || isnan(ds);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) acc[e] = fmaf(ds, __bfloat162float(kb[j * a.ks.t + e]), acc[e]);
@@ -317,7 +319,9 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
     const float scale_log2 = a.scale * kLog2e;
     const uint64_t sc2 = f32x2(scale_log2, scale_log2), nl2 = f32x2(-lse2, -lse2), nd2 = f32x2(-delta_r, -delta_r);
     int lo = 0, hi = 0;
-    if (live) a.mask.keys_of(row, len, lo, hi);
+    // A row of one key has dS = 0, of which dP - delta would leave fp32's rounding: it sees nothing, unless it is NaN or infinite.
+    const bool zero = a.mask.one_key(row, len) && fabsf(lse2) < INFINITY && fabsf(delta_r) < INFINITY;
+    if (live && !zero) a.mask.keys_of(row, len, lo, hi);
     const int sink = min(a.mask.sink, hi);
     int kt = tiles.first();
     for (int j = 0; j < n_tiles; ++j, kt = tiles.next(kt)) {
@@ -409,6 +413,7 @@ __device__ __noinline__ void win_careful_dkv(const WinBwdArgs& a, int kt, int kv
     }
     int first, last;
     a.mask.queries_of(row, len, first, last);
+    const bool alone = a.mask.one_key(row, len);
     for (int h = kvh * a.group; h < (kvh + 1) * a.group; ++h) {
       const size_t stat = (static_cast<size_t>(b) * a.heads + h) * a.mask.n;
       const __nv_bfloat16* qb = a.q + b * a.qs.b + h * a.qs.h + part * kPer;
@@ -436,7 +441,9 @@ __device__ __noinline__ void win_careful_dkv(const WinBwdArgs& a, int kt, int kv
           if (((lanes & 0xffu) == 0xffu) || (lanes >> 8 & 0xffu) == 0xffu || (lanes >> 16 & 0xffu) == 0xffu || lanes >> 24 == 0xffu) break;
         }
         if (there) {
-          const float p = fast_exp2(s * scale_log2 - a.lse[stat + i] * kLog2e), ds = p * (dp - a.delta[stat + i]);
+          const float p = fast_exp2(s * scale_log2 - a.lse[stat + i] * kLog2e);
+          float ds = p * (dp - a.delta[stat + i]);
+          if (alone && i == row && fabsf(ds) < INFINITY) ds = 0.f;
 #pragma unroll
           for (int e = 0; e < kPer; ++e) {
             dk[e] = fmaf(ds, __bfloat162float(qb[i * a.qs.t + e]), dk[e]);
@@ -655,10 +662,12 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     const bool live = key < len;
     int q_first = 0, q_last = 0;
     if (live) a.mask.queries_of(key, len, q_first, q_last);
+    const bool alone = live && a.mask.one_key(key, len);   // the query of the same token sees this key alone: dS = 0, as in dQ
     int qt = t0 + from % per_head;
     for (int i = 0; i < n_tiles; ++i) {
       const float* stat = sStat + (i % kStages) * 2 * kTile + g * kCols;
       const bool full = qt * kTile >= full_first && qt * kTile + kTile <= full_last;
+      const int own = alone ? key - qt * kTile - g * kCols : -1;   // its column
       uint32_t see[NL];
 #pragma unroll
       for (int c2 = 0; c2 < NL; ++c2) {
@@ -725,9 +734,11 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
           ds[c >> 1] = pack_bf16(d0, d1);
         }
         if (!full) {
+          uint32_t m = see[c2];
+          if (own >= c2 * 32 && own < c2 * 32 + 32 && fabsf(stat[own]) < INFINITY && fabsf(stat[kTile + own]) < INFINITY)
+            m &= ~(1u << (own & 31));
 #pragma unroll
-          for (int c = 0; c < 32; c += 2)
-            ds[c >> 1] &= ((see[c2] >> c) & 1u ? 0x0000ffffu : 0u) | ((see[c2] >> (c + 1)) & 1u ? 0xffff0000u : 0u);
+          for (int c = 0; c < 32; c += 2) ds[c >> 1] &= ((m >> c) & 1u ? 0x0000ffffu : 0u) | ((m >> (c + 1)) & 1u ? 0xffff0000u : 0u);
         }
         tmem_st16(tmem_lane + kColdPt + g * kCols + c2 * 16, ds);
       }

@@ -22,6 +22,12 @@ struct WinMask {
     lo = max(0, end - window);
     hi = min(len, end);
   }
+  // Whether query i sees one key alone, which is itself: its weight is 1 whatever the scores, and dS is 0.
+  __device__ __forceinline__ bool one_key(int i, int len) const {
+    int lo, hi;
+    keys_of(i, len, lo, hi);
+    return hi - lo + min(sink, lo) == 1;
+  }
   // the queries of key j: [first, last)
   __host__ __device__ __forceinline__ void queries_of(int j, int len, int& first, int& last) const {
     first = j / block * block;

@@ -236,3 +236,32 @@ def test_offsets_beyond_32_bits():
     for n_q in (2, 70):
         q, kc, vc, _ = tensors(torch, 1, n_q, 3, H, D, 14)
         compare(torch, A, cache, q, kc, vc, D ** -0.5, heads=(0, 15))
+
+
+@pytest.mark.parametrize("n_ctx,n_kc", [(1, 0), (0, 1), (1, 1), (3, 0), (40, 24)])
+def test_few_keys(n_ctx, n_kc):
+    """One key alone has no gradient; over a few, dS can be far smaller than delta, which then comes from the weights."""
+    torch, A = modules()
+    for Bc in (1, 2):
+        cache = A.astro_kvcache8_create(Bc, 4, 64, 1, 0, 64)
+        g = torch.Generator(device="cuda").manual_seed(n_ctx)
+        if n_ctx:
+            A.astro_kvcache8_append(cache, *(torch.randn(Bc, n_ctx, 4, 64, generator=g, device="cuda").bfloat16() for _ in range(2)), n_ctx)
+        q, kc, vc, d_o = tensors(torch, 2, 9, n_kc, 4, 64, n_kc)
+        o, lse = compare(torch, A, cache, q, kc, vc, 0.5, d_o)
+        dq, dk, dv = A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, 0.5)
+        if n_ctx + n_kc == 1:
+            assert not dq.any() and (not n_kc or not dk.any())
+            continue
+        k8, v8 = (x.double() for x in A.astro_kvcache8_read(cache, dtype=torch.float32))
+        for b in range(2):
+            for h in range(4):
+                kk, vv = (torch.cat([x[b if Bc > 1 else 0, :, h]] + ([y[b, :, h].double()] if n_kc else [])) for x, y in ((k8, kc), (v8, vc)))
+                qq, gg = q[b, :, h].double(), d_o[b, :, h].double()
+                p = torch.softmax(0.5 * qq @ kk.T, 1)
+                dp = gg @ vv.T
+                ds = p * (dp - (p * dp).sum(1, keepdim=True))
+                size = 0.5 * (qq.abs() @ kk.abs().T).amax(1, keepdim=True)
+                err = 2.0 ** -8 * ds.abs() + 2.0 ** -18 * (1 + size) * p * (gg.abs() @ vv.abs().T).amax(1, keepdim=True)
+                want = 0.5 * ds @ kk
+                check(dq[b, :, h], (want, 1.1 * (0.5 * err @ kk.abs() + 2.0 ** -8 * want.abs()) + 1e-7), "dQ")

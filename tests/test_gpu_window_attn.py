@@ -355,3 +355,15 @@ def test_rows_of_which_one_key_has_nearly_all_the_weight(D, n):
                 dk = dk + scale * (ds.T @ qq)
                 dk_err = dk_err + scale * (err.T @ qq.abs())
             check(grads[1][b, :, kv], (dk, 1.1 * (dk_err + h8 * dk.abs()) + 1e-7), "dK")
+
+
+def test_rows_of_one_key_have_no_gradient():
+    torch, A = modules()
+    for block, window, sink, lengths in ((1, 1, 0, None), (1, 50, 0, None), (1, 1, 1, (300, 1)), (10, 20, 3, (1, 1)), (1, None, 4, (1, 300))):
+        q, k, v, d_o = tensors(torch, 2, 300, 4, 2, 64, 20)
+        _, _, (dq, dk, dv) = compare(torch, A, q, k, v, d_o, block, window, sink, lengths)
+        one = torch.stack([mask(torch, 300, 300 if lengths is None else n, block, 10 ** 9 if window is None else window, sink).sum(1) == 1
+                           for n in (lengths or (300, 300))])
+        assert not dq[one].any()
+        if block == 1 and window == 1 and sink == 0:
+            assert not dk.any() and torch.equal(dv, d_o.unflatten(2, (2, 2)).float().sum(3).bfloat16())
