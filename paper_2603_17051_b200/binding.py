@@ -872,9 +872,9 @@ def astro_kvcache8_read(cache: KVCache, first_frame: int = 0, n_frames=None, dty
     fresh = []
     with _owned_by(stream):
         if k_out is None:
-            k_out = torch.empty(shape, dtype=dtype, device=cache.k_storage.device); fresh.append(k_out)
+            k_out = cache.k_storage.new_empty(shape, dtype=dtype); fresh.append(k_out)
         if v_out is None:
-            v_out = torch.empty(shape, dtype=dtype, device=cache.k_storage.device); fresh.append(v_out)
+            v_out = torch.empty_like(k_out); fresh.append(v_out)
     _used_here(stream, *fresh)
     _check(lib().astro_kvcache8_read(_handle(cache, dev), _int(first_frame), _int(n_frames), kind, _at(k_out), _at(v_out), on),
            "astro_kvcache8_read")
@@ -951,26 +951,36 @@ def astro_chunk_attn8_bwd(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: float,
     return dq, dk_chunk, dv_chunk
 
 
+def _packed_like(x):
+    """A contiguous tensor of x's shape and type; what keeps x's strides is quicker to make where those are the contiguous ones."""
+    import torch
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 def _window_call(q, k, v, block_tokens, window_tokens, sink_tokens, lengths, dev):
     """(descriptor, [address and strides of q, k, v], address of lengths) of a call on whole sequences."""
     import torch
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+    shape, of_k = q.shape, k.shape
+    if len(shape) != 4 or len(of_k) != 4:
         raise ValueError("q, k and v must be [B, n, heads, head_dim]")
-    B, n, H, D = q.shape
+    B, n, H, D = shape
+    kv_heads = of_k[2]
+    if of_k != (B, n, kv_heads, D) or v.shape != of_k:
+        raise ValueError("q, k and v must be [B, n, heads, head_dim] alike, k and v of the same heads")
     rows = []
-    for x, heads in ((q, H), (k, k.shape[2]), (v, k.shape[2])):
-        if x.dtype is not torch.bfloat16 or x.get_device() != dev or x.shape != (B, n, heads, D):
-            raise ValueError("q, k and v must be bf16 [B, n, heads, head_dim] beside each other, k and v of the same heads")
+    for x in (q, k, v):
+        if x.dtype is not torch.bfloat16 or x.get_device() != dev:
+            raise ValueError("q, k and v must be bf16 on one device")
         if x.is_contiguous():
-            rows += [x.data_ptr(), None]
+            rows += (x.data_ptr(), None)
             continue
         if x.stride(3) != 1:
             raise ValueError("the elements of a head must be contiguous")
-        rows += [x.data_ptr(), C.byref(Strides(*_rope_strides(x)))]
+        rows += (x.data_ptr(), C.byref(Strides(*_rope_strides(x))))
     if lengths is not None:
         _like((B,), torch.int32, dev, lengths)
     window = 0x7fffffff if window_tokens is None else _int(window_tokens)
-    d = WindowDesc(B, _int(n), H, k.shape[2], D, _int(block_tokens), window, _int(sink_tokens))
+    d = WindowDesc(B, _int(n), H, kv_heads, D, _int(block_tokens), window, _int(sink_tokens))
     return d, rows, _at(lengths)
 
 
@@ -989,7 +999,7 @@ def astro_window_attn_fwd(q, k, v, scale: float, block_tokens: int = 1, window_t
     fresh = []
     with _owned_by(stream):
         if o is None:
-            o = torch.empty(shape, dtype=q.dtype, device=q.device); fresh.append(o)
+            o = _packed_like(q); fresh.append(o)
         if lse is None:
             lse = q.new_empty((B, H, n), dtype=torch.float32); fresh.append(lse)
     _used_here(stream, *fresh)
@@ -1014,11 +1024,11 @@ def astro_window_attn_bwd(q, k, v, o, lse, d_o, scale: float, block_tokens: int 
     fresh = []
     with _owned_by(stream):
         if dq is None:
-            dq = torch.empty(shape, dtype=q.dtype, device=q.device); fresh.append(dq)
+            dq = _packed_like(q); fresh.append(dq)
         if dk is None:
-            dk = torch.empty(k.shape, dtype=q.dtype, device=q.device); fresh.append(dk)
+            dk = _packed_like(k); fresh.append(dk)
         if dv is None:
-            dv = torch.empty(k.shape, dtype=q.dtype, device=q.device); fresh.append(dv)
+            dv = _packed_like(v); fresh.append(dv)
         if workspace is None:
             need = astro_window_attn_bwd_workspace_bytes(B, H, n, D)
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)

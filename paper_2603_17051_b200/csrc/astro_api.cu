@@ -2044,10 +2044,11 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
   if (s == ASTRO_OK && n_kc > 0)
     s = astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, batch, heads, head_dim, n_q, n_kc, scale, dk_chunk, dv_chunk, stream);
   if (s != ASTRO_OK || keys > 1) return s;
-  // A softmax over one key is constant: no gradient for queries and keys, where the kernels leave fp32's rounding of dP - delta.
-  const size_t row = static_cast<size_t>(batch) * heads * head_dim * 2;
-  if (cudaMemsetAsync(dq, 0, row * n_q, st) != cudaSuccess) return ASTRO_ERR_CUDA;
-  return n_kc == 0 || cudaMemsetAsync(dk_chunk, 0, row, st) == cudaSuccess ? ASTRO_OK : ASTRO_ERR_CUDA;
+  for (int i = 0; i < (n_kc ? 2 : 1); ++i) {
+    const long long pairs = static_cast<long long>(batch) * heads * (i ? 1 : n_q) * head_dim / 2;
+    attn8_one_key_kernel<<<static_cast<unsigned>((pairs + 255) / 256), 256, 0, st>>>(static_cast<__nv_bfloat162*>(i ? dk_chunk : dq), pairs);
+  }
+  return launch_status();
 }
 
 // ---- sliding window with sinks over whole sequences ---------------------------------------------------

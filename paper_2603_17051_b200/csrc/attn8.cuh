@@ -118,6 +118,15 @@ __global__ void __launch_bounds__(128) attn8_short_delta_kernel(const ShortDelta
   if (lane == 0) a.delta[at] = sum;
 }
 
+// A softmax over one key is constant: no gradient for its queries and for it, where the kernels leave fp32's rounding of
+// dP - delta.  What is NaN or infinite stays.  n pairs of elements.
+__global__ void __launch_bounds__(256) attn8_one_key_kernel(__nv_bfloat162* x, long long n) {
+  const long long i = blockIdx.x * 256ll + threadIdx.x;
+  if (i >= n) return;
+  const float2 v = __bfloat1622float2(x[i]);
+  x[i] = __floats2bfloat162_rn(fabsf(v.x) < INFINITY ? 0.f : v.x, fabsf(v.y) < INFINITY ? 0.f : v.y);
+}
+
 // ---------------------------------------------------------------------------------- few queries
 constexpr int kFewStep = 32;                       // keys of a step: two tiles of 16, whose latencies overlap
 

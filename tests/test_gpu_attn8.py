@@ -265,3 +265,15 @@ def test_few_keys(n_ctx, n_kc):
                 err = 2.0 ** -8 * ds.abs() + 2.0 ** -18 * (1 + size) * p * (gg.abs() @ vv.abs().T).amax(1, keepdim=True)
                 want = 0.5 * ds @ kk
                 check(dq[b, :, h], (want, 1.1 * (0.5 * err @ kk.abs() + 2.0 ** -8 * want.abs()) + 1e-7), "dQ")
+
+
+def test_one_key_of_nan():
+    torch, A = modules()
+    q, kc, vc, d_o = tensors(torch, 1, 9, 1, 4, 64, 3)
+    q[0, 4, 1] = float("nan")
+    o, lse = A.astro_chunk_attn8_fwd(None, q, kc, vc, 0.5)
+    dq, dk, dv = A.astro_chunk_attn8_bwd(None, q, kc, vc, o, lse, d_o, 0.5)
+    bad = torch.zeros(9, 4, dtype=torch.bool, device="cuda")
+    bad[4, 1] = True
+    assert dq[0, bad].isnan().all() and not dq[0, ~bad].any()
+    assert dk[0, 0, 1].isnan().all() and not dk[0, 0, [0, 2, 3]].any()
