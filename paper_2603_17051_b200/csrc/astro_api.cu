@@ -1050,10 +1050,10 @@ astro_status_t check_window(const astro_window_desc_t& d) {
 WinMask window_mask(const astro_window_desc_t& d, const int32_t* lengths) {
   WinMask m;
   m.n = d.n_tokens;
-  m.block = d.block_tokens < d.n_tokens ? d.block_tokens : d.n_tokens;
+  m.block.set(d.block_tokens < d.n_tokens ? d.block_tokens : d.n_tokens);
   // a window that reaches to the first token from the end of any block shows everything in front (a block longer than the
   // sequence is the sequence)
-  const int most = d.n_tokens + m.block;
+  const int most = d.n_tokens + m.block.d;
   m.window = d.block_tokens > d.n_tokens || d.window_tokens > most ? most : d.window_tokens;
   m.sink = d.sink_tokens < d.n_tokens ? d.sink_tokens : d.n_tokens;
   m.lengths = lengths;
@@ -1106,6 +1106,8 @@ astro_status_t launch_window_fwd(const WindowCall& c, float scale, void* o, floa
   a.mask = window_mask(c.d, c.lengths);
   a.heads = c.d.heads;
   a.group = c.d.heads / c.d.kv_heads;
+  a.by_heads.set(a.heads);
+  a.by_group.set(a.group);
   a.order.set(c.d.batch * c.d.heads, (c.d.n_tokens + kTile - 1) / kTile);
   a.scale = scale;
   a.scale_log2 = scale * kLog2e;
@@ -1133,7 +1135,7 @@ WinShares window_shares(const astro_window_desc_t& d) {
   w.front = (m.sink + kTile - 1) / kTile;
   if (w.front == 0) return w;
   const long long tiles = (d.n_tokens + kTile - 1) / kTile, group = d.heads / d.kv_heads;
-  long long usual = (m.window + m.block) / kTile + 2;       // tiles that a tile behind the sinks meets, about
+  long long usual = (m.window + m.block.d) / kTile + 2;       // tiles that a tile behind the sinks meets, about
   if (usual > tiles) usual = tiles;
   const long long longest = tiles * group, lists = static_cast<long long>(d.batch) * d.heads;
   const long long all = 2 * lists * tiles * usual + lists * w.front * tiles;   // dQ's and dK/dV's
@@ -1174,6 +1176,9 @@ astro_status_t launch_window_bwd(const WindowCall& c, const void* o, const float
   a.heads = d.heads;
   a.kv_heads = d.kv_heads;
   a.group = d.heads / d.kv_heads;
+  a.by_heads.set(a.heads);
+  a.by_kv_heads.set(a.kv_heads);
+  a.by_group.set(a.group);
   a.lists = d.batch * d.heads;
   a.kv_lists = d.batch * d.kv_heads;
   a.tiles = (d.n_tokens + kTile - 1) / kTile;

@@ -26,6 +26,7 @@ struct WinBwdArgs {
   __nv_bfloat16 *dq, *dk, *dv;    // [B, n, H or KVH, D]
   WinMask mask;
   int heads, kv_heads, group, lists, kv_lists, tiles;   // lists = batch * heads, kv_lists = batch * kv_heads
+  Divisor by_heads, by_kv_heads, by_group;
   WinOrder q_order, k_order;      // of the query tiles and of the key tiles behind the front ones
   int front;                      // key tiles of the sinks, where they come first
   int shares;                     // CTAs that share each of them
@@ -152,7 +153,7 @@ __device__ __noinline__ void win_careful_dq(const WinBwdArgs& a, int qt, int h, 
 
 template <int D>
 __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CUtensorMap& tm_do,
-                                           const WinBwdArgs& a, const int qt, const int h, const int b) {
+                                           const WinBwdArgs& a, const int qt, const int list) {
   uint8_t* smem = align_1024(smem_raw);
   uint8_t* sdO = smem + DqSmem<D>::kdO;
   uint8_t* sK = smem + DqSmem<D>::kK;
@@ -164,7 +165,8 @@ __device__ __forceinline__ void win_bwd_dq(uint8_t* smem_raw, const CUtensorMap&
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int q0 = qt * kTile, len = a.mask.length(b), kvh = h / a.group;
+  const int b = a.by_heads.quot(list), h = list - b * a.heads;
+  const int q0 = qt * kTile, len = a.mask.length(b), kvh = a.by_group.quot(h);
   constexpr uint32_t kTmemCols = 512;
   constexpr uint32_t kColS = 0, kColdP = 128, kColdS = 256, kColQ = 320, kColdQ = 384;
   constexpr int kMmaWarp = 4 * kWinGroups, kTmaWarp = kMmaWarp + 1, kCols = kTile / kWinGroups, NL = kCols / 32;
@@ -498,7 +500,7 @@ template <int D> struct WinDkvSmem {
 
 template <int D>
 __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap& tm_q, const CUtensorMap& tm_do, const CUtensorMap& tm_k,
-                                            const CUtensorMap& tm_v, const WinBwdArgs& a, const int kt, const int kvh, const int b,
+                                            const CUtensorMap& tm_v, const WinBwdArgs& a, const int kt, const int list,
                                             const int share, const int shares, float* part) {
   using S = WinDkvSmem<D>;
   constexpr int kStages = S::kStages, kSBufs = S::kSBufs;
@@ -515,6 +517,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = a.by_kv_heads.quot(list), kvh = list - b * a.kv_heads;
   const int k0 = kt * kTile, len = a.mask.length(b);
   constexpr uint32_t kTmemCols = 512;
   constexpr uint32_t kColSt = 0, kColdPt = 128 * kSBufs, kColdK = kColdPt + 128, kColdV = kColdK + D;
@@ -535,8 +538,11 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     per_head = (last - 1) / kTile + 1 - t0;
     // this CTA's share of the list of (head, query tile)
     const int all = per_head * a.group;
-    from = static_cast<int>(static_cast<long long>(all) * share / shares);
-    n_tiles = static_cast<int>(static_cast<long long>(all) * (share + 1) / shares) - from;
+    n_tiles = all;
+    if (shares > 1) {
+      from = static_cast<int>(static_cast<long long>(all) * share / shares);
+      n_tiles = static_cast<int>(static_cast<long long>(all) * (share + 1) / shares) - from;
+    }
   }
   if (n_tiles == 0) {   // the same for the whole CTA
     dependency_wait();
@@ -580,7 +586,8 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
       tma_load_tile<D>(sV, &tm_v, kv_full, k0, kvh, b);
     }
     dependency_wait();   // delta
-    int h = kvh * a.group + from / per_head, qt = t0 + from % per_head, fixes = 0;
+    const int skipped = from == 0 ? 0 : from / per_head;
+    int h = kvh * a.group + skipped, qt = t0 + from - skipped * per_head, fixes = 0;
     for (int i = 0; i < n_tiles; ++i) {
       const int st = i % kStages;
       if (!mbar_wait_ok(q_empty + st, ((i / kStages) & 1) ^ 1, abort_flag)) break;   // no copies once a wait has run out
@@ -663,7 +670,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     int q_first = 0, q_last = 0;
     if (live) a.mask.queries_of(key, len, q_first, q_last);
     const bool alone = live && a.mask.one_key(key, len);   // the query of the same token sees this key alone: dS = 0, as in dQ
-    int qt = t0 + from % per_head;
+    int qt = from == 0 ? t0 : t0 + from % per_head;
     for (int i = 0; i < n_tiles; ++i) {
       const float* stat = sStat + (i % kStages) * 2 * kTile + g * kCols;
       const bool full = qt * kTile >= full_first && qt * kTile + kTile <= full_last;
@@ -822,17 +829,20 @@ window_attn_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
   const int behind = a.kv_lists * (a.tiles - a.front);
   int i = blockIdx.x;
   if (i < front) {
-    const int share = i % a.shares, x = i / a.shares, kt = x / a.kv_lists, list = x - kt * a.kv_lists;
-    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, kt, list % a.kv_heads, list / a.kv_heads, share, a.shares,
+    int x = i, share = 0, kt = 0;
+    if (a.shares > 1) { x = i / a.shares; share = i - x * a.shares; }
+    if (a.front > 1) kt = x / a.kv_lists;
+    const int list = x - kt * a.kv_lists;
+    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, kt, list, share, a.shares,
                    a.shares > 1 ? a.parts + static_cast<size_t>(i) * (2 * kTile * D) : nullptr);
   } else if ((i -= front) < behind) {
     int tile, list;
     a.k_order.place(i, tile, list);
-    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, a.front + tile, list % a.kv_heads, list / a.kv_heads, 0, 1, nullptr);
+    win_bwd_dkv<D>(smem_raw, tm_q, tm_do, tm_k, tm_v, a, a.front + tile, list, 0, 1, nullptr);
   } else {
     int tile, list;
     a.q_order.place(i - behind, tile, list);
-    win_bwd_dq<D>(smem_raw, tm_k, tm_v, tm_do, a, a.tiles - 1 - tile, list % a.heads, list / a.heads);
+    win_bwd_dq<D>(smem_raw, tm_k, tm_v, tm_do, a, a.tiles - 1 - tile, list);
   }
 }
 template <int D> constexpr int window_bwd_smem() {

@@ -12,13 +12,37 @@
 
 namespace astro {
 
+// A divisor that a whole launch shares: quotients of 0 <= x < 2^31 by one wide multiplication (Granlund and Montgomery, "Division by
+// invariant integers using multiplication", 1994).  With l = ceil(log2 d) and mul = floor(2^32 (2^l - d) / d) + 1 the quotient is
+// (floor(mul x / 2^32) + x) / 2^l.  A kernel's start is a chain of such quotients: with the operator's some 150 clocks each, a
+// dK/dV CTA took 2300 to its first barrier.
+struct Divisor {
+  int d, shift;
+  uint32_t mul;
+  __host__ void set(int d_) {
+    d = d_;
+    shift = 0;
+    while ((1u << shift) < static_cast<uint32_t>(d)) ++shift;
+    mul = static_cast<uint32_t>((((1ull << shift) - d) << 32) / d + 1);
+  }
+  __host__ __device__ __forceinline__ int quot(int x) const {
+#ifdef __CUDA_ARCH__
+    const uint32_t high = __umulhi(mul, static_cast<uint32_t>(x));
+#else
+    const uint32_t high = static_cast<uint32_t>((static_cast<unsigned long long>(mul) * static_cast<uint32_t>(x)) >> 32);
+#endif
+    return static_cast<int>((high + static_cast<uint32_t>(x)) >> shift);
+  }
+};
+
 struct WinMask {
-  int n, block, window, sink;   // block <= n, window <= n + block, sink <= n
+  int n, window, sink;   // window <= n + block, sink <= n
+  Divisor block;         // <= n
   const int* lengths;           // may be null: n each
   __host__ __device__ __forceinline__ int length(int b) const { return lengths == nullptr ? n : max(0, min(n, lengths[b])); }
   // the keys of query i of a sequence of `len`: [0, sink) below hi, and [lo, hi)
   __host__ __device__ __forceinline__ void keys_of(int i, int len, int& lo, int& hi) const {
-    const int end = (i / block + 1) * block;
+    const int end = (block.quot(i) + 1) * block.d;
     lo = max(0, end - window);
     hi = min(len, end);
   }
@@ -30,8 +54,8 @@ struct WinMask {
   }
   // the queries of key j: [first, last)
   __host__ __device__ __forceinline__ void queries_of(int j, int len, int& first, int& last) const {
-    first = j / block * block;
-    last = j < sink ? len : min(len, (j + window) / block * block);
+    first = block.quot(j) * block.d;
+    last = j < sink ? len : min(len, block.quot(j + window) * block.d);
   }
 };
 
@@ -76,22 +100,22 @@ struct WinTiles {
 // 256 tiles).  So: groups of lists of one size, one after the other, tile by tile within, eight rounds of 148 CTAs and more in each.
 struct WinOrder {
   int lists, tiles, per_group;
+  Divisor group_tiles, by_lists, by_rest;   // a group's tiles; its lists, the last group's
   __host__ void set(int lists_, int tiles_) {
     lists = lists_;
     tiles = tiles_;
     const long long groups = static_cast<long long>(lists) * tiles / (8 * 148);
     per_group = groups <= 1 ? lists : static_cast<int>((lists + groups - 1) / groups);
+    group_tiles.set(max(1, static_cast<int>(min(static_cast<long long>(per_group) * tiles, 0x40000000ll))));
+    by_lists.set(per_group);
+    by_rest.set(lists - (lists - 1) / per_group * per_group);
   }
   __device__ __forceinline__ void place(int i, int& tile, int& list) const {
-    int first = 0, here = lists;
-    if (per_group < lists) {
-      const int group = i / (per_group * tiles);
-      first = group * per_group;
-      i -= first * tiles;
-      here = min(per_group, lists - first);
-    }
-    tile = i / here;
-    list = first + i - tile * here;
+    const int first = group_tiles.quot(i) * per_group;
+    i -= first * tiles;
+    const bool rest = first + per_group > lists;
+    tile = rest ? by_rest.quot(i) : by_lists.quot(i);
+    list = first + i - tile * (rest ? by_rest.d : by_lists.d);
   }
 };
 

@@ -30,6 +30,7 @@ struct WinFwdArgs {
   float* lse;              // [B, H, n], may be null
   WinMask mask;
   int heads, group;        // group: heads that share K and V
+  Divisor by_heads, by_group;
   WinOrder order;
   float scale, scale_log2;
   int careful;             // 1: the second pass only
@@ -62,7 +63,7 @@ struct WinUnit {
     int tile, list;
     a.order.place(id, tile, list);
     qt = a.order.tiles - 1 - tile;
-    b = list / a.heads;
+    b = a.by_heads.quot(list);
     h = list - b * a.heads;
   }
 };
@@ -210,7 +211,7 @@ template <int D> struct WinStream {
     const WinUnit w(a, u.id);
     win_tiles(a, w, len, t);
     qt = w.qt;
-    kvh = w.h / a.group;
+    kvh = a.by_group.quot(w.h);
     b = w.b;
     kt = qt;
     diagonal = true;
@@ -420,57 +421,47 @@ __device__ __forceinline__ bool win_softmax(const WinCta<D>& c, const WinFwdArgs
       const int base = kt * kTile + g * kFwdCols;
       return bits_below(sink, base) | (bits_below(hi, base) & ~bits_below(lo, base));
     };
-    // the diagonal tile fixes the rows' reference
-    float m_ref = 0.f, l_run;
-    {
+    // the diagonal tile comes first and fixes the rows' reference; full tiles in runs, all others, the first too, in one piece of
+    // code, since in short calls much of the time goes into fetching instructions
+    float m_ref = 0.f, l_run = 0.f;
+    bool first = true;
+    for (int kt = w.qt; kt < t.w1;) {
+      if (!first && kt == w.qt) { kt = t.next(kt); continue; }
+      if (!first && t.full(kt)) {
+        const int end = t.run_end(kt), count = end - kt - (w.qt >= kt && w.qt < end ? 1 : 0);
+        l_run = win_run(lane_s, sdone, ready, abort_at, a.scale_log2, -m_ref, l_run, J, count);
+        J += count;
+        kt = t.next(end - 1);
+        continue;
+      }
       const uint32_t colS = lane_s + (J % kFwdSBufs) * 128;
       mbar_wait_at(sdone + 8 * (J % 4), (J / 4) & 1, abort_at);
       tc_fence_after_sync();
       uint32_t s[32], pk[16];
       tmem_ld32(colS, s);
-      const uint32_t bits = see(w.qt);
+      const uint32_t bits = see(kt);
       tmem_wait_ld();
-      float mx = -INFINITY;
+      if (first) {
+        float mx = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < 32; ++k) mx = fmaxf(mx, (bits >> k) & 1u ? __uint_as_float(s[k]) : -INFINITY);
-      float* slot = stats.maxima(n);   // alternates: a fast thread may be a unit ahead of the others
-      slot[g * kTile + r] = mx;
-      warp_arrive(bar.max_full + (warp & 3), lane);
-      mbar_wait(bar.max_full + (warp & 3), n & 1, c.abort_flag);
+        for (int k = 0; k < 32; ++k) mx = fmaxf(mx, (bits >> k) & 1u ? __uint_as_float(s[k]) : -INFINITY);
+        float* slot = stats.maxima(n);   // alternates: a fast thread may be a unit ahead of the others
+        slot[g * kTile + r] = mx;
+        warp_arrive(bar.max_full + (warp & 3), lane);
+        mbar_wait(bar.max_full + (warp & 3), n & 1, c.abort_flag);
 #pragma unroll
-      for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
-      // a live row whose scores are all -infinity or NaN gets an infinite reference, and with it the second pass
-      if (live) m_ref = mx * a.scale_log2;
-      l_run = win_exp32(s, bits, a.scale_log2, -m_ref, pk);
+        for (int og = 0; og < kFwdGroups; ++og) mx = fmaxf(mx, slot[og * kTile + r]);
+        // a live row whose scores are all -infinity or NaN gets an infinite reference, and with it the second pass
+        if (live) m_ref = mx * a.scale_log2;
+      }
+      l_run += win_exp32(s, bits, a.scale_log2, -m_ref, pk);
       tmem_st16(colS, pk);
       tmem_wait_st();
       tc_fence_before_sync();
       warp_arrive_at(ready + 8 * (J % 4), lane);
       ++J;
-    }
-    for (int kt = t.first(); kt < t.w1;) {
-      if (kt == w.qt) { kt = t.next(kt); continue; }
-      if (t.full(kt)) {
-        const int end = t.run_end(kt), count = end - kt - (w.qt >= kt && w.qt < end ? 1 : 0);
-        l_run = win_run(lane_s, sdone, ready, abort_at, a.scale_log2, -m_ref, l_run, J, count);
-        J += count;
-        kt = t.next(end - 1);
-      } else {
-        const uint32_t colS = lane_s + (J % kFwdSBufs) * 128;
-        mbar_wait_at(sdone + 8 * (J % 4), (J / 4) & 1, abort_at);
-        tc_fence_after_sync();
-        uint32_t s[32], pk[16];
-        tmem_ld32(colS, s);
-        const uint32_t bits = see(kt);
-        tmem_wait_ld();
-        l_run += win_exp32(s, bits, a.scale_log2, -m_ref, pk);
-        tmem_st16(colS, pk);
-        tmem_wait_st();
-        tc_fence_before_sync();
-        warp_arrive_at(ready + 8 * (J % 4), lane);
-        ++J;
-        kt = t.next(kt);
-      }
+      kt = first ? t.first() : t.next(kt);
+      first = false;
     }
     // the slots of unit n - 2 are free: the epilogue warps brought Q of unit n after they had read them
     stats.sums(n)[g * kTile + r] = l_run;
