@@ -441,10 +441,14 @@ __device__ __forceinline__ bool win_softmax(const WinCta<D>& c, const WinFwdArgs
       tmem_ld32(colS, s);
       const uint32_t bits = see(kt);
       tmem_wait_ld();
+      // 32 rows by 32 keys of which none is seen: a third of the diagonal tile, most of the sinks'
+      const bool any = __any_sync(0xffffffffu, bits != 0u);
       if (first) {
         float mx = -INFINITY;
+        if (any) {
 #pragma unroll
-        for (int k = 0; k < 32; ++k) mx = fmaxf(mx, (bits >> k) & 1u ? __uint_as_float(s[k]) : -INFINITY);
+          for (int k = 0; k < 32; ++k) mx = fmaxf(mx, (bits >> k) & 1u ? __uint_as_float(s[k]) : -INFINITY);
+        }
         float* slot = stats.maxima(n);   // alternates: a fast thread may be a unit ahead of the others
         slot[g * kTile + r] = mx;
         warp_arrive(bar.max_full + (warp & 3), lane);
@@ -454,7 +458,12 @@ __device__ __forceinline__ bool win_softmax(const WinCta<D>& c, const WinFwdArgs
         // a live row whose scores are all -infinity or NaN gets an infinite reference, and with it the second pass
         if (live) m_ref = mx * a.scale_log2;
       }
-      l_run += win_exp32(s, bits, a.scale_log2, -m_ref, pk);
+      if (any) {
+        l_run += win_exp32(s, bits, a.scale_log2, -m_ref, pk);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) pk[k] = 0u;
+      }
       tmem_st16(colS, pk);
       tmem_wait_st();
       tc_fence_before_sync();
