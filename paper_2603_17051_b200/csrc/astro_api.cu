@@ -345,13 +345,13 @@ astro_status_t launch_bwd_dq(const AttnArgs& a, const __nv_bfloat16* q, const CU
                              const KeySegs& segs, float scale, const float* lse, const float* delta, void* dq,
                              cudaStream_t st) {
   static std::atomic<int> done[kMaxDevices];
-  astro_status_t s = set_smem_once(chunk_attn_bwd_dq_kernel<D>, DqSmem<D>::kTotal, done);
+  astro_status_t s = set_smem_once(chunk_attn_bwd_dq_kernel<D, false>, DqSmem<D>::kTotal, done);
   if (s != ASTRO_OK) return s;
   const int shared = (a.cache && a.cache->d.cache_batch == 1 && a.batch > 1) ? 1 : 0;
   dim3 grid_q((a.n_q + kTile - 1) / kTile, shared ? a.batch : a.heads, shared ? a.heads : a.batch);
-  chunk_attn_bwd_dq_kernel<D><<<grid_q, kDqThreads, DqSmem<D>::kTotal, st>>>(
+  chunk_attn_bwd_dq_kernel<D, false><<<grid_q, kDqThreads, DqSmem<D>::kTotal, st>>>(
       q, tdo, tkc, tvc, tkx[0], tkx[1], tvx, segs, a.n_q, a.heads, shared, scale, lse, delta,
-      static_cast<__nv_bfloat16*>(dq));
+      static_cast<__nv_bfloat16*>(dq), DqParts{});
   return launch_status();
 }
 
@@ -966,6 +966,38 @@ astro_status_t launch_few(const Attn8Call& c, float scale, void* o, float* lse, 
   if ((s = launch_status()) != ASTRO_OK || f.splits == 1) return s;
   return launch_dependent(sparse_combine_kernel<D>, dim3(static_cast<unsigned>((rows + 7) / 8)), 256, 0, st, f.part_o, f.part_lse,
                           f.splits, rows, c.a.n_q, c.a.heads, f.o, lse);
+}
+
+// dQ of few query tiles over many keys: the CTAs that share the keys of each tile.  One CTA takes 1.15 us for a key tile (0.95 at
+// head_dim 64), and 10 us to start, end and have its part joined; so: as many as fill the SMs once, eight key tiles and more to each.
+// (The whole backward, us, undivided and divided: 28080 keys, 12 heads, head_dim 128, 5 queries 288 and 99, 700 queries 303 and 204; one
+// head, 8000 keys, head_dim 64: 77 and 32; one head, 2000 keys: 31 and 25; 1560 keys, 12 heads, 12 key tiles and so undivided: 31.)
+int dq_splits(const astro_kvcache* cache, int batch, int heads, int n_q, int n_kc) {
+  constexpr int kSms = 148;
+  const long long units = (static_cast<long long>(n_q) + kTile - 1) / kTile * heads * batch;
+  const long long tiles = (static_cast<long long>(held_tokens(cache)) + kTile - 1) / kTile + (static_cast<long long>(n_kc) + kTile - 1) / kTile;
+  const long long splits = std::min(kSms / units, tiles / 8);
+  return splits < 2 ? 1 : static_cast<int>(splits);
+}
+size_t dq_part_bytes(const astro_kvcache* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
+  const int splits = dq_splits(cache, batch, heads, n_q, n_kc);
+  return splits == 1 ? 0 : static_cast<size_t>(splits) * batch * heads * n_q * head_dim * sizeof(float);
+}
+template <int D>
+astro_status_t launch_dq_parts(const AttnArgs& a, const __nv_bfloat16* q, const CUtensorMap& tdo, const CUtensorMap& tkc, const CUtensorMap& tvc,
+                               const CUtensorMap& tkx, const CUtensorMap& tvx, const KeySegs& segs, float scale, const float* lse,
+                               const float* delta, int splits, float* parts, void* dq, cudaStream_t st) {
+  static std::atomic<int> done[kMaxDevices];
+  astro_status_t s = set_smem_once(chunk_attn_bwd_dq_kernel<D, true>, DqSmem<D>::kTotal, done);
+  if (s != ASTRO_OK) return s;
+  const int shared = (a.cache && a.cache->d.cache_batch == 1 && a.batch > 1) ? 1 : 0, tiles = (a.n_q + kTile - 1) / kTile;
+  const dim3 grid(tiles * splits, shared ? a.batch : a.heads, shared ? a.heads : a.batch);
+  chunk_attn_bwd_dq_kernel<D, true><<<grid, kDqThreads, DqSmem<D>::kTotal, st>>>(q, tdo, tkc, tvc, tkx, tkx, tvx, segs, a.n_q, a.heads, shared,
+                                                                                 scale, lse, delta, nullptr, DqParts{parts, tiles, splits});
+  if ((s = launch_status()) != ASTRO_OK) return s;
+  const long long rows = static_cast<long long>(a.batch) * a.heads * a.n_q, threads = rows * (D / 4);
+  return launch_dependent(attn8_join_dq_kernel<D>, dim3(static_cast<unsigned>((threads + 255) / 256)), 256, 0, st, parts, splits, rows, a.n_q,
+                          a.heads, scale, static_cast<__nv_bfloat16*>(dq));
 }
 
 // Bytes of the held rows in bf16, K or V.
@@ -1988,7 +2020,8 @@ astro_status_t astro_chunk_attn8_fwd(const astro_kvcache_t* cache, const void* q
 
 size_t astro_chunk_attn8_bwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
   if (check_attn_args(AttnArgs{cache, batch, heads, head_dim, n_q, n_kc}, 1.f, 8) != ASTRO_OK) return 0;
-  return 2 * expanded_bytes(cache) + astro_chunk_attn_bwd_workspace_bytes(batch, heads, n_q, head_dim);
+  return 2 * expanded_bytes(cache) + dq_part_bytes(cache, batch, heads, head_dim, n_q, n_kc) +
+         astro_chunk_attn_bwd_workspace_bytes(batch, heads, n_q, head_dim);
 }
 
 astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
@@ -2014,7 +2047,9 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
     if ((s = make_tmap_user(&tkc, k_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
     if ((s = make_tmap_user(&tvc, v_chunk, head_dim, n_kc, heads, batch)) != ASTRO_OK) return s;
   }
-  float* delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * expanded_bytes(cache));
+  const int splits = dq_splits(cache, batch, heads, n_q, n_kc);
+  float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * expanded_bytes(cache));
+  float* delta = parts + dq_part_bytes(cache, batch, heads, head_dim, n_q, n_kc) / sizeof(float);
   Expanded x;
   if ((s = expand_context(c, workspace, &x, st)) != ASTRO_OK) return s;
   const long long keys = static_cast<long long>(held_tokens(cache)) + n_kc;
@@ -2044,8 +2079,12 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
   if (s != ASTRO_OK) return s;
   const CUtensorMap tkx[2] = {x.k, x.k};
   const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(q);
-  s = head_dim == 128 ? launch_bwd_dq<128>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st)
-                      : launch_bwd_dq<64>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st);
+  if (splits > 1)
+    s = head_dim == 128 ? launch_dq_parts<128>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st)
+                        : launch_dq_parts<64>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st);
+  else
+    s = head_dim == 128 ? launch_bwd_dq<128>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st)
+                        : launch_bwd_dq<64>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st);
   if (s == ASTRO_OK && n_kc > 0)
     s = astro_chunk_attn_bwd_dkv(q, k_chunk, v_chunk, lse, delta, d_o, batch, heads, head_dim, n_q, n_kc, scale, dk_chunk, dv_chunk, stream);
   if (s != ASTRO_OK || keys > 1) return s;

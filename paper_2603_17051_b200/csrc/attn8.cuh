@@ -127,6 +127,24 @@ __global__ void __launch_bounds__(256) attn8_one_key_kernel(__nv_bfloat162* x, l
   x[i] = __floats2bfloat162_rn(fabsf(v.x) < INFINITY ? 0.f : v.x, fabsf(v.y) < INFINITY ? 0.f : v.y);
 }
 
+// dQ from its parts (DqParts), in their order: four elements a thread.
+template <int D>
+__global__ void __launch_bounds__(256) attn8_join_dq_kernel(const float* parts, int splits, long long rows, int n_q, int heads, float scale,
+                                                            __nv_bfloat16* dq) {
+  dependency_wait();
+  const long long at = blockIdx.x * 256ll + threadIdx.x, row = at / (D / 4);
+  if (row >= rows) return;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int p = 0; p < splits; ++p) {
+    const float4 v = reinterpret_cast<const float4*>(parts)[p * rows * (D / 4) + at];
+    sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+  }
+  const long long bh = row / n_q, b = bh / heads;
+  const long long to = ((b * n_q + (row - bh * n_q)) * heads + (bh - b * heads)) * D + at % (D / 4) * 4;
+  *reinterpret_cast<uint2*>(dq + to) = make_uint2(pack_bf16(sum.x * scale, sum.y * scale), pack_bf16(sum.z * scale, sum.w * scale));
+}
+
 // ---------------------------------------------------------------------------------- few queries
 constexpr int kFewStep = 32;                       // keys of a step: two tiles of 16, whose latencies overlap
 

@@ -86,14 +86,40 @@ template <int D> struct DqSmem {
   static constexpr int kTotal = kBars + 256 + 1024;
 };
 
-template <int D>
+// Few query tiles over many keys: the key tiles are divided among `splits` CTAs to a query tile, and each leaves its part of dQ.
+struct DqParts {
+  float* out;              // [split][B][H][n_q][D], without the factor `scale`
+  int q_tiles, splits;
+};
+// The piece of `all` of one split.
+__device__ __forceinline__ KeySegs dq_segs_of(const KeySegs& all, int split, int splits) {
+  const long long tiles = seg_tiles(all);
+  int skip = static_cast<int>(tiles * split / splits), left = static_cast<int>(tiles * (split + 1) / splits) - skip;
+  KeySegs mine;
+  mine.n = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    if (i >= all.n) break;
+    const int here = (all.count[i] + kTile - 1) / kTile, from = min(skip, here), n = min(left, here - from);
+    skip -= from;
+    left -= n;
+    if (n == 0) continue;
+    mine.start[mine.n] = all.start[i] + from * kTile;
+    mine.count[mine.n] = min(n * kTile, all.count[i] - from * kTile);
+    mine.from_chunk[mine.n] = all.from_chunk[i];
+    ++mine.n;
+  }
+  return mine;
+}
+
+template <int D, bool kParts>
 __global__ void __launch_bounds__(kDqThreads, 1)
 chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_constant__ CUtensorMap tm_do,
                          const __grid_constant__ CUtensorMap tm_kc, const __grid_constant__ CUtensorMap tm_vc,
                          const __grid_constant__ CUtensorMap tm_kx0, const __grid_constant__ CUtensorMap tm_kx1,
-                         const __grid_constant__ CUtensorMap tm_vx, const __grid_constant__ KeySegs segs, const int n_q,
+                         const __grid_constant__ CUtensorMap tm_vx, const __grid_constant__ KeySegs all_segs, const int n_q,
                          const int heads, const int cache_shared, const float scale, const float* __restrict__ lse,
-                         const float* __restrict__ delta, __nv_bfloat16* __restrict__ dq) {
+                         const float* __restrict__ delta, __nv_bfloat16* __restrict__ dq, const DqParts parts) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = align_1024(smem_raw);
   uint8_t* sdO = smem + DqSmem<D>::kdO;
@@ -113,9 +139,13 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // With one shared cache (frozen prefix of a sample group) the samples of a head are launched next to each
   // other, so the head's cached K/V is fetched from HBM once and served to the whole group out of L2.
-  const int q0 = blockIdx.x * kTile;
+  const int split = kParts ? blockIdx.x / parts.q_tiles : 0;
+  const int q0 = (blockIdx.x - split * (kParts ? parts.q_tiles : 0)) * kTile;
   const int h = cache_shared ? blockIdx.z : blockIdx.y, b = cache_shared ? blockIdx.y : blockIdx.z;
   const int bx = cache_shared ? 0 : b;
+  KeySegs mine;
+  if (kParts) mine = dq_segs_of(all_segs, split, parts.splits);
+  const KeySegs& segs = kParts ? mine : all_segs;
   constexpr uint32_t kTmemCols = 512;
   constexpr uint32_t kColS = 0, kColdP = 128, kColdS = 256, kColQ = 320, kColdQ = 384;
   constexpr int kMmaWarp = 4 * kDqGroups, kTmaWarp = 4 * kDqGroups + 1;
@@ -147,7 +177,7 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
       KeyTileIter it;
       auto load_kv = [&](int t, uint64_t* k_bar, uint64_t* v_bar) {   // K(t), V(t) of the tile the iterator is on
         const bool fc = it.from_chunk(segs);
-        const CUtensorMap* tk = fc ? &tm_kc : (it.seg == 0 ? &tm_kx0 : &tm_kx1);
+        const CUtensorMap* tk = fc ? &tm_kc : (it.seg == 0 ? &tm_kx0 : &tm_kx1);   // in parts the two are the same
         tma_load_tile<D>(sK + (t % kDqKStages) * TileGeom<D>::kBytes, tk, k_bar, it.row0(segs), h, fc ? b : bx);
         tma_load_tile<D>(sV + (t % kDqVStages) * TileGeom<D>::kBytes, fc ? &tm_vc : &tm_vx, v_bar, it.row0(segs), h,
                          fc ? b : bx);
@@ -313,9 +343,22 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
     // ---- epilogue: groups 0 and 1 write columns [g D/2, (g+1) D/2) of dQ
     mbar_wait(dq_full, 0, abort_flag);
     tc_fence_after_sync();
-    if (g < 2)
+    if (kParts) {
+      float4* out = reinterpret_cast<float4*>(parts.out + (static_cast<size_t>(split) * gridDim.y * gridDim.z * n_q + stat_idx) * D);
+#pragma unroll
+      for (int c = 0; c < D / 2; c += 32) {
+        uint32_t x[32];
+        tmem_ld32(tmem_lane + kColdQ + g * (D / 2) + c, x);
+        tmem_wait_ld();
+        if (!in_range) continue;
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          out[(g * (D / 2) + c + e) / 4] = make_float4(__uint_as_float(x[e]), __uint_as_float(x[e + 1]), __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
+      }
+    } else if (g < 2) {
       store_rows_from_tmem<D / 2>(tmem_lane + kColdQ + g * (D / 2), scale, quad_rows(dq, b, h, n_q, heads, D, row),
                                   g * (D / 2), tid & 31);
+    }
   }
 
   settle_after_abort(abort_flag);

@@ -277,3 +277,22 @@ def test_one_key_of_nan():
     bad[4, 1] = True
     assert dq[0, bad].isnan().all() and not dq[0, ~bad].any()
     assert dk[0, 0, 1].isnan().all() and not dk[0, 0, [0, 2, 3]].any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Bc,B,n_q,held,n_kc", [(2, 2, 5, 3000, 5), (1, 3, 130, 2100, 200), (1, 1, 1, 8001, 0), (1, 1, 129, 0, 2500), (1, 2, 7, 1000, 1200)])
+def test_backward_of_few_queries_over_many_keys(D, Bc, B, n_q, held, n_kc):
+    """Here the keys of a query tile are divided among CTAs, in the middle of the context, at its ragged end, in the chunk."""
+    torch, A = modules()
+    cache = A.astro_kvcache8_create(Bc, 2, D, 1, 100, 9000)
+    g = torch.Generator(device="cuda").manual_seed(held + D)
+    if held:
+        A.astro_kvcache8_append(cache, *(torch.randn(Bc, held, 2, D, generator=g, device="cuda").bfloat16() for _ in range(2)), held)
+    q, kc, vc, d_o = tensors(torch, B, n_q, n_kc, 2, D, n_q + D)
+    o, lse = compare(torch, A, cache, q, kc, vc, D ** -0.5, d_o)
+    first = A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, D ** -0.5)
+    again = A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, D ** -0.5)
+    assert all(x is y or torch.equal(x, y) for x, y in zip(first, again))
+    need = A.astro_chunk_attn8_bwd_workspace_bytes(cache, B, n_q, n_kc)
+    with pytest.raises(A.AstroError):
+        A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, D ** -0.5, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
