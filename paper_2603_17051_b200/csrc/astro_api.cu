@@ -882,7 +882,7 @@ FewSplit few_split(const astro_kvcache* cache, int batch, int heads, int n_q, in
 }
 
 // Whether the call goes to the kernel that reads the codes themselves, or has the rows turned into bf16 for the dense kernel.  The
-// first takes 0.2 us for a step of 32 keys and 16 queries (0.16 at head_dim 64) and CTA, the second 0.71 (0.64) for a tile of 128 keys in each
+// first takes 0.2 us for a step of 32 keys and 16 queries (0.14 at head_dim 64) and CTA, the second 0.71 (0.64) for a tile of 128 keys in each
 // round of 148 query tiles, and the rows' bytes.  (Both measured, us, 28080 keys, head_dim 128, 12 heads: 67 and 211 for 64 queries,
 // 124 and 211 for 128, 238 and 212 for 256; one head: 90 and 174 for 1024, 162 and 175 for 2048; 2000 keys, 12 heads: 41 and 29 for 256.)
 bool few_queries(const astro_kvcache* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
@@ -892,7 +892,7 @@ bool few_queries(const astro_kvcache* cache, int batch, int heads, int head_dim,
   const double keys = static_cast<double>(held_tokens(cache)) + n_kc;
   const FewSplit f = few_split(cache, batch, heads, n_q, n_kc);
   const double few_rounds = std::ceil(static_cast<double>(f.lists) * f.tiles * f.splits / 148.0);
-  const double few = 8.0 + few_rounds * (keys / kFewStep / f.splits + 20.0) * (wide ? 0.2 : 0.16) + (f.splits > 1 ? 4.0 : 0.0);
+  const double few = 8.0 + few_rounds * (keys / kFewStep / f.splits + 20.0) * (wide ? 0.2 : 0.14) + (f.splits > 1 ? 4.0 : 0.0);
   const double rounds = std::ceil(static_cast<double>((n_q - 1) / kTile + 1) * batch * heads / 148.0);
   const double rows = cache ? static_cast<double>(cache->d.cache_batch) * heads * held_tokens(cache) : 0.0;
   const double dense = 16.0 + rounds * std::ceil(keys / kTile) * (wide ? 0.71 : 0.64) + rows * head_dim * 6.0 / 6.0e6;

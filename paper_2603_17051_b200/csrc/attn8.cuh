@@ -148,13 +148,14 @@ __global__ void __launch_bounds__(256) attn8_join_dq_kernel(const float* parts, 
 // ---------------------------------------------------------------------------------- few queries
 constexpr int kFewStep = 32;                       // keys of a step: two tiles of 16, whose latencies overlap
 
-// 8 * NT queries per CTA; twice the queries take twice the registers and half the warps.
+// 8 * NT queries per CTA; at head_dim 128 twice the queries leave registers for fewer warps (at 64 twelve warps with four stages
+// each take 81 us for 128 queries of 12 heads over 28080 keys, eight with five 92).
 template <int D, int NT> struct FewShape {
-  static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = 32 * kWarps;
+  static constexpr int kWarps = NT == 1 || D == 64 ? 12 : 8, kThreads = 32 * kWarps;
   static constexpr int kPieces = D / 64;           // 16-byte pieces of a key's K per lane
   static constexpr int kVBytes = D / 8;            // bytes of a key's V per lane: 16 or 8
   static constexpr int kStageBytes = 2 * kFewStep * D;   // K, then V
-  static constexpr int kStages = (D == 128 ? 2 : 4) + (NT - 1);
+  static constexpr int kStages = D == 128 ? 1 + NT : 4;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kJoined = kWarps * 8 * NT * (D + 4) * 4;               // the warps' outputs and statistics, behind the loop
   static constexpr int kBars = kRing > kJoined ? kRing : kJoined;
