@@ -8,6 +8,9 @@
 // Storage: codes [B_c, H, slot * T + t, D], then, from the next multiple of 16 bytes on, e + 127 as a byte for every row.
 // Everything here is bandwidth work: a thread owns 8 neighbouring elements (16 bytes of bf16, 8 of codes) of one head and walks
 // kQuantTokens tokens, all of them in flight, so that a warp reads 512 contiguous bytes of the caller's tensor and writes whole rows.
+// 3 frames of 1560 tokens, 12 heads of 128, 4 samples, bf16: written in 35 us (174 MB, 4.9 TB/s: 2.9 instructions a clock, the row's
+// maximum and the conversions; 119 us when each element was tested for being finite on its own), read back in 27 (174 MB, 6.5 TB/s).
+// 18 frames of one sample read back in 41.5 us: 260 MB at 6.25 TB/s, 95 % of a plain copy.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -14,6 +14,9 @@
 //     shared memory where a tile straddles the end (0 * NaN would reach O).  Within a sequence an infinity or NaN in a value of a
 //     tile that only some rows see would reach the others the same way: like a row sum beyond 2^100, a result that is not finite sends
 //     the unit to a second pass on the ordinary cores, key by key, which is the formula and nothing else.  Slow and rare.
+// Bound: as the dense forward, by the tensor pipe, the exponentials and power together: a video's 32760 tokens (blocks of 4680, a
+// window of 18720, 4680 sinks, 12 heads of 128) in 2510 us, 1340 TFLOP/s of the pairs that are seen, tensor pipe 73 %.  16384 causal
+// tokens, 12 heads: 637 us at head_dim 128, 528 at 64 (exponentials).  Short calls are latency: 300 tokens in 8.9 us.
 // Precision: bf16 products, fp32 sums; P is rounded to bf16 for P V (half a step, 2^-8 of each weight at most), the row sum is
 // taken from the fp32 values.
 #pragma once
