@@ -282,7 +282,9 @@ size_t astro_chunk_attn8_fwd_workspace_bytes(const astro_kvcache_t* cache, int b
 astro_status_t astro_chunk_attn8_fwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk, int batch,
                                      int heads, int head_dim, int n_q, int n_kc, float scale, void* o, float* lse, void* workspace,
                                      size_t workspace_bytes, void* stream);
-/* astro_chunk_attn_bwd over a cache in 8 bits, the cached context detached: dQ over all keys, dK and dV of the chunk's own. */
+/* astro_chunk_attn_bwd over a cache in 8 bits, the cached context detached: dQ over all keys, dK and dV of the chunk's own.  Over one
+ * key in all dQ and dK are zeros.  workspace: as for the forward, astro_chunk_attn8_bwd_workspace_bytes().  All sums have one fixed
+ * order: the same call gives the same bits. */
 size_t astro_chunk_attn8_bwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc);
 astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk,
                                      const void* o, const float* lse, const void* d_o, int batch, int heads, int head_dim, int n_q,
@@ -376,8 +378,8 @@ astro_status_t astro_window_attn_fwd(const astro_window_desc_t* desc, const void
                                      const astro_strides_t* k_strides, const void* v, const astro_strides_t* v_strides,
                                      const int32_t* lengths, float scale, void* o, float* lse, void* stream);
 /* Its backward, nothing detached: dQ, and dK and dV of every token, summed over the heads that share it, from dO and the forward's
- * O and LSE (all contiguous, as are dq, dk and dv).  Queries and keys from a sequence's length on get zeros, and what o, lse and d_o hold there does not
- * matter.  Outputs must not overlap inputs.  workspace: device scratch, 16-byte aligned, at least astro_window_attn_bwd_workspace_bytes().  All sums have one
+ * O and LSE (all contiguous, as are dq, dk and dv).  Queries and keys from a sequence's length on get zeros, and what o, lse and d_o
+ * hold there does not matter.  A query that sees one key has dQ = 0.  Outputs must not overlap inputs.  workspace: device scratch, 16-byte aligned, at least astro_window_attn_bwd_workspace_bytes().  All sums have one
  * fixed order: the same call gives the same bits. */
 size_t astro_window_attn_bwd_workspace_bytes(int batch, int heads, int n_tokens, int head_dim);
 astro_status_t astro_window_attn_bwd(const astro_window_desc_t* desc, const void* q, const astro_strides_t* q_strides, const void* k,

@@ -951,12 +951,6 @@ def astro_chunk_attn8_bwd(cache, q, k_chunk, v_chunk, o, lse, d_o, scale: float,
     return dq, dk_chunk, dv_chunk
 
 
-def _packed_like(x):
-    """A contiguous tensor of x's shape and type; what keeps x's strides is quicker to make where those are the contiguous ones."""
-    import torch
-    return torch.empty_like(x) if x.is_contiguous() else torch.empty_like(x, memory_format=torch.contiguous_format)
-
-
 def _window_call(q, k, v, block_tokens, window_tokens, sink_tokens, lengths, dev):
     """(descriptor, [address and strides of q, k, v], address of lengths) of a call on whole sequences."""
     import torch
@@ -999,7 +993,7 @@ def astro_window_attn_fwd(q, k, v, scale: float, block_tokens: int = 1, window_t
     fresh = []
     with _owned_by(stream):
         if o is None:
-            o = _packed_like(q); fresh.append(o)
+            o = _dense_like(q); fresh.append(o)
         if lse is None:
             lse = q.new_empty((B, H, n), dtype=torch.float32); fresh.append(lse)
     _used_here(stream, *fresh)
@@ -1024,11 +1018,11 @@ def astro_window_attn_bwd(q, k, v, o, lse, d_o, scale: float, block_tokens: int 
     fresh = []
     with _owned_by(stream):
         if dq is None:
-            dq = _packed_like(q); fresh.append(dq)
+            dq = _dense_like(q); fresh.append(dq)
         if dk is None:
-            dk = _packed_like(k); fresh.append(dk)
+            dk = _dense_like(k); fresh.append(dk)
         if dv is None:
-            dv = _packed_like(v); fresh.append(dv)
+            dv = _dense_like(v); fresh.append(dv)
         if workspace is None:
             need = astro_window_attn_bwd_workspace_bytes(B, H, n, D)
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device); fresh.append(workspace)
