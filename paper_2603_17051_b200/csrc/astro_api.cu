@@ -345,11 +345,11 @@ astro_status_t launch_bwd_dq(const AttnArgs& a, const __nv_bfloat16* q, const CU
                              const KeySegs& segs, float scale, const float* lse, const float* delta, void* dq,
                              cudaStream_t st) {
   static std::atomic<int> done[kMaxDevices];
-  astro_status_t s = set_smem_once(chunk_attn_bwd_dq_kernel<D, false>, DqSmem<D>::kTotal, done);
+  astro_status_t s = set_smem_once(chunk_attn_bwd_dq_kernel<D, kDqWhole>, DqSmem<D>::kTotal, done);
   if (s != ASTRO_OK) return s;
   const int shared = (a.cache && a.cache->d.cache_batch == 1 && a.batch > 1) ? 1 : 0;
   dim3 grid_q((a.n_q + kTile - 1) / kTile, shared ? a.batch : a.heads, shared ? a.heads : a.batch);
-  chunk_attn_bwd_dq_kernel<D, false><<<grid_q, kDqThreads, DqSmem<D>::kTotal, st>>>(
+  chunk_attn_bwd_dq_kernel<D, kDqWhole><<<grid_q, kDqThreads, DqSmem<D>::kTotal, st>>>(
       q, tdo, tkc, tvc, tkx[0], tkx[1], tvx, segs, a.n_q, a.heads, shared, scale, lse, delta,
       static_cast<__nv_bfloat16*>(dq), DqParts{});
   return launch_status();
@@ -968,36 +968,42 @@ astro_status_t launch_few(const Attn8Call& c, float scale, void* o, float* lse, 
                           f.splits, rows, c.a.n_q, c.a.heads, f.o, lse);
 }
 
-// dQ of few query tiles over many keys: the CTAs that share the keys of each tile.  One CTA takes 1.15 us for a key tile (0.95 at
-// head_dim 64), and 10 us to start, end and have its part joined; so: as many as fill the SMs once, eight key tiles and more to each.
-// (The whole backward, us, undivided and divided: 28080 keys, 12 heads, head_dim 128, 5 queries 288 and 99, 700 queries 303 and 204; one
-// head, 8000 keys, head_dim 64: 77 and 32; one head, 2000 keys: 31 and 25; 1560 keys, 12 heads, 12 key tiles and so undivided: 31.)
+// dQ of few query tiles over many keys: the CTAs that share the keys of each tile, as many as fill the SMs once, three key tiles and
+// more to each.  (The whole backward, us, undivided and divided: 28080 keys, 12 heads, head_dim 128, 256 queries 290 and 120, 700
+// queries 303 and 204; one head, 8000 keys, head_dim 64, 64 queries: 77 and 31; 2000 keys, 12 heads, 128 queries: 34 and 27.  With eight
+// tiles and more to each CTA 1000 keys and 5 queries take 42, with three 31.)
 int dq_splits(const astro_kvcache* cache, int batch, int heads, int n_q, int n_kc) {
   constexpr int kSms = 148;
   const long long units = (static_cast<long long>(n_q) + kTile - 1) / kTile * heads * batch;
   const long long tiles = (static_cast<long long>(held_tokens(cache)) + kTile - 1) / kTile + (static_cast<long long>(n_kc) + kTile - 1) / kTile;
-  const long long splits = std::min(kSms / units, tiles / 8);
+  const long long splits = std::min(kSms / units, tiles / 3);
   return splits < 2 ? 1 : static_cast<int>(splits);
 }
 size_t dq_part_bytes(const astro_kvcache* cache, int batch, int heads, int head_dim, int n_q, int n_kc) {
   const int splits = dq_splits(cache, batch, heads, n_q, n_kc);
-  return splits == 1 ? 0 : static_cast<size_t>(splits) * batch * heads * n_q * head_dim * sizeof(float);
+  if (splits == 1) return 0;
+  const size_t bytes = static_cast<size_t>(splits) * batch * heads * n_q * (head_dim + 1) * sizeof(float);   // dQ's and delta's
+  return (bytes + 255) / 256 * 256;
 }
-template <int D>
+// dQ by way of parts, and delta, whose parts lie behind those of dQ (a single one is delta itself).
+template <int D, DqMode kMode>
 astro_status_t launch_dq_parts(const AttnArgs& a, const __nv_bfloat16* q, const CUtensorMap& tdo, const CUtensorMap& tkc, const CUtensorMap& tvc,
                                const CUtensorMap& tkx, const CUtensorMap& tvx, const KeySegs& segs, float scale, const float* lse,
-                               const float* delta, int splits, float* parts, void* dq, cudaStream_t st) {
+                               float* delta, int splits, float* parts, void* dq, cudaStream_t st) {
   static std::atomic<int> done[kMaxDevices];
-  astro_status_t s = set_smem_once(chunk_attn_bwd_dq_kernel<D, true>, DqSmem<D>::kTotal, done);
+  astro_status_t s = set_smem_once(chunk_attn_bwd_dq_kernel<D, kMode>, DqSmem<D>::kTotal, done);
   if (s != ASTRO_OK) return s;
-  const int shared = (a.cache && a.cache->d.cache_batch == 1 && a.batch > 1) ? 1 : 0, tiles = (a.n_q + kTile - 1) / kTile;
-  const dim3 grid(tiles * splits, shared ? a.batch : a.heads, shared ? a.heads : a.batch);
-  chunk_attn_bwd_dq_kernel<D, true><<<grid, kDqThreads, DqSmem<D>::kTotal, st>>>(q, tdo, tkc, tvc, tkx, tkx, tvx, segs, a.n_q, a.heads, shared,
-                                                                                 scale, lse, delta, nullptr, DqParts{parts, tiles, splits});
-  if ((s = launch_status()) != ASTRO_OK) return s;
-  const long long rows = static_cast<long long>(a.batch) * a.heads * a.n_q, threads = rows * (D / 4);
-  return launch_dependent(attn8_join_dq_kernel<D>, dim3(static_cast<unsigned>((threads + 255) / 256)), 256, 0, st, parts, splits, rows, a.n_q,
-                          a.heads, scale, static_cast<__nv_bfloat16*>(dq));
+  const long long rows = static_cast<long long>(a.batch) * a.heads * a.n_q;
+  float* delta_parts = splits > 1 ? parts + splits * rows * D : delta;
+  DqParts p{kMode == kDqDelta ? delta_parts : parts, (a.n_q + kTile - 1) / kTile, splits, nullptr, delta};
+  if (kMode == kDqPart && a.n_q <= kFewRows) p.delta_parts = delta_parts;
+  const int shared = (a.cache && a.cache->d.cache_batch == 1 && a.batch > 1) ? 1 : 0;
+  const dim3 grid(p.q_tiles * splits, shared ? a.batch : a.heads, shared ? a.heads : a.batch);
+  chunk_attn_bwd_dq_kernel<D, kMode><<<grid, kDqThreads, DqSmem<D>::kTotal, st>>>(q, tdo, tkc, tvc, tkx, tkx, tvx, segs, a.n_q, a.heads, shared,
+                                                                                  scale, lse, delta, nullptr, p);
+  if ((s = launch_status()) != ASTRO_OK || kMode == kDqDelta) return s;
+  return launch_dependent(attn8_join_dq_kernel<D>, dim3(static_cast<unsigned>((rows * (D / 4) + 255) / 256)), 256, 0, st, parts, splits, rows,
+                          a.n_q, a.heads, scale, static_cast<__nv_bfloat16*>(dq));
 }
 
 // Bytes of the held rows in bf16, K or V.
@@ -2053,6 +2059,7 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
   Expanded x;
   if ((s = expand_context(c, workspace, &x, st)) != ASTRO_OK) return s;
   const long long keys = static_cast<long long>(held_tokens(cache)) + n_kc;
+  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(q);
   if (keys <= kShortKeys) {
     ShortDelta8 f;
     f.q = static_cast<const __nv_bfloat16*>(q);
@@ -2073,15 +2080,17 @@ astro_status_t astro_chunk_attn8_bwd(const astro_kvcache_t* cache, const void* q
     if (head_dim == 128) attn8_short_delta_kernel<128><<<blocks, 128, 0, st>>>(f);
     else attn8_short_delta_kernel<64><<<blocks, 128, 0, st>>>(f);
     s = launch_status();
+  } else if (n_q <= kFewRows) {
+    s = head_dim == 128 ? launch_dq_parts<128, kDqDelta>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st)
+                        : launch_dq_parts<64, kDqDelta>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st);
   } else {
     s = head_dim == 128 ? launch_delta<128>(o, d_o, batch, heads, n_q, delta, st) : launch_delta<64>(o, d_o, batch, heads, n_q, delta, st);
   }
   if (s != ASTRO_OK) return s;
   const CUtensorMap tkx[2] = {x.k, x.k};
-  const __nv_bfloat16* qp = static_cast<const __nv_bfloat16*>(q);
   if (splits > 1)
-    s = head_dim == 128 ? launch_dq_parts<128>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st)
-                        : launch_dq_parts<64>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st);
+    s = head_dim == 128 ? launch_dq_parts<128, kDqPart>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st)
+                        : launch_dq_parts<64, kDqPart>(c.a, qp, tdo, tkc, tvc, x.k, x.v, x.segs, scale, lse, delta, splits, parts, dq, st);
   else
     s = head_dim == 128 ? launch_bwd_dq<128>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st)
                         : launch_bwd_dq<64>(c.a, qp, tdo, tkc, tvc, tkx, x.v, x.segs, scale, lse, delta, dq, st);

@@ -72,8 +72,11 @@ __global__ void __launch_bounds__(kExpandThreads) expand8_kernel(const Expand8 a
   }
 }
 
-// delta over few keys from the weights, sum_j p_ij dO_i . v_j, instead of dO_i . O_i with the rounded O (window_bwd.cuh has the
-// reason: win_short_delta_kernel).  kx, vx: the expanded rows.  A warp per (sample, head, query).
+// delta from the weights, sum_j p_ij dO_i . v_j, instead of dO_i . O_i with the rounded O, over few keys (here, a warp per (sample,
+// head, query) of the expanded rows kx, vx) and for few queries (kDqDelta): where one key has nearly all the weight of a row, dS is far
+// smaller than delta, and half a step of O's, 2^-8 of delta, is per cents of it (3 queries over 325 keys of uneven sizes: dQ 5.5e-3
+// off with the rounded O, 2.6e-3 from the weights).  Among many rows those with large gradients outweigh such a one.
+constexpr int kFewRows = 8;
 constexpr int kShortKeys = 64;
 struct ShortDelta8 {
   const __nv_bfloat16 *q, *d_o, *kx, *vx, *kc, *vc;

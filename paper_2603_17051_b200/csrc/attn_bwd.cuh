@@ -86,10 +86,16 @@ template <int D> struct DqSmem {
   static constexpr int kTotal = kBars + 256 + 1024;
 };
 
-// Few query tiles over many keys: the key tiles are divided among `splits` CTAs to a query tile, and each leaves its part of dQ.
+// Few query tiles over many keys: the key tiles are divided among `splits` CTAs to a query tile, and each leaves its part
+//   kDqPart     of dQ, without the factor `scale`: [split][B][H][n_q][D]
+//   kDqDelta    of delta, as the sum of P o dP over its keys: [split][B][H][n_q].  kDqPart adds them up again, and its first split leaves
+//               the sum for the kernels behind it.
+enum DqMode { kDqWhole, kDqPart, kDqDelta };
 struct DqParts {
-  float* out;              // [split][B][H][n_q][D], without the factor `scale`
+  float* out;
   int q_tiles, splits;
+  const float* delta_parts;   // kDqPart: null where `delta` is there already
+  float* delta_out;
 };
 // The piece of `all` of one split.
 __device__ __forceinline__ KeySegs dq_segs_of(const KeySegs& all, int split, int splits) {
@@ -112,7 +118,7 @@ __device__ __forceinline__ KeySegs dq_segs_of(const KeySegs& all, int split, int
   return mine;
 }
 
-template <int D, bool kParts>
+template <int D, DqMode kMode>
 __global__ void __launch_bounds__(kDqThreads, 1)
 chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_constant__ CUtensorMap tm_do,
                          const __grid_constant__ CUtensorMap tm_kc, const __grid_constant__ CUtensorMap tm_vc,
@@ -139,6 +145,7 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // With one shared cache (frozen prefix of a sample group) the samples of a head are launched next to each
   // other, so the head's cached K/V is fetched from HBM once and served to the whole group out of L2.
+  constexpr bool kParts = kMode != kDqWhole;
   const int split = kParts ? blockIdx.x / parts.q_tiles : 0;
   const int q0 = (blockIdx.x - split * (kParts ? parts.q_tiles : 0)) * kTile;
   const int h = cache_shared ? blockIdx.z : blockIdx.y, b = cache_shared ? blockIdx.y : blockIdx.z;
@@ -229,7 +236,8 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
         mbar_wait_spin(rb + j % 4, (j / 4) & 1, abort_flag);
         tc_fence_after_sync();
         if (more) issue_dp(j + 1);
-        mma_pb<D, kTile>(tmem_base + kColdQ, tmem_base + kColdS, smem_u32(sK + (j % kDqKStages) * TileGeom<D>::kBytes), j > 0);
+        if (kMode != kDqDelta)
+          mma_pb<D, kTile>(tmem_base + kColdQ, tmem_base + kColdS, smem_u32(sK + (j % kDqKStages) * TileGeom<D>::kBytes), j > 0);
         mma_commit(b_done + (j & 1));                 // commit j + 2
       }
       mma_commit(dq_full);
@@ -242,7 +250,15 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
     const bool in_range = row < n_q;
     const size_t stat_idx = (static_cast<size_t>(b) * heads + h) * n_q + (in_range ? row : 0);
     const float lse2 = in_range ? lse[stat_idx] * kLog2e : 0.f;
-    const float delta_r = in_range ? delta[stat_idx] : 0.f;
+    float delta_r = 0.f;
+    if (kMode == kDqPart && parts.delta_parts != nullptr) {
+      for (int i = 0; i < parts.splits; ++i) delta_r += parts.delta_parts[static_cast<size_t>(i) * gridDim.y * gridDim.z * n_q + stat_idx];
+      if (in_range && split == 0 && g == 0) parts.delta_out[stat_idx] = delta_r;
+      if (!in_range) delta_r = 0.f;
+    } else if (kMode != kDqDelta && in_range) {
+      delta_r = delta[stat_idx];
+    }
+    float delta_sum = 0.f;   // kDqDelta
     const float scale_log2 = scale * kLog2e;
     const uint64_t sc2 = f32x2(scale_log2, scale_log2), nl2 = f32x2(-lse2, -lse2), nd2 = f32x2(-delta_r, -delta_r);
     // Q row -> tensor memory: group g writes elements [64g, 64g+64) of its row as 32 packed columns
@@ -301,6 +317,19 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
 #pragma unroll
       for (int c2 = 0; c2 < NL; ++c2) tmem_ld32(tmem_lane + kColdP + g * kDqCols + c2 * 32, dp[c2]);
       tmem_wait_ld();
+      if (kMode == kDqDelta) {
+#pragma unroll
+        for (int c2 = 0; c2 < NL; ++c2)
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            float d0, d1;
+            f32x2_split(mul2(p2[c2][c >> 1], f32x2(__uint_as_float(dp[c2][c]), __uint_as_float(dp[c2][c + 1]))), d0, d1);
+            delta_sum += (c2 * 32 + c < valid ? d0 : 0.f) + (c2 * 32 + c + 1 < valid ? d1 : 0.f);
+          }
+        tc_fence_before_sync();
+        mbar_arrive(rb + j % 4);
+        return;
+      }
       if (valid >= kDqCols) {   // the usual tile: no key to mask, nothing but the algebra in the loop
 #pragma unroll
         for (int c2 = 0; c2 < NL; ++c2)
@@ -343,7 +372,13 @@ chunk_attn_bwd_dq_kernel(const __nv_bfloat16* __restrict__ q, const __grid_const
     // ---- epilogue: groups 0 and 1 write columns [g D/2, (g+1) D/2) of dQ
     mbar_wait(dq_full, 0, abort_flag);
     tc_fence_after_sync();
-    if (kParts) {
+    if (kMode == kDqDelta) {
+      static_assert(kDqGroups == 2, "two partial sums");
+      float* other = reinterpret_cast<float*>(sdO);   // every product has been made
+      if (g == 1) other[r] = delta_sum;
+      asm volatile("bar.sync 1, %0;" ::"n"(kDqSoftmaxThreads) : "memory");
+      if (g == 0 && in_range) parts.out[static_cast<size_t>(split) * gridDim.y * gridDim.z * n_q + stat_idx] = delta_sum + other[r];
+    } else if (kParts) {
       float4* out = reinterpret_cast<float4*>(parts.out + (static_cast<size_t>(split) * gridDim.y * gridDim.z * n_q + stat_idx) * D);
 #pragma unroll
       for (int c = 0; c < D / 2; c += 32) {

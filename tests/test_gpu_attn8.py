@@ -296,3 +296,41 @@ def test_backward_of_few_queries_over_many_keys(D, Bc, B, n_q, held, n_kc):
     need = A.astro_chunk_attn8_bwd_workspace_bytes(cache, B, n_q, n_kc)
     with pytest.raises(A.AstroError):
         A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, D ** -0.5, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Bc,n_q,held,n_kc", [(1, 3, 324, 1), (2, 8, 3000, 70), (1, 1, 65, 0), (2, 5, 0, 600), (1, 7, 129, 130)])
+def test_few_queries_of_which_one_key_has_nearly_all_the_weight(D, Bc, n_q, held, n_kc):
+    """delta of few queries comes from the weights: the errors of dQ and dK are relative to dS (its rounding, the output's: 2^-8 of
+    each term) beside fp32's, 2^-18 of a weight and its products, which counts the score's own size."""
+    torch, A = modules()
+    B, Hh, scale = 2, 3, 4.0 / D ** 0.5
+    q, kc, vc, d_o = tensors(torch, B, n_q, n_kc, Hh, D, 3 * D + n_q)
+    cache = A.astro_kvcache8_create(Bc, Hh, D, 1, 10, 4000)
+    g = torch.Generator(device="cuda").manual_seed(held + D)
+    if held:
+        ck, cv = (torch.randn(Bc, held, Hh, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+        ck[:, held // 2] = (ck[:, held // 2].float() + 4 * q[:Bc, 0].float() / D ** 0.5 * 2).bfloat16()
+        A.astro_kvcache8_append(cache, ck, cv, held)
+        k8, v8 = (x.double() for x in A.astro_kvcache8_read(cache, dtype=torch.float32))
+    else:
+        kc[:, 7] = (kc[:, 7].float() + 8 * q[:, 0].float() / D ** 0.5).bfloat16()
+        k8 = v8 = torch.zeros(Bc, 0, Hh, D, dtype=torch.float64, device="cuda")
+    o, lse = A.astro_chunk_attn8_fwd(cache, q, kc, vc, scale)
+    dq, dk, dv = A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, scale)
+    A.astro_last_device_status()
+    for b in range(B):
+        for h in range(Hh):
+            kk, vv = (torch.cat([x[b if Bc > 1 else 0, :, h]] + ([y[b, :, h].double()] if n_kc else [])) for x, y in ((k8, kc), (v8, vc)))
+            qq, gg = q[b, :, h].double(), d_o[b, :, h].double()
+            p = torch.softmax(scale * qq @ kk.T, 1)
+            dp = gg @ vv.T
+            ds = p * (dp - (p * dp).sum(1, keepdim=True))
+            size = scale * (qq.abs() @ kk.abs().T).amax(1, keepdim=True)
+            err = 2.0 ** -8 * ds.abs() + 2.0 ** -18 * (1 + size) * p * (gg.abs() @ vv.abs().T).amax(1, keepdim=True)
+            want = scale * ds @ kk
+            check(dq[b, :, h], (want, 1.1 * (scale * err @ kk.abs() + 2.0 ** -8 * want.abs()) + 1e-7), "dQ")
+            if n_kc:
+                err = err + 2.0 ** -13 * p * (dp - (p * dp).sum(1, keepdim=True)).abs()     # the polynomial exp2 of dK/dV: 7.6e-5
+                want, err = (scale * (ds.T @ qq))[held:], (scale * (err.T @ qq.abs()))[held:]
+                check(dk[b, :, h], (want, 1.1 * (err + 2.0 ** -8 * want.abs()) + 1e-7), "dK")
