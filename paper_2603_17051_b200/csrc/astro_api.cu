@@ -874,7 +874,7 @@ FewSplit few_split(const astro_kvcache* cache, int batch, int heads, int n_q, in
   const int warps = f.per_tile == 8 ? FewShape<128, 1>::kWarps : FewShape<128, 2>::kWarps;
   f.splits = 1;
   long long least = 0;
-  for (int i = 1; i <= 148 && (i == 1 || steps / i >= 2 * warps); ++i) {   // two steps for every warp
+  for (int i = 1; i <= 148 && (i == 1 || steps / i >= 2 * warps); ++i) {   // about two steps for every warp
     const long long cost = (units * i + kSms - 1) / kSms * ((steps + i - 1) / i + 20);
     if (i == 1 || cost < least) { f.splits = i; least = cost; }
   }

@@ -334,3 +334,29 @@ def test_few_queries_of_which_one_key_has_nearly_all_the_weight(D, Bc, n_q, held
                 err = err + 2.0 ** -13 * p * (dp - (p * dp).sum(1, keepdim=True)).abs()     # the polynomial exp2 of dK/dV: 7.6e-5
                 want, err = (scale * (ds.T @ qq))[held:], (scale * (err.T @ qq.abs()))[held:]
                 check(dk[b, :, h], (want, 1.1 * (err + 2.0 ** -8 * want.abs()) + 1e-7), "dK")
+
+
+@pytest.mark.parametrize("n_q", [3, 100])
+def test_a_captured_backward_of_few_queries(n_q):
+    """Captured, replayed twice on new inputs, beside eager calls with a workspace of their own."""
+    torch, A = modules()
+    B, H, D, held, n_kc = 2, 3, 64, 1900, 40
+    cache = A.astro_kvcache8_create(B, H, D, 1, 0, held)
+    g = torch.Generator(device="cuda").manual_seed(n_q)
+    A.astro_kvcache8_append(cache, *(torch.randn(B, held, H, D, generator=g, device="cuda").bfloat16() for _ in range(2)), held)
+    q, kc, vc, d_o = tensors(torch, B, n_q, n_kc, H, D, n_q)
+    o, lse = A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.2)
+    need = A.astro_chunk_attn8_bwd_workspace_bytes(cache, B, n_q, n_kc)
+    out = [torch.empty_like(q), torch.empty_like(kc), torch.empty_like(vc)]
+    given = dict(zip(("dq", "dk_chunk", "dv_chunk"), out), workspace=torch.empty(need, dtype=torch.uint8, device="cuda"))
+    A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, 0.2, **given)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, 0.2, **given)
+    for seed in (5, 6):
+        for x, new in zip((q, kc, vc, d_o), tensors(torch, B, n_q, n_kc, H, D, seed)):
+            x.copy_(new)
+        A.astro_chunk_attn8_fwd(cache, q, kc, vc, 0.2, o=o, lse=lse)
+        graph.replay()
+        eager = A.astro_chunk_attn8_bwd(cache, q, kc, vc, o, lse, d_o, 0.2)
+        assert all(torch.equal(x, y) for x, y in zip(out, eager))
