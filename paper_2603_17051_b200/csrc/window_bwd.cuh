@@ -500,6 +500,7 @@ template <int D> struct WinDkvSmem {
   static constexpr int kStats = kdO + kStages * TileGeom<D>::kBytes;      // float [stages][2][128]: -lse*log2e, -delta
   static constexpr int kBars = kStats + kStages * 2 * kTile * 4;
   static constexpr int kTotal = kBars + 256 + 1024;
+  static_assert((9 + 2 * kStages) * 8 + 8 <= 256, "barriers, tensor memory's address, abort flag");
 };
 
 template <int D>
@@ -515,8 +516,10 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
   uint8_t* sdO = smem + S::kdO;
   float* sStat = reinterpret_cast<float*>(smem + S::kStats);   // [stage][-LSE*log2e | -delta][128 queries]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBars);
-  uint64_t *kv_full = bars, *s_full = bars + 1 /* [2] */, *dp_full = bars + 3, *p_full = bars + 4, *ds_full = bars + 5, *acc_full = bars + 6,
-           *landed = bars + 7, *q_full = bars + 8, *q_empty = q_full + kStages;
+  // p_full like s_full, one for every S^T buffer: with two buffers the softmax warps can be done with P^T of the next tile before the
+  // issuer has looked for this one's, or before a slow warp has written its part of it.
+  uint64_t *kv_full = bars, *s_full = bars + 1 /* [2] */, *dp_full = bars + 3, *p_full = bars + 4 /* [2] */, *ds_full = bars + 6,
+           *acc_full = bars + 7, *landed = bars + 8, *q_full = bars + 9, *q_empty = q_full + kStages;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(q_empty + kStages);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
@@ -566,9 +569,9 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
     return;
   }
 
-  if (tid < 8 + 2 * kStages) {
+  if (tid < 9 + 2 * kStages) {
     // q_full: a stage's bytes and the constants of its queries; p_full, ds_full: one arrival per warp
-    mbar_init(bars + tid, tid >= 8 && tid < 8 + kStages ? 2 : tid == 4 || tid == 5 ? kMmaWarp : 1);
+    mbar_init(bars + tid, tid >= 9 && tid < 9 + kStages ? 2 : tid >= 4 && tid <= 6 ? kMmaWarp : 1);
     fence_mbar_init();
   }
   if (tid == 0) *abort_flag = 0;
@@ -650,7 +653,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
       }
       if (kSBufs > 1) issue_s();
       for (int i = 0; ok && i < n_tiles; ++i) {
-        if (!mbar_wait_spin(p_full, i & 1, abort_flag)) break;
+        if (!mbar_wait_spin(p_full + i % kSBufs, (i / kSBufs) & 1, abort_flag)) break;
         tc_fence_after_sync();
         win_mma_groups<D>(tmem_base + kColdV, tmem_base + kColSt + (i % kSBufs) * 128, do_tile(i), i > 0);
         issue_s();   // over P^T(i), behind the products that read it (MMAs run in order)
@@ -727,7 +730,7 @@ __device__ __forceinline__ void win_bwd_dkv(uint8_t* smem_raw, const CUtensorMap
       for (int c2 = 0; c2 < NL; ++c2) tmem_st16(col_s + c2 * 16, pt[c2]);
       tmem_wait_st();
       tc_fence_before_sync();
-      warp_arrive(p_full, lane);
+      warp_arrive(p_full + i % kSBufs, lane);
 
       if (!mbar_wait_ok(dp_full, i & 1, abort_flag)) break;
       tc_fence_after_sync();
