@@ -15,9 +15,12 @@
 //   The operands are fp16, which holds every e4m3 number: one instruction turns two codes.  A query is multiplied by the power
 //   of two that brings its largest element to 2^14 (elements below 2^-38 of it vanish, the others keep all of bf16's bits).
 //   2^ek multiplies the score; 2^ev joins the weight: w = exp2(s + ev - M) with M a running maximum of s + ev, rounded to fp16
-//   (half a step, 2^-11 of a weight; those below 2^-31 of the largest vanish), while the row sum has a reference m of its own
-//   and takes fp32 weights.  (In bf16, whose range needs no second reference, turning the codes took 8 instructions per pair of
-//   pairs and the whole 506 per step: 50 us for 4 x 12 lists of 18720 keys, against 36 of bytes.)
+//   (half a step, 2^-11 of a weight), while the row sum has a reference m of its own and takes fp32 weights.  A step with a weight
+//   below 2^-22 of 2^M, of which fp16 would leave less than eight bits or nothing, takes bf16 weights and codes instead (half a
+//   step, 2^-8): beside a far larger value row the others may still be all that an element is made of.  What is below 2^-120 of the
+//   largest vanishes.  (Call of 4 x 12 lists of 18720 keys, one query each: 44.5 us, 45.2 with scores so far apart that nearly every step is
+//   one in bf16; 40 rows over 8001 keys, head_dim 64: 22.7 and 24.7.  Bf16 without a second reference took 8 instructions per pair
+//   of pairs of codes and 506 per step: 50 us of kernel in the first case.)
 //   A warp streams its own tiles: one lane has 32 rows of K and of V brought by TMA into a ring that no other warp touches,
 //   swizzled so that no two lanes of a quarter warp meet in a bank.  (The same bytes by cp.async, 16 per lane, came at 4.8 TB/s
 //   whatever the warps did with them.)  References move (all lanes agreeing) when exceeded by more than 8.
@@ -219,6 +222,7 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 }
 
 constexpr float kFewSlack = 8.f, kFewBias = 6.f;   // weights reach 2^14 at most
+constexpr float kFewRange = 22.f;                  // in fp16 weights from 2^(kFewBias - 22) on are at most 2^-9 of themselves off
 
 // The running state of a warp: 8 * NT queries.  O is held in units of 2^(top - kFewBias).
 template <int D, int NT> struct FewState {
@@ -237,64 +241,91 @@ template <int D, int NT> struct FewState {
     }
   }
   // Scores of keys g (s[..][..][0..1]) and g + 8 (s[..][..][2..3]) of TILES tiles in log2 units, -infinity where there is no key,
-  // and the exponents of their values -> the weights as the operands of O^T = V^T P^T.
+  // and the exponents of their values -> the weights as the operands of O^T = V^T P^T, in bf16 where it returns true (kBf16: always).
   template <bool kBf16, int TILES>
-  __device__ __forceinline__ void weigh(const float (&s)[TILES][NT][4], const float (&e)[TILES][2], uint32_t (&b)[TILES][NT][2]) {
-    bool over = false;
+  __device__ __forceinline__ bool weigh(const float (&s)[TILES][NT][4], const float (&e)[TILES][2], uint32_t (&b)[TILES][NT][2]) {
+    bool over = false, small = false, wide = kBf16;
+    float least[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         float x = -INFINITY, y = -INFINITY;
+        least[n][c] = INFINITY;
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
           x = max3(x, s[i][n][c], s[i][n][c + 2]);
           y = max3(y, s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]);
+          least[n][c] = fminf(least[n][c], fminf(s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]));
         }
         over = over || x > m[n][c] + kFewSlack || y > top[n][c] + kFewSlack;
+        small = small || (!kBf16 && least[n][c] < top[n][c] - kFewRange);
       }
-    if (__any_sync(0xffffffffu, over)) {
+    if (__any_sync(0xffffffffu, over || small)) {   // rare, or there are places without a key
+      if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float x = m[n][c], y = top[n][c];
+          for (int c = 0; c < 2; ++c) {
+            float x = m[n][c], y = top[n][c];
 #pragma unroll
-          for (int i = 0; i < TILES; ++i) {
-            x = max3(x, s[i][n][c], s[i][n][c + 2]);
-            y = max3(y, s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]);
+            for (int i = 0; i < TILES; ++i) {
+              x = max3(x, s[i][n][c], s[i][n][c + 2]);
+              y = max3(y, s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]);
+            }
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) {
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+              y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
+            }
+            l[n][c] *= m[n][c] == -INFINITY ? 0.f : fast_exp2(m[n][c] - x);
+            const float alpha = top[n][c] == -INFINITY ? 0.f : fast_exp2(top[n][c] - y);
+            m[n][c] = x;
+            top[n][c] = y;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+              o[n][j][c] *= alpha;
+              o[n][j][c + 2] *= alpha;
+            }
           }
+      }
+      if constexpr (!kBf16) {
+        small = false;
 #pragma unroll
-          for (int d = 4; d < 32; d *= 2) {
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
-          }
-          l[n][c] *= m[n][c] == -INFINITY ? 0.f : fast_exp2(m[n][c] - x);
-          const float alpha = top[n][c] == -INFINITY ? 0.f : fast_exp2(top[n][c] - y);
-          m[n][c] = x;
-          top[n][c] = y;
+        for (int n = 0; n < NT; ++n) small = small || least[n][0] < top[n][0] - kFewRange || least[n][1] < top[n][1] - kFewRange;
+        if (__any_sync(0xffffffffu, small)) {
+          small = false;
 #pragma unroll
-          for (int j = 0; j < D / 16; ++j) {
-            o[n][j][c] *= alpha;
-            o[n][j][c + 2] *= alpha;
-          }
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) small = small || (s[i][n][x] != -INFINITY && s[i][n][x] + e[i][x / 2] < top[n][x % 2] - kFewRange);
+          wide = __any_sync(0xffffffffu, small);
         }
+      }
     }
+    auto weights = [&](auto is_wide) {
+      constexpr bool kWide = decltype(is_wide)::value;
 #pragma unroll
-    for (int i = 0; i < TILES; ++i)
+      for (int i = 0; i < TILES; ++i)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float w[4];
+        for (int n = 0; n < NT; ++n) {
+          float w[4];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const float ref = m[n][c] == -INFINITY ? 0.f : m[n][c], wref = (top[n][c] == -INFINITY ? 0.f : top[n][c]) - kFewBias;
-          l[n][c] += fast_exp2(s[i][n][c] - ref) + fast_exp2(s[i][n][c + 2] - ref);
-          w[c] = fast_exp2(s[i][n][c] + (e[i][0] - wref));
-          w[c + 2] = fast_exp2(s[i][n][c + 2] + (e[i][1] - wref));
+          for (int c = 0; c < 2; ++c) {
+            const float ref = m[n][c] == -INFINITY ? 0.f : m[n][c], wref = (top[n][c] == -INFINITY ? 0.f : top[n][c]) - kFewBias;
+            l[n][c] += fast_exp2(s[i][n][c] - ref) + fast_exp2(s[i][n][c + 2] - ref);
+            w[c] = fast_exp2(s[i][n][c] + (e[i][0] - wref));
+            w[c + 2] = fast_exp2(s[i][n][c + 2] + (e[i][1] - wref));
+          }
+          b[i][n][0] = transpose_8x8(kWide ? pack_bf16(w[0], w[1]) : pack_half(w[0], w[1]));
+          b[i][n][1] = transpose_8x8(kWide ? pack_bf16(w[2], w[3]) : pack_half(w[2], w[3]));
         }
-        b[i][n][0] = transpose_8x8(kBf16 ? pack_bf16(w[0], w[1]) : pack_half(w[0], w[1]));
-        b[i][n][1] = transpose_8x8(kBf16 ? pack_bf16(w[2], w[3]) : pack_half(w[2], w[3]));
-      }
+    };
+    if (kBf16 || wide) weights(std::true_type{});
+    else weights(std::false_type{});
+    return wide;
   }
 };
 
@@ -462,33 +493,45 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
             if (16 * tile + g + 8 * (e / 2) >= left) s[tile][n][e] = -INFINITY;
     }
     uint32_t p[2][NT][2];
-    st.template weigh<false, 2>(s, ve_log2, p);
-#pragma unroll
-    for (int tile = 0; tile < 2; ++tile) {
-      // V: words of keys 2t, 2t+1, 2t+8, 2t+9
-      uint32_t w[4][S::kVBytes / 4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 16 * tile + 2 * t + (i & 1) + 8 * (i >> 1);
-        if constexpr (D == 128) {
-          const uint4 x = *reinterpret_cast<const uint4*>(held + kFewStep * D + swizzled<D>(r, g));
-          w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(held + kFewStep * D + swizzled<D>(r, g >> 1) + 8 * (g & 1));
-          w[i][0] = x.x; w[i][1] = x.y;
+    const bool wide = st.template weigh<false, 2>(s, ve_log2, p);
+    auto add_values = [&](auto is_wide) {
+      constexpr bool kWide = decltype(is_wide)::value;
+      auto operand = [](uint32_t codes) {
+        if constexpr (!kWide) return e4m3_to_half2(codes);
+        else {
+          const float2 f = e4m3_to_floats(codes);
+          return pack_bf16(f.x, f.y);
         }
+      };
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) {
+        // V: words of keys 2t, 2t+1, 2t+8, 2t+9
+        uint32_t w[4][S::kVBytes / 4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 16 * tile + 2 * t + (i & 1) + 8 * (i >> 1);
+          if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(held + kFewStep * D + swizzled<D>(r, g));
+            w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(held + kFewStep * D + swizzled<D>(r, g >> 1) + 8 * (g & 1));
+            w[i][0] = x.x; w[i][1] = x.y;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < S::kVBytes / 4; ++i)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t sel = half ? 0x7362u : 0x5140u;   // codes of two elements, keys side by side
+            const uint32_t x = __byte_perm(w[0][i], w[1][i], sel), y = __byte_perm(w[2][i], w[3][i], sel);
+            const uint32_t a0 = operand(x), a1 = operand(x >> 16), a2 = operand(y), a3 = operand(y >> 16);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_16x8x16<kWide>(st.o[n][2 * i + half], a0, a1, a2, a3, p[tile][n][0], p[tile][n][1]);
+          }
       }
-#pragma unroll
-      for (int i = 0; i < S::kVBytes / 4; ++i)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t sel = half ? 0x7362u : 0x5140u;   // codes of two elements, keys side by side
-          const uint32_t x = __byte_perm(w[0][i], w[1][i], sel), y = __byte_perm(w[2][i], w[3][i], sel);
-          const uint32_t a0 = e4m3_to_half2(x), a1 = e4m3_to_half2(x >> 16), a2 = e4m3_to_half2(y), a3 = e4m3_to_half2(y >> 16);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) mma_16x8x16<false>(st.o[n][2 * i + half], a0, a1, a2, a3, p[tile][n][0], p[tile][n][1]);
-        }
-    }
+    };
+    if (wide) add_values(std::true_type{});
+    else add_values(std::false_type{});
     if (++stage == S::kStages) { stage = 0; ++round; }
   }
 
