@@ -221,7 +221,7 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-constexpr float kFewSlack = 8.f, kFewBias = 6.f;   // weights reach 2^14 at most
+constexpr float kFewSlack = 8.f, kFewBias = 6.f, kFewUnit = 1.f / 64.f;   // weights reach 2^14 at most; 2^-kFewBias
 constexpr float kFewRange = 22.f;                  // in fp16 weights from 2^(kFewBias - 22) on are at most 2^-9 of themselves off
 
 // The running state of a warp: 8 * NT queries.  O is held in units of 2^(top - kFewBias).
@@ -626,10 +626,11 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
     for (int w = 0; w < kFewWarps; ++w) {
       const float4 f = stats[w * 8 * NT + i];
       const float2 v = *reinterpret_cast<const float2*>(out + (w * 8 * NT + i) * D + d);
-      const float weight = fast_exp2(f.z - kFewBias - ref);   // 0 for a warp without keys, here and next
+      // by halves: 2^(f.z - ref) alone is no float where all values are of the smallest rows.  0 for a warp without keys, here and next
+      const float half = fast_exp2(0.5f * (f.z - ref));
       l = fmaf(fast_exp2(f.x - ref), f.y, l);
-      o0 = fmaf(weight, v.x, o0);
-      o1 = fmaf(weight, v.y, o1);
+      o0 = fmaf(half, v.x * kFewUnit * half, o0);
+      o1 = fmaf(half, v.y * kFewUnit * half, o1);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const float lse = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;

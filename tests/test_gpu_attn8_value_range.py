@@ -63,3 +63,22 @@ def test_rows_of_sizes_90_powers_of_two_apart(D, n_q, order):
     value, bound = want["o"]
     check(o[0, :, 0], (value, bound - 1e-7), "O")                 # small elements too are held to their own size
     check(lse[0, 0], want["lse"], "LSE")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q", [1, 12])
+@pytest.mark.parametrize("power", [-118, -100, 115])
+def test_values_that_are_all_tiny_or_all_huge(D, n_q, power):
+    torch, A = modules()
+    n = 700
+    g = torch.Generator(device="cuda").manual_seed(n_q)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    q, k, v = make(1, n_q, 1, D), make(1, n, 1, D), make(1, n, 1, D) * 2.0 ** power
+    cache = A.astro_kvcache8_create(1, 1, D, 1, 0, n)
+    A.astro_kvcache8_append(cache, k, v, n)
+    k8, v8 = (x.double() for x in A.astro_kvcache8_read(cache, dtype=torch.float32))
+    o, lse = A.astro_chunk_attn8_fwd(cache, q, None, None, D ** -0.5)
+    A.astro_last_device_status()
+    # in units of 2^power, where the bound's 1e-7 can be taken from it again (1e-7 + 1e-35 is 1e-7 in 64 bits); bf16 has steps of 2^-133
+    value, bound = head(q[0, :, 0].double(), k8[0, :, 0], v8[0, :, 0] * 2.0 ** -power, D ** -0.5)["o"]
+    check(o[0, :, 0].double() * 2.0 ** -power, (value, bound - 1e-7 + 2.0 ** (-133 - power)), "O")
