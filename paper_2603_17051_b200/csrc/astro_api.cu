@@ -1227,11 +1227,20 @@ astro_status_t launch_window_bwd(const WindowCall& c, const void* o, const float
   a.k_order.set(a.kv_lists, a.tiles - a.front);
   a.shares = w.shares;
   a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + astro_chunk_attn_bwd_workspace_bytes(d.batch, d.heads, d.n_tokens, D));
-  if (d.n_tokens <= kWinShort) {
-    win_short_delta_kernel<D><<<static_cast<unsigned>((static_cast<long long>(a.lists) * d.n_tokens + 3) / 4), 128, 0, st>>>(a, static_cast<float*>(workspace));
-    s = launch_status();
+  float* delta = static_cast<float*>(workspace);
+  auto few_delta = [&](bool after, int rows, int longest) {
+    const long long warps = static_cast<long long>(a.lists) * ((rows + 7) / 8), blocks = (warps + 3) / 4;
+    if (blocks > 0x7fffffffLL) return ASTRO_ERR_SHAPE;
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (after) return launch_dependent(win_few_delta_kernel<D>, grid, 128, 0, st, a, rows, longest, delta);
+    win_few_delta_kernel<D><<<grid, 128, 0, st>>>(a, rows, longest, delta);
+    return launch_status();
+  };
+  if (d.n_tokens <= kWinFewKeys || a.mask.window + a.mask.sink <= kWinFewKeys) {
+    s = few_delta(false, d.n_tokens, d.n_tokens);
   } else {
-    s = launch_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, static_cast<float*>(workspace), st);
+    s = launch_delta<D>(o, d_o, d.batch, d.heads, d.n_tokens, delta, st);
+    if (s == ASTRO_OK && c.lengths != nullptr) s = few_delta(true, kWinFewKeys, kWinFewKeys);
   }
   if (s != ASTRO_OK) return s;
   const long long ctas = static_cast<long long>(a.front) * a.kv_lists * a.shares + static_cast<long long>(a.lists) * a.tiles +

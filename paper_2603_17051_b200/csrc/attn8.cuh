@@ -197,19 +197,6 @@ template <int D> __device__ __forceinline__ int swizzled(int row, int chunk) {
   return row * D + ((chunk ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4);
 }
 
-// c[16 x 8] += a[16 x 16] b[16 x 8], bf16 or fp16 products, fp32 sums.
-template <bool kBf16>
-__device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                            uint32_t b1) {
-  if constexpr (kBf16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 // Transposes an 8 x 8 matrix of 16-bit elements, a row per quad of lanes, two neighbours per lane.
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   uint32_t r;

@@ -50,50 +50,90 @@ __device__ __forceinline__ bool win_store_row32(uint32_t taddr, float mult, bool
   return !live || fwd_all_finite(chk2);
 }
 
-// delta of short sequences from the weights, sum_j p_ij dO_i . v_j, instead of dO_i . O_i with the rounded O: a row of two or three keys
-// of which one has nearly all the weight has a dS far smaller than its delta, and half a step of O's (2^-8 of delta) is then per
-// cents of it.  Long sequences' gradients are made of other rows; in short ones such a row can be half of the result.
-// A warp per (sample, head, query); bandwidth and latency, a few microseconds.
-constexpr int kWinShort = 64;
+// delta of rows that see few keys from the weights, sum_j p_ij dO_i . v_j, instead of dO_i . O_i with the rounded O: where one of a few
+// keys has nearly all the weight, dS is far smaller than delta, and half a step of O's (2^-8 of delta) is then per cents of it.
+// Where rows see many keys, those with large gradients outweigh such a one; where all of them see few, because the window is narrow or the
+// sequence short, it can be all of the result.  So: every row where window and sinks are kWinFewKeys keys or fewer, and the samples
+// of that length or less of a batch whose rows see more.
+// A warp per 8 queries of one head of one sample, S^T = K Q^T and dP^T = V dO^T for 16 keys a step by mma.sync (the elements of a head
+// are summed in the order in which lanes load them).  L2: 16384 tokens, 12 heads of 128, a window of 64 in 100 us (of a
+// window of 8 in 48) beside 215 for the gradients, where dO . O takes 21; for 2 x 64 tokens of 12 heads the backward takes 14.3 us, 33.3
+// with a warp per query.
+constexpr int kWinFewKeys = 64;
 template <int D>
-__global__ void __launch_bounds__(128) win_short_delta_kernel(const WinBwdArgs a, float* delta) {
-  constexpr int kPer = D / 32;
+__global__ void __launch_bounds__(128) win_few_delta_kernel(const WinBwdArgs a, const int rows, const int longest, float* delta) {
+  constexpr int kPieces = D / 64;
   dependents_may_start();
-  const int at = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;   // rows are fewer than 2^31
-  if (at >= a.lists * a.mask.n) return;
-  const int list = at / a.mask.n, row = at - list * a.mask.n, b = list / a.heads, h = list - b * a.heads, len = a.mask.length(b);
-  float sum = 0.f;
-  if (row < len) {
-    const __nv_bfloat16* qp = a.q + b * a.qs.b + row * a.qs.t + h * a.qs.h + lane * kPer;
-    const __nv_bfloat16* gp = a.d_o + ((static_cast<size_t>(b) * a.mask.n + row) * a.heads + h) * D + lane * kPer;
-    float q[kPer], g[kPer];
+  const long long groups = (rows + 7) / 8, at = blockIdx.x * 4ll + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const long long list = at / groups;
+  const int i0 = static_cast<int>(at - list * groups) * 8;
+  const int b = static_cast<int>(list / a.heads), h = static_cast<int>(list - static_cast<long long>(b) * a.heads);
+  const int len = list < a.lists ? a.mask.length(b) : 0;
+  if (len > longest || i0 >= len) {
+    dependency_wait();   // what follows this launch waits for this one alone
+    return;
+  }
+  // a lane's pieces of a row: elements 8 (t + 4 (2 c + x)) .. at [c][x], 64 contiguous bytes per row and load
+  auto load_row = [&](const __nv_bfloat16* row, uint4 (&w)[kPieces][2]) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      q[e] = __bfloat162float(qp[e]);
-      g[e] = __bfloat162float(gp[e]);
-    }
-    int lo, hi;
-    a.mask.keys_of(row, len, lo, hi);
-    const float scale_log2 = a.scale * kLog2e, lse2 = a.lse[static_cast<size_t>(list) * a.mask.n + row] * kLog2e;
-    const __nv_bfloat16* kb = a.k + b * a.ks.b + (h / a.group) * a.ks.h + lane * kPer;
-    const __nv_bfloat16* vb = a.v + b * a.vs.b + (h / a.group) * a.vs.h + lane * kPer;
-    for (int j = 0; j < hi; ++j) {
-      if (j >= a.mask.sink && j < lo) continue;
-      float s = 0.f, dp = 0.f;
+    for (int c = 0; c < kPieces; ++c)
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        s = fmaf(q[e], __bfloat162float(kb[j * a.ks.t + e]), s);
-        dp = fmaf(g[e], __bfloat162float(vb[j * a.vs.t + e]), dp);
-      }
+      for (int x = 0; x < 2; ++x) w[c][x] = reinterpret_cast<const uint4*>(row)[t + 4 * (2 * c + x)];
+  };
+  uint4 q[kPieces][2], d_o[kPieces][2];
+  const int own = min(i0 + g, len - 1);   // the query of the operands
+  load_row(a.q + b * a.qs.b + own * a.qs.t + h * a.qs.h, q);
+  load_row(a.d_o + ((static_cast<size_t>(b) * a.mask.n + own) * a.heads + h) * D, d_o);
+  // the queries of the results: 2t, 2t + 1
+  int lo[2], hi[2], from, unused, end;
+  float lse2[2], sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, d);
-        dp += __shfl_xor_sync(0xffffffffu, dp, d);
-      }
-      sum = fmaf(fast_exp2(s * scale_log2 - lse2), dp, sum);
+  for (int c = 0; c < 2; ++c) {
+    const int i = min(i0 + 2 * t + c, len - 1);
+    a.mask.keys_of(i, len, lo[c], hi[c]);
+    lse2[c] = a.lse[(static_cast<size_t>(b) * a.heads + h) * a.mask.n + i] * kLog2e;
+  }
+  a.mask.keys_of(i0, len, from, unused);
+  a.mask.keys_of(min(i0 + 7, len - 1), len, unused, end);
+  const int sink = min(a.mask.sink, from), keys = sink + end - from;   // [0, sink) and [from, end)
+  const float scale_log2 = a.scale * kLog2e;
+  const __nv_bfloat16 *kb = a.k + b * a.ks.b + (h / a.group) * a.ks.h, *vb = a.v + b * a.vs.b + (h / a.group) * a.vs.h;
+  auto key = [&](int x) { return x < sink ? x : from + x - sink; };
+  for (int x0 = 0; x0 < keys; x0 += 16) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, dp[4] = {0.f, 0.f, 0.f, 0.f};
+    const long long j0 = key(min(x0 + g, keys - 1)), j1 = key(min(x0 + g + 8, keys - 1));
+    uint4 k0[kPieces][2], k1[kPieces][2], v0[kPieces][2], v1[kPieces][2];
+    auto products = [&](const uint4 (&x)[kPieces][2], const uint4 (&y)[kPieces][2], const uint4 (&with)[kPieces][2], float (&to)[4]) {
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mma_16x8x16<true>(to, x[c][i].x, y[c][i].x, x[c][i].y, y[c][i].y, with[c][i].x, with[c][i].y);
+          mma_16x8x16<true>(to, x[c][i].z, y[c][i].z, x[c][i].w, y[c][i].w, with[c][i].z, with[c][i].w);
+        }
+    };
+    load_row(kb + j0 * a.ks.t, k0);
+    load_row(kb + j1 * a.ks.t, k1);
+    load_row(vb + j0 * a.vs.t, v0);
+    load_row(vb + j1 * a.vs.t, v1);
+    products(k0, k1, q, s);
+    products(v0, v1, d_o, dp);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at_key = x0 + g + 8 * (e / 2), j = key(at_key), c = e % 2;
+      const bool sees = at_key < keys && j < hi[c] && (j < a.mask.sink || j >= lo[c]);
+      sum[c] += sees ? fast_exp2(s[e] * scale_log2 - lse2[c]) * dp[e] : 0.f;
     }
   }
-  if (lane == 0) delta[at] = sum;
+  dependency_wait();   // this launch may follow one that writes delta of every row
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int d = 4; d < 32; d *= 2) sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], d);
+    const int i = i0 + 2 * t + c;
+    if (g == 0 && i < len) delta[(static_cast<size_t>(b) * a.heads + h) * a.mask.n + i] = sum[c];
+  }
 }
 
 // ------------------------------------------------------------------------------------------ dQ
