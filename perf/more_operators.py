@@ -158,7 +158,8 @@ def _frames_of(x, case, first, count):
 
 
 def _filled(case, batch, k, v):
-    """A cache that holds the frames of k and v; its window starts at the second slot of its ring where it can."""
+    """A cache that holds the frames of k and v; its window starts at the second slot of its ring where it has one, so a full
+    ring wraps.  (A window that becomes empty starts at the first slot again.)"""
     from paper_2603_17051_b200 import binding as A
     sink, held = min(case["sink"], case["held"]), case["held"]
     cache = A.astro_kvcache8_create(batch, case["heads"], case["head_dim"], case["tokens_per_frame"], case["sink"], case["window"])
@@ -168,11 +169,15 @@ def _filled(case, batch, k, v):
             A.astro_kvcache8_append(cache, _frames_of(k, case, first, count), _frames_of(v, case, first, count), count)
 
     put(0, sink)
-    if held > sink:
-        put(sink, 1)                                             # into the ring's first slot, and out again
+    if held > sink and case["window"] > 1:
+        beside = min(held - sink, case["window"] - 1)
+        put(sink, 1)                                             # into the ring's first slot, and out again behind the next ones
+        put(sink, beside)
         A.astro_kvcache_evict(cache, 1)
+        put(sink + beside, held - sink - beside)
         state = A.astro_kvcache_get_state(cache)
-        A.astro_kvcache_set_state(cache, A.KVCacheState(sink, 1 % case["window"], 0, state.frames_seen))
+        assert (state.sink_held, state.window_head, state.window_held) == (sink, 1, held - sink)
+    else:
         put(sink, held - sink)
     return cache
 
@@ -202,8 +207,11 @@ def prepare(case, seed):
         if own:
             from paper_2603_17051_b200 import binding as A
             s["cache"] = A.astro_kvcache8_create(B, H, D, case["tokens_per_frame"], case["sink"], case["window"])
-            A.astro_kvcache_set_state(s["cache"], A.KVCacheState(case["sink"], case["window"] // 2, 0, case["sink"]))
+            # a frame in the middle of the ring is held already, where the new ones leave room for it; they go behind it
+            s["beside"] = 1 if case["frames"] < case["window"] else 0
+            A.astro_kvcache_set_state(s["cache"], A.KVCacheState(case["sink"], case["window"] // 2, s["beside"], case["sink"] + s["beside"]))
             s["before"] = A.astro_kvcache_get_state(s["cache"])
+            assert s["before"].window_head == case["window"] // 2 * s["beside"]
         return s
     of = 1 if case.get("shared") else B
     k, v = _contents(case, normal, g, of, case["held"])
@@ -325,7 +333,7 @@ def run(state):
     if s["op"] == "store":
         A.astro_kvcache_set_state(s["cache"], s["before"])
         A.astro_kvcache8_append(s["cache"], s["k"], s["v"], s["frames"])
-        return A.astro_kvcache8_read(s["cache"], first_frame=s["sink"], n_frames=s["frames"], dtype=TYPES[s["out"]])
+        return A.astro_kvcache8_read(s["cache"], first_frame=s["sink"] + s["beside"], n_frames=s["frames"], dtype=TYPES[s["out"]])
     if s["op"] == "read":
         return A.astro_kvcache8_read(s["cache"], dtype=TYPES[s["out"]])
     if s["op"] == "attend":
