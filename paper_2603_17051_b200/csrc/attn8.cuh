@@ -31,6 +31,8 @@
 #include "attn_common.cuh"
 #include "kv_quant.cuh"
 
+#include <cfloat>
+
 namespace astro {
 
 // ---------------------------------------------------------------------------------- cached rows into bf16
@@ -156,7 +158,7 @@ __global__ void __launch_bounds__(256) attn8_join_dq_kernel(const float* parts, 
 constexpr int kFewStep = 32;                       // keys of a step: two tiles of 16, whose latencies overlap
 
 // 8 * NT queries per CTA; at head_dim 128 twice the queries leave registers for fewer warps (at 64 twelve warps with four stages
-// each take 81 us for 128 queries of 12 heads over 28080 keys, eight with five 92).
+// each take 85 us for 128 queries of 12 heads over 28080 keys; before the look at the weights' range 81, and eight with five 92).
 template <int D, int NT> struct FewShape {
   static constexpr int kWarps = NT == 1 || D == 64 ? 12 : 8, kThreads = 32 * kWarps;
   static constexpr int kPieces = D / 64;           // 16-byte pieces of a key's K per lane
@@ -219,7 +221,7 @@ template <int D, int NT> struct FewState {
   __device__ void clear() {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      m[n][0] = m[n][1] = top[n][0] = top[n][1] = -INFINITY;
+      m[n][0] = m[n][1] = top[n][0] = top[n][1] = -FLT_MAX;   // below every score; differences to it are no NaN
       l[n][0] = l[n][1] = 0.f;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
@@ -243,7 +245,7 @@ template <int D, int NT> struct FewState {
         for (int i = 0; i < TILES; ++i) {
           x = max3(x, s[i][n][c], s[i][n][c + 2]);
           y = max3(y, s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]);
-          least[n][c] = fminf(least[n][c], fminf(s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]));
+          least[n][c] = min3(least[n][c], s[i][n][c] + e[i][0], s[i][n][c + 2] + e[i][1]);
         }
         over = over || x > m[n][c] + kFewSlack || y > top[n][c] + kFewSlack;
         small = small || (!kBf16 && least[n][c] < top[n][c] - kFewRange);
@@ -265,8 +267,8 @@ template <int D, int NT> struct FewState {
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
               y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, d));
             }
-            l[n][c] *= m[n][c] == -INFINITY ? 0.f : fast_exp2(m[n][c] - x);
-            const float alpha = top[n][c] == -INFINITY ? 0.f : fast_exp2(top[n][c] - y);
+            l[n][c] *= fast_exp2(m[n][c] - x);
+            const float alpha = fast_exp2(top[n][c] - y);
             m[n][c] = x;
             top[n][c] = y;
 #pragma unroll
@@ -301,8 +303,8 @@ template <int D, int NT> struct FewState {
           float w[4];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const float ref = m[n][c] == -INFINITY ? 0.f : m[n][c], wref = (top[n][c] == -INFINITY ? 0.f : top[n][c]) - kFewBias;
-            l[n][c] += fast_exp2(s[i][n][c] - ref) + fast_exp2(s[i][n][c + 2] - ref);
+            const float wref = top[n][c] - kFewBias;
+            l[n][c] += fast_exp2(s[i][n][c] - m[n][c]) + fast_exp2(s[i][n][c + 2] - m[n][c]);
             w[c] = fast_exp2(s[i][n][c] + (e[i][0] - wref));
             w[c + 2] = fast_exp2(s[i][n][c + 2] + (e[i][1] - wref));
           }
@@ -604,10 +606,9 @@ __global__ void __launch_bounds__(FewShape<D, NT>::kThreads, 1) attn8_few_kernel
   for (int x = threadIdx.x; x < kVecs; x += kFewThreads) {
     const int i = x / (D / 2), d = x % (D / 2) * 2, row = row0 + i;
     if (row >= a.rows) continue;
-    float top = -INFINITY;
+    float ref = -FLT_MAX;
 #pragma unroll
-    for (int w = 0; w < kFewWarps; ++w) top = fmaxf(top, stats[w * 8 * NT + i].x);
-    const float ref = top == -INFINITY ? 0.f : top;
+    for (int w = 0; w < kFewWarps; ++w) ref = fmaxf(ref, stats[w * 8 * NT + i].x);
     float l = 0.f, o0 = 0.f, o1 = 0.f;
 #pragma unroll
     for (int w = 0; w < kFewWarps; ++w) {
