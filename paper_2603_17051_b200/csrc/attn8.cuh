@@ -49,7 +49,6 @@ constexpr int kExpandThreads = 256, kExpandRows = 8;
 template <int D>
 __global__ void __launch_bounds__(kExpandThreads) expand8_kernel(const Expand8 a) {
   constexpr int kLanes = D / 8, kPerPass = kExpandThreads / kLanes;
-  dependents_may_start();
   const int part = threadIdx.x % kLanes;
   const long long list = blockIdx.x / a.pieces;
   const int r0 = (blockIdx.x - static_cast<int>(list) * a.pieces) * (kPerPass * kExpandRows) + threadIdx.x / kLanes;
