@@ -278,7 +278,8 @@ astro_status_t astro_kvcache8_read(const astro_kvcache_t* cache, int first_frame
  * chunk's are bf16.  Same layouts, results and errors; cache may be null.  workspace: device scratch, 16-byte aligned, at least
  * astro_chunk_attn8_fwd_workspace_bytes() for the frames that the cache holds at the time of the call (it may be null where that is 0).  Many
  * queries: the held rows in bf16; few: the parts of lists that several CTAs share.  With few queries a cached key counts as zero in O where its
- * weight times the power of two of its value row is below 2^-120 of the query's largest such product. */
+ * weight times the power of two of its value row is below 2^-120 of the query's largest such product, and an element of q has fewer
+ * bits below 2^-31 of its row's largest and counts as zero below 2^-38 (for the cached keys). */
 size_t astro_chunk_attn8_fwd_workspace_bytes(const astro_kvcache_t* cache, int batch, int heads, int head_dim, int n_q, int n_kc);
 astro_status_t astro_chunk_attn8_fwd(const astro_kvcache_t* cache, const void* q, const void* k_chunk, const void* v_chunk, int batch,
                                      int heads, int head_dim, int n_q, int n_kc, float scale, void* o, float* lse, void* workspace,

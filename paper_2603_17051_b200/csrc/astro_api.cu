@@ -857,7 +857,8 @@ int held_tokens(const astro_kvcache* c) { return c ? (c->sink_held + c->win_held
 
 // How the kernel for few queries divides its work: the queries of a list (those of every sample over one prefix) into tiles of
 // 8 or 16, and the keys of a list among `splits` CTAs.  One CTA runs on an SM; with `units` lists and tiles, splits CTAs each
-// take ceil(units * splits / 148) rounds of a share of the steps, a CTA's start and end being worth about 20 steps of 32 keys.
+// take ceil(units * splits / 148) rounds of a share of the steps, a CTA's start and end being worth about 20 steps of 32 keys.  (A chunk's
+// keys are counted once; over one prefix a tile walks those of each of its samples.)
 struct FewSplit {
   int rows, per_tile, tiles, splits;
   long long lists;
@@ -1157,7 +1158,7 @@ astro_status_t launch_window_fwd(const WindowCall& c, float scale, void* o, floa
 // Where the window hides the other key tiles from most queries, the sinks' are seen by all of them.  Where one of them alone would
 // take longer than an SM's share of all the work (its list of tiles against all lists over a B200's 148 SMs), it is divided
 // among CTAs, whose parts are joined; at most kWinPartSlots of them, the workspace's.  (12 heads over one of keys, 32760
-// tokens, a window of 1024, 4 sinks: 6200 us with a CTA to a key tile, 840 divided.  2 x 4097 tokens, 12 heads over 4: 198 and 204, not divided.)
+// tokens, a window of 1024, 4 sinks: 6200 us with a CTA to a key tile, 790 divided.  2 x 4097 tokens, 12 heads over 4: 198 and 204, not divided.)
 constexpr int kWinPartSlots = 296;
 struct WinShares {
   int front, shares;

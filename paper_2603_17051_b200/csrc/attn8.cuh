@@ -1,7 +1,7 @@
 // Attention over a cache held in 8 bits (kv_quant.cuh), the chunk's own keys in bf16:
 //   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - LSE_i),  k_j = 2^ek_j c_j for the cache's rows.
 //
-// Many queries: the cached rows are turned into bf16 (exactly: kv_quant.cuh) once per call, in the order of the frames, and the
+// Many queries: the cached rows are turned into bf16 (exactly: kv_quant.cuh) once per call, in the order of the storage, and the
 // dense kernels run over them.  Turning them inside the attention kernel would be done again by each of the 37 query tiles of a
 // chunk; once costs 3 bytes of traffic per element: 42 us (260 MB, 6.2 TB/s) beside the 635 of 4680 queries over 32760 keys, 12 heads.
 //
@@ -13,7 +13,8 @@
 //   for K (16 from 16 t at head_dim 64), and codes 16 g .. 16 g + 15 of keys 2t, 2t+1, 2t+8, 2t+9 for V; Q is brought into the same
 //   order, O leaves in it.  P^T changes from its place as a result into that of an operand by movmatrix.
 //   The operands are fp16, which holds every e4m3 number: one instruction turns two codes.  A query is multiplied by the power
-//   of two that brings its largest element to 2^14 (elements below 2^-38 of it vanish, the others keep all of bf16's bits).
+//   of two that brings its largest element to 2^14 (elements keep all of bf16's bits down to 2^-31 of it, fewer down to 2^-38,
+//   and vanish below).
 //   2^ek multiplies the score; 2^ev joins the weight: w = exp2(s + ev - M) with M a running maximum of s + ev, rounded to fp16
 //   (half a step, 2^-11 of a weight), while the row sum has a reference m of its own and takes fp32 weights.  A step with a weight
 //   below 2^-22 of 2^M, of which fp16 would leave less than eight bits or nothing, takes bf16 weights and codes instead (half a

@@ -1,7 +1,7 @@
 // The rolling cache in 8 bits.  A row x (the D elements of one head and token) is held as one exponent e and D codes:
 //   e = the smallest whole number with max |x_d| <= 448 * 2^e over the row's finite elements, at least -124;
 //   code_d = e4m3(x_d * 2^-e), rounded to nearest even; an infinity or NaN becomes e4m3's NaN and touches no other element.
-//   (Of rows that reach 2^127 e is 120, and elements that would round to 256 * 2^120, beyond every finite float, are held as 240.)
+//   (Of rows beyond 1.75 * 2^127 e is 120, and elements that would round to 256 * 2^120, beyond every finite float, are held as 240.)
 // The factor is a power of two, so that what a code stands for, code * 2^e, has 4 significant bits and a step of 2^-133 or
 // more: it is a bf16 number exactly, and attention over it needs no rounding beyond the one that the write made (half a step
 // of e4m3, 2^-4 of the element, or 2^(e-10) where that is larger).
